@@ -47,6 +47,7 @@
 #ifndef DELTALOG_H
 #define DELTALOG_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -303,6 +304,90 @@ int deltalog_decode_step_host_static(const deltalog_desc *desc, const deltalog_s
                                      const void *host_q, const void *host_k, const void *host_v,
                                      const float *host_g, const float *host_beta, const float *u_bonus,
                                      const int32_t *slot_idx, int32_t B, void *host_out, void *stream);
+
+/*
+ * ---- Sequences -------------------------------------------------------------------------------------------
+ * The decode calls above advance a state by a token or a few.  The calls below take whole prompts or training documents:
+ * sequences of any length, packed one behind the other along the token axis, as
+ *     q, k [tokens, H_qk, d_k]   v, out [tokens, H, d_v]   g [tokens, H] or [tokens, H, d_k]   beta [tokens, H]
+ * with the operators, dtypes, head groups and gates of the decode calls.  Internally a sequence is cut into chunks of
+ * DELTALOG_SCAN_CHUNK tokens whose recurrence runs as matrix products.  Gates are expected to be <= 0 (-inf resets the
+ * state); a value that is not finite reaches, beside what the recurrence gives, other tokens of its own chunk.
+ */
+#define DELTALOG_SCAN_CHUNK 64
+
+/*
+ * The plan of a step, in device memory owned by the caller and written by deltalog_build_plan: where each request's
+ * tokens are, and through which call it goes.  A plan can be rebuilt for every step of a captured graph; its sizes n and
+ * max_tokens are upper bounds fixed on the host.
+ */
+typedef struct {
+    int32_t n;             /* rows (requests)                                                                    */
+    int32_t max_tokens;    /* tokens of all rows together at most; token tensors hold at least this many rows     */
+    int32_t *starts;       /* [n + 1] first token of each row; starts[n] = tokens                                 */
+    int32_t *chunk_starts; /* [n + 1] first chunk of each row; chunk_starts[n] = chunks                           */
+    int32_t *chunk_seq;    /* [max_tokens / DELTALOG_SCAN_CHUNK + n] row of each chunk, -1 behind the last        */
+    int32_t *token_seq;    /* [max_tokens] row of each token, -1 behind the last; or NULL                         */
+    int32_t *scan_slots;   /* [n] slot of the rows that go through deltalog_prefill, -1 for the others            */
+    int32_t *append_slots; /* [n] slot of the rows that go through deltalog_decode_step, -1 for the others; or NULL */
+    int32_t *merge_slots;  /* [n] the same for deltalog_decode_merge_step; or NULL                                */
+    int32_t *totals;       /* [4] tokens, chunks, rows in scan_slots' sense, rows that decode                     */
+} deltalog_plan;
+
+/*
+ * Build a plan from the number of tokens that each row brings to this step: lens [n] (device; <= 0: none), slots [n]
+ * (device, or NULL: row i is slot i).  With decode_rows != 0 a row with one token decodes: it is listed in append_slots,
+ * or, where log_len [num_slots, H] (device, or NULL: no log is full) says that its slot's log holds cap entries, in
+ * merge_slots; rows with more tokens are listed in scan_slots.  With decode_rows == 0 every row with tokens is listed in
+ * scan_slots.  The lists are row-aligned, as the calls want them.  A row whose tokens would end behind max_tokens is
+ * dropped and so is every later row with tokens: they get no tokens and no slot.  A negative slot stays as it is (a
+ * padding row: its tokens keep their place, every call skips them).  log_len NULL: H, cap and num_slots are not read.
+ */
+int deltalog_build_plan(const int32_t *lens, const int32_t *slots, const int32_t *log_len, int32_t H, int32_t cap, int32_t num_slots,
+                        int32_t decode_rows, const deltalog_plan *plan, void *stream);
+
+/* Bytes of workspace (device, 16-byte aligned) that the calls below want for a plan of these sizes: train == 0 for
+ * deltalog_prefill and deltalog_scan_forward without save, train != 0 for save and deltalog_scan_backward.  0: the
+ * descriptor or a size is invalid.  Calls that may overlap on the GPU need workspaces of their own. */
+size_t deltalog_scan_workspace_bytes(const deltalog_desc *desc, int32_t n, int32_t max_tokens, int32_t train);
+
+/*
+ * Prefill: every row of plan->scan_slots runs its tokens through its slot's state.  Entries pending in the slot's log are
+ * folded into the base first; a row with fresh[i] != 0 (fresh: [n] or NULL) starts from a zero state instead, whatever the
+ * slot holds.  On return S_base holds the state behind the row's last token and the slot's log is empty: the next
+ * token goes through deltalog_decode_step.  `out` rows of skipped rows, and slots that are not listed, are left as they were.
+ * status receives DELTALOG_STATUS_BAD_SLOT for slots outside the pool (skipped).
+ */
+int deltalog_prefill(const deltalog_desc *desc, const deltalog_state *state, const deltalog_plan *plan, const void *q, const void *k, const void *v,
+                     const float *g, const float *beta, const float *u_bonus, const int32_t *fresh, void *out, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * The same scan without a slot pool, for training: row i starts from S_init[i] ([n, H, d_k, d_v] fp32, or NULL: zeros)
+ * and leaves its state in S_final[i] (or NULL).  Slots and desc->num_slots, cap and base_dtype play no part.  With
+ * save != 0 the workspace (sized with train != 0) keeps the states in front of the chunks for deltalog_scan_backward.
+ */
+int deltalog_scan_forward(const deltalog_desc *desc, const deltalog_plan *plan, const float *S_init, const void *q, const void *k, const void *v,
+                          const float *g, const float *beta, const float *u_bonus, void *out, float *S_final, int32_t save, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Gradients, laid out and typed like what they belong to (u_bonus: RWKV6 only; g: operators with a gate; beta: delta
+ * rule). */
+typedef struct {
+    void *q, *k, *v;
+    float *g, *beta, *u_bonus;
+    float *S_init; /* or NULL */
+} deltalog_scan_grads;
+
+/*
+ * Gradients of deltalog_scan_forward from dout [tokens, H, d_v] and dS_final [n, H, d_k, d_v] fp32 (or NULL: zeros).
+ * With saved != 0 the workspace is the one that deltalog_scan_forward with save != 0 left for the same plan and inputs;
+ * otherwise its part is run again here.  `rows` is the number of rows of the token tensors (>= plan->max_tokens):
+ * gradient rows behind the last sequence are set to zero.  Sums run in a fixed order: the same call gives the same bits.
+ */
+int deltalog_scan_backward(const deltalog_desc *desc, const deltalog_plan *plan, const float *S_init, const void *q, const void *k, const void *v,
+                           const float *g, const float *beta, const float *u_bonus, const void *dout, const float *dS_final, int32_t saved,
+                           const deltalog_scan_grads *grads, int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Human-readable text for a host return code (static storage). */
 const char *deltalog_status_string(int code);

@@ -31,6 +31,7 @@ LIB_PATH = Path(__file__).resolve().parent / "libdeltalog.so"
 EXPORTS = (
     "deltalog_decode_step", "deltalog_decode_steps", "deltalog_decode_merge_step", "deltalog_merge", "deltalog_reset_slots", "deltalog_eager_step", "deltalog_decode_step_host",
     "deltalog_decode_step_host_static", "deltalog_decode_step_host_overlapped",
+    "deltalog_build_plan", "deltalog_scan_workspace_bytes", "deltalog_prefill", "deltalog_scan_forward", "deltalog_scan_backward",
     "deltalog_status_string", "deltalog_version", "deltalog_build_id", "deltalog_launch_count",
 )
 
@@ -58,6 +59,15 @@ class _Staging(ctypes.Structure):
 class _Lane(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("copy_in_stream", "compute_stream", "copy_out_stream", "in_done", "compute_done", "out_done")]
+
+
+class _Plan(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("max_tokens", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in (
+        "starts", "chunk_starts", "chunk_seq", "token_seq", "scan_slots", "append_slots", "merge_slots", "totals")]
+
+
+class _ScanGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "g", "beta", "u_bonus", "S_init")]
 
 
 _lib = None
@@ -93,6 +103,17 @@ def load_library() -> ctypes.CDLL:
         lib.deltalog_decode_step_host_overlapped.restype = ctypes.c_int
         lib.deltalog_decode_step_host_overlapped.argtypes = [ctypes.POINTER(_Desc), ctypes.POINTER(_State),
                                                              ctypes.POINTER(_Staging), ctypes.POINTER(_Lane)] + [vp] * 7 + [i32, vp]
+        dp, pp = ctypes.POINTER(_Desc), ctypes.POINTER(_Plan)
+        lib.deltalog_build_plan.restype = ctypes.c_int
+        lib.deltalog_build_plan.argtypes = [vp] * 3 + [i32] * 4 + [pp, vp]
+        lib.deltalog_scan_workspace_bytes.restype = ctypes.c_size_t
+        lib.deltalog_scan_workspace_bytes.argtypes = [dp, i32, i32, i32]
+        lib.deltalog_prefill.restype = ctypes.c_int
+        lib.deltalog_prefill.argtypes = [dp, ctypes.POINTER(_State), pp] + [vp] * 9 + [ctypes.c_size_t, vp]
+        lib.deltalog_scan_forward.restype = ctypes.c_int
+        lib.deltalog_scan_forward.argtypes = [dp, pp] + [vp] * 9 + [i32, vp, ctypes.c_size_t, vp]
+        lib.deltalog_scan_backward.restype = ctypes.c_int
+        lib.deltalog_scan_backward.argtypes = [dp, pp] + [vp] * 9 + [i32, ctypes.POINTER(_ScanGrads), i32, vp, ctypes.c_size_t, vp]
         lib.deltalog_status_string.restype = ctypes.c_char_p
         lib.deltalog_status_string.argtypes = [ctypes.c_int]
         lib.deltalog_version.restype = ctypes.c_int
@@ -173,6 +194,25 @@ class State:
         self.decay_log = torch.zeros(n, H, cap, desc.d_lambda, dtype=torch.float32, device=device)
         self.log_len = torch.zeros(n, H, dtype=torch.int32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    @classmethod
+    def wrap(cls, desc: Desc, S_base, K_log, U_log, decay_log, log_len, status=None) -> "State":
+        """A state over tensors that the caller holds already (nothing is copied)."""
+        n, H, cap = desc.num_slots, desc.H, desc.cap
+        io = {F32: torch.float32, BF16: torch.bfloat16}
+        wanted = (("S_base", S_base, (n, H, desc.d_k, desc.d_v), io[desc.base_dtype]),
+                  ("K_log", K_log, (n, H, cap, desc.d_k), io[desc.klog_dtype]),
+                  ("U_log", U_log, (n, H, cap, desc.d_v), io[desc.ulog_dtype]),
+                  ("decay_log", decay_log, (n, H, cap, desc.d_lambda), torch.float32),
+                  ("log_len", log_len, (n, H), torch.int32))
+        self = cls.__new__(cls)
+        self.desc = desc
+        for name, t, shape, dtype in wanted:
+            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != S_base.device:
+                raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on {S_base.device}")
+            setattr(self, name, t)
+        self.status = torch.zeros(1, dtype=torch.int32, device=S_base.device) if status is None else status
+        return self
 
     def c_struct(self) -> _State:
         ptrs = (self.S_base.data_ptr(), self.K_log.data_ptr(), self.U_log.data_ptr(),

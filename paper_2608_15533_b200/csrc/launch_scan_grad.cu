@@ -1,0 +1,49 @@
+// Launches of the scan's per-chunk gradients and of the sums behind them.
+#include "scan_grad_kernel.cuh"
+#include "scan_launch.cuh"
+
+namespace deltalog {
+namespace {
+
+template <int OP, int P, int DK, typename IO>
+int launch_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
+    auto kernel = scan_grad_kernel<OP, P, DK, IO>;
+    const size_t smem = GradSmem<OP, P, DK, IO>::bytes(a.dv);
+    if (int rc = ensure_smem(kernel, smem)) return rc;
+    kernel<<<dim3(a.max_chunks, a.H), 256, smem, s>>>(a);
+    if (int rc = finish_launch()) return rc;
+    const int sms = device_info().sms;
+    if (a.H != a.Hq) {
+        scan_group_sum_kernel<IO><<<sms * 8, 256, 0, s>>>(a, DK);
+        if (int rc = finish_launch()) return rc;
+    }
+    if (OP == DELTALOG_RWKV6) {
+        scan_bonus_sum_kernel<<<a.H, 256, 0, s>>>(a, DK, dbonus);
+        if (int rc = finish_launch()) return rc;
+    }
+    const int e = (int)sizeof(IO), gate = op_has_gate(d->op) ? 4 * a.H * (op_vec_decay(d->op) ? DK : 1) : 0;
+    scan_tail_kernel<<<sms, 256, 0, s>>>(a, rows, a.Hq * DK * e, a.H * a.dv * e, gate, op_delta_rule(d->op) ? 4 * a.H : 0);
+    return finish_launch();
+}
+
+template <int OP>
+int launch_grad_op(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
+    if (d->io_dtype == DELTALOG_F32)
+        return d->d_k == 128 ? launch_grad<OP, 3, 128, float>(d, a, rows, dbonus, s) : launch_grad<OP, 3, 64, float>(d, a, rows, dbonus, s);
+    return d->d_k == 128 ? launch_grad<OP, 1, 128, __nv_bfloat16>(d, a, rows, dbonus, s)
+                         : launch_grad<OP, 1, 64, __nv_bfloat16>(d, a, rows, dbonus, s);
+}
+
+}  // namespace
+
+int launch_scan_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
+    switch (d->op) {
+        case DELTALOG_GDN: return launch_grad_op<DELTALOG_GDN>(d, a, rows, dbonus, s);
+        case DELTALOG_KDA: return launch_grad_op<DELTALOG_KDA>(d, a, rows, dbonus, s);
+        case DELTALOG_RWKV6: return launch_grad_op<DELTALOG_RWKV6>(d, a, rows, dbonus, s);
+        case DELTALOG_GLA: return launch_grad_op<DELTALOG_GLA>(d, a, rows, dbonus, s);
+        default: return launch_grad_op<DELTALOG_RETNET>(d, a, rows, dbonus, s);  // linear attention: null gate
+    }
+}
+
+}  // namespace deltalog

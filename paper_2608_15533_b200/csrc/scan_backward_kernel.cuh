@@ -1,0 +1,243 @@
+// The chain over a sequence's chunks from the last to the first: dS, and with it dU and dV.
+//
+//     dU = A^T dO + (k e^(G_end - G)) dS        dV = T^T dU   (or dV = dU)
+//     dS <- e^(G_end) dS + (scale q e^G)^T dO - (k e^G)^T dV
+//
+// The layout is the forward chain's: transposed, 16 columns of d_v per warp, dS^T [16 x d_k] in its accumulators.
+#pragma once
+
+#include "scan_common.cuh"
+
+namespace deltalog {
+
+template <bool VEC, int P, int DK, bool DELTA, typename IO>
+struct BackwardSmem {
+    static constexpr int kTile = kChunk * DK * 2;
+    static constexpr int kMat = kChunk * kChunk * 2;
+    static constexpr int kVecs = VEC ? kPlanes : P;  // planes of q and k
+    static constexpr int kDecay = VEC ? DK * 4 : 2 * kChunk * 4;
+    // Scalar decay: k (first and last product of a chunk; bf16: two places) and q.  Per channel: k e^(G_end - G), k e^G
+    // (delta rule), scale q e^G.
+    static constexpr bool kTwice = !VEC && P == 1;
+    static constexpr int kh = 0;
+    static constexpr int kt = (kTwice ? 2 : 1) * kVecs * kTile;
+    static constexpr int q = kt + (VEC && DELTA ? kVecs * kTile : 0);
+    static constexpr int A = q + kVecs * kTile;
+    static constexpr int T = A + kPlanes * kMat;
+    static constexpr int decay = T + (DELTA ? kPlanes * kMat : 0);  // twice
+    static constexpr int slices = decay + 2 * kDecay;               // bf16 io, per warp: dO, staging
+    static constexpr int per_warp = sizeof(IO) == 4 ? 0 : 2 * kChunk * 32;
+    static constexpr size_t bytes(int warps) { return slices + (size_t)warps * per_warp; }
+};
+
+template <bool VEC, int P, int DK, bool DELTA, typename IO>
+__global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a) {
+    using L = BackwardSmem<VEC, P, DK, DELTA, IO>;
+    constexpr int NT = DK / 8;
+    constexpr bool F32IO = sizeof(IO) == 4;
+    constexpr int OP1 = F32IO ? kPlanes : 1;             // planes of dO
+    constexpr int OP2 = VEC ? OP1 : kPlanes;             // and of dO times a scalar decay
+    extern __shared__ __align__(128) unsigned char smem[];
+    const uint32_t sm = smem_addr(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x;
+    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int v0 = (blockIdx.y * (nthreads >> 5) + warp) * 16;
+    const int t = lane & 3;
+    const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
+    const int chunk0 = a.chunk_starts[seq];
+    const size_t tile = (size_t)DK * a.dv, s_off = ((size_t)seq * a.H + h) * tile;
+    const size_t v_stride = (size_t)a.H * a.dv;
+    const uint32_t o_s = sm + L::slices + warp * L::per_warp, stage = o_s + kChunk * 32;
+
+    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl)
+            load_tile(dst + pl * L::kTile, src + pl * a.q_plane + ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, (size_t)a.Hq * DK, kChunk, DK,
+                      min(kChunk, len - c * kChunk), tid, nthreads);
+    };
+    auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, size_t unit) {
+        load_tile(dst, src + unit * kPlanes * kChunk * DK, DK, kPlanes * kChunk, DK, kPlanes * kChunk, tid, nthreads);
+    };
+    auto load_first = [&](int c) {  // k for dU, decay factors
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h;
+        if (VEC) load_decayed(sm + L::kh, a.kh, unit);
+        else if (L::kTwice) load_raw(sm + L::kh + (c & 1) * L::kTile, a.kp, c);
+        for (int i = tid; i < L::kDecay / 16; i += nthreads)
+            cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
+    };
+    auto load_matrices = [&](int c) {
+        const size_t at = ((size_t)(chunk0 + c) * a.H + h) * kPlanes * kChunk * kChunk;
+        load_tile(sm + L::A, a.A + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
+        if (DELTA) load_tile(sm + L::T, a.T + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
+    };
+    auto load_update = [&](int c) {  // q, k for dS, and dO
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h;
+        if (VEC) {
+            load_decayed(sm + L::q, a.qt, unit);
+            if (DELTA) load_decayed(sm + L::kt, a.kt, unit);
+        } else {
+            load_raw(sm + L::q, a.qp, c);
+            if (!L::kTwice) load_raw(sm + L::kh, a.kp, c);
+        }
+        if constexpr (!F32IO)
+            load_slice(o_s, static_cast<const IO *>(a.dout) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride,
+                       min(kChunk, len - c * kChunk), lane);
+    };
+    if (nchunks > 0) {
+        load_first(nchunks - 1), cp_async_commit();
+        load_matrices(nchunks - 1), cp_async_commit();
+        load_update(nchunks - 1), cp_async_commit();
+    }
+    float s[NT][4];
+    if (a.dS_final) {
+        load_state<NT>(s, a.dS_final, false, s_off, a.dv, v0, lane);
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+    }
+
+    for (int c = nchunks - 1; c >= 0; --c) {
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h;
+        const int valid = min(kChunk, len - c * kChunk);
+        const float *decay = reinterpret_cast<const float *>(smem + L::decay + (c & 1) * L::kDecay);
+        const uint32_t k_s = sm + L::kh + (L::kTwice ? (c & 1) * L::kTile : 0);
+        const IO *dout = static_cast<const IO *>(a.dout) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0;
+        cp_async_wait<VEC || L::kTwice ? 2 : 0>();
+        __syncthreads();
+        keep_state<NT>(a.dS + unit * tile, s, v0, lane);
+        // dU^T = dS^T (k e^(G_end - G))^T
+        float du[8][4] = {};
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk) {
+            uint32_t f[kPlanes][4];
+            acc_to_a<kPlanes>(s[2 * kk], s[2 * kk + 1], f);
+#pragma unroll
+            for (int nn = 0; nn < 4; ++nn)
+#pragma unroll
+                for (int pl = 0; pl < L::kVecs; ++pl) {
+                    uint32_t b[4];
+                    load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
+                    mma_planes<kPlanes, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
+                }
+        }
+        if (!VEC) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const float2 d = *reinterpret_cast<const float2 *>(decay + kChunk + n * 8 + 2 * t);
+                du[n][0] *= d.x, du[n][1] *= d.y, du[n][2] *= d.x, du[n][3] *= d.y;
+            }
+        }
+        __syncthreads();
+        if (c > 0) load_first(c - 1);
+        cp_async_commit();
+        cp_async_wait<1>();
+        __syncthreads();
+        // + dO^T A: token j takes tokens i >= j
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            float x[2][4];
+            read_slice(x, dout, v_stride, valid, o_s, kb, lane);
+            uint32_t f[OP1][4];
+            acc_to_a<OP1>(x[0], x[1], f);
+#pragma unroll
+            for (int nn = 0; nn <= kb; ++nn)
+#pragma unroll
+                for (int pl = 0; pl < kPlanes; ++pl) {
+                    uint32_t b[4];
+                    load_b_t(b, sm + L::A + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
+                    mma_planes<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
+                }
+        }
+        // dV^T = dU^T T
+        if (DELTA) {
+            float w[8][4] = {};
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                uint32_t f[kPlanes][4], b[4];
+                acc_to_a<kPlanes>(du[2 * kb], du[2 * kb + 1], f);
+#pragma unroll
+                for (int nn = 0; nn <= kb; ++nn)
+#pragma unroll
+                    for (int pl = 0; pl < kPlanes; ++pl) {
+                        load_b_t(b, sm + L::T + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
+                        mma_planes<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], f, b, pl);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) du[n][e] = w[n][e];
+            store_slice(a.dV + unit * kChunk * a.dv + v0, a.dv, kChunk, du, 0u, lane);
+        }
+        store_slice(static_cast<IO *>(a.dv_out) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride, valid, du, stage, lane);
+        __syncthreads();
+        if (c > 0) load_matrices(c - 1);
+        cp_async_commit();
+        // dS^T <- e^(G_end) dS^T + dO^T (scale q e^G) - dV^T (k e^G); scalar decay scales the tokens of dO and dV
+        if (VEC) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float2 d = *reinterpret_cast<const float2 *>(decay + 8 * n + 2 * t);
+                s[n][0] *= d.x, s[n][1] *= d.y, s[n][2] *= d.x, s[n][3] *= d.y;
+            }
+        } else {
+            const float d = decay[kChunk - 1];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= d;
+        }
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            float x[2][4];
+            read_slice(x, dout, v_stride, valid, o_s, kb, lane);
+            float2 d[2] = {};
+            if (!VEC) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    d[n] = *reinterpret_cast<const float2 *>(decay + kb * 16 + 8 * n + 2 * t);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][e] *= ((e & 1) ? d[n].y : d[n].x) * a.scale;
+                }
+            }
+            {
+                uint32_t f[OP2][4];
+                acc_to_a<OP2>(x[0], x[1], f);
+#pragma unroll
+                for (int nn = 0; nn < NT / 2; ++nn)
+#pragma unroll
+                    for (int pl = 0; pl < L::kVecs; ++pl) {
+                        uint32_t b[4];
+                        load_b_t(b, sm + L::q + pl * L::kTile, DK, kb * 16, nn * 16, lane);
+                        mma_planes<OP2, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                    }
+            }
+            if (DELTA) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[n][e] = -du[2 * kb + n][e] * (VEC ? 1.f : ((e & 1) ? d[n].y : d[n].x));
+                uint32_t f[kPlanes][4];
+                acc_to_a<kPlanes>(x[0], x[1], f);
+                const uint32_t kt_s = VEC ? sm + L::kt : k_s;
+#pragma unroll
+                for (int nn = 0; nn < NT / 2; ++nn)
+#pragma unroll
+                    for (int pl = 0; pl < L::kVecs; ++pl) {
+                        uint32_t b[4];
+                        load_b_t(b, kt_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
+                        mma_planes<kPlanes, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                    }
+            }
+        }
+        __syncthreads();
+        if (c > 0) load_update(c - 1);
+        cp_async_commit();
+    }
+    cp_async_wait_all();
+    if (a.dS_init) store_state<NT>(s, a.dS_init, false, s_off, a.dv, v0, lane);
+}
+
+}  // namespace deltalog

@@ -1,0 +1,284 @@
+// Shared pieces of the chunked scan: the arguments of its kernels, the warp-level matrix helpers and the
+// split of fp32 operands into bf16 planes.
+//
+// A sequence is cut into chunks of kChunk tokens.  With G the cumulative log-decay inside a chunk (inclusive;
+// a readout of RWKV6 sees the exclusive one) the token recurrence becomes, per chunk and head,
+//     A_ij = scale sum_c q_ic k_jc e^(G_ic - G_jc)  (j <= i)      T = (I + L)^-1 diag(beta)
+//     L_ij = beta_i sum_c k_ic k_jc e^(G_ic - G_jc) (j < i)       U = T (V - (k e^G) S_0)      (or U = V)
+//     O = scale (q e^G) S_0 + A U          S_1 = e^(G_end) S_0 + (k e^(G_end - G))^T U
+// A and T of every chunk come from one parallel kernel (scan_prep_kernel), the chain over S from a sequential
+// one (scan_forward_kernel).  The backward pass mirrors it: scan_backward_kernel carries dS from the last
+// chunk to the first, scan_grad_kernel forms the gradients of q, k, g and beta chunk by chunk in parallel.
+//
+// Precision: a bf16 value enters the tensor cores exactly.  An fp32 operand enters as three bf16 planes x = x0 + x1 + x2
+// (to 2^-26 of its size), and of a product of two such operands the six plane products with i + j <= 2 are summed in
+// fp32 accumulators, so a product is as good as one in fp32.  Two planes (three products) leave 2^-18 per operand: the
+// states and gate gradients then came out 3e-6 to 4e-5 off, against 5e-8 to 3e-7 of an fp32 computation.  Results that are
+// rounded to bf16 and feed nothing else take two planes: 2^-18 vanishes beside their own 2^-9.
+#pragma once
+
+#include "common.cuh"
+
+namespace deltalog {
+
+constexpr int kChunk = DELTALOG_SCAN_CHUNK;
+constexpr int kPlanes = 3;  // of an fp32 operand
+static_assert(kChunk == 64, "the kernels' tiles are written for 64 tokens");
+
+struct ScanArgs {
+    // the plan
+    const int32_t *starts, *chunk_starts, *chunk_seq;
+    const int32_t *slots;  // state index of each row; NULL: the row itself, every row takes part
+    int32_t n, max_chunks, num_slots;
+    int32_t *status;
+    // the problem
+    int32_t H, Hq, dv;
+    float scale;
+    const void *q, *k, *v;  // io dtype
+    const float *g, *beta, *bonus;
+    const void *dout;
+    // scalar decay: q and k as bf16 planes, `q_plane` elements apart (bf16 io: the tensors themselves, one plane)
+    const __nv_bfloat16 *qp, *kp;
+    size_t q_plane;
+    // workspace, unit = chunk * H + head
+    __nv_bfloat16 *A, *T;        // [unit][3][64][64]
+    float *decay;                // scalar decay: [unit][2][64] e^(G_i), e^(G_end - G_i); per channel: [unit][d_k] e^(G_end)
+    __nv_bfloat16 *qt, *kt, *kh; // per-channel decay: [unit][3][64][d_k]
+    float *U, *dV;               // [unit][64][d_v]
+    float *S, *dS;               // [unit][d_v][d_k], state in front of the chunk / gradient behind it (transposed)
+    // states
+    const void *S_in;            // [.., H, d_k, d_v]
+    void *S_out;
+    int32_t in_bf16, out_bf16;
+    const int32_t *fresh;        // rows that start from zero, or NULL
+    int32_t *log_len;            // [num_slots, H], emptied for the rows that ran, or NULL
+    int32_t keep;                // forward: write S and U for a backward pass
+    void *out;                   // [tokens, H, d_v], or NULL
+    // backward
+    const float *dS_final;
+    float *dS_init;
+    void *dq, *dk, *dv_out;
+    float *dq_part, *dk_part;    // [tokens, H, d_k] where several value heads share one query / key head
+    float *dg, *dbeta, *dbonus_part;
+};
+
+// Row and slot of a (sequence, head) unit; false when the unit has nothing to do.
+__device__ __forceinline__ bool scan_slot(const ScanArgs &a, int seq, int tid, int &slot) {
+    if (!a.slots) {
+        slot = seq;
+        return true;
+    }
+    return resolve_slot(a.slots, seq, a.num_slots, a.status, tid, slot);
+}
+
+// ---- bf16 planes -------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t pack_bf16(float lo_elem, float hi_elem) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo_elem, hi_elem);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// x, y -> their packed planes 0 .. N-1, each the bf16 rounding of what the planes in front of it leave.
+template <int N>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&w)[N]) {
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        w[p] = pack_bf16(x, y);
+        if (p + 1 < N) x -= bf16_lo(w[p]), y -= bf16_hi(w[p]);
+    }
+}
+
+// ---- warp-level products -----------------------------------------------------------------------------------
+// c += a b, m16n8k16.  Accumulator layout: c[0..1] row lane/4, columns 2(lane%4)+{0,1}; c[2..3] row lane/4 + 8.
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two neighbouring accumulator tiles (16 columns) as the A operand of the next product, in N planes.
+template <int N>
+__device__ __forceinline__ void acc_to_a(const float (&c0)[4], const float (&c1)[4], uint32_t (&f)[N][4]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float x = r < 2 ? c0[2 * r] : c1[2 * r - 4], y = r < 2 ? c0[2 * r + 1] : c1[2 * r - 3];
+        uint32_t w[N];
+        split_pair<N>(x, y, w);
+#pragma unroll
+        for (int p = 0; p < N; ++p) f[p][r] = w[p];
+    }
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void stsm4_t(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};\n" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+                 : "memory");
+}
+
+// c0, c1 += a b for a k16 x n16 operand b in plane `pb`: the planes of a whose product with it counts (index sum below
+// LIMIT).
+template <int PA, int LIMIT>
+__device__ __forceinline__ void mma_planes(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[4], int pb) {
+#pragma unroll
+    for (int pa = 0; pa < PA; ++pa)
+        if (pa + pb < LIMIT) mma(c0, a[pa], b[0], b[1]), mma(c1, a[pa], b[2], b[3]);
+}
+
+// ---- shared-memory tiles -----------------------------------------------------------------------------------
+// bf16 tiles, rows of `w` elements (64 or 128), the 16-byte units of a row permuted by the row's low three bits so
+// that eight rows at one unit fall into eight different bank groups.
+__device__ __forceinline__ uint32_t tile_addr(uint32_t base, int w, int row, int unit) {
+    return base + (uint32_t)(row * w * 2 + ((unit ^ (row & 7)) << 4));
+}
+// The same for the per-warp slices of 16 columns (32-byte rows).
+__device__ __forceinline__ uint32_t slice_addr(uint32_t base, int row, int unit) {
+    return base + (uint32_t)(row * 32 + ((unit ^ ((row >> 2) & 1)) << 4));
+}
+
+// Operand B (k16 x n16, two n8 tiles: r[0..1], r[2..3]) of a tile stored [n][k] ...
+__device__ __forceinline__ void load_b(uint32_t (&r)[4], uint32_t base, int w, int n0, int k0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4(r, tile_addr(base, w, n0 + (m >> 1) * 8 + x, (k0 >> 3) + (m & 1)));
+}
+// ... and of a tile stored [k][n].
+__device__ __forceinline__ void load_b_t(uint32_t (&r)[4], uint32_t base, int w, int k0, int n0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4_t(r, tile_addr(base, w, k0 + (m & 1) * 8 + x, (n0 >> 3) + (m >> 1)));
+}
+// Operand A (m16 x k16) of a tile stored [m][k] ...
+__device__ __forceinline__ void load_a(uint32_t (&r)[4], uint32_t base, int w, int m0, int k0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4(r, tile_addr(base, w, m0 + (m & 1) * 8 + x, (k0 >> 3) + (m >> 1)));
+}
+// ... and of a tile stored [k][m].
+__device__ __forceinline__ void load_a_t(uint32_t (&r)[4], uint32_t base, int w, int k0, int m0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4_t(r, tile_addr(base, w, k0 + (m >> 1) * 8 + x, (m0 >> 3) + (m & 1)));
+}
+// Operand A of a 16-column slice stored [token k][16]; read as accumulator tiles it is the slice's transpose:
+// r[0] row lane/4 tokens k0..7, r[1] row lane/4 + 8, r[2], r[3] the same for tokens k0 + 8..15.
+__device__ __forceinline__ void load_slice_t(uint32_t (&r)[4], uint32_t base, int k0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4_t(r, slice_addr(base, k0 + (m >> 1) * 8 + x, m & 1));
+}
+
+// Asynchronous 16-byte copy that writes zeros when `ok` is false (the source is then not read).
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, bool ok) {
+    const int n = ok ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
+}
+// `rows` x w tile of rows `stride` elements apart; rows at and behind `valid` become zeros.
+__device__ __forceinline__ void load_tile(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int rows, int w, int valid, int tid, int nthreads) {
+    const int upr = w >> 3, sh = w == 128 ? 4 : 3;
+    for (int i = tid; i < rows * upr; i += nthreads) {
+        const int row = i >> sh, unit = i & (upr - 1);
+        const bool ok = row < valid;
+        cp_async16_zfill(tile_addr(dst, w, row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
+    }
+}
+// A warp's 64 x 16 slice of rows `stride` elements apart.
+__device__ __forceinline__ void load_slice(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int valid, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 16 + (lane >> 1), unit = lane & 1;
+        const bool ok = row < valid;
+        cp_async16_zfill(slice_addr(dst, row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
+    }
+}
+// Transposed accumulators x[8][4] (16 columns of d_v x 64 tokens) to a tensor of rows `stride` elements apart: bf16
+// through the warp's staging slice, fp32 directly (eight lanes write one 32-byte sector).
+__device__ __forceinline__ void store_slice(__nv_bfloat16 *dst, size_t stride, int valid, const float (&x)[8][4], uint32_t stage, int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int n = 0; n < 8; n += 2) {
+        const int m = lane >> 3, r = lane & 7;
+        stsm4_t(slice_addr(stage, n * 8 + (m >> 1) * 8 + r, m & 1), pack_bf16(x[n][0], x[n][1]), pack_bf16(x[n][2], x[n][3]),
+                pack_bf16(x[n + 1][0], x[n + 1][1]), pack_bf16(x[n + 1][2], x[n + 1][3]));
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 16 + (lane >> 1), unit = lane & 1;
+        if (row < valid) {
+            uint4 w;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];\n" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(slice_addr(stage, row, unit)) : "memory");
+            *reinterpret_cast<uint4 *>(dst + (size_t)row * stride + unit * 8) = w;
+        }
+    }
+}
+__device__ __forceinline__ void store_slice(float *dst, size_t stride, int valid, const float (&x)[8][4], uint32_t, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int tok = n * 8 + 2 * t + (e & 1);
+            if (tok < valid) dst[(size_t)tok * stride + g + (e >> 1) * 8] = x[n][e];
+        }
+}
+// Tokens 16 kb .. + 15 of the warp's 16 columns in the accumulator layout x[2][4]: from the warp's slice of a bf16
+// tensor, or straight from an fp32 one.
+__device__ __forceinline__ void read_slice(float (&x)[2][4], const __nv_bfloat16 *, size_t, int, uint32_t slice, int kb, int lane) {
+    uint32_t f[4];
+    load_slice_t(f, slice, kb * 16, lane);
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) x[n][2 * r] = bf16_lo(f[2 * n + r]), x[n][2 * r + 1] = bf16_hi(f[2 * n + r]);
+}
+__device__ __forceinline__ void read_slice(float (&x)[2][4], const float *src, size_t stride, int valid, uint32_t, int kb, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int tok = kb * 16 + n * 8 + 2 * t + (e & 1);
+            x[n][e] = tok < valid ? __ldg(src + (size_t)tok * stride + g + (e >> 1) * 8) : 0.f;
+        }
+}
+
+// A state tile of this warp: s[n][e] = S[c = 8n + 2t + (e & 1)][v0 + g + 8 (e >> 1)], rows of S d_v apart.
+template <int NT>
+__device__ __forceinline__ void load_state(float (&s)[NT][4], const void *src, bool is_bf16, size_t off, int dv, int v0, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const size_t i = off + (size_t)(8 * n + 2 * t + (e & 1)) * dv + v0 + g + 8 * (e >> 1);
+            s[n][e] = is_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(src)[i]) : static_cast<const float *>(src)[i];
+        }
+}
+template <int NT>
+__device__ __forceinline__ void store_state(const float (&s)[NT][4], void *dst, bool is_bf16, size_t off, int dv, int v0, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const size_t i = off + (size_t)(8 * n + 2 * t + (e & 1)) * dv + v0 + g + 8 * (e >> 1);
+            if (is_bf16) static_cast<__nv_bfloat16 *>(dst)[i] = __float2bfloat16_rn(s[n][e]);
+            else static_cast<float *>(dst)[i] = s[n][e];
+        }
+}
+// A state tile to the workspace, transposed [d_v][8 NT], fp32.
+template <int NT>
+__device__ __forceinline__ void keep_state(float *dst, const float (&s)[NT][4], int v0, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            *reinterpret_cast<float2 *>(dst + (size_t)(v0 + g + 8 * r) * (8 * NT) + 8 * n + 2 * t) = make_float2(s[n][2 * r], s[n][2 * r + 1]);
+}
+
+}  // namespace deltalog

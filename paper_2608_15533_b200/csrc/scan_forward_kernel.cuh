@@ -1,0 +1,246 @@
+// The chain over a sequence's chunks: S, U and the outputs.
+//
+// Everything is computed transposed.  A warp owns 16 columns of d_v and holds S^T [16 x d_k] in its accumulators for
+// the whole sequence: the accumulator layout of one product is the A operand layout of the next, so the chain
+//     S^T -> (k S)^T -> R^T -> U^T = R^T T^T -> O^T, S^T
+// never leaves the registers, and no two warps exchange anything.  Shared memory carries the operands common to a
+// CTA's warps (q, k, A, T), which are replaced as soon as their product is done while the next product runs.
+#pragma once
+
+#include "scan_common.cuh"
+
+namespace deltalog {
+
+template <bool VEC, int P, int DK, bool DELTA, typename IO>
+struct ForwardSmem {
+    static constexpr int kTile = kChunk * DK * 2;       // one plane of q or k
+    static constexpr int kMat = kChunk * kChunk * 2;    // one plane of A or T
+    static constexpr int kOut = sizeof(IO) == 4 ? kPlanes : 2;  // planes of what only the output sees
+    static constexpr int kQ = VEC ? kOut : P, kK = VEC ? kPlanes : P;
+    static constexpr int kDecay = VEC ? DK * 4 : 2 * kChunk * 4;
+    // Scalar decay: q and k, which the first and the last product of a chunk read; bf16 k has two places so that the next
+    // chunk's can be on its way in between.  Per channel: q e^G, k e^G (delta rule) and k e^(G_end - G).
+    static constexpr bool kTwice = !VEC && P == 1;
+    static constexpr int q = 0;
+    static constexpr int k = kQ * kTile;
+    static constexpr int kh = k + (VEC && DELTA ? kK * kTile : 0);
+    static constexpr int A = kh + (kTwice ? 2 : 1) * kK * kTile;
+    static constexpr int T = A + kOut * kMat;
+    static constexpr int decay = T + (DELTA ? kPlanes * kMat : 0);  // twice
+    static constexpr int slices = decay + 2 * kDecay;               // bf16 io, per warp: v, staging
+    static constexpr int per_warp = sizeof(IO) == 4 ? 0 : 2 * kChunk * 32;
+    static constexpr size_t bytes(int warps) { return slices + (size_t)warps * per_warp; }
+};
+
+template <bool VEC, int P, int DK, bool DELTA, typename IO>
+__global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) {
+    using L = ForwardSmem<VEC, P, DK, DELTA, IO>;
+    constexpr int NT = DK / 8;
+    constexpr bool F32IO = sizeof(IO) == 4;
+    constexpr int UP = DELTA || F32IO ? kPlanes : 1;  // planes of U (bf16 v is exact in one)
+    constexpr int UO = UP < L::kOut ? UP : L::kOut;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const uint32_t sm = smem_addr(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x;
+    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int v0 = (blockIdx.y * (nthreads >> 5) + warp) * 16;
+    const int t = lane & 3;
+    int slot;
+    if (!scan_slot(a, seq, tid, slot)) return;
+    const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
+    if (nchunks == 0 && a.slots) return;
+    const int chunk0 = a.chunk_starts[seq];
+    const size_t tile = (size_t)DK * a.dv, s_off = ((size_t)slot * a.H + h) * tile;
+    const size_t v_stride = (size_t)a.H * a.dv;
+    const uint32_t v_s = sm + L::slices + warp * L::per_warp, stage = v_s + kChunk * 32;
+
+    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {  // q or k of a chunk
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl)
+            load_tile(dst + pl * L::kTile, src + pl * a.q_plane + ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, (size_t)a.Hq * DK, kChunk, DK,
+                      min(kChunk, len - c * kChunk), tid, nthreads);
+    };
+    auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, int planes, size_t unit) {
+        load_tile(dst, src + unit * kPlanes * kChunk * DK, DK, planes * kChunk, DK, planes * kChunk, tid, nthreads);
+    };
+    auto load_vectors = [&](int c) {  // operands of the products with S, and the decay factors
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h;
+        if (VEC) {
+            load_decayed(sm + L::q, a.qt, L::kQ, unit);
+            if (DELTA) load_decayed(sm + L::k, a.kt, L::kK, unit);
+        } else {
+            load_raw(sm + L::q, a.qp, c);
+            if (L::kTwice) load_raw(sm + L::k + (c & 1) * L::kTile, a.kp, c);
+        }
+        for (int i = tid; i < L::kDecay / 16; i += nthreads)
+            cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
+    };
+    auto load_matrices = [&](int c) {
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h, at = unit * kPlanes * kChunk * kChunk;
+        load_tile(sm + L::A, a.A + at, kChunk, L::kOut * kChunk, kChunk, L::kOut * kChunk, tid, nthreads);
+        if (DELTA) load_tile(sm + L::T, a.T + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
+        if constexpr (!F32IO)
+            load_slice(v_s, static_cast<const IO *>(a.v) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride,
+                       min(kChunk, len - c * kChunk), lane);
+    };
+    auto load_update = [&](int c) {
+        if (VEC) load_decayed(sm + L::kh, a.kh, L::kK, (size_t)(chunk0 + c) * a.H + h);
+        else if (!L::kTwice) load_raw(sm + L::k, a.kp, c);
+    };
+    if (nchunks > 0) {
+        load_vectors(0), cp_async_commit();
+        load_matrices(0), cp_async_commit();
+        load_update(0), cp_async_commit();
+    }
+    float s[NT][4];
+    if (a.S_in && !(a.fresh && a.fresh[seq])) {
+        load_state<NT>(s, a.S_in, a.in_bf16, s_off, a.dv, v0, lane);
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+    }
+
+    for (int c = 0; c < nchunks; ++c) {
+        const size_t unit = (size_t)(chunk0 + c) * a.H + h;
+        const int valid = min(kChunk, len - c * kChunk);
+        const float *decay = reinterpret_cast<const float *>(smem + L::decay + (c & 1) * L::kDecay);
+        const uint32_t k_s = sm + L::k + (L::kTwice ? (c & 1) * L::kTile : 0);
+        cp_async_wait<VEC || L::kTwice ? 2 : 0>();
+        __syncthreads();
+        if (a.keep) keep_state<NT>(a.S + unit * tile, s, v0, lane);
+        // (k S)^T and (q S)^T
+        float ak[8][4] = {}, aq[8][4] = {};
+#pragma unroll
+        for (int kk = 0; kk < DK / 16; ++kk) {
+            uint32_t f[kPlanes][4];
+            acc_to_a<kPlanes>(s[2 * kk], s[2 * kk + 1], f);
+#pragma unroll
+            for (int nn = 0; nn < 4; ++nn) {
+                uint32_t b[4];
+                if (DELTA) {
+#pragma unroll
+                    for (int pl = 0; pl < L::kK; ++pl) {
+                        load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
+                        mma_planes<kPlanes, kPlanes>(ak[2 * nn], ak[2 * nn + 1], f, b, pl);
+                    }
+                }
+#pragma unroll
+                for (int pl = 0; pl < L::kQ; ++pl) {
+                    load_b(b, sm + L::q + pl * L::kTile, DK, nn * 16, kk * 16, lane);
+                    mma_planes<kPlanes, L::kOut>(aq[2 * nn], aq[2 * nn + 1], f, b, pl);
+                }
+            }
+        }
+        __syncthreads();
+        if (c + 1 < nchunks) load_vectors(c + 1);
+        cp_async_commit();
+        cp_async_wait<2>();
+        __syncthreads();
+        // R^T = V^T - (k e^G S)^T, in the registers of (k S)^T
+        float u[8][4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            float x[2][4];
+            read_slice(x, static_cast<const IO *>(a.v) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride, valid, v_s, kb, lane);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const int col = (2 * kb + n) * 8 + 2 * t;
+                const float d0 = VEC ? 1.f : decay[col], d1 = VEC ? 1.f : decay[col + 1];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (DELTA) ak[2 * kb + n][e] = fmaf(-((e & 1) ? d1 : d0), ak[2 * kb + n][e], x[n][e]);
+                    else u[2 * kb + n][e] = x[n][e];
+                    if (!VEC) aq[2 * kb + n][e] *= ((e & 1) ? d1 : d0) * a.scale;
+                }
+            }
+        }
+        // U^T = R^T T^T: token i takes tokens j <= i
+        if (DELTA) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[n][e] = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+                uint32_t f[kPlanes][4], b[4];
+                acc_to_a<kPlanes>(ak[2 * kb], ak[2 * kb + 1], f);
+#pragma unroll
+                for (int nn = kb; nn < 4; ++nn)
+#pragma unroll
+                    for (int pl = 0; pl < kPlanes; ++pl) {
+                        load_b(b, sm + L::T + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
+                        mma_planes<kPlanes, kPlanes>(u[2 * nn], u[2 * nn + 1], f, b, pl);
+                    }
+            }
+            if (a.keep) store_slice(a.U + unit * kChunk * a.dv + v0, a.dv, kChunk, u, 0u, lane);
+        }
+        // O^T += U^T A^T
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            uint32_t f[UO][4], b[4];
+            acc_to_a<UO>(u[2 * kb], u[2 * kb + 1], f);
+#pragma unroll
+            for (int nn = kb; nn < 4; ++nn)
+#pragma unroll
+                for (int pl = 0; pl < L::kOut; ++pl) {
+                    load_b(b, sm + L::A + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
+                    mma_planes<UO, L::kOut>(aq[2 * nn], aq[2 * nn + 1], f, b, pl);
+                }
+        }
+        if (a.out)
+            store_slice(static_cast<IO *>(a.out) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride, valid, aq, stage, lane);
+        __syncthreads();
+        if (c + 1 < nchunks) load_matrices(c + 1);
+        cp_async_commit();
+        if (VEC) {
+            cp_async_wait<2>();
+            __syncthreads();
+        }
+        // S^T <- e^(G_end) S^T + U^T (k e^(G_end - G)); scalar decay scales U's tokens instead of k's
+        if (VEC) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float2 d = *reinterpret_cast<const float2 *>(decay + 8 * n + 2 * t);
+                s[n][0] *= d.x, s[n][1] *= d.y, s[n][2] *= d.x, s[n][3] *= d.y;
+            }
+        } else {
+            const float d = decay[kChunk - 1];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] *= d;
+        }
+        const uint32_t ku_s = VEC ? sm + L::kh : k_s;
+        constexpr int US = VEC ? UP : kPlanes;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            if (!VEC) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const float2 d = *reinterpret_cast<const float2 *>(decay + kChunk + (2 * kb + n) * 8 + 2 * t);
+                    u[2 * kb + n][0] *= d.x, u[2 * kb + n][1] *= d.y, u[2 * kb + n][2] *= d.x, u[2 * kb + n][3] *= d.y;
+                }
+            }
+            uint32_t f[US][4];
+            acc_to_a<US>(u[2 * kb], u[2 * kb + 1], f);
+#pragma unroll
+            for (int nn = 0; nn < NT / 2; ++nn)
+#pragma unroll
+                for (int pl = 0; pl < L::kK; ++pl) {
+                    uint32_t b[4];
+                    load_b_t(b, ku_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
+                    mma_planes<US, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                }
+        }
+        if (!L::kTwice) __syncthreads();
+        if (c + 1 < nchunks) load_update(c + 1);
+        cp_async_commit();
+    }
+    cp_async_wait_all();
+    if (a.S_out) store_state<NT>(s, a.S_out, a.out_bf16, s_off, a.dv, v0, lane);
+    if (a.log_len && blockIdx.y == 0 && tid == 0) a.log_len[(size_t)slot * a.H + h] = 0;
+}
+
+}  // namespace deltalog

@@ -59,4 +59,15 @@ inline int validate_token(const deltalog_desc *d, const void *q, const void *k, 
     return DELTALOG_OK;
 }
 
+// Entries of a plan's chunk table that n rows of max_tokens tokens together can need.
+inline int32_t scan_max_chunks(int32_t n, int32_t max_tokens) { return max_tokens / DELTALOG_SCAN_CHUNK + n; }
+
+inline int validate_plan(const deltalog_plan *p) {
+    if (!p || p->n < 0 || p->max_tokens < 0) return DELTALOG_ERR_INVALID_ARG;
+    if ((long long)p->n + p->max_tokens > 0x7fffffffll - 64) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
+    if (!p->starts || !p->chunk_starts || !p->scan_slots) return DELTALOG_ERR_INVALID_ARG;
+    if (!p->chunk_seq) return DELTALOG_ERR_INVALID_ARG;
+    return DELTALOG_OK;
+}
+
 }  // namespace deltalog

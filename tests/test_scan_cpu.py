@@ -1,0 +1,170 @@
+"""Packed-sequence entry points without a GPU: every refusal comes back from the host before anything is launched, the
+workspace sizes follow their formula, and the Python layer names the argument it refuses."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2608_15533_b200 as dl
+from paper_2608_15533_b200 import binding, build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build_library()
+    return dl.load_library()
+
+
+def _desc(**kw):
+    return dl.Desc(**(dict(op=dl.GDN, num_slots=4, H=2, d_k=64, d_v=64, cap=8, io_dtype=dl.BF16) | kw))
+
+
+def _plan(**kw):
+    # fake, aligned, never dereferenced
+    names = ("starts", "chunk_starts", "chunk_seq", "token_seq", "scan_slots", "append_slots", "merge_slots", "totals")
+    vals = {"n": 3, "max_tokens": 100} | {x: 0x1000 * (i + 1) for i, x in enumerate(names)} | kw
+    return binding._Plan(**vals)
+
+
+def _state():
+    return binding._State(**{n: 0x100000 * (i + 1) for i, n in enumerate(("S_base", "K_log", "U_log", "decay_log", "log_len", "status"))})
+
+
+P = dict(q=0x10000, k=0x20000, v=0x30000, g=0x40000, beta=0x50000, bonus=None)
+BIG = 1 << 40
+
+
+def _prefill(lib, d, plan, state=None, out=0x60000, ws=0x70000, size=BIG, **kw):
+    a = P | kw
+    return lib.deltalog_prefill(ctypes.byref(d.c_struct()), ctypes.byref(_state() if state is None else state), ctypes.byref(plan), a["q"], a["k"],
+                                a["v"], a["g"], a["beta"], a["bonus"], None, out, ws, size, None)
+
+
+def _forward(lib, d, plan, out=0x60000, save=0, ws=0x70000, size=BIG, **kw):
+    a = P | kw
+    return lib.deltalog_scan_forward(ctypes.byref(d.c_struct()), ctypes.byref(plan), None, a["q"], a["k"], a["v"], a["g"], a["beta"], a["bonus"], out,
+                                     None, save, ws, size, None)
+
+
+def _backward(lib, d, plan, dout=0x80000, rows=100, ws=0x70000, size=BIG, grads=None, **kw):
+    a = P | kw
+    g = {"q": 0x90000, "k": 0xa0000, "v": 0xb0000, "g": 0xc0000, "beta": 0xd0000, "u_bonus": None, "S_init": None} | (grads or {})
+    return lib.deltalog_scan_backward(ctypes.byref(d.c_struct()), ctypes.byref(plan), None, a["q"], a["k"], a["v"], a["g"], a["beta"], a["bonus"],
+                                      dout, None, 0, ctypes.byref(binding._ScanGrads(**g)), rows, ws, size, None)
+
+
+def test_scan_refusals(lib):
+    before = dl.launch_count()
+    INV, SHAPE, CAP = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED_SHAPE, binding.ERR_CAP_RANGE
+    for call in (_prefill, _forward, _backward):
+        assert call(lib, _desc(op=9), _plan()) == INV
+        assert call(lib, _desc(d_k=96), _plan()) == SHAPE
+        assert call(lib, _desc(d_v=256), _plan()) == SHAPE
+        assert call(lib, _desc(cap=0), _plan()) == CAP
+        assert call(lib, _desc(H=3, H_qk=2), _plan()) == INV
+        assert call(lib, _desc(), _plan(n=-1)) == INV
+        assert call(lib, _desc(), _plan(max_tokens=-1)) == INV
+        assert call(lib, _desc(), _plan(max_tokens=2 ** 31 - 1)) == SHAPE
+        assert call(lib, _desc(H=2 ** 20), _plan()) == SHAPE
+        for name in ("starts", "chunk_starts", "chunk_seq", "scan_slots"):
+            assert call(lib, _desc(), _plan(**{name: None})) == INV
+        for name in ("q", "k", "v", "g", "beta"):
+            assert call(lib, _desc(), _plan(), **{name: None}) == INV
+        for name in ("q", "k", "v", "g"):
+            assert call(lib, _desc(), _plan(), **{name: 0x10008}) == INV      # misaligned
+        assert call(lib, _desc(op=dl.RWKV6), _plan()) == INV                  # no bonus
+        assert call(lib, _desc(), _plan(), ws=None) == INV
+        assert call(lib, _desc(), _plan(), ws=0x70004) == INV
+        need = lib.deltalog_scan_workspace_bytes(ctypes.byref(_desc().c_struct()), 3, 100, 1 if call is _backward else 0)
+        assert call(lib, _desc(), _plan(), size=need - 1) == INV
+        assert call(lib, _desc(), _plan(n=0)) == binding.OK                   # no rows: nothing to launch
+    need = lib.deltalog_scan_workspace_bytes(ctypes.byref(_desc().c_struct()), 3, 100, 0)
+    assert _forward(lib, _desc(), _plan(), save=1, size=need) == INV          # save wants the larger workspace
+    assert _prefill(lib, _desc(), _plan(), out=None) == INV and _forward(lib, _desc(), _plan(), out=0x60008) == INV
+    bad = _state()
+    bad.log_len = None
+    assert _prefill(lib, _desc(), _plan(), state=bad) == INV
+    assert _backward(lib, _desc(), _plan(), dout=None) == INV and _backward(lib, _desc(), _plan(), rows=99) == INV
+    for name in ("q", "k", "v", "g", "beta"):
+        assert _backward(lib, _desc(), _plan(), grads={name: None}) == INV
+    assert _backward(lib, _desc(op=dl.RWKV6), _plan(), bonus=0xe0000) == INV  # u_bonus' gradient is missing
+    assert dl.launch_count() == before
+
+
+def test_plan_refusals(lib):
+    def call(plan, lens=0x9000, log=None, H=2, cap=8, num=4):
+        return lib.deltalog_build_plan(lens, None, log, H, cap, num, 1, ctypes.byref(plan), None)
+
+    before = dl.launch_count()
+    assert lib.deltalog_build_plan(0x9000, None, None, 0, 0, 0, 0, None, None) == binding.ERR_INVALID_ARG
+    assert call(_plan(), lens=None) == binding.ERR_INVALID_ARG
+    assert call(_plan(n=-1)) == binding.ERR_INVALID_ARG
+    for name in ("starts", "chunk_starts", "chunk_seq", "scan_slots", "totals"):
+        assert call(_plan(**{name: None})) == binding.ERR_INVALID_ARG
+    assert call(_plan(token_seq=0x4004)) == binding.ERR_INVALID_ARG
+    assert call(_plan(), log=0xa000, H=0) == binding.ERR_INVALID_ARG
+    assert call(_plan(), log=0xa000, cap=0) == binding.ERR_CAP_RANGE and call(_plan(), log=0xa000, cap=65) == binding.ERR_CAP_RANGE
+    assert dl.launch_count() == before
+
+
+def test_workspace_sizes(lib):
+    def size(n, tokens, train, **kw):
+        return lib.deltalog_scan_workspace_bytes(ctypes.byref(_desc(**kw).c_struct()), n, tokens, train)
+
+    units = (640 // 64 + 3) * 2
+    assert size(3, 640, 0) == units * (2 * 3 * 64 * 64 * 2 + 2 * 64 * 4)
+    assert size(3, 640, 0, op=dl.RETNET) == units * (3 * 64 * 64 * 2 + 2 * 64 * 4)
+    assert size(3, 640, 1) == size(3, 640, 0) + units * (2 * 64 * 64 * 4 + 2 * 64 * 64 * 4)
+    assert size(3, 640, 1, H_qk=1) == size(3, 640, 1) + 2 * 640 * 2 * 64 * 4
+    assert size(-1, 640, 0) == 0 and size(3, -1, 0) == 0 and size(3, 640, 0, d_k=32) == 0
+    assert size(1000, 2 ** 30, 1) > 2 ** 40   # 64-bit arithmetic
+
+
+def test_python_layer_names_what_it_refuses():
+    plan = dl.Plan(2, 10, device="cpu")
+    d = _desc()
+    T, bf = 10, torch.bfloat16
+    good = dict(q=torch.zeros(T, 2, 64, dtype=bf), k=torch.zeros(T, 2, 64, dtype=bf), v=torch.zeros(T, 2, 64, dtype=bf), g=torch.zeros(T, 2),
+                beta=torch.zeros(T, 2))
+    lens = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="no path but the GPU"):
+        dl.build_plan(lens, plan)
+    with pytest.raises(ValueError, match="lens"):
+        dl.build_plan(lens.long(), plan)
+    with pytest.raises(ValueError, match="lens"):
+        dl.build_plan(lens[:1], plan)
+    with pytest.raises(ValueError, match="slots"):
+        dl.build_plan(lens, plan, slots=torch.zeros(4, dtype=torch.int32)[::2])
+    with pytest.raises(ValueError):
+        dl.Plan(-1, 10, device="cpu")
+    for name, bad in (("q", good["q"].float()), ("k", good["k"][:, :1]), ("v", good["v"].transpose(0, 1).contiguous().transpose(0, 1)),
+                      ("g", good["g"][:9]), ("beta", None), ("beta", good["beta"].to(bf))):
+        with pytest.raises(ValueError, match=name):
+            dl.scan_forward(d, plan, **(good | {name: bad}))
+        with pytest.raises(ValueError, match=name):
+            dl.scan_backward(d, plan, **(dict(u_bonus=None) | good | {name: bad}), dout=good["v"])
+    with pytest.raises(ValueError, match="reaches over"):
+        dl.scan_forward(d, dl.Plan(2, 11, device="cpu"), **good)
+    with pytest.raises(ValueError, match="no path but the GPU"):
+        dl.scan_forward(d, plan, **good)
+    with pytest.raises(ValueError, match="save"):
+        dl.scan_forward(d, plan, **good, save=True)
+    with pytest.raises(ValueError, match="saved"):
+        dl.scan_backward(d, plan, **good, u_bonus=None, dout=good["v"], saved=True)
+    with pytest.raises(ValueError, match="S_init"):
+        dl.scan_forward(d, plan, **good, S_init=torch.zeros(2, 2, 64, 64, dtype=bf))
+    with pytest.raises(ValueError, match="dout"):
+        dl.scan_backward(d, plan, **good, u_bonus=None, dout=good["v"].float())
+    with pytest.raises(ValueError, match="u_bonus"):
+        dl.scan_forward(_desc(op=dl.RWKV6), plan, **(good | dict(g=torch.zeros(T, 2, 64))))
+    with pytest.raises(ValueError):
+        dl.scan_workspace(_desc(d_k=32), 1, 10, device="cpu")
+    n, H, cap = 4, 2, 8
+    state = [torch.zeros(n, H, 64, 64), torch.zeros(n, H, cap, 64, dtype=bf), torch.zeros(n, H, cap, 64), torch.zeros(n, H, cap, 1),
+             torch.zeros(n, H, dtype=torch.int32)]
+    assert dl.State.wrap(d, *state).S_base is state[0]
+    for i, name in enumerate(("S_base", "K_log", "U_log", "decay_log", "log_len")):
+        bad = list(state)
+        bad[i] = bad[i][:3]
+        with pytest.raises(ValueError, match=name):
+            dl.State.wrap(d, *bad)
