@@ -8,9 +8,9 @@ namespace {
 template <int OP, int P, int DK, typename IO>
 int launch_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
     auto kernel = scan_grad_kernel<OP, P, DK, IO>;
-    const size_t smem = GradSmem<OP, P, DK, IO>::bytes(a.dv);
+    const size_t smem = GradSmem<OP, P, DK, IO>::bytes;
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<dim3(a.max_chunks, a.H), 256, smem, s>>>(a);
+    kernel<<<dim3(a.max_chunks, a.H), kGradThreads, smem, s>>>(a);
     if (int rc = finish_launch()) return rc;
     const int sms = device_info().sms;
     if (a.H != a.Hq) {

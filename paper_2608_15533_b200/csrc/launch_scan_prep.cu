@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(256) split_planes_kernel(const float *x, __nv_
 template <int P, int DK, bool DELTA>
 int launch_scalar(const ScanArgs &a, cudaStream_t s) {
     auto kernel = scan_prep_scalar_kernel<P, DK, DELTA>;
-    const size_t smem = prep_scalar_smem<P, DK>(DELTA);
+    const size_t smem = PrepScalarSmem<P, DK>::bytes(DELTA);
     if (int rc = ensure_smem(kernel, smem)) return rc;
     kernel<<<dim3(a.max_chunks, a.H), 128, smem, s>>>(a);
     return finish_launch();
@@ -25,7 +25,7 @@ int launch_scalar(const ScanArgs &a, cudaStream_t s) {
 template <int OP, int DK, typename IO>
 int launch_vector(const ScanArgs &a, cudaStream_t s) {
     auto kernel = scan_prep_vector_kernel<OP, DK, IO>;
-    const size_t smem = prep_vector_smem<DK>(OpTraits<OP>::kDeltaRule);
+    const size_t smem = PrepVectorSmem<DK>::bytes(OpTraits<OP>::kDeltaRule);
     if (int rc = ensure_smem(kernel, smem)) return rc;
     kernel<<<dim3(a.max_chunks, a.H), 256, smem, s>>>(a);
     return finish_launch();

@@ -71,6 +71,10 @@ __device__ __forceinline__ bool scan_slot(const ScanArgs &a, int seq, int tid, i
     return resolve_slot(a.slots, seq, a.num_slots, a.status, tid, slot);
 }
 
+// e^x for x <= 0 that weighs a term: the argument's rounding costs |x| 2^-24 of the weight, at most 2^-25 of the largest
+// weight.  (Factors above one take expf.)
+__device__ __forceinline__ float decay_exp(float x) { return __expf(x); }
+
 // ---- bf16 planes -------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t pack_bf16(float lo_elem, float hi_elem) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo_elem, hi_elem);
@@ -165,6 +169,58 @@ __device__ __forceinline__ void load_a_t(uint32_t (&r)[4], uint32_t base, int w,
 __device__ __forceinline__ void load_slice_t(uint32_t (&r)[4], uint32_t base, int k0, int lane) {
     const int m = lane >> 3, x = lane & 7;
     ldsm4_t(r, slice_addr(base, k0 + (m >> 1) * 8 + x, m & 1));
+}
+
+// ---- fragments of fp32 tiles in shared memory ---------------------------------------------------------------
+// A pair of values into place r of N planes.
+template <int N>
+__device__ __forceinline__ void frag_pair(uint32_t (&f)[N][4], int r, float x, float y) {
+    uint32_t w[N];
+    split_pair<N>(x, y, w);
+#pragma unroll
+    for (int p = 0; p < N; ++p) f[p][r] = w[p];
+}
+// Operand A (m16 x k16) of a tile [m][k] of rows of `w` floats (w = 8 mod 32: no bank conflicts) ...
+__device__ __forceinline__ void frag_a(uint32_t (&f)[kPlanes][4], const float *tile, int w, int m0, int k0, int lane) {
+    const float *p = tile + (m0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float2 x = *reinterpret_cast<const float2 *>(p + (r & 1) * 8 * w + (r >> 1) * 8);
+        frag_pair(f, r, x.x, x.y);
+    }
+}
+// ... and of a tile [k][m].
+__device__ __forceinline__ void frag_a_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int m0, int lane) {
+    const float *p = tile + (k0 + 2 * (lane & 3)) * w + m0 + (lane >> 2);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float *q = p + (r >> 1) * 8 * w + (r & 1) * 8;
+        frag_pair(f, r, q[0], q[w]);
+    }
+}
+// Operand B (k16 x n16) of a tile [n][k] ...
+__device__ __forceinline__ void frag_b(uint32_t (&f)[kPlanes][4], const float *tile, int w, int n0, int k0, int lane) {
+    const float *p = tile + (n0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float2 x = *reinterpret_cast<const float2 *>(p + (r >> 1) * 8 * w + (r & 1) * 8);
+        frag_pair(f, r, x.x, x.y);
+    }
+}
+// ... and of a tile [k][n] (w = 4 mod 16: no bank conflicts).
+__device__ __forceinline__ void frag_b_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int n0, int lane) {
+    const float *p = tile + (k0 + 2 * (lane & 3)) * w + n0 + (lane >> 2);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float *q = p + (r & 1) * 8 * w + (r >> 1) * 8;
+        frag_pair(f, r, q[0], q[w]);
+    }
+}
+// c0, c1 += a b over all plane products that count.
+template <int PA, int PB>
+__device__ __forceinline__ void mma_all(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][4]) {
+#pragma unroll
+    for (int pb = 0; pb < PB; ++pb) mma_planes<PA, kPlanes>(c0, c1, a, b[pb], pb);
 }
 
 // Asynchronous 16-byte copy that writes zeros when `ok` is false (the source is then not read).

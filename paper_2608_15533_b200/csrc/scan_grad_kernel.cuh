@@ -13,9 +13,11 @@
 // is kept out of the difference (where gates are strong it would be all that is there) and added to dq and dk afterwards;
 // so is, for RWKV6, the readout of the token in front, which crosses none either.
 //
-// 256 threads; warp w owns token rows 16 (w & 3) .. + 15 and the channel half w >> 2 of every [64 x d_k] result.  fp32
-// operands stay fp32 in shared memory (two bytes per element less than three planes, and both orientations from one
-// tile); a warp forms its fragments' planes as it reads them.
+// The [64 x d_k] products contract over d_v, so S_0, dS_1, dO, U and dV stream through shared memory in slices of 32
+// columns of d_v, the next slice on its way while one is multiplied.  fp32 operands stay fp32 there (two bytes per element
+// less than three planes, and both orientations from one tile); a warp forms its fragments' planes as it reads them.
+// 512 threads; warp w owns token rows 16 (w & 3) .. + 15 and the channel quarter w >> 2 of every result: the work between
+// two barriers is a few hundred instructions per warp, and sixteen warps cover each other's latencies where eight did not.
 #pragma once
 
 #include "scan_common.cuh"
@@ -23,111 +25,76 @@
 
 namespace deltalog {
 
-// ---- fragments of fp32 tiles in shared memory ---------------------------------------------------------------
-// A pair of values into place r of N planes.
-template <int N>
-__device__ __forceinline__ void frag_pair(uint32_t (&f)[N][4], int r, float x, float y) {
-    uint32_t w[N];
-    split_pair<N>(x, y, w);
-#pragma unroll
-    for (int p = 0; p < N; ++p) f[p][r] = w[p];
-}
-// Operand A (m16 x k16) of a tile [m][k] of rows of `w` floats (w = 8 mod 32: no bank conflicts) ...
-__device__ __forceinline__ void frag_a(uint32_t (&f)[kPlanes][4], const float *tile, int w, int m0, int k0, int lane) {
-    const float *p = tile + (m0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float2 x = *reinterpret_cast<const float2 *>(p + (r & 1) * 8 * w + (r >> 1) * 8);
-        frag_pair(f, r, x.x, x.y);
-    }
-}
-// ... and of a tile [k][m].
-__device__ __forceinline__ void frag_a_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int m0, int lane) {
-    const float *p = tile + (k0 + 2 * (lane & 3)) * w + m0 + (lane >> 2);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float *q = p + (r >> 1) * 8 * w + (r & 1) * 8;
-        frag_pair(f, r, q[0], q[w]);
-    }
-}
-// Operand B (k16 x n16) of a tile [n][k] ...
-__device__ __forceinline__ void frag_b(uint32_t (&f)[kPlanes][4], const float *tile, int w, int n0, int k0, int lane) {
-    const float *p = tile + (n0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float2 x = *reinterpret_cast<const float2 *>(p + (r >> 1) * 8 * w + (r & 1) * 8);
-        frag_pair(f, r, x.x, x.y);
-    }
-}
-// ... and of a tile [k][n] (w = 4 mod 16: no bank conflicts).
-__device__ __forceinline__ void frag_b_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int n0, int lane) {
-    const float *p = tile + (k0 + 2 * (lane & 3)) * w + n0 + (lane >> 2);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float *q = p + (r & 1) * 8 * w + (r >> 1) * 8;
-        frag_pair(f, r, q[0], q[w]);
-    }
-}
+constexpr int kGradThreads = 512;
+constexpr int kSlice = 32;
+constexpr int kSliceStride = kSlice + 8;
+
 // fp32 tile of rows `stride` elements apart to padded rows of `w` floats; rows at and behind `valid` become zeros.
-__device__ __forceinline__ void load_f32(float *dst, const float *src, size_t stride, int rows, int cols, int w, int valid, int tid) {
-    const int upr = cols >> 2, sh = cols == 128 ? 5 : 4;
-    for (int i = tid; i < rows * upr; i += 256) {
-        const int row = i >> sh, unit = i & (upr - 1);
+template <int COLS>
+__device__ __forceinline__ void load_f32(float *dst, const float *src, size_t stride, int rows, int w, int valid, int tid) {
+    constexpr int kUnits = COLS / 4;
+    for (int i = tid; i < rows * kUnits; i += kGradThreads) {
+        const int row = i / kUnits, unit = i % kUnits;
         const bool ok = row < valid;
         cp_async16_zfill(smem_addr(dst + row * w + unit * 4), src + (ok ? (size_t)row * stride + unit * 4 : 0), ok);
     }
 }
-// The token rows of an io tensor that is an operand of this kernel: bf16 as it is (swizzled), fp32 padded.
-__device__ __forceinline__ void load_io(unsigned char *dst, const __nv_bfloat16 *src, size_t stride, int dv, int valid, int tid) {
-    load_tile(smem_addr(dst), src, stride, kChunk, dv, valid, tid, 256);
+// bf16 tile of 64 rows of 32 elements (64 bytes): 16-byte units permuted by the row's bits 1 and 2.
+__device__ __forceinline__ uint32_t slice32_addr(uint32_t base, int row, int unit) {
+    return base + (uint32_t)(row * 64 + ((unit ^ ((row >> 1) & 3)) << 4));
 }
-__device__ __forceinline__ void load_io(unsigned char *dst, const float *src, size_t stride, int dv, int valid, int tid) {
-    load_f32(reinterpret_cast<float *>(dst), src, stride, kChunk, dv, dv + 8, valid, tid);
+// A slice of the io tensors: bf16 as it is, fp32 padded.
+__device__ __forceinline__ void load_io(unsigned char *dst, const __nv_bfloat16 *src, size_t stride, int valid, int tid) {
+    if (tid < kChunk * 4) {
+        const int row = tid >> 2, unit = tid & 3;
+        const bool ok = row < valid;
+        cp_async16_zfill(slice32_addr(smem_addr(dst), row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
+    }
 }
-__device__ __forceinline__ void io_frag_a(uint32_t (&f)[1][4], const unsigned char *tile, int dv, int m0, int k0, int lane) {
-    load_a(f[0], smem_addr(tile), dv, m0, k0, lane);
+__device__ __forceinline__ void load_io(unsigned char *dst, const float *src, size_t stride, int valid, int tid) {
+    load_f32<kSlice>(reinterpret_cast<float *>(dst), src, stride, kChunk, kSliceStride, valid, tid);
 }
-__device__ __forceinline__ void io_frag_a(uint32_t (&f)[kPlanes][4], const unsigned char *tile, int dv, int m0, int k0, int lane) {
-    frag_a(f, reinterpret_cast<const float *>(tile), dv + 8, m0, k0, lane);
+__device__ __forceinline__ void io_frag_a(uint32_t (&f)[1][4], const unsigned char *tile, int m0, int k0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4(f[0], slice32_addr(smem_addr(tile), m0 + (m & 1) * 8 + x, (k0 >> 3) + (m >> 1)));
 }
-__device__ __forceinline__ void io_frag_b(uint32_t (&f)[1][4], const unsigned char *tile, int dv, int n0, int k0, int lane) {
-    load_b(f[0], smem_addr(tile), dv, n0, k0, lane);
+__device__ __forceinline__ void io_frag_a(uint32_t (&f)[kPlanes][4], const unsigned char *tile, int m0, int k0, int lane) {
+    frag_a(f, reinterpret_cast<const float *>(tile), kSliceStride, m0, k0, lane);
 }
-__device__ __forceinline__ void io_frag_b(uint32_t (&f)[kPlanes][4], const unsigned char *tile, int dv, int n0, int k0, int lane) {
-    frag_b(f, reinterpret_cast<const float *>(tile), dv + 8, n0, k0, lane);
+__device__ __forceinline__ void io_frag_b(uint32_t (&f)[1][4], const unsigned char *tile, int n0, int k0, int lane) {
+    const int m = lane >> 3, x = lane & 7;
+    ldsm4(f[0], slice32_addr(smem_addr(tile), n0 + (m >> 1) * 8 + x, (k0 >> 3) + (m & 1)));
 }
-// c0, c1 += a b over all plane products that count.
-template <int PA, int PB>
-__device__ __forceinline__ void mma_all(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][4]) {
-#pragma unroll
-    for (int pb = 0; pb < PB; ++pb) mma_planes<PA, kPlanes>(c0, c1, a, b[pb], pb);
+__device__ __forceinline__ void io_frag_b(uint32_t (&f)[kPlanes][4], const unsigned char *tile, int n0, int k0, int lane) {
+    frag_b(f, reinterpret_cast<const float *>(tile), kSliceStride, n0, k0, lane);
 }
 
 template <int OP, int P, int DK, typename IO>
 struct GradSmem {
     static constexpr bool VEC = OpTraits<OP>::kVecDecay, DELTA = OpTraits<OP>::kDeltaRule;
     static constexpr int kTile = kChunk * DK * 2;
-    static constexpr int kSW = DK + 4;              // row of a state tile or of a decayed vector
+    static constexpr int kSW = DK + 4;              // row of a state slice or of a decayed vector
     static constexpr int kMW = kChunk + 8;          // row of dA, dL'
     static constexpr int kMat = kChunk * kMW * 4;
-    // last phase: q and k planes, or the three decayed vectors and two more fp32 tiles
-    static constexpr int last = VEC ? (DELTA ? 5 : 4) * kChunk * kSW * 4 : 2 * P * kTile;
-    __host__ __device__ static constexpr int f32_tile(int dv) { return kChunk * (dv + 8) * 4; }
-    __host__ __device__ static constexpr int io_tile(int dv) { return sizeof(IO) == 4 ? f32_tile(dv) : kChunk * dv * 2; }
-    __host__ __device__ static constexpr int u_tile(int dv) { return DELTA ? f32_tile(dv) : io_tile(dv); }
-    __host__ __device__ static constexpr int dout(int dv) { return dv * kSW * 4; }   // behind the state tile
-    __host__ __device__ static constexpr int mats(int dv) {
-        const int first = dout(dv) + io_tile(dv) + u_tile(dv) + (DELTA ? f32_tile(dv) : 0);
-        return first > last ? first : last;
-    }
-    __host__ __device__ static constexpr int small(int dv) { return mats(dv) + (DELTA ? 2 : 1) * kMat; }
-    static constexpr int kSmall = 8 * DK * 4       // partial sums of <dS, S>
-                                  + 4 * kChunk * 4 // row sums
-                                  + 4 * DK * 4     // block decays
-                                  + 2 * kChunk * 4 // beta, diagonal of dA
-                                  + kChunk * 8     // G
-                                  + 16;
-    static constexpr size_t bytes(int dv) { return small(dv) + kSmall; }
+    static constexpr int kF32 = kChunk * kSliceStride * 4;
+    static constexpr int kIO = sizeof(IO) == 4 ? kF32 : kChunk * kSlice * 2;
+    // a stage: slices of S_0, dS_1, dO, U (or v), dV
+    static constexpr int kState = kSlice * kSW * 4;
+    static constexpr int dS = kState, dO = 2 * kState, U = dO + kIO, dV = U + (DELTA ? kF32 : kIO), stage = dV + (DELTA ? kF32 : 0);
+    // after the slices: q and k planes (bf16 io: in a place of their own, loaded meanwhile), or the three decayed vectors and
+    // the decays in front of and behind a token inside its block
+    static constexpr bool kOwnQK = !VEC && P == 1;
+    static constexpr int qk = kOwnQK ? 2 * stage : 0;
+    static constexpr int last = VEC ? (DELTA ? 5 : 4) * kChunk * kSW * 4 : qk + 2 * P * kTile;
+    static constexpr int mats = 2 * stage > last ? 2 * stage : last;
+    static constexpr int small = mats + (DELTA ? 2 : 1) * kMat;
+    static constexpr int part = small;                  // [1024] partial sums of <dS, S>
+    static constexpr int rows = part + 4096;            // [8][64] row sums of the channel quarters
+    static constexpr int tables = rows + 8 * kChunk * 4; // [4][4][DK] e^(decay) of the chunk in front of / behind a block, of the block, inverse
+    static constexpr int beta = tables + (VEC ? 16 * DK * 4 : 0);
+    static constexpr int G = beta + 2 * kChunk * 4;     // beta, diagonal of dA;  sums of the scalar decay
+    static constexpr int deep = G + kChunk * 8;
+    static constexpr size_t bytes = deep + 16;
 };
 
 // A pair of neighbouring channels of the io tensors' row.
@@ -139,124 +106,138 @@ __device__ __forceinline__ float2 load_pair(const void *src, size_t at) {
 }
 
 template <int OP, int P, int DK, typename IO>
-__global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanArgs a) {
     using L = GradSmem<OP, P, DK, IO>;
     constexpr bool VEC = L::VEC, DELTA = L::DELTA, EXCL = OpTraits<OP>::kBonus;
-    constexpr int NT = DK / 16, SW = L::kSW, MW = L::kMW;
+    constexpr int NT = DK / 32, SW = L::kSW, MW = L::kMW;
     constexpr int IP = sizeof(IO) == 4 ? kPlanes : 1;  // planes of dO and of v
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
-    const int g = lane >> 2, t = lane & 3, mt = warp & 3, c0 = (warp >> 2) * (DK / 2);
+    const int g = lane >> 2, t = lane & 3, mt = warp & 3, cq = warp >> 2, c0 = cq * (DK / 4);
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const int dv = a.dv, hq = h / (a.H / a.Hq);
     const size_t unit = (size_t)chunk * a.H + h, tile = (size_t)DK * dv;
-    float *st = reinterpret_cast<float *>(smem);
-    unsigned char *do_t = smem + L::dout(dv), *u_t = do_t + L::io_tile(dv);
-    const float *u_f = reinterpret_cast<const float *>(u_t);            // delta rule: U and dV, fp32
-    float *dv_f = reinterpret_cast<float *>(u_t + L::u_tile(dv));
-    float *da_f = reinterpret_cast<float *>(smem + L::mats(dv)), *dl_f = da_f + kChunk * MW;
-    float *part = reinterpret_cast<float *>(smem + L::small(dv));  // [8][DK]
-    float *rows = part + 8 * DK;                                  // [4][64]: y and b of the two channel halves
-    float *B = rows + 4 * kChunk;                                 // [4][DK]
-    float *beta = B + 4 * DK, *diag = beta + kChunk;
+    float *da_f = reinterpret_cast<float *>(smem + L::mats), *dl_f = da_f + kChunk * MW;
+    float *part = reinterpret_cast<float *>(smem + L::part), *rows = reinterpret_cast<float *>(smem + L::rows);
+    float *beta = reinterpret_cast<float *>(smem + L::beta), *diag = beta + kChunk;
     float *near = beta;  // RWKV6 (no beta): dA's entries next to the diagonal
-    double *G = reinterpret_cast<double *>(diag + kChunk);
-    int *deep = reinterpret_cast<int *>(G + kChunk);
+    float2 *G = reinterpret_cast<float2 *>(smem + L::G);
+    int *deep = reinterpret_cast<int *>(smem + L::deep);
+    const size_t v_off = ((size_t)p.tok0 * a.H + h) * dv, v_stride = (size_t)a.H * dv;
 
-    // S_0, dO, U, dV
-    load_f32(st, a.S + unit * tile, DK, dv, DK, SW, dv, tid);
-    const size_t v_off = ((size_t)p.tok0 * a.H + h) * dv;
-    load_io(do_t, static_cast<const IO *>(a.dout) + v_off, (size_t)a.H * dv, dv, p.valid, tid);
-    if (DELTA) {
-        load_f32(reinterpret_cast<float *>(u_t), a.U + unit * kChunk * dv, dv, kChunk, dv, dv + 8, kChunk, tid);
-        load_f32(dv_f, a.dV + unit * kChunk * dv, dv, kChunk, dv, dv + 8, kChunk, tid);
-    } else {
-        load_io(u_t, static_cast<const IO *>(a.v) + v_off, (size_t)a.H * dv, dv, p.valid, tid);
-    }
-    cp_async_commit();
+    auto load_stage = [&](int s) {
+        unsigned char *st = smem + (s & 1) * L::stage;
+        const int v = s * kSlice;
+        load_f32<DK>(reinterpret_cast<float *>(st), a.S + unit * tile + (size_t)v * DK, DK, kSlice, SW, kSlice, tid);
+        load_f32<DK>(reinterpret_cast<float *>(st + L::dS), a.dS + unit * tile + (size_t)v * DK, DK, kSlice, SW, kSlice, tid);
+        load_io(st + L::dO, static_cast<const IO *>(a.dout) + v_off + v, v_stride, p.valid, tid);
+        if (DELTA) {
+            load_f32<kSlice>(reinterpret_cast<float *>(st + L::U), a.U + unit * kChunk * dv + v, dv, kChunk, kSliceStride, kChunk, tid);
+            load_f32<kSlice>(reinterpret_cast<float *>(st + L::dV), a.dV + unit * kChunk * dv + v, dv, kChunk, kSliceStride, kChunk, tid);
+        } else {
+            load_io(st + L::U, static_cast<const IO *>(a.v) + v_off + v, v_stride, p.valid, tid);
+        }
+    };
+    auto load_qk = [&]() {
+        const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK;
+#pragma unroll
+        for (int pl = 0; pl < P; ++pl) {
+            load_tile(sm + L::qk + pl * L::kTile, a.qp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, kGradThreads);
+            load_tile(sm + L::qk + (P + pl) * L::kTile, a.kp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, kGradThreads);
+        }
+    };
+    const int slices = dv / kSlice;
+    load_stage(0), cp_async_commit();
     if (tid < 4) deep[tid] = 0;
     if (!VEC && warp == 0) chunk_decay_sums(a, p, h, G, lane);
     if (DELTA && tid >= 64 && tid < 128) beta[tid - 64] = scan_beta(tid - 64 < p.valid ? a.beta[(size_t)(p.tok0 + tid - 64) * a.H + h] : 0.f);
-    cp_async_wait_all();
-    __syncthreads();
+    if (L::kOwnQK) load_qk();
 
-    // dO S_0^T and dV S_0^T
-    float dq[NT][4] = {}, dr[NT][4] = {}, dw[NT][4] = {};
-    for (int k0 = 0; k0 < dv; k0 += 16) {
-        uint32_t f[IP][4], e[kPlanes][4];
-        io_frag_a(f, do_t, dv, mt * 16, k0, lane);
-        if (DELTA) frag_a(e, dv_f, dv + 8, mt * 16, k0, lane);
+    // dO S_0^T, dV S_0^T, U dS_1^T [16 x DK/4] and, where the warp's 16 columns are at or below the diagonal, dO U^T, dV U^T
+    float dq[NT][4] = {}, dr[NT][4] = {}, dw[NT][4] = {}, da[2][4] = {}, dl[2][4] = {};
+    float dot0 = 0.f, dot1 = 0.f, db = 0.f;
+    constexpr int kPairs = DK / 2, kGroups = kGradThreads / kPairs;
+    const int cp = tid % kPairs, grp = tid / kPairs;
+    for (int sl = 0; sl < slices; ++sl) {
+        if (sl + 1 < slices) load_stage(sl + 1);
+        cp_async_commit();
+        cp_async_wait<1>();
+        __syncthreads();
+        const unsigned char *st = smem + (sl & 1) * L::stage;
+        const float *S = reinterpret_cast<const float *>(st), *dS = reinterpret_cast<const float *>(st + L::dS);
+        const float *u_f = reinterpret_cast<const float *>(st + L::U), *v_f = reinterpret_cast<const float *>(st + L::dV);
 #pragma unroll
-        for (int nn = 0; nn < NT / 2; ++nn) {
-            uint32_t b[kPlanes][4];
-            frag_b_t(b, st, SW, k0, c0 + nn * 16, lane);
-            mma_all(dq[2 * nn], dq[2 * nn + 1], f, b);
-            if (DELTA) mma_all(dr[2 * nn], dr[2 * nn + 1], e, b);
-        }
-    }
-    // <dS_1, S_0> by channel
-    {
-        constexpr int kPairs = DK / 2, kGroups = 256 / kPairs;
-        const int cp = tid % kPairs, grp = tid / kPairs;
-        float s0 = 0.f, s1 = 0.f;
-        const float *src = a.dS + unit * tile + cp * 2;
-        for (int v = grp; v < dv; v += kGroups) {
-            const float2 d = *reinterpret_cast<const float2 *>(src + (size_t)v * DK), x = *reinterpret_cast<const float2 *>(st + v * SW + cp * 2);
-            s0 = fmaf(d.x, x.x, s0), s1 = fmaf(d.y, x.y, s1);
-        }
-        part[grp * DK + cp * 2] = s0, part[grp * DK + cp * 2 + 1] = s1;
-    }
-    __syncthreads();
-    load_f32(st, a.dS + unit * tile, DK, dv, DK, SW, dv, tid);
-    cp_async_commit();
-    // dbeta: four threads per token
-    if (DELTA) {
-        const int i = tid >> 2, qd = tid & 3;
-        const float rb = 1.f / beta[i];
-        float s = 0.f;
-        for (int v = qd * 2; v < dv; v += 8) {
-            const float2 u = *reinterpret_cast<const float2 *>(u_f + i * (dv + 8) + v), d = *reinterpret_cast<const float2 *>(dv_f + i * (dv + 8) + v);
-            s = fmaf(u.x * rb, d.x * rb, s), s = fmaf(u.y * rb, d.y * rb, s);
-        }
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        s += __shfl_xor_sync(0xffffffffu, s, 2);
-        if (qd == 0 && i < p.valid) a.dbeta[(size_t)(p.tok0 + i) * a.H + h] = s;
-    }
-    // dA and dL', masked; scalar decay multiplies e^(G_i - G_j) in here
-    {
-        const int j0 = (warp >> 2) * 32;
-        float da[4][4] = {}, dl[4][4] = {};
-        if (j0 <= mt * 16 + 15) {
-            for (int k0 = 0; k0 < dv; k0 += 16) {
+        for (int k0 = 0; k0 < kSlice; k0 += 16) {
+            {
                 uint32_t f[IP][4], e[kPlanes][4];
-                io_frag_a(f, do_t, dv, mt * 16, k0, lane);
-                if (DELTA) frag_a(e, dv_f, dv + 8, mt * 16, k0, lane);
+                io_frag_a(f, st + L::dO, mt * 16, k0, lane);
+                if (DELTA) frag_a(e, v_f, kSliceStride, mt * 16, k0, lane);
 #pragma unroll
-                for (int nn = 0; nn < 2; ++nn) {
+                for (int nn = 0; nn < NT / 2; ++nn) {
+                    uint32_t b[kPlanes][4];
+                    frag_b_t(b, S, SW, k0, c0 + nn * 16, lane);
+                    mma_all(dq[2 * nn], dq[2 * nn + 1], f, b);
+                    if (DELTA) mma_all(dr[2 * nn], dr[2 * nn + 1], e, b);
+                }
+                if (cq <= mt) {
                     if constexpr (DELTA) {
                         uint32_t b[kPlanes][4];
-                        frag_b(b, u_f, dv + 8, j0 + nn * 16, k0, lane);
-                        mma_all(da[2 * nn], da[2 * nn + 1], f, b);
-                        mma_all(dl[2 * nn], dl[2 * nn + 1], e, b);
+                        frag_b(b, u_f, kSliceStride, cq * 16, k0, lane);
+                        mma_all(da[0], da[1], f, b);
+                        mma_all(dl[0], dl[1], e, b);
                     } else {
                         uint32_t b[IP][4];
-                        io_frag_b(b, u_t, dv, j0 + nn * 16, k0, lane);
-                        mma_all(da[2 * nn], da[2 * nn + 1], f, b);
+                        io_frag_b(b, st + L::U, cq * 16, k0, lane);
+                        mma_all(da[0], da[1], f, b);
                     }
                 }
             }
-        }
+            constexpr int UP = DELTA ? kPlanes : IP;
+            uint32_t f[UP][4];
+            if constexpr (DELTA) frag_a(f, u_f, kSliceStride, mt * 16, k0, lane);
+            else io_frag_a(f, st + L::U, mt * 16, k0, lane);
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+            for (int nn = 0; nn < NT / 2; ++nn) {
+                uint32_t b[kPlanes][4];
+                frag_b_t(b, dS, SW, k0, c0 + nn * 16, lane);
+                mma_all(dw[2 * nn], dw[2 * nn + 1], f, b);
+            }
+        }
+        // <dS_1, S_0> by channel, and sum_v dV U by token (eight threads each)
+#pragma unroll
+        for (int v = grp; v < kSlice; v += kGroups) {
+            const float2 x = *reinterpret_cast<const float2 *>(S + v * SW + cp * 2), d = *reinterpret_cast<const float2 *>(dS + v * SW + cp * 2);
+            dot0 = fmaf(d.x, x.x, dot0), dot1 = fmaf(d.y, x.y, dot1);
+        }
+        if (DELTA) {
+            const int i = tid >> 3, v = (tid & 7) * 4;
+            const float rb = 1.f / beta[i];
+            const float4 u = *reinterpret_cast<const float4 *>(u_f + i * kSliceStride + v), d = *reinterpret_cast<const float4 *>(v_f + i * kSliceStride + v);
+            db = fmaf(u.x * rb, d.x * rb, db), db = fmaf(u.y * rb, d.y * rb, db), db = fmaf(u.z * rb, d.z * rb, db), db = fmaf(u.w * rb, d.w * rb, db);
+        }
+        __syncthreads();
+    }
+    part[grp * DK + cp * 2] = dot0, part[grp * DK + cp * 2 + 1] = dot1;
+    if (DELTA) {
+        db += __shfl_xor_sync(0xffffffffu, db, 1);
+        db += __shfl_xor_sync(0xffffffffu, db, 2);
+        db += __shfl_xor_sync(0xffffffffu, db, 4);
+        if ((tid & 7) == 0 && (tid >> 3) < p.valid) a.dbeta[(size_t)(p.tok0 + (tid >> 3)) * a.H + h] = db;
+    }
+    if (!VEC && !L::kOwnQK) load_qk(), cp_async_commit();
+    // dA and dL', masked; scalar decay multiplies e^(G_i - G_j) in here
+    if (cq <= mt) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int i = mt * 16 + g + 8 * half, j = j0 + n * 8 + 2 * t;
+                const int i = mt * 16 + g + 8 * half, j = cq * 16 + n * 8 + 2 * t;
                 float x[2], y[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float m = VEC ? 1.f : (j + e <= i ? expf((float)(G[i] - G[j + e])) : 0.f);
+                    const float m = VEC ? 1.f : (j + e <= i ? decay_exp(decay_between(G[i], G[j + e])) : 0.f);
                     const float raw = da[n][2 * half + e];
                     if (i == j + e) diag[i] = raw * a.scale;
                     if (EXCL && i == j + e + 1) near[i] = raw;
@@ -267,23 +248,6 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
                 if (DELTA) *reinterpret_cast<float2 *>(dl_f + i * MW + j) = make_float2(y[0], y[1]);
             }
     }
-    cp_async_wait_all();
-    __syncthreads();
-    // U dS_1^T
-    for (int k0 = 0; k0 < dv; k0 += 16) {
-        constexpr int UP = DELTA ? kPlanes : IP;
-        uint32_t f[UP][4];
-        if constexpr (DELTA) frag_a(f, u_f, dv + 8, mt * 16, k0, lane);
-        else io_frag_a(f, u_t, dv, mt * 16, k0, lane);
-#pragma unroll
-        for (int nn = 0; nn < NT / 2; ++nn) {
-            uint32_t b[kPlanes][4];
-            frag_b_t(b, st, SW, k0, c0 + nn * 16, lane);
-            mma_all(dw[2 * nn], dw[2 * nn + 1], f, b);
-        }
-    }
-    __syncthreads();  // state tile, dO, U, dV are done with
-
     const bool whole = a.H == a.Hq;
     // results of element pair (row i, channels c, c + 1)
     auto put = [&](void *io_dst, float *part_dst, int i, int c, float x, float y) {
@@ -298,28 +262,7 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
     };
 
     if constexpr (!VEC) {
-        const uint32_t q_s = sm, k_s = sm + P * L::kTile;
-        const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK;
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl) {
-            load_tile(q_s + pl * L::kTile, a.qp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, 256);
-            load_tile(k_s + pl * L::kTile, a.kp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, 256);
-        }
-        cp_async_commit();
-        float front[2], back[2];  // e^G and e^(G_end - G) of rows g, g + 8
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int i = mt * 16 + g + 8 * r;
-            front[r] = expf((float)G[i]), back[r] = expf((float)(G[kChunk - 1] - G[i]));
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                dq[n][e] *= a.scale * front[e >> 1];
-                dr[n][e] *= -front[e >> 1];
-                dw[n][e] *= back[e >> 1];
-            }
+        const uint32_t q_s = sm + L::qk, k_s = q_s + P * L::kTile;
         cp_async_wait_all();
         __syncthreads();
         float y[2] = {0.f, 0.f}, b2[2] = {0.f, 0.f};
@@ -335,45 +278,46 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
             return v;
         };
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int r = 0; r < 2; ++r) {
+            const int i = mt * 16 + g + 8 * r;
+            const float front = expf(G[i].x + G[i].y), back = expf(decay_between(G[kChunk - 1], G[i]));
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const float2 kv = value(k_s, mt * 16 + g + 8 * r, c0 + n * 8 + 2 * t);
-                b2[r] = fmaf(kv.x, dw[n][2 * r], fmaf(kv.y, dw[n][2 * r + 1], b2[r]));
+            for (int n = 0; n < NT; ++n) {
+                const float2 kv = value(k_s, i, c0 + n * 8 + 2 * t);
+#pragma unroll
+                for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                    dq[n][e] *= a.scale * front;
+                    dr[n][e] *= -front;
+                    dw[n][e] *= back;
+                    b2[r] = fmaf((e & 1) ? kv.y : kv.x, dw[n][e], b2[r]);
+                }
             }
+        }
         // inside the chunk: dq += dA K, dk as written += dA^T Q + dL'^T K, dk as read += dL' K
         float di[NT][4] = {};
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
-            uint32_t am[kPlanes][4], lm[kPlanes][4];
-            if (kb <= mt) {
-                frag_a(am, da_f, MW, mt * 16, kb * 16, lane);
-                if (DELTA) frag_a(lm, dl_f, MW, mt * 16, kb * 16, lane);
+            uint32_t m[kPlanes][4];
+            // a product of one matrix (or its transpose) with the 16 tokens of block kb of q or k
+            auto product = [&](float (&x)[NT][4], const float *mat, bool transposed, uint32_t vec) {
+                if (transposed) frag_a_t(m, mat, MW, kb * 16, mt * 16, lane);
+                else frag_a(m, mat, MW, mt * 16, kb * 16, lane);
 #pragma unroll
                 for (int nn = 0; nn < NT / 2; ++nn)
 #pragma unroll
                     for (int pl = 0; pl < P; ++pl) {
                         uint32_t b[4];
-                        load_b_t(b, k_s + pl * L::kTile, DK, kb * 16, c0 + nn * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(dq[2 * nn], dq[2 * nn + 1], am, b, pl);
-                        if (DELTA) mma_planes<kPlanes, kPlanes>(dr[2 * nn], dr[2 * nn + 1], lm, b, pl);
+                        load_b_t(b, vec + pl * L::kTile, DK, kb * 16, c0 + nn * 16, lane);
+                        mma_planes<kPlanes, kPlanes>(x[2 * nn], x[2 * nn + 1], m, b, pl);
                     }
+            };
+            if (kb <= mt) {
+                product(dq, da_f, false, k_s);
+                if (DELTA) product(dr, dl_f, false, k_s);
             }
             if (kb >= mt) {
-                frag_a_t(am, da_f, MW, kb * 16, mt * 16, lane);
-                if (DELTA) frag_a_t(lm, dl_f, MW, kb * 16, mt * 16, lane);
-#pragma unroll
-                for (int nn = 0; nn < NT / 2; ++nn)
-#pragma unroll
-                    for (int pl = 0; pl < P; ++pl) {
-                        uint32_t b[4];
-                        load_b_t(b, q_s + pl * L::kTile, DK, kb * 16, c0 + nn * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(di[2 * nn], di[2 * nn + 1], am, b, pl);
-                        if (DELTA) {
-                            load_b_t(b, k_s + pl * L::kTile, DK, kb * 16, c0 + nn * 16, lane);
-                            mma_planes<kPlanes, kPlanes>(di[2 * nn], di[2 * nn + 1], lm, b, pl);
-                        }
-                    }
+                product(di, da_f, true, q_s);
+                if (DELTA) product(di, dl_f, true, k_s);
             }
         }
 #pragma unroll
@@ -396,20 +340,21 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
             y[r] += __shfl_xor_sync(0xffffffffu, y[r], 2), b2[r] += __shfl_xor_sync(0xffffffffu, b2[r], 2);
             if (t == 0) {
                 const int i = mt * 16 + g + 8 * r;
-                rows[(warp >> 2) * kChunk + i] = y[r];
-                rows[(2 + (warp >> 2)) * kChunk + i] = b2[r];
+                rows[cq * kChunk + i] = y[r];
+                rows[(4 + cq) * kChunk + i] = b2[r];
             }
         }
         __syncthreads();
         if (warp == 0) {
             float s = 0.f;
-            for (int i = lane; i < (256 / (DK / 2)) * DK; i += 32) s += part[i];
-            const float across = warp_sum(s) * expf((float)G[kChunk - 1]);
-            // lane holds tokens 2 lane, 2 lane + 1
-            const float y0 = rows[2 * lane] + rows[kChunk + 2 * lane], y1 = rows[2 * lane + 1] + rows[kChunk + 2 * lane + 1];
-            const float w0 = rows[2 * kChunk + 2 * lane] + rows[3 * kChunk + 2 * lane];
-            const float w1 = rows[2 * kChunk + 2 * lane + 1] + rows[3 * kChunk + 2 * lane + 1];
-            float suf = y0 + y1, pre = w0 + w1;
+            for (int i = lane; i < 1024; i += 32) s += part[i];
+            const float across = warp_sum(s) * expf(G[kChunk - 1].x + G[kChunk - 1].y);
+            float yy[2] = {0.f, 0.f}, ww[2] = {0.f, 0.f};  // lane holds tokens 2 lane, 2 lane + 1
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) yy[e] += rows[x * kChunk + 2 * lane + e], ww[e] += rows[(4 + x) * kChunk + 2 * lane + e];
+            float suf = yy[0] + yy[1], pre = ww[0] + ww[1];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const float u = __shfl_down_sync(0xffffffffu, suf, o), v = __shfl_up_sync(0xffffffffu, pre, o);
@@ -420,38 +365,56 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
             if (lane == 31) after = 0.f;
             if (lane == 0) before = 0.f;
             const int i = 2 * lane;
-            if (i < p.valid) a.dg[(size_t)(p.tok0 + i) * a.H + h] = across + before + (after + y1 + y0);
-            if (i + 1 < p.valid) a.dg[(size_t)(p.tok0 + i + 1) * a.H + h] = across + (before + w0) + (after + y1);
+            if (i < p.valid) a.dg[(size_t)(p.tok0 + i) * a.H + h] = across + before + (after + yy[1] + yy[0]);
+            if (i + 1 < p.valid) a.dg[(size_t)(p.tok0 + i + 1) * a.H + h] = across + (before + ww[0]) + (after + yy[1]);
         }
     } else {
-        // decayed vectors, and the decay in front of / behind a token inside its block
+        // decayed vectors, and the decay factors in front of / behind a token inside its block; one (block, channel) per thread
         constexpr int kV = kChunk * SW;
-        float *qs = st, *kc = qs + kV, *ps = kc + kV, *ss = ps + kV, *ks = ss + kV;
-        for (int w = tid; w < 4 * DK; w += 256) {
-            const int blk = w / DK, c = w % DK;
-            BlockVectors<IO> o;
-            block_vectors<IO, EXCL>(a, p, h, hq, DK, blk, c, true, o);
-            B[blk * DK + c] = o.B;
-            if (!(o.B > -kBlockDecay)) deep[blk] = 1;
-            float pre = 0.f, suf = 0.f;
+        float *qs = reinterpret_cast<float *>(smem), *kc = qs + kV, *ps = kc + kV, *ss = ps + kV, *ks = ss + kV;
+        float *front = reinterpret_cast<float *>(smem + L::tables), *back = front + 4 * DK, *eB = back + 4 * DK, *eI = eB + 4 * DK;
+        const int blk = tid / DK, c = tid % DK;
+        const bool mine = tid < 4 * DK;
+        auto raw = [&](const void *src, int i, int ch) { return i < p.valid ? to_f32(static_cast<const IO *>(src)[((size_t)(p.tok0 + i) * a.Hq + hq) * DK + ch]) : 0.f; };
+        auto gate_at = [&](int i, int ch) { return i < p.valid ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + ch] : 0.f; };
+        float Bc = 0.f;
+        if (mine) {
+            float gate[kBlock], kk[kBlock], qq[kBlock];
+#pragma unroll
+            for (int r = 0; r < kBlock; ++r) gate[r] = gate_at(blk * kBlock + r, c), kk[r] = raw(a.k, blk * kBlock + r, c), qq[r] = raw(a.q, blk * kBlock + r, c);
+            float e = 1.f;
 #pragma unroll
             for (int r = 0; r < kBlock; ++r) {
-                const int i = blk * kBlock + r;
-                const float gate = i < p.valid ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + c] : 0.f;
-                if (EXCL) ps[i * SW + c] = pre;
-                pre += gate;
-                if (!EXCL) ps[i * SW + c] = pre;
-                qs[i * SW + c] = o.qs[r];
-                kc[i * SW + c] = o.kc[r];
-                if (DELTA) ks[i * SW + c] = o.ks[r];
+                const int at = (blk * kBlock + r) * SW + c;
+                if (EXCL) qs[at] = qq[r] * e, ps[at] = e;
+                Bc += gate[r];
+                e = decay_exp(Bc);
+                if (!EXCL) qs[at] = qq[r] * e, ps[at] = e;
+                if (DELTA) ks[at] = kk[r] * e;
             }
+            float s = 0.f;
 #pragma unroll
             for (int r = kBlock - 1; r >= 0; --r) {
-                const int i = blk * kBlock + r;
-                ss[i * SW + c] = suf;
-                suf += i < p.valid ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + c] : 0.f;
+                const int at = (blk * kBlock + r) * SW + c;
+                e = decay_exp(s);
+                kc[at] = kk[r] * e, ss[at] = e;
+                s += gate[r];
             }
+            if (!(Bc > -kBlockDecay)) deep[blk] = 1;
+            eB[blk * DK + c] = Bc;
         }
+        __syncthreads();
+        if (mine) {
+            float f = 0.f, b = 0.f;
+            for (int m = 0; m < 4; ++m) {
+                const float x = eB[m * DK + c];
+                if (m < blk) f += x;
+                if (m > blk) b += x;
+            }
+            front[blk * DK + c] = decay_exp(f), back[blk * DK + c] = decay_exp(b), eI[blk * DK + c] = expf(-Bc);
+        }
+        __syncthreads();
+        if (mine) eB[blk * DK + c] = decay_exp(Bc);
         __syncthreads();
         float acc[NT][4], dia[NT][4];
         // sum over blocks J < mt (towards the front) or I > mt (towards the back) of a row block's pairs, the decay of the
@@ -462,115 +425,85 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
         };
-        auto times_block = [&](float (&x)[NT][4], int blk, float sign) {
+        auto times_block = [&](float (&x)[NT][4], const float *table, int b) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float2 d = *reinterpret_cast<const float2 *>(B + blk * DK + c0 + n * 8 + 2 * t);
-                const float e0 = expf(sign * d.x), e1 = expf(sign * d.y);
-                x[n][0] *= e0, x[n][1] *= e1, x[n][2] *= e0, x[n][3] *= e1;
+                const float2 d = *reinterpret_cast<const float2 *>(table + b * DK + c0 + n * 8 + 2 * t);
+                x[n][0] *= d.x, x[n][1] *= d.y, x[n][2] *= d.x, x[n][3] *= d.y;
             }
         };
-        auto product = [&](float (&x)[NT][4], const float *mat, bool transposed, int blk, const float *vec) {
+        auto product = [&](float (&x)[NT][4], const float *mat, bool transposed, int b_, const float *vec) {
             uint32_t m[kPlanes][4];
-            if (transposed) frag_a_t(m, mat, MW, blk * 16, mt * 16, lane);
-            else frag_a(m, mat, MW, mt * 16, blk * 16, lane);
+            if (transposed) frag_a_t(m, mat, MW, b_ * 16, mt * 16, lane);
+            else frag_a(m, mat, MW, mt * 16, b_ * 16, lane);
 #pragma unroll
             for (int nn = 0; nn < NT / 2; ++nn) {
                 uint32_t b[kPlanes][4];
-                frag_b_t(b, vec, SW, blk * 16, c0 + nn * 16, lane);
+                frag_b_t(b, vec, SW, b_ * 16, c0 + nn * 16, lane);
                 mma_all(x[2 * nn], x[2 * nn + 1], m, b);
             }
         };
-        // a strongly decaying block's own pairs, one by one: for element (i, c) the sum over j of mat[i][j] x_jc e^(..),
-        // or (transposed) over the later rows
-        auto raw = [&](const void *src, int i, int c) { return i < p.valid ? to_f32(static_cast<const IO *>(src)[((size_t)(p.tok0 + i) * a.Hq + hq) * DK + c]) : 0.f; };
-        auto gate_at = [&](int i, int c) { return i < p.valid ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + c] : 0.f; };
-        auto pairs_front = [&](const float *mat, int i, int c) {  // sum_(j <= i) mat_ij k_jc e^(G_i - G_j)
+        // a strongly decaying block's own pairs, one by one: for element (i, c) the sum over j of mat[i][j] k_jc e^(..),
+        // or over the later rows
+        auto pairs_front = [&](const float *mat, int i, int ch) {  // sum_(j <= i) mat_ij k_jc e^(G_i - G_j)
             float s = 0.f, x = 0.f;
             for (int j = i; j >= mt * 16; --j) {
-                if (j < i && !(EXCL && j + 1 == i)) x += gate_at(j + 1, c);
-                s = fmaf(mat[i * MW + j] * raw(a.k, j, c), expf(x), s);
+                if (j < i && !(EXCL && j + 1 == i)) x += gate_at(j + 1, ch);
+                s = fmaf(mat[i * MW + j] * raw(a.k, j, ch), expf(x), s);
             }
             return s;
         };
-        auto pairs_back = [&](int j, int c) {  // sum_(i >= j) (dA_ij q_ic + dL'_ij k_ic) e^(G_i - G_j)
+        auto pairs_back = [&](int j, int ch) {  // sum_(i >= j) (dA_ij q_ic + dL'_ij k_ic) e^(G_i - G_j)
             float s = 0.f, x = 0.f;
             for (int i = j; i < mt * 16 + 16; ++i) {
-                if (i > j && !EXCL) x += gate_at(i, c);
-                if (EXCL && i > j + 1) x += gate_at(i - 1, c);
-                float w = da_f[i * MW + j] * raw(a.q, i, c);
-                if (DELTA) w = fmaf(dl_f[i * MW + j], raw(a.k, i, c), w);
+                if (i > j && !EXCL) x += gate_at(i, ch);
+                if (EXCL && i > j + 1) x += gate_at(i - 1, ch);
+                float w = da_f[i * MW + j] * raw(a.q, i, ch);
+                if (DELTA) w = fmaf(dl_f[i * MW + j], raw(a.k, i, ch), w);
                 s = fmaf(w, expf(x), s);
             }
             return s;
         };
         const bool own_deep = deep[mt] != 0;
-        auto chunk_front = [&](int c) {
-            float s = 0.f;
-            for (int m = 0; m < mt; ++m) s += B[m * DK + c];
-            return s;
-        };
-        auto chunk_back = [&](int c) {
-            float s = 0.f;
-            for (int m = mt + 1; m < 4; ++m) s += B[m * DK + c];
-            return s;
-        };
-        // dq
-        zero(acc), zero(dia);
-        for (int J = 0; J < mt; ++J) {
-            if (J) times_block(acc, J, 1.f);
-            product(acc, da_f, false, J, kc);
-        }
-        if (!own_deep) product(dia, da_f, false, mt, kc), times_block(dia, mt, -1.f);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = mt * 16 + g + 8 * (e >> 1), c = c0 + n * 8 + 2 * t + (e & 1);
-                const float ep = expf(ps[i * SW + c]);
-                float x = fmaf(expf(chunk_front(c)) * ep * a.scale, dq[n][e], ep * (acc[n][e] + dia[n][e]));
-                if (own_deep) x += pairs_front(da_f, i, c);
-                dq[n][e] = x;
-            }
-        // dk as read
-        if (DELTA) {
+        // dq (and dk as read): x <- sign e^G x + e^p (pairs inside the chunk)
+        auto towards_front = [&](float (&x)[NT][4], const float *mat, float sign) {
             zero(acc), zero(dia);
             for (int J = 0; J < mt; ++J) {
-                if (J) times_block(acc, J, 1.f);
-                product(acc, dl_f, false, J, kc);
+                if (J) times_block(acc, eB, J);
+                product(acc, mat, false, J, kc);
             }
-            if (!own_deep) product(dia, dl_f, false, mt, kc), times_block(dia, mt, -1.f);
+            if (!own_deep) product(dia, mat, false, mt, kc), times_block(dia, eI, mt);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int i = mt * 16 + g + 8 * (e >> 1), c = c0 + n * 8 + 2 * t + (e & 1);
-                    const float ep = expf(ps[i * SW + c]);
-                    float x = fmaf(-expf(chunk_front(c)) * ep, dr[n][e], ep * (acc[n][e] + dia[n][e]));
-                    if (own_deep) x += pairs_front(dl_f, i, c);
-                    dr[n][e] = x;
+                    const int i = mt * 16 + g + 8 * (e >> 1), ch = c0 + n * 8 + 2 * t + (e & 1);
+                    x[n][e] = ps[i * SW + ch] * fmaf(sign * front[mt * DK + ch], x[n][e], acc[n][e] + dia[n][e]);
+                    if (own_deep) x[n][e] += pairs_front(mat, i, ch);
                 }
-        }
+        };
+        towards_front(dq, da_f, a.scale);
+        if (DELTA) towards_front(dr, dl_f, -1.f);
         // dk as written: behind the chunk (dw), inside it (acc)
         zero(acc), zero(dia);
         for (int I = 3; I > mt; --I) {
-            if (I < 3) times_block(acc, I, 1.f);
+            if (I < 3) times_block(acc, eB, I);
             product(acc, da_f, true, I, qs);
             if (DELTA) product(acc, dl_f, true, I, ks);
         }
         if (!own_deep) {
             product(dia, da_f, true, mt, qs);
             if (DELTA) product(dia, dl_f, true, mt, ks);
-            times_block(dia, mt, -1.f);
+            times_block(dia, eI, mt);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const int i = mt * 16 + g + 8 * r, c = c0 + n * 8 + 2 * t;
+                const int i = mt * 16 + g + 8 * r, ch = c0 + n * 8 + 2 * t;
                 float2 qv = make_float2(0.f, 0.f), kv = qv, q_next = qv, k_prev = qv;
                 if (i < p.valid) {
-                    const size_t at = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK + c, row = (size_t)a.Hq * DK;
+                    const size_t at = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK + ch, row = (size_t)a.Hq * DK;
                     qv = load_pair<IO>(a.q, at), kv = load_pair<IO>(a.k, at);
                     if (EXCL && i > 0) k_prev = load_pair<IO>(a.k, at - row);
                     if (EXCL && i + 1 < p.valid) q_next = load_pair<IO>(a.q, at + row);
@@ -580,24 +513,24 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int el = 2 * r + e;
-                    const float es = expf(ss[i * SW + c + e]);
+                    const float es = ss[i * SW + ch + e];
                     float in = es * (acc[n][el] + dia[n][el]);
-                    if (own_deep) in += pairs_back(i, c + e);
-                    const float out = expf(chunk_back(c + e)) * es * dw[n][el];
+                    if (own_deep) in += pairs_back(i, ch + e);
+                    const float out = back[mt * DK + ch + e] * es * dw[n][el];
                     const float qe = e ? qv.y : qv.x, ke = e ? kv.y : kv.x;
                     // the readout of RWKV6 sees the decays in front of its token only: its term belongs to the token before
                     float y = ke * ((DELTA ? dr[n][el] : 0.f) - in);
                     if (!EXCL) y = fmaf(qe, dq[n][el], y);
-                    ps[i * SW + c + e] = y;
-                    ss[i * SW + c + e] = ke * out;
+                    ps[i * SW + ch + e] = y;
+                    ss[i * SW + ch + e] = ke * out;
                     oq[e] = dq[n][el], ok[e] = out + in + (DELTA ? dr[n][el] : 0.f);
                     if (EXCL) dq[n][el] *= qe;
-                    const float own = EXCL ? diag[i] * a.bonus[h * DK + c + e] : diag[i];
+                    const float own = EXCL ? diag[i] * a.bonus[h * DK + ch + e] : diag[i];
                     oq[e] = fmaf(own, ke, oq[e]), ok[e] = fmaf(own, qe, ok[e]);
                     if (EXCL) oq[e] = fmaf(to_prev, e ? k_prev.y : k_prev.x, oq[e]), ok[e] = fmaf(from_next, e ? q_next.y : q_next.x, ok[e]);
                 }
-                put(a.dq, a.dq_part, i, c, oq[0], oq[1]);
-                put(a.dk, a.dk_part, i, c, ok[0], ok[1]);
+                put(a.dq, a.dq_part, i, ch, oq[0], oq[1]);
+                put(a.dk, a.dk_part, i, ch, ok[0], ok[1]);
             }
         if (EXCL) {  // q dq goes one token up, now that every y stands
             __syncthreads();
@@ -605,33 +538,44 @@ __global__ void __launch_bounds__(256, 1) scan_grad_kernel(const ScanArgs a) {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int i = mt * 16 + g + 8 * (e >> 1), c = c0 + n * 8 + 2 * t + (e & 1);
-                    if (i > 0) ps[(i - 1) * SW + c] += dq[n][e];
+                    const int i = mt * 16 + g + 8 * (e >> 1), ch = c0 + n * 8 + 2 * t + (e & 1);
+                    if (i > 0) ps[(i - 1) * SW + ch] += dq[n][e];
                 }
         }
         __syncthreads();
-        if (tid < DK) {
-            const int c = tid;
-            float x = 0.f, db = 0.f;
-            for (int i = 0; i < 256 / (DK / 2); ++i) x += part[i * DK + c];
-            x *= expf(B[c] + B[DK + c] + B[2 * DK + c] + B[3 * DK + c]);
-            for (int i = 0; i < p.valid; ++i) {  // <dS, S> and what comes from the tokens in front, into ss
-                const float w = ss[i * SW + c];
-                ss[i * SW + c] = x;
-                x += w;
+        // sums over the tokens of a block, then over the blocks (the tables' places are free, but for the chunk's decay)
+        float *ysum = eI, *bsum = kc, *bonus_sum = kc + 4 * DK;
+        if (mine) {
+            float y = 0.f, b = 0.f, w = 0.f;
+#pragma unroll
+            for (int r = 0; r < kBlock; ++r) {
+                const int i = blk * kBlock + r;
+                y += ps[i * SW + c], b += ss[i * SW + c];
+                if (EXCL) w = fmaf(diag[i], raw(a.q, i, c) * raw(a.k, i, c), w);
             }
-            float y = 0.f;
-            for (int i = kChunk - 1; i >= 0; --i) {
+            ysum[blk * DK + c] = y, bsum[blk * DK + c] = b;
+            if (EXCL) bonus_sum[blk * DK + c] = w;
+        }
+        __syncthreads();
+        if (mine) {
+            float x = 0.f, y = 0.f;
+            for (int i = 0; i < kGroups; ++i) x += part[i * DK + c];
+            x *= front[3 * DK + c] * eB[3 * DK + c];  // e^(G_end)
+            for (int m = 0; m < 4; ++m) {
+                if (m < blk) x += bsum[m * DK + c];
+                if (m > blk) y += ysum[m * DK + c];
+            }
+            float before[kBlock];  // <dS, S> and what comes from the tokens in front
+#pragma unroll
+            for (int r = 0; r < kBlock; ++r) before[r] = x, x += ss[(blk * kBlock + r) * SW + c];
+#pragma unroll
+            for (int r = kBlock - 1; r >= 0; --r) {
+                const int i = blk * kBlock + r;
                 y += ps[i * SW + c];
-                if (i < p.valid) a.dg[((size_t)(p.tok0 + i) * a.H + h) * DK + c] = ss[i * SW + c] + y;
+                if (i < p.valid) a.dg[((size_t)(p.tok0 + i) * a.H + h) * DK + c] = before[r] + y;
             }
-            if (EXCL) {
-                for (int i = 0; i < p.valid; ++i) {
-                    const size_t at = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK + c;
-                    db = fmaf(diag[i], to_f32(static_cast<const IO *>(a.q)[at]) * to_f32(static_cast<const IO *>(a.k)[at]), db);
-                }
-                a.dbonus_part[unit * DK + c] = db;
-            }
+            if (EXCL && blk == 0)
+                a.dbonus_part[unit * DK + c] = (bonus_sum[c] + bonus_sum[DK + c]) + (bonus_sum[2 * DK + c] + bonus_sum[3 * DK + c]);
         }
     }
 }

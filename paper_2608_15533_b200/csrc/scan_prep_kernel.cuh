@@ -27,42 +27,60 @@ __device__ __forceinline__ bool chunk_place(const ScanArgs &a, int chunk, ChunkP
     return true;
 }
 
-constexpr int kInvStride = 65;
+constexpr int kInvStride = kChunk + 8;  // row of the fp32 matrices: fragment reads without bank conflicts
 
-// T = (I + N)^-1 for the strictly lower N (64 x 64, fp32): the four diagonal 16 x 16 blocks by forward substitution,
-// one column per thread, then the blocks below them, one block diagonal after the other.
-__device__ __forceinline__ void invert_unit_lower(const float *N, float *T, float *X, int tid, int nthreads) {
+// T = (I + N)^-1 for the strictly lower N (64 x 64, fp32).  The four diagonal 16 x 16 blocks by forward substitution, one
+// column per thread; then warp J solves column block J downwards, T_IJ = -T_II sum_(J <= K < I) N_IK T_KJ, on the tensor
+// cores and transposed: the accumulators of a block are the A operand of the next.  (With fp32 FMAs in place of the
+// products this step took two thirds of the kernel.)
+__device__ __forceinline__ void invert_unit_lower(const float *N, float *T, int tid) {
+    const int lane = tid & 31, J = tid >> 5;
     if (tid < kChunk) {
         const int b = tid & ~15, c = tid & 15;
         float x[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            float s = r == c ? 1.f : 0.f;
+            float s0 = r == c ? 1.f : 0.f, s1 = 0.f;
 #pragma unroll
-            for (int k = 0; k < r; ++k) s = fmaf(-N[(b + r) * kInvStride + b + k], x[k], s);
-            x[r] = s;
-            T[(b + r) * kInvStride + b + c] = s;
+            for (int k = 0; k < r; k += 2) {
+                const float2 n = *reinterpret_cast<const float2 *>(N + (b + r) * kInvStride + b + k);
+                s0 = fmaf(-n.x, x[k], s0);
+                if (k + 1 < r) s1 = fmaf(-n.y, x[k + 1], s1);
+            }
+            x[r] = s0 + s1;
+            T[(b + r) * kInvStride + b + c] = x[r];
         }
     }
     __syncthreads();
-    for (int d = 1; d < 4; ++d) {
-        const int count = (4 - d) * 256;
-        for (int i = tid; i < count; i += nthreads) {
-            const int bi = d + (i >> 8), r = (i >> 4) & 15, c = i & 15, j0 = (bi - d) * 16;
-            float s = 0.f;
-            for (int k = j0; k < bi * 16; ++k) s = fmaf(N[(bi * 16 + r) * kInvStride + k], T[k * kInvStride + j0 + c], s);
-            X[i] = s;
-        }
-        __syncthreads();
-        for (int i = tid; i < count; i += nthreads) {
-            const int bi = d + (i >> 8), r = (i >> 4) & 15, c = i & 15, j0 = (bi - d) * 16;
-            float s = 0.f;
+    if (J < 3) {
+        const int g = lane >> 2, t = lane & 3;
+        uint32_t f[3][kPlanes][4];  // blocks (J + r, J) of T, transposed, as A operands
+        frag_a_t(f[0], T, kInvStride, J * 16, J * 16, lane);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) s = fmaf(-T[(bi * 16 + r) * kInvStride + bi * 16 + k], X[(i & ~255) + k * 16 + c], s);
-            T[(bi * 16 + r) * kInvStride + j0 + c] = s;
+        for (int r = 1; r < 4; ++r) {
+            const int I = J + r;
+            if (I > 3) break;
+            float x[2][4] = {}, y[2][4] = {};
+            uint32_t b[kPlanes][4], w[kPlanes][4];
+#pragma unroll
+            for (int k = 0; k < r; ++k) {
+                frag_b(b, N, kInvStride, I * 16, (J + k) * 16, lane);
+                mma_all(x[0], x[1], f[k], b);
+            }
+            acc_to_a<kPlanes>(x[0], x[1], w);
+            frag_b(b, T, kInvStride, I * 16, I * 16, lane);
+            mma_all(y[0], y[1], w, b);
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[n][e] = -y[n][e];
+                    T[(I * 16 + n * 8 + 2 * t + (e & 1)) * kInvStride + J * 16 + g + 8 * (e >> 1)] = y[n][e];
+                }
+            if (r < 3) acc_to_a<kPlanes>(y[0], y[1], f[r]);
         }
-        __syncthreads();
     }
+    __syncthreads();
 }
 
 // A pair of values to the same place of kPlanes planes.
@@ -73,20 +91,21 @@ __device__ __forceinline__ void put_planes(__nv_bfloat16 *dst, size_t plane, flo
     for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<uint32_t *>(dst + p * plane) = w[p];
 }
 
-// T diag(beta) as planes, zeros above the diagonal.
+// T diag(beta) as planes.  Of A and T the 16 x 16 blocks above the diagonal are neither written nor read.
 __device__ __forceinline__ void write_inverse(const float *T, const float *beta, __nv_bfloat16 *dst, int tid, int nthreads) {
-    for (int i = tid; i < kChunk * kChunk / 2; i += nthreads) {
-        const int r = i >> 5, c = (i & 31) * 2;
-        const float x = c <= r ? T[r * kInvStride + c] * beta[c] : 0.f;
-        const float y = c + 1 <= r ? T[r * kInvStride + c + 1] * beta[c + 1] : 0.f;
-        put_planes(dst + r * kChunk + c, kChunk * kChunk, x, y);
+    for (int i = tid; i < 10 * 128; i += nthreads) {  // ten blocks of 128 pairs
+        const int blk = i >> 7, I = blk < 1 ? 0 : blk < 3 ? 1 : blk < 6 ? 2 : 3, J = blk - I * (I + 1) / 2;
+        const int r = I * 16 + ((i >> 3) & 15), c = J * 16 + (i & 7) * 2;
+        const float2 x = *reinterpret_cast<const float2 *>(T + r * kInvStride + c);
+        put_planes(dst + r * kChunk + c, kChunk * kChunk, c <= r ? x.x * beta[c] : 0.f, c + 1 <= r ? x.y * beta[c + 1] : 0.f);
     }
 }
 
 // Cumulative scalar log-decay of the chunk's tokens, in fp64: differences of the sums, not the sums, go into
-// exponentials, and after a strong decay fp32 sums would leave the later differences few bits.  A gate below -1e4
+// exponentials, and after a strong decay fp32 sums would leave the later differences few bits (so a sum is kept as two
+// floats).  A gate below -1e4
 // counts as -1e4 (its exponential is zero all the same), so that a reset (-inf) gives no inf - inf.
-__device__ __forceinline__ void chunk_decay_sums(const ScanArgs &a, const ChunkPlace &p, int h, double *G, int lane) {
+__device__ __forceinline__ void chunk_decay_sums(const ScanArgs &a, const ChunkPlace &p, int h, float2 *G, int lane) {
     double x[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -100,29 +119,40 @@ __device__ __forceinline__ void chunk_decay_sums(const ScanArgs &a, const ChunkP
         const double y = __shfl_up_sync(0xffffffffu, s, o);
         if (lane >= o) s += y;
     }
-    G[2 * lane + 1] = s;
-    G[2 * lane] = s - x[1];
+#pragma unroll
+    for (int e = 1; e >= 0; --e) {
+        const float hi = (float)s;
+        G[2 * lane + e] = make_float2(hi, (float)(s - hi));
+        s -= x[e];
+    }
 }
+__device__ __forceinline__ float decay_between(const float2 &i, const float2 &j) { return (i.x - j.x) + (i.y - j.y); }
 
 template <int P, int DK>
-constexpr size_t prep_scalar_smem(bool delta) {
-    return (size_t)2 * P * kChunk * DK * 2 + (kChunk * 8) + kChunk * 4 + (delta ? (2 * kChunk * kInvStride + 3 * 256) * 4 : 0);
-}
+struct PrepScalarSmem {
+    static constexpr int kTile = kChunk * DK * 2;
+    static constexpr int kMat = kChunk * kInvStride * 4;
+    static constexpr int first = 2 * P * kTile > kMat ? 2 * P * kTile : kMat;  // q and k, then T
+    static constexpr int small = first, N = small + kChunk * 8 + kChunk * 4;
+    static constexpr size_t bytes(bool delta) { return N + (delta ? kMat : 0); }
+};
 
-// Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.
+// Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.  Four CTAs share an SM: the steps of
+// one chunk depend on each other, and only other chunks fill the gaps.
 template <int P, int DK, bool DELTA>
-__global__ void __launch_bounds__(128) scan_prep_scalar_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs a) {
+    using L = PrepScalarSmem<P, DK>;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const size_t unit = (size_t)chunk * a.H + h;
     const int hq = h / (a.H / a.Hq);
-    constexpr int kTile = kChunk * DK * 2;
+    constexpr int kTile = L::kTile;
     const uint32_t q_s = smem_addr(smem), k_s = q_s + P * kTile;
-    double *G = reinterpret_cast<double *>(smem + 2 * P * kTile);
+    float *T = reinterpret_cast<float *>(smem), *N = reinterpret_cast<float *>(smem + L::N);
+    float2 *G = reinterpret_cast<float2 *>(smem + L::small);
     float *beta = reinterpret_cast<float *>(G + kChunk);
-    float *N = beta + kChunk, *T = N + kChunk * kInvStride, *X = T + kChunk * kInvStride;
     const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK;
 #pragma unroll
     for (int pl = 0; pl < P; ++pl) {
@@ -138,8 +168,8 @@ __global__ void __launch_bounds__(128) scan_prep_scalar_kernel(const ScanArgs a)
     cp_async_wait_all();
     __syncthreads();
     if (tid < kChunk) {
-        a.decay[unit * 2 * kChunk + tid] = expf((float)G[tid]);
-        a.decay[unit * 2 * kChunk + kChunk + tid] = expf((float)(G[kChunk - 1] - G[tid]));
+        a.decay[unit * 2 * kChunk + tid] = expf(G[tid].x + G[tid].y);
+        a.decay[unit * 2 * kChunk + kChunk + tid] = expf(decay_between(G[kChunk - 1], G[tid]));
     }
     const int m0 = warp * 16;
     float qa[8][4] = {}, ka[8][4] = {};
@@ -158,37 +188,34 @@ __global__ void __launch_bounds__(128) scan_prep_scalar_kernel(const ScanArgs a)
             for (int pl = 0; pl < P; ++pl) {
                 uint32_t b[4];
                 load_b(b, k_s + pl * kTile, DK, nn * 16, k0, lane);
-#pragma unroll
-                for (int pa = 0; pa + pl < P; ++pa) {  // P = 3: the six products that count
-                    mma(qa[2 * nn], aq[pa], b[0], b[1]);
-                    mma(qa[2 * nn + 1], aq[pa], b[2], b[3]);
-                    if (DELTA) {
-                        mma(ka[2 * nn], ak[pa], b[0], b[1]);
-                        mma(ka[2 * nn + 1], ak[pa], b[2], b[3]);
-                    }
-                }
+                mma_planes<P, P>(qa[2 * nn], qa[2 * nn + 1], aq, b, pl);
+                if (DELTA) mma_planes<P, P>(ka[2 * nn], ka[2 * nn + 1], ak, b, pl);
             }
         }
     }
     const int g = lane >> 2, t = lane & 3;
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
+    const float2 Gi[2] = {G[m0 + g], G[m0 + g + 8]};
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+    for (int n = 0; n < 8; ++n) {
+        if (n > 2 * warp + 1) break;
+        const int j = n * 8 + 2 * t;
+        const float2 G0 = G[j], G1 = G[j + 1];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int i = m0 + g + 8 * half, j = n * 8 + 2 * t;
-            float m[2], x[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                m[e] = j + e <= i ? expf((float)(G[i] - G[j + e])) : 0.f;
-                x[e] = j + e <= i ? a.scale * qa[n][2 * half + e] * m[e] : 0.f;
-                if (DELTA) N[i * kInvStride + j + e] = j + e < i ? beta[i] * ka[n][2 * half + e] * m[e] : 0.f;
-            }
-            put_planes(A + i * kChunk + j, kChunk * kChunk, x[0], x[1]);
+            const int i = m0 + g + 8 * half;
+            const float d0 = j <= i ? decay_exp(decay_between(Gi[half], G0)) : 0.f, d1 = j + 1 <= i ? decay_exp(decay_between(Gi[half], G1)) : 0.f;
+            // (selected, not multiplied: a product above the diagonal may be anything)
+            put_planes(A + i * kChunk + j, kChunk * kChunk, j <= i ? a.scale * qa[n][2 * half] * d0 : 0.f,
+                       j + 1 <= i ? a.scale * qa[n][2 * half + 1] * d1 : 0.f);
+            if (DELTA)
+                *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(j < i ? beta[i] * ka[n][2 * half] * d0 : 0.f,
+                                                                                  j + 1 < i ? beta[i] * ka[n][2 * half + 1] * d1 : 0.f);
         }
+    }
     if (DELTA) {
         __syncthreads();
-        invert_unit_lower(N, T, X, tid, 128);
+        invert_unit_lower(N, T, tid);
         write_inverse(T, beta, a.T + unit * kPlanes * kChunk * kChunk, tid, 128);
     }
 }
@@ -204,52 +231,56 @@ __global__ void __launch_bounds__(128) scan_prep_scalar_kernel(const ScanArgs a)
 constexpr int kBlock = 16;
 constexpr float kBlockDecay = 60.f;
 
-// q_i e^(p_i) (RWKV6: its readout sees the decay in front of the token), k_i e^(p_i), k_j e^(s_j) of a (block, channel).
-template <typename IO>
+// The decayed vectors of one block and one pair of neighbouring channels: q_i e^(p_i) (RWKV6: the decay in front of the
+// token), k_i e^(p_i), k_j e^(s_j), and the block's total B.
 struct BlockVectors {
-    float qs[kBlock], ks[kBlock], kc[kBlock];
-    float B;
+    float2 qs[kBlock], ks[kBlock], kc[kBlock];
+    float2 B;
 };
-template <typename IO, bool EXCL>
-__device__ __forceinline__ void block_vectors(const ScanArgs &a, const ChunkPlace &p, int h, int hq, int DK, int blk, int c, bool with_q,
-                                              BlockVectors<IO> &o) {
-    float gate[kBlock];
+template <typename IO, bool EXCL, bool DELTA>
+__device__ __forceinline__ void block_vectors(const ScanArgs &a, const ChunkPlace &p, int h, int hq, int DK, int blk, int c, BlockVectors &o) {
+    float2 gate[kBlock];
 #pragma unroll
     for (int r = 0; r < kBlock; ++r) {
         const int i = blk * kBlock + r;
-        const bool ok = i < p.valid;
-        gate[r] = ok ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + c] : 0.f;
-        const size_t at = ((size_t)(p.tok0 + (ok ? i : 0)) * a.Hq + hq) * DK + c;
-        o.kc[r] = ok ? to_f32(static_cast<const IO *>(a.k)[at]) : 0.f;
-        if (with_q) o.qs[r] = ok ? to_f32(static_cast<const IO *>(a.q)[at]) : 0.f;
+        gate[r] = o.kc[r] = o.qs[r] = make_float2(0.f, 0.f);
+        if (i < p.valid) {
+            gate[r] = *reinterpret_cast<const float2 *>(a.g + ((size_t)(p.tok0 + i) * a.H + h) * DK + c);
+            const size_t at = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK + c;
+            float x[2];
+            load_vec<IO, 2>(static_cast<const IO *>(a.k) + at, x);
+            o.kc[r] = make_float2(x[0], x[1]);
+            load_vec<IO, 2>(static_cast<const IO *>(a.q) + at, x);
+            o.qs[r] = make_float2(x[0], x[1]);
+        }
     }
-    float s = 0.f;
+    float2 s = make_float2(0.f, 0.f), e = make_float2(1.f, 1.f);
 #pragma unroll
     for (int r = 0; r < kBlock; ++r) {
-        if (EXCL && with_q) o.qs[r] *= expf(s);
-        s += gate[r];
-        const float e = expf(s);
-        if (!EXCL && with_q) o.qs[r] *= e;
-        o.ks[r] = o.kc[r] * e;
+        if (EXCL) o.qs[r].x *= e.x, o.qs[r].y *= e.y;
+        s.x += gate[r].x, s.y += gate[r].y;
+        e = make_float2(decay_exp(s.x), decay_exp(s.y));
+        if (!EXCL) o.qs[r].x *= e.x, o.qs[r].y *= e.y;
+        if (DELTA) o.ks[r] = make_float2(o.kc[r].x * e.x, o.kc[r].y * e.y);
     }
-    s = 0.f;
+    s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int r = kBlock - 1; r >= 0; --r) {
-        o.kc[r] *= expf(s);
-        s += gate[r];
+        o.kc[r].x *= decay_exp(s.x), o.kc[r].y *= decay_exp(s.y);
+        s.x += gate[r].x, s.y += gate[r].y;
     }
     o.B = s;
 }
 
-// fp32 tile of 64 x DK in shared memory, rows padded by four
 template <int DK>
-constexpr int kVecStride = DK + 4;
-
-template <int DK>
-constexpr size_t prep_vector_smem(bool delta) {
-    return (size_t)(delta ? 2 : 1) * kChunk * kVecStride<DK> * 4 + kPlanes * kChunk * DK * 2 + 4 * DK * 4 + kChunk * 4 + 16 +
-           (delta ? (2 * kChunk * kInvStride + 3 * 256) * 4 : 0);
-}
+struct PrepVectorSmem {
+    static constexpr int kVS = DK + 8;                    // row of the fp32 vectors
+    static constexpr int kVec = kChunk * kVS * 4;
+    // q e^p, k e^s, (delta rule) k e^p, in whose place N and T come later; factors between blocks.  Two CTAs share an SM.
+    __host__ __device__ static constexpr int factors(bool delta) { return (delta ? 3 : 2) * kVec; }
+    __host__ __device__ static constexpr int small(bool delta) { return factors(delta) + 11 * DK * 4; }
+    static constexpr size_t bytes(bool delta) { return small(delta) + kChunk * 4 + 16; }
+};
 
 // One pair (i, j) of a strongly decaying block: sum_c x_ic k_jc e^(g_(j+1) + .. + g_i) with the gates added up directly.
 template <typename IO, bool EXCL>
@@ -271,115 +302,110 @@ __device__ __forceinline__ void pair_sums(const ScanArgs &a, const ChunkPlace &p
 
 // OP selects the readout (RWKV6) and the delta rule; 256 threads.
 template <int OP, int DK, typename IO>
-__global__ void __launch_bounds__(256) scan_prep_vector_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs a) {
     constexpr bool DELTA = OpTraits<OP>::kDeltaRule, EXCL = OpTraits<OP>::kBonus;
+    using L = PrepVectorSmem<DK>;
+    constexpr int VS = L::kVS;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const size_t unit = (size_t)chunk * a.H + h;
     const int hq = h / (a.H / a.Hq);
-    constexpr int VS = kVecStride<DK>;
-    constexpr int kTile = kChunk * DK * 2;
-    const uint32_t kc_s = smem_addr(smem);
-    float *qs = reinterpret_cast<float *>(smem + kPlanes * kTile);
-    float *ks = qs + kChunk * VS;                       // delta rule only
-    float *B = DELTA ? ks + kChunk * VS : ks;           // [4][DK]
-    float *beta = B + 4 * DK;
-    int *deep = reinterpret_cast<int *>(beta + kChunk); // [4] blocks that decay too far for the factored form
-    float *N = reinterpret_cast<float *>(deep + 4), *T = N + kChunk * kInvStride, *X = T + kChunk * kInvStride;
+    float *qs = reinterpret_cast<float *>(smem), *kc = qs + kChunk * VS, *ks = kc + kChunk * VS;
+    float *B = reinterpret_cast<float *>(smem + L::factors(DELTA));  // [4][DK] block decays
+    float *F = B + 4 * DK;                                          // [7][DK] e^(-B_I), e^(B_1), e^(B_2), e^(B_1 + B_2)
+    float *beta = reinterpret_cast<float *>(smem + L::small(DELTA));
+    int *deep = reinterpret_cast<int *>(beta + kChunk);             // [4] blocks that decay too far for the factored form
+    float *T = reinterpret_cast<float *>(smem), *N = T + kChunk * kInvStride;
     if (tid < 4) deep[tid] = 0;
     if (DELTA && tid >= 64 && tid < 128) {
         const int i = tid - 64;
         beta[i] = scan_beta(i < p.valid ? a.beta[(size_t)(p.tok0 + i) * a.H + h] : 0.f);
     }
     __syncthreads();
-    for (int w = tid; w < 4 * DK; w += 256) {
-        const int blk = w / DK, c = w % DK;
-        BlockVectors<IO> o;
-        block_vectors<IO, EXCL>(a, p, h, hq, DK, blk, c, true, o);
-        B[blk * DK + c] = o.B;
-        if (!(o.B > -kBlockDecay)) deep[blk] = 1;
+    // a thread's block and channel pair: the block's vectors into shared memory, then, with the other blocks' decays at hand,
+    // the whole chunk's to the chain kernels
+    constexpr int kPairs = DK / 2;
+    const int blk = tid / kPairs, c = (tid % kPairs) * 2;
+    const bool mine = tid < 4 * kPairs;
+    if (mine) {
+        BlockVectors o;
+        block_vectors<IO, EXCL, DELTA>(a, p, h, hq, DK, blk, c, o);
+        *reinterpret_cast<float2 *>(B + blk * DK + c) = o.B;
+        if (!(o.B.x > -kBlockDecay && o.B.y > -kBlockDecay)) deep[blk] = 1;
 #pragma unroll
         for (int r = 0; r < kBlock; ++r) {
-            const int i = blk * kBlock + r;
-            qs[i * VS + c] = o.qs[r] * a.scale;
-            if (DELTA) ks[i * VS + c] = o.ks[r];
-            unsigned char *at = smem + i * DK * 2 + (((c >> 3) ^ (i & 7)) << 4) + (c & 7) * 2;
-            float x = o.kc[r];
-#pragma unroll
-            for (int pl = 0; pl < kPlanes; ++pl) {
-                const __nv_bfloat16 w = __float2bfloat16_rn(x);
-                *reinterpret_cast<__nv_bfloat16 *>(at + pl * kTile) = w;
-                x -= __bfloat162float(w);
-            }
+            const int at = (blk * kBlock + r) * VS + c;
+            o.qs[r].x *= a.scale, o.qs[r].y *= a.scale;
+            *reinterpret_cast<float2 *>(qs + at) = o.qs[r];
+            *reinterpret_cast<float2 *>(kc + at) = o.kc[r];
+            if (DELTA) *reinterpret_cast<float2 *>(ks + at) = o.ks[r];
         }
     }
     __syncthreads();
-    // decayed vectors of the whole chunk for the chain kernels
-    const size_t vec = unit * kPlanes * kChunk * DK;
-    for (int w = tid; w < kChunk * DK / 2; w += 256) {
-        const int i = w / (DK / 2), c = (w % (DK / 2)) * 2, blk = i >> 4;
-        float front[2] = {0.f, 0.f}, back[2] = {0.f, 0.f};
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float x = B[m * DK + c + e];
-                if (m < blk) front[e] += x;
-                if (m > blk) back[e] += x;
-            }
-        const float f0 = expf(front[0]), f1 = expf(front[1]);
-        const size_t at = vec + (size_t)i * DK + c;
-        put_planes(a.qt + at, kChunk * DK, qs[i * VS + c] * f0, qs[i * VS + c + 1] * f1);
-        if (DELTA) put_planes(a.kt + at, kChunk * DK, ks[i * VS + c] * f0, ks[i * VS + c + 1] * f1);
-        float x = 0.f, y = 0.f;
-#pragma unroll
-        for (int pl = kPlanes - 1; pl >= 0; --pl) {
-            const uint32_t w2 = *reinterpret_cast<const uint32_t *>(smem + pl * kTile + i * DK * 2 + (((c >> 3) ^ (i & 7)) << 4) + (c & 7) * 2);
-            x += bf16_lo(w2), y += bf16_hi(w2);
+    if (mine) {
+        float2 front = make_float2(0.f, 0.f), back = front;
+        for (int m = 0; m < 4; ++m) {
+            const float2 x = *reinterpret_cast<const float2 *>(B + m * DK + c);
+            if (m < blk) front.x += x.x, front.y += x.y;
+            if (m > blk) back.x += x.x, back.y += x.y;
         }
-        put_planes(a.kh + at, kChunk * DK, x * expf(back[0]), y * expf(back[1]));
+        front = make_float2(decay_exp(front.x), decay_exp(front.y)), back = make_float2(decay_exp(back.x), decay_exp(back.y));
+        const size_t at = unit * kPlanes * kChunk * DK + (size_t)blk * kBlock * DK + c;
+#pragma unroll
+        for (int r = 0; r < kBlock; ++r) {
+            const int own = (blk * kBlock + r) * VS + c;
+            float2 x = *reinterpret_cast<const float2 *>(qs + own);
+            put_planes(a.qt + at + r * DK, kChunk * DK, x.x * front.x, x.y * front.y);
+            if (DELTA) {
+                x = *reinterpret_cast<const float2 *>(ks + own);
+                put_planes(a.kt + at + r * DK, kChunk * DK, x.x * front.x, x.y * front.y);
+            }
+            x = *reinterpret_cast<const float2 *>(kc + own);
+            put_planes(a.kh + at + r * DK, kChunk * DK, x.x * back.x, x.y * back.y);
+        }
+        const float2 b = *reinterpret_cast<const float2 *>(B + blk * DK + c);
+        *reinterpret_cast<float2 *>(F + blk * DK + c) = make_float2(expf(-b.x), expf(-b.y));
+        if (blk == 1 || blk == 2) *reinterpret_cast<float2 *>(F + (3 + blk) * DK + c) = make_float2(decay_exp(b.x), decay_exp(b.y));
+        if (blk == 1) {
+            const float2 x = *reinterpret_cast<const float2 *>(B + 2 * DK + c);
+            *reinterpret_cast<float2 *>(F + 6 * DK + c) = make_float2(decay_exp(b.x + x.x), decay_exp(b.y + x.y));
+        }
     }
+    __syncthreads();
     if (tid < DK) a.decay[unit * DK + tid] = expf(B[tid] + B[DK + tid] + B[2 * DK + tid] + B[3 * DK + tid]);
     // block pairs (I, J <= I) of A and L, 16 x 16 each, one warp per pair and matrix
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
     const int g = lane >> 2, t = lane & 3;
-    constexpr int kMats = DELTA ? 2 : 1;
-    for (int task = warp; task < 16 * kMats; task += 8) {
-        const int which = task >> 4, I = (task >> 2) & 3, J = task & 3;
-        float acc[2][4] = {};
-        if (J < I || (J == I && !deep[I])) {
+    constexpr int kTasks = DELTA ? 20 : 10, kRounds = (kTasks + 7) / 8;
+    float acc[kRounds][2][4] = {};
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round) {
+        const int task = warp + 8 * round;
+        if (task >= kTasks) break;
+        const bool which = task >= 10;  // L
+        const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
+        if (J < I || !deep[I]) {
             const float *src = which ? ks : qs;
+            const float *f = J == I ? F + I * DK : I - J == 3 ? F + 6 * DK : F + (3 + J + 1) * DK;  // (not read for I = J + 1)
 #pragma unroll 2
             for (int k0 = 0; k0 < DK; k0 += 16) {
-                float f[4];  // channels k0 + 2t + {0, 1, 8, 9}
+                uint32_t x[kPlanes][4], b[kPlanes][4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int c = k0 + 2 * t + (e & 1) + 8 * (e >> 1);
-                    float x = 0.f;
-                    if (J == I) x = -B[I * DK + c];
-                    else
-                        for (int m = J + 1; m < I; ++m) x += B[m * DK + c];
-                    f[e] = expf(x);
+                    const int k = k0 + 2 * t + 8 * (e >> 1);
+                    float2 y = *reinterpret_cast<const float2 *>(src + (I * kBlock + g + 8 * (e & 1)) * VS + k);
+                    if (I != J + 1) {
+                        const float2 w = *reinterpret_cast<const float2 *>(f + k);
+                        y.x *= w.x, y.y *= w.y;
+                    }
+                    frag_pair(x, e, y.x, y.y);
                 }
-                uint32_t x[kPlanes][4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = I * kBlock + g + 8 * (e & 1), c = k0 + 2 * t + 8 * (e >> 1);
-                    const float2 y = *reinterpret_cast<const float2 *>(src + row * VS + c);
-                    uint32_t w[kPlanes];
-                    split_pair<kPlanes>(y.x * f[2 * (e >> 1)], y.y * f[2 * (e >> 1) + 1], w);
-#pragma unroll
-                    for (int pl = 0; pl < kPlanes; ++pl) x[pl][e] = w[pl];
-                }
-#pragma unroll
-                for (int pl = 0; pl < kPlanes; ++pl) {
-                    uint32_t b[4];
-                    load_b(b, kc_s + pl * kTile, DK, J * kBlock, k0, lane);
-                    mma_planes<kPlanes, kPlanes>(acc[0], acc[1], x, b, pl);
-                }
+                frag_b(b, kc, VS, J * kBlock, k0, lane);
+                mma_all(acc[round][0], acc[round][1], x, b);
             }
-        } else if (J == I) {
+        } else {
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -388,37 +414,57 @@ __global__ void __launch_bounds__(256) scan_prep_vector_kernel(const ScanArgs a)
                     if (j <= i) {
                         float sq, sk;
                         pair_sums<IO, EXCL>(a, p, h, hq, DK, i, j, sq, sk);
-                        acc[n][e] = which ? sk : sq * a.scale;
+                        acc[round][n][e] = which ? sk : sq * a.scale;
                     }
                 }
         }
+    }
+    if (DELTA) __syncthreads();  // the vectors make room for N
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round) {
+        const int task = warp + 8 * round;
+        if (task >= kTasks) break;
+        const bool which = task >= 10;
+        const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int i = I * kBlock + g + 8 * half, j = J * kBlock + n * 8 + 2 * t;
-                float x[2];
+                const int last = which || EXCL ? i - 1 : i;  // A: j <= i (RWKV6: j < i), L: j < i
+                const float x = j <= last ? acc[round][n][2 * half] : 0.f, y = j + 1 <= last ? acc[round][n][2 * half + 1] : 0.f;
+                if (which) *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(beta[i] * x, beta[i] * y);
+                else put_planes(A + i * kChunk + j, kChunk * kChunk, x, y);
+            }
+    }
+    if (EXCL) {
+        // the diagonal's bonus term q . (bonus * k), four threads per token
+        __syncthreads();  // (the zeros above are in place)
+        const int i = tid >> 2;
+        float s = 0.f;
+        if (i < p.valid) {
+            const size_t r = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK;
+#pragma unroll 4
+            for (int d = (tid & 3) * 2; d < DK; d += 8) {
+                float x[2], y[2];
+                load_vec<IO, 2>(static_cast<const IO *>(a.q) + r + d, x);
+                load_vec<IO, 2>(static_cast<const IO *>(a.k) + r + d, y);
+                s = fmaf(x[0] * y[0], a.bonus[h * DK + d], s), s = fmaf(x[1] * y[1], a.bonus[h * DK + d + 1], s);
+            }
+        }
+        s += __shfl_xor_sync(0xffffffffu, s, 1);
+        s += __shfl_xor_sync(0xffffffffu, s, 2);
+        if ((tid & 3) == 0)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const bool in = which || EXCL ? j + e < i : j + e <= i;
-                    x[e] = in ? acc[n][2 * half + e] : 0.f;
-                    if (which) N[i * kInvStride + j + e] = in ? beta[i] * x[e] : 0.f;
-                }
-                if (!which) {
-                    if (EXCL && (i == j || i == j + 1) && i < p.valid) {  // the bonus term q . (bonus * k)
-                        float s = 0.f;
-                        const size_t r = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK;
-                        for (int c = 0; c < DK; ++c)
-                            s = fmaf(to_f32(static_cast<const IO *>(a.q)[r + c]) * to_f32(static_cast<const IO *>(a.k)[r + c]), a.bonus[h * DK + c], s);
-                        x[i - j] = s;
-                    }
-                    put_planes(A + i * kChunk + j, kChunk * kChunk, x[0], x[1]);
-                }
+            for (int pl = 0; pl < kPlanes; ++pl) {
+                const __nv_bfloat16 w = __float2bfloat16_rn(s);
+                A[pl * kChunk * kChunk + i * kChunk + i] = w;
+                s -= __bfloat162float(w);
             }
     }
     if (DELTA) {
         __syncthreads();
-        invert_unit_lower(N, T, X, tid, 256);
+        invert_unit_lower(N, T, tid);
         write_inverse(T, beta, a.T + unit * kPlanes * kChunk * kChunk, tid, 256);
     }
 }
