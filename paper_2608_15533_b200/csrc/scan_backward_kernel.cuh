@@ -114,12 +114,13 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
             uint32_t f[kPlanes][4];
             acc_to_a<kPlanes>(s[2 * kk], s[2 * kk + 1], f);
 #pragma unroll
-            for (int nn = 0; nn < 4; ++nn)
+            for (int nn = 0; nn < 4; nn += 2)
 #pragma unroll
                 for (int pl = 0; pl < L::kVecs; ++pl) {
-                    uint32_t b[4];
+                    uint32_t b[4], e[4];
                     load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                    mma_planes<kPlanes, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
+                    load_b(e, k_s + pl * L::kTile, DK, nn * 16 + 16, kk * 16, lane);
+                    mma_planes2<kPlanes, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
                 }
         }
         if (!VEC) {
@@ -142,28 +143,35 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
             uint32_t f[OP1][4];
             acc_to_a<OP1>(x[0], x[1], f);
 #pragma unroll
-            for (int nn = 0; nn <= kb; ++nn)
+            for (int pl = 0; pl < kPlanes; ++pl) {
+                uint32_t b[4], e[4];
 #pragma unroll
-                for (int pl = 0; pl < kPlanes; ++pl) {
-                    uint32_t b[4];
+                for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
                     load_b_t(b, sm + L::A + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
-                    mma_planes<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
+                    if (nn < kb) load_b_t(e, sm + L::A + pl * L::kMat, kChunk, kb * 16, nn * 16 + 16, lane);
+                    if (nn < kb) mma_planes2<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
+                    else mma_planes<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
                 }
+            }
         }
         // dV^T = dU^T T
         if (DELTA) {
             float w[8][4] = {};
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
-                uint32_t f[kPlanes][4], b[4];
+                uint32_t f[kPlanes][4];
                 acc_to_a<kPlanes>(du[2 * kb], du[2 * kb + 1], f);
 #pragma unroll
-                for (int nn = 0; nn <= kb; ++nn)
+                for (int pl = 0; pl < kPlanes; ++pl) {
+                    uint32_t b[4], e[4];
 #pragma unroll
-                    for (int pl = 0; pl < kPlanes; ++pl) {
+                    for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
                         load_b_t(b, sm + L::T + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], f, b, pl);
+                        if (nn < kb) load_b_t(e, sm + L::T + pl * L::kMat, kChunk, kb * 16, nn * 16 + 16, lane);
+                        if (nn < kb) mma_planes2<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], w[2 * nn + 2], w[2 * nn + 3], f, b, e, pl);
+                        else mma_planes<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], f, b, pl);
                     }
+                }
             }
 #pragma unroll
             for (int n = 0; n < 8; ++n)
@@ -206,12 +214,13 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
                 uint32_t f[OP2][4];
                 acc_to_a<OP2>(x[0], x[1], f);
 #pragma unroll
-                for (int nn = 0; nn < NT / 2; ++nn)
+                for (int nn = 0; nn < NT / 2; nn += 2)
 #pragma unroll
                     for (int pl = 0; pl < L::kVecs; ++pl) {
-                        uint32_t b[4];
+                        uint32_t b[4], e[4];
                         load_b_t(b, sm + L::q + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                        mma_planes<OP2, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                        load_b_t(e, sm + L::q + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                        mma_planes2<OP2, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                     }
             }
             if (DELTA) {
@@ -223,12 +232,13 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
                 acc_to_a<kPlanes>(x[0], x[1], f);
                 const uint32_t kt_s = VEC ? sm + L::kt : k_s;
 #pragma unroll
-                for (int nn = 0; nn < NT / 2; ++nn)
+                for (int nn = 0; nn < NT / 2; nn += 2)
 #pragma unroll
                     for (int pl = 0; pl < L::kVecs; ++pl) {
-                        uint32_t b[4];
+                        uint32_t b[4], e[4];
                         load_b_t(b, kt_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                        load_b_t(e, kt_s + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                        mma_planes2<kPlanes, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                     }
             }
         }

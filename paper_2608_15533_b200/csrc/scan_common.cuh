@@ -133,6 +133,16 @@ __device__ __forceinline__ void mma_planes(float (&c0)[4], float (&c1)[4], const
         if (pa + pb < LIMIT) mma(c0, a[pa], b[0], b[1]), mma(c1, a[pa], b[2], b[3]);
 }
 
+// The same for two n16 operands side by side, four accumulators in turn: a product waits 22 cycles
+// for the one before it into the same accumulator, and one is issued every eight.
+template <int PA, int LIMIT>
+__device__ __forceinline__ void mma_planes2(float (&c0)[4], float (&c1)[4], float (&d0)[4], float (&d1)[4], const uint32_t (&a)[PA][4],
+                                            const uint32_t (&b)[4], const uint32_t (&e)[4], int pb) {
+#pragma unroll
+    for (int pa = 0; pa < PA; ++pa)
+        if (pa + pb < LIMIT) mma(c0, a[pa], b[0], b[1]), mma(c1, a[pa], b[2], b[3]), mma(d0, a[pa], e[0], e[1]), mma(d1, a[pa], e[2], e[3]);
+}
+
 // ---- shared-memory tiles -----------------------------------------------------------------------------------
 // bf16 tiles, rows of `w` elements (64 or 128), the 16-byte units of a row permuted by the row's low three bits so
 // that eight rows at one unit fall into eight different bank groups.
@@ -181,7 +191,8 @@ __device__ __forceinline__ void frag_pair(uint32_t (&f)[N][4], int r, float x, f
     for (int p = 0; p < N; ++p) f[p][r] = w[p];
 }
 // Operand A (m16 x k16) of a tile [m][k] of rows of `w` floats (w = 8 mod 32: no bank conflicts) ...
-__device__ __forceinline__ void frag_a(uint32_t (&f)[kPlanes][4], const float *tile, int w, int m0, int k0, int lane) {
+template <int N>
+__device__ __forceinline__ void frag_a(uint32_t (&f)[N][4], const float *tile, int w, int m0, int k0, int lane) {
     const float *p = tile + (m0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -190,7 +201,8 @@ __device__ __forceinline__ void frag_a(uint32_t (&f)[kPlanes][4], const float *t
     }
 }
 // ... and of a tile [k][m].
-__device__ __forceinline__ void frag_a_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int m0, int lane) {
+template <int N>
+__device__ __forceinline__ void frag_a_t(uint32_t (&f)[N][4], const float *tile, int w, int k0, int m0, int lane) {
     const float *p = tile + (k0 + 2 * (lane & 3)) * w + m0 + (lane >> 2);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -199,7 +211,8 @@ __device__ __forceinline__ void frag_a_t(uint32_t (&f)[kPlanes][4], const float 
     }
 }
 // Operand B (k16 x n16) of a tile [n][k] ...
-__device__ __forceinline__ void frag_b(uint32_t (&f)[kPlanes][4], const float *tile, int w, int n0, int k0, int lane) {
+template <int N>
+__device__ __forceinline__ void frag_b(uint32_t (&f)[N][4], const float *tile, int w, int n0, int k0, int lane) {
     const float *p = tile + (n0 + (lane >> 2)) * w + k0 + 2 * (lane & 3);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -208,7 +221,8 @@ __device__ __forceinline__ void frag_b(uint32_t (&f)[kPlanes][4], const float *t
     }
 }
 // ... and of a tile [k][n] (w = 4 mod 16: no bank conflicts).
-__device__ __forceinline__ void frag_b_t(uint32_t (&f)[kPlanes][4], const float *tile, int w, int k0, int n0, int lane) {
+template <int N>
+__device__ __forceinline__ void frag_b_t(uint32_t (&f)[N][4], const float *tile, int w, int k0, int n0, int lane) {
     const float *p = tile + (k0 + 2 * (lane & 3)) * w + n0 + (lane >> 2);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -216,11 +230,11 @@ __device__ __forceinline__ void frag_b_t(uint32_t (&f)[kPlanes][4], const float 
         frag_pair(f, r, q[0], q[w]);
     }
 }
-// c0, c1 += a b over all plane products that count.
+// c0, c1 += a b over all plane products that count: index sums below the larger number of planes.
 template <int PA, int PB>
 __device__ __forceinline__ void mma_all(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][4]) {
 #pragma unroll
-    for (int pb = 0; pb < PB; ++pb) mma_planes<PA, kPlanes>(c0, c1, a, b[pb], pb);
+    for (int pb = 0; pb < PB; ++pb) mma_planes<PA, (PA > PB ? PA : PB)>(c0, c1, a, b[pb], pb);
 }
 
 // Asynchronous 16-byte copy that writes zeros when `ok` is false (the source is then not read).

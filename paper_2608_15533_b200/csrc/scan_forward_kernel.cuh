@@ -117,19 +117,22 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
             uint32_t f[kPlanes][4];
             acc_to_a<kPlanes>(s[2 * kk], s[2 * kk + 1], f);
 #pragma unroll
-            for (int nn = 0; nn < 4; ++nn) {
-                uint32_t b[4];
-                if (DELTA) {
+            for (int nn = 0; nn < 4; nn += DELTA ? 1 : 2) {
+                // delta rule: k and q in turn; otherwise two tiles of q
 #pragma unroll
-                    for (int pl = 0; pl < L::kK; ++pl) {
-                        load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(ak[2 * nn], ak[2 * nn + 1], f, b, pl);
+                for (int pl = 0; pl < kPlanes; ++pl) {
+                    uint32_t b[4], e[4];
+                    if (DELTA && pl < L::kK) load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
+                    if (pl < L::kQ) load_b(e, sm + L::q + pl * L::kTile, DK, nn * 16, kk * 16, lane);
+                    if (!DELTA && pl < L::kQ) load_b(b, sm + L::q + pl * L::kTile, DK, nn * 16 + 16, kk * 16, lane);
+#pragma unroll
+                    for (int pa = 0; pa + pl < kPlanes; ++pa) {
+                        if (DELTA && pl < L::kK) mma(ak[2 * nn], f[pa], b[0], b[1]), mma(ak[2 * nn + 1], f[pa], b[2], b[3]);
+                        if (pl < L::kQ && pa + pl < L::kOut) {
+                            mma(aq[2 * nn], f[pa], e[0], e[1]), mma(aq[2 * nn + 1], f[pa], e[2], e[3]);
+                            if (!DELTA) mma(aq[(2 * nn + 2) & 7], f[pa], b[0], b[1]), mma(aq[(2 * nn + 3) & 7], f[pa], b[2], b[3]);
+                        }
                     }
-                }
-#pragma unroll
-                for (int pl = 0; pl < L::kQ; ++pl) {
-                    load_b(b, sm + L::q + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                    mma_planes<kPlanes, L::kOut>(aq[2 * nn], aq[2 * nn + 1], f, b, pl);
                 }
             }
         }
@@ -167,12 +170,16 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
                 uint32_t f[kPlanes][4], b[4];
                 acc_to_a<kPlanes>(ak[2 * kb], ak[2 * kb + 1], f);
 #pragma unroll
-                for (int nn = kb; nn < 4; ++nn)
+                for (int pl = 0; pl < kPlanes; ++pl) {
+                    uint32_t e[4];
 #pragma unroll
-                    for (int pl = 0; pl < kPlanes; ++pl) {
-                        load_b(b, sm + L::T + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(u[2 * nn], u[2 * nn + 1], f, b, pl);
+                    for (int nn = kb & ~1; nn < 4; nn += 2) {  // the block pairs' first may lie above the diagonal
+                        if (nn >= kb) load_b(b, sm + L::T + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
+                        load_b(e, sm + L::T + pl * L::kMat, kChunk, nn * 16 + 16, kb * 16, lane);
+                        if (nn >= kb) mma_planes2<kPlanes, kPlanes>(u[2 * nn], u[2 * nn + 1], u[2 * nn + 2], u[2 * nn + 3], f, b, e, pl);
+                        else mma_planes<kPlanes, kPlanes>(u[2 * nn + 2], u[2 * nn + 3], f, e, pl);
                     }
+                }
             }
             if (a.keep) store_slice(a.U + unit * kChunk * a.dv + v0, a.dv, kChunk, u, 0u, lane);
         }
@@ -182,12 +189,16 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
             uint32_t f[UO][4], b[4];
             acc_to_a<UO>(u[2 * kb], u[2 * kb + 1], f);
 #pragma unroll
-            for (int nn = kb; nn < 4; ++nn)
+            for (int pl = 0; pl < L::kOut; ++pl) {
+                uint32_t e[4];
 #pragma unroll
-                for (int pl = 0; pl < L::kOut; ++pl) {
-                    load_b(b, sm + L::A + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
-                    mma_planes<UO, L::kOut>(aq[2 * nn], aq[2 * nn + 1], f, b, pl);
+                for (int nn = kb & ~1; nn < 4; nn += 2) {
+                    if (nn >= kb) load_b(b, sm + L::A + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
+                    load_b(e, sm + L::A + pl * L::kMat, kChunk, nn * 16 + 16, kb * 16, lane);
+                    if (nn >= kb) mma_planes2<UO, L::kOut>(aq[2 * nn], aq[2 * nn + 1], aq[2 * nn + 2], aq[2 * nn + 3], f, b, e, pl);
+                    else mma_planes<UO, L::kOut>(aq[2 * nn + 2], aq[2 * nn + 3], f, e, pl);
                 }
+            }
         }
         if (a.out)
             store_slice(static_cast<IO *>(a.out) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride, valid, aq, stage, lane);
@@ -226,12 +237,13 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
             uint32_t f[US][4];
             acc_to_a<US>(u[2 * kb], u[2 * kb + 1], f);
 #pragma unroll
-            for (int nn = 0; nn < NT / 2; ++nn)
+            for (int nn = 0; nn < NT / 2; nn += 2)
 #pragma unroll
                 for (int pl = 0; pl < L::kK; ++pl) {
-                    uint32_t b[4];
+                    uint32_t b[4], e[4];
                     load_b_t(b, ku_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                    mma_planes<US, kPlanes>(s[2 * nn], s[2 * nn + 1], f, b, pl);
+                    load_b_t(e, ku_s + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                    mma_planes2<US, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                 }
         }
         if (!L::kTwice) __syncthreads();

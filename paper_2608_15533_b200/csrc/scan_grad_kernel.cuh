@@ -16,6 +16,9 @@
 // The [64 x d_k] products contract over d_v, so S_0, dS_1, dO, U and dV stream through shared memory in slices of 32
 // columns of d_v, the next slice on its way while one is multiplied.  fp32 operands stay fp32 there (two bytes per element
 // less than three planes, and both orientations from one tile); a warp forms its fragments' planes as it reads them.
+// With bf16 io the products over d_v take fp32 operands in two planes: they end in dq, dk (bf16) and in sums that do not
+// cancel.  The products inside the chunk take three: dg is the difference of their sums, and two planes left 2e-5 of it
+// for per-channel gates.
 // 512 threads; warp w owns token rows 16 (w & 3) .. + 15 and the channel quarter w >> 2 of every result: the work between
 // two barriers is a few hundred instructions per warp, and sixteen warps cover each other's latencies where eight did not.
 #pragma once
@@ -110,7 +113,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
     using L = GradSmem<OP, P, DK, IO>;
     constexpr bool VEC = L::VEC, DELTA = L::DELTA, EXCL = OpTraits<OP>::kBonus;
     constexpr int NT = DK / 32, SW = L::kSW, MW = L::kMW;
-    constexpr int IP = sizeof(IO) == 4 ? kPlanes : 1;  // planes of dO and of v
+    constexpr int GP = sizeof(IO) == 4 ? kPlanes : 2;  // planes of an fp32 operand
+    constexpr int IP = sizeof(IO) == 4 ? GP : 1;       // and of dO and v
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
@@ -171,19 +175,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
 #pragma unroll
         for (int k0 = 0; k0 < kSlice; k0 += 16) {
             {
-                uint32_t f[IP][4], e[kPlanes][4];
+                uint32_t f[IP][4], e[GP][4];
                 io_frag_a(f, st + L::dO, mt * 16, k0, lane);
                 if (DELTA) frag_a(e, v_f, kSliceStride, mt * 16, k0, lane);
 #pragma unroll
                 for (int nn = 0; nn < NT / 2; ++nn) {
-                    uint32_t b[kPlanes][4];
+                    uint32_t b[GP][4];
                     frag_b_t(b, S, SW, k0, c0 + nn * 16, lane);
                     mma_all(dq[2 * nn], dq[2 * nn + 1], f, b);
                     if (DELTA) mma_all(dr[2 * nn], dr[2 * nn + 1], e, b);
                 }
                 if (cq <= mt) {
                     if constexpr (DELTA) {
-                        uint32_t b[kPlanes][4];
+                        uint32_t b[GP][4];
                         frag_b(b, u_f, kSliceStride, cq * 16, k0, lane);
                         mma_all(da[0], da[1], f, b);
                         mma_all(dl[0], dl[1], e, b);
@@ -194,13 +198,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
                     }
                 }
             }
-            constexpr int UP = DELTA ? kPlanes : IP;
+            constexpr int UP = DELTA ? GP : IP;
             uint32_t f[UP][4];
             if constexpr (DELTA) frag_a(f, u_f, kSliceStride, mt * 16, k0, lane);
             else io_frag_a(f, st + L::U, mt * 16, k0, lane);
 #pragma unroll
             for (int nn = 0; nn < NT / 2; ++nn) {
-                uint32_t b[kPlanes][4];
+                uint32_t b[GP][4];
                 frag_b_t(b, dS, SW, k0, c0 + nn * 16, lane);
                 mma_all(dw[2 * nn], dw[2 * nn + 1], f, b);
             }

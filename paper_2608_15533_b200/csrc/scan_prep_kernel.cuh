@@ -242,18 +242,18 @@ __device__ __forceinline__ void block_vectors(const ScanArgs &a, const ChunkPlac
     float2 gate[kBlock];
 #pragma unroll
     for (int r = 0; r < kBlock; ++r) {
-        const int i = blk * kBlock + r;
-        gate[r] = o.kc[r] = o.qs[r] = make_float2(0.f, 0.f);
-        if (i < p.valid) {
-            gate[r] = *reinterpret_cast<const float2 *>(a.g + ((size_t)(p.tok0 + i) * a.H + h) * DK + c);
-            const size_t at = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK + c;
-            float x[2];
-            load_vec<IO, 2>(static_cast<const IO *>(a.k) + at, x);
-            o.kc[r] = make_float2(x[0], x[1]);
-            load_vec<IO, 2>(static_cast<const IO *>(a.q) + at, x);
-            o.qs[r] = make_float2(x[0], x[1]);
-        }
+        // (rows behind the last token read it again and are cleared below: loads without branches go out together)
+        const size_t i = p.tok0 + min(blk * kBlock + r, p.valid - 1), at = (i * a.Hq + hq) * DK + c;
+        float x[2];
+        gate[r] = *reinterpret_cast<const float2 *>(a.g + (i * a.H + h) * DK + c);
+        load_vec<IO, 2>(static_cast<const IO *>(a.k) + at, x);
+        o.kc[r] = make_float2(x[0], x[1]);
+        load_vec<IO, 2>(static_cast<const IO *>(a.q) + at, x);
+        o.qs[r] = make_float2(x[0], x[1]);
     }
+#pragma unroll
+    for (int r = 0; r < kBlock; ++r)
+        if (blk * kBlock + r >= p.valid) gate[r] = o.kc[r] = o.qs[r] = make_float2(0.f, 0.f);
     float2 s = make_float2(0.f, 0.f), e = make_float2(1.f, 1.f);
 #pragma unroll
     for (int r = 0; r < kBlock; ++r) {
@@ -300,9 +300,9 @@ __device__ __forceinline__ void pair_sums(const ScanArgs &a, const ChunkPlace &p
     }
 }
 
-// OP selects the readout (RWKV6) and the delta rule; 256 threads.
+// OP selects the readout (RWKV6) and the delta rule; one thread per block and channel pair, so 256 or 128.
 template <int OP, int DK, typename IO>
-__global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(const ScanArgs a) {
     constexpr bool DELTA = OpTraits<OP>::kDeltaRule, EXCL = OpTraits<OP>::kBonus;
     using L = PrepVectorSmem<DK>;
     constexpr int VS = L::kVS;
@@ -319,17 +319,13 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
     int *deep = reinterpret_cast<int *>(beta + kChunk);             // [4] blocks that decay too far for the factored form
     float *T = reinterpret_cast<float *>(smem), *N = T + kChunk * kInvStride;
     if (tid < 4) deep[tid] = 0;
-    if (DELTA && tid >= 64 && tid < 128) {
-        const int i = tid - 64;
-        beta[i] = scan_beta(i < p.valid ? a.beta[(size_t)(p.tok0 + i) * a.H + h] : 0.f);
-    }
+    if (DELTA && tid < kChunk) beta[tid] = scan_beta(tid < p.valid ? a.beta[(size_t)(p.tok0 + tid) * a.H + h] : 0.f);
     __syncthreads();
     // a thread's block and channel pair: the block's vectors into shared memory, then, with the other blocks' decays at hand,
     // the whole chunk's to the chain kernels
-    constexpr int kPairs = DK / 2;
+    constexpr int kPairs = DK / 2, kThreads = 4 * kPairs, kWarps = kThreads / 32;
     const int blk = tid / kPairs, c = (tid % kPairs) * 2;
-    const bool mine = tid < 4 * kPairs;
-    if (mine) {
+    {
         BlockVectors o;
         block_vectors<IO, EXCL, DELTA>(a, p, h, hq, DK, blk, c, o);
         *reinterpret_cast<float2 *>(B + blk * DK + c) = o.B;
@@ -344,7 +340,7 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
         }
     }
     __syncthreads();
-    if (mine) {
+    {
         float2 front = make_float2(0.f, 0.f), back = front;
         for (int m = 0; m < 4; ++m) {
             const float2 x = *reinterpret_cast<const float2 *>(B + m * DK + c);
@@ -378,11 +374,11 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
     // block pairs (I, J <= I) of A and L, 16 x 16 each, one warp per pair and matrix
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
     const int g = lane >> 2, t = lane & 3;
-    constexpr int kTasks = DELTA ? 20 : 10, kRounds = (kTasks + 7) / 8;
+    constexpr int kTasks = DELTA ? 20 : 10, kRounds = (kTasks + kWarps - 1) / kWarps;
     float acc[kRounds][2][4] = {};
 #pragma unroll
     for (int round = 0; round < kRounds; ++round) {
-        const int task = warp + 8 * round;
+        const int task = warp + kWarps * round;
         if (task >= kTasks) break;
         const bool which = task >= 10;  // L
         const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
@@ -422,7 +418,7 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
     if (DELTA) __syncthreads();  // the vectors make room for N
 #pragma unroll
     for (int round = 0; round < kRounds; ++round) {
-        const int task = warp + 8 * round;
+        const int task = warp + kWarps * round;
         if (task >= kTasks) break;
         const bool which = task >= 10;
         const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
@@ -438,23 +434,24 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
             }
     }
     if (EXCL) {
-        // the diagonal's bonus term q . (bonus * k), four threads per token
+        // the diagonal's bonus term q . (bonus * k), `kEach` threads per token
+        constexpr int kEach = kThreads / kChunk;
         __syncthreads();  // (the zeros above are in place)
-        const int i = tid >> 2;
+        const int i = tid / kEach;
         float s = 0.f;
         if (i < p.valid) {
             const size_t r = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK;
 #pragma unroll 4
-            for (int d = (tid & 3) * 2; d < DK; d += 8) {
+            for (int d = (tid % kEach) * 2; d < DK; d += 2 * kEach) {
                 float x[2], y[2];
                 load_vec<IO, 2>(static_cast<const IO *>(a.q) + r + d, x);
                 load_vec<IO, 2>(static_cast<const IO *>(a.k) + r + d, y);
                 s = fmaf(x[0] * y[0], a.bonus[h * DK + d], s), s = fmaf(x[1] * y[1], a.bonus[h * DK + d + 1], s);
             }
         }
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        s += __shfl_xor_sync(0xffffffffu, s, 2);
-        if ((tid & 3) == 0)
+#pragma unroll
+        for (int o = 1; o < kEach; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (tid % kEach == 0)
 #pragma unroll
             for (int pl = 0; pl < kPlanes; ++pl) {
                 const __nv_bfloat16 w = __float2bfloat16_rn(s);
@@ -465,7 +462,7 @@ __global__ void __launch_bounds__(256, 2) scan_prep_vector_kernel(const ScanArgs
     if (DELTA) {
         __syncthreads();
         invert_unit_lower(N, T, tid);
-        write_inverse(T, beta, a.T + unit * kPlanes * kChunk * kChunk, tid, 256);
+        write_inverse(T, beta, a.T + unit * kPlanes * kChunk * kChunk, tid, kThreads);
     }
 }
 
