@@ -332,6 +332,8 @@ typedef struct {
     int32_t *append_slots; /* [n] slot of the rows that go through deltalog_decode_step, -1 for the others; or NULL */
     int32_t *merge_slots;  /* [n] the same for deltalog_decode_merge_step; or NULL                                */
     int32_t *totals;       /* [4] tokens, chunks, rows in scan_slots' sense, rows that decode                     */
+    int32_t *status;       /* one word of DELTALOG_STATUS_* bits from deltalog_scan_forward / _backward, or NULL;
+                              the library only sets bits                                                        */
 } deltalog_plan;
 
 /*

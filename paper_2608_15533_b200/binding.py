@@ -63,7 +63,7 @@ class _Lane(ctypes.Structure):
 
 class _Plan(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("max_tokens", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in (
-        "starts", "chunk_starts", "chunk_seq", "token_seq", "scan_slots", "append_slots", "merge_slots", "totals")]
+        "starts", "chunk_starts", "chunk_seq", "token_seq", "scan_slots", "append_slots", "merge_slots", "totals", "status")]
 
 
 class _ScanGrads(ctypes.Structure):

@@ -23,7 +23,7 @@ ScanArgs scan_args(const deltalog_desc *d, const deltalog_plan *plan, const void
                    const float *u_bonus, void *workspace, const ScanLayout &l) {
     ScanArgs a = {};
     a.starts = plan->starts, a.chunk_starts = plan->chunk_starts, a.chunk_seq = plan->chunk_seq;
-    a.n = plan->n, a.max_chunks = scan_max_chunks(plan->n, plan->max_tokens), a.num_slots = d->num_slots;
+    a.n = plan->n, a.max_chunks = scan_max_chunks(plan->n, plan->max_tokens), a.num_slots = d->num_slots, a.status = plan->status;
     a.H = d->H, a.Hq = d->H_qk > 0 ? d->H_qk : d->H, a.dv = d->d_v;
     a.scale = d->op == DELTALOG_RWKV6 ? 1.f : d->scale;
     a.q = q, a.k = k, a.v = v;
@@ -34,21 +34,12 @@ ScanArgs scan_args(const deltalog_desc *d, const deltalog_plan *plan, const void
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
     a.U = floats(l.U), a.S = floats(l.S), a.dV = floats(l.dV), a.dS = floats(l.dS), a.decay = floats(l.decay);
     a.dq_part = floats(l.dq_part), a.dk_part = floats(l.dk_part), a.dbonus_part = floats(l.dbonus_part);
-    if (d->io_dtype == DELTALOG_F32) {
-        a.qp = plane(l.qp), a.kp = plane(l.kp);
-        a.q_plane = (size_t)plan->max_tokens * a.Hq * d->d_k;
-    } else {
-        a.qp = static_cast<const __nv_bfloat16 *>(q), a.kp = static_cast<const __nv_bfloat16 *>(k);
-    }
+    a.qi = plane(l.qi), a.ki = plane(l.ki);
     return a;
 }
 
-// fp32 inputs as planes, the chunks' matrices, the chain.
+// The chunks' matrices and operands, then the chain.
 int run_forward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s) {
-    if (d->io_dtype == DELTALOG_F32 && !op_vec_decay(d->op)) {
-        if (int rc = launch_scan_split(static_cast<const float *>(a.q), const_cast<__nv_bfloat16 *>(a.qp), a.q_plane, s)) return rc;
-        if (int rc = launch_scan_split(static_cast<const float *>(a.k), const_cast<__nv_bfloat16 *>(a.kp), a.q_plane, s)) return rc;
-    }
     if (int rc = launch_scan_prep(d, a, s)) return rc;
     return launch_scan_forward(d, a, s);
 }

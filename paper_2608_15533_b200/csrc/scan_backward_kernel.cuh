@@ -49,35 +49,32 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
     const size_t v_stride = (size_t)a.H * a.dv;
     const uint32_t o_s = sm + L::slices + warp * L::per_warp, stage = o_s + kChunk * 32;
 
-    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl)
-            load_tile(dst + pl * L::kTile, src + pl * a.q_plane + ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, (size_t)a.Hq * DK, kChunk, DK,
-                      min(kChunk, len - c * kChunk), tid, nthreads);
+    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {  // q or k of a chunk
+        load_image(dst, src + ((size_t)(chunk0 + c) * a.Hq + hq) * P * kChunk * DK, P * L::kTile, tid, nthreads);
     };
-    auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, size_t unit) {
-        load_tile(dst, src + unit * kPlanes * kChunk * DK, DK, kPlanes * kChunk, DK, kPlanes * kChunk, tid, nthreads);
+    auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, int planes, size_t unit) {
+        load_image(dst, src + unit * kPlanes * kChunk * DK, planes * L::kTile, tid, nthreads);
     };
     auto load_first = [&](int c) {  // k for dU, decay factors
         const size_t unit = (size_t)(chunk0 + c) * a.H + h;
-        if (VEC) load_decayed(sm + L::kh, a.kh, unit);
-        else if (L::kTwice) load_raw(sm + L::kh + (c & 1) * L::kTile, a.kp, c);
+        if (VEC) load_decayed(sm + L::kh, a.kh, kPlanes, unit);
+        else if (L::kTwice) load_raw(sm + L::kh + (c & 1) * L::kTile, a.ki, c);
         for (int i = tid; i < L::kDecay / 16; i += nthreads)
             cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
     };
     auto load_matrices = [&](int c) {
         const size_t at = ((size_t)(chunk0 + c) * a.H + h) * kPlanes * kChunk * kChunk;
-        load_tile(sm + L::A, a.A + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
-        if (DELTA) load_tile(sm + L::T, a.T + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
+        load_image(sm + L::A, a.A + at, kPlanes * L::kMat, tid, nthreads);
+        if (DELTA) load_image(sm + L::T, a.T + at, kPlanes * L::kMat, tid, nthreads);
     };
     auto load_update = [&](int c) {  // q, k for dS, and dO
         const size_t unit = (size_t)(chunk0 + c) * a.H + h;
         if (VEC) {
-            load_decayed(sm + L::q, a.qt, unit);
-            if (DELTA) load_decayed(sm + L::kt, a.kt, unit);
+            load_decayed(sm + L::q, a.qt, kPlanes, unit);
+            if (DELTA) load_decayed(sm + L::kt, a.kt, kPlanes, unit);
         } else {
-            load_raw(sm + L::q, a.qp, c);
-            if (!L::kTwice) load_raw(sm + L::kh, a.kp, c);
+            load_raw(sm + L::q, a.qi, c);
+            if (!L::kTwice) load_raw(sm + L::kh, a.ki, c);
         }
         if constexpr (!F32IO)
             load_slice(o_s, static_cast<const IO *>(a.dout) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride,
@@ -118,8 +115,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
 #pragma unroll
                 for (int pl = 0; pl < L::kVecs; ++pl) {
                     uint32_t b[4], e[4];
-                    load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                    load_b(e, k_s + pl * L::kTile, DK, nn * 16 + 16, kk * 16, lane);
+                    load_b(b, k_s + pl * L::kTile, nn * 16, kk * 16, lane);
+                    load_b(e, k_s + pl * L::kTile, nn * 16 + 16, kk * 16, lane);
                     mma_planes2<kPlanes, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
                 }
         }
@@ -147,8 +144,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
                 uint32_t b[4], e[4];
 #pragma unroll
                 for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
-                    load_b_t(b, sm + L::A + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
-                    if (nn < kb) load_b_t(e, sm + L::A + pl * L::kMat, kChunk, kb * 16, nn * 16 + 16, lane);
+                    load_b_t(b, sm + L::A + pl * L::kMat, kb * 16, nn * 16, lane);
+                    if (nn < kb) load_b_t(e, sm + L::A + pl * L::kMat, kb * 16, nn * 16 + 16, lane);
                     if (nn < kb) mma_planes2<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
                     else mma_planes<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
                 }
@@ -166,8 +163,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
                     uint32_t b[4], e[4];
 #pragma unroll
                     for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
-                        load_b_t(b, sm + L::T + pl * L::kMat, kChunk, kb * 16, nn * 16, lane);
-                        if (nn < kb) load_b_t(e, sm + L::T + pl * L::kMat, kChunk, kb * 16, nn * 16 + 16, lane);
+                        load_b_t(b, sm + L::T + pl * L::kMat, kb * 16, nn * 16, lane);
+                        if (nn < kb) load_b_t(e, sm + L::T + pl * L::kMat, kb * 16, nn * 16 + 16, lane);
                         if (nn < kb) mma_planes2<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], w[2 * nn + 2], w[2 * nn + 3], f, b, e, pl);
                         else mma_planes<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], f, b, pl);
                     }
@@ -218,8 +215,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
 #pragma unroll
                     for (int pl = 0; pl < L::kVecs; ++pl) {
                         uint32_t b[4], e[4];
-                        load_b_t(b, sm + L::q + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                        load_b_t(e, sm + L::q + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                        load_b_t(b, sm + L::q + pl * L::kTile, kb * 16, nn * 16, lane);
+                        load_b_t(e, sm + L::q + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
                         mma_planes2<OP2, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                     }
             }
@@ -236,8 +233,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
 #pragma unroll
                     for (int pl = 0; pl < L::kVecs; ++pl) {
                         uint32_t b[4], e[4];
-                        load_b_t(b, kt_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                        load_b_t(e, kt_s + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                        load_b_t(b, kt_s + pl * L::kTile, kb * 16, nn * 16, lane);
+                        load_b_t(e, kt_s + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
                         mma_planes2<kPlanes, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                     }
             }

@@ -11,10 +11,10 @@
 // chunk to the first, scan_grad_kernel forms the gradients of q, k, g and beta chunk by chunk in parallel.
 //
 // Precision: a bf16 value enters the tensor cores exactly.  An fp32 operand enters as three bf16 planes x = x0 + x1 + x2
-// (to 2^-26 of its size), and of a product of two such operands the six plane products with i + j <= 2 are summed in
-// fp32 accumulators, so a product is as good as one in fp32.  Two planes (three products) leave 2^-18 per operand: the
+// (all 24 bits), and of a product of two such operands the six plane products with i + j <= 2 are summed in
+// fp32 accumulators, so a product is as good as one in fp32.  Two planes (three products) leave 2^-16 to 2^-18 per operand: the
 // states and gate gradients then came out 3e-6 to 4e-5 off, against 5e-8 to 3e-7 of an fp32 computation.  Results that are
-// rounded to bf16 and feed nothing else take two planes: 2^-18 vanishes beside their own 2^-9.
+// rounded to bf16 and feed nothing else take two planes: 2^-16 vanishes beside their own 2^-9.
 #pragma once
 
 #include "common.cuh"
@@ -37,13 +37,11 @@ struct ScanArgs {
     const void *q, *k, *v;  // io dtype
     const float *g, *beta, *bonus;
     const void *dout;
-    // scalar decay: q and k as bf16 planes, `q_plane` elements apart (bf16 io: the tensors themselves, one plane)
-    const __nv_bfloat16 *qp, *kp;
-    size_t q_plane;
     // workspace, unit = chunk * H + head
-    __nv_bfloat16 *A, *T;        // [unit][3][64][64]
+    __nv_bfloat16 *qi, *ki;      // scalar decay: images of q and k [chunk * Hq + head][planes][64][d_k] (bf16 io: one plane)
+    __nv_bfloat16 *A, *T;        // images [unit][3][64][64]
     float *decay;                // scalar decay: [unit][2][64] e^(G_i), e^(G_end - G_i); per channel: [unit][d_k] e^(G_end)
-    __nv_bfloat16 *qt, *kt, *kh; // per-channel decay: [unit][3][64][d_k]
+    __nv_bfloat16 *qt, *kt, *kh; // per-channel decay: images [unit][3][64][d_k]
     float *U, *dV;               // [unit][64][d_v]
     float *S, *dS;               // [unit][d_v][d_k], state in front of the chunk / gradient behind it (transposed)
     // states
@@ -82,13 +80,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo_elem, float hi_elem) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// x, y -> their packed planes 0 .. N-1, each the bf16 rounding of what the planes in front of it leave.
+// x, y -> their packed planes 0 .. N-1: each takes the leading eight bits of what the planes in front of it leave, so three
+// planes hold all 24 bits.  (Cut, not rounded: one byte permutation instead of a conversion, and nothing overflows.)
 template <int N>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&w)[N]) {
+    float2 r = make_float2(x, y);
 #pragma unroll
     for (int p = 0; p < N; ++p) {
-        w[p] = pack_bf16(x, y);
-        if (p + 1 < N) x -= bf16_lo(w[p]), y -= bf16_hi(w[p]);
+        w[p] = __byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x7632);
+        if (p + 1 < N)
+            r = __ffma2_rn(make_float2(__uint_as_float(__float_as_uint(r.x) & 0xffff0000u), __uint_as_float(__float_as_uint(r.y) & 0xffff0000u)),
+                           make_float2(-1.f, -1.f), r);
     }
 }
 
@@ -144,35 +146,40 @@ __device__ __forceinline__ void mma_planes2(float (&c0)[4], float (&c1)[4], floa
 }
 
 // ---- shared-memory tiles -----------------------------------------------------------------------------------
-// bf16 tiles, rows of `w` elements (64 or 128), the 16-byte units of a row permuted by the row's low three bits so
-// that eight rows at one unit fall into eight different bank groups.
-__device__ __forceinline__ uint32_t tile_addr(uint32_t base, int w, int row, int unit) {
-    return base + (uint32_t)(row * w * 2 + ((unit ^ (row & 7)) << 4));
+// A bf16 tile of `kChunk` rows (w = 64 or 128 columns): 64 columns at a time, rows of 128 bytes, the 16-byte units of a
+// row permuted by the row's low three bits.  Eight rows at one unit fall into eight different bank groups, and it is the
+// 128-byte swizzle of the tensor cores' descriptors.  The workspace holds tiles in this very form ("images"), so a
+// chain kernel's load is a plain copy.
+__device__ __forceinline__ uint32_t tile_offset(int row, int unit) {
+    return (uint32_t)(((unit >> 3) * kChunk + row) * 128 + (((unit & 7) ^ (row & 7)) << 4));
 }
+__device__ __forceinline__ uint32_t tile_addr(uint32_t base, int row, int unit) { return base + tile_offset(row, unit); }
+// Place of element (row, column c) of an image, in elements.
+__device__ __forceinline__ int image_at(int row, int c) { return (int)(tile_offset(row, c >> 3) >> 1) + (c & 7); }
 // The same for the per-warp slices of 16 columns (32-byte rows).
 __device__ __forceinline__ uint32_t slice_addr(uint32_t base, int row, int unit) {
     return base + (uint32_t)(row * 32 + ((unit ^ ((row >> 2) & 1)) << 4));
 }
 
 // Operand B (k16 x n16, two n8 tiles: r[0..1], r[2..3]) of a tile stored [n][k] ...
-__device__ __forceinline__ void load_b(uint32_t (&r)[4], uint32_t base, int w, int n0, int k0, int lane) {
+__device__ __forceinline__ void load_b(uint32_t (&r)[4], uint32_t base, int n0, int k0, int lane) {
     const int m = lane >> 3, x = lane & 7;
-    ldsm4(r, tile_addr(base, w, n0 + (m >> 1) * 8 + x, (k0 >> 3) + (m & 1)));
+    ldsm4(r, tile_addr(base, n0 + (m >> 1) * 8 + x, (k0 >> 3) + (m & 1)));
 }
 // ... and of a tile stored [k][n].
-__device__ __forceinline__ void load_b_t(uint32_t (&r)[4], uint32_t base, int w, int k0, int n0, int lane) {
+__device__ __forceinline__ void load_b_t(uint32_t (&r)[4], uint32_t base, int k0, int n0, int lane) {
     const int m = lane >> 3, x = lane & 7;
-    ldsm4_t(r, tile_addr(base, w, k0 + (m & 1) * 8 + x, (n0 >> 3) + (m >> 1)));
+    ldsm4_t(r, tile_addr(base, k0 + (m & 1) * 8 + x, (n0 >> 3) + (m >> 1)));
 }
 // Operand A (m16 x k16) of a tile stored [m][k] ...
-__device__ __forceinline__ void load_a(uint32_t (&r)[4], uint32_t base, int w, int m0, int k0, int lane) {
+__device__ __forceinline__ void load_a(uint32_t (&r)[4], uint32_t base, int m0, int k0, int lane) {
     const int m = lane >> 3, x = lane & 7;
-    ldsm4(r, tile_addr(base, w, m0 + (m & 1) * 8 + x, (k0 >> 3) + (m >> 1)));
+    ldsm4(r, tile_addr(base, m0 + (m & 1) * 8 + x, (k0 >> 3) + (m >> 1)));
 }
 // ... and of a tile stored [k][m].
-__device__ __forceinline__ void load_a_t(uint32_t (&r)[4], uint32_t base, int w, int k0, int m0, int lane) {
+__device__ __forceinline__ void load_a_t(uint32_t (&r)[4], uint32_t base, int k0, int m0, int lane) {
     const int m = lane >> 3, x = lane & 7;
-    ldsm4_t(r, tile_addr(base, w, k0 + (m >> 1) * 8 + x, (m0 >> 3) + (m & 1)));
+    ldsm4_t(r, tile_addr(base, k0 + (m >> 1) * 8 + x, (m0 >> 3) + (m & 1)));
 }
 // Operand A of a 16-column slice stored [token k][16]; read as accumulator tiles it is the slice's transpose:
 // r[0] row lane/4 tokens k0..7, r[1] row lane/4 + 8, r[2], r[3] the same for tokens k0 + 8..15.
@@ -246,14 +253,20 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
     asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
 }
-// `rows` x w tile of rows `stride` elements apart; rows at and behind `valid` become zeros.
-__device__ __forceinline__ void load_tile(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int rows, int w, int valid, int tid, int nthreads) {
-    const int upr = w >> 3, sh = w == 128 ? 4 : 3;
-    for (int i = tid; i < rows * upr; i += nthreads) {
-        const int row = i >> sh, unit = i & (upr - 1);
+// kChunk x w tile of rows `stride` elements apart; rows at and behind `valid` become zeros.
+template <int W>
+__device__ __forceinline__ void load_tile(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int valid, int tid, int nthreads) {
+    constexpr int kUnits = W / 8;
+    for (int i = tid; i < kChunk * kUnits; i += nthreads) {
+        const int row = i / kUnits, unit = i % kUnits;
         const bool ok = row < valid;
-        cp_async16_zfill(tile_addr(dst, w, row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
+        cp_async16_zfill(tile_addr(dst, row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
     }
+}
+// An image, `bytes` long.
+__device__ __forceinline__ void load_image(uint32_t dst, const void *src, int bytes, int tid, int nthreads) {
+    for (int i = tid * 16; i < bytes; i += nthreads * 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst + i), "l"(static_cast<const char *>(src) + i) : "memory");
 }
 // A warp's 64 x 16 slice of rows `stride` elements apart.
 __device__ __forceinline__ void load_slice(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int valid, int lane) {

@@ -55,13 +55,10 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
     const uint32_t v_s = sm + L::slices + warp * L::per_warp, stage = v_s + kChunk * 32;
 
     auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {  // q or k of a chunk
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl)
-            load_tile(dst + pl * L::kTile, src + pl * a.q_plane + ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, (size_t)a.Hq * DK, kChunk, DK,
-                      min(kChunk, len - c * kChunk), tid, nthreads);
+        load_image(dst, src + ((size_t)(chunk0 + c) * a.Hq + hq) * P * kChunk * DK, P * L::kTile, tid, nthreads);
     };
     auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, int planes, size_t unit) {
-        load_tile(dst, src + unit * kPlanes * kChunk * DK, DK, planes * kChunk, DK, planes * kChunk, tid, nthreads);
+        load_image(dst, src + unit * kPlanes * kChunk * DK, planes * L::kTile, tid, nthreads);
     };
     auto load_vectors = [&](int c) {  // operands of the products with S, and the decay factors
         const size_t unit = (size_t)(chunk0 + c) * a.H + h;
@@ -69,23 +66,23 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
             load_decayed(sm + L::q, a.qt, L::kQ, unit);
             if (DELTA) load_decayed(sm + L::k, a.kt, L::kK, unit);
         } else {
-            load_raw(sm + L::q, a.qp, c);
-            if (L::kTwice) load_raw(sm + L::k + (c & 1) * L::kTile, a.kp, c);
+            load_raw(sm + L::q, a.qi, c);
+            if (L::kTwice) load_raw(sm + L::k + (c & 1) * L::kTile, a.ki, c);
         }
         for (int i = tid; i < L::kDecay / 16; i += nthreads)
             cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
     };
     auto load_matrices = [&](int c) {
         const size_t unit = (size_t)(chunk0 + c) * a.H + h, at = unit * kPlanes * kChunk * kChunk;
-        load_tile(sm + L::A, a.A + at, kChunk, L::kOut * kChunk, kChunk, L::kOut * kChunk, tid, nthreads);
-        if (DELTA) load_tile(sm + L::T, a.T + at, kChunk, kPlanes * kChunk, kChunk, kPlanes * kChunk, tid, nthreads);
+        load_image(sm + L::A, a.A + at, L::kOut * L::kMat, tid, nthreads);
+        if (DELTA) load_image(sm + L::T, a.T + at, kPlanes * L::kMat, tid, nthreads);
         if constexpr (!F32IO)
             load_slice(v_s, static_cast<const IO *>(a.v) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride,
                        min(kChunk, len - c * kChunk), lane);
     };
     auto load_update = [&](int c) {
         if (VEC) load_decayed(sm + L::kh, a.kh, L::kK, (size_t)(chunk0 + c) * a.H + h);
-        else if (!L::kTwice) load_raw(sm + L::k, a.kp, c);
+        else if (!L::kTwice) load_raw(sm + L::k, a.ki, c);
     };
     if (nchunks > 0) {
         load_vectors(0), cp_async_commit();
@@ -122,9 +119,9 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
 #pragma unroll
                 for (int pl = 0; pl < kPlanes; ++pl) {
                     uint32_t b[4], e[4];
-                    if (DELTA && pl < L::kK) load_b(b, k_s + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                    if (pl < L::kQ) load_b(e, sm + L::q + pl * L::kTile, DK, nn * 16, kk * 16, lane);
-                    if (!DELTA && pl < L::kQ) load_b(b, sm + L::q + pl * L::kTile, DK, nn * 16 + 16, kk * 16, lane);
+                    if (DELTA && pl < L::kK) load_b(b, k_s + pl * L::kTile, nn * 16, kk * 16, lane);
+                    if (pl < L::kQ) load_b(e, sm + L::q + pl * L::kTile, nn * 16, kk * 16, lane);
+                    if (!DELTA && pl < L::kQ) load_b(b, sm + L::q + pl * L::kTile, nn * 16 + 16, kk * 16, lane);
 #pragma unroll
                     for (int pa = 0; pa + pl < kPlanes; ++pa) {
                         if (DELTA && pl < L::kK) mma(ak[2 * nn], f[pa], b[0], b[1]), mma(ak[2 * nn + 1], f[pa], b[2], b[3]);
@@ -174,8 +171,8 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
                     uint32_t e[4];
 #pragma unroll
                     for (int nn = kb & ~1; nn < 4; nn += 2) {  // the block pairs' first may lie above the diagonal
-                        if (nn >= kb) load_b(b, sm + L::T + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
-                        load_b(e, sm + L::T + pl * L::kMat, kChunk, nn * 16 + 16, kb * 16, lane);
+                        if (nn >= kb) load_b(b, sm + L::T + pl * L::kMat, nn * 16, kb * 16, lane);
+                        load_b(e, sm + L::T + pl * L::kMat, nn * 16 + 16, kb * 16, lane);
                         if (nn >= kb) mma_planes2<kPlanes, kPlanes>(u[2 * nn], u[2 * nn + 1], u[2 * nn + 2], u[2 * nn + 3], f, b, e, pl);
                         else mma_planes<kPlanes, kPlanes>(u[2 * nn + 2], u[2 * nn + 3], f, e, pl);
                     }
@@ -193,8 +190,8 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
                 uint32_t e[4];
 #pragma unroll
                 for (int nn = kb & ~1; nn < 4; nn += 2) {
-                    if (nn >= kb) load_b(b, sm + L::A + pl * L::kMat, kChunk, nn * 16, kb * 16, lane);
-                    load_b(e, sm + L::A + pl * L::kMat, kChunk, nn * 16 + 16, kb * 16, lane);
+                    if (nn >= kb) load_b(b, sm + L::A + pl * L::kMat, nn * 16, kb * 16, lane);
+                    load_b(e, sm + L::A + pl * L::kMat, nn * 16 + 16, kb * 16, lane);
                     if (nn >= kb) mma_planes2<UO, L::kOut>(aq[2 * nn], aq[2 * nn + 1], aq[2 * nn + 2], aq[2 * nn + 3], f, b, e, pl);
                     else mma_planes<UO, L::kOut>(aq[2 * nn + 2], aq[2 * nn + 3], f, e, pl);
                 }
@@ -241,8 +238,8 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
 #pragma unroll
                 for (int pl = 0; pl < L::kK; ++pl) {
                     uint32_t b[4], e[4];
-                    load_b_t(b, ku_s + pl * L::kTile, DK, kb * 16, nn * 16, lane);
-                    load_b_t(e, ku_s + pl * L::kTile, DK, kb * 16, nn * 16 + 16, lane);
+                    load_b_t(b, ku_s + pl * L::kTile, kb * 16, nn * 16, lane);
+                    load_b_t(e, ku_s + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
                     mma_planes2<US, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
                 }
         }

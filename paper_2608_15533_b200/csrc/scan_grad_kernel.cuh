@@ -145,12 +145,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         }
     };
     auto load_qk = [&]() {
-        const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK;
-#pragma unroll
-        for (int pl = 0; pl < P; ++pl) {
-            load_tile(sm + L::qk + pl * L::kTile, a.qp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, kGradThreads);
-            load_tile(sm + L::qk + (P + pl) * L::kTile, a.kp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, kGradThreads);
-        }
+        const size_t at = ((size_t)chunk * a.Hq + hq) * P * kChunk * DK;
+        load_image(sm + L::qk, a.qi + at, P * L::kTile, tid, kGradThreads);
+        load_image(sm + L::qk + P * L::kTile, a.ki + at, P * L::kTile, tid, kGradThreads);
     };
     const int slices = dv / kSlice;
     load_stage(0), cp_async_commit();
@@ -271,7 +268,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         __syncthreads();
         float y[2] = {0.f, 0.f}, b2[2] = {0.f, 0.f};
         auto value = [&](uint32_t base, int i, int c) {
-            const unsigned char *at = smem + (base - sm) + i * DK * 2 + (((c >> 3) ^ (i & 7)) << 4) + (c & 7) * 2;
+            const unsigned char *at = smem + (base - sm) + image_at(i, c) * 2;
             const uint32_t w = *reinterpret_cast<const uint32_t *>(at);
             float2 v = make_float2(bf16_lo(w), bf16_hi(w));
 #pragma unroll
@@ -311,7 +308,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
 #pragma unroll
                     for (int pl = 0; pl < P; ++pl) {
                         uint32_t b[4];
-                        load_b_t(b, vec + pl * L::kTile, DK, kb * 16, c0 + nn * 16, lane);
+                        load_b_t(b, vec + pl * L::kTile, kb * 16, c0 + nn * 16, lane);
                         mma_planes<kPlanes, kPlanes>(x[2 * nn], x[2 * nn + 1], m, b, pl);
                     }
             };

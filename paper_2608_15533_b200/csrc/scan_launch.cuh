@@ -9,7 +9,7 @@ namespace deltalog {
 
 // Byte offsets into the caller's workspace.
 struct ScanLayout {
-    size_t A, T, decay, qt, kt, kh, qp, kp, U, S, dV, dS, dq_part, dk_part, dbonus_part, total;
+    size_t A, T, decay, qt, kt, kh, qi, ki, U, S, dV, dS, dq_part, dk_part, dbonus_part, total;
 };
 
 inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tokens, bool train) {
@@ -30,8 +30,9 @@ inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tok
     l.qt = take(vec, vecs);
     l.kt = take(vec && delta, vecs);
     l.kh = take(vec, vecs);
-    l.qp = take(f32 && !vec, kPlanes * tok * Hq * dk * 2);
-    l.kp = take(f32 && !vec, kPlanes * tok * Hq * dk * 2);
+    const size_t raw = (size_t)scan_max_chunks(n, max_tokens) * Hq * (f32 ? kPlanes : 1) * kChunk * dk * 2;
+    l.qi = take(!vec, raw);
+    l.ki = take(!vec, raw);
     l.U = take(train && delta, vals);
     l.S = take(train, units * dk * dv * 4);
     l.dV = take(train && delta, vals);
@@ -73,9 +74,9 @@ inline int scan_chain_warps(int units, int dv) {
     return warps;
 }
 
-int launch_scan_split(const float *x, __nv_bfloat16 *planes, size_t elements, cudaStream_t s);
 int launch_scan_prep(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_forward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
+int launch_scan_forward_tc(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_backward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s);
 

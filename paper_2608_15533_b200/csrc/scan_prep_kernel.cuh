@@ -97,7 +97,7 @@ __device__ __forceinline__ void write_inverse(const float *T, const float *beta,
         const int blk = i >> 7, I = blk < 1 ? 0 : blk < 3 ? 1 : blk < 6 ? 2 : 3, J = blk - I * (I + 1) / 2;
         const int r = I * 16 + ((i >> 3) & 15), c = J * 16 + (i & 7) * 2;
         const float2 x = *reinterpret_cast<const float2 *>(T + r * kInvStride + c);
-        put_planes(dst + r * kChunk + c, kChunk * kChunk, c <= r ? x.x * beta[c] : 0.f, c + 1 <= r ? x.y * beta[c + 1] : 0.f);
+        put_planes(dst + image_at(r, c), kChunk * kChunk, c <= r ? x.x * beta[c] : 0.f, c + 1 <= r ? x.y * beta[c + 1] : 0.f);
     }
 }
 
@@ -139,7 +139,7 @@ struct PrepScalarSmem {
 
 // Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.  Four CTAs share an SM: the steps of
 // one chunk depend on each other, and only other chunks fill the gaps.
-template <int P, int DK, bool DELTA>
+template <int P, int DK, bool DELTA, typename IO>
 __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs a) {
     using L = PrepScalarSmem<P, DK>;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -153,13 +153,22 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
     float *T = reinterpret_cast<float *>(smem), *N = reinterpret_cast<float *>(smem + L::N);
     float2 *G = reinterpret_cast<float2 *>(smem + L::small);
     float *beta = reinterpret_cast<float *>(G + kChunk);
-    const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK;
-#pragma unroll
-    for (int pl = 0; pl < P; ++pl) {
-        load_tile(q_s + pl * kTile, a.qp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, 128);
-        load_tile(k_s + pl * kTile, a.kp + pl * a.q_plane + off, (size_t)a.Hq * DK, kChunk, DK, p.valid, tid, 128);
+    const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK, stride = (size_t)a.Hq * DK;
+    if constexpr (sizeof(IO) == 2) {
+        load_tile<DK>(q_s, static_cast<const IO *>(a.q) + off, stride, p.valid, tid, 128);
+        load_tile<DK>(k_s, static_cast<const IO *>(a.k) + off, stride, p.valid, tid, 128);
+        cp_async_commit();
+    } else {
+        for (int i = tid; i < kChunk * DK / 2; i += 128) {
+            const int row = i / (DK / 2), c = i % (DK / 2) * 2;
+            const bool ok = row < p.valid;
+            const size_t at = off + (ok ? row * stride + c : 0);
+            const float2 q = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.q) + at), k = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.k) + at);
+            __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(smem) + image_at(row, c);
+            put_planes(dst, kTile / 2, ok ? q.x : 0.f, ok ? q.y : 0.f);
+            put_planes(dst + P * kTile / 2, kTile / 2, ok ? k.x : 0.f, ok ? k.y : 0.f);
+        }
     }
-    cp_async_commit();
     if (warp == 0) chunk_decay_sums(a, p, h, G, lane);
     if (DELTA && tid >= 64) {
         const int i = tid - 64;
@@ -171,6 +180,14 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
         a.decay[unit * 2 * kChunk + tid] = expf(G[tid].x + G[tid].y);
         a.decay[unit * 2 * kChunk + kChunk + tid] = expf(decay_between(G[kChunk - 1], G[tid]));
     }
+    if (h % (a.H / a.Hq) == 0) {  // the tiles as they are: the chain kernels' operands
+        const size_t at = ((size_t)chunk * a.Hq + hq) * P * kTile / 16;
+        const uint4 *src = reinterpret_cast<const uint4 *>(smem);
+        for (int i = tid; i < P * kTile / 16; i += 128) {
+            reinterpret_cast<uint4 *>(a.qi)[at + i] = src[i];
+            reinterpret_cast<uint4 *>(a.ki)[at + i] = src[P * kTile / 16 + i];
+        }
+    }
     const int m0 = warp * 16;
     float qa[8][4] = {}, ka[8][4] = {};
 #pragma unroll
@@ -178,8 +195,8 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
         uint32_t aq[P][4], ak[P][4];
 #pragma unroll
         for (int pl = 0; pl < P; ++pl) {
-            load_a(aq[pl], q_s + pl * kTile, DK, m0, k0, lane);
-            if (DELTA) load_a(ak[pl], k_s + pl * kTile, DK, m0, k0, lane);
+            load_a(aq[pl], q_s + pl * kTile, m0, k0, lane);
+            if (DELTA) load_a(ak[pl], k_s + pl * kTile, m0, k0, lane);
         }
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
@@ -187,7 +204,7 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
 #pragma unroll
             for (int pl = 0; pl < P; ++pl) {
                 uint32_t b[4];
-                load_b(b, k_s + pl * kTile, DK, nn * 16, k0, lane);
+                load_b(b, k_s + pl * kTile, nn * 16, k0, lane);
                 mma_planes<P, P>(qa[2 * nn], qa[2 * nn + 1], aq, b, pl);
                 if (DELTA) mma_planes<P, P>(ka[2 * nn], ka[2 * nn + 1], ak, b, pl);
             }
@@ -206,7 +223,7 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
             const int i = m0 + g + 8 * half;
             const float d0 = j <= i ? decay_exp(decay_between(Gi[half], G0)) : 0.f, d1 = j + 1 <= i ? decay_exp(decay_between(Gi[half], G1)) : 0.f;
             // (selected, not multiplied: a product above the diagonal may be anything)
-            put_planes(A + i * kChunk + j, kChunk * kChunk, j <= i ? a.scale * qa[n][2 * half] * d0 : 0.f,
+            put_planes(A + image_at(i, j), kChunk * kChunk, j <= i ? a.scale * qa[n][2 * half] * d0 : 0.f,
                        j + 1 <= i ? a.scale * qa[n][2 * half + 1] * d1 : 0.f);
             if (DELTA)
                 *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(j < i ? beta[i] * ka[n][2 * half] * d0 : 0.f,
@@ -348,18 +365,19 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
             if (m > blk) back.x += x.x, back.y += x.y;
         }
         front = make_float2(decay_exp(front.x), decay_exp(front.y)), back = make_float2(decay_exp(back.x), decay_exp(back.y));
-        const size_t at = unit * kPlanes * kChunk * DK + (size_t)blk * kBlock * DK + c;
+        const size_t base = unit * kPlanes * kChunk * DK;
 #pragma unroll
         for (int r = 0; r < kBlock; ++r) {
+            const size_t at = base + image_at(blk * kBlock + r, c);
             const int own = (blk * kBlock + r) * VS + c;
             float2 x = *reinterpret_cast<const float2 *>(qs + own);
-            put_planes(a.qt + at + r * DK, kChunk * DK, x.x * front.x, x.y * front.y);
+            put_planes(a.qt + at, kChunk * DK, x.x * front.x, x.y * front.y);
             if (DELTA) {
                 x = *reinterpret_cast<const float2 *>(ks + own);
-                put_planes(a.kt + at + r * DK, kChunk * DK, x.x * front.x, x.y * front.y);
+                put_planes(a.kt + at, kChunk * DK, x.x * front.x, x.y * front.y);
             }
             x = *reinterpret_cast<const float2 *>(kc + own);
-            put_planes(a.kh + at + r * DK, kChunk * DK, x.x * back.x, x.y * back.y);
+            put_planes(a.kh + at, kChunk * DK, x.x * back.x, x.y * back.y);
         }
         const float2 b = *reinterpret_cast<const float2 *>(B + blk * DK + c);
         *reinterpret_cast<float2 *>(F + blk * DK + c) = make_float2(expf(-b.x), expf(-b.y));
@@ -430,7 +448,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
                 const int last = which || EXCL ? i - 1 : i;  // A: j <= i (RWKV6: j < i), L: j < i
                 const float x = j <= last ? acc[round][n][2 * half] : 0.f, y = j + 1 <= last ? acc[round][n][2 * half + 1] : 0.f;
                 if (which) *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(beta[i] * x, beta[i] * y);
-                else put_planes(A + i * kChunk + j, kChunk * kChunk, x, y);
+                else put_planes(A + image_at(i, j), kChunk * kChunk, x, y);
             }
     }
     if (EXCL) {
@@ -455,7 +473,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
 #pragma unroll
             for (int pl = 0; pl < kPlanes; ++pl) {
                 const __nv_bfloat16 w = __float2bfloat16_rn(s);
-                A[pl * kChunk * kChunk + i * kChunk + i] = w;
+                A[pl * kChunk * kChunk + image_at(i, i)] = w;
                 s -= __bfloat162float(w);
             }
     }

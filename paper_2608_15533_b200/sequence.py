@@ -60,6 +60,7 @@ class Plan:
         self.token_seq = table(max_tokens) if token_map and max_tokens > 0 else None
         self.scan_slots, self.append_slots, self.merge_slots = (torch.full((max(1, n),), -1, dtype=torch.int32, device=device)[:n] for _ in range(3))
         self.totals = table(4)
+        self.status = table(1)   # STATUS_* bits of the scans over this plan
         self.builds = 0   # how often build_plan has filled the tables
         self.device = self.starts.device
 
@@ -67,7 +68,7 @@ class Plan:
         if "_c" not in self.__dict__:
             # zero-sized views keep the address of their one-element storage
             ptr = [None if t is None else t.untyped_storage().data_ptr() + t.storage_offset() * 4 for t in (
-                self.starts, self.chunk_starts, self.chunk_seq, self.token_seq, self.scan_slots, self.append_slots, self.merge_slots, self.totals)]
+                self.starts, self.chunk_starts, self.chunk_seq, self.token_seq, self.scan_slots, self.append_slots, self.merge_slots, self.totals, self.status)]
             self._c = _Plan(self.n, self.max_tokens, *ptr)
         return self._c
 
