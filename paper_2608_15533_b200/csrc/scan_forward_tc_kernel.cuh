@@ -102,8 +102,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             bulk_copy_g2s(st + L::kh, ku, L::kK * L::kTile, bar);
         }
     };
-    // who does what besides: warp 0 issues the products, one thread of warp 4 the loads, warps 8 and 9 the output rows
-    const bool loader = tid == 128, storer = tid >= 256 && tid < 256 + kChunk;
+    // who does what besides: warp 0 issues the products, one thread of warp 4 the loads, four lanes of each warp the output rows
+    const bool loader = tid == 128, storer = lane < 4;
     constexpr int kGroups = L::kOwnKh ? 3 : 2;
     if (loader)
         for (int g = 0; g < kGroups; ++g) load_group(g, 0);
@@ -162,8 +162,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     };
     auto store_out = [&](int c) {
         if constexpr (!F32IO) {
-            if (a.out && storer) tc_store_rows(odst + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), out_s, tid - 256);
+            if (a.out && storer) tc_store_row(odst + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), out_s, warp * 4 + lane);
         }
+    };
+
+    // behind the second barrier of chunk c: v's tile is read, the last chunk's output tile written
+    auto between = [&](int c) {
+        load_v(c + 1);
+        cp_async_commit();
+        if (c > 0) store_out(c - 1);
+        if (NST == 1 && VEC && loader) load_group(0, c + 1);
     };
 
     for (int c = 0; c < nchunks; ++c) {
@@ -221,15 +229,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             for (int i = 0; i < HT; ++i) u[i] = VEC ? x[i] - u[i] : fmaf(-d[i], u[i], x[i]);
             tmem_st_planes<kPlanes>(row + PL + HT / 2 * f, 32, u);
             handed_over();
-            load_v(c + 1);
-            cp_async_commit();
-            if (c > 0) store_out(c - 1);
-            if (NST == 1 && VEC && loader) load_group(0, c + 1);
             if (warp == 0) ok = bounded_wait(full(1, c), parity, tc.abort_flag) && ok;
             if (issuing()) {
                 tc_product_lower<kPlanes, kPlanes, kPlanes, 32>(tc.tmem + ACC0, tc.tmem + PL, st + L::T);
                 tc_commit(mma_bar);
             }
+            between(c);
             products_done();
             tmem_ld16(row + ACC0 + HT * f, u);
             if (a.keep) {
@@ -249,13 +254,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         }
         tmem_st_planes<US>(row + PL + HT / 2 * f, 32, u);
         handed_over();
-        if (!DELTA) {
-            load_v(c + 1);
-            cp_async_commit();
-            if (c > 0) store_out(c - 1);
-            if (NST == 1 && VEC && loader) load_group(0, c + 1);
-            if (warp == 0) ok = bounded_wait(full(1, c), parity, tc.abort_flag) && ok;
-        }
+        if (!DELTA && warp == 0) ok = bounded_wait(full(1, c), parity, tc.abort_flag) && ok;
         if (L::kOwnKh && warp == 0) ok = bounded_wait(full(2, c), parity, tc.abort_flag) && ok;
         if (issuing()) {
             if (L::kOwnKh) tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PL, st + L::kh);
@@ -263,6 +262,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             tc_product_lower<UO, L::kOut, L::kOut, 32>(tc.tmem + ACC2, tc.tmem + PLO, st + L::A);
             tc_commit(mma_bar);
         }
+        if (!DELTA) between(c);
         if (!F32IO && storer) tc_stores_read();  // the last chunk's output has left its tile
         products_done();
 #pragma unroll

@@ -78,6 +78,7 @@ int launch_scan_prep(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_forward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_forward_tc(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_backward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
+int launch_scan_backward_tc(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s);
 
 }  // namespace deltalog

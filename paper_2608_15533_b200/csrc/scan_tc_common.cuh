@@ -181,10 +181,11 @@ __device__ __forceinline__ void tc_load_rows(uint32_t dst, const __nv_bfloat16 *
         cp_async16_zfill(dst + r * 256 + u * 16, src + (ok ? (size_t)r * stride + u * 8 : 0), ok);
     }
 }
-// One row per thread, asynchronously (the tile's writers have fenced towards the async proxy and met at a barrier).
-__device__ __forceinline__ void tc_store_rows(__nv_bfloat16 *dst, size_t stride, int valid, uint32_t src, int tid) {
-    if (tid < valid)
-        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 256;\n" ::"l"(dst + (size_t)tid * stride), "r"(src + tid * 256) : "memory");
+// Row `r` of the tile, asynchronously, by one thread (the tile's writers have fenced towards the async proxy and met at a
+// barrier).  Every warp's first four lanes take a row each: a warp issues such copies one after the other.
+__device__ __forceinline__ void tc_store_row(__nv_bfloat16 *dst, size_t stride, int valid, uint32_t src, int r) {
+    if (r < valid)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 256;\n" ::"l"(dst + (size_t)r * stride), "r"(src + r * 256) : "memory");
     asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
 }
 __device__ __forceinline__ void tc_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory"); }
