@@ -8,7 +8,7 @@ extern "C" int deltalog_build_plan(const int32_t *lens, const int32_t *slots, co
                                    int32_t decode_rows, const deltalog_plan *plan, void *stream) {
     if (int rc = validate_plan(plan)) return rc;
     if (plan->n > 0 && !lens) return DELTALOG_ERR_INVALID_ARG;
-    if (!plan->totals || (plan->token_seq && !aligned16(plan->token_seq))) return DELTALOG_ERR_INVALID_ARG;
+    if (!plan->totals || !aligned16(plan->totals) || (plan->token_seq && !aligned16(plan->token_seq))) return DELTALOG_ERR_INVALID_ARG;
     if (log_len && (H <= 0 || num_slots <= 0)) return DELTALOG_ERR_INVALID_ARG;
     if (log_len && (cap < 1 || cap > kMaxCapHost)) return DELTALOG_ERR_CAP_RANGE;
     PlanArgs a{lens, slots, log_len, plan->n, H, cap, num_slots, decode_rows, plan->max_tokens, scan_max_chunks(plan->n, plan->max_tokens),

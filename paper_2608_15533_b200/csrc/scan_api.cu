@@ -34,6 +34,7 @@ ScanArgs scan_args(const deltalog_desc *d, const deltalog_plan *plan, const void
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
     a.U = floats(l.U), a.S = floats(l.S), a.dV = floats(l.dV), a.dS = floats(l.dS), a.decay = floats(l.decay);
     a.dq_part = floats(l.dq_part), a.dk_part = floats(l.dk_part), a.dbonus_part = floats(l.dbonus_part);
+    a.order = reinterpret_cast<int32_t *>(w + l.order);
     a.qi = plane(l.qi), a.ki = plane(l.ki);
     return a;
 }

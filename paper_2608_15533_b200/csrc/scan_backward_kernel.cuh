@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x;
-    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     const int v0 = (blockIdx.y * (nthreads >> 5) + warp) * 16;
     const int t = lane & 3;
     const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
@@ -49,8 +49,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
     const size_t v_stride = (size_t)a.H * a.dv;
     const uint32_t o_s = sm + L::slices + warp * L::per_warp, stage = o_s + kChunk * 32;
 
-    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {  // q or k of a chunk
-        load_image(dst, src + ((size_t)(chunk0 + c) * a.Hq + hq) * P * kChunk * DK, P * L::kTile, tid, nthreads);
+    auto load_raw = [&](uint32_t dst, const void *raw, const __nv_bfloat16 *image, int c) {  // q or k of a chunk
+        load_vectors_tile<P, DK>(dst, raw, image, a, tok0 + c * kChunk, chunk0 + c, hq, min(kChunk, len - c * kChunk), tid, nthreads);
     };
     auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, int planes, size_t unit) {
         load_image(dst, src + unit * kPlanes * kChunk * DK, planes * L::kTile, tid, nthreads);
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
     auto load_first = [&](int c) {  // k for dU, decay factors
         const size_t unit = (size_t)(chunk0 + c) * a.H + h;
         if (VEC) load_decayed(sm + L::kh, a.kh, kPlanes, unit);
-        else if (L::kTwice) load_raw(sm + L::kh + (c & 1) * L::kTile, a.ki, c);
+        else if (L::kTwice) load_raw(sm + L::kh + (c & 1) * L::kTile, a.k, a.ki, c);
         for (int i = tid; i < L::kDecay / 16; i += nthreads)
             cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
     };
@@ -73,8 +73,8 @@ __global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a)
             load_decayed(sm + L::q, a.qt, kPlanes, unit);
             if (DELTA) load_decayed(sm + L::kt, a.kt, kPlanes, unit);
         } else {
-            load_raw(sm + L::q, a.qi, c);
-            if (!L::kTwice) load_raw(sm + L::kh, a.ki, c);
+            load_raw(sm + L::q, a.q, a.qi, c);
+            if (!L::kTwice) load_raw(sm + L::kh, a.k, a.ki, c);
         }
         if constexpr (!F32IO)
             load_slice(o_s, static_cast<const IO *>(a.dout) + (size_t)(tok0 + c * kChunk) * v_stride + (size_t)h * a.dv + v0, v_stride,

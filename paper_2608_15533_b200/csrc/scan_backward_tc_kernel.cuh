@@ -15,6 +15,7 @@ struct BackwardTcSmem {
     static constexpr int kVecs = VEC ? kPlanes : P;
     static constexpr int kDecay = VEC ? DK * 4 : 2 * kChunk * 4;
     static constexpr int kStages = !VEC && P == 1 ? 2 : 1;
+    static constexpr bool kRaw = !VEC && P == 1;  // q and k as they are, copied by all threads
     // group 0: k for dU (scalar decay: for the update as well) and the decay factors; group 1: A, T; group 2: q and, per channel,
     // k e^G.
     static constexpr int kh = 0;
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
     const uint32_t sm = smem_addr(smem_tc);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int v = 32 * (warp & 3) + lane, f = warp >> 2;
-    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
     const int chunk0 = a.chunk_starts[seq];
     const size_t tile = (size_t)DK * DV, s_off = ((size_t)seq * a.H + h) * tile;
@@ -68,8 +69,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
         const uint32_t st = sm + (n % NST) * L::stage, bar = full(group, n);
         const size_t vec = unit * kPlanes * kChunk * DK, qvec = qunit * P * kChunk * DK, mat = unit * kPlanes * kChunk * kChunk;
         if (group == 0) {
-            mbar_arrive_expect_tx(bar, L::kVecs * L::kTile + L::kDecay);
-            bulk_copy_g2s(st + L::kh, VEC ? a.kh + vec : a.ki + qvec, L::kVecs * L::kTile, bar);
+            mbar_arrive_expect_tx(bar, (L::kRaw ? 0 : L::kVecs * L::kTile) + L::kDecay);
+            if (!L::kRaw) bulk_copy_g2s(st + L::kh, VEC ? a.kh + vec : a.ki + qvec, L::kVecs * L::kTile, bar);
             bulk_copy_g2s(sm + L::decay + (n & 1) * L::kDecay, a.decay + unit * (L::kDecay / 4), L::kDecay, bar);
         } else if (group == 1) {
             mbar_arrive_expect_tx(bar, (DELTA ? 2 : 1) * kPlanes * L::kMat);
@@ -81,15 +82,27 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
             if (VEC && DELTA) bulk_copy_g2s(st + L::kt, a.kt + vec, L::kVecs * L::kTile, bar);
         }
     };
+    constexpr int kGroups = L::kRaw ? 2 : 3;
     if (loader)
-        for (int g = 0; g < 3; ++g) load_group(g, 0);
+        for (int g = 0; g < kGroups; ++g) load_group(g, 0);
     auto load_do = [&](int n) {
         if constexpr (!F32IO) {
             const int c = nchunks - 1 - n;
             if (c >= 0) tc_load_rows(do_s, dsrc + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), tid);
         }
     };
-    load_do(0);
+    auto load_qk = [&](int n) {
+        if constexpr (L::kRaw) {
+            const int c = nchunks - 1 - n;
+            if (c < 0) return;
+            const uint32_t st = sm + (n % NST) * L::stage;
+            const size_t at = ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, stride = (size_t)a.Hq * DK;
+            const int valid = min(kChunk, len - c * kChunk);
+            tc_load_operand<DK, kChunk * 128>(st + L::kh, a.k, at, stride, valid, tid);
+            tc_load_operand<DK, kChunk * 128>(st + L::q, a.q, at, stride, valid, tid);
+        }
+    };
+    load_do(0), load_qk(0);
 
     float s[HC];
 #pragma unroll
@@ -127,13 +140,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
         const uint32_t st = sm + (n % NST) * L::stage, parity = (uint32_t)(n / NST) & 1u;
         const float *decay = reinterpret_cast<const float *>(smem_tc + L::decay + (n & 1) * L::kDecay);
         tmem_st_planes<kPlanes>(row + PL + f * HC / 2, DK / 2, s);
-        if (!F32IO) cp_async_wait_all();  // this chunk's dO
+        if (!F32IO) cp_async_wait_all();  // this chunk's dO, q, k
+        if (L::kRaw) fence_async_proxy();
         handed_over();
         // (behind a barrier of this chunk every wait of the last one is over: see scan_forward_tc_kernel)
         if (loader && NST == 2)
-            for (int g = 0; g < 3; ++g) load_group(g, n + 1);
+            for (int g = 0; g < kGroups; ++g) load_group(g, n + 1);
         if (loader && NST == 1 && n > 0)
-            for (int g = VEC ? 1 : 0; g < 3; ++g) load_group(g, n);
+            for (int g = VEC ? 1 : 0; g < kGroups; ++g) load_group(g, n);
         ok = bounded_wait(full(0, n), parity, tc.abort_flag) && ok;
         if (issuing()) {
             tc_product<kPlanes, 0, L::kVecs, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, tc.tmem + PL, st + L::kh);
@@ -165,7 +179,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
             tc_product_upper<OP1, kPlanes, kPlanes, 32>(tc.tmem + ACC1, tc.tmem + PLO, st + L::A);
             tc_commit(mma_bar);
         }
-        load_do(n + 1);
+        load_do(n + 1), load_qk(n + 1);
         cp_async_commit();
         if (n > 0) store_out(c + 1);
         if (loader && NST == 1 && VEC) load_group(0, n + 1);
@@ -200,7 +214,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
             tmem_st_planes<kPlanes>(row + PL + HT / 2 * f, 32, x);
         }
         handed_over();
-        if (warp == 0) ok = bounded_wait(full(2, n), parity, tc.abort_flag) && ok;
+        if (kGroups == 3 && warp == 0) ok = bounded_wait(full(2, n), parity, tc.abort_flag) && ok;
         if (issuing()) {
             tc_product<OP2, 0, L::kVecs, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PLO, st + L::q);
             if (DELTA) tc_product<kPlanes, 0, L::kVecs, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PL, st + (VEC ? L::kt : L::kh), false);

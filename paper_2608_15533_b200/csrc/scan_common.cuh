@@ -38,7 +38,8 @@ struct ScanArgs {
     const float *g, *beta, *bonus;
     const void *dout;
     // workspace, unit = chunk * H + head
-    __nv_bfloat16 *qi, *ki;      // scalar decay: images of q and k [chunk * Hq + head][planes][64][d_k] (bf16 io: one plane)
+    int32_t *order;              // [n] rows, the longest first: the order in which the chain kernels' CTAs take them
+    __nv_bfloat16 *qi, *ki;      // scalar decay, fp32 io: images of q and k [chunk * Hq + head][3][64][d_k]
     __nv_bfloat16 *A, *T;        // images [unit][3][64][64]
     float *decay;                // scalar decay: [unit][2][64] e^(G_i), e^(G_end - G_i); per channel: [unit][d_k] e^(G_end)
     __nv_bfloat16 *qt, *kt, *kh; // per-channel decay: images [unit][3][64][d_k]
@@ -277,6 +278,16 @@ __device__ __forceinline__ void load_slice(uint32_t dst, const __nv_bfloat16 *sr
         cp_async16_zfill(slice_addr(dst, row, unit), src + (ok ? (size_t)row * stride + unit * 8 : 0), ok);
     }
 }
+// q or k of a chunk with scalar decay: from the tensor (bf16 io), or the image that prep made of it (fp32 io).
+template <int P, int DK>
+__device__ __forceinline__ void load_vectors_tile(uint32_t dst, const void *raw, const __nv_bfloat16 *image, const ScanArgs &a, int tok, int chunk, int hq,
+                                                  int valid, int tid, int nthreads) {
+    if constexpr (P == 1)
+        load_tile<DK>(dst, static_cast<const __nv_bfloat16 *>(raw) + ((size_t)tok * a.Hq + hq) * DK, (size_t)a.Hq * DK, valid, tid, nthreads);
+    else
+        load_image(dst, image + ((size_t)chunk * a.Hq + hq) * P * kChunk * DK, P * kChunk * DK * 2, tid, nthreads);
+}
+
 // Transposed accumulators x[8][4] (16 columns of d_v x 64 tokens) to a tensor of rows `stride` elements apart: bf16
 // through the warp's staging slice, fp32 directly (eight lanes write one 32-byte sector).
 __device__ __forceinline__ void store_slice(__nv_bfloat16 *dst, size_t stride, int valid, const float (&x)[8][4], uint32_t stage, int lane) {

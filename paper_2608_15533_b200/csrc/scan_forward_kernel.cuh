@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x;
-    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     const int v0 = (blockIdx.y * (nthreads >> 5) + warp) * 16;
     const int t = lane & 3;
     int slot;
@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
     const size_t v_stride = (size_t)a.H * a.dv;
     const uint32_t v_s = sm + L::slices + warp * L::per_warp, stage = v_s + kChunk * 32;
 
-    auto load_raw = [&](uint32_t dst, const __nv_bfloat16 *src, int c) {  // q or k of a chunk
-        load_image(dst, src + ((size_t)(chunk0 + c) * a.Hq + hq) * P * kChunk * DK, P * L::kTile, tid, nthreads);
+    auto load_raw = [&](uint32_t dst, const void *raw, const __nv_bfloat16 *image, int c) {  // q or k of a chunk
+        load_vectors_tile<P, DK>(dst, raw, image, a, tok0 + c * kChunk, chunk0 + c, hq, min(kChunk, len - c * kChunk), tid, nthreads);
     };
     auto load_decayed = [&](uint32_t dst, const __nv_bfloat16 *src, int planes, size_t unit) {
         load_image(dst, src + unit * kPlanes * kChunk * DK, planes * L::kTile, tid, nthreads);
@@ -66,8 +66,8 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
             load_decayed(sm + L::q, a.qt, L::kQ, unit);
             if (DELTA) load_decayed(sm + L::k, a.kt, L::kK, unit);
         } else {
-            load_raw(sm + L::q, a.qi, c);
-            if (L::kTwice) load_raw(sm + L::k + (c & 1) * L::kTile, a.ki, c);
+            load_raw(sm + L::q, a.q, a.qi, c);
+            if (L::kTwice) load_raw(sm + L::k + (c & 1) * L::kTile, a.k, a.ki, c);
         }
         for (int i = tid; i < L::kDecay / 16; i += nthreads)
             cp_async16(smem + L::decay + (c & 1) * L::kDecay + i * 16, a.decay + unit * (L::kDecay / 4) + i * 4);
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
     };
     auto load_update = [&](int c) {
         if (VEC) load_decayed(sm + L::kh, a.kh, L::kK, (size_t)(chunk0 + c) * a.H + h);
-        else if (!L::kTwice) load_raw(sm + L::k, a.ki, c);
+        else if (!L::kTwice) load_raw(sm + L::k, a.k, a.ki, c);
     };
     if (nchunks > 0) {
         load_vectors(0), cp_async_commit();

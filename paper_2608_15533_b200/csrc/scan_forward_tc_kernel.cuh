@@ -23,6 +23,7 @@ struct ForwardTcSmem {
     static constexpr int kQ = VEC ? kOut : P, kK = VEC ? kPlanes : P;
     static constexpr int kDecay = VEC ? DK * 4 : 2 * kChunk * 4;
     static constexpr int kStages = !VEC && P == 1 ? 2 : 1;  // what fits
+    static constexpr bool kRaw = !VEC && P == 1;            // q and k as they are, copied by all threads
     // delta rule: planes of k (per channel: k e^G) and q, 64 channels of the one and then of the other, then k's further
     // planes; otherwise q, and for scalar decay k
     static constexpr int kPair = DELTA ? 2 * kTile : kTile, kPairHalf = DELTA ? 2 * kHalf : kHalf;
@@ -56,7 +57,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     const uint32_t sm = smem_addr(smem_tc);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int v = 32 * (warp & 3) + lane, f = warp >> 2;
-    const int seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     int slot;
     if (!scan_slot(a, seq, tid, slot)) return;
     const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
@@ -82,8 +83,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         const size_t vec = unit * kPlanes * kChunk * DK, qvec = qunit * P * kChunk * DK, mat = unit * kPlanes * kChunk * kChunk;
         const __nv_bfloat16 *q = VEC ? a.qt + vec : a.qi + qvec, *k = VEC ? a.kt + vec : a.ki + qvec, *ku = VEC ? a.kh + vec : a.ki + qvec;
         if (group == 0) {
-            mbar_arrive_expect_tx(bar, L::kh - L::kq + L::kDecay);
-            if (DELTA) {
+            mbar_arrive_expect_tx(bar, (L::kRaw ? 0 : L::kh - L::kq) + L::kDecay);
+            if (L::kRaw) {
+            } else if (DELTA) {
                 for (int i = 0; i < L::kQ * (DK / 64); ++i) {  // halves of k and q by turns
                     bulk_copy_g2s(st + L::kq + 2 * i * L::kHalf, k + (size_t)i * L::kHalf / 2, L::kHalf, bar);
                     bulk_copy_g2s(st + L::kq + (2 * i + 1) * L::kHalf, q + (size_t)i * L::kHalf / 2, L::kHalf, bar);
@@ -104,7 +106,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     };
     // who does what besides: warp 0 issues the products, one thread of warp 4 the loads, four lanes of each warp the output rows
     const bool loader = tid == 128, storer = lane < 4;
-    constexpr int kGroups = L::kOwnKh ? 3 : 2;
+    constexpr int kGroups = L::kOwnKh && !L::kRaw ? 3 : 2;
     if (loader)
         for (int g = 0; g < kGroups; ++g) load_group(g, 0);
     auto load_v = [&](int c) {
@@ -112,7 +114,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             if (c < nchunks) tc_load_rows(v_s, vsrc + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), tid);
         }
     };
-    load_v(0);
+    auto load_qk = [&](int c) {
+        if constexpr (L::kRaw) {
+            if (c >= nchunks) return;
+            const uint32_t st = sm + (c % NST) * L::stage;
+            const size_t at = ((size_t)(tok0 + c * kChunk) * a.Hq + hq) * DK, stride = (size_t)a.Hq * DK;
+            const int valid = min(kChunk, len - c * kChunk);
+            if (DELTA) {
+                tc_load_operand<DK, 2 * L::kHalf>(st + L::kq, a.k, at, stride, valid, tid);
+                tc_load_operand<DK, 2 * L::kHalf>(st + L::kq + L::kHalf, a.q, at, stride, valid, tid);
+            } else {
+                tc_load_operand<DK, L::kHalf>(st + L::kq, a.q, at, stride, valid, tid);
+                tc_load_operand<DK, L::kHalf>(st + L::kh, a.k, at, stride, valid, tid);
+            }
+        }
+    };
+    load_v(0), load_qk(0);
 
     float s[HC];
     const bool from = a.S_in && !(a.fresh && a.fresh[seq]);
@@ -168,7 +185,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
 
     // behind the second barrier of chunk c: v's tile is read, the last chunk's output tile written
     auto between = [&](int c) {
-        load_v(c + 1);
+        load_v(c + 1), load_qk(c + 1);
         cp_async_commit();
         if (c > 0) store_out(c - 1);
         if (NST == 1 && VEC && loader) load_group(0, c + 1);
@@ -180,7 +197,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         const uint32_t st = sm + (c % NST) * L::stage, parity = (uint32_t)(c / NST) & 1u;
         const float *decay = reinterpret_cast<const float *>(smem_tc + L::decay + (c & 1) * L::kDecay);
         tmem_st_planes<kPlanes>(row + PL + f * HC / 2, DK / 2, s);
-        if (!F32IO) cp_async_wait_all();  // this chunk's v
+        if (!F32IO) cp_async_wait_all();  // this chunk's v, q, k
+        if (L::kRaw) fence_async_proxy();
         handed_over();
         // Behind a barrier of this chunk every wait of the last one is over, as is every read of its decay factors: its
         // barriers may go on to their next phase.  (A thread that comes late to a wait would else find the phase behind it gone
@@ -255,7 +273,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         tmem_st_planes<US>(row + PL + HT / 2 * f, 32, u);
         handed_over();
         if (!DELTA && warp == 0) ok = bounded_wait(full(1, c), parity, tc.abort_flag) && ok;
-        if (L::kOwnKh && warp == 0) ok = bounded_wait(full(2, c), parity, tc.abort_flag) && ok;
+        if (kGroups == 3 && warp == 0) ok = bounded_wait(full(2, c), parity, tc.abort_flag) && ok;
         if (issuing()) {
             if (L::kOwnKh) tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PL, st + L::kh);
             else tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kPair, L::kPairHalf>(tc.tmem + UPD, tc.tmem + PL, st + L::kq);

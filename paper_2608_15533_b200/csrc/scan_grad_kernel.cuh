@@ -145,9 +145,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         }
     };
     auto load_qk = [&]() {
-        const size_t at = ((size_t)chunk * a.Hq + hq) * P * kChunk * DK;
-        load_image(sm + L::qk, a.qi + at, P * L::kTile, tid, kGradThreads);
-        load_image(sm + L::qk + P * L::kTile, a.ki + at, P * L::kTile, tid, kGradThreads);
+        load_vectors_tile<P, DK>(sm + L::qk, a.q, a.qi, a, p.tok0, chunk, hq, p.valid, tid, kGradThreads);
+        load_vectors_tile<P, DK>(sm + L::qk + P * L::kTile, a.k, a.ki, a, p.tok0, chunk, hq, p.valid, tid, kGradThreads);
     };
     const int slices = dv / kSlice;
     load_stage(0), cp_async_commit();

@@ -9,7 +9,7 @@ namespace deltalog {
 
 // Byte offsets into the caller's workspace.
 struct ScanLayout {
-    size_t A, T, decay, qt, kt, kh, qi, ki, U, S, dV, dS, dq_part, dk_part, dbonus_part, total;
+    size_t order, A, T, decay, qt, kt, kh, qi, ki, U, S, dV, dS, dq_part, dk_part, dbonus_part, total;
 };
 
 inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tokens, bool train) {
@@ -24,15 +24,16 @@ inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tok
     };
     ScanLayout l;
     const size_t mats = units * kPlanes * kChunk * kChunk * 2, vecs = units * kPlanes * kChunk * dk * 2, vals = units * kChunk * dv * 4;
+    l.order = take(true, (size_t)n * 4);
     l.A = take(true, mats);
     l.T = take(delta, mats);
     l.decay = take(true, units * (vec ? dk : 2 * kChunk) * 4);
     l.qt = take(vec, vecs);
     l.kt = take(vec && delta, vecs);
     l.kh = take(vec, vecs);
-    const size_t raw = (size_t)scan_max_chunks(n, max_tokens) * Hq * (f32 ? kPlanes : 1) * kChunk * dk * 2;
-    l.qi = take(!vec, raw);
-    l.ki = take(!vec, raw);
+    const size_t raw = (size_t)scan_max_chunks(n, max_tokens) * Hq * kPlanes * kChunk * dk * 2;
+    l.qi = take(f32 && !vec, raw);
+    l.ki = take(f32 && !vec, raw);
     l.U = take(train && delta, vals);
     l.S = take(train, units * dk * dv * 4);
     l.dV = take(train && delta, vals);

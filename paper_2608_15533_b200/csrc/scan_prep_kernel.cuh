@@ -83,12 +83,13 @@ __device__ __forceinline__ void invert_unit_lower(const float *N, float *T, int 
     __syncthreads();
 }
 
-// A pair of values to the same place of kPlanes planes.
-__device__ __forceinline__ void put_planes(__nv_bfloat16 *dst, size_t plane, float x, float y) {
+// A pair of values to the same place of kPlanes planes; `all` false: of the first two (what only a bf16 output sees).
+__device__ __forceinline__ void put_planes(__nv_bfloat16 *dst, size_t plane, float x, float y, bool all = true) {
     uint32_t w[kPlanes];
     split_pair<kPlanes>(x, y, w);
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p) *reinterpret_cast<uint32_t *>(dst + p * plane) = w[p];
+    for (int p = 0; p < kPlanes; ++p)
+        if (p < 2 || all) *reinterpret_cast<uint32_t *>(dst + p * plane) = w[p];
 }
 
 // T diag(beta) as planes.  Of A and T the 16 x 16 blocks above the diagonal are neither written nor read.
@@ -128,30 +129,62 @@ __device__ __forceinline__ void chunk_decay_sums(const ScanArgs &a, const ChunkP
 }
 __device__ __forceinline__ float decay_between(const float2 &i, const float2 &j) { return (i.x - j.x) + (i.y - j.y); }
 
+// Rows of the plan, the longest first (sorted by chunks, those of 511 and more together): what the chain kernels run
+// through.  A chain's time is its length, and the longest one started last would run alone at the end.
+__device__ __forceinline__ void order_rows(const ScanArgs &a, int tid, int nthreads) {
+    __shared__ int bins[512];
+    for (int i = tid; i < 512; i += nthreads) bins[i] = 0;
+    __syncthreads();
+    auto bin = [&](int i) { return 511 - min(511, a.chunk_starts[i + 1] - a.chunk_starts[i]); };
+    for (int i = tid; i < a.n; i += nthreads) atomicAdd(bins + bin(i), 1);
+    __syncthreads();
+    if (tid < 32) {  // exclusive scan, sixteen bins a lane
+        int sum = 0, own[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own[i] = bins[tid * 16 + i], sum += own[i];
+        int s = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, s, o);
+            if (tid >= o) s += y;
+        }
+        s -= sum;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bins[tid * 16 + i] = s, s += own[i];
+    }
+    __syncthreads();
+    for (int i = tid; i < a.n; i += nthreads) a.order[atomicAdd(bins + bin(i), 1)] = i;
+}
+
 template <int P, int DK>
 struct PrepScalarSmem {
     static constexpr int kTile = kChunk * DK * 2;
     static constexpr int kMat = kChunk * kInvStride * 4;
-    static constexpr int first = 2 * P * kTile > kMat ? 2 * P * kTile : kMat;  // q and k, then T
-    static constexpr int small = first, N = small + kChunk * 8 + kChunk * 4;
-    static constexpr size_t bytes(bool delta) { return N + (delta ? kMat : 0); }
+    // q and k, in whose place N and T come later
+    static constexpr int small(bool delta) { return delta && 2 * kMat > 2 * P * kTile ? 2 * kMat : 2 * P * kTile; }
+    static constexpr size_t bytes(bool delta) { return small(delta) + kChunk * 8 + kChunk * 4; }
 };
 
-// Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.  Four CTAs share an SM: the steps of
+// Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.  Five CTAs share an SM: the steps of
 // one chunk depend on each other, and only other chunks fill the gaps.
 template <int P, int DK, bool DELTA, typename IO>
-__global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(const ScanArgs a) {
     using L = PrepScalarSmem<P, DK>;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
+    if (chunk == a.max_chunks) {  // one CTA beyond the chunks
+        if (h == 0) order_rows(a, tid, 128);
+        return;
+    }
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const size_t unit = (size_t)chunk * a.H + h;
     const int hq = h / (a.H / a.Hq);
     constexpr int kTile = L::kTile;
     const uint32_t q_s = smem_addr(smem), k_s = q_s + P * kTile;
-    float *T = reinterpret_cast<float *>(smem), *N = reinterpret_cast<float *>(smem + L::N);
-    float2 *G = reinterpret_cast<float2 *>(smem + L::small);
+    float *N = reinterpret_cast<float *>(smem), *T = reinterpret_cast<float *>(smem + L::kMat);
+    constexpr int kSmall = DELTA && 2 * L::kMat > 2 * P * kTile ? 2 * L::kMat : 2 * P * kTile;
+    float2 *G = reinterpret_cast<float2 *>(smem + kSmall);
     float *beta = reinterpret_cast<float *>(G + kChunk);
     const size_t off = ((size_t)p.tok0 * a.Hq + hq) * DK, stride = (size_t)a.Hq * DK;
     if constexpr (sizeof(IO) == 2) {
@@ -159,14 +192,23 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
         load_tile<DK>(k_s, static_cast<const IO *>(a.k) + off, stride, p.valid, tid, 128);
         cp_async_commit();
     } else {
-        for (int i = tid; i < kChunk * DK / 2; i += 128) {
-            const int row = i / (DK / 2), c = i % (DK / 2) * 2;
-            const bool ok = row < p.valid;
-            const size_t at = off + (ok ? row * stride + c : 0);
-            const float2 q = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.q) + at), k = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.k) + at);
-            __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(smem) + image_at(row, c);
-            put_planes(dst, kTile / 2, ok ? q.x : 0.f, ok ? q.y : 0.f);
-            put_planes(dst + P * kTile / 2, kTile / 2, ok ? k.x : 0.f, ok ? k.y : 0.f);
+#pragma unroll 1
+        for (int i0 = 0; i0 < kChunk * DK / 2; i0 += 128 * 8) {
+            float2 q[8], k[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * 128 + tid;
+                const size_t at = off + min(i / (DK / 2), p.valid - 1) * stride + i % (DK / 2) * 2;
+                q[u] = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.q) + at), k[u] = *reinterpret_cast<const float2 *>(static_cast<const IO *>(a.k) + at);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = i0 + u * 128 + tid, row = i / (DK / 2), c = i % (DK / 2) * 2;
+                const bool ok = row < p.valid;
+                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(smem) + image_at(row, c);
+                put_planes(dst, kTile / 2, ok ? q[u].x : 0.f, ok ? q[u].y : 0.f);
+                put_planes(dst + P * kTile / 2, kTile / 2, ok ? k[u].x : 0.f, ok ? k[u].y : 0.f);
+            }
         }
     }
     if (warp == 0) chunk_decay_sums(a, p, h, G, lane);
@@ -180,7 +222,7 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
         a.decay[unit * 2 * kChunk + tid] = expf(G[tid].x + G[tid].y);
         a.decay[unit * 2 * kChunk + kChunk + tid] = expf(decay_between(G[kChunk - 1], G[tid]));
     }
-    if (h % (a.H / a.Hq) == 0) {  // the tiles as they are: the chain kernels' operands
+    if (P > 1 && h % (a.H / a.Hq) == 0) {  // the tiles as they are: the chain kernels' operands
         const size_t at = ((size_t)chunk * a.Hq + hq) * P * kTile / 16;
         const uint4 *src = reinterpret_cast<const uint4 *>(smem);
         for (int i = tid; i < P * kTile / 16; i += 128) {
@@ -213,6 +255,8 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
     const int g = lane >> 2, t = lane & 3;
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
     const float2 Gi[2] = {G[m0 + g], G[m0 + g + 8]};
+    const bool all = sizeof(IO) == 4 || a.keep;  // planes of A
+    if (DELTA) __syncthreads();  // the tiles make room for N
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
         if (n > 2 * warp + 1) break;
@@ -224,7 +268,7 @@ __global__ void __launch_bounds__(128, 4) scan_prep_scalar_kernel(const ScanArgs
             const float d0 = j <= i ? decay_exp(decay_between(Gi[half], G0)) : 0.f, d1 = j + 1 <= i ? decay_exp(decay_between(Gi[half], G1)) : 0.f;
             // (selected, not multiplied: a product above the diagonal may be anything)
             put_planes(A + image_at(i, j), kChunk * kChunk, j <= i ? a.scale * qa[n][2 * half] * d0 : 0.f,
-                       j + 1 <= i ? a.scale * qa[n][2 * half + 1] * d1 : 0.f);
+                       j + 1 <= i ? a.scale * qa[n][2 * half + 1] * d1 : 0.f, all);
             if (DELTA)
                 *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(j < i ? beta[i] * ka[n][2 * half] * d0 : 0.f,
                                                                                   j + 1 < i ? beta[i] * ka[n][2 * half + 1] * d1 : 0.f);
@@ -325,6 +369,10 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     constexpr int VS = L::kVS;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
+    if (chunk == a.max_chunks) {  // one CTA beyond the chunks
+        if (h == 0) order_rows(a, tid, 2 * DK);
+        return;
+    }
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const size_t unit = (size_t)chunk * a.H + h;
@@ -340,6 +388,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     __syncthreads();
     // a thread's block and channel pair: the block's vectors into shared memory, then, with the other blocks' decays at hand,
     // the whole chunk's to the chain kernels
+    const bool all = sizeof(IO) == 4 || a.keep;  // planes of A and of q e^G
     constexpr int kPairs = DK / 2, kThreads = 4 * kPairs, kWarps = kThreads / 32;
     const int blk = tid / kPairs, c = (tid % kPairs) * 2;
     {
@@ -371,7 +420,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
             const size_t at = base + image_at(blk * kBlock + r, c);
             const int own = (blk * kBlock + r) * VS + c;
             float2 x = *reinterpret_cast<const float2 *>(qs + own);
-            put_planes(a.qt + at, kChunk * DK, x.x * front.x, x.y * front.y);
+            put_planes(a.qt + at, kChunk * DK, x.x * front.x, x.y * front.y, all);
             if (DELTA) {
                 x = *reinterpret_cast<const float2 *>(ks + own);
                 put_planes(a.kt + at, kChunk * DK, x.x * front.x, x.y * front.y);
@@ -448,7 +497,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
                 const int last = which || EXCL ? i - 1 : i;  // A: j <= i (RWKV6: j < i), L: j < i
                 const float x = j <= last ? acc[round][n][2 * half] : 0.f, y = j + 1 <= last ? acc[round][n][2 * half + 1] : 0.f;
                 if (which) *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(beta[i] * x, beta[i] * y);
-                else put_planes(A + image_at(i, j), kChunk * kChunk, x, y);
+                else put_planes(A + image_at(i, j), kChunk * kChunk, x, y, all);
             }
     }
     if (EXCL) {

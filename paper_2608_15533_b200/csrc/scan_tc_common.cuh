@@ -181,6 +181,18 @@ __device__ __forceinline__ void tc_load_rows(uint32_t dst, const __nv_bfloat16 *
         cp_async16_zfill(dst + r * 256 + u * 16, src + (ok ? (size_t)r * stride + u * 8 : 0), ok);
     }
 }
+// A chunk's q or k of a bf16 tensor as an operand: column halves HALF bytes apart.
+template <int DK, int HALF>
+__device__ __forceinline__ void tc_load_operand(uint32_t dst, const void *src, size_t at, size_t stride, int valid, int tid) {
+    constexpr int kUnits = DK / 8;
+    const __nv_bfloat16 *p = static_cast<const __nv_bfloat16 *>(src) + at;
+#pragma unroll
+    for (int i = 0; i < kChunk * kUnits / kTcThreads; ++i) {
+        const int r = (i * kTcThreads + tid) / kUnits, u = tid % kUnits;
+        const bool ok = r < valid;
+        cp_async16_zfill(dst + (u >> 3) * HALF + r * 128 + (((u & 7) ^ (r & 7)) << 4), p + (ok ? (size_t)r * stride + u * 8 : 0), ok);
+    }
+}
 // Row `r` of the tile, asynchronously, by one thread (the tile's writers have fenced towards the async proxy and met at a
 // barrier).  Every warp's first four lanes take a row each: a warp issues such copies one after the other.
 __device__ __forceinline__ void tc_store_row(__nv_bfloat16 *dst, size_t stride, int valid, uint32_t src, int r) {

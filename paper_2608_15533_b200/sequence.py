@@ -30,6 +30,8 @@ def _stream_of(stream, device) -> int:
 def _want(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optional[int]:
     """Pointer of a contiguous tensor of this shape, type and device; ValueError otherwise.  A shape entry of None is any
     size."""
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: a tensor is needed")
     if t.dtype != dtype or t.device != device or t.dim() != len(shape) or any(s is not None and s != x for s, x in zip(shape, t.shape)):
@@ -37,6 +39,24 @@ def _want(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optiona
     if not t.is_contiguous():
         raise ValueError(f"{name}: the tensor has to be contiguous")
     return t.data_ptr()
+
+
+class _on:
+    """The device made current around a call, where it is not already."""
+
+    __slots__ = ("index", "before")
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
 
 
 def _gpu(device) -> None:
@@ -90,7 +110,7 @@ def build_plan(lens: torch.Tensor, plan: Plan, slots: Optional[torch.Tensor] = N
         p_log = _want("log_len", log_len, (None, None), torch.int32, dev)
         num, H = log_len.shape
     _gpu(dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         rc = load_library().deltalog_build_plan(p_lens if plan.n else None, p_slots, p_log, int(H), int(cap), int(num), int(bool(decode_rows)),
                                                 ctypes.byref(plan.c_struct()), _stream_of(stream, dev))
     _check(rc, "deltalog_build_plan")
@@ -153,7 +173,7 @@ def prefill(desc: Desc, state: State, plan: Plan, q, k, v, g=None, beta=None, u_
     p_out = _want("out", out, tk.out_shape, tk.io, dev) or 16
     _gpu(dev)
     ws = _workspace(desc, plan, workspace, False)
-    with torch.cuda.device(dev):
+    with _on(dev):
         rc = load_library().deltalog_prefill(ctypes.byref(desc.c_struct()), ctypes.byref(state.c_struct()), ctypes.byref(plan.c_struct()), *tk.ptr,
                                              p_fresh, p_out, ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
     _check(rc, "deltalog_prefill")
@@ -176,7 +196,7 @@ def scan_forward(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=Non
     _gpu(dev)
     S_final = torch.empty(s_shape, dtype=torch.float32, device=dev)
     ws = _workspace(desc, plan, workspace, save)
-    with torch.cuda.device(dev):
+    with _on(dev):
         rc = load_library().deltalog_scan_forward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr, p_out,
                                                   S_final.data_ptr(), int(bool(save)), ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
     _check(rc, "deltalog_scan_forward")
@@ -216,7 +236,7 @@ def scan_backward(desc: Desc, plan: Plan, q, k, v, g, beta, u_bonus, dout, S_ini
             if t is not None:
                 t.zero_()
     ptr = _ScanGrads(*(None if t is None else t.data_ptr() or 16 for t in (new.q, new.k, new.v, new.g, new.beta, new.u_bonus, new.S_init)))
-    with torch.cuda.device(dev):
+    with _on(dev):
         rc = load_library().deltalog_scan_backward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr, p_dout, p_dS,
                                                    int(bool(saved)), ctypes.byref(ptr), tk.rows, ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
     _check(rc, "deltalog_scan_backward")
