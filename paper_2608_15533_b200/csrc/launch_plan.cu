@@ -20,9 +20,11 @@ extern "C" int deltalog_build_plan(const int32_t *lens, const int32_t *slots, co
     const long long ctas = (work + kPlanThreads - 1) / kPlanThreads;
     const int grid = (int)(ctas < 1 ? 1 : ctas > device_info().sms ? device_info().sms : ctas);
     if (a.n <= kPlanShared) {
+        // few rows and tokens: fewer threads meet at the barriers sooner
+        const int threads = a.n <= 256 && work <= 1024 ? 256 : kPlanThreads;
         const size_t smem = (size_t)2 * (a.n + 1) * sizeof(int32_t);
         if (int rc = ensure_smem(plan_kernel, smem)) return rc;
-        plan_kernel<<<grid, kPlanThreads, smem, s>>>(a);
+        plan_kernel<<<grid, threads, smem, s>>>(a);
         return finish_launch();
     }
     plan_offsets_kernel<<<1, 1024, 0, s>>>(a);

@@ -11,7 +11,7 @@
 
 namespace deltalog {
 
-constexpr int kPlanThreads = 512;
+constexpr int kPlanThreads = 1024;
 constexpr int kPlanShared = 24576;
 
 struct PlanArgs {
@@ -46,7 +46,12 @@ __device__ __forceinline__ int plan_chunks(int len) { return (len + DELTALOG_SCA
 // Offsets of all rows into `starts` and `chunk_starts` ([n + 1], shared or global); `starts` holds the lengths before (the
 // caller has put them there, so that a thread's run of rows costs no strided loads).  A row whose tokens would end behind
 // max_tokens is dropped (it counts as empty), and so is every row behind it that has tokens.
+template <bool SHARED>
 __device__ __forceinline__ void plan_offsets(const PlanArgs &a, int32_t *starts, int32_t *chunk_starts, bool write_totals) {
+    if (SHARED) {
+        __builtin_assume(__isShared(starts));
+        __builtin_assume(__isShared(chunk_starts));
+    }
     __shared__ unsigned long long warps[2][2][32];
     // an odd run per thread: neighbours' accesses fall into different banks
     const int per = ((a.n + blockDim.x - 1) / blockDim.x) | 1, first = min(a.n, (int)threadIdx.x * per), last = min(a.n, first + per);
@@ -106,7 +111,12 @@ __device__ __forceinline__ int plan_find(const int32_t *offsets, int n, int x) {
     return lo;
 }
 
+template <bool SHARED>
 __device__ __forceinline__ void plan_tables(const PlanArgs &a, const int32_t *starts, const int32_t *chunk_starts) {
+    if (SHARED) {
+        __builtin_assume(__isShared(starts));
+        __builtin_assume(__isShared(chunk_starts));
+    }
     const int stride = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
     for (int i = first; i < a.n; i += stride) {
         const int len = starts[i + 1] - starts[i], slot = a.slots ? a.slots[i] : i;
@@ -129,7 +139,12 @@ __device__ __forceinline__ void plan_tables(const PlanArgs &a, const int32_t *st
     const long long end = min(steps, step + each);
     int row = step < end && step * 128 < tokens ? plan_find(starts, a.n, (int)(step * 128)) : 0;
     for (; step < end; ++step) {
-        const int t0 = (int)(step * 128) + lane * 4;
+        const int base = (int)(step * 128), t0 = base + lane * 4;
+        if (base + 127 < tokens && starts[row + 1] > base + 127) {  // all of one row
+            *reinterpret_cast<int4 *>(a.token_seq + t0) = make_int4(row, row, row, row);
+            continue;
+        }
+        const int before = row;
         if (t0 < tokens) {
             int ahead = 1;
             while (row + ahead <= a.n && starts[row + ahead] <= t0) ahead <<= 1;
@@ -153,28 +168,32 @@ __device__ __forceinline__ void plan_tables(const PlanArgs &a, const int32_t *st
         } else {
             for (int e = 0; t0 + e < a.max_tokens; ++e) a.token_seq[t0 + e] = out[e];
         }
-        row = __shfl_sync(0xffffffffu, row, 0);  // (the next step's tokens lie behind all of these)
+        // the next step's tokens lie behind all of these; its first row is that of the last token here or of the next one
+        row = __shfl_sync(0xffffffffu, t0 < tokens ? row : before, 31);
+        if (row < a.n && base + 128 < tokens)
+            while (starts[row + 1] <= base + 128) ++row;
     }
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a) {
     extern __shared__ int32_t offsets[];
     int32_t *starts = offsets, *chunk_starts = offsets + a.n + 1;
+#pragma unroll 8
     for (int i = threadIdx.x; i < a.n; i += blockDim.x) starts[i] = a.lens[i];
     __syncthreads();
-    plan_offsets(a, starts, chunk_starts, blockIdx.x == 0);
+    plan_offsets<true>(a, starts, chunk_starts, blockIdx.x == 0);
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i <= a.n; i += gridDim.x * blockDim.x) {
         a.starts[i] = starts[i];
         a.chunk_starts[i] = chunk_starts[i];
     }
-    plan_tables(a, starts, chunk_starts);
+    plan_tables<true>(a, starts, chunk_starts);
 }
 
 __global__ void __launch_bounds__(1024) plan_offsets_kernel(const PlanArgs a) {
     for (int i = threadIdx.x; i < a.n; i += blockDim.x) a.starts[i] = a.lens[i];
     __syncthreads();
-    plan_offsets(a, a.starts, a.chunk_starts, true);
+    plan_offsets<false>(a, a.starts, a.chunk_starts, true);
 }
-__global__ void __launch_bounds__(kPlanThreads) plan_tables_kernel(const PlanArgs a) { plan_tables(a, a.starts, a.chunk_starts); }
+__global__ void __launch_bounds__(kPlanThreads) plan_tables_kernel(const PlanArgs a) { plan_tables<false>(a, a.starts, a.chunk_starts); }
 
 }  // namespace deltalog
