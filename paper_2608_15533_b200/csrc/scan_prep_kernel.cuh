@@ -438,35 +438,35 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     }
     __syncthreads();
     if (tid < DK) a.decay[unit * DK + tid] = expf(B[tid] + B[DK + tid] + B[2 * DK + tid] + B[3 * DK + tid]);
-    // block pairs (I, J <= I) of A and L, 16 x 16 each, one warp per pair and matrix
+    // block pairs (I, J <= I) of A and L, 16 x 16 each, one warp per pair
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
     const int g = lane >> 2, t = lane & 3;
-    constexpr int kTasks = DELTA ? 20 : 10, kRounds = (kTasks + kWarps - 1) / kWarps;
-    float acc[kRounds][2][4] = {};
+    constexpr int kPairsAll = 10, kRounds = (kPairsAll + kWarps - 1) / kWarps, kMats = DELTA ? 2 : 1;
+    float acc[kRounds][kMats][2][4] = {};
 #pragma unroll
     for (int round = 0; round < kRounds; ++round) {
-        const int task = warp + kWarps * round;
-        if (task >= kTasks) break;
-        const bool which = task >= 10;  // L
-        const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
+        const int pair = warp + kWarps * round;
+        if (pair >= kPairsAll) break;
+        const int I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
         if (J < I || !deep[I]) {
-            const float *src = which ? ks : qs;
             const float *f = J == I ? F + I * DK : I - J == 3 ? F + 6 * DK : F + (3 + J + 1) * DK;  // (not read for I = J + 1)
 #pragma unroll 2
             for (int k0 = 0; k0 < DK; k0 += 16) {
-                uint32_t x[kPlanes][4], b[kPlanes][4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = k0 + 2 * t + 8 * (e >> 1);
-                    float2 y = *reinterpret_cast<const float2 *>(src + (I * kBlock + g + 8 * (e & 1)) * VS + k);
-                    if (I != J + 1) {
-                        const float2 w = *reinterpret_cast<const float2 *>(f + k);
-                        y.x *= w.x, y.y *= w.y;
-                    }
-                    frag_pair(x, e, y.x, y.y);
-                }
+                uint32_t b[kPlanes][4];
                 frag_b(b, kc, VS, J * kBlock, k0, lane);
-                mma_all(acc[round][0], acc[round][1], x, b);
+                float2 w[2] = {make_float2(1.f, 1.f), make_float2(1.f, 1.f)};
+                if (I != J + 1) w[0] = *reinterpret_cast<const float2 *>(f + k0 + 2 * t), w[1] = *reinterpret_cast<const float2 *>(f + k0 + 2 * t + 8);
+#pragma unroll
+                for (int m = 0; m < kMats; ++m) {
+                    const float *src = (m ? ks : qs) + (I * kBlock + g) * VS + k0 + 2 * t;
+                    uint32_t x[kPlanes][4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 y = *reinterpret_cast<const float2 *>(src + (e & 1) * 8 * VS + (e >> 1) * 8);
+                        frag_pair(x, e, y.x * w[e >> 1].x, y.y * w[e >> 1].y);
+                    }
+                    mma_all(acc[round][m][0], acc[round][m][1], x, b);
+                }
             }
         } else {
 #pragma unroll
@@ -477,7 +477,8 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
                     if (j <= i) {
                         float sq, sk;
                         pair_sums<IO, EXCL>(a, p, h, hq, DK, i, j, sq, sk);
-                        acc[round][n][e] = which ? sk : sq * a.scale;
+                        acc[round][0][n][e] = sq * a.scale;
+                        if (DELTA) acc[round][kMats - 1][n][e] = sk;
                     }
                 }
         }
@@ -485,20 +486,21 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     if (DELTA) __syncthreads();  // the vectors make room for N
 #pragma unroll
     for (int round = 0; round < kRounds; ++round) {
-        const int task = warp + kWarps * round;
-        if (task >= kTasks) break;
-        const bool which = task >= 10;
-        const int pair = which ? task - 10 : task, I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
+        const int pair = warp + kWarps * round;
+        if (pair >= kPairsAll) break;
+        const int I = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, J = pair - I * (I + 1) / 2;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int m = 0; m < kMats; ++m)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int i = I * kBlock + g + 8 * half, j = J * kBlock + n * 8 + 2 * t;
-                const int last = which || EXCL ? i - 1 : i;  // A: j <= i (RWKV6: j < i), L: j < i
-                const float x = j <= last ? acc[round][n][2 * half] : 0.f, y = j + 1 <= last ? acc[round][n][2 * half + 1] : 0.f;
-                if (which) *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(beta[i] * x, beta[i] * y);
-                else put_planes(A + image_at(i, j), kChunk * kChunk, x, y, all);
-            }
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int i = I * kBlock + g + 8 * half, j = J * kBlock + n * 8 + 2 * t;
+                    const int last = m || EXCL ? i - 1 : i;  // A: j <= i (RWKV6: j < i), L: j < i
+                    const float x = j <= last ? acc[round][m][n][2 * half] : 0.f, y = j + 1 <= last ? acc[round][m][n][2 * half + 1] : 0.f;
+                    if (m) *reinterpret_cast<float2 *>(N + i * kInvStride + j) = make_float2(beta[i] * x, beta[i] * y);
+                    else put_planes(A + image_at(i, j), kChunk * kChunk, x, y, all);
+                }
     }
     if (EXCL) {
         // the diagonal's bonus term q . (bonus * k), `kEach` threads per token
