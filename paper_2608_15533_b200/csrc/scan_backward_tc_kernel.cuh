@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
         }
     };
     load_do(0), load_qk(0);
+    cp_async_commit();
 
     float s[HC];
 #pragma unroll

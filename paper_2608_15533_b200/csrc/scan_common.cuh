@@ -11,10 +11,10 @@
 // chunk to the first, scan_grad_kernel forms the gradients of q, k, g and beta chunk by chunk in parallel.
 //
 // Precision: a bf16 value enters the tensor cores exactly.  An fp32 operand enters as three bf16 planes x = x0 + x1 + x2
-// (all 24 bits), and of a product of two such operands the six plane products with i + j <= 2 are summed in
-// fp32 accumulators, so a product is as good as one in fp32.  Two planes (three products) leave 2^-16 to 2^-18 per operand: the
+// (to 2^-26 of its size), and of a product of two such operands the six plane products with i + j <= 2 are summed in
+// fp32 accumulators, so a product is as good as one in fp32.  Two planes (three products) leave 2^-18 per operand: the
 // states and gate gradients then came out 3e-6 to 4e-5 off, against 5e-8 to 3e-7 of an fp32 computation.  Results that are
-// rounded to bf16 and feed nothing else take two planes: 2^-16 vanishes beside their own 2^-9.
+// rounded to bf16 and feed nothing else take two planes: 2^-18 vanishes beside their own 2^-9.
 #pragma once
 
 #include "common.cuh"
@@ -81,17 +81,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo_elem, float hi_elem) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// x, y -> their packed planes 0 .. N-1: each takes the leading eight bits of what the planes in front of it leave, so three
-// planes hold all 24 bits.  (Cut, not rounded: one byte permutation instead of a conversion, and nothing overflows.)
+// x, y -> their packed planes 0 .. N-1, each the bf16 rounding of what the planes in front of it leave.  (Rounded, not cut:
+// cutting costs as many instructions, leaves twice as much, and always with the same sign -- sums over long contractions
+// were ten times further off.)
 template <int N>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&w)[N]) {
     float2 r = make_float2(x, y);
 #pragma unroll
     for (int p = 0; p < N; ++p) {
-        w[p] = __byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x7632);
-        if (p + 1 < N)
-            r = __ffma2_rn(make_float2(__uint_as_float(__float_as_uint(r.x) & 0xffff0000u), __uint_as_float(__float_as_uint(r.y) & 0xffff0000u)),
-                           make_float2(-1.f, -1.f), r);
+        w[p] = pack_bf16(r.x, r.y);
+        if (p + 1 < N) r = __ffma2_rn(make_float2(bf16_lo(w[p]), bf16_hi(w[p])), make_float2(-1.f, -1.f), r);
     }
 }
 

@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         }
     };
     load_v(0), load_qk(0);
+    cp_async_commit();
 
     float s[HC];
     const bool from = a.S_in && !(a.fresh && a.fresh[seq]);

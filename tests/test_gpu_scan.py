@@ -481,3 +481,23 @@ def test_status_of_a_bad_slot_only():
     before = state.S_base.clone()
     dl.prefill(desc, state, make_plan([5, 5], [2, -3]), **t)
     assert state.status.item() == binding.STATUS_BAD_SLOT and torch.equal(state.S_base, before)
+
+
+@pytest.mark.parametrize("op", [ref.GDN, ref.KDA, ref.RWKV6])
+def test_bits_do_not_depend_on_what_the_memory_held(op):
+    """More units than the device holds at once, again and again over workspaces and outputs full of other patterns."""
+    H, dk, lens = 32, 128, [300, 64, 7, 1, 190, 90, 129, 65]
+    t, S0 = ref.inputs(op, lens, H, H, dk, dk, BF16, seed=op + 90)
+    desc, plan = make_desc(op, H, H, dk, dk, BF16), make_plan(lens)
+    ws = dl.scan_workspace(desc, len(lens), plan.max_tokens, train=True)
+    dout = torch.randn(t["v"].shape, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    first = None
+    for i in range(8):
+        ws.random_(generator=torch.Generator("cuda").manual_seed(i))
+        out = torch.full_like(t["v"], float("nan"))
+        out, S = dl.scan_forward(desc, plan, **t, S_init=S0, out=out, workspace=ws, save=True)
+        d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, workspace=ws, saved=True)
+        got = [out, S, d.q, d.k, d.v, d.g, d.S_init]
+        first = first or got
+        assert all(torch.equal(x, y) for x, y in zip(first, got)), i
+    assert all(torch.isfinite(x).all() for x in first) and plan.status.item() == 0
