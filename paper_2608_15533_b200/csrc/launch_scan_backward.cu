@@ -18,8 +18,7 @@ int launch_chain(const ScanArgs &a, cudaStream_t s) {
 }  // namespace
 
 int launch_scan_backward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s) {
-    static const int tc = env_int("DELTALOG_SCAN_TC", 1);
-    if (a.dv == 128 && tc) return launch_scan_backward_tc(d, a, s);
+    if (a.dv == 128) return launch_scan_backward_tc(d, a, s);
 #define CALL_CHAIN(VEC, P, DK, DELTA, IO) return launch_chain<VEC, P, DK, DELTA, IO>(a, s)
     DELTALOG_SCAN_DISPATCH(d, CALL_CHAIN);
 #undef CALL_CHAIN

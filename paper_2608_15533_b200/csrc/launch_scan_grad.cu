@@ -5,10 +5,10 @@
 namespace deltalog {
 namespace {
 
-template <int OP, int P, int DK, typename IO>
+template <int OP, int P, int DK, typename IO, bool TC>
 int launch_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
-    auto kernel = scan_grad_kernel<OP, P, DK, IO>;
-    const size_t smem = GradSmem<OP, P, DK, IO>::bytes;
+    auto kernel = scan_grad_kernel<OP, P, DK, IO, TC>;
+    const size_t smem = GradSmem<OP, P, DK, IO, TC>::bytes;
     if (int rc = ensure_smem(kernel, smem)) return rc;
     kernel<<<dim3(a.max_chunks, a.H), kGradThreads, smem, s>>>(a);
     if (int rc = finish_launch()) return rc;
@@ -29,9 +29,12 @@ int launch_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbon
 template <int OP>
 int launch_grad_op(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
     if (d->io_dtype == DELTALOG_F32)
-        return d->d_k == 128 ? launch_grad<OP, 3, 128, float>(d, a, rows, dbonus, s) : launch_grad<OP, 3, 64, float>(d, a, rows, dbonus, s);
-    return d->d_k == 128 ? launch_grad<OP, 1, 128, __nv_bfloat16>(d, a, rows, dbonus, s)
-                         : launch_grad<OP, 1, 64, __nv_bfloat16>(d, a, rows, dbonus, s);
+        return d->d_k == 128 ? launch_grad<OP, 3, 128, float, false>(d, a, rows, dbonus, s) : launch_grad<OP, 3, 64, float, false>(d, a, rows, dbonus, s);
+    if (a.dv == 128)  // as the chains: what they keep is laid out for this
+        return d->d_k == 128 ? launch_grad<OP, 1, 128, __nv_bfloat16, true>(d, a, rows, dbonus, s)
+                             : launch_grad<OP, 1, 64, __nv_bfloat16, true>(d, a, rows, dbonus, s);
+    return d->d_k == 128 ? launch_grad<OP, 1, 128, __nv_bfloat16, false>(d, a, rows, dbonus, s)
+                         : launch_grad<OP, 1, 64, __nv_bfloat16, false>(d, a, rows, dbonus, s);
 }
 
 }  // namespace

@@ -155,10 +155,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
             tc_commit(mma_bar);
         }
         // while it runs: the gradient for the per-chunk kernel; dO of this thread's tokens
-        {
+        if constexpr (F32IO) {
             float4 *dst = reinterpret_cast<float4 *>(a.dS + unit * tile + (size_t)v * DK + f * HC);
 #pragma unroll
             for (int i = 0; i < HC / 4; ++i) dst[i] = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+        } else {
+            keep_state_planes<DK>(a.dS + unit * tile, s, v, f * HC);
         }
         float x[HT];
 #pragma unroll
@@ -222,10 +224,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
             tc_commit(mma_bar);
         }
         // while it runs: dV, for the per-chunk kernel and as the gradient of v
-        if (DELTA) {
+        if constexpr (DELTA && F32IO) {
             float *dst = a.dV + unit * kChunk * DV + (size_t)(HT * f) * DV + v;
 #pragma unroll
             for (int i = 0; i < HT; ++i) dst[(size_t)i * DV] = u[i];
+        } else if constexpr (DELTA) {
+            keep_value_planes<false>(a.dV + unit * kChunk * DV, u, HT * f, v);
         }
 #pragma unroll
         for (int i = 0; i < HT; ++i) {

@@ -222,9 +222,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         }
         // while they run: the state for the backward pass, the last chunk's output, v of this thread's tokens
         if (a.keep) {
-            float4 *dst = reinterpret_cast<float4 *>(a.S + unit * tile + (size_t)v * DK + f * HC);
+            if constexpr (F32IO) {
+                float4 *dst = reinterpret_cast<float4 *>(a.S + unit * tile + (size_t)v * DK + f * HC);
 #pragma unroll
-            for (int i = 0; i < HC / 4; ++i) dst[i] = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+                for (int i = 0; i < HC / 4; ++i) dst[i] = make_float4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+            } else {
+                keep_state_planes<DK>(a.S + unit * tile, s, v, f * HC);
+            }
         }
         if (c > 0) write_out(c - 1);
         float x[HT];
@@ -257,9 +261,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             products_done();
             tmem_ld16(row + ACC0 + HT * f, u);
             if (a.keep) {
-                float *dst = a.U + unit * kChunk * DV + (size_t)(HT * f) * DV + v;
+                if constexpr (F32IO) {
+                    float *dst = a.U + unit * kChunk * DV + (size_t)(HT * f) * DV + v;
 #pragma unroll
-                for (int i = 0; i < HT; ++i) dst[(size_t)i * DV] = u[i];
+                    for (int i = 0; i < HT; ++i) dst[(size_t)i * DV] = u[i];
+                } else {
+                    keep_value_planes<true>(a.U + unit * kChunk * DV, u, HT * f, v);
+                }
             }
         } else {
 #pragma unroll

@@ -25,6 +25,7 @@
 
 #include "scan_common.cuh"
 #include "scan_prep_kernel.cuh"
+#include "scan_tc_common.cuh"
 
 namespace deltalog {
 
@@ -72,32 +73,39 @@ __device__ __forceinline__ void io_frag_b(uint32_t (&f)[kPlanes][4], const unsig
     frag_b(f, reinterpret_cast<const float *>(tile), kSliceStride, n0, k0, lane);
 }
 
-template <int OP, int P, int DK, typename IO>
+template <int OP, int P, int DK, typename IO, bool TC>
 struct GradSmem {
     static constexpr bool VEC = OpTraits<OP>::kVecDecay, DELTA = OpTraits<OP>::kDeltaRule;
     static constexpr int kTile = kChunk * DK * 2;
     static constexpr int kSW = DK + 4;              // row of a state slice or of a decayed vector
     static constexpr int kMW = kChunk + 8;          // row of dA, dL'
-    static constexpr int kMat = kChunk * kMW * 4;
+    static constexpr int kMat = kChunk * kMW * 4, kMats = (DELTA ? 2 : 1) * kMat;
     static constexpr int kF32 = kChunk * kSliceStride * 4;
     static constexpr int kIO = sizeof(IO) == 4 ? kF32 : kChunk * kSlice * 2;
-    // a stage: slices of S_0, dS_1, dO, U (or v), dV
-    static constexpr int kState = kSlice * kSW * 4;
-    static constexpr int dS = kState, dO = 2 * kState, U = dO + kIO, dV = U + (DELTA ? kF32 : kIO), stage = dV + (DELTA ? kF32 : 0);
-    // after the slices: q and k planes (bf16 io: in a place of their own, loaded meanwhile), or the three decayed vectors and
-    // the decays in front of and behind a token inside its block
+    static constexpr int most(int x, int y) { return x > y ? x : y; }
+    // a stage: slices of S_0, dS_1, dO, U (or v), dV;  TC: S_0, dS_1, U (or v) whole, as images
+    static constexpr int kState = TC ? 2 * DK * 256 : kSlice * kSW * 4;
+    static constexpr int dS = kState, dO = 2 * kState, U = TC ? 2 * kState : dO + kIO;
+    static constexpr int dV = U + (TC ? (DELTA ? 2 : 1) * kChunk * 256 : DELTA ? kF32 : kIO), stage = TC ? dV : dV + (DELTA ? kF32 : 0);
+    static constexpr int loaded = TC ? stage : 2 * stage;
+    // after them: q and k planes (bf16 io: in a place of their own, loaded meanwhile), or the three decayed vectors and the
+    // decays in front of and behind a token inside its block
     static constexpr bool kOwnQK = !VEC && P == 1;
-    static constexpr int qk = kOwnQK ? 2 * stage : 0;
+    static constexpr int qk = kOwnQK ? loaded : 0;
     static constexpr int last = VEC ? (DELTA ? 5 : 4) * kChunk * kSW * 4 : qk + 2 * P * kTile;
-    static constexpr int mats = 2 * stage > last ? 2 * stage : last;
-    static constexpr int small = mats + (DELTA ? 2 : 1) * kMat;
+    // dA, dL': behind all that; where that is too much (TC, scalar decay, d_k = 128) in S_0's place, which is done with by then
+    static constexpr bool kInPlace = TC && !VEC && DK == 128;
+    static constexpr int mats = kInPlace ? 0 : most(loaded, last);
+    static constexpr int small = kInPlace ? most(loaded, last) : mats + kMats;
     static constexpr int part = small;                  // [1024] partial sums of <dS, S>
     static constexpr int rows = part + 4096;            // [8][64] row sums of the channel quarters
     static constexpr int tables = rows + 8 * kChunk * 4; // [4][4][DK] e^(decay) of the chunk in front of / behind a block, of the block, inverse
     static constexpr int beta = tables + (VEC ? 16 * DK * 4 : 0);
     static constexpr int G = beta + 2 * kChunk * 4;     // beta, diagonal of dA;  sums of the scalar decay
     static constexpr int deep = G + kChunk * 8;
-    static constexpr size_t bytes = deep + 16;
+    static constexpr int control = deep + 16;
+    static constexpr size_t total = control + (TC ? kTcControlBytes : 0);
+    static constexpr size_t bytes = TC && total < kTcMinSmem ? kTcMinSmem : total;
 };
 
 // A pair of neighbouring channels of the io tensors' row.
@@ -108,16 +116,17 @@ __device__ __forceinline__ float2 load_pair(const void *src, size_t at) {
     return make_float2(x[0], x[1]);
 }
 
-template <int OP, int P, int DK, typename IO>
+template <int OP, int P, int DK, typename IO, bool TC>
 __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanArgs a) {
-    using L = GradSmem<OP, P, DK, IO>;
+    using L = GradSmem<OP, P, DK, IO, TC>;
     constexpr bool VEC = L::VEC, DELTA = L::DELTA, EXCL = OpTraits<OP>::kBonus;
     constexpr int NT = DK / 32, SW = L::kSW, MW = L::kMW;
     constexpr int GP = sizeof(IO) == 4 ? kPlanes : 2;  // planes of an fp32 operand
     constexpr int IP = sizeof(IO) == 4 ? GP : 1;       // and of dO and v
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ __align__(1024) unsigned char smem_grad[];
+    unsigned char *smem = smem_grad;
     const uint32_t sm = smem_addr(smem);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), chunk = blockIdx.x, h = blockIdx.y;
     const int g = lane >> 2, t = lane & 3, mt = warp & 3, cq = warp >> 2, c0 = cq * (DK / 4);
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
@@ -148,18 +157,166 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         load_vectors_tile<P, DK>(sm + L::qk, a.q, a.qi, a, p.tok0, chunk, hq, p.valid, tid, kGradThreads);
         load_vectors_tile<P, DK>(sm + L::qk + P * L::kTile, a.k, a.ki, a, p.tok0, chunk, hq, p.valid, tid, kGradThreads);
     };
-    const int slices = dv / kSlice;
-    load_stage(0), cp_async_commit();
     if (tid < 4) deep[tid] = 0;
     if (!VEC && warp == 0) chunk_decay_sums(a, p, h, G, lane);
     if (DELTA && tid >= 64 && tid < 128) beta[tid - 64] = scan_beta(tid - 64 < p.valid ? a.beta[(size_t)(p.tok0 + tid - 64) * a.H + h] : 0.f);
-    if (L::kOwnQK) load_qk();
-
     // dO S_0^T, dV S_0^T, U dS_1^T [16 x DK/4] and, where the warp's 16 columns are at or below the diagonal, dO U^T, dV U^T
     float dq[NT][4] = {}, dr[NT][4] = {}, dw[NT][4] = {}, da[2][4] = {}, dl[2][4] = {};
     float dot0 = 0.f, dot1 = 0.f, db = 0.f;
     constexpr int kPairs = DK / 2, kGroups = kGradThreads / kPairs;
     const int cp = tid % kPairs, grp = tid / kPairs;
+    // dA and dL', masked; scalar decay multiplies e^(G_i - G_j) in here
+    auto write_mats = [&]() {
+        if (cq > mt) return;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int i = mt * 16 + g + 8 * half, j = cq * 16 + n * 8 + 2 * t;
+                    float x[2], y[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float m = VEC ? 1.f : (j + e <= i ? decay_exp(decay_between(G[i], G[j + e])) : 0.f);
+                        const float raw = da[n][2 * half + e];
+                        if (i == j + e) diag[i] = raw * a.scale;
+                        if (EXCL && i == j + e + 1) near[i] = raw;
+                        x[e] = j + e + (EXCL ? 1 : 0) < i ? raw * m * a.scale : 0.f;
+                        y[e] = j + e < i ? -dl[n][2 * half + e] * m : 0.f;
+                    }
+                    *reinterpret_cast<float2 *>(da_f + i * MW + j) = make_float2(x[0], x[1]);
+                    if (DELTA) *reinterpret_cast<float2 *>(dl_f + i * MW + j) = make_float2(y[0], y[1]);
+                }
+    };
+    TcBlock tc = {};
+    if constexpr (TC) {
+        // On the tensor cores, d_v = 128: row 32 q + r of the A operand is dO of token 16 q + r (r < 16) or dV of token 16 q + r - 16, so
+        // that the warp that owns a token block reads its results from its own lanes, in mma.sync's accumulator layout.
+        // Tensor memory: planes of A (of U later), [dO; dV] S_0^T, [dO; dV] U^T, U dS_1^T.
+        constexpr uint32_t PA = 0, D1 = 128, D2 = 256, D3 = 320;
+        constexpr int UP = DELTA ? 2 : 1;
+        tc = tc_setup(smem + L::control, 4, tid);
+        auto bar = [&](int i) { return tc.bars + 8u * i; };  // 0: S_0, 1: U, 2: dS_1, 3: products
+        if (tid == 0) {
+            mbar_arrive_expect_tx(bar(0), L::kState);
+            bulk_copy_g2s(sm, a.S + unit * tile, L::kState, bar(0));
+            if (DELTA) {
+                mbar_arrive_expect_tx(bar(1), 2 * kChunk * 256);
+                bulk_copy_g2s(sm + L::U, a.U + unit * kChunk * 128, 2 * kChunk * 256, bar(1));
+            }
+            mbar_arrive_expect_tx(bar(2), L::kState);
+            bulk_copy_g2s(sm + L::dS, a.dS + unit * tile, L::kState, bar(2));
+        }
+        if constexpr (!DELTA && sizeof(IO) == 2) tc_load_operand<128, kChunk * 128>(sm + L::U, a.v, v_off, v_stride, p.valid, tid);
+        if (L::kOwnQK) load_qk();
+        cp_async_commit();
+        bool ok = true;
+        uint32_t phase = 0;
+        auto handed_over = [&]() {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncthreads();
+            tc_fence_after();
+        };
+        auto products_done = [&]() {
+            ok = bounded_wait(bar(3), phase, tc.abort_flag) && ok;
+            phase ^= 1;
+            tc_fence_after();
+        };
+        auto issuing = [&]() { return warp == 0 && __all_sync(0xffffffffu, ok) && elect_one(); };
+        const uint32_t row = tc.tmem + ((uint32_t)(32 * mt) << 16);
+        const int tok = mt * 16 + (lane & 15), v0 = 32 * cq;  // this thread's row of A and columns
+        const bool upper = lane >= 16, inside = tok < p.valid;
+        auto put_row = [&](int plane, const uint4 (&w)[4]) {
+            const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+            const uint32_t y[8] = {w[2].x, w[2].y, w[2].z, w[2].w, w[3].x, w[3].y, w[3].z, w[3].w};
+            tmem_st8(row + PA + plane * 64 + v0 / 2, x), tmem_st8(row + PA + plane * 64 + v0 / 2 + 8, y);
+        };
+        {
+            uint4 hi[4], lo[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[i] = lo[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (!upper && inside) {
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.dout) + v_off + (size_t)tok * v_stride + v0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) hi[i] = src[i];
+            }
+            if (DELTA && upper) {
+                const unsigned char *src = reinterpret_cast<const unsigned char *>(a.dV + unit * kChunk * 128) + kept_dv_at(tok, v0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) hi[i] = reinterpret_cast<const uint4 *>(src)[i], lo[i] = reinterpret_cast<const uint4 *>(src + kChunk * 256)[i];
+            }
+            put_row(0, hi);
+            if (DELTA) put_row(1, lo);
+        }
+        if (!DELTA) cp_async_wait_all(), fence_async_proxy();  // v
+        handed_over();
+        ok = bounded_wait(bar(0), 0u, tc.abort_flag) && ok;
+        if (DELTA) ok = bounded_wait(bar(1), 0u, tc.abort_flag) && ok;
+        if (issuing()) {
+            tc_product<UP, 0, 2, 0, 2, true, 8, DK, 64, DK * 256, kKeptHalf>(tc.tmem + D1, tc.tmem + PA, sm);
+            tc_product<UP, 0, UP, 0, 2, false, 8, kChunk, 64, kChunk * 256, kChunk * 128>(tc.tmem + D2, tc.tmem + PA, sm + L::U);
+            tc_commit(bar(3));
+        }
+        // meanwhile the sums of products: dbeta (eight threads a token), <dS_1, S_0> by channel
+        auto both = [&](const unsigned char *at, int plane) {  // a pair of values of two planes
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(at), y = *reinterpret_cast<const uint32_t *>(at + plane);
+            return make_float2(bf16_lo(x) + bf16_lo(y), bf16_hi(x) + bf16_hi(y));
+        };
+        if (DELTA) {
+            const int i = tid >> 3, v = (tid & 7) * 16;
+            const float rb = 1.f / beta[i];
+            const unsigned char *d = reinterpret_cast<const unsigned char *>(a.dV + unit * kChunk * 128);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float2 x = both(smem + L::U + kept_u_at(i, v + j), kChunk * 256), y = both(d + kept_dv_at(i, v + j), kChunk * 256);
+                db = fmaf(x.x * rb, y.x * rb, db), db = fmaf(x.y * rb, y.y * rb, db);
+            }
+        }
+        ok = bounded_wait(bar(2), 0u, tc.abort_flag) && ok;
+        for (int v = grp; v < 128; v += kGroups) {
+            const int at = (cp >> 5) * kKeptHalf + v * 128 + ((((cp >> 2) & 7) ^ (v & 7)) << 4) + (cp & 3) * 4;
+            const float2 x = both(smem + at, DK * 256), d = both(smem + L::dS + at, DK * 256);
+            dot0 = fmaf(d.x, x.x, dot0), dot1 = fmaf(d.y, x.y, dot1);
+        }
+        products_done();
+        tmem_ld_frag(row + D1 + c0, dq);
+        if (DELTA) tmem_ld_frag(row + (16u << 16) + D1 + c0, dr);
+        tmem_ld_frag(row + D2 + cq * 16, da);
+        if (DELTA) tmem_ld_frag(row + (16u << 16) + D2 + cq * 16, dl);
+        {
+            uint4 x[4];
+#pragma unroll
+            for (int pl = 0; pl < UP; ++pl) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    x[i] = upper ? make_uint4(0u, 0u, 0u, 0u) : *reinterpret_cast<const uint4 *>(smem + L::U + pl * kChunk * 256 + kept_u_at(tok, v0 + 8 * i));
+                put_row(pl, x);
+            }
+        }
+        handed_over();
+        if (issuing()) {
+            tc_product<UP, 0, 2, 0, 2, true, 8, DK, 64, DK * 256, kKeptHalf>(tc.tmem + D3, tc.tmem + PA, sm + L::dS);
+            tc_commit(bar(3));
+        }
+        write_mats();  // (S_0's place, if so, is free: its product and the sums are behind the barrier)
+        products_done();
+        tmem_ld_frag(row + D3 + c0, dw);
+        tc_fence_before();
+        if (__syncthreads_or(!ok)) {  // a wait gave up: nothing of this chunk is valid
+            if (tid == 0) {
+                if (a.status) atomicOr(a.status, DELTALOG_STATUS_TIMEOUT);
+                for (int i = 0; i < 3; ++i) bounded_wait(bar(i), 0u, tc.abort_flag + 1);
+            }
+            cp_async_wait_all();
+            tc_teardown(tc, tid);
+            return;
+        }
+        if (tid < 32) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tc.tmem), "r"(kTmemCols));
+    } else {
+    const int slices = dv / kSlice;
+    load_stage(0), cp_async_commit();
+    if (L::kOwnQK) load_qk();
+    __syncthreads();  // beta
     for (int sl = 0; sl < slices; ++sl) {
         if (sl + 1 < slices) load_stage(sl + 1);
         cp_async_commit();
@@ -219,6 +376,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         }
         __syncthreads();
     }
+    }
     part[grp * DK + cp * 2] = dot0, part[grp * DK + cp * 2 + 1] = dot1;
     if (DELTA) {
         db += __shfl_xor_sync(0xffffffffu, db, 1);
@@ -227,27 +385,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         if ((tid & 7) == 0 && (tid >> 3) < p.valid) a.dbeta[(size_t)(p.tok0 + (tid >> 3)) * a.H + h] = db;
     }
     if (!VEC && !L::kOwnQK) load_qk(), cp_async_commit();
-    // dA and dL', masked; scalar decay multiplies e^(G_i - G_j) in here
-    if (cq <= mt) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int i = mt * 16 + g + 8 * half, j = cq * 16 + n * 8 + 2 * t;
-                float x[2], y[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float m = VEC ? 1.f : (j + e <= i ? decay_exp(decay_between(G[i], G[j + e])) : 0.f);
-                    const float raw = da[n][2 * half + e];
-                    if (i == j + e) diag[i] = raw * a.scale;
-                    if (EXCL && i == j + e + 1) near[i] = raw;
-                    x[e] = j + e + (EXCL ? 1 : 0) < i ? raw * m * a.scale : 0.f;
-                    y[e] = j + e < i ? -dl[n][2 * half + e] * m : 0.f;
-                }
-                *reinterpret_cast<float2 *>(da_f + i * MW + j) = make_float2(x[0], x[1]);
-                if (DELTA) *reinterpret_cast<float2 *>(dl_f + i * MW + j) = make_float2(y[0], y[1]);
-            }
-    }
+    if (!TC) write_mats();
     const bool whole = a.H == a.Hq;
     // results of element pair (row i, channels c, c + 1)
     auto put = [&](void *io_dst, float *part_dst, int i, int c, float x, float y) {

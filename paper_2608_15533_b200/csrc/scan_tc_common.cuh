@@ -172,6 +172,74 @@ __device__ __forceinline__ void tc_teardown(const TcBlock &b, int tid) {
     if (tid < 32) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(b.tmem), "r"(kTmemCols));
 }
 
+// ---- what the chains keep for the per-chunk gradients (bf16 io) ------------------------------------------------
+// Two planes take fp32's room and are operands as they stand.  States: images of 128 rows v, columns c, [plane][c / 64].
+// U: an image of 64 tokens by 128 columns v.  dV: rows of 128 columns.
+constexpr int kKeptHalf = 128 * 128;  // bytes of 64 columns of a state image
+template <int DK, int HC>
+__device__ __forceinline__ void keep_state_planes(void *dst, const float (&s)[HC], int v, int c0) {
+    unsigned char *base = static_cast<unsigned char *>(dst) + v * 128;
+#pragma unroll
+    for (int i = 0; i < HC; i += 8) {
+        const int c = c0 + i, unit = (c >> 3) & 7;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t w[2];
+            split_pair<2>(s[i + 2 * j], s[i + 2 * j + 1], w);
+            hi[j] = w[0], lo[j] = w[1];
+        }
+        unsigned char *at = base + (c >> 6) * kKeptHalf + ((unit ^ (v & 7)) << 4);
+        *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4 *>(at + DK * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+// Place of (token, column v) in U's image / dV's rows, in bytes.
+__device__ __forceinline__ int kept_u_at(int tok, int v) { return (v >> 6) * (kChunk * 128) + tok * 128 + ((((v >> 3) & 7) ^ (tok & 7)) << 4) + (v & 7) * 2; }
+__device__ __forceinline__ int kept_dv_at(int tok, int v) { return tok * 256 + v * 2; }
+// Values of column v for COUNT tokens from t0 on as planes.  Lanes in pairs: the even one takes a pair's first token, the odd
+// one its second, two neighbouring columns each.
+template <bool IMAGE, int COUNT>
+__device__ __forceinline__ void keep_value_planes(void *dst, const float (&u)[COUNT], int t0, int v) {
+    const bool odd = v & 1;
+#pragma unroll
+    for (int i = 0; i < COUNT; i += 2) {
+        const float got = __shfl_xor_sync(0xffffffffu, odd ? u[i] : u[i + 1], 1);
+        uint32_t w[2];
+        split_pair<2>(odd ? got : u[i], odd ? u[i + 1] : got, w);
+        const int tok = t0 + i + (odd ? 1 : 0), at = IMAGE ? kept_u_at(tok, v & ~1) : kept_dv_at(tok, v & ~1);
+        unsigned char *p = static_cast<unsigned char *>(dst) + at;
+        *reinterpret_cast<uint32_t *>(p) = w[0];
+        *reinterpret_cast<uint32_t *>(p + kChunk * 256) = w[1];
+    }
+}
+
+// 16 lanes x 8 N columns in the accumulator layout of mma.sync: x[n][0..1] lane t/4, columns 8 n + 2 (t % 4) + {0, 1}, x[n][2..3]
+// lane t/4 + 8.
+__device__ __forceinline__ void tmem_ld_frag(uint32_t addr, float (&x)[4][4]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i >> 2][i & 3] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld_frag(uint32_t addr, float (&x)[2][4]) {
+    uint32_t r[8];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+        "tcgen05.wait::ld.sync.aligned;\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = __uint_as_float(r[i]);
+}
+
 // A tile of 64 tokens x 128 columns of a bf16 tensor to and from shared memory, rows of 256 bytes.
 __device__ __forceinline__ void tc_load_rows(uint32_t dst, const __nv_bfloat16 *src, size_t stride, int valid, int tid) {
 #pragma unroll
