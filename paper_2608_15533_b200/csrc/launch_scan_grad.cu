@@ -6,7 +6,9 @@ namespace deltalog {
 namespace {
 
 template <int OP, int P, int DK, typename IO, bool TC>
-int launch_grad(const deltalog_desc *d, const ScanArgs &a, int rows, float *dbonus, cudaStream_t s) {
+int launch_grad(const deltalog_desc *d, const ScanArgs &args, int rows, float *dbonus, cudaStream_t s) {
+    ScanArgs a = args;
+    a.wave = device_info().sms;
     auto kernel = scan_grad_kernel<OP, P, DK, IO, TC>;
     const size_t smem = GradSmem<OP, P, DK, IO, TC>::bytes;
     if (int rc = ensure_smem(kernel, smem)) return rc;

@@ -59,6 +59,7 @@ struct ScanArgs {
     void *dq, *dk, *dv_out;
     float *dq_part, *dk_part;    // [tokens, H, d_k] where several value heads share one query / key head
     float *dg, *dbeta, *dbonus_part;
+    int32_t wave;                // CTAs of one wave
 };
 
 // Row and slot of a (sequence, head) unit; false when the unit has nothing to do.

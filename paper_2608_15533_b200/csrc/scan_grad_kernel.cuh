@@ -73,6 +73,34 @@ __device__ __forceinline__ void io_frag_b(uint32_t (&f)[kPlanes][4], const unsig
     frag_b(f, reinterpret_cast<const float *>(tile), kSliceStride, n0, k0, lane);
 }
 
+// A strongly decaying block's own pairs, one by one: for element (i, c) the sum over j <= i of mat_ij k_jc e^(G_i - G_j) ...
+// (Out of line, with pointers to the chunk's first token at channel c: rarely taken, and inlined at every element they pushed
+// the kernel out of the instruction cache.)
+template <typename IO, bool EXCL>
+__device__ __noinline__ float pairs_front(const IO *k, int k_stride, const float *gate, int g_stride, int valid, const float *mat, int w, int i) {
+    float s = 0.f, x = 0.f;
+    for (int j = i; j >= (i & ~(kBlock - 1)); --j) {
+        if (j < i && !(EXCL && j + 1 == i) && j + 1 < valid) x += gate[(size_t)(j + 1) * g_stride];
+        s = fmaf(j < valid ? mat[i * w + j] * to_f32(k[(size_t)j * k_stride]) : 0.f, expf(x), s);
+    }
+    return s;
+}
+// ... and over i >= j of (dA_ij q_ic + dL'_ij k_ic) e^(G_i - G_j).
+template <typename IO, bool EXCL, bool DELTA>
+__device__ __noinline__ float pairs_back(const IO *q, const IO *k, int k_stride, const float *gate, int g_stride, int valid, const float *da, const float *dl,
+                                         int w, int j) {
+    float s = 0.f, x = 0.f;
+    const int end = min((j & ~(kBlock - 1)) + kBlock, valid);
+    for (int i = j; i < end; ++i) {
+        const int m = EXCL ? i - 1 : i;  // the last gate that decays the pair
+        if (m > j) x += gate[(size_t)m * g_stride];
+        float y = da[i * w + j] * to_f32(q[(size_t)i * k_stride]);
+        if (DELTA) y = fmaf(dl[i * w + j], to_f32(k[(size_t)i * k_stride]), y);
+        s = fmaf(y, expf(x), s);
+    }
+    return s;
+}
+
 template <int OP, int P, int DK, typename IO, bool TC>
 struct GradSmem {
     static constexpr bool VEC = OpTraits<OP>::kVecDecay, DELTA = OpTraits<OP>::kDeltaRule;
@@ -194,6 +222,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         // Tensor memory: planes of A (of U later), [dO; dV] S_0^T, [dO; dV] U^T, U dS_1^T.
         constexpr uint32_t PA = 0, D1 = 128, D2 = 256, D3 = 320;
         constexpr int UP = DELTA ? 2 : 1;
+        const int tok = mt * 16 + (lane & 15), v0 = 32 * cq;  // this thread's row of A and columns
+        const bool upper = lane >= 16, inside = tok < p.valid;
+        uint4 hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hi[i] = lo[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (!upper && inside) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.dout) + v_off + (size_t)tok * v_stride + v0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[i] = src[i];
+        }
+        if (DELTA && upper) {
+            const unsigned char *src = reinterpret_cast<const unsigned char *>(a.dV + unit * kChunk * 128) + kept_dv_at(tok, v0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[i] = reinterpret_cast<const uint4 *>(src)[i], lo[i] = reinterpret_cast<const uint4 *>(src + kChunk * 256)[i];
+        }
         tc = tc_setup(smem + L::control, 4, tid);
         auto bar = [&](int i) { return tc.bars + 8u * i; };  // 0: S_0, 1: U, 2: dS_1, 3: products
         if (tid == 0) {
@@ -205,6 +248,18 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
             }
             mbar_arrive_expect_tx(bar(2), L::kState);
             bulk_copy_g2s(sm + L::dS, a.dS + unit * tile, L::kState, bar(2));
+            // One CTA fills an SM and begins by waiting for 200 KB.  What the CTA a wave further on will want goes from DRAM to
+            // L2 meanwhile (a CTA's wait 12k -> 5k cycles); the wave is 37 MB.
+            const size_t next = (size_t)h * gridDim.x + chunk + a.wave, ahead = next % gridDim.x * a.H + next / gridDim.x;
+            if (next < (size_t)gridDim.x * a.H) {
+                l2_prefetch(a.S + ahead * tile, L::kState), l2_prefetch(a.dS + ahead * tile, L::kState);
+                if (DELTA) l2_prefetch(a.U + ahead * kChunk * 128, 2 * kChunk * 256), l2_prefetch(a.dV + ahead * kChunk * 128, 2 * kChunk * 256);
+            }
+        }
+        if (VEC && tid >= 64 && tid < 128 && tid - 64 < p.valid) {  // read from there later on
+            const size_t at = p.tok0 + tid - 64;
+            l2_prefetch(a.g + (at * a.H + h) * DK, DK * 4);
+            l2_prefetch(static_cast<const IO *>(a.q) + (at * a.Hq + hq) * DK, DK * 2), l2_prefetch(static_cast<const IO *>(a.k) + (at * a.Hq + hq) * DK, DK * 2);
         }
         if constexpr (!DELTA && sizeof(IO) == 2) tc_load_operand<128, kChunk * 128>(sm + L::U, a.v, v_off, v_stride, p.valid, tid);
         if (L::kOwnQK) load_qk();
@@ -224,30 +279,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         };
         auto issuing = [&]() { return warp == 0 && __all_sync(0xffffffffu, ok) && elect_one(); };
         const uint32_t row = tc.tmem + ((uint32_t)(32 * mt) << 16);
-        const int tok = mt * 16 + (lane & 15), v0 = 32 * cq;  // this thread's row of A and columns
-        const bool upper = lane >= 16, inside = tok < p.valid;
         auto put_row = [&](int plane, const uint4 (&w)[4]) {
             const uint32_t x[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
             const uint32_t y[8] = {w[2].x, w[2].y, w[2].z, w[2].w, w[3].x, w[3].y, w[3].z, w[3].w};
             tmem_st8(row + PA + plane * 64 + v0 / 2, x), tmem_st8(row + PA + plane * 64 + v0 / 2 + 8, y);
         };
-        {
-            uint4 hi[4], lo[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) hi[i] = lo[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (!upper && inside) {
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.dout) + v_off + (size_t)tok * v_stride + v0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) hi[i] = src[i];
-            }
-            if (DELTA && upper) {
-                const unsigned char *src = reinterpret_cast<const unsigned char *>(a.dV + unit * kChunk * 128) + kept_dv_at(tok, v0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) hi[i] = reinterpret_cast<const uint4 *>(src)[i], lo[i] = reinterpret_cast<const uint4 *>(src + kChunk * 256)[i];
-            }
-            put_row(0, hi);
-            if (DELTA) put_row(1, lo);
-        }
+        put_row(0, hi);
+        if (DELTA) put_row(1, lo);
         if (!DELTA) cp_async_wait_all(), fence_async_proxy();  // v
         handed_over();
         ok = bounded_wait(bar(0), 0u, tc.abort_flag) && ok;
@@ -257,20 +295,26 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
             tc_product<UP, 0, UP, 0, 2, false, 8, kChunk, 64, kChunk * 256, kChunk * 128>(tc.tmem + D2, tc.tmem + PA, sm + L::U);
             tc_commit(bar(3));
         }
-        // meanwhile the sums of products: dbeta (eight threads a token), <dS_1, S_0> by channel
+        // meanwhile the sums of products: dbeta (by the threads that hold dV), <dS_1, S_0> by channel
         auto both = [&](const unsigned char *at, int plane) {  // a pair of values of two planes
             const uint32_t x = *reinterpret_cast<const uint32_t *>(at), y = *reinterpret_cast<const uint32_t *>(at + plane);
             return make_float2(bf16_lo(x) + bf16_lo(y), bf16_hi(x) + bf16_hi(y));
         };
-        if (DELTA) {
-            const int i = tid >> 3, v = (tid & 7) * 16;
-            const float rb = 1.f / beta[i];
-            const unsigned char *d = reinterpret_cast<const unsigned char *>(a.dV + unit * kChunk * 128);
+        if (DELTA && upper) {
+            const float rb = 1.f / beta[tok];
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const float2 x = both(smem + L::U + kept_u_at(i, v + j), kChunk * 256), y = both(d + kept_dv_at(i, v + j), kChunk * 256);
-                db = fmaf(x.x * rb, y.x * rb, db), db = fmaf(x.y * rb, y.y * rb, db);
+            for (int i = 0; i < 4; ++i) {
+                const unsigned char *at = smem + L::U + kept_u_at(tok, v0 + 8 * i);
+                const uint4 uh = *reinterpret_cast<const uint4 *>(at), ul = *reinterpret_cast<const uint4 *>(at + kChunk * 256);
+                const uint32_t x[4] = {uh.x, uh.y, uh.z, uh.w}, y[4] = {ul.x, ul.y, ul.z, ul.w};
+                const uint32_t d[4] = {hi[i].x, hi[i].y, hi[i].z, hi[i].w}, e[4] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    db = fmaf((bf16_lo(x[j]) + bf16_lo(y[j])) * rb, (bf16_lo(d[j]) + bf16_lo(e[j])) * rb, db);
+                    db = fmaf((bf16_hi(x[j]) + bf16_hi(y[j])) * rb, (bf16_hi(d[j]) + bf16_hi(e[j])) * rb, db);
+                }
             }
+            rows[cq * kChunk + tok] = db;
         }
         ok = bounded_wait(bar(2), 0u, tc.abort_flag) && ok;
         for (int v = grp; v < 128; v += kGroups) {
@@ -378,12 +422,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
     }
     }
     part[grp * DK + cp * 2] = dot0, part[grp * DK + cp * 2 + 1] = dot1;
-    if (DELTA) {
+    if (DELTA && !TC) {
         db += __shfl_xor_sync(0xffffffffu, db, 1);
         db += __shfl_xor_sync(0xffffffffu, db, 2);
         db += __shfl_xor_sync(0xffffffffu, db, 4);
         if ((tid & 7) == 0 && (tid >> 3) < p.valid) a.dbeta[(size_t)(p.tok0 + (tid >> 3)) * a.H + h] = db;
     }
+    if (DELTA && TC && tid < p.valid)  // (the quarters' sums met at a barrier)
+        a.dbeta[(size_t)(p.tok0 + tid) * a.H + h] = (rows[tid] + rows[kChunk + tid]) + (rows[2 * kChunk + tid] + rows[3 * kChunk + tid]);
     if (!VEC && !L::kOwnQK) load_qk(), cp_async_commit();
     if (!TC) write_mats();
     const bool whole = a.H == a.Hq;
@@ -554,85 +600,77 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         __syncthreads();
         if (mine) eB[blk * DK + c] = decay_exp(Bc);
         __syncthreads();
-        float acc[NT][4], dia[NT][4];
         // sum over blocks J < mt (towards the front) or I > mt (towards the back) of a row block's pairs, the decay of the
         // blocks in between multiplied in by Horner's rule, then the block's own pairs
-        auto zero = [&](float (&x)[NT][4]) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
-        };
-        auto times_block = [&](float (&x)[NT][4], const float *table, int b) {
+        float acc[NT][4] = {}, acc_l[NT][4] = {};
+        auto times_block = [&](float (&x)[NT][4], int b) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float2 d = *reinterpret_cast<const float2 *>(table + b * DK + c0 + n * 8 + 2 * t);
+                const float2 d = *reinterpret_cast<const float2 *>(eB + b * DK + c0 + n * 8 + 2 * t);
                 x[n][0] *= d.x, x[n][1] *= d.y, x[n][2] *= d.x, x[n][3] *= d.y;
             }
         };
-        auto product = [&](float (&x)[NT][4], const float *mat, bool transposed, int b_, const float *vec) {
-            uint32_t m[kPlanes][4];
-            if (transposed) frag_a_t(m, mat, MW, b_ * 16, mt * 16, lane);
-            else frag_a(m, mat, MW, mt * 16, b_ * 16, lane);
+        // the 16 tokens of block b_ of a decayed vector as operand B; of the warp's own block times e^(-B)
+        auto vector_frag = [&](uint32_t (&b)[kPlanes][4], const float *vec, int b_, int nn) {
+            const int c = c0 + nn * 16 + g;
+            const float f0 = b_ == mt ? eI[mt * DK + c] : 1.f, f1 = b_ == mt ? eI[mt * DK + c + 8] : 1.f;
+            const float *at = vec + (b_ * 16 + 2 * t) * SW + c;
+            frag_pair(b, 0, at[0] * f0, at[SW] * f0), frag_pair(b, 1, at[8 * SW] * f0, at[9 * SW] * f0);
+            frag_pair(b, 2, at[8] * f1, at[SW + 8] * f1), frag_pair(b, 3, at[8 * SW + 8] * f1, at[9 * SW + 8] * f1);
+        };
+        const bool own_deep = deep[mt] != 0;
+        const IO *q0 = static_cast<const IO *>(a.q) + ((size_t)p.tok0 * a.Hq + hq) * DK, *k0 = static_cast<const IO *>(a.k) + ((size_t)p.tok0 * a.Hq + hq) * DK;
+        const float *g0 = a.g + ((size_t)p.tok0 * a.H + h) * DK;
+        // dq, and dk as read: x <- sign e^G x + e^p (pairs inside the chunk), both over the same k
+        for (int J = 0; J <= mt; ++J) {
+            if (J == mt && own_deep) break;
+            if (J && J < mt) {
+                times_block(acc, J);
+                if (DELTA) times_block(acc_l, J);
+            }
+            uint32_t m[kPlanes][4], l[kPlanes][4];
+            frag_a(m, da_f, MW, mt * 16, J * 16, lane);
+            if (DELTA) frag_a(l, dl_f, MW, mt * 16, J * 16, lane);
 #pragma unroll
             for (int nn = 0; nn < NT / 2; ++nn) {
                 uint32_t b[kPlanes][4];
-                frag_b_t(b, vec, SW, b_ * 16, c0 + nn * 16, lane);
-                mma_all(x[2 * nn], x[2 * nn + 1], m, b);
+                vector_frag(b, kc, J, nn);
+                mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
+                if (DELTA) mma_all(acc_l[2 * nn], acc_l[2 * nn + 1], l, b);
             }
-        };
-        // a strongly decaying block's own pairs, one by one: for element (i, c) the sum over j of mat[i][j] k_jc e^(..),
-        // or over the later rows
-        auto pairs_front = [&](const float *mat, int i, int ch) {  // sum_(j <= i) mat_ij k_jc e^(G_i - G_j)
-            float s = 0.f, x = 0.f;
-            for (int j = i; j >= mt * 16; --j) {
-                if (j < i && !(EXCL && j + 1 == i)) x += gate_at(j + 1, ch);
-                s = fmaf(mat[i * MW + j] * raw(a.k, j, ch), expf(x), s);
-            }
-            return s;
-        };
-        auto pairs_back = [&](int j, int ch) {  // sum_(i >= j) (dA_ij q_ic + dL'_ij k_ic) e^(G_i - G_j)
-            float s = 0.f, x = 0.f;
-            for (int i = j; i < mt * 16 + 16; ++i) {
-                if (i > j && !EXCL) x += gate_at(i, ch);
-                if (EXCL && i > j + 1) x += gate_at(i - 1, ch);
-                float w = da_f[i * MW + j] * raw(a.q, i, ch);
-                if (DELTA) w = fmaf(dl_f[i * MW + j], raw(a.k, i, ch), w);
-                s = fmaf(w, expf(x), s);
-            }
-            return s;
-        };
-        const bool own_deep = deep[mt] != 0;
-        // dq (and dk as read): x <- sign e^G x + e^p (pairs inside the chunk)
-        auto towards_front = [&](float (&x)[NT][4], const float *mat, float sign) {
-            zero(acc), zero(dia);
-            for (int J = 0; J < mt; ++J) {
-                if (J) times_block(acc, eB, J);
-                product(acc, mat, false, J, kc);
-            }
-            if (!own_deep) product(dia, mat, false, mt, kc), times_block(dia, eI, mt);
+        }
+        auto finish_front = [&](float (&x)[NT][4], float (&in)[NT][4], const float *mat, float sign) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = mt * 16 + g + 8 * (e >> 1), ch = c0 + n * 8 + 2 * t + (e & 1);
-                    x[n][e] = ps[i * SW + ch] * fmaf(sign * front[mt * DK + ch], x[n][e], acc[n][e] + dia[n][e]);
-                    if (own_deep) x[n][e] += pairs_front(mat, i, ch);
+                    x[n][e] = ps[i * SW + ch] * fmaf(sign * front[mt * DK + ch], x[n][e], in[n][e]);
+                    if (own_deep) x[n][e] += pairs_front<IO, EXCL>(k0 + ch, a.Hq * DK, g0 + ch, a.H * DK, p.valid, mat, MW, i);
+                    in[n][e] = 0.f;
                 }
         };
-        towards_front(dq, da_f, a.scale);
-        if (DELTA) towards_front(dr, dl_f, -1.f);
+        finish_front(dq, acc, da_f, a.scale);
+        if (DELTA) finish_front(dr, acc_l, dl_f, -1.f);
         // dk as written: behind the chunk (dw), inside it (acc)
-        zero(acc), zero(dia);
-        for (int I = 3; I > mt; --I) {
-            if (I < 3) times_block(acc, eB, I);
-            product(acc, da_f, true, I, qs);
-            if (DELTA) product(acc, dl_f, true, I, ks);
-        }
-        if (!own_deep) {
-            product(dia, da_f, true, mt, qs);
-            if (DELTA) product(dia, dl_f, true, mt, ks);
-            times_block(dia, eI, mt);
+        for (int I = 3; I >= mt; --I) {
+            if (I == mt && own_deep) break;
+            if (I < 3 && I > mt) times_block(acc, I);
+            uint32_t m[kPlanes][4], b[kPlanes][4];
+            frag_a_t(m, da_f, MW, I * 16, mt * 16, lane);
+#pragma unroll
+            for (int nn = 0; nn < NT / 2; ++nn) {
+                vector_frag(b, qs, I, nn);
+                mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
+            }
+            if (DELTA) {
+                frag_a_t(m, dl_f, MW, I * 16, mt * 16, lane);
+#pragma unroll
+                for (int nn = 0; nn < NT / 2; ++nn) {
+                    vector_frag(b, ks, I, nn);
+                    mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
+                }
+            }
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -652,8 +690,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
                 for (int e = 0; e < 2; ++e) {
                     const int el = 2 * r + e;
                     const float es = ss[i * SW + ch + e];
-                    float in = es * (acc[n][el] + dia[n][el]);
-                    if (own_deep) in += pairs_back(i, ch + e);
+                    float in = es * acc[n][el];
+                    if (own_deep) in += pairs_back<IO, EXCL, DELTA>(q0 + ch + e, k0 + ch + e, a.Hq * DK, g0 + ch + e, a.H * DK, p.valid, da_f, dl_f, MW, i);
                     const float out = back[mt * DK + ch + e] * es * dw[n][el];
                     const float qe = e ? qv.y : qv.x, ke = e ? kv.y : kv.x;
                     // the readout of RWKV6 sees the decays in front of its token only: its term belongs to the token before

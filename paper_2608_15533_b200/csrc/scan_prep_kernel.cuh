@@ -343,22 +343,20 @@ struct PrepVectorSmem {
     static constexpr size_t bytes(bool delta) { return small(delta) + kChunk * 4 + 16; }
 };
 
-// One pair (i, j) of a strongly decaying block: sum_c x_ic k_jc e^(g_(j+1) + .. + g_i) with the gates added up directly.
+// One pair (i, j) of a strongly decaying block: sum_c x_ic k_jc e^(g_(j+1) + .. + g_i) with the gates added up directly,
+// for x = q and x = k.  (Out of line: rarely taken, large.)
 template <typename IO, bool EXCL>
-__device__ __forceinline__ void pair_sums(const ScanArgs &a, const ChunkPlace &p, int h, int hq, int DK, int i, int j, float &sq, float &sk) {
-    sq = sk = 0.f;
-    if (i >= p.valid) return;
-    const size_t ri = ((size_t)(p.tok0 + i) * a.Hq + hq) * DK, rj = ((size_t)(p.tok0 + j) * a.Hq + hq) * DK;
+__device__ __noinline__ float2 pair_sums(const IO *q, const IO *k, int stride, const float *gate, int g_stride, int valid, int DK, int i, int j) {
+    float sq = 0.f, sk = 0.f;
+    if (i >= valid) return make_float2(0.f, 0.f);
     for (int c = 0; c < DK; ++c) {
-        float s = 0.f, last = 0.f;
-        for (int m = j + 1; m <= i; ++m) {
-            last = a.g[((size_t)(p.tok0 + m) * a.H + h) * DK + c];
-            if (!EXCL || m < i) s += last;
-        }
-        const float kj = to_f32(static_cast<const IO *>(a.k)[rj + c]);
-        sq = fmaf(to_f32(static_cast<const IO *>(a.q)[ri + c]) * kj, expf(s), sq);
-        sk = fmaf(to_f32(static_cast<const IO *>(a.k)[ri + c]) * kj, expf(s), sk);
+        float s = 0.f;
+        for (int m = j + 1; m <= (EXCL ? i - 1 : i); ++m) s += gate[(size_t)m * g_stride + c];
+        const float kj = to_f32(k[(size_t)j * stride + c]);
+        sq = fmaf(to_f32(q[(size_t)i * stride + c]) * kj, expf(s), sq);
+        sk = fmaf(to_f32(k[(size_t)i * stride + c]) * kj, expf(s), sk);
     }
+    return make_float2(sq, sk);
 }
 
 // OP selects the readout (RWKV6) and the delta rule; one thread per block and channel pair, so 256 or 128.
@@ -475,10 +473,11 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
                 for (int e = 0; e < 4; ++e) {
                     const int i = I * kBlock + g + 8 * (e >> 1), j = J * kBlock + n * 8 + 2 * t + (e & 1);
                     if (j <= i) {
-                        float sq, sk;
-                        pair_sums<IO, EXCL>(a, p, h, hq, DK, i, j, sq, sk);
-                        acc[round][0][n][e] = sq * a.scale;
-                        if (DELTA) acc[round][kMats - 1][n][e] = sk;
+                        const size_t at = ((size_t)p.tok0 * a.Hq + hq) * DK;
+                        const float2 x = pair_sums<IO, EXCL>(static_cast<const IO *>(a.q) + at, static_cast<const IO *>(a.k) + at, a.Hq * DK,
+                                                             a.g + ((size_t)p.tok0 * a.H + h) * DK, a.H * DK, p.valid, DK, i, j);
+                        acc[round][0][n][e] = x.x * a.scale;
+                        if (DELTA) acc[round][kMats - 1][n][e] = x.y;
                     }
                 }
         }

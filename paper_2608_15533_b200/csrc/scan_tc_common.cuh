@@ -214,6 +214,9 @@ __device__ __forceinline__ void keep_value_planes(void *dst, const float (&u)[CO
     }
 }
 
+__device__ __forceinline__ void l2_prefetch(const void *p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(p), "r"(bytes) : "memory");
+}
 // 16 lanes x 8 N columns in the accumulator layout of mma.sync: x[n][0..1] lane t/4, columns 8 n + 2 (t % 4) + {0, 1}, x[n][2..3]
 // lane t/4 + 8.
 __device__ __forceinline__ void tmem_ld_frag(uint32_t addr, float (&x)[4][4]) {
