@@ -83,9 +83,9 @@ int resident_ctas(K kernel, int threads, size_t smem) {
 // the kernel in front of this one on the stream does not write this state's base tiles, so this
 // kernel's CTAs may start, and request base tiles, while that kernel is still retiring.
 template <typename K, typename... Args>
-int launch_chained(K kernel, int grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+int launch_chained(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(grid);
+    lc.gridDim = grid;
     lc.blockDim = dim3(threads);
     lc.dynamicSmemBytes = smem;
     lc.stream = stream;

@@ -18,10 +18,12 @@ extern "C" int deltalog_build_plan(const int32_t *lens, const int32_t *slots, co
     // a thread's share of the tables: four tokens and a row or so each, one wave of CTAs at most
     const long long work = (plan->token_seq ? (plan->max_tokens + 3ll) / 4 : 0) + a.n + a.max_chunks;
     const long long ctas = (work + kPlanThreads - 1) / kPlanThreads;
-    const int grid = (int)(ctas < 1 ? 1 : ctas > device_info().sms ? device_info().sms : ctas);
     if (a.n <= kPlanShared) {
-        // few rows and tokens: fewer threads meet at the barriers sooner
-        const int threads = a.n <= 256 && work <= 1024 ? 256 : kPlanThreads;
+        // few rows: fewer threads meet at the barriers sooner (512 requests, 50k tokens: 8.4 us with 1024, 7.3 us with 512;
+        // 20k requests: 38 us with 512, 26 us with 1024)
+        const int threads = a.n <= 256 && work <= 1024 ? 256 : a.n <= 4096 ? 512 : kPlanThreads;
+        const long long need = (work + threads - 1) / threads;
+        const int grid = (int)(need < 1 ? 1 : need > device_info().sms ? device_info().sms : need);
         const size_t smem = (size_t)2 * (a.n + 1) * sizeof(int32_t);
         if (int rc = ensure_smem(plan_kernel, smem)) return rc;
         plan_kernel<<<grid, threads, smem, s>>>(a);
@@ -29,6 +31,7 @@ extern "C" int deltalog_build_plan(const int32_t *lens, const int32_t *slots, co
     }
     plan_offsets_kernel<<<1, 1024, 0, s>>>(a);
     if (int rc = finish_launch()) return rc;
+    const int grid = (int)(ctas > device_info().sms ? device_info().sms : ctas);
     plan_tables_kernel<<<grid, kPlanThreads, 0, s>>>(a);
     return finish_launch();
 }

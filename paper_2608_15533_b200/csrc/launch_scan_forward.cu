@@ -11,8 +11,7 @@ int launch_chain(const ScanArgs &a, cudaStream_t s) {
     const int warps = scan_chain_warps(a.n * a.H, a.dv);
     const size_t smem = ForwardSmem<VEC, P, DK, DELTA, IO>::bytes(warps);
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<dim3(a.n * a.H, a.dv / 16 / warps), warps * 32, smem, s>>>(a);
-    return finish_launch();
+    return launch_chained(kernel, dim3(a.n * a.H, a.dv / 16 / warps), warps * 32, smem, s, a);
 }
 
 }  // namespace

@@ -11,8 +11,7 @@ int launch_chain(const ScanArgs &a, cudaStream_t s) {
     constexpr size_t smem = ForwardTcSmem<VEC, P, DK, DELTA, IO>::bytes;
     static_assert(smem <= 227 * 1024, "shared memory of one SM");
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<a.n * a.H, kTcThreads, smem, s>>>(a);
-    return finish_launch();
+    return launch_chained(kernel, dim3(a.n * a.H), kTcThreads, smem, s, a);
 }
 
 }  // namespace

@@ -12,20 +12,16 @@ int launch_grad(const deltalog_desc *d, const ScanArgs &args, int rows, float *d
     auto kernel = scan_grad_kernel<OP, P, DK, IO, TC>;
     const size_t smem = GradSmem<OP, P, DK, IO, TC>::bytes;
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<dim3(a.max_chunks, a.H), kGradThreads, smem, s>>>(a);
-    if (int rc = finish_launch()) return rc;
+    if (int rc = launch_chained(kernel, dim3(a.max_chunks, a.H), kGradThreads, smem, s, a)) return rc;
     const int sms = device_info().sms;
     if (a.H != a.Hq) {
-        scan_group_sum_kernel<IO><<<sms * 8, 256, 0, s>>>(a, DK);
-        if (int rc = finish_launch()) return rc;
+        if (int rc = launch_chained(scan_group_sum_kernel<IO>, dim3(sms * 8), 256, 0, s, a, DK)) return rc;
     }
     if (OP == DELTALOG_RWKV6) {
-        scan_bonus_sum_kernel<<<a.H, 256, 0, s>>>(a, DK, dbonus);
-        if (int rc = finish_launch()) return rc;
+        if (int rc = launch_chained(scan_bonus_sum_kernel, dim3(a.H), 256, 0, s, a, DK, dbonus)) return rc;
     }
     const int e = (int)sizeof(IO), gate = op_has_gate(d->op) ? 4 * a.H * (op_vec_decay(d->op) ? DK : 1) : 0;
-    scan_tail_kernel<<<sms, 256, 0, s>>>(a, rows, a.Hq * DK * e, a.H * a.dv * e, gate, op_delta_rule(d->op) ? 4 * a.H : 0);
-    return finish_launch();
+    return launch_chained(scan_tail_kernel, dim3(sms), 256, 0, s, a, rows, a.Hq * DK * e, a.H * a.dv * e, gate, op_delta_rule(d->op) ? 4 * a.H : 0);
 }
 
 template <int OP>

@@ -10,8 +10,7 @@ int launch_scalar(const ScanArgs &a, cudaStream_t s) {
     auto kernel = scan_prep_scalar_kernel<P, DK, DELTA, IO>;
     const size_t smem = PrepScalarSmem<P, DK>::bytes(DELTA);
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<dim3(a.max_chunks + 1, a.H), 128, smem, s>>>(a);
-    return finish_launch();
+    return launch_chained(kernel, dim3(a.max_chunks + 1, a.H), 128, smem, s, a);
 }
 
 template <int OP, int DK, typename IO>
@@ -19,8 +18,7 @@ int launch_vector(const ScanArgs &a, cudaStream_t s) {
     auto kernel = scan_prep_vector_kernel<OP, DK, IO>;
     const size_t smem = PrepVectorSmem<DK>::bytes(OpTraits<OP>::kDeltaRule);
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    kernel<<<dim3(a.max_chunks + 1, a.H), 2 * DK, smem, s>>>(a);
-    return finish_launch();
+    return launch_chained(kernel, dim3(a.max_chunks + 1, a.H), 2 * DK, smem, s, a);
 }
 
 template <int OP>

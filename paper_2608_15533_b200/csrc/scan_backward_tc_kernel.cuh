@@ -46,6 +46,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_backward_tc_kernel(const S
     const uint32_t sm = smem_addr(smem_tc);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int v = 32 * (warp & 3) + lane, f = warp >> 2;
+    scan_kernel_begin();
     const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
     const int chunk0 = a.chunk_starts[seq];

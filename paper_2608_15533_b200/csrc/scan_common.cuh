@@ -62,6 +62,14 @@ struct ScanArgs {
     int32_t wave;                // CTAs of one wave
 };
 
+// The scan's kernels follow one another on the stream and are launched so that a kernel's CTAs may be set up while the one in
+// front retires (a microsecond or two per kernel, which short prompts notice).  First thing, each waits until
+// everything in front of it is complete and visible, and then lets its successor be set up.
+__device__ __forceinline__ void scan_kernel_begin() {
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+}
+
 // Row and slot of a (sequence, head) unit; false when the unit has nothing to do.
 __device__ __forceinline__ bool scan_slot(const ScanArgs &a, int seq, int tid, int &slot) {
     if (!a.slots) {

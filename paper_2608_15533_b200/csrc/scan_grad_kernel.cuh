@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), chunk = blockIdx.x, h = blockIdx.y;
     const int g = lane >> 2, t = lane & 3, mt = warp & 3, cq = warp >> 2, c0 = cq * (DK / 4);
+    scan_kernel_begin();
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) return;
     const int dv = a.dv, hq = h / (a.H / a.Hq);
@@ -759,6 +760,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
 // dq, dk of heads that several value heads share: the sum over them, in order.
 template <typename IO>
 __global__ void __launch_bounds__(256) scan_group_sum_kernel(const ScanArgs a, int dk) {
+    scan_kernel_begin();
     const int tokens = a.starts[a.n], rep = a.H / a.Hq, upr = dk / 4;
     const size_t total = (size_t)tokens * a.Hq * upr;
     for (size_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += gridDim.x * 256ull) {
@@ -779,6 +781,7 @@ __global__ void __launch_bounds__(256) scan_group_sum_kernel(const ScanArgs a, i
 
 // Bonus gradient: the chunks' parts summed in order, one CTA per head.
 __global__ void __launch_bounds__(256) scan_bonus_sum_kernel(const ScanArgs a, int dk, float *dbonus) {
+    scan_kernel_begin();
     __shared__ float s[256];
     const int h = blockIdx.x, c = threadIdx.x % dk, lane = threadIdx.x / dk, lanes = 256 / dk;
     const int chunks = a.chunk_starts[a.n];
@@ -794,6 +797,7 @@ __global__ void __launch_bounds__(256) scan_bonus_sum_kernel(const ScanArgs a, i
 
 // Gradient rows behind the last sequence are zero.
 __global__ void __launch_bounds__(256) scan_tail_kernel(const ScanArgs a, int rows, int qk_bytes, int v_bytes, int g_bytes, int beta_bytes) {
+    scan_kernel_begin();
     const int first = a.starts[a.n];
     auto clear = [&](void *p, int row_bytes) {
         if (!p || !row_bytes) return;

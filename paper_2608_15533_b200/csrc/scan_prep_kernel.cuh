@@ -131,8 +131,7 @@ __device__ __forceinline__ float decay_between(const float2 &i, const float2 &j)
 
 // Rows of the plan, the longest first (sorted by chunks, those of 511 and more together): what the chain kernels run
 // through.  A chain's time is its length, and the longest one started last would run alone at the end.
-__device__ __forceinline__ void order_rows(const ScanArgs &a, int tid, int nthreads) {
-    __shared__ int bins[512];
+__device__ __forceinline__ void order_rows(const ScanArgs &a, int *bins, int tid, int nthreads) {  // bins: 512, shared
     for (int i = tid; i < 512; i += nthreads) bins[i] = 0;
     __syncthreads();
     auto bin = [&](int i) { return 511 - min(511, a.chunk_starts[i + 1] - a.chunk_starts[i]); };
@@ -172,8 +171,9 @@ __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(c
     using L = PrepScalarSmem<P, DK>;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
+    scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
-        if (h == 0) order_rows(a, tid, 128);
+        if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 128);
         return;
     }
     ChunkPlace p;
@@ -339,7 +339,7 @@ struct PrepVectorSmem {
     static constexpr int kVec = kChunk * kVS * 4;
     // q e^p, k e^s, (delta rule) k e^p, in whose place N and T come later; factors between blocks.  Two CTAs share an SM.
     __host__ __device__ static constexpr int factors(bool delta) { return (delta ? 3 : 2) * kVec; }
-    __host__ __device__ static constexpr int small(bool delta) { return factors(delta) + 11 * DK * 4; }
+    __host__ __device__ static constexpr int small(bool delta) { return factors(delta) + 19 * DK * 4; }
     static constexpr size_t bytes(bool delta) { return small(delta) + kChunk * 4 + 16; }
 };
 
@@ -367,8 +367,9 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     constexpr int VS = L::kVS;
     extern __shared__ __align__(128) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunk = blockIdx.x, h = blockIdx.y;
+    scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
-        if (h == 0) order_rows(a, tid, 2 * DK);
+        if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 2 * DK);
         return;
     }
     ChunkPlace p;
@@ -378,6 +379,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     float *qs = reinterpret_cast<float *>(smem), *kc = qs + kChunk * VS, *ks = kc + kChunk * VS;
     float *B = reinterpret_cast<float *>(smem + L::factors(DELTA));  // [4][DK] block decays
     float *F = B + 4 * DK;                                          // [7][DK] e^(-B_I), e^(B_1), e^(B_2), e^(B_1 + B_2)
+    float *W = F + 7 * DK;                                          // [2][4][DK] decay of the chunk in front of / behind a block
     float *beta = reinterpret_cast<float *>(smem + L::small(DELTA));
     int *deep = reinterpret_cast<int *>(beta + kChunk);             // [4] blocks that decay too far for the factored form
     float *T = reinterpret_cast<float *>(smem), *N = T + kChunk * kInvStride;
@@ -411,21 +413,8 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
             if (m < blk) front.x += x.x, front.y += x.y;
             if (m > blk) back.x += x.x, back.y += x.y;
         }
-        front = make_float2(decay_exp(front.x), decay_exp(front.y)), back = make_float2(decay_exp(back.x), decay_exp(back.y));
-        const size_t base = unit * kPlanes * kChunk * DK;
-#pragma unroll
-        for (int r = 0; r < kBlock; ++r) {
-            const size_t at = base + image_at(blk * kBlock + r, c);
-            const int own = (blk * kBlock + r) * VS + c;
-            float2 x = *reinterpret_cast<const float2 *>(qs + own);
-            put_planes(a.qt + at, kChunk * DK, x.x * front.x, x.y * front.y, all);
-            if (DELTA) {
-                x = *reinterpret_cast<const float2 *>(ks + own);
-                put_planes(a.kt + at, kChunk * DK, x.x * front.x, x.y * front.y);
-            }
-            x = *reinterpret_cast<const float2 *>(kc + own);
-            put_planes(a.kh + at, kChunk * DK, x.x * back.x, x.y * back.y);
-        }
+        *reinterpret_cast<float2 *>(W + blk * DK + c) = make_float2(decay_exp(front.x), decay_exp(front.y));
+        *reinterpret_cast<float2 *>(W + (4 + blk) * DK + c) = make_float2(decay_exp(back.x), decay_exp(back.y));
         const float2 b = *reinterpret_cast<const float2 *>(B + blk * DK + c);
         *reinterpret_cast<float2 *>(F + blk * DK + c) = make_float2(expf(-b.x), expf(-b.y));
         if (blk == 1 || blk == 2) *reinterpret_cast<float2 *>(F + (3 + blk) * DK + c) = make_float2(decay_exp(b.x), decay_exp(b.y));
@@ -435,6 +424,34 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
         }
     }
     __syncthreads();
+    // the whole chunk's decayed vectors, eight channels of a token at a time: 16-byte stores, one per plane
+    {
+        const size_t base = unit * kPlanes * kChunk * DK;
+        auto write = [&](__nv_bfloat16 *dst, const float *vec, const float *factor, int i, int c8, bool three) {
+            uint32_t w[kPlanes][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 x = *reinterpret_cast<const float4 *>(vec + i * VS + c8 + 4 * j), y = *reinterpret_cast<const float4 *>(factor + (i >> 4) * DK + c8 + 4 * j);
+                uint32_t z[kPlanes];
+                split_pair<kPlanes>(x.x * y.x, x.y * y.y, z);
+#pragma unroll
+                for (int pl = 0; pl < kPlanes; ++pl) w[pl][2 * j] = z[pl];
+                split_pair<kPlanes>(x.z * y.z, x.w * y.w, z);
+#pragma unroll
+                for (int pl = 0; pl < kPlanes; ++pl) w[pl][2 * j + 1] = z[pl];
+            }
+#pragma unroll
+            for (int pl = 0; pl < kPlanes; ++pl)
+                if (pl < 2 || three) *reinterpret_cast<uint4 *>(dst + base + pl * kChunk * DK + image_at(i, c8)) = make_uint4(w[pl][0], w[pl][1], w[pl][2], w[pl][3]);
+        };
+#pragma unroll 1
+        for (int n = tid; n < kChunk * DK / 8; n += kThreads) {
+            const int i = n / (DK / 8), c8 = n % (DK / 8) * 8;
+            write(a.qt, qs, W, i, c8, all);
+            if (DELTA) write(a.kt, ks, W, i, c8, true);
+            write(a.kh, kc, W + 4 * DK, i, c8, true);
+        }
+    }
     if (tid < DK) a.decay[unit * DK + tid] = expf(B[tid] + B[DK + tid] + B[2 * DK + tid] + B[3 * DK + tid]);
     // block pairs (I, J <= I) of A and L, 16 x 16 each, one warp per pair
     __nv_bfloat16 *A = a.A + unit * kPlanes * kChunk * kChunk;
