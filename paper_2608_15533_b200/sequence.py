@@ -9,6 +9,7 @@ fp32 log-decay, ``beta [tokens, H]`` fp32, ``u_bonus [H, d_k]`` fp32; ``plan.sta
 from __future__ import annotations
 
 import ctypes
+import weakref
 from dataclasses import dataclass
 from typing import Optional, Tuple
 
@@ -18,13 +19,7 @@ from . import binding
 from .binding import BF16, F32, RWKV6, Desc, State, _DELTA_RULE, _DT_TO_TORCH, _check, _Plan, _ScanGrads, _VEC_DECAY, load_library
 
 SCAN_CHUNK = 64
-
-
-def _stream_of(stream, device) -> int:
-    """The stream that was asked for, or the current stream of the tensors' device."""
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+_STATE_FIELDS = ("num_slots", "H", "d_k", "d_v", "cap", "d_lambda", "base_dtype", "klog_dtype", "ulog_dtype")
 
 
 def _want(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optional[int]:
@@ -42,19 +37,32 @@ def _want(name: str, t: Optional[torch.Tensor], shape, dtype, device) -> Optiona
 
 
 class _on:
-    """The device made current around a call, where it is not already."""
+    """A call's device and stream made current around it, where they are not already: the call's own buffers then belong to
+    the stream that its kernels run on.  Yields the stream's handle."""
 
-    __slots__ = ("index", "before")
+    __slots__ = ("index", "stream", "before")
 
-    def __init__(self, device):
-        self.index = device.index
+    def __init__(self, device, stream):
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+            stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream: the tensors are on {device}, the stream is of {stream.device}")
+        self.index, self.stream = device.index, stream
 
     def __enter__(self):
         self.before = torch.cuda.current_device()
         if self.before != self.index:
             torch.cuda.set_device(self.index)
+        if self.stream is None:
+            return torch.cuda.current_stream().cuda_stream
+        self.stream, asked = torch.cuda.current_stream(), self.stream
+        torch.cuda.set_stream(asked)
+        return asked.cuda_stream
 
     def __exit__(self, *exc):
+        if self.stream is not None:
+            torch.cuda.set_stream(self.stream)
         if self.before != self.index:
             torch.cuda.set_device(self.before)
 
@@ -110,9 +118,9 @@ def build_plan(lens: torch.Tensor, plan: Plan, slots: Optional[torch.Tensor] = N
         p_log = _want("log_len", log_len, (None, None), torch.int32, dev)
         num, H = log_len.shape
     _gpu(dev)
-    with _on(dev):
+    with _on(dev, stream) as handle:
         rc = load_library().deltalog_build_plan(p_lens if plan.n else None, p_slots, p_log, int(H), int(cap), int(num), int(bool(decode_rows)),
-                                                ctypes.byref(plan.c_struct()), _stream_of(stream, dev))
+                                                ctypes.byref(plan.c_struct()), handle)
     _check(rc, "deltalog_build_plan")
     plan.builds += 1
     return plan
@@ -155,6 +163,14 @@ def _workspace(desc, plan, workspace, train) -> torch.Tensor:
     return workspace
 
 
+def _out(out, tk: _Tokens, make: bool = False) -> Optional[torch.Tensor]:
+    """The caller's output tensor, checked; a new one in its place with ``make``."""
+    if out is None:
+        return torch.empty(tk.out_shape, dtype=tk.io, device=tk.device) if make else None
+    _want("out", out, tk.out_shape, tk.io, tk.device)
+    return out
+
+
 def _bytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
@@ -168,14 +184,14 @@ def prefill(desc: Desc, state: State, plan: Plan, q, k, v, g=None, beta=None, u_
     p_fresh = None if fresh is None else _want("fresh", fresh, (plan.n,), torch.int32, dev)
     if state.S_base.device != dev:
         raise ValueError(f"state: expected tensors on {dev}")
-    if out is None:
-        out = torch.empty(tk.out_shape, dtype=tk.io, device=dev)
-    p_out = _want("out", out, tk.out_shape, tk.io, dev) or 16
+    if state.desc is not desc and any(getattr(state.desc, x) != getattr(desc, x) for x in _STATE_FIELDS):
+        raise ValueError("state: its tensors were laid out for another descriptor")
+    _out(out, tk)
     _gpu(dev)
-    ws = _workspace(desc, plan, workspace, False)
-    with _on(dev):
+    with _on(dev, stream) as handle:
+        out, ws = _out(out, tk, True), _workspace(desc, plan, workspace, False)
         rc = load_library().deltalog_prefill(ctypes.byref(desc.c_struct()), ctypes.byref(state.c_struct()), ctypes.byref(plan.c_struct()), *tk.ptr,
-                                             p_fresh, p_out, ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
+                                             p_fresh, out.data_ptr() or 16, ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_prefill")
     return out
 
@@ -190,15 +206,13 @@ def scan_forward(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=Non
     p_init = None if S_init is None else _want("S_init", S_init, s_shape, torch.float32, dev)
     if save and workspace is None:
         raise ValueError("workspace: save=True needs the caller's workspace, which scan_backward reads")
-    if out is None:
-        out = torch.empty(tk.out_shape, dtype=tk.io, device=dev)
-    p_out = _want("out", out, tk.out_shape, tk.io, dev) or 16
+    _out(out, tk)
     _gpu(dev)
-    S_final = torch.empty(s_shape, dtype=torch.float32, device=dev)
-    ws = _workspace(desc, plan, workspace, save)
-    with _on(dev):
-        rc = load_library().deltalog_scan_forward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr, p_out,
-                                                  S_final.data_ptr(), int(bool(save)), ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
+    with _on(dev, stream) as handle:
+        out, ws = _out(out, tk, True), _workspace(desc, plan, workspace, save)
+        S_final = torch.empty(s_shape, dtype=torch.float32, device=dev)
+        rc = load_library().deltalog_scan_forward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr,
+                                                  out.data_ptr() or 16, S_final.data_ptr(), int(bool(save)), ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_scan_forward")
     return out, S_final
 
@@ -228,30 +242,48 @@ def scan_backward(desc: Desc, plan: Plan, q, k, v, g, beta, u_bonus, dout, S_ini
     if saved and workspace is None:
         raise ValueError("workspace: saved=True needs the workspace of scan_forward")
     _gpu(dev)
-    ws = _workspace(desc, plan, workspace, True)
-    new = ScanGrads(*(None if p is None else torch.empty_like(t) for p, t in zip(tk.ptr, (q, k, v, g, beta, u_bonus))),
-                    torch.empty(s_shape, dtype=torch.float32, device=dev))
-    if plan.n == 0:
-        for t in (new.q, new.k, new.v, new.g, new.beta, new.u_bonus):
-            if t is not None:
-                t.zero_()
-    ptr = _ScanGrads(*(None if t is None else t.data_ptr() or 16 for t in (new.q, new.k, new.v, new.g, new.beta, new.u_bonus, new.S_init)))
-    with _on(dev):
+    with _on(dev, stream) as handle:
+        ws = _workspace(desc, plan, workspace, True)
+        # without rows nothing is launched, and the token tensors' rows are all behind the last sequence
+        make = torch.zeros_like if plan.n == 0 else torch.empty_like
+        new = ScanGrads(*(None if p is None else make(t) for p, t in zip(tk.ptr, (q, k, v, g, beta, u_bonus))),
+                        torch.empty(s_shape, dtype=torch.float32, device=dev))
+        ptr = _ScanGrads(*(None if t is None else t.data_ptr() or 16 for t in (new.q, new.k, new.v, new.g, new.beta, new.u_bonus, new.S_init)))
         rc = load_library().deltalog_scan_backward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr, p_dout, p_dS,
-                                                   int(bool(saved)), ctypes.byref(ptr), tk.rows, ws.data_ptr(), _bytes(ws), _stream_of(stream, dev))
+                                                   int(bool(saved)), ctypes.byref(ptr), tk.rows, ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_scan_backward")
     return new
+
+
+_eager = weakref.WeakSet()  # graph nodes of the scans that ran on the default stream, outside of a capture
+
+
+def _refuse_capture_beside_eager(inputs) -> None:
+    """A leaf's gradient is accumulated on the stream that its first graph was built on, and as long as that graph lives a later
+    one shares the place.  A captured backward pass would have to leave for the default stream, which a capture does not
+    survive, and with it the process may end."""
+    leaves = [t for t in inputs if t is not None and t.requires_grad and t.is_leaf]
+    for node in list(_eager):
+        if any(t is mine() for mine in node.leaves for t in leaves):
+            raise RuntimeError("a graph of the same leaves, built on the default stream, is alive: drop its outputs before the capture, or "
+                               "build it on a side stream")
 
 
 class _Scan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, desc, plan, q, k, v, g, beta, u_bonus, S_init):
-        ctx.save = any(t is not None and t.requires_grad for t in (q, k, v, g, beta, u_bonus, S_init))
-        ws = scan_workspace(desc, plan.n, plan.max_tokens, train=ctx.save, device=plan.device)
+        inputs = (q, k, v, g, beta, u_bonus, S_init)
+        if torch.cuda.is_current_stream_capturing():
+            _refuse_capture_beside_eager(inputs)
+        elif torch.cuda.current_stream(plan.device) == torch.cuda.default_stream(plan.device):
+            ctx.leaves = [weakref.ref(t) for t in inputs if t is not None and t.requires_grad and t.is_leaf]
+            _eager.add(ctx)
+        ws = scan_workspace(desc, plan.n, plan.max_tokens, train=True, device=plan.device)
         out = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
-        out, S_final = scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, out=out, workspace=ws, save=ctx.save)
+        out, S_final = scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, out=out, workspace=ws, save=True)
+        ctx.set_materialize_grads(False)
         ctx.desc, ctx.plan, ctx.builds = desc, plan, plan.builds
-        ctx.save_for_backward(q, k, v, g, beta, u_bonus, S_init, ws)
+        ctx.save_for_backward(*inputs, ws)
         return out, S_final
 
     @staticmethod
@@ -267,6 +299,12 @@ class _Scan(torch.autograd.Function):
 
 
 def scan(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=None, S_init=None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """The differentiable scan: ``(out, S_final)`` of the plan's rows with gradients for every tensor argument.  The plan's
-    tables belong to the graph until its backward pass has run: rebuilding the plan in between is an error."""
-    return _Scan.apply(desc, plan, q, k, v, g, beta, u_bonus, S_init)
+    """The differentiable scan: ``(out, S_final)`` of the plan's rows with gradients for every tensor argument; ``out`` rows
+    behind the last sequence are zero.  The plan's tables belong to the graph until its backward pass has run: rebuilding
+    the plan in between is an error, and so is capturing a scan while an eager graph of the same leaves lives."""
+    _Tokens(desc, plan, q, k, v, g, beta, u_bonus)
+    _gpu(plan.device)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, g, beta, u_bonus, S_init)):
+        return _Scan.apply(desc, plan, q, k, v, g, beta, u_bonus, S_init)
+    out = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
+    return scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, out=out)

@@ -168,3 +168,28 @@ def test_python_layer_names_what_it_refuses():
         bad[i] = bad[i][:3]
         with pytest.raises(ValueError, match=name):
             dl.State.wrap(d, *bad)
+
+
+def test_prefill_refuses_a_state_of_another_shape():
+    plan, d, T, bf = dl.Plan(2, 10, device="cpu"), _desc(), 10, torch.bfloat16
+    tokens = dict(q=torch.zeros(T, 2, 64, dtype=bf), k=torch.zeros(T, 2, 64, dtype=bf), v=torch.zeros(T, 2, 64, dtype=bf), g=torch.zeros(T, 2),
+                  beta=torch.zeros(T, 2))
+    import dataclasses
+    for other in (dict(num_slots=d.num_slots - 1), dict(cap=d.cap - 1), dict(H=1, H_qk=1), dict(d_k=128), dict(ulog_dtype=dl.BF16)):
+        od = dataclasses.replace(d, **other)
+        state = dl.State(od, torch.zeros(od.num_slots, od.H, od.d_k, od.d_v))
+        with pytest.raises(ValueError, match="another descriptor"):
+            dl.prefill(d, state, plan, **tokens)
+    same = dl.State(dataclasses.replace(d), torch.zeros(d.num_slots, 2, 64, 64))
+    with pytest.raises(ValueError, match="no path but the GPU"):   # an equal descriptor passes this check
+        dl.prefill(d, same, plan, **tokens)
+
+
+def test_scan_names_what_it_refuses():
+    plan, d, T, bf = dl.Plan(2, 10, device="cpu"), _desc(), 10, torch.bfloat16
+    tokens = dict(q=torch.zeros(T, 2, 64, dtype=bf, requires_grad=True), k=torch.zeros(T, 2, 64, dtype=bf), v=torch.zeros(T, 2, 64, dtype=bf),
+                  g=torch.zeros(T, 2), beta=torch.zeros(T, 2))
+    with pytest.raises(ValueError, match="beta"):
+        dl.scan(d, plan, **(tokens | dict(beta=None)))
+    with pytest.raises(ValueError, match="no path but the GPU"):
+        dl.scan(d, plan, **tokens)
