@@ -106,8 +106,8 @@ typedef struct {
  *   DELTALOG_HINT_BASE_UNTOUCHED  The work queued on the stream directly in front of this
  *       deltalog_decode_step does not WRITE S_base of the slots this call reads.  (True when it was
  *       another decode step on this state, or the kernel that produced this step's q, k, v, g, beta;
- *       NOT true for deltalog_merge, deltalog_decode_merge_step, deltalog_reset_slots or
- *       deltalog_eager_step on these slots.)  The decode kernel is then launched with programmatic
+ *       NOT true for deltalog_merge, deltalog_decode_merge_step, deltalog_reset_slots,
+ *       deltalog_eager_step or deltalog_prefill on these slots.)  The decode kernel is then launched with programmatic
  *       stream serialisation: its CTAs may start while the preceding kernel is still retiring.  Ahead of
  *       that kernel's completion they read base tiles and nothing else -- unless the next hint allows the
  *       slot list too.  Everything else this call reads (q, k, v, g, beta, u_bonus, lengths, log
@@ -344,6 +344,8 @@ typedef struct {
  * scan_slots.  The lists are row-aligned, as the calls want them.  A row whose tokens would end behind max_tokens is
  * dropped and so is every later row with tokens: they get no tokens and no slot.  A negative slot stays as it is (a
  * padding row: its tokens keep their place, every call skips them).  log_len NULL: H, cap and num_slots are not read.
+ * A slot must not be listed twice, here as in every call.  A new request whose prompt is one token decodes like any other
+ * such row, from what its slot holds: deltalog_reset_slots goes in front.
  */
 int deltalog_build_plan(const int32_t *lens, const int32_t *slots, const int32_t *log_len, int32_t H, int32_t cap, int32_t num_slots,
                         int32_t decode_rows, const deltalog_plan *plan, void *stream);
@@ -366,7 +368,7 @@ int deltalog_prefill(const deltalog_desc *desc, const deltalog_state *state, con
 
 /*
  * The same scan without a slot pool, for training: row i starts from S_init[i] ([n, H, d_k, d_v] fp32, or NULL: zeros)
- * and leaves its state in S_final[i] (or NULL).  Slots and desc->num_slots, cap and base_dtype play no part.  With
+ * and leaves its state in S_final[i] (or NULL).  desc has to be valid, but slots, num_slots, cap and base_dtype play no part.  With
  * save != 0 the workspace (sized with train != 0) keeps the states in front of the chunks for deltalog_scan_backward.
  */
 int deltalog_scan_forward(const deltalog_desc *desc, const deltalog_plan *plan, const float *S_init, const void *q, const void *k, const void *v,

@@ -11,7 +11,15 @@ int launch_chain(const ScanArgs &a, cudaStream_t s) {
     constexpr size_t smem = ForwardTcSmem<VEC, P, DK, DELTA, IO>::bytes;
     static_assert(smem <= 227 * 1024, "shared memory of one SM");
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    return launch_chained(kernel, dim3(a.n * a.H), kTcThreads, smem, s, a);
+    if (a.split <= 1) return launch_chained(kernel, dim3(a.n * a.H), kTcThreads, smem, s, a);
+    ScanArgs b = a;
+    b.pass = 1;
+    if (int rc = launch_chained(kernel, dim3(a.n * a.H * scan_pieces(a.split)), kTcThreads, smem, s, b)) return rc;
+    constexpr size_t join_smem = JoinSmem<DK>::bytes;
+    if (int rc = ensure_smem(scan_join_kernel<DK>, join_smem)) return rc;
+    if (int rc = launch_chained(scan_join_kernel<DK>, dim3(a.n * a.H, 128 / kJoinCols), DK, join_smem, s, a)) return rc;
+    b.pass = 2;
+    return launch_chained(kernel, dim3(a.n * a.H * (a.split - 1)), kTcThreads, smem, s, b);
 }
 
 }  // namespace

@@ -36,6 +36,7 @@ ScanArgs scan_args(const deltalog_desc *d, const deltalog_plan *plan, const void
     a.dq_part = floats(l.dq_part), a.dk_part = floats(l.dk_part), a.dbonus_part = floats(l.dbonus_part);
     a.order = reinterpret_cast<int32_t *>(w + l.order);
     a.qi = plane(l.qi), a.ki = plane(l.ki);
+    a.split = l.split, a.pieces = floats(l.pieces);
     return a;
 }
 

@@ -60,14 +60,60 @@ struct ScanArgs {
     float *dq_part, *dk_part;    // [tokens, H, d_k] where several value heads share one query / key head
     float *dg, *dbeta, *dbonus_part;
     int32_t wave;                // CTAs of one wave
+    // split of long rows (d_v = 128; see ScanSegment): segments per row at most, which of the two passes, the pieces' states
+    int32_t split, pass;
+    float *pieces;               // [n * H][2 * split - 3][d_k][d_v]
 };
+
+// Few rows leave most of the device idle while one chain runs, so long rows are cut into segments.  A segment is an affine map
+// of the state in front of it, S_end = M S + E: pass 1 runs the first segment as it is and, for each one behind it but
+// the last, two chains side by side -- E from a zero state, and M from the identity with v = 0 (its columns are as many as a
+// state's, so it is the same kernel).  scan_join_kernel then carries the state over the segments, and pass 2 runs all but
+// the first from the state they really start with.  Two passes of 1 / segments of the row each.
+constexpr int kMinSegment = 8;    // chunks
+constexpr int kSplitCtas = 148;   // CTAs of pass 1 at most: one per SM, and the same on every host
+inline __host__ __device__ int scan_segments(int chunks, int most) {
+    const int p = chunks / kMinSegment < most ? chunks / kMinSegment : most;
+    return p < 3 ? 1 : p;  // two segments would run one behind the other
+}
+inline __host__ __device__ int scan_pieces(int segments) { return 2 * segments - 3; }
+// Where the state in front of segment s >= 1 is among the pieces: behind the first segment, then in E's place.
+__device__ __forceinline__ int scan_piece_of_start(int s) { return s == 1 ? 0 : 2 * s - 3; }
+
+// What a chain CTA runs: chunks [first, end) of its row, from and to where.
+struct ScanSegment {
+    int seq, h, first, end;
+    int from, to;   // piece; -1: the call's own states; to: -2 for nothing
+    bool map;       // the chain for M
+    bool emit;      // output and what the backward pass reads
+};
+__device__ __forceinline__ bool scan_segment(const ScanArgs &a, int block, ScanSegment &g) {
+    const int each = a.split <= 1 ? 1 : a.pass == 1 ? scan_pieces(a.split) : a.split - 1;
+    g.h = block % a.H;
+    const int i = block / a.H % each;
+    g.seq = a.order[block / a.H / each];
+    const int chunks = a.chunk_starts[g.seq + 1] - a.chunk_starts[g.seq];
+    const int segments = a.split <= 1 ? 1 : scan_segments(chunks, a.split);
+    const int s = a.split <= 1 ? 0 : a.pass == 1 ? (i + 1) / 2 : i + 1;
+    if (s >= segments || (a.pass == 1 && s > 0 && s == segments - 1)) return false;
+    g.first = (int)((long long)chunks * s / segments), g.end = (int)((long long)chunks * (s + 1) / segments);
+    const bool last = s == segments - 1, early = a.pass == 1 && s > 0;  // early: ahead of the state it starts with
+    g.map = early && i == 2 * s;
+    g.emit = !early;
+    g.from = s == 0 || early ? -1 : scan_piece_of_start(s);
+    g.to = last ? -1 : a.pass == 1 || a.split <= 1 ? i : -2;
+    if (early) g.from = -2;
+    return true;
+}
 
 // The scan's kernels follow one another on the stream and are launched so that a kernel's CTAs may be set up while the one in
 // front retires (a microsecond or two per kernel, which short prompts notice).  First thing, each waits until
-// everything in front of it is complete and visible, and then lets its successor be set up.
-__device__ __forceinline__ void scan_kernel_begin() {
+// everything in front of it is complete and visible, and then lets its successor be set up.  A kernel that writes states
+// does not: a decode step that may start early (DELTALOG_HINT_BASE_UNTOUCHED) lets its own successor start before it has
+// itself waited, and that one reads base tiles at once; all that keeps it off these is that the first one starts late.
+__device__ __forceinline__ void scan_kernel_begin(bool writes_states = false) {
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    if (!writes_states) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 }
 
 // Row and slot of a (sequence, head) unit; false when the unit has nothing to do.

@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) 
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t sm = smem_addr(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nthreads = blockDim.x;
-    scan_kernel_begin();
+    scan_kernel_begin(a.S_out != nullptr);
     const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
     const int v0 = (blockIdx.y * (nthreads >> 5) + warp) * 16;
     const int t = lane & 3;

@@ -57,14 +57,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     const uint32_t sm = smem_addr(smem_tc);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int v = 32 * (warp & 3) + lane, f = warp >> 2;
-    scan_kernel_begin();
-    const int seq = a.order[blockIdx.x / a.H], h = blockIdx.x % a.H, hq = h / (a.H / a.Hq);
+    scan_kernel_begin(a.S_out != nullptr);
+    ScanSegment seg;
+    if (!scan_segment(a, blockIdx.x, seg)) return;
+    const int seq = seg.seq, h = seg.h, hq = h / (a.H / a.Hq);
     int slot;
     if (!scan_slot(a, seq, tid, slot)) return;
-    const int tok0 = a.starts[seq], len = a.starts[seq + 1] - tok0, nchunks = (len + kChunk - 1) / kChunk;
+    const int nchunks = seg.end - seg.first;
     if (nchunks == 0 && a.slots) return;
-    const int chunk0 = a.chunk_starts[seq];
+    const int tok0 = a.starts[seq] + seg.first * kChunk, len = min(a.starts[seq + 1] - tok0, nchunks * kChunk);
+    const int chunk0 = a.chunk_starts[seq] + seg.first;
+    const bool keep = a.keep && seg.emit, emit = a.out && seg.emit;
     const size_t tile = (size_t)DK * DV, s_off = ((size_t)slot * a.H + h) * tile;
+    const size_t pieces = ((size_t)seq * a.H + h) * scan_pieces(a.split);
     const size_t v_stride = (size_t)a.H * DV;
     const TcBlock tc = tc_setup(smem_tc + L::control, 3 * NST + 1, tid);
     const uint32_t row = tc.tmem + ((uint32_t)(32 * (warp & 3)) << 16);
@@ -134,11 +139,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     cp_async_commit();
 
     float s[HC];
-    const bool from = a.S_in && !(a.fresh && a.fresh[seq]);
+    const bool zero = seg.from == -2 || (seg.from == -1 && (!a.S_in || (a.fresh && a.fresh[seq]))), as_bf16 = seg.from == -1 && a.in_bf16;
+    const void *S_in = seg.from >= 0 ? a.pieces + (pieces + seg.from) * tile : a.S_in;
+    const size_t in_off = seg.from >= 0 ? 0 : s_off;
 #pragma unroll
     for (int i = 0; i < HC; ++i) {
-        const size_t at = s_off + (size_t)(f * HC + i) * DV + v;
-        s[i] = !from ? 0.f : a.in_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(a.S_in)[at]) : static_cast<const float *>(a.S_in)[at];
+        const size_t at = in_off + (size_t)(f * HC + i) * DV + v;
+        s[i] = zero ? (seg.map && f * HC + i == v ? 1.f : 0.f) : as_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(S_in)[at]) : static_cast<const float *>(S_in)[at];
     }
     uint32_t mma_phase = 0;
     // the products that one thread has issued are complete
@@ -167,7 +174,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     // and, behind a barrier, from there
     float o[HT];
     auto write_out = [&](int c) {
-        if (!a.out) return;
+        if (!emit) return;
 #pragma unroll
         for (int i = 0; i < HT; ++i) {
             const int t = HT * f + i;
@@ -181,7 +188,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     };
     auto store_out = [&](int c) {
         if constexpr (!F32IO) {
-            if (a.out && storer) tc_store_row(odst + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), out_s, warp * 4 + lane);
+            if (emit && storer) tc_store_row(odst + (size_t)c * kChunk * v_stride, v_stride, min(kChunk, len - c * kChunk), out_s, warp * 4 + lane);
         }
     };
 
@@ -212,17 +219,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         ok = bounded_wait(full(0, c), parity, tc.abort_flag) && ok;
         if (issuing()) {
             const uint32_t pl = tc.tmem + PL, b = st + L::kq;
-            if (DELTA) {
+            if (DELTA && !emit) {
+                tc_product<kPlanes, 0, L::kQ, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b);
+                tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more, false);
+            } else if (DELTA) {
                 tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, 2 * kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b);
                 tc_product<kPlanes, 0, L::kQ, L::kOut, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b, false);
                 tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more, false);
-            } else {
+            } else if (emit) {
                 tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC1, pl, b);
             }
             tc_commit(mma_bar);
         }
         // while they run: the state for the backward pass, the last chunk's output, v of this thread's tokens
-        if (a.keep) {
+        if (keep) {
             if constexpr (F32IO) {
                 float4 *dst = reinterpret_cast<float4 *>(a.S + unit * tile + (size_t)v * DK + f * HC);
 #pragma unroll
@@ -238,9 +248,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             const int t = HT * f + i;
             if constexpr (F32IO) {
                 x[i] = vsrc[(size_t)(c * kChunk + min(t, valid - 1)) * v_stride + v];
-                if (t >= valid) x[i] = 0.f;
+                if (t >= valid || seg.map) x[i] = 0.f;
             } else {
                 x[i] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(smem_tc + L::rows + t * 256 + v * 2));
+                if (seg.map) x[i] = 0.f;
             }
         }
         products_done();
@@ -261,7 +272,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             between(c);
             products_done();
             tmem_ld16(row + ACC0 + HT * f, u);
-            if (a.keep) {
+            if (keep) {
                 if constexpr (F32IO) {
                     float *dst = a.U + unit * kChunk * DV + (size_t)(HT * f) * DV + v;
 #pragma unroll
@@ -287,7 +298,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         if (issuing()) {
             if (L::kOwnKh) tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PL, st + L::kh);
             else tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kPair, L::kPairHalf>(tc.tmem + UPD, tc.tmem + PL, st + L::kq);
-            tc_product_lower<UO, L::kOut, L::kOut, 32>(tc.tmem + ACC2, tc.tmem + PLO, st + L::A);
+            if (emit) tc_product_lower<UO, L::kOut, L::kOut, 32>(tc.tmem + ACC2, tc.tmem + PLO, st + L::A);
             tc_commit(mma_bar);
         }
         if (!DELTA) between(c);
@@ -304,7 +315,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
                 s[i + j + 2] = fmaf(e.z, s[i + j + 2], y[j + 2]), s[i + j + 3] = fmaf(e.w, s[i + j + 3], y[j + 3]);
             }
         }
-        if (a.out) {
+        if (emit) {
             float z[HT];
             tmem_ld16(row + ACC1 + HT * f, o);
             tmem_ld16(row + ACC2 + HT * f, z);
@@ -329,18 +340,89 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             }
         }
     } else {
-        if (a.S_out) {
+        if (seg.to >= 0 || (seg.to == -1 && a.S_out)) {
+            float *piece = a.pieces + (pieces + max(seg.to, 0)) * tile;
 #pragma unroll
             for (int i = 0; i < HC; ++i) {
-                const size_t at = s_off + (size_t)(f * HC + i) * DV + v;
-                if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.S_out)[at] = __float2bfloat16_rn(s[i]);
-                else static_cast<float *>(a.S_out)[at] = s[i];
+                const size_t at = (size_t)(f * HC + i) * DV + v;
+                if (seg.to >= 0) piece[at] = s[i];
+                else if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.S_out)[s_off + at] = __float2bfloat16_rn(s[i]);
+                else static_cast<float *>(a.S_out)[s_off + at] = s[i];
             }
         }
-        if (a.log_len && tid == 0) a.log_len[(size_t)slot * a.H + h] = 0;
+        if (a.log_len && seg.to == -1 && tid == 0) a.log_len[(size_t)slot * a.H + h] = 0;
     }
     if (!F32IO && storer) tc_stores_done();
     tc_teardown(tc, tid);
+}
+
+// The states in front of a split row's segments: X_1 is the first segment's end, X_(s+1) = M_s X_s + E_s in E_s' place.
+// Sixteen columns per CTA, one row of M per thread; the next M is on its way while one is multiplied.  In fp32 throughout.
+// 8 CTAs per head keep a join at two microseconds or so, against the tens to hundreds that a segment takes.
+constexpr int kJoinCols = 16;
+template <int DK>
+struct JoinSmem {
+    static constexpr int stride = DK + 4;
+    static constexpr size_t bytes = (size_t)(2 * DK * stride + 2 * DK * kJoinCols) * 4;
+};
+template <int DK>
+__global__ void __launch_bounds__(DK) scan_join_kernel(const ScanArgs a) {
+    constexpr int DV = 128, kStride = JoinSmem<DK>::stride;
+    extern __shared__ __align__(16) unsigned char smem_join[];
+    float *M = reinterpret_cast<float *>(smem_join), *X = M + 2 * DK * kStride;  // twice each
+    const int tid = threadIdx.x, v0 = blockIdx.y * kJoinCols;
+    scan_kernel_begin();
+    const int seq = blockIdx.x / a.H;
+    const int segments = scan_segments(a.chunk_starts[seq + 1] - a.chunk_starts[seq], a.split);
+    if (segments < 3) return;
+    if (a.slots) {
+        const int slot = a.slots[seq];
+        if (slot < 0 || slot >= a.num_slots) return;
+    }
+    float *pieces = a.pieces + (size_t)blockIdx.x * scan_pieces(a.split) * DK * DV;
+    auto fetch = [&](int s) {  // M_s; its rows hold d_k of their d_v columns
+        if (s <= segments - 2) {
+            const float *src = pieces + (size_t)(2 * s) * DK * DV;
+            const uint32_t dst = smem_addr(M + (s & 1) * DK * kStride);
+            for (int i = tid; i < DK * DK / 4; i += DK) cp_async16_zfill(dst + ((i / (DK / 4)) * kStride + i % (DK / 4) * 4) * 4, src + (size_t)(i / (DK / 4)) * DV + i % (DK / 4) * 4, true);
+        }
+        cp_async_commit();
+    };
+    fetch(1);
+#pragma unroll
+    for (int j = 0; j < kJoinCols; j += 4)
+        *reinterpret_cast<float4 *>(X + DK * kJoinCols + tid * kJoinCols + j) = *reinterpret_cast<const float4 *>(pieces + (size_t)tid * DV + v0 + j);
+    for (int s = 1; s <= segments - 2; ++s) {
+        float *E = pieces + (size_t)(2 * s - 1) * DK * DV + (size_t)tid * DV + v0;
+        float x[kJoinCols];
+#pragma unroll
+        for (int j = 0; j < kJoinCols; j += 4) {
+            const float4 e = *reinterpret_cast<const float4 *>(E + j);
+            x[j] = e.x, x[j + 1] = e.y, x[j + 2] = e.z, x[j + 3] = e.w;
+        }
+        cp_async_wait_all();
+        __syncthreads();  // M_s and X_s are there, the places of the ones before are free
+        fetch(s + 1);
+        const float *m = M + (s & 1) * DK * kStride + tid * kStride, *in = X + (s & 1) * DK * kJoinCols;
+#pragma unroll 4
+        for (int c = 0; c < DK; ++c) {
+            const float w = m[c];
+#pragma unroll
+            for (int j = 0; j < kJoinCols; j += 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(in + c * kJoinCols + j);
+                x[j] = fmaf(w, y.x, x[j]), x[j + 1] = fmaf(w, y.y, x[j + 1]);
+                x[j + 2] = fmaf(w, y.z, x[j + 2]), x[j + 3] = fmaf(w, y.w, x[j + 3]);
+            }
+        }
+        float *next = X + ((s + 1) & 1) * DK * kJoinCols + tid * kJoinCols;
+#pragma unroll
+        for (int j = 0; j < kJoinCols; j += 4) {
+            const float4 y = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+            *reinterpret_cast<float4 *>(E + j) = y;
+            *reinterpret_cast<float4 *>(next + j) = y;
+        }
+    }
+    cp_async_wait_all();
 }
 
 }  // namespace deltalog

@@ -9,8 +9,17 @@ namespace deltalog {
 
 // Byte offsets into the caller's workspace.
 struct ScanLayout {
-    size_t order, A, T, decay, qt, kt, kh, qi, ki, U, S, dV, dS, dq_part, dk_part, dbonus_part, total;
+    size_t order, A, T, decay, qt, kt, kh, qi, ki, U, S, dV, dS, dq_part, dk_part, dbonus_part, pieces, total;
+    int split;
 };
+
+// Segments that a row may be cut into: as many as leave every chain of the first pass an SM of its own, none for rows that
+// are short for it.  (One 16k-token row of 32 heads: see scan_forward_tc_kernel.)
+inline int scan_split(const deltalog_desc *d, int32_t n, int32_t max_tokens) {
+    const long long units = (long long)n * d->H;
+    if (d->d_v != 128 || units < 1 || units * scan_pieces(3) > kSplitCtas) return 1;
+    return scan_segments(scan_max_chunks(n, max_tokens), ((int)(kSplitCtas / units) + 3) / 2);
+}
 
 inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tokens, bool train) {
     const size_t H = d->H, Hq = d->H_qk > 0 ? d->H_qk : d->H, dk = d->d_k, dv = d->d_v, tok = max_tokens;
@@ -41,6 +50,8 @@ inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tok
     l.dq_part = take(train && H != Hq, tok * H * dk * 4);
     l.dk_part = take(train && H != Hq, tok * H * dk * 4);
     l.dbonus_part = take(train && d->op == DELTALOG_RWKV6, units * dk * 4);
+    l.split = scan_split(d, n, max_tokens);
+    l.pieces = take(l.split > 1, (size_t)n * H * scan_pieces(l.split) * dk * dv * 4);
     l.total = at;
     return l;
 }

@@ -451,7 +451,8 @@ def test_training_step_captured():
 
 
 def test_offsets_beyond_32_bits():
-    """Token tensors of more than 2^31 elements: the last head of the last tokens equals the same head run alone."""
+    """Token tensors of more than 2^31 elements: the last head of the last tokens equals the same head run alone (to rounding:
+    one head alone is cut into segments)."""
     op, H, dk, T = ref.RETNET, 160, 128, 110_000
     assert T * H * dk > 2 ** 31
     gen = torch.Generator("cuda").manual_seed(1)
@@ -464,7 +465,7 @@ def test_offsets_beyond_32_bits():
     plan = make_plan([T])
     out, S = dl.scan_forward(make_desc(op, H, 1, dk, dk, BF16), plan, q, k, v, g)
     one, S1 = dl.scan_forward(make_desc(op, 1, 1, dk, dk, BF16), plan, q, k, v[:, -1:].contiguous(), g[:, -1:].contiguous())
-    assert torch.equal(out[:, -1:], one) and torch.equal(S[:, -1:], S1)
+    assert err(out[-4096:, -1:], one[-4096:]) < 2 * TOL[BF16] and err(S[:, -1:], S1) < 2 * TOL_F32
 
 
 def test_launches_are_the_librarys():
@@ -501,3 +502,186 @@ def test_bits_do_not_depend_on_what_the_memory_held(op):
         first = first or got
         assert all(torch.equal(x, y) for x, y in zip(first, got)), i
     assert all(torch.isfinite(x).all() for x in first) and plan.status.item() == 0
+
+
+def stream_of_memory(t):
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+
+
+def test_buffers_belong_to_the_stream_asked_for():
+    """A call on another stream than the current one: its results' memory is that stream's, so that no work queued on the
+    current one, in front or behind, shares it; the same for its workspace, which is free again when the call returns."""
+    op, H, dk, lens = ref.GDN, 2, 64, [70, 9]
+    t, S0 = ref.inputs(op, lens, H, 2, dk, dk, BF16, seed=64)
+    desc, plan = make_desc(op, H, 2, dk, dk, BF16, num_slots=2), make_plan(lens)
+    dout, state = torch.ones_like(t["v"]), pool(desc, 6)
+    want, S_want = dl.scan_forward(desc, plan, **t, S_init=S0)
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.Stream(), torch.cuda.Stream().cuda_stream):
+        handle = stream if isinstance(stream, int) else stream.cuda_stream
+        out, S = dl.scan_forward(desc, plan, **t, S_init=S0, stream=stream)
+        d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, stream=stream)
+        served = dl.prefill(desc, state, plan, **t, stream=stream)
+        torch.cuda.synchronize()
+        dl.build_plan(torch.tensor(lens, dtype=torch.int32, device="cuda"), plan, stream=0)
+        torch.cuda.synchronize()
+        assert torch.cuda.current_stream() == torch.cuda.default_stream()
+        assert {stream_of_memory(x) for x in (out, S, d.q, d.k, d.v, d.g, d.beta, d.S_init, served)} == {handle}
+        assert torch.equal(out, want) and torch.equal(S, S_want)
+
+
+@pytest.mark.parametrize("dk,op", [(128, ref.GDN), (64, ref.RWKV6)])
+def test_early_decode_steps_behind_a_prefill(dk, op):
+    """Decode steps that may start ahead of the kernel in front: the second one, on the prefilled state, keeps its promise (the
+    first one writes another state) and must still see the bases that the prefill writes."""
+    H, lens = 32, [1900, 30, 64, 500]
+    t, _ = ref.inputs(op, lens, H, H, dk, dk, BF16, seed=65)
+    desc = make_desc(op, H, H, dk, dk, BF16, num_slots=4)
+    early = make_desc(op, H, H, dk, dk, BF16, num_slots=4)
+    early.hints = dl.HINT_BASE_UNTOUCHED | dl.HINT_SLOTS_STABLE
+    plan = make_plan(lens)
+    step, _ = ref.inputs(op, [4], H, H, dk, dk, BF16, seed=66)
+    ws = dl.scan_workspace(desc, 4, sum(lens))
+    results = []
+    for hinted in (False, True, True, True):
+        a, b = pool(desc, 7), pool(desc, 8)
+        torch.cuda.synchronize()
+        dl.prefill(desc, a, plan, **t, workspace=ws)
+        for state in (b, a):
+            if not hinted:
+                torch.cuda.synchronize()
+            got = dl.decode_step(early if hinted else desc, state, **step)
+        results.append((got, a.S_base.clone(), b.K_log.clone()))
+    for r in results[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, results[0]))
+
+
+def test_captured_autograd():
+    """Forward and backward of the differentiable scan in one graph, replayed over changed inputs."""
+    op, H, dk, lens = ref.KDA, 2, 64, [70, 129, 1]
+    t, S0 = ref.inputs(op, lens, H, 1, dk, dk, F32, seed=67)
+    other, _ = ref.inputs(op, lens, H, 1, dk, dk, F32, seed=68)
+    desc, plan = make_desc(op, H, 1, dk, dk, F32), make_plan(lens)
+    names = [x for x, y in t.items() if y is not None]
+    fixed = {x: y.clone().requires_grad_() if y is not None else None for x, y in t.items()}
+
+    def grads(leaf):
+        out, S = dl.scan(desc, plan, **leaf, S_init=S0)
+        return [out, *torch.autograd.grad((out ** 2).sum() + S.sum(), [leaf[x] for x in names])]
+
+    kept = dl.scan(desc, plan, **fixed, S_init=S0)      # an eager graph of the same leaves
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="same leaves"):
+        with torch.cuda.graph(graph):
+            grads(fixed)
+    del kept
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        grads(fixed)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = grads(fixed)
+    for values in (t, other, t):
+        with torch.no_grad():
+            for x in names:
+                fixed[x].copy_(values[x])
+        graph.replay()
+        torch.cuda.synchronize()
+        want = grads({x: None if y is None else y.clone().requires_grad_() for x, y in values.items()})
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    with torch.no_grad():
+        out, _ = dl.scan(desc, plan, **fixed, S_init=S0)
+    assert not out.requires_grad and torch.equal(out, got[0])
+
+
+# A row that is cut into s segments passes s - 2 joins, each a contraction over 128 channels more: 128 additions of at most one
+# unit 2^-23 of the largest partial sum.
+def tol_joined(segments):
+    return TOL_F32 + max(0, segments - 2) * 128 * 2.0 ** -23
+
+
+SPLIT_LENS = [1900, 3, 0, 1100, 512, 1537]   # with 6 rows of one head up to 13 segments of 8 chunks: 3, 1, 1, 1 (17 chunks), 1, 3
+
+
+@pytest.mark.parametrize("op", sorted(ref.OPS.values()))
+@pytest.mark.parametrize("io,dk", [(BF16, 128), (F32, 128), (BF16, 64), (F32, 64)])
+def test_rows_cut_into_segments(op, io, dk):
+    H, dv = 1, 128
+    t, S0 = ref.inputs(op, SPLIT_LENS, H, H, dk, dv, io, seed=op + 110, tail=3)
+    desc, plan = make_desc(op, H, H, dk, dv, io), make_plan(SPLIT_LENS, tail=3)
+    want, S_want = ref.scan(op, desc.scale, SPLIT_LENS, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    out = torch.full(t["v"].shape, 7.0, dtype=io, device="cuda")
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0, out=out)
+    at = np.cumsum([0] + SPLIT_LENS)
+    more = tol_joined(3) - TOL_F32
+    for i, n in enumerate(SPLIT_LENS):   # row by row: a row's error is measured against its own size
+        assert err(out[at[i]:at[i + 1]], want[at[i]:at[i + 1]]) < TOL[io] + more, i
+        assert err(S[i], S_want[i]) < TOL_F32 + more, i
+    assert (out[at[-1]:] == 7.0).all()
+    again, S2 = dl.scan_forward(desc, plan, **t, S_init=S0)
+    assert torch.equal(again[:at[-1]], out[:at[-1]]) and torch.equal(S, S2) and plan.status.item() == 0
+
+
+@pytest.mark.parametrize("op", [ref.GDN, ref.KDA, ref.GLA])
+@pytest.mark.parametrize("gates", ["as drawn", "none", "mixed"])
+def test_one_long_row_in_many_segments(op, gates):
+    """4100 tokens, 65 chunks, 8 segments; gates that are drawn, absent (nothing is forgotten) or strong and reset by turns."""
+    lens, H, dk = [4100], 2, 128
+    t, S0 = ref.inputs(op, lens, H, 1, dk, dk, F32, seed=op + 120)
+    gen = torch.Generator().manual_seed(7)
+    pick = torch.rand(t["g"].shape, generator=gen).cuda()
+    if gates == "none":
+        t["g"] = torch.zeros_like(t["g"])
+    elif gates == "mixed":
+        t["g"] = torch.where(pick < 0.01, -torch.inf, torch.where(pick < 0.1, -50.0, torch.where(pick < 0.5, 0.0, t["g"]))).contiguous()
+    desc, plan = make_desc(op, H, 1, dk, dk, F32), make_plan(lens)
+    want, S_want = ref.scan(op, desc.scale, lens, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0)
+    assert err(out, want) < tol_joined(8) and err(S, S_want) < tol_joined(8)
+
+
+@pytest.mark.parametrize("op,io", [(ref.GDN, BF16), (ref.KDA, F32), (ref.RETNET, BF16)])
+def test_gradients_of_rows_cut_into_segments(op, io):
+    lens, H, dk = [1600, 70], 1, 128
+    t, S0 = ref.inputs(op, lens, H, H, dk, dk, io, seed=op + 130)
+    desc, plan = make_desc(op, H, H, dk, dk, io), make_plan(lens)
+    gen = torch.Generator().manual_seed(8)
+    dout, dS = torch.randn(t["v"].shape, generator=gen).to(io).cuda(), torch.randn(S0.shape, generator=gen).cuda() * 0.1
+    ws = dl.scan_workspace(desc, len(lens), plan.max_tokens, train=True)
+    ws.random_(generator=torch.Generator("cuda").manual_seed(1))
+    dl.scan_forward(desc, plan, **t, S_init=S0, workspace=ws, save=True)
+    d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, dS_final=dS, workspace=ws, saved=True)
+    for name, w in grads_of(op, desc.scale, lens, t, S0, dout, dS).items():
+        tol = TOL[io] if name in ("q", "k", "v") else TOL_F32
+        assert err(getattr(d, name), w) < tol + tol_joined(3) - TOL_F32, name
+
+
+@pytest.mark.parametrize("base", [dl.F32, dl.BF16])
+def test_prefill_of_rows_cut_into_segments(base):
+    """Slots of the pool: a row that continues, one that starts afresh over a poisoned slot, padding, one outside the pool."""
+    op, H, dk = ref.GDN, 2, 128
+    lens, slots = [1700, 1600, 1540, 1540, 9], [3, 0, -1, 17, 2]
+    desc = make_desc(op, H, 1, dk, dk, BF16, num_slots=5, base=base)
+    state = pool(desc, 9)
+    start = state.S_base.float().clone()
+    keep = state.S_base[[1, 4]].clone()
+    state.S_base[0] = float("nan")
+    state.log_len[0] = 2
+    t, _ = ref.inputs(op, lens, H, 1, dk, dk, BF16, seed=140)
+    out = torch.full(t["v"].shape, 7.0, dtype=BF16, device="cuda")
+    fresh = torch.tensor([0, 1, 1, 1, 0], dtype=torch.int32, device="cuda")
+    dl.prefill(desc, state, make_plan(lens, slots), **t, fresh=fresh, out=out)
+    at = np.cumsum([0] + lens)
+    assert state.status.item() == dl.STATUS_BAD_SLOT and (out[at[2]:at[4]] == 7.0).all()
+    assert torch.equal(state.S_base[[1, 4]], keep) and not state.log_len.any()
+    more = tol_joined(3) - TOL_F32
+    for row, S0 in ((0, start[3]), (1, torch.zeros_like(start[0])), (4, start[2])):
+        part = {x: None if y is None else y[at[row]:at[row + 1]].contiguous() for x, y in t.items()}
+        want, S_want = ref.scan(op, desc.scale, [lens[row]], part["q"], part["k"], part["v"], part["g"], part["beta"], None, S0[None])
+        assert err(out[at[row]:at[row + 1]], want) < TOL[BF16] + more
+        assert err(state.S_base[slots[row]], S_want[0]) < TOL_F32 + more + (0 if base == dl.F32 else 2.0 ** -8)
