@@ -193,7 +193,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
     float dq[NT][4] = {}, dr[NT][4] = {}, dw[NT][4] = {}, da[2][4] = {}, dl[2][4] = {};
     float dot0 = 0.f, dot1 = 0.f, db = 0.f;
     constexpr int kPairs = DK / 2, kGroups = kGradThreads / kPairs;
-    const int cp = tid % kPairs, grp = tid / kPairs;
+    // (TC: a warp reads eight v of eight channels, 128 bytes in one piece)
+    const int cp = TC ? warp % (kPairs / 4) * 4 + (lane & 3) : tid % kPairs, grp = TC ? warp / (kPairs / 4) * 8 + (lane >> 2) : tid / kPairs;
     // dA and dL', masked; scalar decay multiplies e^(G_i - G_j) in here
     auto write_mats = [&]() {
         if (cq > mt) return;
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         ok = bounded_wait(bar(0), 0u, tc.abort_flag) && ok;
         if (DELTA) ok = bounded_wait(bar(1), 0u, tc.abort_flag) && ok;
         if (issuing()) {
-            tc_product<UP, 0, 2, 0, 2, true, 8, DK, 64, DK * 256, kKeptHalf>(tc.tmem + D1, tc.tmem + PA, sm);
+            tc_product_state<UP, DK>(tc.tmem + D1, tc.tmem + PA, sm);
             tc_product<UP, 0, UP, 0, 2, false, 8, kChunk, 64, kChunk * 256, kChunk * 128>(tc.tmem + D2, tc.tmem + PA, sm + L::U);
             tc_commit(bar(3));
         }
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         }
         ok = bounded_wait(bar(2), 0u, tc.abort_flag) && ok;
         for (int v = grp; v < 128; v += kGroups) {
-            const int at = (cp >> 5) * kKeptHalf + v * 128 + ((((cp >> 2) & 7) ^ (v & 7)) << 4) + (cp & 3) * 4;
+            const int at = kept_state_at(2 * cp, v);
             const float2 x = both(smem + at, DK * 256), d = both(smem + L::dS + at, DK * 256);
             dot0 = fmaf(d.x, x.x, dot0), dot1 = fmaf(d.y, x.y, dot1);
         }
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         }
         handed_over();
         if (issuing()) {
-            tc_product<UP, 0, 2, 0, 2, true, 8, DK, 64, DK * 256, kKeptHalf>(tc.tmem + D3, tc.tmem + PA, sm + L::dS);
+            tc_product_state<UP, DK>(tc.tmem + D3, tc.tmem + PA, sm + L::dS);
             tc_commit(bar(3));
         }
         write_mats();  // (S_0's place, if so, is free: its product and the sums are behind the barrier)

@@ -173,15 +173,17 @@ __device__ __forceinline__ void tc_teardown(const TcBlock &b, int tid) {
 }
 
 // ---- what the chains keep for the per-chunk gradients (bf16 io) ------------------------------------------------
-// Two planes take fp32's room and are operands as they stand.  States: images of 128 rows v, columns c, [plane][c / 64].
-// U: an image of 64 tokens by 128 columns v.  dV: rows of 128 columns.
-constexpr int kKeptHalf = 128 * 128;  // bytes of 64 columns of a state image
+// Two planes take fp32's room and are operands as they stand.  States: [plane][c / 8][v][c % 8], 16 bytes a unit: the lanes of a
+// chain's warp are neighbouring v, so a warp's store is four whole lines.  (As rows v of 128 bytes, swizzled, every lane wrote
+// into a line of its own, 32 cycles a store: 4k of the 14k cycles of a chunk.)  U: an image of 64 tokens by 128 columns v.
+// dV: rows of 128 columns.
+constexpr int kKeptGroup = 128 * 16;  // bytes of eight channels of a state
+__device__ __forceinline__ int kept_state_at(int c, int v) { return (c >> 3) * kKeptGroup + v * 16 + (c & 7) * 2; }
 template <int DK, int HC>
 __device__ __forceinline__ void keep_state_planes(void *dst, const float (&s)[HC], int v, int c0) {
-    unsigned char *base = static_cast<unsigned char *>(dst) + v * 128;
+    unsigned char *base = static_cast<unsigned char *>(dst);
 #pragma unroll
     for (int i = 0; i < HC; i += 8) {
-        const int c = c0 + i, unit = (c >> 3) & 7;
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -189,10 +191,28 @@ __device__ __forceinline__ void keep_state_planes(void *dst, const float (&s)[HC
             split_pair<2>(s[i + 2 * j], s[i + 2 * j + 1], w);
             hi[j] = w[0], lo[j] = w[1];
         }
-        unsigned char *at = base + (c >> 6) * kKeptHalf + ((unit ^ (v & 7)) << 4);
+        unsigned char *at = base + kept_state_at(c0 + i, v);
         *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4 *>(at + DK * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
+}
+// D[., c] = sum_v A[., v] S[v][c] with the two planes of a kept state: c-major without a swizzle, core matrices of 8 v by 16
+// bytes, the next v 128 bytes on, the next c a group.
+template <int PA, int DK>
+__device__ __forceinline__ void tc_product_state(uint32_t d, uint32_t a, uint32_t b) {
+    const uint64_t desc = (uint64_t)((b & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(kKeptGroup >> 4) << 32) | ((uint64_t)1 << 46);
+    bool clear = true;
+#pragma unroll
+    for (int pb = 0; pb < 2; ++pb)
+#pragma unroll
+        for (int pa = 0; pa < PA; ++pa) {
+            if (pa + pb >= 2) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                tc_mma(d, a + pa * 64 + k * 8, desc + ((pb * DK * 256 + k * 256) >> 4), tc_idesc(DK, true), !clear);
+                clear = false;
+            }
+        }
 }
 // Place of (token, column v) in U's image / dV's rows, in bytes.
 __device__ __forceinline__ int kept_u_at(int tok, int v) { return (v >> 6) * (kChunk * 128) + tok * 128 + ((((v >> 3) & 7) ^ (tok & 7)) << 4) + (v & 7) * 2; }
