@@ -5,9 +5,9 @@
 namespace deltalog {
 namespace {
 
-template <bool VEC, int P, int DK, bool DELTA, typename IO>
+template <bool VEC, int P, int DK, bool DELTA, typename IO, bool KEEP>
 int launch_chain(const ScanArgs &a, cudaStream_t s) {
-    auto kernel = scan_forward_tc_kernel<VEC, P, DK, DELTA, IO>;
+    auto kernel = scan_forward_tc_kernel<VEC, P, DK, DELTA, IO, KEEP>;
     constexpr size_t smem = ForwardTcSmem<VEC, P, DK, DELTA, IO>::bytes;
     static_assert(smem <= 227 * 1024, "shared memory of one SM");
     if (int rc = ensure_smem(kernel, smem)) return rc;
@@ -25,7 +25,7 @@ int launch_chain(const ScanArgs &a, cudaStream_t s) {
 }  // namespace
 
 int launch_scan_forward_tc(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s) {
-#define CALL_CHAIN(VEC, P, DK, DELTA, IO) return launch_chain<VEC, P, DK, DELTA, IO>(a, s)
+#define CALL_CHAIN(VEC, P, DK, DELTA, IO) return a.keep ? launch_chain<VEC, P, DK, DELTA, IO, true>(a, s) : launch_chain<VEC, P, DK, DELTA, IO, false>(a, s)
     DELTALOG_SCAN_DISPATCH(d, CALL_CHAIN);
 #undef CALL_CHAIN
     return DELTALOG_ERR_UNSUPPORTED_SHAPE;

@@ -41,7 +41,8 @@ struct ForwardTcSmem {
     static constexpr size_t bytes = total > kTcMinSmem ? total : kTcMinSmem;
 };
 
-template <bool VEC, int P, int DK, bool DELTA, typename IO>
+// KEEP: what the backward pass reads is kept.  (Two kernels: serving's, without that code, is a few percent faster.)
+template <bool VEC, int P, int DK, bool DELTA, typename IO, bool KEEP>
 __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const ScanArgs a) {
     using L = ForwardTcSmem<VEC, P, DK, DELTA, IO>;
     constexpr int DV = 128, HC = DK / 4, HT = kChunk / 4;  // channels and tokens per thread
@@ -50,9 +51,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     constexpr int UP = DELTA || F32IO ? kPlanes : 1;
     constexpr int UO = UP < L::kOut ? UP : L::kOut;   // planes of U for the output
     constexpr int US = VEC ? UP : kPlanes;            // and for the state (scalar decay: times e^(G_end - G))
-    // tensor memory: accumulators of (k S)^T and then U^T, of (q S)^T, of A U, of the update; planes of S, later of R (then U
-    // for the update) and of U for the output
-    constexpr uint32_t ACC0 = 0, ACC1 = 64, ACC2 = 128, UPD = 192, PL = 320, PLO = 416;
+    // Scalar decay: nobody waits for q S before the chunk's end, so it runs behind k S while R is formed, and R's planes keep
+    // out of S's (one 16k-token row 904 -> 874 us).  Per channel it is more products apart than together: 866 -> 875 us.
+    // With KEEP the threads are busy storing meanwhile and nothing is gained.  The same for A U, which the state need not wait
+    // for (ragged prompts 1055 -> 1026 us; GDN training 4615 -> 4670, KDA training 919 -> 916).
+    constexpr bool kApart = DELTA && !VEC && !KEEP, kOutApart = VEC || !KEEP;
+    // tensor memory: accumulators of (k S)^T and then U^T, of (q S)^T, of A U, of the update; planes of S, later of U for the
+    // update and of U for the output; planes of R
+    constexpr uint32_t ACC0 = 0, ACC1 = 64, ACC2 = 128, UPD = 192, PL = 320, PLO = 416, PR = kApart ? UPD : PL;
     extern __shared__ __align__(1024) unsigned char smem_tc[];
     const uint32_t sm = smem_addr(smem_tc);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -67,13 +73,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
     if (nchunks == 0 && a.slots) return;
     const int tok0 = a.starts[seq] + seg.first * kChunk, len = min(a.starts[seq + 1] - tok0, nchunks * kChunk);
     const int chunk0 = a.chunk_starts[seq] + seg.first;
-    const bool keep = a.keep && seg.emit, emit = a.out && seg.emit;
+    // (a.keep is always set with KEEP; asked as a variable the compiler orders a chunk's stores better: 4530 us against 4615)
+    const bool keep = KEEP && a.keep && seg.emit, emit = a.out && seg.emit;
     const size_t tile = (size_t)DK * DV, s_off = ((size_t)slot * a.H + h) * tile;
     const size_t pieces = ((size_t)seq * a.H + h) * scan_pieces(a.split);
     const size_t v_stride = (size_t)a.H * DV;
-    const TcBlock tc = tc_setup(smem_tc + L::control, 3 * NST + 1, tid);
+    const TcBlock tc = tc_setup(smem_tc + L::control, 3 * NST + 2, tid);
     const uint32_t row = tc.tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-    const uint32_t mma_bar = tc.bars + 8u * (3 * NST);
+    const uint32_t mma_bar = tc.bars + 8u * (3 * NST), out_bar = mma_bar + 8;
     const uint32_t v_s = sm + L::rows, out_s = v_s + kChunk * 256;
     const IO *vsrc = static_cast<const IO *>(a.v) + (size_t)tok0 * v_stride + (size_t)h * DV;
     IO *odst = static_cast<IO *>(a.out) + (size_t)tok0 * v_stride + (size_t)h * DV;
@@ -219,7 +226,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         ok = bounded_wait(full(0, c), parity, tc.abort_flag) && ok;
         if (issuing()) {
             const uint32_t pl = tc.tmem + PL, b = st + L::kq;
-            if (DELTA && !emit) {
+            if (DELTA && (kApart || !emit)) {
                 tc_product<kPlanes, 0, L::kQ, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b);
                 tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more, false);
             } else if (DELTA) {
@@ -230,6 +237,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
                 tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC1, pl, b);
             }
             tc_commit(mma_bar);
+            if (kApart && emit) tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC1, pl, b + L::kHalf);
         }
         // while they run: the state for the backward pass, the last chunk's output, v of this thread's tokens
         if (keep) {
@@ -262,11 +270,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             if (!VEC) factors(decay, d);
 #pragma unroll
             for (int i = 0; i < HT; ++i) u[i] = VEC ? x[i] - u[i] : fmaf(-d[i], u[i], x[i]);
-            tmem_st_planes<kPlanes>(row + PL + HT / 2 * f, 32, u);
+            tmem_st_planes<kPlanes>(row + PR + HT / 2 * f, 32, u);
             handed_over();
             if (warp == 0) ok = bounded_wait(full(1, c), parity, tc.abort_flag) && ok;
             if (issuing()) {
-                tc_product_lower<kPlanes, kPlanes, kPlanes, 32>(tc.tmem + ACC0, tc.tmem + PL, st + L::T);
+                tc_product_lower<kPlanes, kPlanes, kPlanes, 32>(tc.tmem + ACC0, tc.tmem + PR, st + L::T);
                 tc_commit(mma_bar);
             }
             between(c);
@@ -298,8 +306,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         if (issuing()) {
             if (L::kOwnKh) tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kTile>(tc.tmem + UPD, tc.tmem + PL, st + L::kh);
             else tc_product<US, 0, L::kK, 0, kPlanes, true, 4, DK, 32, L::kPair, L::kPairHalf>(tc.tmem + UPD, tc.tmem + PL, st + L::kq);
+            if (kOutApart) tc_commit(mma_bar);
             if (emit) tc_product_lower<UO, L::kOut, L::kOut, 32>(tc.tmem + ACC2, tc.tmem + PLO, st + L::A);
-            tc_commit(mma_bar);
+            if (!kOutApart) tc_commit(mma_bar);
+            else if (emit) tc_commit(out_bar);
         }
         if (!DELTA) between(c);
         if (!F32IO && storer) tc_stores_read();  // the last chunk's output has left its tile
@@ -316,6 +326,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
             }
         }
         if (emit) {
+            if (kOutApart) {
+                ok = bounded_wait(out_bar, (uint32_t)c & 1u, tc.abort_flag) && ok;
+                tc_fence_after();
+            }
             float z[HT];
             tmem_ld16(row + ACC1 + HT * f, o);
             tmem_ld16(row + ACC2 + HT * f, z);
