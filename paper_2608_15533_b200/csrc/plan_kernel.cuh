@@ -5,6 +5,8 @@
 // memory and then writes its share of the tables: the scan costs a CTA a few microseconds whatever the grid, so one
 // launch without any exchange between CTAs beats a scan launch in front of an expansion launch.  More rows than shared
 // memory holds: one CTA scans into the plan's own offset arrays and a second launch expands from there.
+// 512 requests with 50k tokens 8 us, 20k requests with 8M tokens 26 us (33 MB of tables: 1.3 TB/s, the scan in front is most of it),
+// a few requests 5 us.
 #pragma once
 
 #include "common.cuh"

@@ -8,7 +8,12 @@
 //     A U and the state's update;  S <- e^(G_end) S + update, output.
 // B operands are images that prep wrote, fetched by bulk copies a step ahead; k and q lie interleaved so that one product
 // of 128 columns serves both.  The tensor cores need a quarter of mma.sync's time for the products; the rest of a chunk's
-// time is the threads' plane splits in between.
+// time is the threads' plane splits in between.  Of some 8k cycles a chunk (GDN, bf16) the products take half, the splits of S, R
+// and U and the update the other half, one behind the other; an SM's registers hold one such chain.
+// Against the mma.sync chain, bf16, 32 heads of 128: 48 ragged prompts of 36k tokens 1328 -> 659 us, one of 16k tokens 1671 -> 1091
+// us, 13k tokens of KDA 747 -> 323 us.  d_v = 64 would leave half of an MMA's rows empty and stays there.
+// Now: 630 us of the first; the second in three segments, 362 + 16 + 359 us; 305 us of the third.  With kept states, GDN: 195 us for
+// four rows of 2048 tokens, 811 us for 36.7k tokens of 19 rows (3.3 GB kept and read, 4 TB/s).
 #pragma once
 
 #include "scan_tc_common.cuh"
