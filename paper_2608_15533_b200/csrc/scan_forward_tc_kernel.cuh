@@ -13,7 +13,8 @@
 // Against the mma.sync chain, bf16, 32 heads of 128: 48 ragged prompts of 36k tokens 1328 -> 659 us, one of 16k tokens 1671 -> 1091
 // us, 13k tokens of KDA 747 -> 323 us.  d_v = 64 would leave half of an MMA's rows empty and stays there.
 // Now: 630 us of the first; the second in three segments, 362 + 16 + 359 us; 305 us of the third.  With kept states, GDN: 195 us for
-// four rows of 2048 tokens, 811 us for 36.7k tokens of 19 rows (3.3 GB kept and read, 4 TB/s).
+// four rows of 2048 tokens, 811 us for 36.7k tokens of 19 rows (3.9 TB/s
+// of DRAM traffic, most of it what is kept).
 #pragma once
 
 #include "scan_tc_common.cuh"
