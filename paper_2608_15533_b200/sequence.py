@@ -14,6 +14,7 @@ from dataclasses import dataclass
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 from .binding import BF16, F32, RWKV6, Desc, State, _DELTA_RULE, _DT_TO_TORCH, _check, _Plan, _ScanGrads, _VEC_DECAY, load_library
@@ -301,8 +302,12 @@ class _Scan(torch.autograd.Function):
 def scan(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=None, S_init=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The differentiable scan: ``(out, S_final)`` of the plan's rows with gradients for every tensor argument; ``out`` rows
     behind the last sequence are zero.  The plan's tables belong to the graph until its backward pass has run: rebuilding
-    the plan in between is an error, and so is capturing a scan while an eager graph of the same leaves lives."""
+    the plan in between is an error, and so is capturing a scan while an eager graph of the same leaves lives.  Forward-mode
+    differentiation is refused."""
     _Tokens(desc, plan, q, k, v, g, beta, u_bonus)
+    if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in (q, k, v, g, beta, u_bonus, S_init)):
+        # (a dual tensor need not require a gradient, and the kernels would read its value alone: a derivative of zero)
+        raise RuntimeError("scan has no forward-mode derivative: an argument carries a tangent")
     _gpu(plan.device)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, g, beta, u_bonus, S_init)):
         return _Scan.apply(desc, plan, q, k, v, g, beta, u_bonus, S_init)

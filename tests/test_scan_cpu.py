@@ -193,3 +193,19 @@ def test_scan_names_what_it_refuses():
         dl.scan(d, plan, **(tokens | dict(beta=None)))
     with pytest.raises(ValueError, match="no path but the GPU"):
         dl.scan(d, plan, **tokens)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "g", "beta", "S_init"])
+def test_scan_refuses_forward_mode(name):
+    """A dual tensor does not require a gradient: its tangent must not be dropped without a word."""
+    from torch.autograd import forward_ad
+
+    plan, d, T, bf = dl.Plan(2, 10, device="cpu"), _desc(), 10, torch.bfloat16
+    tokens = dict(q=torch.zeros(T, 2, 64, dtype=bf), k=torch.zeros(T, 2, 64, dtype=bf), v=torch.zeros(T, 2, 64, dtype=bf), g=torch.zeros(T, 2),
+                  beta=torch.zeros(T, 2), S_init=torch.zeros(2, 2, 64, 64))
+    with forward_ad.dual_level():
+        with pytest.raises(ValueError, match="no path but the GPU"):
+            dl.scan(d, plan, **tokens)
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), pytest.raises(RuntimeError, match="forward-mode"):
+                dl.scan(d, plan, **(tokens | {name: forward_ad.make_dual(tokens[name], torch.ones_like(tokens[name]))}))
