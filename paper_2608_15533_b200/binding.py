@@ -211,6 +211,8 @@ class State:
             if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != S_base.device:
                 raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on {S_base.device}")
             setattr(self, name, t)
+        if status is not None and (status.dtype != torch.int32 or status.device != S_base.device or status.numel() < 1):
+            raise ValueError(f"status: expected an int32 tensor of one word on {S_base.device}")  # the kernels set bits in it
         self.status = torch.zeros(1, dtype=torch.int32, device=S_base.device) if status is None else status
         return self
 

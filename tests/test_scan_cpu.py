@@ -209,3 +209,14 @@ def test_scan_refuses_forward_mode(name):
         for grad in (True, False):
             with torch.set_grad_enabled(grad), pytest.raises(RuntimeError, match="forward-mode"):
                 dl.scan(d, plan, **(tokens | {name: forward_ad.make_dual(tokens[name], torch.ones_like(tokens[name]))}))
+
+
+def test_wrap_refuses_a_status_word_that_the_kernels_cannot_set():
+    d, bf, n, H, cap = _desc(), torch.bfloat16, 4, 2, 8
+    state = [torch.zeros(n, H, 64, 64), torch.zeros(n, H, cap, 64, dtype=bf), torch.zeros(n, H, cap, 64), torch.zeros(n, H, cap, 1),
+             torch.zeros(n, H, dtype=torch.int32)]
+    word = torch.zeros(1, dtype=torch.int32)
+    assert dl.State.wrap(d, *state, status=word).status is word
+    for bad in (torch.zeros(1, dtype=torch.int64), torch.zeros(1), torch.zeros(0, dtype=torch.int32), torch.zeros(1, dtype=torch.int32, device="meta")):
+        with pytest.raises(ValueError, match="status"):
+            dl.State.wrap(d, *state, status=bad)
