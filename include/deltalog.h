@@ -351,8 +351,9 @@ int deltalog_build_plan(const int32_t *lens, const int32_t *slots, const int32_t
                         int32_t decode_rows, const deltalog_plan *plan, void *stream);
 
 /* Bytes of workspace (device, 16-byte aligned) that the calls below want for a plan of these sizes: train == 0 for
- * deltalog_prefill and deltalog_scan_forward without save, train != 0 for save and deltalog_scan_backward.  0: the
- * descriptor or a size is invalid.  Calls that may overlap on the GPU need workspaces of their own. */
+ * deltalog_prefill and deltalog_scan_forward without save, train != 0 for save and deltalog_scan_backward.  What is enough
+ * for n rows of max_tokens is enough for fewer rows and for fewer tokens.  0: the descriptor or a size is invalid.  Calls
+ * that may overlap on the GPU need workspaces of their own. */
 size_t deltalog_scan_workspace_bytes(const deltalog_desc *desc, int32_t n, int32_t max_tokens, int32_t train);
 
 /*

@@ -52,7 +52,10 @@ inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tok
     l.dk_part = take(train && H != Hq, tok * H * dk * 4);
     l.dbonus_part = take(train && d->op == DELTALOG_RWKV6, units * dk * 4);
     l.split = scan_split(d, n, max_tokens);
-    l.pieces = take(l.split > 1, (size_t)n * H * scan_pieces(l.split) * dk * dv * 4);
+    // (one tile per CTA of the first pass at most, whether or not these rows are cut: fewer rows might be, and a workspace
+    // for more rows has to do for them)
+    const bool may_cut = dv == 128 && (long long)H * scan_pieces(3) <= kSplitCtas && scan_max_chunks(n, max_tokens) >= 3 * kMinSegment;
+    l.pieces = take(may_cut, (size_t)kSplitCtas * dk * dv * 4);
     l.total = at;
     return l;
 }

@@ -220,3 +220,17 @@ def test_wrap_refuses_a_status_word_that_the_kernels_cannot_set():
     for bad in (torch.zeros(1, dtype=torch.int64), torch.zeros(1), torch.zeros(0, dtype=torch.int32), torch.zeros(1, dtype=torch.int32, device="meta")):
         with pytest.raises(ValueError, match="status"):
             dl.State.wrap(d, *state, status=bad)
+
+
+@pytest.mark.parametrize("H,dv", [(1, 128), (2, 64), (8, 128), (32, 128), (49, 128), (50, 128)])
+@pytest.mark.parametrize("train", [0, 1])
+def test_a_workspace_serves_every_smaller_plan(lib, H, dv, train):
+    """A program that allocates once for its largest step passes the same workspace with every smaller plan."""
+    def size(n, tokens):
+        return lib.deltalog_scan_workspace_bytes(ctypes.byref(_desc(H=H, d_k=128, d_v=dv).c_struct()), n, tokens, train)
+
+    ns, tokens = (1, 2, 3, 4, 7, 13, 49, 50, 148, 149), (0, 1, 64, 1400, 1408, 1471, 1472, 1535, 1536, 1600, 5000, 16384)
+    sizes = {(n, t): size(n, t) for n in ns for t in tokens}
+    for (n, t), most in sizes.items():
+        for (m, u), less in sizes.items():
+            assert less <= most or m > n or u > t, ((m, u), (n, t))
