@@ -127,8 +127,11 @@ typedef struct {
  *       one of them should walk upwards.  deltalog_eager_step honours the bit as well (its CTAs are
  *       numbered downwards: a step then begins with the tiles the step before wrote last); the other
  *       kernels with one CTA per unit ignore it.
+ *   DELTALOG_HINT_ZERO_UNWRITTEN  No promise, a request to deltalog_prefill and deltalog_scan_forward: the rows of `out`
+ *       below max_tokens that no row of the call writes (decoding, padding and dropped rows, and behind the last
+ *       sequence) are set to zero instead of being left as they were.  Without rows (n = 0) nothing is launched.
  */
-enum { DELTALOG_HINT_BASE_UNTOUCHED = 1, DELTALOG_HINT_SLOTS_STABLE = 2, DELTALOG_HINT_WALK_DOWN = 4 };
+enum { DELTALOG_HINT_BASE_UNTOUCHED = 1, DELTALOG_HINT_SLOTS_STABLE = 2, DELTALOG_HINT_WALK_DOWN = 4, DELTALOG_HINT_ZERO_UNWRITTEN = 8 };
 
 /* Physical state (Section 3.1).  Device pointers, caller-owned. d_lambda = 1 (GDN) or d_k. */
 typedef struct {
@@ -360,7 +363,8 @@ size_t deltalog_scan_workspace_bytes(const deltalog_desc *desc, int32_t n, int32
  * Prefill: every row of plan->scan_slots runs its tokens through its slot's state.  Entries pending in the slot's log are
  * folded into the base first; a row with fresh[i] != 0 (fresh: [n] or NULL) starts from a zero state instead, whatever the
  * slot holds.  On return S_base holds the state behind the row's last token and the slot's log is empty: the next
- * token goes through deltalog_decode_step.  `out` rows of skipped rows, and slots that are not listed, are left as they were.
+ * token goes through deltalog_decode_step.  Slots that are not listed are left as they were, and so are the rows of `out` that
+ * no listed row's tokens hold, unless DELTALOG_HINT_ZERO_UNWRITTEN asks for zeros there.
  * status receives DELTALOG_STATUS_BAD_SLOT for slots outside the pool (skipped).
  */
 int deltalog_prefill(const deltalog_desc *desc, const deltalog_state *state, const deltalog_plan *plan, const void *q, const void *k, const void *v,

@@ -23,7 +23,7 @@ ScanArgs scan_args(const deltalog_desc *d, const deltalog_plan *plan, const void
                    const float *u_bonus, void *workspace, const ScanLayout &l) {
     ScanArgs a = {};
     a.starts = plan->starts, a.chunk_starts = plan->chunk_starts, a.chunk_seq = plan->chunk_seq;
-    a.n = plan->n, a.max_chunks = scan_max_chunks(plan->n, plan->max_tokens), a.num_slots = d->num_slots, a.status = plan->status;
+    a.n = plan->n, a.max_chunks = scan_max_chunks(plan->n, plan->max_tokens), a.max_tokens = plan->max_tokens, a.num_slots = d->num_slots, a.status = plan->status;
     a.H = d->H, a.Hq = d->H_qk > 0 ? d->H_qk : d->H, a.dv = d->d_v;
     a.scale = d->op == DELTALOG_RWKV6 ? 1.f : d->scale;
     a.q = q, a.k = k, a.v = v;
@@ -70,6 +70,7 @@ int deltalog_prefill(const deltalog_desc *desc, const deltalog_state *state, con
     a.S_in = a.S_out = state->S_base;
     a.in_bf16 = a.out_bf16 = desc->base_dtype == DELTALOG_BF16;
     a.fresh = fresh, a.log_len = state->log_len, a.out = out;
+    a.clear = (desc->hints & DELTALOG_HINT_ZERO_UNWRITTEN) != 0;
     return run_forward(desc, a, s);
 }
 
@@ -81,6 +82,7 @@ int deltalog_scan_forward(const deltalog_desc *desc, const deltalog_plan *plan, 
     if (plan->n == 0) return DELTALOG_OK;
     ScanArgs a = scan_args(desc, plan, q, k, v, g, beta, u_bonus, workspace, scan_layout(desc, plan->n, plan->max_tokens, save != 0));
     a.S_in = S_init, a.S_out = S_final, a.out = out, a.keep = save != 0;
+    a.clear = (desc->hints & DELTALOG_HINT_ZERO_UNWRITTEN) != 0;
     return run_forward(desc, a, static_cast<cudaStream_t>(stream));
 }
 

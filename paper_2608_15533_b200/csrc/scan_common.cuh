@@ -29,7 +29,7 @@ struct ScanArgs {
     // the plan
     const int32_t *starts, *chunk_starts, *chunk_seq;
     const int32_t *slots;  // state index of each row; NULL: the row itself, every row takes part
-    int32_t n, max_chunks, num_slots;
+    int32_t n, max_chunks, max_tokens, num_slots;
     int32_t *status;
     // the problem
     int32_t H, Hq, dv;
@@ -53,6 +53,7 @@ struct ScanArgs {
     int32_t *log_len;            // [num_slots, H], emptied for the rows that ran, or NULL
     int32_t keep;                // forward: write S and U for a backward pass
     void *out;                   // [tokens, H, d_v], or NULL
+    int32_t clear;               // zeros to the rows of out below max_tokens that no row writes
     // backward
     const float *dS_final;
     float *dS_init;

@@ -27,6 +27,27 @@ __device__ __forceinline__ bool chunk_place(const ScanArgs &a, int chunk, ChunkP
     return true;
 }
 
+// Zeros to the rows of `out` that no chain will write, for the CTA of a chunk that has nothing to prepare: a skipped row's
+// chunk clears its own tokens, and the entries behind the last chunk (with the CTA beyond the table) share those behind the last
+// sequence.  No launch of its own, and nothing is written twice, as a memset of the whole tensor in front would.
+template <typename IO>
+__device__ __forceinline__ void clear_unwritten(const ScanArgs &a, int chunk, int h, int tid, int nthreads) {
+    if (!a.clear) return;
+    const int seq = chunk < a.max_chunks ? a.chunk_seq[chunk] : -1;
+    long long first, last;
+    if (seq >= 0) {
+        first = a.starts[seq] + (chunk - a.chunk_starts[seq]) * kChunk;
+        last = min(first + kChunk, (long long)a.starts[seq + 1]);
+    } else {
+        const int chunks = a.chunk_starts[a.n];
+        const long long tokens = a.starts[a.n], tail = a.max_tokens - tokens, parts = a.max_chunks - chunks + 1;
+        first = tokens + tail * (chunk - chunks) / parts, last = tokens + tail * (chunk - chunks + 1) / parts;
+    }
+    const int units = a.dv * (int)sizeof(IO) / 16;
+    uint4 *out = reinterpret_cast<uint4 *>(static_cast<IO *>(a.out) + ((size_t)first * a.H + h) * a.dv);
+    for (long long i = tid; i < (last - first) * units; i += nthreads) out[(size_t)(i / units) * a.H * units + i % units] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 constexpr int kInvStride = kChunk + 8;  // row of the fp32 matrices: fragment reads without bank conflicts
 
 // T = (I + N)^-1 for the strictly lower N (64 x 64, fp32).  The four diagonal 16 x 16 blocks by forward substitution, one
@@ -175,10 +196,14 @@ __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(c
     scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
         if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 128);
+        clear_unwritten<IO>(a, chunk, h, tid, 128);
         return;
     }
     ChunkPlace p;
-    if (!chunk_place(a, chunk, p)) return;
+    if (!chunk_place(a, chunk, p)) {
+        clear_unwritten<IO>(a, chunk, h, tid, 128);
+        return;
+    }
     const size_t unit = (size_t)chunk * a.H + h;
     const int hq = h / (a.H / a.Hq);
     constexpr int kTile = L::kTile;
@@ -373,10 +398,14 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
         if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 2 * DK);
+        clear_unwritten<IO>(a, chunk, h, tid, 2 * DK);
         return;
     }
     ChunkPlace p;
-    if (!chunk_place(a, chunk, p)) return;
+    if (!chunk_place(a, chunk, p)) {
+        clear_unwritten<IO>(a, chunk, h, tid, 2 * DK);
+        return;
+    }
     const size_t unit = (size_t)chunk * a.H + h;
     const int hq = h / (a.H / a.Hq);
     float *qs = reinterpret_cast<float *>(smem), *kc = qs + kChunk * VS, *ks = kc + kChunk * VS;

@@ -17,7 +17,9 @@ import torch
 from torch.autograd import forward_ad
 
 from . import binding
-from .binding import BF16, F32, RWKV6, Desc, State, _DELTA_RULE, _DT_TO_TORCH, _check, _Plan, _ScanGrads, _VEC_DECAY, load_library
+from .binding import (
+    BF16, F32, HINT_ZERO_UNWRITTEN, RWKV6, Desc, State, _DELTA_RULE, _DT_TO_TORCH, _check, _Desc, _Plan, _ScanGrads, _VEC_DECAY, load_library,
+)
 
 SCAN_CHUNK = 64
 _STATE_FIELDS = ("num_slots", "H", "d_k", "d_v", "cap", "d_lambda", "base_dtype", "klog_dtype", "ulog_dtype")
@@ -164,12 +166,24 @@ def _workspace(desc, plan, workspace, train) -> torch.Tensor:
     return workspace
 
 
-def _out(out, tk: _Tokens, make: bool = False) -> Optional[torch.Tensor]:
-    """The caller's output tensor, checked; a new one in its place with ``make``."""
-    if out is None:
-        return torch.empty(tk.out_shape, dtype=tk.io, device=tk.device) if make else None
-    _want("out", out, tk.out_shape, tk.io, tk.device)
-    return out
+def _out_ok(out, tk: _Tokens) -> None:
+    if out is not None:
+        _want("out", out, tk.out_shape, tk.io, tk.device)
+
+
+def _out(out, tk: _Tokens, desc: Desc, plan: Plan):
+    """The output tensor and the call's descriptor: the caller's own, or a new tensor whose rows that the call does not write
+    are to be zero (the kernels see to those below ``plan.max_tokens``)."""
+    d = desc.c_struct()
+    if out is not None:
+        return out, d
+    out = torch.empty(tk.out_shape, dtype=tk.io, device=tk.device)
+    first = plan.max_tokens if plan.n > 0 else 0
+    if first < tk.rows:
+        out[first:].zero_()
+    d = _Desc.from_buffer_copy(d)
+    d.hints |= HINT_ZERO_UNWRITTEN
+    return out, d
 
 
 def _bytes(t: torch.Tensor) -> int:
@@ -179,7 +193,9 @@ def _bytes(t: torch.Tensor) -> int:
 def prefill(desc: Desc, state: State, plan: Plan, q, k, v, g=None, beta=None, u_bonus=None, fresh: Optional[torch.Tensor] = None, out=None,
             workspace=None, stream=None) -> torch.Tensor:
     """``deltalog_prefill``: the rows of ``plan.scan_slots`` run their tokens through their slots' states; returns
-    ``out [tokens, H, d_v]``.  ``fresh [n]`` int32: rows that start from a zero state.  The slots' logs are empty afterwards."""
+    ``out [tokens, H, d_v]``.  ``fresh [n]`` int32: rows that start from a zero state.  The slots' logs are empty afterwards.
+    Output rows that no row of the call writes (decoding, padding and dropped rows, behind the last sequence) stay as they were
+    in the caller's ``out``; in a tensor that the call makes they are zero."""
     tk = _Tokens(desc, plan, q, k, v, g, beta, u_bonus)
     dev = tk.device
     p_fresh = None if fresh is None else _want("fresh", fresh, (plan.n,), torch.int32, dev)
@@ -187,11 +203,11 @@ def prefill(desc: Desc, state: State, plan: Plan, q, k, v, g=None, beta=None, u_
         raise ValueError(f"state: expected tensors on {dev}")
     if state.desc is not desc and any(getattr(state.desc, x) != getattr(desc, x) for x in _STATE_FIELDS):
         raise ValueError("state: its tensors were laid out for another descriptor")
-    _out(out, tk)
+    _out_ok(out, tk)
     _gpu(dev)
     with _on(dev, stream) as handle:
-        out, ws = _out(out, tk, True), _workspace(desc, plan, workspace, False)
-        rc = load_library().deltalog_prefill(ctypes.byref(desc.c_struct()), ctypes.byref(state.c_struct()), ctypes.byref(plan.c_struct()), *tk.ptr,
+        (out, d), ws = _out(out, tk, desc, plan), _workspace(desc, plan, workspace, False)
+        rc = load_library().deltalog_prefill(ctypes.byref(d), ctypes.byref(state.c_struct()), ctypes.byref(plan.c_struct()), *tk.ptr,
                                              p_fresh, out.data_ptr() or 16, ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_prefill")
     return out
@@ -201,18 +217,18 @@ def scan_forward(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=Non
                  stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """``deltalog_scan_forward``: row i of the plan starts from ``S_init[i]`` (zeros without it); returns ``(out, S_final)``
     with ``S_final [n, H, d_k, d_v]`` fp32.  ``save``: the workspace (``scan_workspace(.., train=True)``) keeps what
-    ``scan_backward(.., saved=True)`` reads."""
+    ``scan_backward(.., saved=True)`` reads.  Rows behind the last sequence: as in ``prefill``."""
     tk = _Tokens(desc, plan, q, k, v, g, beta, u_bonus)
     dev, s_shape = tk.device, (plan.n, desc.H, desc.d_k, desc.d_v)
     p_init = None if S_init is None else _want("S_init", S_init, s_shape, torch.float32, dev)
     if save and workspace is None:
         raise ValueError("workspace: save=True needs the caller's workspace, which scan_backward reads")
-    _out(out, tk)
+    _out_ok(out, tk)
     _gpu(dev)
     with _on(dev, stream) as handle:
-        out, ws = _out(out, tk, True), _workspace(desc, plan, workspace, save)
+        (out, d), ws = _out(out, tk, desc, plan), _workspace(desc, plan, workspace, save)
         S_final = torch.empty(s_shape, dtype=torch.float32, device=dev)
-        rc = load_library().deltalog_scan_forward(ctypes.byref(desc.c_struct()), ctypes.byref(plan.c_struct()), p_init, *tk.ptr,
+        rc = load_library().deltalog_scan_forward(ctypes.byref(d), ctypes.byref(plan.c_struct()), p_init, *tk.ptr,
                                                   out.data_ptr() or 16, S_final.data_ptr(), int(bool(save)), ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_scan_forward")
     return out, S_final
@@ -280,8 +296,7 @@ class _Scan(torch.autograd.Function):
             ctx.leaves = [weakref.ref(t) for t in inputs if t is not None and t.requires_grad and t.is_leaf]
             _eager.add(ctx)
         ws = scan_workspace(desc, plan.n, plan.max_tokens, train=True, device=plan.device)
-        out = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
-        out, S_final = scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, out=out, workspace=ws, save=True)
+        out, S_final = scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, workspace=ws, save=True)
         ctx.set_materialize_grads(False)
         ctx.desc, ctx.plan, ctx.builds = desc, plan, plan.builds
         ctx.save_for_backward(*inputs, ws)
@@ -311,5 +326,4 @@ def scan(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=None, S_ini
     _gpu(plan.device)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, g, beta, u_bonus, S_init)):
         return _Scan.apply(desc, plan, q, k, v, g, beta, u_bonus, S_init)
-    out = torch.zeros(v.shape, dtype=v.dtype, device=v.device)
-    return scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, out=out)
+    return scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init)
