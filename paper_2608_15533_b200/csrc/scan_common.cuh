@@ -126,8 +126,8 @@ __device__ __forceinline__ bool scan_slot(const ScanArgs &a, int seq, int tid, i
     return resolve_slot(a.slots, seq, a.num_slots, a.status, tid, slot);
 }
 
-// e^x for x <= 0 that weighs a term: the argument's rounding costs |x| 2^-24 of the weight, at most 2^-25 of the largest
-// weight.  (Factors above one take expf.)
+// e^x for x <= 0 that weighs a term as it is: the argument's rounding costs |x| 2^-24 of the weight e^x, at most 2^-25 of the
+// largest weight.  (Not for a weight that a factor above one brings back up: see block_vectors.)
 __device__ __forceinline__ float decay_exp(float x) { return __expf(x); }
 
 // ---- bf16 planes -------------------------------------------------------------------------------------------

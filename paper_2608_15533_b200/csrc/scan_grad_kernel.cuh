@@ -569,28 +569,27 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
         const bool mine = tid < 4 * DK;
         auto raw = [&](const void *src, int i, int ch) { return i < p.valid ? to_f32(static_cast<const IO *>(src)[((size_t)(p.tok0 + i) * a.Hq + hq) * DK + ch]) : 0.f; };
         auto gate_at = [&](int i, int ch) { return i < p.valid ? a.g[((size_t)(p.tok0 + i) * a.H + h) * DK + ch] : 0.f; };
-        float Bc = 0.f;
+        float Bc = 0.f, Ec = 1.f;  // sum of the gates, product of their exponentials (see block_vectors)
         if (mine) {
             float gate[kBlock], kk[kBlock], qq[kBlock];
 #pragma unroll
             for (int r = 0; r < kBlock; ++r) gate[r] = gate_at(blk * kBlock + r, c), kk[r] = raw(a.k, blk * kBlock + r, c), qq[r] = raw(a.q, blk * kBlock + r, c);
-            float e = 1.f;
 #pragma unroll
             for (int r = 0; r < kBlock; ++r) {
                 const int at = (blk * kBlock + r) * SW + c;
-                if (EXCL) qs[at] = qq[r] * e, ps[at] = e;
+                if (EXCL) qs[at] = qq[r] * Ec, ps[at] = Ec;
                 Bc += gate[r];
-                e = decay_exp(Bc);
-                if (!EXCL) qs[at] = qq[r] * e, ps[at] = e;
-                if (DELTA) ks[at] = kk[r] * e;
+                gate[r] = expf(gate[r]);
+                Ec *= gate[r];
+                if (!EXCL) qs[at] = qq[r] * Ec, ps[at] = Ec;
+                if (DELTA) ks[at] = kk[r] * Ec;
             }
-            float s = 0.f;
+            float e = 1.f;
 #pragma unroll
             for (int r = kBlock - 1; r >= 0; --r) {
                 const int at = (blk * kBlock + r) * SW + c;
-                e = decay_exp(s);
                 kc[at] = kk[r] * e, ss[at] = e;
-                s += gate[r];
+                e *= gate[r];
             }
             if (!(Bc > -kBlockDecay)) deep[blk] = 1;
             eB[blk * DK + c] = Bc;
@@ -603,7 +602,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
                 if (m < blk) f += x;
                 if (m > blk) b += x;
             }
-            front[blk * DK + c] = decay_exp(f), back[blk * DK + c] = decay_exp(b), eI[blk * DK + c] = expf(-Bc);
+            front[blk * DK + c] = decay_exp(f), back[blk * DK + c] = decay_exp(b), eI[blk * DK + c] = 1.f / Ec;
         }
         __syncthreads();
         if (mine) eB[blk * DK + c] = decay_exp(Bc);

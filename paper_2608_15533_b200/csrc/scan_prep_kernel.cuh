@@ -314,7 +314,10 @@ __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(c
 //     e^(G_i - G_j) = e^(p_i) e^(B_(J+1) + .. + B_(I-1)) e^(s_j),
 // every exponent a sum of gates of one sign: nothing overflows and nothing cancels.  Inside a block
 // e^(p_i - p_j) = e^(p_i) e^(-B) e^(s_j), which is used while -B stays below kBlockDecay (e^60 is far from the range
-// of fp32 and bf16 planes); where a block decays further, its pairs are summed one by one.
+// of fp32 and bf16 planes); where a block decays further, its pairs are summed one by one.  There the factor e^(-B) brings
+// small weights back up to one, and what counts is their relative error.  Exponentials of sums rounded to fp32 are off by |x| 2^-24
+// each: up to 2.4e-5 of a pair's weight at gates of -3.5.  So the weights of a block are running products of e^(gate): of
+// a pair's weight the tokens outside of it cancel, up to one rounding of 2^-24 per product.
 constexpr int kBlock = 16;
 constexpr float kBlockDecay = 60.f;
 
@@ -322,7 +325,7 @@ constexpr float kBlockDecay = 60.f;
 // token), k_i e^(p_i), k_j e^(s_j), and the block's total B.
 struct BlockVectors {
     float2 qs[kBlock], ks[kBlock], kc[kBlock];
-    float2 B;
+    float2 B, E;  // and e^B as the product that the weights are made of
 };
 template <typename IO, bool EXCL, bool DELTA>
 __device__ __forceinline__ void block_vectors(const ScanArgs &a, const ChunkPlace &p, int h, int hq, int DK, int blk, int c, BlockVectors &o) {
@@ -346,17 +349,18 @@ __device__ __forceinline__ void block_vectors(const ScanArgs &a, const ChunkPlac
     for (int r = 0; r < kBlock; ++r) {
         if (EXCL) o.qs[r].x *= e.x, o.qs[r].y *= e.y;
         s.x += gate[r].x, s.y += gate[r].y;
-        e = make_float2(decay_exp(s.x), decay_exp(s.y));
+        gate[r] = make_float2(expf(gate[r].x), expf(gate[r].y));
+        e.x *= gate[r].x, e.y *= gate[r].y;
         if (!EXCL) o.qs[r].x *= e.x, o.qs[r].y *= e.y;
         if (DELTA) o.ks[r] = make_float2(o.kc[r].x * e.x, o.kc[r].y * e.y);
     }
-    s = make_float2(0.f, 0.f);
+    o.B = s, o.E = e;
+    e = make_float2(1.f, 1.f);
 #pragma unroll
     for (int r = kBlock - 1; r >= 0; --r) {
-        o.kc[r].x *= decay_exp(s.x), o.kc[r].y *= decay_exp(s.y);
-        s.x += gate[r].x, s.y += gate[r].y;
+        o.kc[r].x *= e.x, o.kc[r].y *= e.y;
+        e.x *= gate[r].x, e.y *= gate[r].y;
     }
-    o.B = s;
 }
 
 template <int DK>
@@ -423,10 +427,12 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     const bool all = sizeof(IO) == 4 || a.keep;  // planes of A and of q e^G
     constexpr int kPairs = DK / 2, kThreads = 4 * kPairs, kWarps = kThreads / 32;
     const int blk = tid / kPairs, c = (tid % kPairs) * 2;
+    float2 E;
     {
         BlockVectors o;
         block_vectors<IO, EXCL, DELTA>(a, p, h, hq, DK, blk, c, o);
         *reinterpret_cast<float2 *>(B + blk * DK + c) = o.B;
+        E = o.E;
         if (!(o.B.x > -kBlockDecay && o.B.y > -kBlockDecay)) deep[blk] = 1;
 #pragma unroll
         for (int r = 0; r < kBlock; ++r) {
@@ -448,7 +454,7 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
         *reinterpret_cast<float2 *>(W + blk * DK + c) = make_float2(decay_exp(front.x), decay_exp(front.y));
         *reinterpret_cast<float2 *>(W + (4 + blk) * DK + c) = make_float2(decay_exp(back.x), decay_exp(back.y));
         const float2 b = *reinterpret_cast<const float2 *>(B + blk * DK + c);
-        *reinterpret_cast<float2 *>(F + blk * DK + c) = make_float2(expf(-b.x), expf(-b.y));
+        *reinterpret_cast<float2 *>(F + blk * DK + c) = make_float2(1.f / E.x, 1.f / E.y);  // (not read where E may be 0)
         if (blk == 1 || blk == 2) *reinterpret_cast<float2 *>(F + (3 + blk) * DK + c) = make_float2(decay_exp(b.x), decay_exp(b.y));
         if (blk == 1) {
             const float2 x = *reinterpret_cast<const float2 *>(B + 2 * DK + c);

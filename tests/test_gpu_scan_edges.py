@@ -68,3 +68,67 @@ def test_new_outputs_without_rows_or_tokens_are_zero():
         for call in (lambda: dl.prefill(desc, pool(desc, 1), plan, **t), lambda: dl.scan_forward(desc, plan, **t)[0]):
             poison(t["v"].shape, BF16)
             assert not call().any()
+
+
+# Weights of pairs inside a block of 16 tokens.  A pair's weight is the product of the gates' exponentials between its tokens, made
+# of the block's prefix and suffix products and the reciprocal of the whole: up to 15 exponentials of the pair, two units 2^-23
+# each, 16 products of half a unit in the prefix, in the suffix and in the whole, three half units joining them and q, k: 30
+# + 24 + 1.5 units.  The matrix product adds eight: one per sum of the six plane products, one for the others' zeros, one for scale.
+TOL_PAIR = 64 * 2.0 ** -23
+
+
+def relative(x, want):
+    x, want = x.double().cpu(), want.double().cpu()
+    live = want != 0
+    assert x.shape == want.shape and not x[~live].any()
+    return ((x - want).abs()[live] / want.abs()[live]).max().item()
+
+
+@pytest.mark.parametrize("op", [ref.GLA, ref.RWKV6, ref.KDA])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128)])
+@pytest.mark.parametrize("depth", [1.0, 20.0, 40.0, 59.0])
+def test_weights_of_pairs_inside_a_block(op, dk, dv, depth):
+    """Every pair's weight by itself: one channel is live in each run, v_j is the j-th unit vector, so that out_ij is the weight
+    of pair (i, j); for the gradients one token's k (or q) is live, so that dq (dk) is the weight of one pair per channel."""
+    T, H = 16, 1
+    gen = torch.Generator().manual_seed(int(depth) + dk)
+    g = -torch.rand(T, H, dk, generator=gen, dtype=torch.float64) - 0.05
+    g = (g * (depth / -g.sum(0).min())).float()                     # the deepest channel's block decays by e^-depth
+    G = g.double().cumsum(0)[:, 0]
+    before = G - g[:, 0].double() if op == ref.RWKV6 else G         # what a readout sees
+    low = torch.ones(T, T, dtype=torch.bool).tril(-1 if op == ref.RWKV6 else 0)
+    desc, plan = make_desc(op, H, H, dk, dv, F32, scale=1.0), make_plan([T])
+    ones = torch.ones(T, H, dk)
+    more = dict(beta=torch.ones(T, H).cuda() if op == ref.KDA else None, u_bonus=torch.zeros(H, dk).cuda() if op == ref.RWKV6 else None)
+    v = torch.eye(T, dv)[:, None].contiguous()
+    S0 = torch.zeros(1, H, dk, dv, device="cuda")
+
+    def weights(c):
+        return torch.exp(before[:, None, c] - G[None, :, c]).masked_fill(~low, 0.0)
+
+    if op != ref.KDA:       # the delta rule's outputs mix the pairs; its gradients' weights are looked at below
+        for c in (0, 1, dk // 2 + 3, dk - 1):
+            one = torch.zeros(T, H, dk)
+            one[..., c] = 1.0
+            out, _ = dl.scan_forward(desc, plan, one.cuda(), one.cuda(), v.cuda(), g.cuda(), **more, S_init=S0)
+            assert relative(out[:, 0, :T], weights(c)) < TOL_PAIR
+    # one live token: with k = 0 but for token j the delta rule has nothing to remove, and u_j = v_j
+    for j in (0, 5, 14):
+        k = torch.zeros(T, H, dk)
+        k[j] = 1.0
+        dout = torch.zeros(T, H, dv)
+        dout[:, 0, j] = 1.0
+        d = dl.scan_backward(desc, plan, ones.cuda(), k.cuda(), v.cuda(), g.cuda(), more["beta"], more["u_bonus"], dout.cuda(), S_init=S0)
+        want = torch.exp(before - G[j]) * low[:, j, None]
+        assert relative(d.q[:, 0], want) < TOL_PAIR
+    # with q = 0 but for token i, dk_j is the weight of (i, j) (RWKV6, GLA)
+    if op != ref.KDA:
+        for i in (15, 7):
+            q = torch.zeros(T, H, dk)
+            q[i] = 1.0
+            dout = torch.zeros(T, H, dv)
+            dout[i, 0] = 1.0
+            vv = torch.zeros(T, H, dv)
+            vv[:, 0, 0] = 1.0
+            d = dl.scan_backward(desc, plan, q.cuda(), ones.cuda(), vv.cuda(), g.cuda(), None, more["u_bonus"], dout.cuda(), S_init=S0)
+            assert relative(d.k[:, 0], torch.exp(before[i] - G) * low[i, :, None]) < TOL_PAIR
