@@ -309,6 +309,8 @@ class _Scan(torch.autograd.Function):
         if ctx.plan.builds != ctx.builds:
             raise RuntimeError("the plan of this scan was rebuilt before its backward pass")
         dout = torch.zeros_like(v) if dout is None else dout.to(v.dtype).contiguous()
+        if dout.data_ptr() % 16:  # a gradient is a view of whatever autograd hands over; the kernels want 16-byte boundaries
+            dout = dout.clone()
         dS_final = None if dS_final is None else dS_final.float().contiguous()
         d = scan_backward(ctx.desc, ctx.plan, q, k, v, g, beta, u_bonus, dout, S_init=S_init, dS_final=dS_final, workspace=ws, saved=True)
         return None, None, d.q, d.k, d.v, d.g, d.beta, d.u_bonus, None if S_init is None else d.S_init

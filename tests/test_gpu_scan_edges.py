@@ -132,3 +132,24 @@ def test_weights_of_pairs_inside_a_block(op, dk, dv, depth):
             vv[:, 0, 0] = 1.0
             d = dl.scan_backward(desc, plan, q.cuda(), ones.cuda(), vv.cuda(), g.cuda(), None, more["u_bonus"], dout.cuda(), S_init=S0)
             assert relative(d.k[:, 0], torch.exp(before[i] - G) * low[i, :, None]) < TOL_PAIR
+
+
+@pytest.mark.parametrize("op,io,d", [(ref.GDN, BF16, 128), (ref.RWKV6, BF16, 64), (ref.GLA, F32, 64)])
+def test_gradients_that_arrive_off_a_16_byte_boundary(op, io, d):
+    """Flattened outputs joined behind a single number: their gradients are contiguous views that start in between."""
+    H, lens = 2, [70, 9]
+    t, S0 = ref.inputs(op, lens, H, H, d, d, io, seed=op + 210)
+    desc, plan = make_desc(op, H, H, d, d, io), make_plan(lens)
+    names = [x for x, y in t.items() if y is not None]
+    gen = torch.Generator().manual_seed(2)
+    w_out, w_S = torch.randn(t["v"].numel(), generator=gen).to(io).cuda(), torch.randn(S0.numel(), generator=gen).cuda()
+
+    def grads(offset):
+        leaf = {x: None if y is None else y.clone().requires_grad_() for x, y in t.items()}
+        out, S = dl.scan(desc, plan, **leaf, S_init=S0)
+        front = torch.zeros(offset, dtype=io, device="cuda"), torch.zeros(offset, device="cuda")
+        loss = (torch.cat((front[0], out.flatten()))[offset:] * w_out).sum() + (torch.cat((front[1], S.flatten()))[offset:] * w_S).sum()
+        return torch.autograd.grad(loss, [leaf[x] for x in names])
+
+    for x, y in zip(grads(1), grads(0)):
+        assert torch.equal(x, y)
