@@ -275,15 +275,30 @@ def scan_backward(desc: Desc, plan: Plan, q, k, v, g, beta, u_bonus, dout, S_ini
 _eager = weakref.WeakSet()  # graph nodes of the scans that ran on the default stream, outside of a capture
 
 
+def _leaves(nodes) -> list:
+    """The leaf tensors whose gradients graphs with these nodes at their ends accumulate."""
+    found, seen, todo = [], set(), [n for n in nodes if n is not None]
+    while todo:
+        node = todo.pop()
+        if node in seen:
+            continue
+        seen.add(node)
+        if hasattr(node, "variable"):
+            found.append(node.variable)
+        todo += [n for n, _ in node.next_functions if n is not None]
+    return found
+
+
 def _refuse_capture_beside_eager(inputs) -> None:
     """A leaf's gradient is accumulated on the stream that its first graph was built on, and as long as that graph lives a later
     one shares the place.  A captured backward pass would have to leave for the default stream, which a capture does not
-    survive, and with it the process may end."""
-    leaves = [t for t in inputs if t is not None and t.requires_grad and t.is_leaf]
-    for node in list(_eager):
-        if any(t is mine() for mine in node.leaves for t in leaves):
-            raise RuntimeError("a graph of the same leaves, built on the default stream, is alive: drop its outputs before the capture, or "
-                               "build it on a side stream")
+    survive, and with it the process may end.  The leaves are the inputs themselves or what they were computed from."""
+    eager = _leaves(list(_eager))
+    asked = [t for t in inputs if t is not None and t.requires_grad]
+    mine = [t for t in asked if t.is_leaf] + _leaves([t.grad_fn for t in asked])
+    if any(x is y for x in mine for y in eager):
+        raise RuntimeError("a graph of the same leaves, built on the default stream, is alive: drop its outputs before the capture, or "
+                           "build it on a side stream")
 
 
 class _Scan(torch.autograd.Function):
@@ -293,7 +308,6 @@ class _Scan(torch.autograd.Function):
         if torch.cuda.is_current_stream_capturing():
             _refuse_capture_beside_eager(inputs)
         elif torch.cuda.current_stream(plan.device) == torch.cuda.default_stream(plan.device):
-            ctx.leaves = [weakref.ref(t) for t in inputs if t is not None and t.requires_grad and t.is_leaf]
             _eager.add(ctx)
         ws = scan_workspace(desc, plan.n, plan.max_tokens, train=True, device=plan.device)
         out, S_final = scan_forward(desc, plan, q, k, v, g, beta, u_bonus, S_init=S_init, workspace=ws, save=True)

@@ -153,3 +153,43 @@ def test_gradients_that_arrive_off_a_16_byte_boundary(op, io, d):
 
     for x, y in zip(grads(1), grads(0)):
         assert torch.equal(x, y)
+
+
+def test_capture_of_a_layer_beside_an_eager_graph_of_its_weights():
+    """q, k and v are computed from weights, which are the leaves: refused while an eager graph of them lives, fine afterwards."""
+    op, H, d, lens = ref.RETNET, 2, 64, [40, 9]
+    T = sum(lens)
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(T, 32, generator=gen).cuda()
+    w = {n: (torch.randn(32, H * d, generator=gen) * 0.1).cuda().requires_grad_() for n in "qkv"}
+    g = torch.full((T, H), -0.05, device="cuda")
+    desc, plan = make_desc(op, H, H, d, d, F32), make_plan(lens)
+
+    def layer():
+        out, S = dl.scan(desc, plan, *(torch.matmul(x, w[n]).view(T, H, d) for n in "qkv"), g)
+        return [out, *torch.autograd.grad((out ** 2).sum() + S.sum(), list(w.values()))]
+
+    def forward():
+        return dl.scan(desc, plan, *(torch.matmul(x, w[n]).view(T, H, d) for n in "qkv"), g)
+
+    kept = forward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(RuntimeError, match="same leaves"):
+        with torch.cuda.graph(graph):
+            forward()
+    del kept
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = layer()
+    x.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, layer()):
+        assert torch.equal(a, b)

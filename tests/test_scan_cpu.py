@@ -234,3 +234,30 @@ def test_a_workspace_serves_every_smaller_plan(lib, H, dv, train):
     for (n, t), most in sizes.items():
         for (m, u), less in sizes.items():
             assert less <= most or m > n or u > t, ((m, u), (n, t))
+
+
+def test_capture_check_sees_leaves_behind_computed_inputs():
+    """The leaves that a live eager graph shares with a captured one need not be arguments of the scan: weights are not."""
+    from paper_2608_15533_b200 import sequence
+
+    class Node(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, *x):
+            return sum(x)
+
+        @staticmethod
+        def backward(ctx, d):
+            return d, d
+
+    w, u, other = (torch.ones(3, requires_grad=True) for _ in range(3))
+    x = torch.ones(3)
+    out = Node.apply((w * x).exp() + w, u)
+    assert {id(t) for t in sequence._leaves([out.grad_fn])} == {id(w), id(u)}
+    sequence._eager.add(out.grad_fn)
+    for mine in ([w], [u], [x, w * 2], [other * w], [None, (u + other).sum()]):
+        with pytest.raises(RuntimeError, match="same leaves"):
+            sequence._refuse_capture_beside_eager(mine)
+    for mine in ([], [None], [x], [other], [other * 2, x], [w.detach()]):
+        sequence._refuse_capture_beside_eager(mine)
+    del out     # the graph is gone
+    sequence._refuse_capture_beside_eager([w, u, w * 2])
