@@ -193,3 +193,228 @@ def test_capture_of_a_layer_beside_an_eager_graph_of_its_weights():
     torch.cuda.synchronize()
     for a, b in zip(got, layer()):
         assert torch.equal(a, b)
+
+
+# bf16 tensors with d_v = 128: the gradients' products over d_v take states, U and dV as two bf16 planes, each off by at most 2^-18 of
+# its value.  A sum of 128 products of random sign is about 1 / sqrt(128) of the sum of their sizes, so a gate's or beta's
+# gradient is off by 2 * 2^-18 * sqrt(128) of itself on top of the fp32 sums.
+TOL_TWO_PLANES = TOL_F32 + 128 ** 0.5 * 2.0 ** -17
+
+
+def check_all(op, io, lens, H, Hq, dk, dv, t, S0, seed, saved=True):
+    """Forward and every gradient of one batch against the fp64 recurrence."""
+    desc, plan = make_desc(op, H, Hq, dk, dv, io), make_plan(lens)
+    gen = torch.Generator().manual_seed(seed)
+    dout, dS = torch.randn(t["v"].shape, generator=gen).to(io).cuda(), torch.randn(S0.shape, generator=gen).cuda() * 0.1
+    want, S_want = ref.scan(op, desc.scale, lens, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    ws = dl.scan_workspace(desc, len(lens), plan.max_tokens, train=True)
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0, workspace=ws, save=True)
+    assert err(out, want) < TOL[io] and err(S, S_want) < TOL_F32
+    d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, dS_final=dS, workspace=ws, saved=True)
+    two = io == BF16 and dv == 128
+    for name, w in grads_of(op, desc.scale, lens, t, S0, dout, dS).items():
+        tol = TOL[io] if name in ("q", "k", "v") else TOL_TWO_PLANES if two and name in ("g", "beta", "u_bonus") else TOL_F32
+        assert err(getattr(d, name), w) < tol, name
+    served, S = dl.scan_forward(desc, plan, **t, S_init=S0)      # serving's kernels, which keep nothing
+    assert err(served, want) < TOL[io] and err(S, S_want) < TOL_F32
+    assert plan.status.item() == 0
+
+
+@pytest.mark.parametrize("op", sorted(ref.OPS.values()))
+@pytest.mark.parametrize("io,H,Hq,dk,dv", [(BF16, 2, 2, 64, 64), (BF16, 4, 2, 128, 64), (F32, 2, 1, 64, 128)])
+def test_forward_and_gradients_of_the_other_shapes(op, io, H, Hq, dk, dv):
+    lens = [17, 0, 1, 64, 2, 129, 63, 16, 200]
+    t, S0 = ref.inputs(op, lens, H, Hq, dk, dv, io, seed=op + 220)
+    check_all(op, io, lens, H, Hq, dk, dv, t, S0, 11)
+
+
+SHAPES = [(BF16, 128, 128), (BF16, 64, 128), (F32, 128, 128), (BF16, 128, 64)]
+
+
+@pytest.mark.parametrize("op", [ref.GDN, ref.RETNET, ref.KDA, ref.RWKV6, ref.GLA])
+@pytest.mark.parametrize("gates", ["none", "slow", "strong", "reset", "mixed", "some channels"])
+@pytest.mark.parametrize("io,dk,dv", SHAPES)
+def test_gates_of_every_strength(op, gates, io, dk, dv):
+    """No decay, that of trained layers (-0.001 to -0.1), gates that empty the state within a block, resets, all by turns; and, per
+    channel, a tenth of the channels that forget fast beside ordinary ones."""
+    lens, H = [150, 40], 2
+    t, S0 = ref.inputs(op, lens, H, 1, dk, dv, io, seed=op + 230)
+    g = t["g"]
+    gen = torch.Generator().manual_seed(5)
+    pick = torch.rand(g.shape, generator=gen).cuda()
+    if gates == "none":
+        g = torch.zeros_like(g)
+    elif gates == "slow":
+        g = -0.001 - 0.099 * pick
+    elif gates == "strong":
+        g = g * 40 - 3
+    elif gates == "reset":
+        g = torch.where(pick < 0.1, -torch.inf, g)
+    elif gates == "mixed":
+        g = torch.where(pick < 0.05, -torch.inf, torch.where(pick < 0.2, -50.0, torch.where(pick < 0.5, 0.0, g)))
+    else:
+        g = torch.where(torch.arange(g.shape[-1], device="cuda") % 10 == 3, g - 5.0, g)
+    t["g"] = g.contiguous()
+    check_all(op, io, lens, H, 1, dk, dv, t, S0, 12)
+
+
+@pytest.mark.parametrize("op", [ref.GDN, ref.KDA])
+@pytest.mark.parametrize("case", ["beta0", "beta1", "same_key", "tiny_beta", "all_beta0"])
+@pytest.mark.parametrize("io,dk,dv", SHAPES)
+def test_delta_rule_at_its_edges(op, case, io, dk, dv):
+    lens, H = [100, 7], 2
+    t, S0 = ref.inputs(op, lens, H, H, dk, dv, io, seed=op + 240)
+    if case == "beta0":
+        t["beta"][::2] = 0.0
+    elif case == "all_beta0":
+        t["beta"].zero_()
+    elif case == "beta1":
+        t["beta"].fill_(1.0)
+    elif case == "tiny_beta":
+        t["beta"][::3] = 1e-25
+    else:
+        t["k"] = t["k"][:1].expand_as(t["k"]).contiguous()
+        t["beta"].fill_(1.0)
+        t["g"] = t["g"] * 0.01
+    check_all(op, io, lens, H, H, dk, dv, t, S0, 13)
+
+
+@pytest.mark.parametrize("op,io,dk", [(ref.GDN, BF16, 64), (ref.GDN, F32, 128), (ref.KDA, BF16, 128), (ref.RWKV6, BF16, 64), (ref.GLA, F32, 64)])
+def test_head_size_64_on_both_sides_of_a_wave(op, io, dk):
+    """The chain kernels for d_v = 64 take two warps per CTA while the units do not fill the device, four beyond: the same bits, forward and
+    backward, and those of the recurrence."""
+    H, dv, n0 = 32, 64, 130
+    t, S0 = ref.inputs(op, [n0], H, H, dk, dv, io, seed=op + 250)
+    desc = make_desc(op, H, H, dk, dv, io)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    gen = torch.Generator().manual_seed(14)
+    dout, dS = torch.randn(t["v"].shape, generator=gen).to(io).cuda(), torch.randn(S0.shape, generator=gen).cuda() * 0.1
+    want, S_want = ref.scan(op, desc.scale, [n0], t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    grads = grads_of(op, desc.scale, [n0], t, S0, dout, dS)
+    sides, first = set(), None
+    for n in (1, 4, 5, 11):
+        sides.add(n * H < sms)
+
+        def rep(x):
+            return None if x is None else x.repeat(n, *[1] * (x.dim() - 1))
+
+        big = {x: y if x == "u_bonus" else rep(y) for x, y in t.items()}
+        plan = make_plan([n0] * n)
+        out, S = dl.scan_forward(desc, plan, **big, S_init=rep(S0))
+        d = dl.scan_backward(desc, plan, **big, dout=rep(dout), S_init=rep(S0), dS_final=rep(dS))
+        rows = [x.view(n, -1) for x in (out, S, d.q, d.k, d.v, d.S_init, *(y for y in (d.g, d.beta) if y is not None))]
+        assert all(torch.equal(x[i], x[0]) for x in rows for i in range(n))
+        first = first or [x[0] for x in rows]
+        assert all(torch.equal(x[0], y) for x, y in zip(rows, first))
+        if n in (4, 5):
+            assert err(out[-n0:], want) < TOL[io] and err(S[-1], S_want[0]) < TOL_F32
+            for name, w in grads.items():
+                x = getattr(d, name)
+                x = x / n if name == "u_bonus" else x[-1:] if name == "S_init" else x[-n0:]
+                assert err(x, w) < (TOL[io] if name in ("q", "k", "v") else TOL_F32), name
+    assert sides == {True, False}
+
+
+@pytest.mark.parametrize("op", sorted(ref.OPS.values()))
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (64, 128)])
+def test_prefill_fp32(op, dk, dv):
+    """fp32 token tensors into the pool: a slot with pending log entries goes on, a fresh row over NaN, a padding row, a slot
+    outside the pool; then a decode step."""
+    H, Hq, cap, steps = 2, 1, 8, 3
+    lens, slots = [70, 129, 20, 9, 0, 1], [5, 2, -1, 11, 0, 7]
+    desc = make_desc(op, H, Hq, dk, dv, F32, num_slots=9, cap=cap)
+    state = pool(desc, 1)
+    S5, S7 = state.S_base[5].clone(), state.S_base[7].clone()
+    pre, _ = ref.inputs(op, [steps], H, Hq, dk, dv, F32, seed=op + 260)
+    t, _ = ref.inputs(op, lens, H, Hq, dk, dv, F32, seed=op + 261)
+    t["u_bonus"] = bonus = pre["u_bonus"]
+
+    def rows(x, sl):
+        return {n: y if y is None or n == "u_bonus" else y[sl].clone() for n, y in x.items()}   # (16-byte boundaries)
+
+    five = torch.tensor([5], dtype=torch.int32, device="cuda")
+    for s in range(steps):
+        dl.decode_step(desc, state, **rows(pre, slice(s, s + 1)), slot_idx=five)
+    state.S_base[2], state.log_len[2] = float("nan"), 4
+    keep = state.S_base[[0, 1, 3, 4, 6, 8]].clone()
+    fresh = torch.tensor([0, 1, 0, 0, 1, 0], dtype=torch.int32, device="cuda")
+    out = dl.prefill(desc, state, make_plan(lens, slots), **t, fresh=fresh)
+    at = np.cumsum([0] + lens)
+    assert state.status.item() == dl.STATUS_BAD_SLOT and torch.equal(state.S_base[[0, 1, 3, 4, 6, 8]], keep)
+    assert not out[at[2]:at[4]].any() and not state.log_len[[5, 2, 7]].any()
+    for row, front, S0 in ((0, pre, S5), (1, None, torch.zeros_like(S5)), (5, None, S7)):
+        x = rows(t, slice(at[row], at[row + 1]))
+        if front:
+            x = {n: y if y is None or n == "u_bonus" else torch.cat((front[n], y)) for n, y in x.items()}
+        n = lens[row] + (steps if front else 0)
+        want, S_want = ref.scan(op, desc.scale, [n], x["q"], x["k"], x["v"], x["g"], x["beta"], bonus, S0[None])
+        assert err(out[at[row]:at[row + 1]], want[n - lens[row]:]) < TOL_F32
+        assert err(state.S_base[slots[row]], S_want[0]) < TOL_F32
+    more, _ = ref.inputs(op, [1], H, Hq, dk, dv, F32, seed=op + 262)
+    more["u_bonus"] = bonus
+    S_from = state.S_base[5].clone()[None]
+    got = dl.decode_step(desc, state, **more, slot_idx=five)
+    want, _ = ref.scan(op, desc.scale, [1], more["q"], more["k"], more["v"], more["g"], more["beta"], bonus, S_from)
+    assert err(got, want) < TOL_F32
+
+
+@pytest.mark.parametrize("op,io", [(ref.GDN, BF16), (ref.KDA, BF16), (ref.GDN, F32), (ref.GLA, BF16)])
+@pytest.mark.parametrize("lens,H", [([1900, 3, 0, 1537], 1), ([4100], 2)])
+def test_segments_of_rows_that_forget_slowly(op, io, lens, H):
+    """Gates of -0.001 to -0.02 and small betas: what a segment's map carries over its 500 tokens and more is a good part of the
+    state, so the join counts (with gates of -0.7 the map is zero to working precision)."""
+    dk = 128
+    t, S0 = ref.inputs(op, lens, H, 1, dk, dk, io, seed=op + 270)
+    gen = torch.Generator().manual_seed(15)
+    t["g"] = (-0.001 - 0.019 * torch.rand(t["g"].shape, generator=gen) ** 4).cuda()   # mean -0.005
+    if t["beta"] is not None:
+        t["beta"] *= 0.1
+    desc, plan = make_desc(op, H, 1, dk, dk, io), make_plan(lens)
+    want, S_want = ref.scan(op, desc.scale, lens, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0)
+    at = np.cumsum([0] + lens)
+    for i, n in enumerate(lens):
+        chunks = (n + 63) // 64
+        segments = chunks // 8 if chunks >= 24 else 1
+        more = max(0, segments - 2) * 128 * 2.0 ** -23      # a contraction over 128 channels more for each join
+        assert err(out[at[i]:at[i + 1]], want[at[i]:at[i + 1]]) < TOL[io] + more, i
+        assert err(S[i], S_want[i]) < TOL_F32 + more, i
+        if segments > 1:    # the last segment behind a segment that starts from nothing, as if its map were zero: told apart
+            last, before = (64 * (chunks * (segments - x) // segments) for x in (1, 2))
+            part = [None if t[x] is None else t[x][at[i] + before:at[i + 1]] for x in ("q", "k", "v", "g", "beta")]
+            cold, _ = ref.scan(op, desc.scale, [n - before], *part, None, torch.zeros_like(S0[i:i + 1]))
+            first = slice(last - before, last - before + 64)
+            assert err(cold[first], want[at[i] + before:at[i + 1]][first]) > 4 * (TOL[io] + more)
+
+
+@pytest.mark.parametrize("io", [BF16, F32])
+def test_new_output_of_a_captured_prefill(io):
+    """The output's place is the graph's own and is written again by every replay: rows that ran in one replay and do not in the
+    next are zero then."""
+    op, H, d, n, most = ref.GDN, 2, 64, 5, 210
+    desc = make_desc(op, H, H, d, d, io, num_slots=n)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    lens, slots, plan, state = torch.zeros(n, **i32), torch.arange(n, **i32), dl.Plan(n, most, device="cuda"), pool(desc, 1)
+    ws = dl.scan_workspace(desc, n, most)
+    t, _ = ref.inputs(op, [most + 7], H, H, d, d, io, seed=280)
+
+    def step(out=None):
+        dl.build_plan(lens, plan, slots=slots, decode_rows=True)
+        return dl.prefill(desc, state, plan, **t, out=out, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    start = state.S_base.clone()
+    for ln in ([64, 1, 70, 0, 30], [1, 90, 0, 0, 1], [1] * 5, [0] * 5, [2, 200, 5, 3, 1], [1, 1, 1, 1, 206]):
+        lens.copy_(torch.tensor(ln, **i32))
+        slots.copy_(torch.tensor([0, 1, -1, 3, 4], **i32))
+        out.fill_(float("nan"))
+        state.S_base.copy_(start)
+        graph.replay()
+        got, S = out.clone(), state.S_base.clone()
+        state.S_base.copy_(start)
+        want = step(out=torch.zeros_like(out))
+        assert torch.equal(got, want) and torch.equal(S, state.S_base), ln
