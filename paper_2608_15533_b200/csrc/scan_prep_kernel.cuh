@@ -29,23 +29,33 @@ __device__ __forceinline__ bool chunk_place(const ScanArgs &a, int chunk, ChunkP
 
 // Zeros to the rows of `out` that no chain will write, for the CTA of a chunk that has nothing to prepare: a skipped row's
 // chunk clears its own tokens, and the entries behind the last chunk (with the CTA beyond the table) share those behind the last
-// sequence.  No launch of its own, and nothing is written twice, as a memset of the whole tensor in front would.
-template <typename IO>
-__device__ __forceinline__ void clear_unwritten(const ScanArgs &a, int chunk, int h, int tid, int nthreads) {
-    if (!a.clear) return;
-    const int seq = chunk < a.max_chunks ? a.chunk_seq[chunk] : -1;
-    long long first, last;
-    if (seq >= 0) {
-        first = a.starts[seq] + (chunk - a.chunk_starts[seq]) * kChunk;
-        last = min(first + kChunk, (long long)a.starts[seq + 1]);
-    } else {
-        const int chunks = a.chunk_starts[a.n];
-        const long long tokens = a.starts[a.n], tail = a.max_tokens - tokens, parts = a.max_chunks - chunks + 1;
-        first = tokens + tail * (chunk - chunks) / parts, last = tokens + tail * (chunk - chunks + 1) / parts;
+// sequence.  No launch of its own, and nothing is written twice, as a memset of the whole tensor in front would.  (Out of line:
+// inside, the code between a short prompt's instructions cost it a microsecond.)
+static __device__ __noinline__ void clear_rows(void *out, int first, int last, int H, int h, int row_bytes) {
+    const int lane = threadIdx.x & 31, units = row_bytes / 16;
+    for (int row = first + (int)(threadIdx.x >> 5); row < last; row += (int)(blockDim.x >> 5)) {
+        uint4 *dst = reinterpret_cast<uint4 *>(out) + ((size_t)row * H + h) * units;
+        for (int u = lane; u < units; u += 32) dst[u] = make_uint4(0u, 0u, 0u, 0u);
     }
-    const int units = a.dv * (int)sizeof(IO) / 16;
-    uint4 *out = reinterpret_cast<uint4 *>(static_cast<IO *>(a.out) + ((size_t)first * a.H + h) * a.dv);
-    for (long long i = tid; i < (last - first) * units; i += nthreads) out[(size_t)(i / units) * a.H * units + i % units] = make_uint4(0u, 0u, 0u, 0u);
+}
+static __device__ __noinline__ void clear_unwritten(void *out, const int32_t *starts, const int32_t *chunk_starts, const int32_t *chunk_seq, int n,
+                                                    int max_tokens, int max_chunks, int chunk, int H, int h, int row_bytes) {
+    const int seq = chunk < max_chunks ? chunk_seq[chunk] : -1;
+    if (seq >= 0) {
+        const int first = starts[seq] + (chunk - chunk_starts[seq]) * kChunk;
+        clear_rows(out, first, min(first + kChunk, starts[seq + 1]), H, h, row_bytes);
+        return;
+    }
+    const int tokens = starts[n], chunks = chunk_starts[n], tail = max_tokens - tokens;
+    if (tail <= 0) return;
+    const int parts = max_chunks - chunks + 1, each = (tail + parts - 1) / parts;
+    const long long first = tokens + (long long)each * (chunk - chunks);
+    if (first < max_tokens) clear_rows(out, (int)first, (int)min(first + each, (long long)max_tokens), H, h, row_bytes);
+}
+template <typename IO>
+__device__ __forceinline__ void clear_unwritten(const ScanArgs &a, int chunk, int h) {
+    if (a.clear)
+        clear_unwritten(a.out, a.starts, a.chunk_starts, a.chunk_seq, a.n, a.max_tokens, a.max_chunks, chunk, a.H, h, a.dv * (int)sizeof(IO));
 }
 
 constexpr int kInvStride = kChunk + 8;  // row of the fp32 matrices: fragment reads without bank conflicts
@@ -196,12 +206,12 @@ __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(c
     scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
         if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 128);
-        clear_unwritten<IO>(a, chunk, h, tid, 128);
+        clear_unwritten<IO>(a, chunk, h);
         return;
     }
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) {
-        clear_unwritten<IO>(a, chunk, h, tid, 128);
+        clear_unwritten<IO>(a, chunk, h);
         return;
     }
     const size_t unit = (size_t)chunk * a.H + h;
@@ -402,12 +412,12 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
     scan_kernel_begin();
     if (chunk == a.max_chunks) {  // one CTA beyond the chunks
         if (h == 0) order_rows(a, reinterpret_cast<int *>(smem), tid, 2 * DK);
-        clear_unwritten<IO>(a, chunk, h, tid, 2 * DK);
+        clear_unwritten<IO>(a, chunk, h);
         return;
     }
     ChunkPlace p;
     if (!chunk_place(a, chunk, p)) {
-        clear_unwritten<IO>(a, chunk, h, tid, 2 * DK);
+        clear_unwritten<IO>(a, chunk, h);
         return;
     }
     const size_t unit = (size_t)chunk * a.H + h;

@@ -181,9 +181,12 @@ def _out(out, tk: _Tokens, desc: Desc, plan: Plan):
     first = plan.max_tokens if plan.n > 0 else 0
     if first < tk.rows:
         out[first:].zero_()
-    d = _Desc.from_buffer_copy(d)
-    d.hints |= HINT_ZERO_UNWRITTEN
-    return out, d
+    cached = desc.__dict__.get("_c_zero")
+    if cached is None or cached[0] is not d:
+        zero = _Desc.from_buffer_copy(d)
+        zero.hints |= HINT_ZERO_UNWRITTEN
+        cached = desc.__dict__["_c_zero"] = (d, zero)
+    return out, cached[1]
 
 
 def _bytes(t: torch.Tensor) -> int:
