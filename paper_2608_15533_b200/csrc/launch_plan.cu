@@ -19,9 +19,10 @@ extern "C" int deltalog_build_plan(const int32_t *lens, const int32_t *slots, co
     const long long work = (plan->token_seq ? (plan->max_tokens + 3ll) / 4 : 0) + a.n + a.max_chunks;
     const long long ctas = (work + kPlanThreads - 1) / kPlanThreads;
     if (a.n <= kPlanShared) {
-        // few rows: fewer threads meet at the barriers sooner (512 requests, 50k tokens: 8.4 us with 1024, 7.3 us with 512;
-        // 20k requests: 38 us with 512, 26 us with 1024)
-        const int threads = a.n <= 256 && work <= 1024 ? 256 : a.n <= 4096 ? 512 : kPlanThreads;
+        // few rows: fewer threads meet at the barriers sooner; many: more share the scan that every CTA runs.  us per call, back
+        // to back in a graph, with 256 / 512 / 1024 threads: 64 requests 4.3 / 4.6 / 5.5, 512 requests (51k tokens) 5.0 / 5.1 / 6.3,
+        // 2048 requests 6.7 / 6.4 / 7.4, 4096 requests 9.3 / 7.5 / 8.2, 8192 requests 13.8 / 10.5 / 9.9, 20k documents 40 / 25 / 19
+        const int threads = a.n <= 512 ? 256 : a.n <= 4096 ? 512 : kPlanThreads;
         const long long need = (work + threads - 1) / threads;
         const int grid = (int)(need < 1 ? 1 : need > device_info().sms ? device_info().sms : need);
         const size_t smem = (size_t)2 * (a.n + 1) * sizeof(int32_t);
