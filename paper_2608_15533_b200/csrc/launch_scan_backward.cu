@@ -8,10 +8,10 @@ namespace {
 template <bool VEC, int P, int DK, bool DELTA, typename IO>
 int launch_chain(const ScanArgs &a, cudaStream_t s) {
     auto kernel = scan_backward_kernel<VEC, P, DK, DELTA, IO>;
-    const int warps = scan_chain_warps(a.n * a.H, a.dv);
+    const int warps = scan_chain_warps(a.n * a.H);
     const size_t smem = BackwardSmem<VEC, P, DK, DELTA, IO>::bytes(warps);
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    return launch_chained(kernel, dim3(a.n * a.H, a.dv / 16 / warps), warps * 32, smem, s, a);
+    return launch_chained(kernel, dim3(a.n * a.H, 4 / warps), warps * 32, smem, s, a);
 }
 
 }  // namespace

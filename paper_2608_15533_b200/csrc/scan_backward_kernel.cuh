@@ -32,7 +32,7 @@ struct BackwardSmem {
 };
 
 template <bool VEC, int P, int DK, bool DELTA, typename IO>
-__global__ void __launch_bounds__(256, 1) scan_backward_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a) {
     using L = BackwardSmem<VEC, P, DK, DELTA, IO>;
     constexpr int NT = DK / 8;
     constexpr bool F32IO = sizeof(IO) == 4;

@@ -37,7 +37,7 @@ struct ForwardSmem {
 };
 
 template <bool VEC, int P, int DK, bool DELTA, typename IO>
-__global__ void __launch_bounds__(256, 1) scan_forward_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(128, 1) scan_forward_kernel(const ScanArgs a) {
     using L = ForwardSmem<VEC, P, DK, DELTA, IO>;
     constexpr int NT = DK / 8;
     constexpr bool F32IO = sizeof(IO) == 4;

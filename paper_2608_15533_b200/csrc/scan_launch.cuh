@@ -82,13 +82,10 @@ inline ScanLayout scan_layout(const deltalog_desc *d, int32_t n, int32_t max_tok
         }                                                                            \
     } while (0)
 
-// Warps (16 columns of d_v each) of a chain CTA.  The warps of a CTA share the loads of q, k, A and T; a unit spread over
-// more CTAs reads them again, from L2.  While the units do not fill the device, smaller CTAs put it to work on more SMs.
-inline int scan_chain_warps(int units, int dv) {
-    int warps = dv / 16;
-    while (warps > 2 && units * (dv / 16 / warps) < device_info().sms) warps >>= 1;
-    return warps;
-}
+// Warps (16 columns of d_v = 64 each) of a CTA of the mma.sync chains.  The warps of a CTA share the loads of q, k, A and T; a
+// unit spread over two CTAs reads them again, from L2.  While the units do not fill the device, smaller CTAs put it to work on
+// more SMs.
+inline int scan_chain_warps(int units) { return units < device_info().sms ? 2 : 4; }
 
 int launch_scan_prep(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
 int launch_scan_forward(const deltalog_desc *d, const ScanArgs &a, cudaStream_t s);
