@@ -11,10 +11,10 @@
 // time is the threads' plane splits in between.  Of some 8k cycles a chunk (GDN, bf16) the products take half, the splits of S, R
 // and U and the update the other half, one behind the other; an SM's registers hold one such chain.
 // Against the mma.sync chain, bf16, 32 heads of 128: 48 ragged prompts of 36k tokens 1328 -> 659 us, one of 16k tokens 1671 -> 1091
-// us, 13k tokens of KDA 747 -> 323 us.  d_v = 64 would leave half of an MMA's rows empty and stays there.
-// Now: 630 us of the first; the second in three segments, 362 + 16 + 359 us; 305 us of the third.  With kept states, GDN: 195 us for
-// four rows of 2048 tokens, 811 us for 36.7k tokens of 19 rows (3.9 TB/s
-// of DRAM traffic, most of it what is kept).
+// us, 13k tokens of KDA 747 -> 323 us.  d_v = 64 stays there: half of an MMA's rows would be empty, though by the cycle counts
+// (32 for 128 x 64 x 16 half empty, 64 on mma.sync) its products would still be faster here; no such form has been built.
+// Now: 602 us of the first; the second in three segments, 350 + 16 + 354 us; 292 us of the third.  With kept states, GDN: 186 us for
+// four rows of 2048 tokens, 789 us for 36.7k tokens of 19 rows (3.9 TB/s of DRAM traffic, most of it what is kept).
 #pragma once
 
 #include "scan_tc_common.cuh"
@@ -378,7 +378,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
 
 // The states in front of a split row's segments: X_1 is the first segment's end, X_(s+1) = M_s X_s + E_s in E_s' place.
 // Sixteen columns per CTA, one row of M per thread; the next M is on its way while one is multiplied.  In fp32 throughout.
-// 8 CTAs per head keep a join at two microseconds or so, against the tens to hundreds that a segment takes.
+// Bound by latency: a join is d_k dependent steps of loads from shared memory behind a copy of M, 5 us or so for each, one behind the
+// other (16k tokens of GDN: 1 head, 29 joins 148 us of 242; 8 heads, 7 joins 43 us of 312; 32 heads, one join 16.4 us of 896, where
+// 256 CTAs of 148 KB also take two waves).
 constexpr int kJoinCols = 16;
 template <int DK>
 struct JoinSmem {

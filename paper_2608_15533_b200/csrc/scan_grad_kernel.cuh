@@ -21,9 +21,9 @@
 // for per-channel gates.
 // Bound by the phases of a chunk, one behind the other in the only CTA of an SM: 200 KB of operands (5k cycles, from L2), the
 // products over d_v and the sums beside them (9k), the products inside the chunk (10k; per-channel gates 30k).  bf16, 32 heads of 128:
-// GDN 8k tokens 437 us, 36.7k tokens 1955 us (2.8 TB/s of DRAM traffic; 2644 us before the next wave's
+// GDN 8k tokens 427 us, 36.7k tokens 1946 us (2.8 TB/s of DRAM traffic; 2644 us before the next wave's
 // operands went to L2 ahead and the in-chunk part shared its own), KDA 3.9k tokens
-// 461 us; RWKV6, 64 heads of 64, 4k tokens 451 us on mma.sync.  With the products over d_v on mma.sync as well GDN took 1.5 times
+// 455 us; RWKV6, 64 heads of 64, 4k tokens 440 us on mma.sync.  With the products over d_v on mma.sync as well GDN took 1.5 times
 // as long.
 // 512 threads; warp w owns token rows 16 (w & 3) .. + 15 and the channel quarter w >> 2 of every result: the work between
 // two barriers is a few hundred instructions per warp, and sixteen warps cover each other's latencies where eight did not.
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
             mbar_arrive_expect_tx(bar(2), L::kState);
             bulk_copy_g2s(sm + L::dS, a.dS + unit * tile, L::kState, bar(2));
             // One CTA fills an SM and begins by waiting for 200 KB.  What the CTA a wave further on will want goes from DRAM to
-            // L2 meanwhile (a CTA's wait 12k -> 5k cycles); the wave is 37 MB.
+            // L2 meanwhile (a CTA's wait 12k -> 5k cycles); the wave is 148 x 192 KB, 29 MB.
             const size_t next = (size_t)h * gridDim.x + chunk + a.wave, ahead = next % gridDim.x * a.H + next / gridDim.x;
             if (next < (size_t)gridDim.x * a.H) {
                 l2_prefetch(a.S + ahead * tile, L::kState), l2_prefetch(a.dS + ahead * tile, L::kState);

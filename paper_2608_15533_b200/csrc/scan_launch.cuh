@@ -16,6 +16,8 @@ struct ScanLayout {
 // Segments that a row may be cut into: as many as leave every chain of the first pass an SM of its own, none for rows that
 // are short for it.  One GDN row in segments against one chain, us with preparation: 8 heads, 1536 tokens 97 / 116, 4096 tokens
 // 127 / 280, 16k tokens 303 / 1079; 32 heads 116 / 127, 244 / 308, 859 / 1185; 48 heads 127 / 131, 271 / 328, 934 / 1256.
+// (n counts the plan's rows, those that decode among them, since the host knows no lengths: the 16k row of 32 heads takes 874 us by
+// itself and 1210 among 47 decoding rows, where it runs as one chain.)
 inline int scan_split(const deltalog_desc *d, int32_t n, int32_t max_tokens) {
     const long long units = (long long)n * d->H;
     if (d->d_v != 128 || units < 1 || units * scan_pieces(3) > kSplitCtas) return 1;

@@ -418,3 +418,44 @@ def test_new_output_of_a_captured_prefill(io):
         state.S_base.copy_(start)
         want = step(out=torch.zeros_like(out))
         assert torch.equal(got, want) and torch.equal(S, state.S_base), ln
+
+
+@pytest.mark.parametrize("op,io,H,Hq,dk,dv,lens,tail", [
+    (ref.GDN, BF16, 4, 2, 128, 128, [17, 0, 1, 64, 200], 5), (ref.KDA, BF16, 2, 1, 128, 128, [129, 63], 0), (ref.RWKV6, BF16, 2, 2, 64, 64, [65, 3, 190], 1),
+    (ref.KDA, F32, 2, 1, 64, 128, [70, 64], 64), (ref.GLA, F32, 3, 3, 128, 64, [5, 127], 0), (ref.RETNET, F32, 2, 1, 64, 64, [64], 0),
+    (ref.LINATTN, BF16, 1, 1, 64, 128, [1537, 9], 70), (ref.GDN, BF16, 1, 1, 128, 128, [1700], 0)])
+def test_nothing_is_written_beside_the_tensors(op, io, H, Hq, dk, dv, lens, tail):
+    """The workspace at its very size, the output and the plan's tables lie in larger buffers whose other bytes stay as they were."""
+    room = 4096
+
+    def inside(shape, dtype):
+        size = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        whole = torch.full((size + 2 * room,), 0x5A, dtype=torch.uint8, device="cuda")
+        return whole, whole[room:room + size].view(dtype).view(shape)
+
+    wholes = []
+
+    def place(like_shape, dtype):
+        whole, view = inside(like_shape, dtype)
+        wholes.append((whole, view.numel() * view.element_size()))
+        return view
+
+    n, most = len(lens), sum(lens) + tail
+    t, S0 = ref.inputs(op, lens, H, Hq, dk, dv, io, seed=op + 290, tail=tail)
+    desc = make_desc(op, H, Hq, dk, dv, io, num_slots=n)
+    plan = dl.Plan(n, most, device="cuda")
+    for name in ("starts", "chunk_starts", "chunk_seq", "token_seq", "scan_slots", "append_slots", "merge_slots", "totals"):
+        setattr(plan, name, place((getattr(plan, name).numel(),), torch.int32))
+    dl.build_plan(torch.tensor(lens, dtype=torch.int32, device="cuda"), plan)
+    out = place(tuple(t["v"].shape), io)
+    dout = torch.ones_like(t["v"])
+    serve, train = ((place((dl.scan_workspace(desc, n, most, train=x).numel(),), torch.uint8)) for x in (False, True))
+    dl.prefill(desc, pool(desc, 1), plan, **t, out=out, workspace=serve)
+    dl.scan_forward(desc, plan, **t, S_init=S0, out=out, workspace=serve)
+    dl.scan_forward(desc, plan, **t, S_init=S0, out=out, workspace=train, save=True)
+    dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, workspace=train, saved=True)
+    torch.cuda.synchronize()
+    for whole, size in wholes:
+        assert (whole[:room] == 0x5A).all() and (whole[room + size:] == 0x5A).all()
+    want, S_want = ref.scan(op, desc.scale, lens, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
+    assert err(out[:sum(lens)], want) < TOL[io] + 128 * 2.0 ** -23 and (out[sum(lens):].contiguous().view(torch.uint8) == 0x5A).all()
