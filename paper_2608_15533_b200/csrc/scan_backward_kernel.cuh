@@ -113,14 +113,20 @@ __global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a)
             uint32_t f[kPlanes][4];
             acc_to_a<kPlanes>(s[2 * kk], s[2 * kk + 1], f);
 #pragma unroll
-            for (int nn = 0; nn < 4; nn += 2)
+            for (int nn = 0; nn < 4; nn += 2) {
+                // (fp32 io: a step's products apart from the sum, see mma_planes)
+                float x[4][4] = {};
+                float (&u0)[4] = F32IO ? x[0] : du[2 * nn], (&u1)[4] = F32IO ? x[1] : du[2 * nn + 1];
+                float (&u2)[4] = F32IO ? x[2] : du[2 * nn + 2], (&u3)[4] = F32IO ? x[3] : du[2 * nn + 3];
 #pragma unroll
-                for (int pl = 0; pl < L::kVecs; ++pl) {
+                for (int pl = L::kVecs - 1; pl >= 0; --pl) {
                     uint32_t b[4], e[4];
                     load_b(b, k_s + pl * L::kTile, nn * 16, kk * 16, lane);
                     load_b(e, k_s + pl * L::kTile, nn * 16 + 16, kk * 16, lane);
-                    mma_planes2<kPlanes, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
+                    mma_planes2<kPlanes, kPlanes>(u0, u1, u2, u3, f, b, e, pl);
                 }
+                if (F32IO) add_to(du[2 * nn], x[0]), add_to(du[2 * nn + 1], x[1]), add_to(du[2 * nn + 2], x[2]), add_to(du[2 * nn + 3], x[3]);
+            }
         }
         if (!VEC) {
 #pragma unroll
@@ -142,15 +148,20 @@ __global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a)
             uint32_t f[OP1][4];
             acc_to_a<OP1>(x[0], x[1], f);
 #pragma unroll
-            for (int pl = 0; pl < kPlanes; ++pl) {
-                uint32_t b[4], e[4];
+            for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
+                float y[4][4] = {};
+                float (&u0)[4] = F32IO ? y[0] : du[2 * nn], (&u1)[4] = F32IO ? y[1] : du[2 * nn + 1];
+                float (&u2)[4] = F32IO ? y[2] : du[(2 * nn + 2) & 7], (&u3)[4] = F32IO ? y[3] : du[(2 * nn + 3) & 7];
 #pragma unroll
-                for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
+                for (int pl = kPlanes - 1; pl >= 0; --pl) {
+                    uint32_t b[4], e[4];
                     load_b_t(b, sm + L::A + pl * L::kMat, kb * 16, nn * 16, lane);
                     if (nn < kb) load_b_t(e, sm + L::A + pl * L::kMat, kb * 16, nn * 16 + 16, lane);
-                    if (nn < kb) mma_planes2<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], du[2 * nn + 2], du[2 * nn + 3], f, b, e, pl);
-                    else mma_planes<OP1, kPlanes>(du[2 * nn], du[2 * nn + 1], f, b, pl);
+                    if (nn < kb) mma_planes2<OP1, kPlanes>(u0, u1, u2, u3, f, b, e, pl);
+                    else mma_planes<OP1, kPlanes>(u0, u1, f, b, pl);
                 }
+                if (F32IO) add_to(du[2 * nn], y[0]), add_to(du[2 * nn + 1], y[1]);
+                if (F32IO && nn < kb) add_to(du[2 * nn + 2], y[2]), add_to(du[2 * nn + 3], y[3]);
             }
         }
         // dV^T = dU^T T
@@ -161,15 +172,20 @@ __global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a)
                 uint32_t f[kPlanes][4];
                 acc_to_a<kPlanes>(du[2 * kb], du[2 * kb + 1], f);
 #pragma unroll
-                for (int pl = 0; pl < kPlanes; ++pl) {
-                    uint32_t b[4], e[4];
+                for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
+                    float y[4][4] = {};
+                    float (&w0)[4] = F32IO ? y[0] : w[2 * nn], (&w1)[4] = F32IO ? y[1] : w[2 * nn + 1];
+                    float (&w2)[4] = F32IO ? y[2] : w[(2 * nn + 2) & 7], (&w3)[4] = F32IO ? y[3] : w[(2 * nn + 3) & 7];
 #pragma unroll
-                    for (int nn = 0; nn <= kb; nn += 2) {  // the last block pair's second may lie above the diagonal
+                    for (int pl = kPlanes - 1; pl >= 0; --pl) {
+                        uint32_t b[4], e[4];
                         load_b_t(b, sm + L::T + pl * L::kMat, kb * 16, nn * 16, lane);
                         if (nn < kb) load_b_t(e, sm + L::T + pl * L::kMat, kb * 16, nn * 16 + 16, lane);
-                        if (nn < kb) mma_planes2<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], w[2 * nn + 2], w[2 * nn + 3], f, b, e, pl);
-                        else mma_planes<kPlanes, kPlanes>(w[2 * nn], w[2 * nn + 1], f, b, pl);
+                        if (nn < kb) mma_planes2<kPlanes, kPlanes>(w0, w1, w2, w3, f, b, e, pl);
+                        else mma_planes<kPlanes, kPlanes>(w0, w1, f, b, pl);
                     }
+                    if (F32IO) add_to(w[2 * nn], y[0]), add_to(w[2 * nn + 1], y[1]);
+                    if (F32IO && nn < kb) add_to(w[2 * nn + 2], y[2]), add_to(w[2 * nn + 3], y[3]);
                 }
             }
 #pragma unroll
@@ -213,14 +229,19 @@ __global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a)
                 uint32_t f[OP2][4];
                 acc_to_a<OP2>(x[0], x[1], f);
 #pragma unroll
-                for (int nn = 0; nn < NT / 2; nn += 2)
+                for (int nn = 0; nn < NT / 2; nn += 2) {
+                    float y[4][4] = {};
+                    float (&s0)[4] = F32IO ? y[0] : s[2 * nn], (&s1)[4] = F32IO ? y[1] : s[2 * nn + 1];
+                    float (&s2)[4] = F32IO ? y[2] : s[2 * nn + 2], (&s3)[4] = F32IO ? y[3] : s[2 * nn + 3];
 #pragma unroll
-                    for (int pl = 0; pl < L::kVecs; ++pl) {
+                    for (int pl = L::kVecs - 1; pl >= 0; --pl) {
                         uint32_t b[4], e[4];
                         load_b_t(b, sm + L::q + pl * L::kTile, kb * 16, nn * 16, lane);
                         load_b_t(e, sm + L::q + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
-                        mma_planes2<OP2, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
+                        mma_planes2<OP2, kPlanes>(s0, s1, s2, s3, f, b, e, pl);
                     }
+                    if (F32IO) add_to(s[2 * nn], y[0]), add_to(s[2 * nn + 1], y[1]), add_to(s[2 * nn + 2], y[2]), add_to(s[2 * nn + 3], y[3]);
+                }
             }
             if (DELTA) {
 #pragma unroll
@@ -231,14 +252,19 @@ __global__ void __launch_bounds__(128, 1) scan_backward_kernel(const ScanArgs a)
                 acc_to_a<kPlanes>(x[0], x[1], f);
                 const uint32_t kt_s = VEC ? sm + L::kt : k_s;
 #pragma unroll
-                for (int nn = 0; nn < NT / 2; nn += 2)
+                for (int nn = 0; nn < NT / 2; nn += 2) {
+                    float y[4][4] = {};
+                    float (&s0)[4] = F32IO ? y[0] : s[2 * nn], (&s1)[4] = F32IO ? y[1] : s[2 * nn + 1];
+                    float (&s2)[4] = F32IO ? y[2] : s[2 * nn + 2], (&s3)[4] = F32IO ? y[3] : s[2 * nn + 3];
 #pragma unroll
-                    for (int pl = 0; pl < L::kVecs; ++pl) {
+                    for (int pl = L::kVecs - 1; pl >= 0; --pl) {
                         uint32_t b[4], e[4];
                         load_b_t(b, kt_s + pl * L::kTile, kb * 16, nn * 16, lane);
                         load_b_t(e, kt_s + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
-                        mma_planes2<kPlanes, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
+                        mma_planes2<kPlanes, kPlanes>(s0, s1, s2, s3, f, b, e, pl);
                     }
+                    if (F32IO) add_to(s[2 * nn], y[0]), add_to(s[2 * nn + 1], y[1]), add_to(s[2 * nn + 2], y[2]), add_to(s[2 * nn + 3], y[3]);
+                }
             }
         }
         __syncthreads();

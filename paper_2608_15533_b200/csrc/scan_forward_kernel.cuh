@@ -121,21 +121,28 @@ __global__ void __launch_bounds__(128, 1) scan_forward_kernel(const ScanArgs a) 
 #pragma unroll
             for (int nn = 0; nn < 4; nn += DELTA ? 1 : 2) {
                 // delta rule: k and q in turn; otherwise two tiles of q
+                // (fp32 io: a step's products apart from the sum, see mma_planes)
+                float x[4][4] = {};
+                float (&k0)[4] = F32IO ? x[2] : ak[2 * nn], (&k1)[4] = F32IO ? x[3] : ak[2 * nn + 1];
+                float (&q0)[4] = F32IO ? x[0] : aq[2 * nn], (&q1)[4] = F32IO ? x[1] : aq[2 * nn + 1];
+                float (&q2)[4] = F32IO ? x[2] : aq[(2 * nn + 2) & 7], (&q3)[4] = F32IO ? x[3] : aq[(2 * nn + 3) & 7];
 #pragma unroll
-                for (int pl = 0; pl < kPlanes; ++pl) {
+                for (int pl = kPlanes - 1; pl >= 0; --pl) {
                     uint32_t b[4], e[4];
                     if (DELTA && pl < L::kK) load_b(b, k_s + pl * L::kTile, nn * 16, kk * 16, lane);
                     if (pl < L::kQ) load_b(e, sm + L::q + pl * L::kTile, nn * 16, kk * 16, lane);
                     if (!DELTA && pl < L::kQ) load_b(b, sm + L::q + pl * L::kTile, nn * 16 + 16, kk * 16, lane);
 #pragma unroll
-                    for (int pa = 0; pa + pl < kPlanes; ++pa) {
-                        if (DELTA && pl < L::kK) mma(ak[2 * nn], f[pa], b[0], b[1]), mma(ak[2 * nn + 1], f[pa], b[2], b[3]);
-                        if (pl < L::kQ && pa + pl < L::kOut) {
-                            mma(aq[2 * nn], f[pa], e[0], e[1]), mma(aq[2 * nn + 1], f[pa], e[2], e[3]);
-                            if (!DELTA) mma(aq[(2 * nn + 2) & 7], f[pa], b[0], b[1]), mma(aq[(2 * nn + 3) & 7], f[pa], b[2], b[3]);
-                        }
+                    for (int pa = kPlanes - 1 - pl; pa >= 0; --pa) {
+                        const bool q = pl < L::kQ && pa + pl < L::kOut;
+                        if (DELTA && pl < L::kK) mma(k0, f[pa], b[0], b[1]), mma(k1, f[pa], b[2], b[3]);
+                        if (q) mma(q0, f[pa], e[0], e[1]), mma(q1, f[pa], e[2], e[3]);
+                        if (q && !DELTA) mma(q2, f[pa], b[0], b[1]), mma(q3, f[pa], b[2], b[3]);
                     }
                 }
+                if (F32IO) add_to(aq[2 * nn], x[0]), add_to(aq[2 * nn + 1], x[1]);
+                if (F32IO && !DELTA) add_to(aq[(2 * nn + 2) & 7], x[2]), add_to(aq[(2 * nn + 3) & 7], x[3]);
+                if (F32IO && DELTA) add_to(ak[2 * nn], x[2]), add_to(ak[2 * nn + 1], x[3]);
             }
         }
         __syncthreads();
@@ -172,15 +179,20 @@ __global__ void __launch_bounds__(128, 1) scan_forward_kernel(const ScanArgs a) 
                 uint32_t f[kPlanes][4], b[4];
                 acc_to_a<kPlanes>(ak[2 * kb], ak[2 * kb + 1], f);
 #pragma unroll
-                for (int pl = 0; pl < kPlanes; ++pl) {
-                    uint32_t e[4];
+                for (int nn = kb & ~1; nn < 4; nn += 2) {  // the block pairs' first may lie above the diagonal
+                    float x[4][4] = {};
+                    float (&u0)[4] = F32IO ? x[0] : u[2 * nn], (&u1)[4] = F32IO ? x[1] : u[2 * nn + 1];
+                    float (&u2)[4] = F32IO ? x[2] : u[2 * nn + 2], (&u3)[4] = F32IO ? x[3] : u[2 * nn + 3];
 #pragma unroll
-                    for (int nn = kb & ~1; nn < 4; nn += 2) {  // the block pairs' first may lie above the diagonal
+                    for (int pl = kPlanes - 1; pl >= 0; --pl) {
+                        uint32_t e[4];
                         if (nn >= kb) load_b(b, sm + L::T + pl * L::kMat, nn * 16, kb * 16, lane);
                         load_b(e, sm + L::T + pl * L::kMat, nn * 16 + 16, kb * 16, lane);
-                        if (nn >= kb) mma_planes2<kPlanes, kPlanes>(u[2 * nn], u[2 * nn + 1], u[2 * nn + 2], u[2 * nn + 3], f, b, e, pl);
-                        else mma_planes<kPlanes, kPlanes>(u[2 * nn + 2], u[2 * nn + 3], f, e, pl);
+                        if (nn >= kb) mma_planes2<kPlanes, kPlanes>(u0, u1, u2, u3, f, b, e, pl);
+                        else mma_planes<kPlanes, kPlanes>(u2, u3, f, e, pl);
                     }
+                    if (F32IO && nn >= kb) add_to(u[2 * nn], x[0]), add_to(u[2 * nn + 1], x[1]);
+                    if (F32IO) add_to(u[2 * nn + 2], x[2]), add_to(u[2 * nn + 3], x[3]);
                 }
             }
             if (a.keep) store_slice(a.U + unit * kChunk * a.dv + v0, a.dv, kChunk, u, 0u, lane);
@@ -191,15 +203,20 @@ __global__ void __launch_bounds__(128, 1) scan_forward_kernel(const ScanArgs a) 
             uint32_t f[UO][4], b[4];
             acc_to_a<UO>(u[2 * kb], u[2 * kb + 1], f);
 #pragma unroll
-            for (int pl = 0; pl < L::kOut; ++pl) {
-                uint32_t e[4];
+            for (int nn = kb & ~1; nn < 4; nn += 2) {
+                float x[4][4] = {};
+                float (&o0)[4] = F32IO ? x[0] : aq[2 * nn], (&o1)[4] = F32IO ? x[1] : aq[2 * nn + 1];
+                float (&o2)[4] = F32IO ? x[2] : aq[2 * nn + 2], (&o3)[4] = F32IO ? x[3] : aq[2 * nn + 3];
 #pragma unroll
-                for (int nn = kb & ~1; nn < 4; nn += 2) {
+                for (int pl = L::kOut - 1; pl >= 0; --pl) {
+                    uint32_t e[4];
                     if (nn >= kb) load_b(b, sm + L::A + pl * L::kMat, nn * 16, kb * 16, lane);
                     load_b(e, sm + L::A + pl * L::kMat, nn * 16 + 16, kb * 16, lane);
-                    if (nn >= kb) mma_planes2<UO, L::kOut>(aq[2 * nn], aq[2 * nn + 1], aq[2 * nn + 2], aq[2 * nn + 3], f, b, e, pl);
-                    else mma_planes<UO, L::kOut>(aq[2 * nn + 2], aq[2 * nn + 3], f, e, pl);
+                    if (nn >= kb) mma_planes2<UO, L::kOut>(o0, o1, o2, o3, f, b, e, pl);
+                    else mma_planes<UO, L::kOut>(o2, o3, f, e, pl);
                 }
+                if (F32IO && nn >= kb) add_to(aq[2 * nn], x[0]), add_to(aq[2 * nn + 1], x[1]);
+                if (F32IO) add_to(aq[2 * nn + 2], x[2]), add_to(aq[2 * nn + 3], x[3]);
             }
         }
         if (a.out)
@@ -239,14 +256,19 @@ __global__ void __launch_bounds__(128, 1) scan_forward_kernel(const ScanArgs a) 
             uint32_t f[US][4];
             acc_to_a<US>(u[2 * kb], u[2 * kb + 1], f);
 #pragma unroll
-            for (int nn = 0; nn < NT / 2; nn += 2)
+            for (int nn = 0; nn < NT / 2; nn += 2) {
+                float x[4][4] = {};
+                float (&s0)[4] = F32IO ? x[0] : s[2 * nn], (&s1)[4] = F32IO ? x[1] : s[2 * nn + 1];
+                float (&s2)[4] = F32IO ? x[2] : s[2 * nn + 2], (&s3)[4] = F32IO ? x[3] : s[2 * nn + 3];
 #pragma unroll
-                for (int pl = 0; pl < L::kK; ++pl) {
+                for (int pl = L::kK - 1; pl >= 0; --pl) {
                     uint32_t b[4], e[4];
                     load_b_t(b, ku_s + pl * L::kTile, kb * 16, nn * 16, lane);
                     load_b_t(e, ku_s + pl * L::kTile, kb * 16, nn * 16 + 16, lane);
-                    mma_planes2<US, kPlanes>(s[2 * nn], s[2 * nn + 1], s[2 * nn + 2], s[2 * nn + 3], f, b, e, pl);
+                    mma_planes2<US, kPlanes>(s0, s1, s2, s3, f, b, e, pl);
                 }
+                if (F32IO) add_to(s[2 * nn], x[0]), add_to(s[2 * nn + 1], x[1]), add_to(s[2 * nn + 2], x[2]), add_to(s[2 * nn + 3], x[3]);
+            }
         }
         if (!L::kTwice) __syncthreads();
         if (c + 1 < nchunks) load_update(c + 1);

@@ -232,13 +232,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
         ok = bounded_wait(full(0, c), parity, tc.abort_flag) && ok;
         if (issuing()) {
             const uint32_t pl = tc.tmem + PL, b = st + L::kq;
-            if (DELTA && (kApart || !emit)) {
-                tc_product<kPlanes, 0, L::kQ, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b);
-                tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more, false);
-            } else if (DELTA) {
-                tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, 2 * kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b);
-                tc_product<kPlanes, 0, L::kQ, L::kOut, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b, false);
-                tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more, false);
+            if (DELTA) {
+                // (k S takes the same products in the same order with and without q S beside it: the same bits)
+                constexpr bool kMore = L::kK > L::kQ, kAlone = kMore || L::kOut < kPlanes;
+                tc_product<kPlanes, L::kQ, L::kK, 0, kPlanes, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC0, pl, st + L::k_more);
+                tc_product<kPlanes, 0, L::kQ, L::kOut, kPlanes, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b, !kMore);
+                if (kApart || !emit)
+                    tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, kChunk, DK / 2, L::kPair, L::kPairHalf>(tc.tmem + ACC0, pl, b, !kAlone);
+                else
+                    tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, 2 * kChunk, DK / 2, L::kPair, L::kPairHalf, kAlone>(tc.tmem + ACC0, pl, b);
             } else if (emit) {
                 tc_product<kPlanes, 0, L::kQ, 0, L::kOut, false, DK / 16, kChunk, DK / 2, L::kTile>(tc.tmem + ACC1, pl, b);
             }

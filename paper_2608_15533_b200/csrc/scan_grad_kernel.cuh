@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
     constexpr int NT = DK / 32, SW = L::kSW, MW = L::kMW;
     constexpr int GP = sizeof(IO) == 4 ? kPlanes : 2;  // planes of an fp32 operand
     constexpr int IP = sizeof(IO) == 4 ? GP : 1;       // and of dO and v
+    constexpr bool kApart = sizeof(IO) == 4;           // a step's plane products apart from the sum (two planes leave more than the cut)
     extern __shared__ __align__(1024) unsigned char smem_grad[];
     unsigned char *smem = smem_grad;
     const uint32_t sm = smem_addr(smem);
@@ -387,19 +388,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
                 for (int nn = 0; nn < NT / 2; ++nn) {
                     uint32_t b[GP][4];
                     frag_b_t(b, S, SW, k0, c0 + nn * 16, lane);
-                    mma_all(dq[2 * nn], dq[2 * nn + 1], f, b);
-                    if (DELTA) mma_all(dr[2 * nn], dr[2 * nn + 1], e, b);
+                    mma_all<kApart>(dq[2 * nn], dq[2 * nn + 1], f, b);
+                    if (DELTA) mma_all<kApart>(dr[2 * nn], dr[2 * nn + 1], e, b);
                 }
                 if (cq <= mt) {
                     if constexpr (DELTA) {
                         uint32_t b[GP][4];
                         frag_b(b, u_f, kSliceStride, cq * 16, k0, lane);
-                        mma_all(da[0], da[1], f, b);
-                        mma_all(dl[0], dl[1], e, b);
+                        mma_all<kApart>(da[0], da[1], f, b);
+                        mma_all<kApart>(dl[0], dl[1], e, b);
                     } else {
                         uint32_t b[IP][4];
                         io_frag_b(b, st + L::U, cq * 16, k0, lane);
-                        mma_all(da[0], da[1], f, b);
+                        mma_all<kApart>(da[0], da[1], f, b);
                     }
                 }
             }
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
             for (int nn = 0; nn < NT / 2; ++nn) {
                 uint32_t b[GP][4];
                 frag_b_t(b, dS, SW, k0, c0 + nn * 16, lane);
-                mma_all(dw[2 * nn], dw[2 * nn + 1], f, b);
+                mma_all<kApart>(dw[2 * nn], dw[2 * nn + 1], f, b);
             }
         }
         // <dS_1, S_0> by channel, and sum_v dV U by token (eight threads each)
@@ -495,13 +496,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
                 if (transposed) frag_a_t(m, mat, MW, kb * 16, mt * 16, lane);
                 else frag_a(m, mat, MW, mt * 16, kb * 16, lane);
 #pragma unroll
-                for (int nn = 0; nn < NT / 2; ++nn)
+                for (int nn = 0; nn < NT / 2; ++nn) {
+                    uint32_t b[P][4];
 #pragma unroll
-                    for (int pl = 0; pl < P; ++pl) {
-                        uint32_t b[4];
-                        load_b_t(b, vec + pl * L::kTile, kb * 16, c0 + nn * 16, lane);
-                        mma_planes<kPlanes, kPlanes>(x[2 * nn], x[2 * nn + 1], m, b, pl);
-                    }
+                    for (int pl = 0; pl < P; ++pl) load_b_t(b[pl], vec + pl * L::kTile, kb * 16, c0 + nn * 16, lane);
+                    mma_all<kApart>(x[2 * nn], x[2 * nn + 1], m, b);
+                }
             };
             if (kb <= mt) {
                 product(dq, da_f, false, k_s);
@@ -642,8 +642,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
             for (int nn = 0; nn < NT / 2; ++nn) {
                 uint32_t b[kPlanes][4];
                 vector_frag(b, kc, J, nn);
-                mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
-                if (DELTA) mma_all(acc_l[2 * nn], acc_l[2 * nn + 1], l, b);
+                mma_all<kApart>(acc[2 * nn], acc[2 * nn + 1], m, b);
+                if (DELTA) mma_all<kApart>(acc_l[2 * nn], acc_l[2 * nn + 1], l, b);
             }
         }
         auto finish_front = [&](float (&x)[NT][4], float (&in)[NT][4], const float *mat, float sign) {
@@ -668,14 +668,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) scan_grad_kernel(const ScanAr
 #pragma unroll
             for (int nn = 0; nn < NT / 2; ++nn) {
                 vector_frag(b, qs, I, nn);
-                mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
+                mma_all<kApart>(acc[2 * nn], acc[2 * nn + 1], m, b);
             }
             if (DELTA) {
                 frag_a_t(m, dl_f, MW, I * 16, mt * 16, lane);
 #pragma unroll
                 for (int nn = 0; nn < NT / 2; ++nn) {
                     vector_frag(b, ks, I, nn);
-                    mma_all(acc[2 * nn], acc[2 * nn + 1], m, b);
+                    mma_all<kApart>(acc[2 * nn], acc[2 * nn + 1], m, b);
                 }
             }
         }

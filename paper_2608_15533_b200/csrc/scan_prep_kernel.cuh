@@ -279,12 +279,12 @@ __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(c
 #pragma unroll
         for (int nn = 0; nn < 4; ++nn) {
             if (nn > warp) break;
+            {
+                uint32_t b[P][4];
 #pragma unroll
-            for (int pl = 0; pl < P; ++pl) {
-                uint32_t b[4];
-                load_b(b, k_s + pl * kTile, nn * 16, k0, lane);
-                mma_planes<P, P>(qa[2 * nn], qa[2 * nn + 1], aq, b, pl);
-                if (DELTA) mma_planes<P, P>(ka[2 * nn], ka[2 * nn + 1], ak, b, pl);
+                for (int pl = 0; pl < P; ++pl) load_b(b[pl], k_s + pl * kTile, nn * 16, k0, lane);
+                mma_all(qa[2 * nn], qa[2 * nn + 1], aq, b);
+                if (DELTA) mma_all(ka[2 * nn], ka[2 * nn + 1], ak, b);
             }
         }
     }
@@ -530,7 +530,9 @@ __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(cons
                         const float2 y = *reinterpret_cast<const float2 *>(src + (e & 1) * 8 * VS + (e >> 1) * 8);
                         frag_pair(x, e, y.x * w[e >> 1].x, y.y * w[e >> 1].y);
                     }
-                    mma_all(acc[round][m][0], acc[round][m][1], x, b);
+                    // (A of bf16 tensors meets bf16 values only: its steps straight into the sum)
+                    if (m == 0 && sizeof(IO) == 2) mma_all<false>(acc[round][m][0], acc[round][m][1], x, b);
+                    else mma_all(acc[round][m][0], acc[round][m][1], x, b);
                 }
             }
         } else {

@@ -82,20 +82,30 @@ __device__ __forceinline__ void tmem_st_planes(uint32_t addr, int plane, const f
 // The plane products (index sum LO <= pa + pb < HI) of A (planes A_PLANE columns apart) with the image planes PB0 .. PB1 - 1
 // of B (`b`: plane PB0), issued by one thread.  Everything but the addresses is a constant and the loops unroll: a product of
 // 128 x 64 x 16 takes the tensor core 32 cycles, and with descriptors put together for each the issuing thread needed 60.
+// The smallest products go first, where the sum is still small: the tensor cores cut an accumulator's last bits (see mma_planes), and behind
+// the leading products the others cut the sum forty times more (states 6e-7 off instead of 8e-8).
 // K-major B (rows are n): a step of 16 is 32 bytes of a row, 64 columns per image half.  MN-major B (rows are k): 16 rows.
-template <int PA, int PB0, int PB1, int LO, int HI, bool MN, int STEPS, int N, int A_PLANE, int B_PLANE, int HALF = kChunk * 128>
+// SPLIT: B's rows are two operands of N / 2 = 64, and D's first half is a sum already while the second starts here.
+template <int PA, int PB0, int PB1, int LO, int HI, bool MN, int STEPS, int N, int A_PLANE, int B_PLANE, int HALF = kChunk * 128, bool SPLIT = false>
 __device__ __forceinline__ void tc_product(uint32_t d, uint32_t a, uint32_t b, bool first = true) {
     const uint64_t desc = image_desc(b, HALF);
-    bool clear = first;
+    bool clear = first, split = SPLIT;
 #pragma unroll
-    for (int pb = PB0; pb < PB1; ++pb)
+    for (int order = PA + PB1 - 2; order >= 0; --order)
 #pragma unroll
-        for (int pa = 0; pa < PA; ++pa) {
-            if (pa + pb < LO || pa + pb >= HI) continue;
+        for (int pb = PB0; pb < PB1; ++pb) {
+            const int pa = order - pb;
+            if (pa < 0 || pa >= PA || order < LO || order >= HI) continue;
 #pragma unroll
             for (int k = 0; k < STEPS; ++k) {
                 const int off = (pb - PB0) * B_PLANE + (MN ? k * 2048 : (k >> 2) * HALF + (k & 3) * 32);
-                tc_mma(d, a + pa * A_PLANE + k * 8, desc + (off >> 4), tc_idesc(N, MN), !clear);
+                if (split) {
+                    tc_mma(d, a + pa * A_PLANE + k * 8, desc + (off >> 4), tc_idesc(N / 2, MN), true);
+                    tc_mma(d + N / 2, a + pa * A_PLANE + k * 8, desc + ((off + kChunk * 128) >> 4), tc_idesc(N / 2, MN), false);
+                    split = false;
+                } else {
+                    tc_mma(d, a + pa * A_PLANE + k * 8, desc + (off >> 4), tc_idesc(N, MN), !clear);
+                }
                 clear = false;
             }
         }
@@ -106,10 +116,11 @@ __device__ __forceinline__ void tc_product_lower(uint32_t d, uint32_t a, uint32_
     const uint64_t desc = image_desc(b);
     bool clear = true;
 #pragma unroll
-    for (int pb = 0; pb < PB; ++pb)
+    for (int order = LIMIT - 1; order >= 0; --order)
 #pragma unroll
-        for (int pa = 0; pa < PA; ++pa) {
-            if (pa + pb >= LIMIT) continue;
+        for (int pb = 0; pb < PB; ++pb) {
+            const int pa = order - pb;
+            if (pa < 0 || pa >= PA) continue;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int off = pb * (kChunk * kChunk * 2) + k * 2048 + k * 32;
@@ -125,10 +136,11 @@ __device__ __forceinline__ void tc_product_upper(uint32_t d, uint32_t a, uint32_
     const uint64_t desc = image_desc(b);
     bool clear = first;
 #pragma unroll
-    for (int pb = 0; pb < PB; ++pb)
+    for (int order = LIMIT - 1; order >= 0; --order)
 #pragma unroll
-        for (int pa = 0; pa < PA; ++pa) {
-            if (pa + pb >= LIMIT) continue;
+        for (int pb = 0; pb < PB; ++pb) {
+            const int pa = order - pb;
+            if (pa < 0 || pa >= PA) continue;
 #pragma unroll
             for (int k = 3; k >= 0; --k) {
                 const int off = pb * (kChunk * kChunk * 2) + k * 2048;
@@ -203,10 +215,11 @@ __device__ __forceinline__ void tc_product_state(uint32_t d, uint32_t a, uint32_
     const uint64_t desc = (uint64_t)((b & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(kKeptGroup >> 4) << 32) | ((uint64_t)1 << 46);
     bool clear = true;
 #pragma unroll
-    for (int pb = 0; pb < 2; ++pb)
+    for (int order = 1; order >= 0; --order)
 #pragma unroll
-        for (int pa = 0; pa < PA; ++pa) {
-            if (pa + pb >= 2) continue;
+        for (int pb = 0; pb < 2; ++pb) {
+            const int pa = order - pb;
+            if (pa < 0 || pa >= PA) continue;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 tc_mma(d, a + pa * 64 + k * 8, desc + ((pb * DK * 256 + k * 256) >> 4), tc_idesc(DK, true), !clear);

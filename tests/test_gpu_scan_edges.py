@@ -459,3 +459,58 @@ def test_nothing_is_written_beside_the_tensors(op, io, H, Hq, dk, dv, lens, tail
         assert (whole[:room] == 0x5A).all() and (whole[room + size:] == 0x5A).all()
     want, S_want = ref.scan(op, desc.scale, lens, t["q"], t["k"], t["v"], t["g"], t["beta"], t["u_bonus"], S0)
     assert err(out[:sum(lens)], want) < TOL[io] + 128 * 2.0 ** -23 and (out[sum(lens):].contiguous().view(torch.uint8) == 0x5A).all()
+
+
+# The tensor cores cut an accumulator's last bits: every addition into a sum loses half a unit 2^-23 of the partial sum on average,
+# always towards zero.  A contraction over 128 channels takes eight additions of the operands' leading planes, whose partial
+# sums are half of the sum on average: two units.  The lower planes' products have to come first, where the sums are still small
+# (behind the leading ones they were forty more additions).  Twice that is allowed, for the sums are made of several contractions.
+MEAN_CUT = 4 * 2.0 ** -23
+
+
+def mean_relative(x, want):
+    want = want.double().cpu()
+    return ((x.double().cpu() - want) / want).mean().item()
+
+
+@pytest.mark.parametrize("op", [ref.LINATTN, ref.RETNET])
+@pytest.mark.parametrize("dk", [64, 128])
+def test_fp32_sums_are_not_cut_on_tcgen05(op, dk):
+    """One chunk of positive numbers, so that nothing averages out: the mean error of states, outputs and their gradients."""
+    H, dv, T = 2, 128, 64
+    gen = torch.Generator().manual_seed(16)
+
+    def rand(*shape):
+        return (0.5 + torch.rand(*shape, generator=gen)).cuda()
+
+    t = dict(q=rand(T, H, dk), k=rand(T, H, dk), v=rand(T, H, dv), g=None if op == ref.LINATTN else -0.01 * rand(T, H), beta=None, u_bonus=None)
+    S0, dS, dout = rand(1, H, dk, dv), rand(1, H, dk, dv), rand(T, H, dv)
+    desc, plan = make_desc(op, H, H, dk, dv, F32, scale=1.0), make_plan([T])
+    want, S_want = ref.scan(op, 1.0, [T], t["q"], t["k"], t["v"], t["g"], None, None, S0)
+    grads = grads_of(op, 1.0, [T], t, S0, dout, dS)
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0)
+    d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, dS_final=dS)
+    got = dict(out=mean_relative(out, want), S=mean_relative(S, S_want), dv=mean_relative(d.v, grads["v"]), dS=mean_relative(d.S_init, grads["S_init"]))
+    assert all(abs(x) < MEAN_CUT for x in got.values()), got
+
+
+@pytest.mark.parametrize("op", [ref.LINATTN, ref.RETNET, ref.GLA])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 64), (128, 128)])
+def test_fp32_sums_are_not_cut(op, dk, dv):
+    """The same for every output and gradient, head size 64 and per-channel gates among them."""
+    H, T = 2, 64
+    gen = torch.Generator().manual_seed(17)
+
+    def rand(*shape):
+        return (0.5 + torch.rand(*shape, generator=gen)).cuda()
+
+    gate = (T, H, dk) if op == ref.GLA else (T, H)
+    t = dict(q=rand(T, H, dk), k=rand(T, H, dk), v=rand(T, H, dv), g=None if op == ref.LINATTN else -0.01 * rand(*gate), beta=None, u_bonus=None)
+    S0, dS, dout = rand(1, H, dk, dv), rand(1, H, dk, dv), rand(T, H, dv)
+    desc, plan = make_desc(op, H, H, dk, dv, F32, scale=1.0), make_plan([T])
+    want, S_want = ref.scan(op, 1.0, [T], t["q"], t["k"], t["v"], t["g"], None, None, S0)
+    grads = grads_of(op, 1.0, [T], t, S0, dout, dS)
+    out, S = dl.scan_forward(desc, plan, **t, S_init=S0)
+    d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, dS_final=dS)
+    got = dict(out=mean_relative(out, want), S=mean_relative(S, S_want)) | {n: mean_relative(getattr(d, n), grads[n]) for n in ("q", "k", "v", "S_init")}
+    assert all(abs(x) < MEAN_CUT for x in got.values()), got
