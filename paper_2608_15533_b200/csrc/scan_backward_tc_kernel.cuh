@@ -4,7 +4,7 @@
 //     dO and dV planes (scalar decay: times their tokens' factors);  dS <- e^(G_end) dS + dO^T (scale q e^G) - dV^T (k e^G).
 // Bound as the forward chain is, and by the 64 KB of dS that every chunk leaves for its gradients.  (Taking dO's products off the
 // chain's path -- its planes up front, dO^T q beside T^T dU -- changed nothing: 939 us and 939 for a step of 8k tokens.)
-// GDN, bf16, 32 heads of 128: 225 us for four rows of 2048 tokens, 955 us for 36.7k tokens of 19 rows; KDA 3.9k tokens of 5 rows 141 us.
+// GDN, bf16, 32 heads of 128: 225 us for four rows of 2048 tokens, 942 us for 36.7k tokens of 19 rows; KDA 3.9k tokens of 5 rows 141 us.
 #pragma once
 
 #include "scan_tc_common.cuh"

@@ -13,7 +13,7 @@
 // Against the mma.sync chain, bf16, 32 heads of 128: 48 ragged prompts of 36k tokens 1328 -> 659 us, one of 16k tokens 1671 -> 1091
 // us, 13k tokens of KDA 747 -> 323 us.  d_v = 64 stays there: half of an MMA's rows would be empty, though by the cycle counts
 // (32 for 128 x 64 x 16 half empty, 64 on mma.sync) its products would still be faster here; no such form has been built.
-// Now: 602 us of the first; the second in three segments, 350 + 16 + 354 us; 292 us of the third.  With kept states, GDN: 186 us for
+// Now: 606 us of the first; the second in three segments, 349 + 17 + 352 us; 288 us of the third.  With kept states, GDN: 186 us for
 // four rows of 2048 tokens, 789 us for 36.7k tokens of 19 rows (3.9 TB/s of DRAM traffic, most of it what is kept).
 #pragma once
 

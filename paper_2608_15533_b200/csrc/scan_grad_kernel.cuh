@@ -21,9 +21,9 @@
 // for per-channel gates.
 // Bound by the phases of a chunk, one behind the other in the only CTA of an SM: 200 KB of operands (5k cycles, from L2), the
 // products over d_v and the sums beside them (9k), the products inside the chunk (10k; per-channel gates 30k).  bf16, 32 heads of 128:
-// GDN 8k tokens 427 us, 36.7k tokens 1946 us (2.8 TB/s of DRAM traffic; 2644 us before the next wave's
+// GDN 8k tokens 427 us, 36.7k tokens 1936 us (2.8 TB/s of DRAM traffic; 2644 us before the next wave's
 // operands went to L2 ahead and the in-chunk part shared its own), KDA 3.9k tokens
-// 455 us; RWKV6, 64 heads of 64, 4k tokens 440 us on mma.sync.  With the products over d_v on mma.sync as well GDN took 1.5 times
+// 441 us; RWKV6, 64 heads of 64, 4k tokens 435 us on mma.sync.  With the products over d_v on mma.sync as well GDN took 1.5 times
 // as long.
 // 512 threads; warp w owns token rows 16 (w & 3) .. + 15 and the channel quarter w >> 2 of every result: the work between
 // two barriers is a few hundred instructions per warp, and sixteen warps cover each other's latencies where eight did not.

@@ -196,7 +196,7 @@ struct PrepScalarSmem {
 };
 
 // Scalar decay: A and L are masked products of whole tiles, scaled entry by entry.  Five CTAs share an SM: the steps of
-// one chunk depend on each other, and only other chunks fill the gaps.  bf16, 32 heads of 128: 36k tokens 333 us, 8k tokens 78 us
+// one chunk depend on each other, and only other chunks fill the gaps.  bf16, 32 heads of 128: 36k tokens 336 us, 8k tokens 79 us
 // (2.8 TB/s of DRAM traffic).
 template <int P, int DK, bool DELTA, typename IO>
 __global__ void __launch_bounds__(128, P == 1 ? 5 : 3) scan_prep_scalar_kernel(const ScanArgs a) {
@@ -403,7 +403,7 @@ __device__ __noinline__ float2 pair_sums(const IO *q, const IO *k, int stride, c
 
 // OP selects the readout (RWKV6) and the delta rule; one thread per block and channel pair, so 256 or 128.
 // Bound by latency at 16 warps per SM (a block's vectors take 96 registers of a thread, the chunk's 104 KB of an SM).
-// bf16: KDA, 32 heads of 128, 13k tokens 525 us (2.2 TB/s of DRAM traffic); RWKV6, 64 heads of 64, 17k tokens 467 us.
+// bf16: KDA, 32 heads of 128, 13k tokens 532 us (2.1 TB/s of DRAM traffic); RWKV6, 64 heads of 64, 17k tokens 468 us.
 template <int OP, int DK, typename IO>
 __global__ void __launch_bounds__(2 * DK, 256 / DK) scan_prep_vector_kernel(const ScanArgs a) {
     constexpr bool DELTA = OpTraits<OP>::kDeltaRule, EXCL = OpTraits<OP>::kBonus;
