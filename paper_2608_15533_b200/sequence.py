@@ -336,7 +336,8 @@ class _Scan(torch.autograd.Function):
 def scan(desc: Desc, plan: Plan, q, k, v, g=None, beta=None, u_bonus=None, S_init=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The differentiable scan: ``(out, S_final)`` of the plan's rows with gradients for every tensor argument; ``out`` rows
     behind the last sequence are zero.  The plan's tables belong to the graph until its backward pass has run: rebuilding
-    the plan in between is an error, and so is capturing a scan while an eager graph of the same leaves lives.  Forward-mode
+    the plan in between is an error (a build that a replayed graph makes changes the tables just the same, but is not
+    noticed), and so is capturing a scan while an eager graph of the same leaves lives.  Forward-mode
     differentiation is refused."""
     _Tokens(desc, plan, q, k, v, g, beta, u_bonus)
     if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in (q, k, v, g, beta, u_bonus, S_init)):

@@ -514,3 +514,67 @@ def test_fp32_sums_are_not_cut(op, dk, dv):
     d = dl.scan_backward(desc, plan, **t, dout=dout, S_init=S0, dS_final=dS)
     got = dict(out=mean_relative(out, want), S=mean_relative(S, S_want)) | {n: mean_relative(getattr(d, n), grads[n]) for n in ("q", "k", "v", "S_init")}
     assert all(abs(x) < MEAN_CUT for x in got.values()), got
+
+
+@pytest.mark.parametrize("op,io,H,Hq,dk,dv", [(ref.GDN, BF16, 4, 2, 128, 128), (ref.KDA, F32, 2, 1, 128, 128), (ref.RWKV6, BF16, 2, 2, 64, 64),
+                                              (ref.GLA, F32, 2, 2, 64, 64), (ref.KDA, BF16, 2, 2, 64, 128)])
+def test_what_no_row_runs_may_hold_anything(op, io, H, Hq, dk, dv):
+    """NaN and infinities in the tokens of padding rows, of a slot outside the pool and behind the last sequence reach nothing: the same
+    bits as with zeros there, forward and backward."""
+    lens, slots, tail = [70, 33, 64, 9, 130], [2, -1, 0, 50, 1], 21
+    t, S0 = ref.inputs(op, lens, H, Hq, dk, dv, io, seed=op + 300, tail=tail)
+    desc = make_desc(op, H, Hq, dk, dv, io, num_slots=4)
+    at = np.cumsum([0] + lens)
+    skipped = torch.zeros(t["v"].shape[0], dtype=torch.bool)
+    skipped[at[1]:at[2]] = skipped[at[3]:at[4]] = skipped[at[5]:] = True
+    behind = torch.zeros_like(skipped)
+    behind[at[5]:] = True
+    gen = torch.Generator().manual_seed(18)
+    dout = torch.randn(t["v"].shape, generator=gen).to(io).cuda()
+
+    def filled(x, rows, value):
+        x = x.clone()
+        x[rows.cuda()] = value
+        return x
+
+    def run(value):
+        def put(rows):
+            return {n: y if y is None or n == "u_bonus" else filled(y, rows, value) for n, y in t.items()}
+
+        state = pool(desc, 1)
+        served = dl.prefill(desc, state, make_plan(lens, slots, tail=tail), **put(skipped))
+        plan = make_plan(lens, tail=tail)
+        ws = dl.scan_workspace(desc, len(lens), plan.max_tokens, train=True)
+        out, S = dl.scan_forward(desc, plan, **put(behind), S_init=S0, workspace=ws, save=True)
+        d = dl.scan_backward(desc, plan, **put(behind), dout=filled(dout, behind, value), S_init=S0, workspace=ws, saved=True)
+        return [served, state.S_base, out, S, *(x for x in (d.q, d.k, d.v, d.g, d.beta, d.u_bonus, d.S_init) if x is not None)]
+
+    clean = run(0.0)
+    assert all(torch.isfinite(x).all() for x in clean)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        for x, y in zip(clean, run(value)):
+            assert torch.equal(x, y)
+
+
+def test_two_scans_at_once():
+    """One plan, two streams, a workspace each: both give what they give alone."""
+    op, H, d, lens = ref.GDN, 8, 128, [900, 64, 3, 400]
+    desc, plan = make_desc(op, H, H, d, d, BF16), make_plan(lens)
+    sets = [ref.inputs(op, lens, H, H, d, d, BF16, seed=310 + i) for i in range(2)]
+    spaces = [dl.scan_workspace(desc, len(lens), plan.max_tokens, train=True) for _ in sets]
+
+    def run(i, stream=None):
+        t, S0 = sets[i]
+        out, S = dl.scan_forward(desc, plan, **t, S_init=S0, workspace=spaces[i], save=True, stream=stream)
+        g = dl.scan_backward(desc, plan, **t, dout=t["v"], S_init=S0, workspace=spaces[i], saved=True, stream=stream)
+        return out, S, g.q, g.k, g.v, g.g, g.beta, g.S_init
+
+    alone = [run(0), run(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        both = [run(i, streams[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        for got, want in zip(both, alone):
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert plan.status.item() == 0
