@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) scan_forward_tc_kernel(const Sc
 // The states in front of a split row's segments: X_1 is the first segment's end, X_(s+1) = M_s X_s + E_s in E_s' place.
 // Sixteen columns per CTA, one row of M per thread; the next M is on its way while one is multiplied.  In fp32 throughout.
 // Bound by latency: a join is d_k dependent steps of loads from shared memory behind a copy of M, 5 us or so for each, one behind the
-// other (16k tokens of GDN: 1 head, 29 joins 148 us of 242; 8 heads, 7 joins 43 us of 312; 32 heads, one join 16.4 us of 896, where
+// other (16k tokens of GDN: 1 head, 30 joins 148 us of 242; 8 heads, 8 joins 43 us of 313; 32 heads, one join 16.4 us of 896, where
 // 256 CTAs of 148 KB also take two waves).
 constexpr int kJoinCols = 16;
 template <int DK>
