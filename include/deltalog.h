@@ -73,7 +73,8 @@ enum {
 enum {
     DELTALOG_STATUS_LOG_FULL = 1, /* decode on a (slot, head) whose log already holds cap entries: row skipped */
     DELTALOG_STATUS_BAD_SLOT = 2, /* slot index >= num_slots: row skipped */
-    DELTALOG_STATUS_TIMEOUT = 4   /* a bounded wait inside a kernel gave up: results of that launch are invalid */
+    DELTALOG_STATUS_TIMEOUT = 4,  /* a bounded wait inside a kernel gave up: results of that launch are invalid */
+    DELTALOG_STATUS_BAD_POSITION = 8 /* a token's position lies behind the rotation's tables: its outputs are zero */
 };
 
 /* Problem description (host memory). */
@@ -397,6 +398,157 @@ typedef struct {
 int deltalog_scan_backward(const deltalog_desc *desc, const deltalog_plan *plan, const float *S_init, const void *q, const void *k, const void *v,
                            const float *g, const float *beta, const float *u_bonus, const void *dout, const float *dS_final, int32_t saved,
                            const deltalog_scan_grads *grads, int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ---- Around the scan -------------------------------------------------------------------------------------
+ * What a recurrent layer runs in front of its scan or its decode step, and the selective state space scan that takes its
+ * place in other layers.  Packed sequences come with a plan (the calls read starts, token_seq and, for prefill, scan_slots),
+ * single tokens with a slot list, as above.  `x_stride` and its like are elements from one token to the next: a token's own
+ * values are dense, the tokens may be columns of a wider tensor.  Addresses and strides are multiples of 16 bytes where
+ * nothing else is said.  Sums, statistics and states are fp32; 16-bit outputs and gradients are rounded once.  Every call
+ * gives the same bits for the same arguments.
+ */
+
+/*
+ * Short causal convolution of every channel for itself, with the last width - 1 inputs of a sequence as its state:
+ *     pre[t, c] = bias[c] + sum_j weight[c, j] * x[t - (width - 1) + j, c],   out = pre, or pre * sigmoid(pre) with silu
+ * In front of a row's first token stand the inputs that its window holds, oldest first.
+ *   x [tokens, channels] io_dtype, token stride x_stride; weight [channels, width] fp32; bias [channels] fp32 or NULL;
+ *   window [num_slots, width - 1, channels] io_dtype; out [tokens, channels] io_dtype
+ */
+typedef struct {
+    int32_t channels;  /* a multiple of 8 */
+    int32_t width;     /* 2..4 */
+    int32_t io_dtype;  /* deltalog_dtype */
+    int32_t silu;
+    int32_t num_slots; /* windows in the pool (step and prefill) */
+    int32_t hints;     /* DELTALOG_HINT_ZERO_UNWRITTEN, as for deltalog_prefill */
+} deltalog_conv_desc;
+
+/* One token for each of B rows: row b reads and advances window slot_idx[b] (b without a list).  Rows with a negative slot
+ * are padding: their rows of `out` stay as they were.  Slots outside the pool: the same, and DELTALOG_STATUS_BAD_SLOT in
+ * *status (may be NULL). */
+int deltalog_conv_step(const deltalog_conv_desc *desc, void *window, const void *x, int64_t x_stride, const float *weight, const float *bias,
+                       const int32_t *slot_idx, int32_t B, void *out, int32_t *status, void *stream);
+
+/* The rows of plan->scan_slots; rows with fresh[i] != 0 (fresh: [n] or NULL) start from zeros.  Rows of `out` and of the pool
+ * that no listed row owns stay as they were (unless the hint asks for zeros in `out`). */
+int deltalog_conv_prefill(const deltalog_conv_desc *desc, void *window, const deltalog_plan *plan, const void *x, int64_t x_stride, const float *weight,
+                          const float *bias, const int32_t *fresh, void *out, int32_t *status, void *stream);
+
+/* For training: row i starts from init[i] ([n, width - 1, channels] io_dtype, or NULL: zeros) and leaves its last inputs in
+ * final[i] (or NULL).  init and final do not overlap.  Slots play no part. */
+int deltalog_conv_forward(const deltalog_conv_desc *desc, const deltalog_plan *plan, const void *init, const void *x, int64_t x_stride,
+                          const float *weight, const float *bias, void *out, void *final, void *stream);
+
+typedef struct {
+    void *x;       /* [rows, channels], rows behind the last sequence are set to zero */
+    float *weight; /* [channels, width] */
+    float *bias;   /* [channels], or NULL */
+    void *init;    /* [n, width - 1, channels], or NULL */
+} deltalog_conv_grads;
+
+size_t deltalog_conv_workspace_bytes(const deltalog_conv_desc *desc, int32_t rows); /* of the backward pass over `rows` tokens; 0: invalid */
+
+/* Gradients for dout [rows, channels] and dfinal (or NULL: zeros); `rows` >= plan->max_tokens as in deltalog_scan_backward. */
+int deltalog_conv_backward(const deltalog_conv_desc *desc, const deltalog_plan *plan, const void *init, const void *x, int64_t x_stride,
+                           const float *weight, const float *bias, const void *dout, const void *dfinal, const deltalog_conv_grads *grads,
+                           int32_t rows, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norm of query and key heads, their rotation by position and the scale of the queries, both tensors in one pass:
+ *     y = q_scale * R(position) (w * x / norm(x))     (keys: without q_scale)
+ *   norm: DELTALOG_NORM_L2   sqrt(sum x^2 + eps), no weights: the unit vectors that the delta rule's calls expect
+ *         DELTALOG_NORM_RMS  sqrt(mean x^2 + eps), w_q, w_k [d] fp32 or both NULL: ones
+ *         DELTALOG_NORM_NONE the rotation and the scale alone
+ *   rot   leading values of a head that are rotated: 0 (cos, sin and positions are not read) or a multiple of 16 up to d.
+ *         Pair i is (x[i], x[i + rot / 2]), or (x[2 i], x[2 i + 1]) with `interleaved`; it turns by the angle whose cosine and
+ *         sine are cos[p, i], sin[p, i] ([table_rows, rot / 2] fp32, so angles of far positions are as good as the caller's).
+ *   q [tokens, H_q, d], k [tokens, H_k, d] io_dtype, token strides q_stride, k_stride (the heads of a token are dense);
+ *   positions [tokens] int32; out_q, out_k dense.  H_k = 0: q alone, k is not read.  In place (out_q == q) is allowed where
+ *   the strides agree.
+ * A negative position marks a padding token: its outputs and gradients are zero.  Positions >= table_rows: the same, and
+ * DELTALOG_STATUS_BAD_POSITION in *status (may be NULL).
+ */
+typedef enum { DELTALOG_NORM_L2 = 0, DELTALOG_NORM_RMS = 1, DELTALOG_NORM_NONE = 2 } deltalog_norm;
+typedef struct {
+    int32_t H_q, H_k;
+    int32_t d;         /* a multiple of 8 up to 256 */
+    int32_t io_dtype;  /* deltalog_dtype */
+    int32_t norm;      /* deltalog_norm */
+    int32_t rot;
+    int32_t interleaved;
+    int32_t table_rows;
+    float eps;         /* >= 0 */
+    float q_scale;
+} deltalog_norm_desc;
+
+int deltalog_head_norm_forward(const deltalog_norm_desc *desc, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const float *w_q,
+                               const float *w_k, const float *cos, const float *sin, const int32_t *positions, int32_t tokens, void *out_q,
+                               void *out_k, int32_t *status, void *stream);
+
+/* Bytes of workspace for the backward pass (0 without weights). */
+size_t deltalog_head_norm_workspace_bytes(const deltalog_norm_desc *desc, int32_t tokens);
+
+/* Gradients of q, k [tokens, H, d] and of w_q, w_k [d] fp32 (NULL without weights) for dout_q, dout_k (dense). */
+int deltalog_head_norm_backward(const deltalog_norm_desc *desc, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const float *w_q,
+                                const float *w_k, const float *cos, const float *sin, const int32_t *positions, int32_t tokens,
+                                const void *dout_q, const void *dout_k, void *dq, void *dk, float *dw_q, float *dw_k, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
+ * The selective state space scan: a diagonal state of d_state values per channel, its decay and its input scaled by a step size
+ * that every token brings,
+ *     delta = softplus(dt + dt_bias), or dt + dt_bias        (per token and channel)
+ *     S <- exp(delta A) S + delta x B                         (S, A [channels, d_state]; B, C [tokens, groups, d_state])
+ *     y = S C + D x,   out = y, or y z sigmoid(z)
+ * Channel c belongs to group c / (channels / groups).
+ *   x, dt, z, out [tokens, channels] io_dtype; B, C [tokens, groups, d_state] io_dtype, the groups of a token dense; A fp32 (negative in
+ *   use: a decay); D, dt_bias [channels] fp32 or NULL; z may be NULL; states fp32 [num_slots or n, channels, d_state].
+ */
+typedef struct {
+    int32_t channels;  /* channels / groups a multiple of 8 */
+    int32_t d_state;   /* 8, 16, 32 or 64 */
+    int32_t groups;
+    int32_t io_dtype;  /* deltalog_dtype */
+    int32_t softplus;
+    int32_t num_slots; /* states in the pool (step and prefill) */
+    int32_t hints;     /* DELTALOG_HINT_ZERO_UNWRITTEN, as for deltalog_prefill */
+} deltalog_ssm_desc;
+
+typedef struct {
+    const void *x, *dt, *B, *C, *z;
+    int64_t x_stride, dt_stride, B_stride, C_stride, z_stride; /* elements from token to token */
+    const float *A, *D, *dt_bias;
+} deltalog_ssm_inputs;
+
+/* One token for each of B rows, as in deltalog_conv_step. */
+int deltalog_ssm_step(const deltalog_ssm_desc *desc, float *S, const deltalog_ssm_inputs *in, const int32_t *slot_idx, int32_t B, void *out,
+                      int32_t *status, void *stream);
+
+/* Bytes of workspace for max_tokens tokens or fewer: train == 0 for prefill and forward without save, train != 0 for save and
+ * the backward pass, where max_tokens is the rows of the token tensors.  0: invalid. */
+size_t deltalog_ssm_workspace_bytes(const deltalog_ssm_desc *desc, int32_t n, int32_t max_tokens, int32_t train);
+
+/* The rows of plan->scan_slots, as in deltalog_conv_prefill. */
+int deltalog_ssm_prefill(const deltalog_ssm_desc *desc, float *S, const deltalog_plan *plan, const deltalog_ssm_inputs *in, const int32_t *fresh,
+                         void *out, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* For training: row i starts from S_init[i] (or NULL: zeros) and leaves S_final[i] (or NULL).  With save != 0 the workspace
+ * keeps the states in front of every eighth token for deltalog_ssm_backward. */
+int deltalog_ssm_forward(const deltalog_ssm_desc *desc, const deltalog_plan *plan, const float *S_init, const deltalog_ssm_inputs *in, void *out,
+                         float *S_final, int32_t save, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients, dense, typed like what they belong to; z, D, dt_bias where there is such an input; S_init may be NULL. */
+typedef struct {
+    void *x, *dt, *B, *C, *z;
+    float *A, *D, *dt_bias, *S_init;
+} deltalog_ssm_grads;
+
+/* Gradients for dout [rows, channels] (dense) and dS_final (or NULL: zeros); saved and rows as in deltalog_scan_backward. */
+int deltalog_ssm_backward(const deltalog_ssm_desc *desc, const deltalog_plan *plan, const float *S_init, const deltalog_ssm_inputs *in,
+                          const void *dout, const float *dS_final, int32_t saved, const deltalog_ssm_grads *grads, int32_t rows, void *workspace,
+                          size_t workspace_bytes, void *stream);
 
 /* Human-readable text for a host return code (static storage). */
 const char *deltalog_status_string(int code);

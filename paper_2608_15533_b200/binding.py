@@ -19,7 +19,7 @@ HINT_BASE_UNTOUCHED, HINT_SLOTS_STABLE, HINT_WALK_DOWN, HINT_ZERO_UNWRITTEN = 1,
 _DELTA_RULE = (GDN, KDA)            # b = beta (v - S'^T k): U log in fp32
 _VEC_DECAY = (KDA, RWKV6, GLA)      # one log-decay per key channel
 F32, BF16 = 0, 1
-STATUS_LOG_FULL, STATUS_BAD_SLOT, STATUS_TIMEOUT = 1, 2, 4
+STATUS_LOG_FULL, STATUS_BAD_SLOT, STATUS_TIMEOUT, STATUS_BAD_POSITION = 1, 2, 4, 8
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED_SHAPE, ERR_CAP_RANGE, ERR_CUDA, ERR_STATIC_LIMIT = 0, 1, 2, 3, 4, 5
 STATIC_STAGING_BYTES = 8 << 20
 
@@ -32,6 +32,9 @@ EXPORTS = (
     "deltalog_decode_step", "deltalog_decode_steps", "deltalog_decode_merge_step", "deltalog_merge", "deltalog_reset_slots", "deltalog_eager_step", "deltalog_decode_step_host",
     "deltalog_decode_step_host_static", "deltalog_decode_step_host_overlapped",
     "deltalog_build_plan", "deltalog_scan_workspace_bytes", "deltalog_prefill", "deltalog_scan_forward", "deltalog_scan_backward",
+    "deltalog_conv_step", "deltalog_conv_prefill", "deltalog_conv_forward", "deltalog_conv_workspace_bytes", "deltalog_conv_backward",
+    "deltalog_ssm_step", "deltalog_ssm_workspace_bytes", "deltalog_ssm_prefill", "deltalog_ssm_forward", "deltalog_ssm_backward",
+    "deltalog_head_norm_forward", "deltalog_head_norm_workspace_bytes", "deltalog_head_norm_backward",
     "deltalog_status_string", "deltalog_version", "deltalog_build_id", "deltalog_launch_count",
 )
 
@@ -68,6 +71,33 @@ class _Plan(ctypes.Structure):
 
 class _ScanGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "g", "beta", "u_bonus", "S_init")]
+
+
+class _ConvDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("channels", "width", "io_dtype", "silu", "num_slots", "hints")]
+
+
+class _ConvGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "weight", "bias", "init")]
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("H_q", "H_k", "d", "io_dtype", "norm", "rot", "interleaved", "table_rows")] + \
+               [(n, ctypes.c_float) for n in ("eps", "q_scale")]
+
+
+class _SsmDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("channels", "d_state", "groups", "io_dtype", "softplus", "num_slots", "hints")]
+
+
+class _SsmInputs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "B", "C", "z")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "dt_stride", "B_stride", "C_stride", "z_stride")] + \
+               [(n, ctypes.c_void_p) for n in ("A", "D", "dt_bias")]
+
+
+class _SsmGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "B", "C", "z", "A", "D", "dt_bias", "S_init")]
 
 
 _lib = None
@@ -114,6 +144,25 @@ def load_library() -> ctypes.CDLL:
         lib.deltalog_scan_forward.argtypes = [dp, pp] + [vp] * 9 + [i32, vp, ctypes.c_size_t, vp]
         lib.deltalog_scan_backward.restype = ctypes.c_int
         lib.deltalog_scan_backward.argtypes = [dp, pp] + [vp] * 9 + [i32, ctypes.POINTER(_ScanGrads), i32, vp, ctypes.c_size_t, vp]
+        i64, size = ctypes.c_int64, ctypes.c_size_t
+        cp, sp, np_, ip = (ctypes.POINTER(t) for t in (_ConvDesc, _SsmDesc, _NormDesc, _SsmInputs))
+        head = [np_, vp, i64, vp, i64] + [vp] * 5 + [i32]
+        for name, args, res in (
+                ("conv_step", [cp, vp, vp, i64] + [vp] * 3 + [i32] + [vp] * 3, ctypes.c_int),
+                ("conv_prefill", [cp, vp, pp, vp, i64] + [vp] * 6, ctypes.c_int),
+                ("conv_forward", [cp, pp, vp, vp, i64] + [vp] * 5, ctypes.c_int),
+                ("conv_workspace_bytes", [cp, i32], size),
+                ("conv_backward", [cp, pp, vp, vp, i64] + [vp] * 4 + [ctypes.POINTER(_ConvGrads), i32, vp, size, vp], ctypes.c_int),
+                ("ssm_step", [sp, vp, ip, vp, i32] + [vp] * 3, ctypes.c_int),
+                ("ssm_workspace_bytes", [sp, i32, i32, i32], size),
+                ("ssm_prefill", [sp, vp, pp, ip] + [vp] * 4 + [size, vp], ctypes.c_int),
+                ("ssm_forward", [sp, pp, vp, ip, vp, vp, i32, vp, size, vp], ctypes.c_int),
+                ("ssm_backward", [sp, pp, vp, ip, vp, vp, i32, ctypes.POINTER(_SsmGrads), i32, vp, size, vp], ctypes.c_int),
+                ("head_norm_forward", head + [vp] * 4, ctypes.c_int),
+                ("head_norm_workspace_bytes", [np_, i32], size),
+                ("head_norm_backward", head + [vp] * 7 + [size, vp], ctypes.c_int)):
+            entry = getattr(lib, "deltalog_" + name)
+            entry.argtypes, entry.restype = args, res
         lib.deltalog_status_string.restype = ctypes.c_char_p
         lib.deltalog_status_string.argtypes = [ctypes.c_int]
         lib.deltalog_version.restype = ctypes.c_int

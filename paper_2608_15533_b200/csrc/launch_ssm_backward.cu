@@ -1,0 +1,40 @@
+// Launches of the state space scan's backward pass.
+#include "ssm_backward_kernel.cuh"
+#include "ssm_launch.cuh"
+
+namespace deltalog {
+
+namespace {
+
+template <typename IO, int N>
+int backward(const SsmArgs &a, cudaStream_t s) {
+    const size_t smem = sizeof(typename SsmBackward<IO, N>::Shared);
+    const unsigned cols = (unsigned)(a.G * a.blocks);
+    if (a.spans > 1) {
+        auto local = ssm_backward_kernel<IO, N, true>;
+        if (int rc = ensure_smem(local, smem)) return rc;
+        local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
+        if (int rc = finish_launch()) return rc;
+    }
+    const unsigned rest = a.dS_init ? 1 : 0;
+    if (a.spans + rest > 0) {
+        auto kernel = ssm_backward_kernel<IO, N, false>;
+        if (int rc = ensure_smem(kernel, smem)) return rc;
+        kernel<<<dim3(cols, (unsigned)a.spans + rest), kSsmThreads, smem, s>>>(a);
+        if (int rc = finish_launch()) return rc;
+    }
+    const long long token_blocks = ssm_ceil((long long)a.total_rows * a.G * (2 * N / 4), 256), param_blocks = ssm_ceil((long long)a.D_ * (N + 2), 256);
+    if (token_blocks + param_blocks > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
+    ssm_sums_kernel<IO, N><<<(unsigned)(token_blocks + param_blocks), 256, 0, s>>>(a, token_blocks);
+    return finish_launch();
+}
+
+}  // namespace
+
+int launch_ssm_backward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s) {
+#define CALL(IO, N) return backward<IO, N>(a, s)
+    SSM_DISPATCH(d, CALL);
+#undef CALL
+}
+
+}  // namespace deltalog

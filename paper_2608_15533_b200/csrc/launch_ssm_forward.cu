@@ -1,0 +1,54 @@
+// Launches of the state space scan's forward pass and of its single-token form.
+#include "ssm_forward_kernel.cuh"
+#include "ssm_launch.cuh"
+
+namespace deltalog {
+
+namespace {
+
+template <typename IO, int N>
+int forward(const SsmArgs &a, cudaStream_t s) {
+    const size_t smem = sizeof(typename SsmForward<IO, N>::Shared);
+    const unsigned cols = (unsigned)(a.G * a.blocks);
+    if (a.spans > 1) {
+        auto local = ssm_forward_kernel<IO, N, true>;
+        if (int rc = ensure_smem(local, smem)) return rc;
+        local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
+        if (int rc = finish_launch()) return rc;
+    }
+    auto kernel = ssm_forward_kernel<IO, N, false>;
+    if (int rc = ensure_smem(kernel, smem)) return rc;
+    // one more row of CTAs for the rows without tokens, whose states a training call hands on
+    const unsigned rest = a.S_out && !a.slots ? 1 : 0;
+    if (a.spans + rest == 0) return DELTALOG_OK;
+    kernel<<<dim3(cols, (unsigned)a.spans + rest), kSsmThreads, smem, s>>>(a);
+    return finish_launch();
+}
+
+template <typename IO, int N>
+int step(const SsmArgs &a, cudaStream_t s) {
+    const int cols = (int)ssm_ceil(a.D_, kSsmWarps * SsmLanes<N>::kChannels);
+    // four rows per CTA, which are in flight together; more once there are enough CTAs for all SMs
+    const long long per = (long long)cols * a.total_rows / (16ll * device_info().sms);
+    const int run = per <= 4 ? 4 : per >= 16 ? 16 : (int)per / 4 * 4;
+    const long long grid = ssm_ceil(a.total_rows, run) * cols;
+    if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
+    ssm_step_kernel<IO, N><<<(unsigned)grid, kSsmThreads, 0, s>>>(a, cols, run);
+    return finish_launch();
+}
+
+}  // namespace
+
+int launch_ssm_forward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s) {
+#define CALL(IO, N) return forward<IO, N>(a, s)
+    SSM_DISPATCH(d, CALL);
+#undef CALL
+}
+
+int launch_ssm_step(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s) {
+#define CALL(IO, N) return step<IO, N>(a, s)
+    SSM_DISPATCH(d, CALL);
+#undef CALL
+}
+
+}  // namespace deltalog

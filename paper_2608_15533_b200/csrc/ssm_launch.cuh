@@ -1,0 +1,80 @@
+// Host-side pieces of the state space scan's entry points: how the tokens are cut, which tensors live where in the workspace,
+// and the launch functions of its kernels (one translation unit per direction).
+#pragma once
+
+#include "launch_common.cuh"
+#include "ssm_common.cuh"
+
+namespace deltalog {
+
+inline long long ssm_ceil(long long a, long long b) { return (a + b - 1) / b; }
+
+constexpr int kSsmSpanMin = 256;  // tokens of a stretch at least
+
+// Channels of a CTA: forward, backward.
+inline int ssm_cols(const deltalog_ssm_desc *d, bool backward) {
+    if (!backward) return d->d_state == 8 ? 64 : 32;
+    return d->d_state == 8 ? 128 : d->d_state == 16 ? 64 : d->d_state == 32 ? 32 : 16;
+}
+inline int ssm_blocks(const deltalog_ssm_desc *d, bool backward) { return (int)ssm_ceil(d->channels / d->groups, ssm_cols(d, backward)); }
+
+// Stretches that the tokens are cut into at most, for CTAs of `want` in all: a cut makes the row that crosses it run twice
+// behind its last border, so there are no more than fill the SMs.  (148 SMs whatever the device: workspaces depend on it.)
+inline int ssm_most_spans(const deltalog_ssm_desc *d, bool backward) {
+    const long long blocks = (long long)ssm_blocks(d, backward) * d->groups, want = backward ? 148 * 3 : 148 * 6;
+    return (int)(blocks >= want ? 1 : ssm_ceil(want, blocks));
+}
+struct SsmCut { int span, spans; };
+inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {
+    SsmCut c;
+    const long long most = ssm_most_spans(d, backward);
+    const long long span = ssm_ceil(ssm_ceil(tokens, most), 32) * 32;
+    c.span = (int)(span < kSsmSpanMin ? kSsmSpanMin : span);
+    c.spans = (int)ssm_ceil(tokens, c.span);
+    return c;
+}
+// What ssm_cut gives at most for this many tokens or fewer.
+inline int ssm_room(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {
+    const long long most = ssm_most_spans(d, backward), spans = ssm_ceil(tokens, kSsmSpanMin);
+    return (int)(spans < most ? spans : most);
+}
+
+// Byte offsets into the caller's workspace.
+struct SsmLayout {
+    size_t kept, local, front, sums, part_bc, part_A, part_cols, total;
+};
+inline SsmLayout ssm_layout(const deltalog_ssm_desc *d, int32_t tokens, bool train) {
+    const size_t D = d->channels, N = d->d_state;
+    size_t at = 0;
+    auto take = [&](bool wanted, size_t bytes) {
+        const size_t off = at;
+        if (wanted) at += (bytes + 255) / 256 * 256;
+        return off;
+    };
+    SsmLayout l;
+    const int f = ssm_room(d, tokens, false), b = train ? ssm_room(d, tokens, true) : 0, joined = f > b ? f : b;
+    l.kept = take(train, (size_t)ssm_ceil(tokens, kSsmBlock) * D * N * 4);
+    l.local = take(joined > 1, (size_t)joined * D * N * 4);
+    l.front = take(f > 1 && !train, (size_t)f * D * N * 4);
+    l.sums = take(joined > 1, (size_t)joined * D * 4);
+    l.part_bc = take(train, (size_t)d->groups * ssm_blocks(d, true) * tokens * 2 * N * 4);
+    l.part_A = take(train, (size_t)b * D * N * 4);
+    l.part_cols = take(train, (size_t)b * 2 * D * 4);
+    l.total = at ? at : 256;
+    return l;
+}
+
+// FN<io type, states>
+#define SSM_DISPATCH(desc_, CALL)                                                                        \
+    do {                                                                                                 \
+        if ((desc_)->io_dtype == DELTALOG_F32) { SSM_STATES(float, (desc_)->d_state, CALL); }            \
+        else { SSM_STATES(__nv_bfloat16, (desc_)->d_state, CALL); }                                      \
+    } while (0)
+#define SSM_STATES(IO, n_, CALL)                                                                         \
+    if ((n_) == 8) { CALL(IO, 8); } else if ((n_) == 16) { CALL(IO, 16); } else if ((n_) == 32) { CALL(IO, 32); } else { CALL(IO, 64); }
+
+int launch_ssm_forward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s);   // both passes
+int launch_ssm_step(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s);
+int launch_ssm_backward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s);  // both passes and the sums
+
+}  // namespace deltalog
