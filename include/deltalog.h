@@ -518,11 +518,11 @@ typedef struct {
 
 typedef struct {
     const void *x, *dt, *B, *C, *z;
-    int64_t x_stride, dt_stride, B_stride, C_stride, z_stride; /* elements from token to token */
+    int64_t x_stride, dt_stride, B_stride, C_stride, z_stride; /* elements from token to token, 2^25 at most */
     const float *A, *D, *dt_bias;
 } deltalog_ssm_inputs;
 
-/* One token for each of B rows, as in deltalog_conv_step. */
+/* One token for each of B rows, as in deltalog_conv_step.  S and A on 32-byte boundaries. */
 int deltalog_ssm_step(const deltalog_ssm_desc *desc, float *S, const deltalog_ssm_inputs *in, const int32_t *slot_idx, int32_t B, void *out,
                       int32_t *status, void *stream);
 

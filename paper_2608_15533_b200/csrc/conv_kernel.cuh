@@ -29,7 +29,7 @@ struct ConvArgs {
     float *partial;
 };
 
-constexpr int kConvThreads = 128;
+constexpr int kConvThreads = 128, kConvVec = 4;  // channels per lane: eight would need up to 200 registers
 
 // Window of a row: slot or row, -1 for a row that the call skips.
 __device__ __forceinline__ int conv_slot(const ConvArgs &a, int row, bool tell) {
@@ -57,7 +57,21 @@ __device__ __forceinline__ void conv_weights(const ConvArgs &a, int c, float (&w
     }
 }
 
-// pre-activations from the window `p` (p[0] the oldest input)
+// pre-activations from the window `p` (p[0] the oldest input): as it is in memory, or widened
+template <int W, int V>
+__device__ __forceinline__ void conv_pre(const float (&p)[W][V], const float (&w)[W][V], const float (&b)[V], float (&pre)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        pre[v] = b[v];
+#pragma unroll
+        for (int j = 0; j < W; ++j) pre[v] = fmaf(w[j][v], p[j][v], pre[v]);
+    }
+}
+template <typename IO, int V>
+__device__ __forceinline__ void conv_floats(const Pack<IO, V> &v, float (&f)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
+}
 template <typename IO, int W, int V>
 __device__ __forceinline__ void conv_pre(const Pack<IO, V> (&p)[W], const float (&w)[W][V], const float (&b)[V], float (&pre)[V]) {
 #pragma unroll
@@ -78,8 +92,8 @@ __device__ __forceinline__ Pack<IO, V> conv_act(float (&pre)[V], bool silu) {
 // ---- forward over packed rows ------------------------------------------------------------------------------------
 // Blocks [0, head_blocks): the rows' first tokens and windows.  The others: runs of tokens.
 template <typename IO, int W>
-__global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
-    constexpr int V = 16 / sizeof(IO), U = 8;
+__global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
+    constexpr int V = kConvVec, U = 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
     const bool live = c < a.C;  // C is a multiple of 8
@@ -145,69 +159,97 @@ __global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvAr
         end = r >= 0 ? a.rows.starts[r + 1] : a.max_tokens;
     };
     enter(row);
+    float f[W][V];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int t = t0 - (W - 1) + j;
-        p[j] = t >= 0 ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : pack_zero<IO, V>();
+        conv_floats(t >= 0 ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : pack_zero<IO, V>(), f[j]);
     }
     Pack<IO, V> in[U];
+    auto fetch = [&](int t) {
+        if (t + U <= t1) {
+            const IO *from = x + (size_t)t * a.x_stride;
 #pragma unroll
-    for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(x + (size_t)min(t0 + u, t1 - 1) * a.x_stride);
+            for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(from + u * a.x_stride);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(x + (size_t)min(t + u, t1 - 1) * a.x_stride);
+        }
+    };
+    fetch(t0);
     for (int t = t0; t < t1; t += U) {
         Pack<IO, V> cur[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) cur[u] = in[u];
-        if (t + U < t1) {
+        if (t + U < t1) fetch(t + U);
+        IO *to = out + (size_t)t * a.C;
+        auto token = [&](int u) {
+            conv_floats(cur[u], f[W - 1]);
+            float pre[V];
+            conv_pre<W, V>(f, w, b, pre);
 #pragma unroll
-            for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(x + (size_t)min(t + U + u, t1 - 1) * a.x_stride);
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) f[j][v] = f[j + 1][v];
+            return conv_act<IO, V>(pre, a.silu);
+        };
+        if (mine && t - begin >= W - 1 && t + U <= min(t1, end)) {  // one row, none of its first tokens
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Pack<IO, V> o = token(u);
+                if (live) pack_store(to + u * a.C, o);
+            }
+            continue;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int at = t + u;
-            if (at < t1) {
-                if (at >= end) enter(a.rows.of(at));
-                p[W - 1] = cur[u];
-                float pre[V];
-                conv_pre<IO, W, V>(p, w, b, pre);
-                const Pack<IO, V> o = conv_act<IO, V>(pre, a.silu);
-                if (mine) {
-                    if (live && at - begin >= W - 1) pack_store(out + (size_t)at * a.C, o);
-                } else if (a.clear && live) {
-                    pack_store(out + (size_t)at * a.C, pack_zero<IO, V>());
-                }
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j) p[j] = p[j + 1];
+            if (at >= t1) break;
+            if (at >= end) enter(a.rows.of(at));
+            const Pack<IO, V> o = token(u);
+            if (mine) {
+                if (live && at - begin >= W - 1) pack_store(to + u * a.C, o);
+            } else if (a.clear && live) {
+                pack_store(to + u * a.C, pack_zero<IO, V>());
             }
         }
     }
 }
 
 // ---- single tokens ------------------------------------------------------------------------------------------------
-// A thread takes the same vector of channels of `run` rows, with the weights in registers.
+// A lane takes the same channels of `run` rows, with the weights in registers and four rows in flight.
 template <typename IO, int W>
 __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs a, int col_blocks) {
-    constexpr int V = 16 / sizeof(IO);
+    constexpr int V = kConvVec, U = 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
-    if (c >= a.C) return;
-    const int first = ((int)(blockIdx.x / col_blocks) * (kConvThreads / 32) + warp) * a.run;
-    if (first >= a.total_rows) return;
+    const long long first = ((long long)(blockIdx.x / col_blocks) * (kConvThreads / 32) + warp) * a.run;
+    if (c >= a.C || first >= a.total_rows) return;
+    const int end = (int)min((long long)a.total_rows, first + a.run);
     float w[W][V], b[V];
-    conv_weights<W, V>(a, c, w, b);
-    const int end = min(a.total_rows, first + a.run);
-    for (int row = first; row < end; ++row) {
-        int slot;
-        if (!resolve_slot(a.slots, row, a.num_slots, a.status, lane, slot)) continue;
-        IO *win = static_cast<IO *>(a.final) + (size_t)slot * (W - 1) * a.C + c;
-        Pack<IO, V> p[W];
+    for (int row = (int)first; row < end; row += U) {
+        int slot[U];
+        Pack<IO, V> p[U][W];
+        step_slots(a.slots, row, end, a.num_slots, a.status, slot);
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) p[j] = pack_load<IO, V>(win + (size_t)j * a.C);
-        p[W - 1] = pack_load<IO, V>(static_cast<const IO *>(a.x) + (size_t)row * a.x_stride + c);
-        float pre[V];
-        conv_pre<IO, W, V>(p, w, b, pre);
-        pack_store(static_cast<IO *>(a.out) + (size_t)row * a.C + c, conv_act<IO, V>(pre, a.silu));
+        for (int u = 0; u < U; ++u) {
+            if (slot[u] < 0) continue;
+            const IO *win = static_cast<const IO *>(a.init) + (size_t)slot[u] * (W - 1) * a.C + c;
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) pack_store(win + (size_t)j * a.C, p[j + 1]);
+            for (int j = 0; j < W - 1; ++j) p[u][j] = pack_load<IO, V>(win + (size_t)j * a.C);
+            p[u][W - 1] = pack_load<IO, V>(static_cast<const IO *>(a.x) + (size_t)(row + u) * a.x_stride + c);
+        }
+        if (row == (int)first) conv_weights<W, V>(a, c, w, b);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (slot[u] < 0) continue;
+            IO *win = static_cast<IO *>(a.final) + (size_t)slot[u] * (W - 1) * a.C + c;
+            float pre[V];
+            conv_pre<IO, W, V>(p[u], w, b, pre);
+            pack_store(static_cast<IO *>(a.out) + (size_t)(row + u) * a.C + c, conv_act<IO, V>(pre, a.silu));
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) pack_store(win + (size_t)j * a.C, p[u][j + 1]);
+        }
     }
 }
 
@@ -216,7 +258,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs 
 // row holds t);  dw[j] = sum_t dpre[t] x[t - (W - 1) + j];  dbias = sum_t dpre[t].
 // The walk goes W - 1 tokens beyond its run, since dx[t] is complete with dpre[t + W - 1]; dx of the last W tokens waits in
 // registers.  dw and dbias: a thread's sums over its run, a block's over its warps, then conv_reduce_kernel over the blocks,
-// each in a fixed order.  Four channels per thread: eight would need 150 registers.
+// each in a fixed order.
 template <int V>
 __device__ __forceinline__ void conv_dpre(float (&pre)[V], const float (&g)[V], bool silu) {
 #pragma unroll
@@ -231,8 +273,8 @@ __device__ __forceinline__ void conv_dpre(float (&pre)[V], const float (&g)[V], 
 }
 
 template <typename IO, int W>
-__global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
-    constexpr int V = 4, U = 4;
+__global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
+    constexpr int V = kConvVec, U = 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
     const bool live = c < a.C;
@@ -245,10 +287,6 @@ __global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvA
     auto window = [&](int row, int j) {  // input j of the row's window
         return init ? pack_load<IO, V>(init + ((size_t)row * (W - 1) + j) * a.C + cc) : pack_zero<IO, V>();
     };
-    auto floats = [](const Pack<IO, V> &v, float (&f)[V]) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
-    };
     const long long block = blockIdx.x / col_blocks;
     if (block < head_blocks) {  // gradients of the windows
         const long long row = block * (kConvThreads / 32) + warp;
@@ -260,7 +298,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvA
             p[i] = window((int)row, i);
 #pragma unroll
             for (int v = 0; v < V; ++v) d[i][v] = 0.f;
-            if (dfinal && i >= len) floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (i - len)) * a.C + cc), d[i]);
+            if (dfinal && i >= len) conv_floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (i - len)) * a.C + cc), d[i]);
         }
 #pragma unroll
         for (int t = 0; t < W - 1; ++t) {
@@ -268,7 +306,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvA
             p[W - 1] = pack_load<IO, V>(x + (size_t)(s + t) * a.x_stride);
             float pre[V], g[V];
             conv_pre<IO, W, V>(p, w, b, pre);
-            floats(pack_load<IO, V>(dout + (size_t)(s + t) * a.C), g);
+            conv_floats(pack_load<IO, V>(dout + (size_t)(s + t) * a.C), g);
             conv_dpre<V>(pre, g, a.silu);
 #pragma unroll
             for (int i = t; i < W - 1; ++i)  // input i of the window is input i - t of this token's
@@ -300,12 +338,13 @@ __global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvA
             row = a.rows.of(t);
             begin = a.rows.starts[row], end = a.rows.starts[row + 1];
         };
+        float f[W][V];
         if (t0 < tokens) {
             enter(t0);
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
                 const int t = t0 - (W - 1) + j;  // of the row, or of its window
-                p[j] = t >= begin ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : window(row, W - 1 + t - begin);
+                conv_floats(t >= begin ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : window(row, W - 1 + t - begin), f[j]);
             }
         }
         Pack<IO, V> in[U], dn[U];
@@ -322,48 +361,63 @@ __global__ void __launch_bounds__(kConvThreads) conv_backward_kernel(const ConvA
 #pragma unroll
             for (int u = 0; u < U; ++u) cur[u] = in[u], dcur[u] = dn[u];
             if (t + U < te) fetch(t + U);
+            IO *to = static_cast<IO *>(a.dx) + cc + ((long long)t - (W - 1)) * a.C;
+            auto shift = [&]() {
+#pragma unroll
+                for (int k = W - 1; k > 0; --k)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) pend[k][v] = pend[k - 1][v];
+#pragma unroll
+                for (int v = 0; v < V; ++v) pend[0][v] = 0.f;
+            };
+            auto token = [&](int u, int reach, bool own) {  // dpre of a token, into its own and the `reach` pending dx in front
+                conv_floats(cur[u], f[W - 1]);
+                float pre[V], g[V];
+                conv_pre<W, V>(f, w, b, pre);
+                conv_floats(dcur[u], g);
+                conv_dpre<V>(pre, g, a.silu);
+                if (own)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        dw[W][v] += pre[v];
+#pragma unroll
+                        for (int j = 0; j < W; ++j) dw[j][v] = fmaf(pre[v], f[j][v], dw[j][v]);
+                    }
+#pragma unroll
+                for (int k = 0; k < W; ++k)
+                    if (k <= reach)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) pend[k][v] = fmaf(w[W - 1 - k][v], pre[v], pend[k][v]);
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) f[j][v] = f[j + 1][v];
+            };
+            if (t - t0 >= W - 1 && t - begin >= W - 1 && t + U <= min(t1, end - (W - 1))) {  // one row, away from both ends
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    shift();
+                    token(u, W - 1, true);
+                    if (live) pack_store(to + u * a.C, pack_round<IO, V>(pend[W - 1]));
+                }
+                continue;
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int at = t + u;
-                if (at < t1 + W - 1) {
+                if (at >= t1 + W - 1) break;
+                shift();
+                if (at < te) {
+                    if (at >= end) {
+                        enter(at);
 #pragma unroll
-                    for (int k = W - 1; k > 0; --k)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) pend[k][v] = pend[k - 1][v];
-#pragma unroll
-                    for (int v = 0; v < V; ++v) pend[0][v] = 0.f;
-                    if (at < te) {
-                        if (at >= end) {
-                            enter(at);
-#pragma unroll
-                            for (int j = 0; j < W - 1; ++j) p[j] = window(row, j);
-                        }
-                        p[W - 1] = cur[u];
-                        float pre[V], g[V];
-                        conv_pre<IO, W, V>(p, w, b, pre);
-                        floats(dcur[u], g);
-                        conv_dpre<V>(pre, g, a.silu);
-                        if (at < t1) {
-#pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                dw[W][v] += pre[v];
-#pragma unroll
-                                for (int j = 0; j < W; ++j) dw[j][v] = fmaf(pre[v], to_f32(p[j].e[v]), dw[j][v]);
-                            }
-                            if (dfinal && at >= end - (W - 1))
-                                floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (at - end + W - 1)) * a.C + cc), pend[0]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < W; ++k)
-                            if (at - begin >= k)
-#pragma unroll
-                                for (int v = 0; v < V; ++v) pend[k][v] = fmaf(w[W - 1 - k][v], pre[v], pend[k][v]);
-#pragma unroll
-                        for (int j = 0; j < W - 1; ++j) p[j] = p[j + 1];
+                        for (int j = 0; j < W - 1; ++j) conv_floats(window(row, j), f[j]);
                     }
-                    const int done = at - (W - 1);
-                    if (done >= t0 && live) pack_store(static_cast<IO *>(a.dx) + (size_t)done * a.C + cc, pack_round<IO, V>(pend[W - 1]));
+                    if (at < t1 && dfinal && at >= end - (W - 1))
+                        conv_floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (at - end + W - 1)) * a.C + cc), pend[0]);
+                    token(u, at - begin, at < t1);
                 }
+                if (at - (W - 1) >= t0 && live) pack_store(to + u * a.C, pack_round<IO, V>(pend[W - 1]));
             }
         }
     }

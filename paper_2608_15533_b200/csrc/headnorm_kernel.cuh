@@ -26,7 +26,8 @@ struct NormArgs {
     float eps, q_scale;
 };
 
-constexpr int kNormThreads = 128, kNormHeads = 4;  // heads in flight per lane
+constexpr int kNormThreads = 128;
+constexpr int kNormHeads = 4, kNormHeadsBack = 2;  // heads in flight per lane
 
 template <typename IO>
 __device__ __forceinline__ void norm_load8(const IO *p, float (&x)[8]) { load8(p, x); }
@@ -98,15 +99,15 @@ __device__ __forceinline__ void norm_rotate(const NormArgs &a, const Turn &t, fl
     }
 }
 
-// Which heads of which token a warp's work item is: kNormHeads * 32 / L of q or of k.
+// Which heads of which token a warp's work item is: HEADS * 32 / L of q or of k.
 struct NormItem {
     int token, head, heads;  // first head and how many heads the tensor has
     bool is_k;
 };
 __host__ __device__ __forceinline__ int norm_chunks(int heads, int per) { return (heads + per - 1) / per; }
-template <int L>
+template <int L, int HEADS>
 __device__ __forceinline__ NormItem norm_item(const NormArgs &a, long long item) {
-    constexpr int per = kNormHeads * 32 / L;
+    constexpr int per = HEADS * 32 / L;
     const int cq = norm_chunks(a.H_q, per), all = cq + norm_chunks(a.H_k, per);
     NormItem w;
     w.token = (int)(item / all);
@@ -116,9 +117,9 @@ __device__ __forceinline__ NormItem norm_item(const NormArgs &a, long long item)
     w.heads = w.is_k ? a.H_k : a.H_q;
     return w;
 }
-template <int L>
+template <int L, int HEADS>
 __host__ __device__ __forceinline__ long long norm_items(int tokens, int H_q, int H_k) {
-    constexpr int per = kNormHeads * 32 / L;
+    constexpr int per = HEADS * 32 / L;
     return (long long)tokens * (norm_chunks(H_q, per) + norm_chunks(H_k, per));
 }
 
@@ -127,8 +128,8 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_forward_kernel(const N
     constexpr int G = 32 / L;
     const int lane = threadIdx.x & 31, l = lane & (L - 1), group = lane / L;
     const long long item = (long long)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
-    if (item >= norm_items<L>(a.tokens, a.H_q, a.H_k)) return;
-    const NormItem w = norm_item<L>(a, item);
+    if (item >= norm_items<L, kNormHeads>(a.tokens, a.H_q, a.H_k)) return;
+    const NormItem w = norm_item<L, kNormHeads>(a, item);
     const bool in = l * 8 < a.d;
     const IO *x = static_cast<const IO *>(w.is_k ? a.k : a.q) + (size_t)w.token * (w.is_k ? a.k_stride : a.q_stride) + l * 8;
     IO *out = static_cast<IO *>(w.is_k ? a.out_k : a.out_q) + (size_t)w.token * w.heads * a.d + l * 8;
@@ -170,24 +171,24 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_forward_kernel(const N
 }
 
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads) head_norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, 4) head_norm_backward_kernel(const NormArgs a) {
     constexpr int G = 32 / L;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
     const bool in = l * 8 < a.d, weighted = a.w_q != nullptr;
     const float c = a.norm == DELTALOG_NORM_RMS ? __fdividef(1.f, (float)a.d) : 1.f;
-    const long long items = norm_items<L>(a.tokens, a.H_q, a.H_k);
+    const long long items = norm_items<L, kNormHeadsBack>(a.tokens, a.H_q, a.H_k);
     float dw[2][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.f;
     for (long long item = (long long)blockIdx.x * (kNormThreads / 32) + warp; item < items; item += (long long)gridDim.x * (kNormThreads / 32)) {
-        const NormItem w = norm_item<L>(a, item);
+        const NormItem w = norm_item<L, kNormHeadsBack>(a, item);
         const IO *x = static_cast<const IO *>(w.is_k ? a.k : a.q) + (size_t)w.token * (w.is_k ? a.k_stride : a.q_stride) + l * 8;
         const size_t at = (size_t)w.token * w.heads * a.d + l * 8;
         const IO *dout = static_cast<const IO *>(w.is_k ? a.dout_k : a.dout_q) + at;
         IO *dx = static_cast<IO *>(w.is_k ? a.out_k : a.out_q) + at;
-        float v[kNormHeads][8], g[kNormHeads][8];
+        float v[kNormHeadsBack][8], g[kNormHeadsBack][8];
 #pragma unroll
-        for (int i = 0; i < kNormHeads; ++i) {
+        for (int i = 0; i < kNormHeadsBack; ++i) {
             const int h = w.head + i * G + group;
             if (in && h < w.heads) {
                 norm_load8(dout + (size_t)h * a.d, g[i]);
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_backward_kernel(const 
         if (wp && in) load8(wp + l * 8, weight);
         const float scale = w.is_k ? 1.f : a.q_scale;
 #pragma unroll
-        for (int i = 0; i < kNormHeads; ++i) {
+        for (int i = 0; i < kNormHeadsBack; ++i) {
             const int h = w.head + i * G + group;
             norm_rotate<true>(a, turn, g[i]);
 #pragma unroll

@@ -15,7 +15,7 @@ int validate_conv(const deltalog_conv_desc *d, const void *x, int64_t x_stride, 
     return DELTALOG_OK;
 }
 
-int conv_columns(const deltalog_conv_desc *d, int vec) { return (d->channels / vec + 31) / 32; }
+int conv_columns(const deltalog_conv_desc *d) { return (d->channels / kConvVec + 31) / 32; }
 
 ConvArgs conv_args(const deltalog_conv_desc *d, const void *x, int64_t x_stride, const float *weight, const float *bias) {
     ConvArgs a = {};
@@ -42,7 +42,7 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
     if ((d)->width == 2) { CALL(IO, 2); } else if ((d)->width == 3) { CALL(IO, 3); } else { CALL(IO, 4); }
 
 int conv_packed(const deltalog_conv_desc *d, ConvArgs &a, cudaStream_t s) {
-    const int cols = conv_columns(d, d->io_dtype == DELTALOG_F32 ? 4 : 8);
+    const int cols = conv_columns(d);
     // A run of 32 tokens reads 3 more than it owns; where that leaves SMs without warps the runs are shorter.
     const long long warps = (long long)cols * a.max_tokens;
     a.run = warps >= 32ll * 16 * device_info().sms ? 32 : 8;
@@ -60,7 +60,7 @@ int conv_packed(const deltalog_conv_desc *d, ConvArgs &a, cudaStream_t s) {
 struct ConvSplit { int run; long long groups; };
 ConvSplit conv_split(const deltalog_conv_desc *d, int32_t rows) {
     // (148 SMs whatever the device: the workspace's size must not depend on which device is current)
-    const long long most = ceil_div(148 * 16, conv_columns(d, 4));
+    const long long most = ceil_div(148 * 16, conv_columns(d));
     const long long run = ceil_div(rows, most * kWarpsPerCta);
     ConvSplit c;
     c.run = (int)(run < 16 ? 16 : run);
@@ -79,11 +79,9 @@ int deltalog_conv_step(const deltalog_conv_desc *desc, void *window, const void 
     if (!slot_idx && B > desc->num_slots) return DELTALOG_ERR_INVALID_ARG;
     if (B == 0) return DELTALOG_OK;
     ConvArgs a = conv_args(desc, x, x_stride, weight, bias);
-    a.final = window, a.out = out, a.slots = slot_idx, a.status = status, a.total_rows = B;
-    const int cols = conv_columns(desc, desc->io_dtype == DELTALOG_F32 ? 4 : 8);
-    // one row per warp until there are eight warps an SM; then rows share the weights' registers, eight at most
-    const long long per = (long long)cols * B / (8ll * device_info().sms);
-    a.run = (int)(per < 1 ? 1 : per > 8 ? 8 : per);
+    a.init = window, a.final = window, a.out = out, a.slots = slot_idx, a.status = status, a.total_rows = B;
+    const int cols = conv_columns(desc);
+    a.run = 4;  // in flight together; 250 rows of 12288 channels with 1, 2, 4, 8, 16 rows a warp: 24, 19, 16.6, 19, 18.6 us
     const long long grid = ceil_div(ceil_div(B, a.run), kWarpsPerCta) * cols;
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -122,7 +120,7 @@ int deltalog_conv_forward(const deltalog_conv_desc *desc, const deltalog_plan *p
 size_t deltalog_conv_workspace_bytes(const deltalog_conv_desc *desc, int32_t rows) {
     if (!desc || desc->channels <= 0 || desc->channels % 8 || desc->width < 2 || desc->width > 4 || rows < 0) return 0;
     // (room for the most blocks that this many rows or fewer make)
-    const long long most = ceil_div(148 * 16, conv_columns(desc, 4)), blocks = ceil_div(rows, 16 * kWarpsPerCta);
+    const long long most = ceil_div(148 * 16, conv_columns(desc)), blocks = ceil_div(rows, 16 * kWarpsPerCta);
     const size_t groups = (size_t)(blocks < 1 ? 1 : blocks < most ? blocks : most);
     return groups * (desc->width + 1) * desc->channels * sizeof(float);
 }
@@ -141,7 +139,7 @@ int deltalog_conv_backward(const deltalog_conv_desc *desc, const deltalog_plan *
     const ConvSplit split = conv_split(desc, rows);
     a.init = init, a.dout = dout, a.dfinal = dfinal, a.dx = grads->x, a.dinit = grads->init;
     a.total_rows = rows, a.run = split.run, a.partial = static_cast<float *>(workspace);
-    const int cols = conv_columns(desc, 4);
+    const int cols = conv_columns(desc);
     const long long heads = grads->init ? ceil_div(plan->n, kWarpsPerCta) : 0, grid = (heads + split.groups) * cols;
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

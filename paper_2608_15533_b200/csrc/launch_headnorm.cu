@@ -42,18 +42,19 @@ NormArgs norm_args(const deltalog_norm_desc *d, const void *q, int64_t q_stride,
 
 int norm_lanes(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
+template <int HEADS>
 long long norm_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     const int L = norm_lanes(d->d);
-    const long long items = L == 4 ? norm_items<4>(tokens, d->H_q, d->H_k) : L == 8 ? norm_items<8>(tokens, d->H_q, d->H_k)
-                          : L == 16 ? norm_items<16>(tokens, d->H_q, d->H_k) : norm_items<32>(tokens, d->H_q, d->H_k);
+    const long long items = L == 4 ? norm_items<4, HEADS>(tokens, d->H_q, d->H_k) : L == 8 ? norm_items<8, HEADS>(tokens, d->H_q, d->H_k)
+                          : L == 16 ? norm_items<16, HEADS>(tokens, d->H_q, d->H_k) : norm_items<32, HEADS>(tokens, d->H_q, d->H_k);
     return (items + kNormThreads / 32 - 1) / (kNormThreads / 32);
 }
 
-// Blocks of the backward pass with weights, whose sums they keep: four an SM (of 148, whichever device is current: the
+// Blocks of the backward pass with weights, whose sums they keep: eight an SM (of 148, whichever device is current: the
 // workspace's size depends on it).
 long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
-    const long long b = norm_blocks(d, tokens);
-    return b < 148 * 4 ? b : 148 * 4;
+    const long long b = norm_blocks<kNormHeadsBack>(d, tokens);
+    return b < 148 * 8 ? b : 148 * 8;
 }
 
 #define NORM_DISPATCH(desc_, CALL)                                                                  \
@@ -77,7 +78,7 @@ int deltalog_head_norm_forward(const deltalog_norm_desc *desc, const void *q, in
     if (tokens == 0) return DELTALOG_OK;
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = out_q, a.out_k = out_k, a.status = status;
-    const long long grid = norm_blocks(desc, tokens);
+    const long long grid = norm_blocks<kNormHeads>(desc, tokens);
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
 #define CALL(IO, L) head_norm_forward_kernel<IO, L><<<(unsigned)grid, kNormThreads, 0, s>>>(a)
@@ -104,7 +105,7 @@ int deltalog_head_norm_backward(const deltalog_norm_desc *desc, const void *q, i
         return DELTALOG_ERR_INVALID_ARG;
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = dq, a.out_k = dk, a.dout_q = dout_q, a.dout_k = dout_k, a.partial = static_cast<float *>(workspace);
-    const long long grid = weighted ? norm_kept_blocks(desc, tokens) : norm_blocks(desc, tokens);
+    const long long grid = weighted ? norm_kept_blocks(desc, tokens) : norm_blocks<kNormHeadsBack>(desc, tokens);
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (grid > 0) {

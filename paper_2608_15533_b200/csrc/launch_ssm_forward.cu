@@ -27,10 +27,8 @@ int forward(const SsmArgs &a, cudaStream_t s) {
 
 template <typename IO, int N>
 int step(const SsmArgs &a, cudaStream_t s) {
-    const int cols = (int)ssm_ceil(a.D_, kSsmWarps * SsmLanes<N>::kChannels);
-    // four rows per CTA, which are in flight together; more once there are enough CTAs for all SMs
-    const long long per = (long long)cols * a.total_rows / (16ll * device_info().sms);
-    const int run = per <= 4 ? 4 : per >= 16 ? 16 : (int)per / 4 * 4;
+    const int cols = (int)ssm_ceil(a.D_, kSsmWarps * 32 / (N / 8));
+    constexpr int run = 4;  // 125 rows of 4096 channels with 2, 4, 6, 8, 16 rows a CTA: 20.5, 20.7, 20.5, 22.9, 23.3 us
     const long long grid = ssm_ceil(a.total_rows, run) * cols;
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     ssm_step_kernel<IO, N><<<(unsigned)grid, kSsmThreads, 0, s>>>(a, cols, run);

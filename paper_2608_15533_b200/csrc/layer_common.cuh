@@ -28,8 +28,28 @@ __device__ __forceinline__ Pack<T, V> pack_round(const float (&x)[V]) {
     return v;
 }
 
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // 1 / (1 + e^-x): 0 and 1 at the infinities.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return rcp_fast(1.f + exp2_fast(-1.4426950408889634f * x)); }
+
+// Two neighbouring elements as floats, and back.
+__device__ __forceinline__ float2 load2(const float *p) { return *reinterpret_cast<const float2 *>(p); }
+__device__ __forceinline__ float2 load2(const __nv_bfloat16 *p) {
+    const uint32_t v = *reinterpret_cast<const uint32_t *>(p);
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ void store2(float *p, float2 v) { *reinterpret_cast<float2 *>(p) = v; }
+__device__ __forceinline__ void store2(__nv_bfloat16 *p, float2 v) { *reinterpret_cast<__nv_bfloat162 *>(p) = __float22bfloat162_rn(v); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // The packed rows of a plan.
 struct Rows {
@@ -49,6 +69,22 @@ struct Rows {
         return lo;
     }
 };
+
+// Slots of U rows of a single-token call, -1 for rows that it skips.  The list's entries are loaded together: one after the
+// other, each behind the test of the one before, they would cost a trip to memory each.
+template <int U>
+__device__ __forceinline__ void step_slots(const int32_t *slots, int row, int end, int num_slots, int32_t *status, int (&slot)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) slot[u] = slots ? slots[min(row + u, end - 1)] : row + u;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (row + u >= end) slot[u] = -1;
+        if (slot[u] >= num_slots) {
+            if ((threadIdx.x & 31) == 0 && status) atomicOr(status, DELTALOG_STATUS_BAD_SLOT);
+            slot[u] = -1;
+        }
+    }
+}
 
 // Column sums of a block's 32 columns over the rows of partial [rows, cols], eight threads a column, in a fixed order; the
 // sum arrives at the threads of the first warp (column blockIdx.x * 32 + lane), 0 elsewhere.  Blocks of 256 threads.

@@ -19,9 +19,12 @@ int validate_ssm(const deltalog_ssm_desc *d, const deltalog_ssm_inputs *in) {
     const int vec = d->io_dtype == DELTALOG_F32 ? 4 : 8;
     const long long states = (long long)d->groups * d->d_state;
     auto tokens_ok = [&](const void *p, long long stride, long long width) { return aligned16(p) && stride >= width && stride % vec == 0; };
+    auto too_wide = [](long long stride) { return stride > (1 << 25); };  // a tile's offsets are kept in 32 bits
     if (!tokens_ok(in->x, in->x_stride, d->channels) || !tokens_ok(in->dt, in->dt_stride, d->channels) ||
         !tokens_ok(in->B, in->B_stride, states) || !tokens_ok(in->C, in->C_stride, states) || (in->z && !tokens_ok(in->z, in->z_stride, d->channels)))
         return DELTALOG_ERR_INVALID_ARG;
+    if (too_wide(in->x_stride) || too_wide(in->dt_stride) || too_wide(in->B_stride) || too_wide(in->C_stride) || (in->z && too_wide(in->z_stride)))
+        return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(in->A) || !aligned16(in->D) || !aligned16(in->dt_bias)) return DELTALOG_ERR_INVALID_ARG;
     return DELTALOG_OK;
 }
@@ -61,6 +64,7 @@ int deltalog_ssm_step(const deltalog_ssm_desc *desc, float *S, const deltalog_ss
     if (int rc = validate_ssm(desc, in)) return rc;
     if (desc->num_slots <= 0 || B < 0 || !S || !out || !aligned16(S) || !aligned16(out)) return DELTALOG_ERR_INVALID_ARG;
     if (!slot_idx && B > desc->num_slots) return DELTALOG_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(S) % 32 || reinterpret_cast<uintptr_t>(in->A) % 32) return DELTALOG_ERR_INVALID_ARG;  // 32-byte accesses
     if (B == 0) return DELTALOG_OK;
     SsmArgs a = ssm_args(desc, in);
     a.S_in = S, a.S_out = S, a.slots = slot_idx, a.out = out, a.status = status, a.total_rows = B;

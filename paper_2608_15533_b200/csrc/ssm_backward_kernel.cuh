@@ -22,11 +22,12 @@ template <typename IO, int N> struct SsmBackward {
     struct Raw {
         IO x[kTile * kCols], dt[kTile * kCols], z[kTile * kCols], dout[kTile * kCols], B[kTile * N], C[kTile * N];
     };
+    static constexpr int kPitch = kCols + 16;  // lanes that answer for neighbouring tokens store to different banks
     struct alignas(16) Shared {
         Raw raw[2];
-        float2 step[kTile * kCols];  // delta, delta x
-        float dy[kTile * kCols], B[kTile * N], C[kTile * N];
-        float sums[3][kTile * kCols];  // C . h, sum dh B, sum dh a h_(t-1) A (in powers of two)
+        float2 step[kTile * kCols];                          // delta, delta x
+        float dy[kTile * kCols], slope[kTile * kCols];       // slope: softplus'
+        float sums[3][kTile * kPitch];                       // C . h, sum dh B, sum dh a h_(t-1) A (A in powers of two)
         float bc[kSsmWarps][kTile][2 * N];
         int state[kTile], row[kTile];
         unsigned begins, ends, there;
@@ -35,9 +36,9 @@ template <typename IO, int N> struct SsmBackward {
 
 // LOCAL: the first pass over a stretch whose first row began in front of it: the adjoint that the stretch alone hands back.
 template <typename IO, int N, bool LOCAL>
-__global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs a) {
+__global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmArgs a) {
     using F = SsmBackward<IO, N>;
-    constexpr int KC = F::kPer, CB = F::kCols, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels, VE = 16 / sizeof(IO), U = kSsmBlock;
+    constexpr int KC = F::kPer, CB = F::kCols, PB = F::kPitch, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels, U = kSsmBlock;
     extern __shared__ __align__(16) char smem[];
     typename F::Shared &s = *reinterpret_cast<typename F::Shared *>(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -45,26 +46,25 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs
     const int c0 = group * per_group + in_group, cols = min(CB, per_group - in_group);
     const int span = LOCAL ? blockIdx.y + 1 : blockIdx.y;
     const int nl = lane & (LN - 1), cl = lane / LN;
-    int mine[KC];
+    const int first = warp * KC * LC + cl;  // this lane's channels of the block: first, first + LC
+    auto at = [&](size_t state, int q) { return (state * a.D_ + c0 + first + q * LC) * N + nl * 4; };
+    auto mine = [&](int q) { return first + q * LC < cols; };
+    auto load = [&](const float *p, size_t state, float2 (&v)[KC][2]) {
 #pragma unroll
-    for (int k = 0; k < KC; ++k) mine[k] = (warp * KC + k) * LC + cl;
-    auto at = [&](size_t state, int k) { return (state * a.D_ + c0 + mine[k]) * N + nl * 4; };
-    auto load = [&](const float *p, size_t state, float (&v)[KC][4]) {
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-            const float4 f = p && mine[k] < cols ? *reinterpret_cast<const float4 *>(p + at(state, k)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            v[k][0] = f.x, v[k][1] = f.y, v[k][2] = f.z, v[k][3] = f.w;
+        for (int q = 0; q < KC; ++q) {
+            v[q][0] = v[q][1] = both(0.f);
+            if (p && mine(q)) ssm_load(p + at(state, q), v[q]);
         }
     };
-    auto store = [&](float *p, size_t state, const float (&v)[KC][4]) {
+    auto store = [&](float *p, size_t state, const float2 (&v)[KC][2]) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
-            if (mine[k] < cols) *reinterpret_cast<float4 *>(p + at(state, k)) = make_float4(v[k][0], v[k][1], v[k][2], v[k][3]);
+        for (int q = 0; q < KC; ++q)
+            if (mine(q)) ssm_store(p + at(state, q), v[q]);
     };
     if (!LOCAL && span >= a.spans) {  // rows without tokens hand on what they get
         for (int row = 0; row < a.rows.n; ++row) {
             if (a.rows.starts[row] != a.rows.starts[row + 1]) continue;
-            float v[KC][4];
+            float2 v[KC][2];
             load(a.dS_final, row, v);
             store(a.dS_init, row, v);
         }
@@ -73,22 +73,23 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs
     const int lo = span * a.span;
     int hi = (int)min((long long)a.total_rows, (long long)lo + a.span), only = -1;
     if (LOCAL) {
-        const SsmToken first = ssm_token(a, lo, false);
-        if (first.row < 0 || first.begin >= lo) return;
-        only = first.row;
-        hi = min(hi, first.end);
+        const SsmToken head = ssm_token(a, lo, false);
+        if (head.row < 0 || head.begin >= lo) return;
+        only = head.row;
+        hi = min(hi, head.end);
     }
     const IO *x = static_cast<const IO *>(a.x) + c0, *dt = static_cast<const IO *>(a.dt) + c0, *z = static_cast<const IO *>(a.z) + (a.z ? c0 : 0);
     const IO *dout = static_cast<const IO *>(a.dout) + c0;
     const IO *Bp = static_cast<const IO *>(a.B) + group * N, *Cp = static_cast<const IO *>(a.C) + group * N;
 
-    float A2[KC][4], carry[KC][4], dA[KC][4], kept[KC][4], sum[KC];
+    float2 A2[KC][2], carry[KC][2], dA[KC][2], kept[KC][2];
+    float sum[KC];
     load(a.A, 0, A2);
 #pragma unroll
-    for (int k = 0; k < KC; ++k) {
-        sum[k] = 0.f;
+    for (int q = 0; q < KC; ++q) {
+        sum[q] = 0.f;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) A2[k][n] *= 1.4426950408889634f, carry[k][n] = 0.f, dA[k][n] = 0.f;
+        for (int p = 0; p < 2; ++p) A2[q][p] = __fmul2_rn(A2[q][p], both(1.4426950408889634f)), carry[q][p] = dA[q][p] = both(0.f);
     }
     if (!LOCAL && span + 1 < a.spans) {
         const SsmToken last = ssm_token(a, hi - 1, false);
@@ -96,34 +97,38 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs
             int j = (last.end - 1) / a.span;
             load(a.local, j, carry);
             for (--j; j > span; --j) {
-                float own[KC][4];
+                float2 own[KC][2];
                 load(a.local, j, own);
 #pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    const float total = mine[k] < cols ? a.sums[(size_t)j * a.D_ + c0 + mine[k]] : 0.f;
+                for (int q = 0; q < KC; ++q) {
+                    const float total = mine(q) ? a.sums[(size_t)j * a.D_ + c0 + first + q * LC] : 0.f;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) carry[k][n] = fmaf(exp2_fast(A2[k][n] * total), carry[k][n], own[k][n]);
+                    for (int p = 0; p < 2; ++p) carry[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(total))), carry[q][p], own[q][p]);
                 }
             }
         }
     }
-    const int vec = (tid % (CB / VE)) * VE, vec_token = tid / (CB / VE);
-    constexpr int kTokenStep = kSsmThreads / (CB / VE) < TT ? kSsmThreads / (CB / VE) : TT;  // (narrow blocks leave threads without a token)
-    float bias[VE], skip[VE], dD[VE], dbias[VE];
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-        bias[e] = a.bias && vec < cols ? a.bias[c0 + vec + e] : 0.f;
-        skip[e] = a.D && vec < cols ? a.D[c0 + vec + e] : 0.f;
-        dD[e] = dbias[e] = 0.f;
-    }
+    // the two channels that this thread brings in and out, and its first token of a tile
+    const int col = (tid % (CB / 2)) * 2, col_token = tid / (CB / 2);
+    constexpr int kTokenStep = kSsmThreads / (CB / 2);
+    static_assert(kTokenStep <= TT, "every thread has tokens");
+    const float2 bias = a.bias && col < cols ? load2(a.bias + c0 + col) : both(0.f), skip = a.D && col < cols ? load2(a.D + c0 + col) : both(0.f);
+    float2 dD = both(0.f), dbias = both(0.f);
     auto fetch = [&](int t, int stage) {
         typename F::Raw &r = s.raw[stage];
-        if (!LOCAL) ssm_stage(r.x, x, a.x_stride, t, TT, lo, hi, CB, cols, kSsmThreads);
-        ssm_stage(r.dt, dt, a.dt_stride, t, TT, lo, hi, CB, cols, kSsmThreads);
-        ssm_stage(r.dout, dout, a.D_, t, TT, lo, hi, CB, cols, kSsmThreads);
-        if (a.z) ssm_stage(r.z, z, a.z_stride, t, TT, lo, hi, CB, cols, kSsmThreads);
-        if (!LOCAL) ssm_stage(r.B, Bp, a.B_stride, t, TT, lo, hi, N, N, kSsmThreads);
-        ssm_stage(r.C, Cp, a.C_stride, t, TT, lo, hi, N, N, kSsmThreads);
+        auto parts = [&](auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            ssm_stage<ALL, TT, CB>(r.dt, dt, a.dt_stride, t, lo, hi, cols);
+            ssm_stage<ALL, TT, CB>(r.dout, dout, a.D_, t, lo, hi, cols);
+            if (a.z) ssm_stage<ALL, TT, CB>(r.z, z, a.z_stride, t, lo, hi, cols);
+            ssm_stage<ALL, TT, N>(r.C, Cp, a.C_stride, t, lo, hi, N);
+            if (!LOCAL) {
+                ssm_stage<ALL, TT, CB>(r.x, x, a.x_stride, t, lo, hi, cols);
+                ssm_stage<ALL, TT, N>(r.B, Bp, a.B_stride, t, lo, hi, N);
+            }
+        };
+        if (t + TT <= hi && cols == CB) parts(std::true_type{});
+        else parts(std::false_type{});
         cp_async_commit();
     };
     const int top = (hi - 1) & ~(TT - 1);  // lo is a multiple of the tile
@@ -133,7 +138,7 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs
     if (!LOCAL) fetch_kept((hi - 1) & ~(U - 1));
     int stage = 0;
     for (int t = top; t >= lo; t -= TT, stage ^= 1) {
-        const typename F::Raw &r = s.raw[stage];
+        typename F::Raw &r = s.raw[stage];
         if (warp == 0) {
             SsmToken k{-1, -1, 0, 0};
             if (lane < TT && t + lane < hi) k = ssm_token(a, t + lane, false);
@@ -149,192 +154,223 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_backward_kernel(const SsmArgs
         if (t - TT >= lo) fetch(t - TT, stage ^ 1);
         const unsigned there = s.there, begins = s.begins, ends = s.ends;
 #pragma unroll
-        for (int q = 0; q < TT / kTokenStep; ++q) {
-            const int k = vec_token + q * kTokenStep;
-            if (vec_token >= kTokenStep) break;
-            const Pack<IO, VE> dv = pack_load<IO, VE>(r.dt + k * CB + vec), gv = pack_load<IO, VE>(r.dout + k * CB + vec);
-            Pack<IO, VE> xv, zv;
-            if (!LOCAL) xv = pack_load<IO, VE>(r.x + k * CB + vec);
-            if (a.z) zv = pack_load<IO, VE>(r.z + k * CB + vec);
-            const bool ok = there >> k & 1;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                float d = to_f32(dv.e[e]) + bias[e], g = to_f32(gv.e[e]);
-                if (a.softplus) d = ssm_softplus(d);
-                if (a.z) {
-                    const float zf = to_f32(zv.e[e]);
-                    g *= zf * sigmoid(zf);
-                }
-                s.step[k * CB + vec + e] = ok ? make_float2(d, LOCAL ? 0.f : d * to_f32(xv.e[e])) : make_float2(0.f, 0.f);
-                s.dy[k * CB + vec + e] = ok ? g : 0.f;
+        for (int i = 0; i < TT / kTokenStep; ++i) {
+            const int k = col_token + i * kTokenStep, to = k * CB + col;
+            const float2 v = __fadd2_rn(load2(r.dt + to), bias);
+            float2 d = v, e, g = load2(r.dout + to), u = both(0.f);
+            if (a.softplus) {
+                d = ssm_softplus(v, e);
+                if (!LOCAL) store2(s.slope + to, make_float2(ssm_sigmoid(v.x, e.x), ssm_sigmoid(v.y, e.y)));
             }
+            if (a.z) {
+                const float2 zf = load2(r.z + to);
+                g = __fmul2_rn(g, make_float2(zf.x * sigmoid(zf.x), zf.y * sigmoid(zf.y)));
+            }
+            if (!LOCAL) u = __fmul2_rn(d, load2(r.x + to));
+            *reinterpret_cast<float4 *>(s.step + to) = make_float4(d.x, u.x, d.y, u.y);
+            store2(s.dy + to, g);
         }
-        for (int i = tid; i < TT * N; i += kSsmThreads) {
-            const bool ok = there >> (i / N) & 1;
-            if (!LOCAL) s.B[i] = ok ? to_f32(r.B[i]) : 0.f;
-            s.C[i] = ok ? to_f32(r.C[i]) : 0.f;
+        if (there != (1u << TT) - 1) {  // a skipped token may hold anything, and changes nothing
+#pragma unroll
+            for (int i = 0; i < TT / kTokenStep; ++i) {
+                const int k = col_token + i * kTokenStep, to = k * CB + col;
+                if (there >> k & 1) continue;
+                *reinterpret_cast<float4 *>(s.step + to) = make_float4(0.f, 0.f, 0.f, 0.f);
+                store2(s.dy + to, both(0.f));
+            }
+            for (int i = tid; i < TT * N; i += kSsmThreads)
+                if (!(there >> (i / N) & 1)) r.B[i] = r.C[i] = from_f32<IO>(0.f);
         }
         __syncthreads();
-#pragma unroll 1
-        for (int k0 = TT - U; k0 >= 0; k0 -= U) {
-            if (t + k0 >= hi) continue;
-            if (LOCAL) {
+        // four tokens; MARKED: where rows may begin or end
+        auto back = [&](int k0, auto marked) {
+            constexpr bool MARKED = decltype(marked)::value;
+            const float2 *step = s.step + k0 * CB + first;
+            const float *dys = s.dy + k0 * CB + first;
 #pragma unroll
-                for (int i = U - 1; i >= 0; --i) {
-                    const int k = k0 + i;
-                    if (ends >> k & 1) load(a.dS_final, s.state[k], carry);
-                    const float4 Cv = *reinterpret_cast<const float4 *>(s.C + k * N + nl * 4);
-                    const float c[4] = {Cv.x, Cv.y, Cv.z, Cv.w};
-#pragma unroll
-                    for (int q = 0; q < KC; ++q) {
-                        const float d = s.step[k * CB + mine[q]].x, dy = s.dy[k * CB + mine[q]];
-                        sum[q] += d;
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) carry[q][n] = exp2_fast(d * A2[q][n]) * fmaf(c[n], dy, carry[q][n]);
-                    }
-                }
-                continue;
-            }
-            float h[KC][4], decay[U][KC][4], moved[U][KC][4];
-#pragma unroll
-            for (int q = 0; q < KC; ++q)
-#pragma unroll
-                for (int n = 0; n < 4; ++n) h[q][n] = kept[q][n];
-            if (t + k0 > lo) fetch_kept(t + k0 - U);
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int k = k0 + i;
-                if (begins >> k & 1) load(a.S_in, s.state[k], h);
-                const float4 Bv = *reinterpret_cast<const float4 *>(s.B + k * N + nl * 4);
-                const float b[4] = {Bv.x, Bv.y, Bv.z, Bv.w};
+            for (int i = 3; i >= 0; --i) {
+                if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
+                float2 c[2];
+                ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
-                    const float2 d = s.step[k * CB + mine[q]];
+                    const float d = step[i * CB + q * LC].x, dy = dys[i * CB + q * LC];
+                    sum[q] += d;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        decay[i][q][n] = exp2_fast(d.x * A2[q][n]);
-                        moved[i][q][n] = decay[i][q][n] * h[q][n];
-                        h[q][n] = fmaf(d.y, b[n], moved[i][q][n]);
+                    for (int p = 0; p < 2; ++p)
+                        carry[q][p] = __fmul2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d))), __ffma2_rn(c[p], both(dy), carry[q][p]));
+                }
+            }
+        };
+        auto ahead = [&](int k0, auto &h, auto marked) {
+            constexpr bool MARKED = decltype(marked)::value;
+            const float2 *step = s.step + k0 * CB + first;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (MARKED && (begins >> (k0 + i) & 1)) load(a.S_in, s.state[k0 + i], h);
+                float2 b[2];
+                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+#pragma unroll
+                for (int q = 0; q < KC; ++q) {
+                    const float2 d = step[i * CB + q * LC];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d.x))), h[q][p], __fmul2_rn(both(d.y), b[p]));
+                }
+            }
+        };
+        auto both_ways = [&](int k0, auto &h, auto marked) {
+            constexpr bool MARKED = decltype(marked)::value;
+            const float2 *step = s.step + k0 * CB + first;
+            const float *dys = s.dy + k0 * CB + first;
+            float2 decay[4][KC][2], moved[4][KC][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (MARKED && (begins >> (k0 + i) & 1)) load(a.S_in, s.state[k0 + i], h);
+                float2 b[2];
+                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+#pragma unroll
+                for (int q = 0; q < KC; ++q) {
+                    const float2 d = step[i * CB + q * LC];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        decay[i][q][p] = exp2_fast(__fmul2_rn(A2[q][p], both(d.x)));
+                        moved[i][q][p] = __fmul2_rn(decay[i][q][p], h[q][p]);
+                        if (i < 3) h[q][p] = __ffma2_rn(both(d.y), b[p], moved[i][q][p]);
                     }
                 }
             }
-            constexpr int kTogether = LN / 2;  // tokens whose sums over the states run together: three results a lane
+            constexpr int kTogether = LN / 2 < 4 ? LN / 2 : 4;  // tokens whose sums over the states run together: three results a lane
             float out[3 * KC * kTogether];
 #pragma unroll
-            for (int i = U - 1; i >= 0; --i) {
-                const int k = k0 + i;
-                if (ends >> k & 1) load(a.dS_final, s.state[k], carry);
-                const float4 Bv = *reinterpret_cast<const float4 *>(s.B + k * N + nl * 4), Cv = *reinterpret_cast<const float4 *>(s.C + k * N + nl * 4);
-                const float b[4] = {Bv.x, Bv.y, Bv.z, Bv.w}, c[4] = {Cv.x, Cv.y, Cv.z, Cv.w};
-                float bc[8];
+            for (int i = 3; i >= 0; --i) {
+                if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
+                float2 b[2], c[2], bc[4];
+                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+                ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
-                    const float2 d = s.step[k * CB + mine[q]];
-                    const float dy = s.dy[k * CB + mine[q]];
-                    float y = 0.f, sB = 0.f, sA = 0.f;
+                    const float2 d = step[i * CB + q * LC];
+                    const float2 dy = both(dys[i * CB + q * LC]), delta = both(d.x), u = both(d.y);
+                    float2 y, sB, sA;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float dh = fmaf(c[n], dy, carry[q][n]), hn = fmaf(d.y, b[n], moved[i][q][n]), w = dh * moved[i][q][n];
-                        y = fmaf(c[n], hn, y);
-                        sB = fmaf(dh, b[n], sB);
-                        sA = fmaf(w, A2[q][n], sA);
-                        dA[q][n] = fmaf(w, d.x, dA[q][n]);
-                        bc[n] = q ? fmaf(dh, d.y, bc[n]) : dh * d.y;
-                        bc[4 + n] = q ? fmaf(dy, hn, bc[4 + n]) : dy * hn;
-                        carry[q][n] = decay[i][q][n] * dh;
+                    for (int p = 0; p < 2; ++p) {
+                        const float2 dh = __ffma2_rn(c[p], dy, carry[q][p]), hn = __ffma2_rn(u, b[p], moved[i][q][p]), w = __fmul2_rn(dh, moved[i][q][p]);
+                        y = p ? __ffma2_rn(c[p], hn, y) : __fmul2_rn(c[p], hn);
+                        sB = p ? __ffma2_rn(dh, b[p], sB) : __fmul2_rn(dh, b[p]);
+                        sA = p ? __ffma2_rn(w, A2[q][p], sA) : __fmul2_rn(w, A2[q][p]);
+                        dA[q][p] = __ffma2_rn(w, delta, dA[q][p]);
+                        bc[p] = q ? __ffma2_rn(dh, u, bc[p]) : __fmul2_rn(dh, u);
+                        bc[2 + p] = q ? __ffma2_rn(dy, hn, bc[2 + p]) : __fmul2_rn(dy, hn);
+                        carry[q][p] = __fmul2_rn(decay[i][q][p], dh);
                     }
                     float *o = out + ((i % kTogether) * KC + q) * 3;
-                    o[0] = y, o[1] = sB, o[2] = sA;
+                    o[0] = y.x + y.y, o[1] = sB.x + sB.y, o[2] = sA.x + sA.y;
                 }
-                if (begins >> k & 1) {
-                    if (a.dS_init) store(a.dS_init, s.state[k], carry);
+                if (MARKED && (begins >> (k0 + i) & 1)) {
+                    if (a.dS_init) store(a.dS_init, s.state[k0 + i], carry);
 #pragma unroll
-                    for (int q = 0; q < KC; ++q)
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) carry[q][n] = 0.f;
+                    for (int q = 0; q < KC; ++q) carry[q][0] = carry[q][1] = both(0.f);
                 }
-                const int v0 = lanes_reduce<8, LC, LN>(bc, lane);
+                float v[8] = {bc[0].x, bc[0].y, bc[1].x, bc[1].y, bc[2].x, bc[2].y, bc[3].x, bc[3].y};
+                const int v0 = lanes_reduce<8, LC, LN>(v, lane);
 #pragma unroll
-                for (int j = 0; j < (LC >= 8 ? 1 : 8 / LC); ++j) s.bc[warp][k][((v0 + j) / 4) * N + nl * 4 + (v0 + j) % 4] = bc[j];
+                for (int j = 0; j < (LC >= 8 ? 1 : 8 / LC); ++j) s.bc[warp][k0 + i][((v0 + j) / 4) * N + nl * 4 + (v0 + j) % 4] = v[j];
                 if (i % kTogether == 0) {
-                    const int first = lanes_reduce<3 * KC * kTogether, LN>(out, lane) / 3, q = first % KC;
-                    const int to = (k + first / KC) * CB + (warp * KC + q) * LC + cl;
+                    const int o0 = lanes_reduce<3 * KC * kTogether, LN>(out, lane) / 3;
+                    const int to = (k0 + i + o0 / KC) * PB + first + o0 % KC * LC;
                     s.sums[0][to] = out[0], s.sums[1][to] = out[1], s.sums[2][to] = out[2];
                 }
             }
+        };
+#pragma unroll 1
+        for (int k0 = TT - U; k0 >= 0; k0 -= U) {
+            if (t + k0 >= hi) continue;
+            const bool low = (begins | ends) >> k0 & 15, high = (begins | ends) >> (k0 + 4) & 15;
+            if constexpr (LOCAL) {
+                if (high) back(k0 + 4, std::true_type{});
+                else back(k0 + 4, std::false_type{});
+                if (low) back(k0, std::true_type{});
+                else back(k0, std::false_type{});
+            } else {
+                float2 h[KC][2];
+#pragma unroll
+                for (int q = 0; q < KC; ++q) h[q][0] = kept[q][0], h[q][1] = kept[q][1];
+                if (low || high) {
+                    ahead(k0, h, std::true_type{});
+                    both_ways(k0 + 4, h, std::true_type{});
+                } else {
+                    ahead(k0, h, std::false_type{});
+                    both_ways(k0 + 4, h, std::false_type{});
+                }
+#pragma unroll
+                for (int q = 0; q < KC; ++q) h[q][0] = kept[q][0], h[q][1] = kept[q][1];
+                if (t + k0 > lo) fetch_kept(t + k0 - U);
+                if (low || high) both_ways(k0, h, std::true_type{});
+                else both_ways(k0, h, std::false_type{});
+            }
         }
         __syncthreads();
-        if (LOCAL) continue;
-        for (int i = tid; i < TT * 2 * N; i += kSsmThreads) {
-            const int k = i / (2 * N), j = i - k * 2 * N;
-            if (t + k >= hi) break;
-            float v = s.bc[0][k][j];
+        if constexpr (!LOCAL) {
+            for (int i = tid; i < TT * 2 * N; i += kSsmThreads) {
+                const int k = i / (2 * N), j = i - k * 2 * N;
+                if (t + k >= hi) break;
+                float v = s.bc[0][k][j];
 #pragma unroll
-            for (int w = 1; w < kSsmWarps; ++w) v += s.bc[w][k][j];
-            a.part_bc[((size_t)blockIdx.x * a.total_rows + t + k) * 2 * N + j] = v;
-        }
-        if (vec < cols) {
+                for (int w = 1; w < kSsmWarps; ++w) v += s.bc[w][k][j];
+                a.part_bc[((size_t)blockIdx.x * a.total_rows + t + k) * 2 * N + j] = v;
+            }
+            if (col < cols) {
+                const int here = min(TT, hi - t);
 #pragma unroll
-            for (int q = 0; q < TT / kTokenStep; ++q) {
-                const int k = vec_token + q * kTokenStep;
-                if (vec_token >= kTokenStep || t + k >= hi) break;
-                const size_t to = (size_t)(t + k) * a.D_ + c0 + vec;
-                if (!(there >> k & 1)) {
-                    pack_store(static_cast<IO *>(a.dx) + to, pack_zero<IO, VE>());
-                    pack_store(static_cast<IO *>(a.ddt) + to, pack_zero<IO, VE>());
-                    if (a.dz) pack_store(static_cast<IO *>(a.dz) + to, pack_zero<IO, VE>());
-                    continue;
-                }
-                const Pack<IO, VE> xv = pack_load<IO, VE>(r.x + k * CB + vec), dv = pack_load<IO, VE>(r.dt + k * CB + vec),
-                                   gv = pack_load<IO, VE>(r.dout + k * CB + vec);
-                Pack<IO, VE> zv, o;
-                if (a.z) zv = pack_load<IO, VE>(r.z + k * CB + vec);
-                float ddt[VE], dx[VE];
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const int i = k * CB + vec + e;
-                    const float xf = to_f32(xv.e[e]), dy = s.dy[i], sB = s.sums[1][i];
-                    dx[e] = fmaf(s.step[i].x, sB, skip[e] * dy);
-                    ddt[e] = fmaf(xf, sB, s.sums[2][i] * 0.6931471805599453f);
-                    if (a.softplus) ddt[e] *= sigmoid(to_f32(dv.e[e]) + bias[e]);
-                    dD[e] = fmaf(dy, xf, dD[e]);
-                    dbias[e] += ddt[e];
+                for (int i = 0; i < TT / kTokenStep; ++i) {
+                    const int k = col_token + i * kTokenStep, n = k * CB + col, sn = k * PB + col;
+                    if (k >= here) break;
+                    const size_t to = (size_t)(t + k) * a.D_ + c0 + col;
+                    IO *dx = static_cast<IO *>(a.dx) + to, *ddt = static_cast<IO *>(a.ddt) + to, *dz = static_cast<IO *>(a.dz) + (a.dz ? to : 0);
+                    if (!(there >> k & 1)) {
+                        store2(dx, both(0.f)), store2(ddt, both(0.f));
+                        if (a.dz) store2(dz, both(0.f));
+                        continue;
+                    }
+                    const float4 st = *reinterpret_cast<const float4 *>(s.step + n);
+                    const float2 xf = load2(r.x + n), dy = load2(s.dy + n), sB = load2(s.sums[1] + sn), sA = load2(s.sums[2] + sn);
+                    float2 g = __ffma2_rn(xf, sB, __fmul2_rn(sA, both(0.6931471805599453f)));
+                    if (a.softplus) g = __fmul2_rn(g, load2(s.slope + n));
+                    store2(dx, __ffma2_rn(make_float2(st.x, st.z), sB, __fmul2_rn(skip, dy)));
+                    store2(ddt, g);
+                    dD = __ffma2_rn(dy, xf, dD), dbias = __fadd2_rn(dbias, g);
                     if (a.z) {
-                        const float zf = to_f32(zv.e[e]), g = sigmoid(zf);
-                        o.e[e] = from_f32<IO>(to_f32(gv.e[e]) * fmaf(skip[e], xf, s.sums[0][i]) * g * (1.f + zf * (1.f - g)));
+                        const float2 zf = load2(r.z + n), y = __fmul2_rn(load2(r.dout + n), __ffma2_rn(skip, xf, load2(s.sums[0] + sn)));
+                        const float g0 = sigmoid(zf.x), g1 = sigmoid(zf.y);
+                        store2(dz, make_float2(y.x * g0 * fmaf(zf.x, 1.f - g0, 1.f), y.y * g1 * fmaf(zf.y, 1.f - g1, 1.f)));
                     }
                 }
-                pack_store(static_cast<IO *>(a.dx) + to, pack_round<IO, VE>(dx));
-                pack_store(static_cast<IO *>(a.ddt) + to, pack_round<IO, VE>(ddt));
-                if (a.dz) pack_store(static_cast<IO *>(a.dz) + to, o);
             }
         }
     }
-    if (LOCAL) {
+    if constexpr (LOCAL) {
         store(a.local, span, carry);
         if (nl == 0)
 #pragma unroll
-            for (int k = 0; k < KC; ++k)
-                if (mine[k] < cols) a.sums[(size_t)span * a.D_ + c0 + mine[k]] = sum[k];
-        return;
-    }
-    store(a.part_A, span, dA);
-    // dD and dbias: over the threads that share a vector of channels
-    __syncthreads();
-    float *over = &s.sums[0][0];  // [kTokenStep][2][CB] of 3 * kTile * CB
-    static_assert(kTokenStep * 2 <= 3 * TT, "the tile's sums have room for the columns' ones");
-    if (vec_token < kTokenStep)
+            for (int q = 0; q < KC; ++q)
+                if (mine(q)) a.sums[(size_t)span * a.D_ + c0 + first + q * LC] = sum[q];
+    } else {
+        store(a.part_A, span, dA);
+        // dD and dbias: over the threads that share a pair of channels
+        __syncthreads();
+        float *over = &s.sums[0][0];  // [2][kTokenStep][CB]
+        static_assert(2 * kTokenStep * CB <= 3 * TT * PB, "the tile's sums have room for the columns' ones");
+        store2(over + col_token * CB + col, dD);
+        store2(over + (kTokenStep + col_token) * CB + col, dbias);
+        __syncthreads();
+        for (int i = tid; i < 2 * cols; i += kSsmThreads) {
+            const int n = i / cols, c = i - n * cols;
+            float v = 0.f;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            over[(vec_token * 2) * CB + vec + e] = dD[e];
-            over[(vec_token * 2 + 1) * CB + vec + e] = dbias[e];
+            for (int k = 0; k < kTokenStep; ++k) v += over[(n * kTokenStep + k) * CB + c];
+            a.part_cols[((size_t)span * 2 + n) * a.D_ + c0 + c] = v;
         }
-    __syncthreads();
-    for (int i = tid; i < 2 * cols; i += kSsmThreads) {
-        const int n = i / cols, c = i - n * cols;
-        float v = 0.f;
-        for (int k = 0; k < kTokenStep; ++k) v += over[(k * 2 + n) * CB + c];
-        a.part_cols[((size_t)span * 2 + n) * a.D_ + c0 + c] = v;
     }
 }
 

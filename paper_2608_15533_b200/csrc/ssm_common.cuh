@@ -9,6 +9,8 @@
 //     h = exp(A sum_j) (.. exp(A sum_i) h_i + h_(i+1) ..) + h_j.
 #pragma once
 
+#include <type_traits>
+
 #include "layer_common.cuh"
 
 namespace deltalog {
@@ -44,48 +46,55 @@ template <int N> struct SsmLanes {
     static constexpr int kStates = N / 4, kChannels = 32 / kStates;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+__device__ __forceinline__ float2 exp2_fast(float2 x) { return make_float2(exp2_fast(x.x), exp2_fast(x.y)); }
+
+// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|) in (0, 1], of two values.  The exponent of two is rounded, by up to |v| / 2^24:
+// what it lost goes into the result by the first-order term.  log(1 + e) = e P(e) with P the polynomial of degree 9 of least relative
+// error on [0, 1] (5e-9, by exchange of its extrema; 1.4e-7 with the roundings): small step sizes keep their relative accuracy,
+// which the logarithm of a rounded 1 + e would lose.  `e` comes back for the derivative.
+__device__ __forceinline__ float2 ssm_softplus(float2 v, float2 &e) {
+    const float2 m = make_float2(-fabsf(v.x), -fabsf(v.y)), x = __fmul2_rn(m, both(1.4426950408889634f));
+    const float2 lost = __fmul2_rn(__ffma2_rn(m, both(1.4426950408889634f), make_float2(-x.x, -x.y)), both(0.6931471805599453f));
+    e = exp2_fast(x);
+    e = __ffma2_rn(e, lost, e);
+    constexpr float kP[10] = {1.f, -0.4999990165233612f, 0.3332996368408203f, -0.24954134225845337f, 0.1967593878507614f,
+                              -0.15305592119693756f, 0.10603655129671097f, -0.05695953220129013f, 0.01985146291553974f, -0.0032440251670777798f};
+    float2 p = both(kP[9]);
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = __ffma2_rn(p, e, both(kP[i]));
+    return __ffma2_rn(p, e, make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+// softplus'(v) = 1 / (1 + exp(-v)) from that e.
+__device__ __forceinline__ float ssm_sigmoid(float v, float e) {
+    const float r = rcp_fast(1.f + e);
+    return v >= 0.f ? r : e * r;
 }
 
-// softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|) <= 1, with log(1 + e) = 2 atanh(t), t = e / (2 + e) <= 1/3, by the
-// series t + t^3/3 + ..: what is left out is below t^14 / 15 < 2e-8 of the sum, and small e keep their relative accuracy.
-__device__ __forceinline__ float ssm_softplus(float v) {
-    const float e = __expf(-fabsf(v)), t = __fdividef(e, 2.f + e), s = t * t;
-    float p = 1.f / 13.f;
-    p = fmaf(p, s, 1.f / 11.f);
-    p = fmaf(p, s, 1.f / 9.f);
-    p = fmaf(p, s, 1.f / 7.f);
-    p = fmaf(p, s, 1.f / 5.f);
-    p = fmaf(p, s, 1.f / 3.f);
-    p = fmaf(p, s, 1.f);
-    return fmaxf(v, 0.f) + 2.f * t * p;
-}
-
-// Sums over the LN neighbouring lanes of a group, of V values at once: every step halves the values that a lane answers
-// for.  On return v[0 .. V / LN) hold the sums of the values from the returned index on.
+// Sums over the LN lanes of a group (STRIDE apart) of V values at once: every step halves the values that a lane answers for, as
+// long as their number is even.  On return v[0..] holds the sums of the values from the returned index on.
 template <int V, int LN, int STRIDE = 1>
 __device__ __forceinline__ int lanes_reduce(float (&v)[V], int lane) {
-    int first = 0, have = V;
+    int first = 0;
+    auto step = [&](auto have_, auto o_) {
+        constexpr int HAVE = decltype(have_)::value, O = decltype(o_)::value;
+        const bool up = lane & (O * STRIDE);
+        if constexpr (HAVE % 2 == 0) {
 #pragma unroll
-    for (int o = LN / 2; o > 0; o >>= 1) {
-        const bool up = lane & (o * STRIDE);
-        if (have > 1) {
-            have >>= 1;
-#pragma unroll
-            for (int j = 0; j < V / 2; ++j) {
-                if (j < have) {
-                    const float send = up ? v[j] : v[j + have], stay = up ? v[j + have] : v[j];
-                    v[j] = stay + __shfl_xor_sync(0xffffffffu, send, o * STRIDE);
-                }
+            for (int j = 0; j < HAVE / 2; ++j) {
+                const float send = up ? v[j] : v[j + HAVE / 2], stay = up ? v[j + HAVE / 2] : v[j];
+                v[j] = stay + __shfl_xor_sync(0xffffffffu, send, O * STRIDE);
             }
-            first += up ? have : 0;
+            first += up ? HAVE / 2 : 0;
         } else {
-            v[0] += __shfl_xor_sync(0xffffffffu, v[0], o * STRIDE);
+#pragma unroll
+            for (int j = 0; j < HAVE; ++j) v[j] += __shfl_xor_sync(0xffffffffu, v[j], O * STRIDE);
         }
-    }
+    };
+    constexpr int H1 = V % 2 ? V : V / 2, H2 = H1 % 2 ? H1 : H1 / 2, H3 = H2 % 2 ? H2 : H2 / 2;
+    if constexpr (LN >= 2) step(std::integral_constant<int, V>{}, std::integral_constant<int, LN / 2>{});
+    if constexpr (LN >= 4) step(std::integral_constant<int, H1>{}, std::integral_constant<int, LN / 4>{});
+    if constexpr (LN >= 8) step(std::integral_constant<int, H2>{}, std::integral_constant<int, LN / 8>{});
+    if constexpr (LN >= 16) step(std::integral_constant<int, H3>{}, std::integral_constant<int, LN / 16>{});
     return first;
 }
 
@@ -94,18 +103,38 @@ __device__ __forceinline__ void ssm_copy16(void *dst, const void *src, bool ther
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(smem_addr(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// A tile of `rows` tokens x `cols` elements (16-byte multiples) into dense shared memory; tokens from `first` on are those
-// of [lo, hi), columns those below `cols_there`; everything else becomes zero.
-template <typename IO>
-__device__ __forceinline__ void ssm_stage(IO *dst, const IO *src, long long stride, int first, int rows, int lo, int hi, int cols, int cols_there, int threads) {
-    constexpr int V = 16 / sizeof(IO);
-    const int per = cols / V;
-    for (int i = threadIdx.x; i < rows * per; i += threads) {
-        const int r = i / per, c = (i - r * per) * V, t = first + r;
-        const bool there = t >= lo && t < hi && c < cols_there;
-        ssm_copy16(dst + r * cols + c, there ? src + (size_t)t * stride + c : src, there);
+// A tile of ROWS tokens x COLS elements (multiples of 16 bytes) into dense shared memory; tokens from `first` on are those of
+// [lo, hi), columns those below `there`; everything else becomes zero.  ALL: nothing is missing.
+template <bool ALL, int ROWS, int COLS, typename IO>
+__device__ __forceinline__ void ssm_stage(IO *dst, const IO *src, long long stride, int first, int lo, int hi, int there) {
+    constexpr int V = 16 / sizeof(IO), PER = COLS / V, N = ROWS * PER;
+    const IO *tile = src + first * stride;
+#pragma unroll
+    for (int i0 = 0; i0 < N; i0 += kSsmThreads) {
+        const int i = i0 + threadIdx.x;
+        if (N % kSsmThreads && i >= N) break;
+        const int r = i / PER, c = (i % PER) * V, t = first + r, off = r * (int)stride + c;
+        if (ALL) {
+            cp_async16(dst + i * V, tile + off);
+        } else {
+            const bool ok = t >= lo && t < hi && c < there;
+            ssm_copy16(dst + i * V, ok ? tile + off : src, ok);
+        }
     }
 }
+
+// Four neighbouring states' values of a token as two pairs.
+template <typename IO>
+__device__ __forceinline__ void ssm_pairs(const IO *p, float2 (&v)[2]) {
+    float f[4];
+    load_vec<IO, 4>(p, f);
+    v[0] = make_float2(f[0], f[1]), v[1] = make_float2(f[2], f[3]);
+}
+__device__ __forceinline__ void ssm_load(const float *p, float2 (&v)[2]) {
+    const float4 f = *reinterpret_cast<const float4 *>(p);
+    v[0] = make_float2(f.x, f.y), v[1] = make_float2(f.z, f.w);
+}
+__device__ __forceinline__ void ssm_store(float *p, const float2 (&v)[2]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y); }
 
 // What a token's row says: looked up by one lane per token of a tile.
 struct SsmToken {

@@ -11,15 +11,16 @@
 namespace deltalog {
 
 template <typename IO, int N> struct SsmForward {
-    static constexpr int kPer = N <= 16 ? 1 : N / 16;                                       // channels per lane
+    static constexpr int kPer = N <= 32 ? 2 : 4;                                            // channels per lane
     static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = 32;    // channels of a CTA, tokens of a tile
+    static constexpr int kPitch = kCols + 8;  // lanes that answer for neighbouring tokens store to different banks
+    static constexpr int kCtas = N <= 32 ? 5 : 3;                                           // on an SM, by their registers
     struct Raw {
         IO x[kTile * kCols], dt[kTile * kCols], z[kTile * kCols], B[kTile * N], C[kTile * N];
     };
     struct alignas(16) Shared {
         Raw raw[2];
-        float2 step[kTile * kCols];  // delta, delta x
-        float B[kTile * N], C[kTile * N], y[kTile * kCols];
+        float2 step[kTile * kPitch];  // delta, delta x; then C . h in the first's place
         int state[kTile], row[kTile];
         unsigned begins, ends, there, open;  // one bit per token of the tile; open: its row goes on behind the stretch
     };
@@ -27,9 +28,9 @@ template <typename IO, int N> struct SsmForward {
 
 // LOCAL: the first pass over a stretch whose last row goes on behind it.
 template <typename IO, int N, bool LOCAL>
-__global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs a) {
+__global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_forward_kernel(const SsmArgs a) {
     using F = SsmForward<IO, N>;
-    constexpr int KC = F::kPer, CB = F::kCols, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels, VE = 16 / sizeof(IO);
+    constexpr int KC = F::kPer, CB = F::kCols, PB = F::kPitch, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels;
     extern __shared__ __align__(16) char smem[];
     typename F::Shared &s = *reinterpret_cast<typename F::Shared *>(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -37,19 +38,18 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     const int c0 = group * per_group + in_group, cols = min(CB, per_group - in_group);  // this CTA's channels
     const int span = blockIdx.y;
     const int nl = lane & (LN - 1), cl = lane / LN;
-    int mine[KC];  // this lane's channels within the block
-#pragma unroll
-    for (int k = 0; k < KC; ++k) mine[k] = (warp * KC + k) * LC + cl;
-    auto at = [&](size_t state, int k) { return (state * a.D_ + c0 + mine[k]) * N + nl * 4; };
+    const int first = warp * KC * LC + cl;  // this lane's channels of the block: first, first + LC ..
+    auto at = [&](size_t state, int q) { return (state * a.D_ + c0 + first + q * LC) * N + nl * 4; };
+    auto mine = [&](int q) { return first + q * LC < cols; };
 
     if (!LOCAL && span >= a.spans) {  // rows without tokens: their state is the one they came with
         for (int row = 0; row < a.rows.n; ++row) {
             if (a.rows.starts[row] != a.rows.starts[row + 1]) continue;
 #pragma unroll
-            for (int k = 0; k < KC; ++k)
-                if (mine[k] < cols)
-                    *reinterpret_cast<float4 *>(a.S_out + at(row, k)) =
-                        a.S_in ? *reinterpret_cast<const float4 *>(a.S_in + at(row, k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int q = 0; q < KC; ++q)
+                if (mine(q))
+                    *reinterpret_cast<float4 *>(a.S_out + at(row, q)) =
+                        a.S_in ? *reinterpret_cast<const float4 *>(a.S_in + at(row, q)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
         return;
     }
@@ -64,72 +64,68 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     const IO *x = static_cast<const IO *>(a.x) + c0, *dt = static_cast<const IO *>(a.dt) + c0, *z = static_cast<const IO *>(a.z) + (a.z ? c0 : 0);
     const IO *Bp = static_cast<const IO *>(a.B) + group * N, *Cp = static_cast<const IO *>(a.C) + group * N;
 
-    float A2[KC][4], h[KC][4], sum[KC];
+    float2 A2[KC][2], h[KC][2];  // A in powers of two
+    float sum[KC];
+    auto load_state = [&](const float *p, size_t state, float2 (&v)[KC][2]) {
 #pragma unroll
-    for (int k = 0; k < KC; ++k) {
-        const float4 f = mine[k] < cols ? *reinterpret_cast<const float4 *>(a.A + (size_t)(c0 + mine[k]) * N + nl * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-        A2[k][0] = f.x, A2[k][1] = f.y, A2[k][2] = f.z, A2[k][3] = f.w;
-        sum[k] = 0.f;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) A2[k][n] *= 1.4426950408889634f, h[k][n] = 0.f;
-    }
-    auto load_state = [&](const float *p, size_t state) {
-#pragma unroll
-        for (int k = 0; k < KC; ++k) {
-            const float4 f = p && mine[k] < cols ? *reinterpret_cast<const float4 *>(p + at(state, k)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            h[k][0] = f.x, h[k][1] = f.y, h[k][2] = f.z, h[k][3] = f.w;
+        for (int q = 0; q < KC; ++q) {
+            v[q][0] = v[q][1] = both(0.f);
+            if (p && mine(q)) ssm_load(p + at(state, q), v[q]);
         }
     };
     auto store_state = [&](float *p, size_t state) {
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
-            if (mine[k] < cols) *reinterpret_cast<float4 *>(p + at(state, k)) = make_float4(h[k][0], h[k][1], h[k][2], h[k][3]);
+        for (int q = 0; q < KC; ++q)
+            if (mine(q)) ssm_store(p + at(state, q), h[q]);
     };
+    load_state(a.A, 0, A2);
+#pragma unroll
+    for (int q = 0; q < KC; ++q) {
+        sum[q] = 0.f;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) A2[q][p] = __fmul2_rn(A2[q][p], both(1.4426950408889634f)), h[q][p] = both(0.f);
+    }
     if (!LOCAL && span > 0) {
-        const SsmToken first = ssm_token(a, lo, false);
-        if (first.row >= 0 && first.begin < lo) {  // a row from an earlier stretch: its states joined
-            int j = first.begin / a.span;
-            load_state(a.local, j);
+        const SsmToken head = ssm_token(a, lo, false);
+        if (head.row >= 0 && head.begin < lo) {  // a row from an earlier stretch: its states joined
+            int j = head.begin / a.span;
+            load_state(a.local, j, h);
             for (++j; j < span; ++j) {
-                float before[KC][4];
+                float2 own[KC][2];
+                load_state(a.local, j, own);
 #pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    const float total = mine[k] < cols ? a.sums[(size_t)j * a.D_ + c0 + mine[k]] : 0.f;
+                for (int q = 0; q < KC; ++q) {
+                    const float total = mine(q) ? a.sums[(size_t)j * a.D_ + c0 + first + q * LC] : 0.f;
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) before[k][n] = exp2_fast(A2[k][n] * total) * h[k][n];
+                    for (int p = 0; p < 2; ++p) h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(total))), h[q][p], own[q][p]);
                 }
-                load_state(a.local, j);
-#pragma unroll
-                for (int k = 0; k < KC; ++k)
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) h[k][n] += before[k][n];
             }
         }
     }
-    // the vector of channels that this thread brings in and out, and its first token of a tile
-    const int vec = (tid % (CB / VE)) * VE, vec_token = tid / (CB / VE);
-    constexpr int kTokenStep = kSsmThreads / (CB / VE);
-    float bias[VE], skip[VE];
-#pragma unroll
-    for (int e = 0; e < VE; ++e) {
-        bias[e] = a.bias && vec < cols ? a.bias[c0 + vec + e] : 0.f;
-        skip[e] = a.D && vec < cols ? a.D[c0 + vec + e] : 0.f;
-    }
+    // the two channels that this thread brings in and out, and its first token of a tile
+    const int col = (tid % (CB / 2)) * 2, col_token = tid / (CB / 2);
+    constexpr int kTokenStep = kSsmThreads / (CB / 2);
+    const float2 bias = a.bias && col < cols ? load2(a.bias + c0 + col) : both(0.f), skip = a.D && col < cols ? load2(a.D + c0 + col) : both(0.f);
     auto fetch = [&](int t, int stage) {
         typename F::Raw &r = s.raw[stage];
-        ssm_stage(r.x, x, a.x_stride, t, TT, from, hi, CB, cols, kSsmThreads);
-        ssm_stage(r.dt, dt, a.dt_stride, t, TT, from, hi, CB, cols, kSsmThreads);
-        ssm_stage(r.B, Bp, a.B_stride, t, TT, from, hi, N, N, kSsmThreads);
-        if (!LOCAL) {
-            if (a.z) ssm_stage(r.z, z, a.z_stride, t, TT, from, hi, CB, cols, kSsmThreads);
-            ssm_stage(r.C, Cp, a.C_stride, t, TT, from, hi, N, N, kSsmThreads);
-        }
+        auto parts = [&](auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            ssm_stage<ALL, TT, CB>(r.x, x, a.x_stride, t, from, hi, cols);
+            ssm_stage<ALL, TT, CB>(r.dt, dt, a.dt_stride, t, from, hi, cols);
+            ssm_stage<ALL, TT, N>(r.B, Bp, a.B_stride, t, from, hi, N);
+            if (!LOCAL) {
+                if (a.z) ssm_stage<ALL, TT, CB>(r.z, z, a.z_stride, t, from, hi, cols);
+                ssm_stage<ALL, TT, N>(r.C, Cp, a.C_stride, t, from, hi, N);
+            }
+        };
+        if (t + TT <= hi && cols == CB) parts(std::true_type{});
+        else parts(std::false_type{});
         cp_async_commit();
     };
     fetch(from, 0);
     int stage = 0;
     for (int t = from; t < hi; t += TT, stage ^= 1) {
-        const typename F::Raw &r = s.raw[stage];
+        typename F::Raw &r = s.raw[stage];
         if (warp == 0) {
             SsmToken k{-1, -1, 0, 0};
             if (t + lane < hi) k = ssm_token(a, t + lane, !LOCAL && blockIdx.x == 0);
@@ -145,97 +141,86 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
         if (t + TT < hi) fetch(t + TT, stage ^ 1);
         const unsigned there = s.there, begins = s.begins, ends = s.ends;
 #pragma unroll
-        for (int q = 0; q < TT / kTokenStep; ++q) {
-            const int k = vec_token + q * kTokenStep;
-            const Pack<IO, VE> xv = pack_load<IO, VE>(r.x + k * CB + vec), dv = pack_load<IO, VE>(r.dt + k * CB + vec);
-            const bool ok = there >> k & 1;
-#pragma unroll
-            for (int e = 0; e < VE; e += 2) {
-                float d[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    d[f] = to_f32(dv.e[e + f]) + bias[e + f];
-                    if (a.softplus) d[f] = ssm_softplus(d[f]);
-                    if (!ok) d[f] = 0.f;
-                }
-                *reinterpret_cast<float4 *>(s.step + k * CB + vec + e) =
-                    make_float4(d[0], ok ? d[0] * to_f32(xv.e[e]) : 0.f, d[1], ok ? d[1] * to_f32(xv.e[e + 1]) : 0.f);
-            }
+        for (int i = 0; i < TT / kTokenStep; ++i) {
+            const int k = col_token + i * kTokenStep;
+            float2 d = __fadd2_rn(load2(r.dt + k * CB + col), bias), unused;
+            if (a.softplus) d = ssm_softplus(d, unused);
+            const float2 u = __fmul2_rn(d, load2(r.x + k * CB + col));
+            *reinterpret_cast<float4 *>(s.step + k * PB + col) = make_float4(d.x, u.x, d.y, u.y);
         }
-        for (int i = tid; i < TT * N; i += kSsmThreads) {  // (a skipped token may hold anything)
-            const bool ok = there >> (i / N) & 1;
-            s.B[i] = ok ? to_f32(r.B[i]) : 0.f;
-            if (!LOCAL) s.C[i] = ok ? to_f32(r.C[i]) : 0.f;
+        if (there != 0xffffffffu) {  // a skipped token may hold anything, and changes nothing
+#pragma unroll
+            for (int i = 0; i < TT / kTokenStep; ++i) {
+                const int k = col_token + i * kTokenStep;
+                if (!(there >> k & 1)) *reinterpret_cast<float4 *>(s.step + k * PB + col) = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            for (int i = tid; i < TT * N; i += kSsmThreads)
+                if (!(there >> (i / N) & 1)) r.B[i] = r.C[i] = from_f32<IO>(0.f);
         }
         __syncthreads();
-        for (int k0 = 0; k0 < min(TT, hi - t); k0 += 4) {
-            if (!LOCAL && a.kept && k0 % kSsmBlock == 0) store_state(a.kept, (size_t)(t + k0) / kSsmBlock);
+        // four tokens; MARKED: where rows may begin or end
+        auto four = [&](int k0, auto marked) {
+            constexpr bool MARKED = decltype(marked)::value;
             float y[4 * KC];
+            const float2 *step = s.step + k0 * PB + first;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int k = k0 + i;
-                if (begins >> k & 1) {
+                if (MARKED && (begins >> (k0 + i) & 1)) {
+                    const int k = k0 + i;
                     const bool old = a.S_in && !(a.fresh && a.fresh[s.row[k]]);
                     // another CTA may have written the pool's state of an open row already: the first pass kept it
-                    if (!LOCAL && a.front && (s.open >> k & 1)) load_state(a.front, span);
-                    else load_state(old ? a.S_in : nullptr, s.state[k]);
+                    if (!LOCAL && a.front && (s.open >> k & 1)) load_state(a.front, span, h);
+                    else load_state(old ? a.S_in : nullptr, s.state[k], h);
                     if (LOCAL && a.front) store_state(a.front, span);
                 }
-                const float4 Bv = *reinterpret_cast<const float4 *>(s.B + k * N + nl * 4);
-                const float b[4] = {Bv.x, Bv.y, Bv.z, Bv.w};
-                float c[4];
-                if (!LOCAL) {
-                    const float4 Cv = *reinterpret_cast<const float4 *>(s.C + k * N + nl * 4);
-                    c[0] = Cv.x, c[1] = Cv.y, c[2] = Cv.z, c[3] = Cv.w;
-                }
+                float2 b[2], c[2];
+                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+                if (!LOCAL) ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
-                    const float2 d = s.step[k * CB + mine[q]];
-                    float out = 0.f;
+                    const float2 d = step[i * PB + q * LC];
+                    float2 out = both(0.f);
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        h[q][n] = fmaf(exp2_fast(d.x * A2[q][n]), h[q][n], d.y * b[n]);
-                        if (!LOCAL) out = fmaf(c[n], h[q][n], out);
+                    for (int p = 0; p < 2; ++p) {
+                        h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d.x))), h[q][p], __fmul2_rn(b[p], both(d.y)));
+                        if (!LOCAL) out = p ? __ffma2_rn(c[p], h[q][p], out) : __fmul2_rn(c[p], h[q][p]);
                     }
                     if (LOCAL) sum[q] += d.x;
-                    else y[i * KC + q] = out;
+                    else y[i * KC + q] = out.x + out.y;
                 }
-                if (!LOCAL && a.S_out && (ends >> k & 1)) store_state(a.S_out, s.state[k]);
+                if (MARKED && !LOCAL && a.S_out && (ends >> (k0 + i) & 1)) store_state(a.S_out, s.state[k0 + i]);
             }
-            if (!LOCAL) {
-                const int first = lanes_reduce<4 * KC, LN>(y, lane);
+            if (!LOCAL) {  // the warp is done with these tokens' steps
+                const int v0 = lanes_reduce<4 * KC, LN>(y, lane);
 #pragma unroll
-                for (int j = 0; j < 4 * KC / LN; ++j) {
-                    const int v = first + j, i = v / KC, q = v % KC;
-                    s.y[(k0 + i) * CB + (warp * KC + q) * LC + cl] = y[j];
-                }
+                for (int j = 0; j < (4 * KC > LN ? 4 * KC / LN : 1); ++j) s.step[(k0 + (v0 + j) / KC) * PB + first + (v0 + j) % KC * LC].x = y[j];
             }
+        };
+        for (int k0 = 0; k0 < min(TT, hi - t); k0 += 4) {
+            if (!LOCAL && a.kept && k0 % kSsmBlock == 0) store_state(a.kept, (size_t)(t + k0) / kSsmBlock);
+            if ((begins | ends) >> k0 & 15) four(k0, std::true_type{});
+            else four(k0, std::false_type{});
         }
         __syncthreads();
         if (LOCAL) continue;
-        if (a.out && vec < cols) {
+        if (a.out && col < cols) {
+            const int here = min(TT, hi - t);
 #pragma unroll
-            for (int q = 0; q < TT / kTokenStep; ++q) {
-                const int k = vec_token + q * kTokenStep;
-                if (t + k >= hi) break;
-                IO *out = static_cast<IO *>(a.out) + (size_t)(t + k) * a.D_ + c0 + vec;
+            for (int i = 0; i < TT / kTokenStep; ++i) {
+                const int k = col_token + i * kTokenStep;
+                if (k >= here) break;
+                IO *out = static_cast<IO *>(a.out) + (size_t)(t + k) * a.D_ + c0 + col;
                 if (!(there >> k & 1)) {
-                    if (a.clear) pack_store(out, pack_zero<IO, VE>());
+                    if (a.clear) store2(out, both(0.f));
                     continue;
                 }
-                const Pack<IO, VE> xv = pack_load<IO, VE>(r.x + k * CB + vec);
-                Pack<IO, VE> zv, o;
-                if (a.z) zv = pack_load<IO, VE>(r.z + k * CB + vec);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    float v = fmaf(skip[e], to_f32(xv.e[e]), s.y[k * CB + vec + e]);
-                    if (a.z) {
-                        const float g = to_f32(zv.e[e]);
-                        v *= g * sigmoid(g);
-                    }
-                    o.e[e] = from_f32<IO>(v);
+                const float4 y = *reinterpret_cast<const float4 *>(s.step + k * PB + col);
+                float2 o = __ffma2_rn(skip, load2(r.x + k * CB + col), make_float2(y.x, y.z));
+                if (a.z) {
+                    const float2 g = load2(r.z + k * CB + col);
+                    o = __fmul2_rn(o, make_float2(g.x * sigmoid(g.x), g.y * sigmoid(g.y)));
                 }
-                pack_store(out, o);
+                store2(out, o);
             }
         }
     }
@@ -243,63 +228,86 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
         store_state(a.local, span);
         if (nl == 0)
 #pragma unroll
-            for (int k = 0; k < KC; ++k)
-                if (mine[k] < cols) a.sums[(size_t)span * a.D_ + c0 + mine[k]] = sum[k];
+            for (int q = 0; q < KC; ++q)
+                if (mine(q)) a.sums[(size_t)span * a.D_ + c0 + first + q * LC] = sum[q];
     }
 }
 
-// One token per row.  Bound by HBM, the states' read and write.  A lane keeps its channel's A for all of its rows, four of
-// which are in flight.
+// One token per row.  Bound by HBM, the states' read and write.  A lane holds eight states of a channel (32 bytes, one access),
+// so that step size and gate are worked out by d_state / 8 lanes, and keeps its channel's A for all of its rows, two of which are in
+// flight.
+__device__ __forceinline__ void ssm_load8(const float *p, float2 (&v)[4]) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y), "=f"(v[2].x), "=f"(v[2].y), "=f"(v[3].x), "=f"(v[3].y) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void ssm_store8(float *p, const float2 (&v)[4]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y) : "memory");
+}
+
 template <typename IO, int N>
 __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs a, int col_blocks, int run) {
-    constexpr int LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels, U = 4;
+    constexpr int LN = N / 8, LC = 32 / LN, U = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nl = lane & (LN - 1), cl = lane / LN;
     const int c = ((int)(blockIdx.x % col_blocks) * kSsmWarps + warp) * LC + cl;
     const bool live = c < a.D_;
     const int cc = live ? c : 0, group = cc / (a.D_ / a.G);
     const long long first = (long long)(blockIdx.x / col_blocks) * run;
-    const float4 Af = *reinterpret_cast<const float4 *>(a.A + (size_t)cc * N + nl * 4);
-    const float A2[4] = {Af.x * 1.4426950408889634f, Af.y * 1.4426950408889634f, Af.z * 1.4426950408889634f, Af.w * 1.4426950408889634f};
-    const float bias = a.bias ? a.bias[cc] : 0.f, skip = a.D ? a.D[cc] : 0.f;
     const int end = (int)min((long long)a.total_rows, first + run);
+    const IO *x = static_cast<const IO *>(a.x) + cc, *dt = static_cast<const IO *>(a.dt) + cc, *z = static_cast<const IO *>(a.z) + (a.z ? cc : 0);
+    const IO *B = static_cast<const IO *>(a.B) + group * N + nl * 8, *C = static_cast<const IO *>(a.C) + group * N + nl * 8;
+    const size_t at = (size_t)cc * N + nl * 8, pitch = (size_t)a.D_ * N;
+    float2 A2[4];
+    float bias = 0.f, skip = 0.f;
     for (int row = (int)first; row < end; row += U) {
-        float4 h[U];
-        float b[U][4], cv[U][4], x[U], d[U], z[U];
+        float2 h[U][4];
+        Pack<IO, 8> b[U], cv[U];
+        IO xv[U], d[U], zv[U];
         int slot[U];
+        step_slots(a.slots, row, end, a.num_slots, a.status, slot);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            slot[u] = -1;
-            if (row + u < end && !resolve_slot(a.slots, row + u, a.num_slots, a.status, threadIdx.x, slot[u])) slot[u] = -1;
+            if (slot[u] < 0) continue;
+            const long long t = row + u;
+            ssm_load8(a.S_in + slot[u] * pitch + at, h[u]);
+            xv[u] = x[t * a.x_stride], d[u] = dt[t * a.dt_stride], zv[u] = a.z ? z[t * a.z_stride] : xv[u];
+#pragma unroll
+            for (int e = 0; e < 8; e += 16 / sizeof(IO)) {
+                *reinterpret_cast<uint4 *>(b[u].e + e) = *reinterpret_cast<const uint4 *>(B + t * a.B_stride + e);
+                *reinterpret_cast<uint4 *>(cv[u].e + e) = *reinterpret_cast<const uint4 *>(C + t * a.C_stride + e);
+            }
+        }
+        if (row == (int)first) {
+            ssm_load8(a.A + at, A2);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) A2[p] = __fmul2_rn(A2[p], both(1.4426950408889634f));
+            if (a.bias) bias = a.bias[cc];
+            if (a.D) skip = a.D[cc];
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (slot[u] < 0) continue;
-            const size_t t = row + u;
-            h[u] = *reinterpret_cast<const float4 *>(a.S_in + ((size_t)slot[u] * a.D_ + cc) * N + nl * 4);
-            load_vec<IO, 4>(static_cast<const IO *>(a.B) + t * a.B_stride + group * N + nl * 4, b[u]);
-            load_vec<IO, 4>(static_cast<const IO *>(a.C) + t * a.C_stride + group * N + nl * 4, cv[u]);
-            x[u] = to_f32(static_cast<const IO *>(a.x)[t * a.x_stride + cc]);
-            d[u] = to_f32(static_cast<const IO *>(a.dt)[t * a.dt_stride + cc]) + bias;
-            z[u] = a.z ? to_f32(static_cast<const IO *>(a.z)[t * a.z_stride + cc]) : 0.f;
-        }
+            const float v = to_f32(d[u]) + bias, xf = to_f32(xv[u]);
+            float2 unused, y = both(0.f);
+            const float delta = a.softplus ? ssm_softplus(both(v), unused).x : v, in = delta * xf;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (slot[u] < 0) continue;
-            const float delta = a.softplus ? ssm_softplus(d[u]) : d[u], dx = delta * x[u];
-            float4 &s = h[u];
-            s.x = fmaf(exp2_fast(delta * A2[0]), s.x, dx * b[u][0]);
-            s.y = fmaf(exp2_fast(delta * A2[1]), s.y, dx * b[u][1]);
-            s.z = fmaf(exp2_fast(delta * A2[2]), s.z, dx * b[u][2]);
-            s.w = fmaf(exp2_fast(delta * A2[3]), s.w, dx * b[u][3]);
-            float y = s.x * cv[u][0] + s.y * cv[u][1] + s.z * cv[u][2] + s.w * cv[u][3];
+            for (int p = 0; p < 4; ++p) {
+                const float2 bp = load2(b[u].e + 2 * p), cp = load2(cv[u].e + 2 * p);
+                h[u][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[p], both(delta))), h[u][p], __fmul2_rn(bp, both(in)));
+                y = __ffma2_rn(cp, h[u][p], y);
+            }
+            float o = y.x + y.y;
 #pragma unroll
-            for (int o = LN / 2; o > 0; o >>= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
+            for (int k = LN / 2; k > 0; k >>= 1) o += __shfl_xor_sync(0xffffffffu, o, k);
             if (!live) continue;
-            *reinterpret_cast<float4 *>(a.S_out + ((size_t)slot[u] * a.D_ + cc) * N + nl * 4) = s;
+            ssm_store8(a.S_out + slot[u] * pitch + at, h[u]);
             if (nl == 0) {
-                y = fmaf(skip, x[u], y);
-                if (a.z) y *= z[u] * sigmoid(z[u]);
-                static_cast<IO *>(a.out)[(size_t)(row + u) * a.D_ + cc] = from_f32<IO>(y);
+                o = fmaf(skip, xf, o);
+                if (a.z) {
+                    const float g = to_f32(zv[u]);
+                    o *= g * sigmoid(g);
+                }
+                static_cast<IO *>(a.out)[(size_t)(row + u) * a.D_ + cc] = from_f32<IO>(o);
             }
         }
     }

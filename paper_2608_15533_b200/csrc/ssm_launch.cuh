@@ -13,16 +13,15 @@ constexpr int kSsmSpanMin = 256;  // tokens of a stretch at least
 
 // Channels of a CTA: forward, backward.
 inline int ssm_cols(const deltalog_ssm_desc *d, bool backward) {
-    if (!backward) return d->d_state == 8 ? 64 : 32;
-    return d->d_state == 8 ? 128 : d->d_state == 16 ? 64 : d->d_state == 32 ? 32 : 16;
+    return d->d_state == 8 ? 128 : d->d_state == 16 ? 64 : d->d_state == 32 || !backward ? 32 : 16;
 }
 inline int ssm_blocks(const deltalog_ssm_desc *d, bool backward) { return (int)ssm_ceil(d->channels / d->groups, ssm_cols(d, backward)); }
 
-// Stretches that the tokens are cut into at most, for CTAs of `want` in all: a cut makes the row that crosses it run twice
-// behind its last border, so there are no more than fill the SMs.  (148 SMs whatever the device: workspaces depend on it.)
+// Stretches that the tokens are cut into at most: as many as one wave of CTAs has (a cut makes the row that crosses it run twice
+// behind its last border).  (148 SMs whatever the device: workspaces depend on it.)
 inline int ssm_most_spans(const deltalog_ssm_desc *d, bool backward) {
-    const long long blocks = (long long)ssm_blocks(d, backward) * d->groups, want = backward ? 148 * 3 : 148 * 6;
-    return (int)(blocks >= want ? 1 : ssm_ceil(want, blocks));
+    const int blocks = ssm_blocks(d, backward) * d->groups, wave = 148 * (backward || d->d_state == 64 ? 3 : 5);
+    return blocks >= wave ? 1 : wave / blocks;
 }
 struct SsmCut { int span, spans; };
 inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {

@@ -26,15 +26,20 @@ NORM_L2, NORM_RMS, NORM_NONE = 0, 1, 2
 class _Described:
     """A descriptor whose C struct is made once per set of values; the second form asks for zeros in unwritten rows."""
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_c", None)
+        object.__setattr__(self, name, value)
+
+    def _forms(self):
+        made = self.__dict__.get("_c")
+        if made is None:
+            second = self._struct(*self._key())
+            second.hints |= HINT_ZERO_UNWRITTEN
+            made = self.__dict__["_c"] = (self._struct(*self._key()), second)
+        return made
+
     def c_struct(self, zero: bool = False):
-        key = self._key()
-        cached = self.__dict__.get("_c")
-        if cached is None or cached[0] != key:
-            second = self._struct(*key)
-            if hasattr(second, "hints"):
-                second.hints |= HINT_ZERO_UNWRITTEN
-            cached = self.__dict__["_c"] = (key, self._struct(*key), second)
-        return cached[2 if zero else 1]
+        return self._forms()[1 if zero else 0]
 
 
 @dataclass
@@ -83,15 +88,13 @@ class NormDesc(_Described):
     rot: int = 0
     interleaved: bool = False
     q_scale: float = 1.0
-    _struct = _NormDesc
 
-    def _key(self):
-        return self.H_q, self.H_k, self.d, self.io_dtype, self.norm, self.rot, int(self.interleaved), getattr(self, "_table_rows", 0), self.eps, self.q_scale
-
-    def with_table(self, rows: int):
-        if self.__dict__.get("_table_rows", 0) != rows:
-            self.__dict__["_table_rows"] = rows
-        return self.c_struct()
+    def c_struct(self, table_rows: int = 0):
+        made = self.__dict__.get("_c")
+        if made is None or made[0] != table_rows:
+            made = self.__dict__["_c"] = (table_rows, _NormDesc(self.H_q, self.H_k, self.d, self.io_dtype, self.norm, self.rot, int(self.interleaved),
+                                                                table_rows, self.eps, self.q_scale))
+        return made[1]
 
 
 class _Pool:
@@ -106,11 +109,12 @@ class _Pool:
         self.status = torch.zeros(1, dtype=torch.int32, device=tensor.device)
         self._tensor, self._shape = tensor, shape
 
-    def _fits(self, desc, name, shape, device):
-        if self._shape != shape or self._tensor.dtype is not self._dtype(desc):
-            raise ValueError(f"{name}: its tensor was laid out for another descriptor")
+    def _fits(self, desc, device):
+        """Addresses of the pool and of the status word for a call with this descriptor."""
+        if desc is not self.desc and (self._shape != self._want(desc) or self._tensor.dtype is not self._dtype(desc)):
+            raise ValueError("state: its tensor was laid out for another descriptor")
         if self._tensor.device != device:
-            raise ValueError(f"{name}: expected a tensor on {device}, got one on {self._tensor.device}")
+            raise ValueError(f"state: expected a tensor on {device}, got one on {self._tensor.device}")
         return self._tensor.data_ptr(), self.status.data_ptr()
 
 
@@ -148,33 +152,54 @@ class SsmState(_Pool):
         return torch.float32
 
 
-def _tokens(name: str, t, rows: Optional[int], width: Tuple[int, ...], dtype, device) -> Tuple[int, int]:
-    """Pointer and token stride of a tensor [rows, *width] whose tokens are dense."""
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name}: a tensor is needed")
-    shape = t.shape
-    if t.dtype is not dtype or t.device != device or len(shape) != 1 + len(width) or shape[1:] != width or (rows is not None and shape[0] != rows):
-        raise ValueError(f"{name}: expected {dtype} {('tokens' if rows is None else rows, *width)} on {device}, got {t.dtype} {tuple(shape)} on {t.device}")
-    size = t.numel() // shape[0] if shape[0] else 1
+def _tokens(name: str, t, shape: Tuple[int, ...], dtype, device) -> Tuple[int, int]:
+    """Pointer and token stride of a tensor [tokens, width] or [tokens, heads, width] of this shape whose tokens are dense."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == device and t.shape == shape):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name}: a tensor is needed")
+        raise ValueError(f"{name}: expected {dtype} {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    width = shape[-1]
+    dense = width if len(shape) == 2 else shape[1] * width
     if t.is_contiguous():
-        return t.data_ptr() or 16, size if shape[0] else _product(width)
-    strides, dense = t.stride(), 1
-    for s, w in zip(reversed(strides[1:]), reversed(width)):
-        if s != dense and w != 1:
-            raise ValueError(f"{name}: a token's values have to be dense, the strides are {strides}")
-        dense *= w
-    stride = strides[0] if shape[0] > 1 else dense
-    align = 16 // t.element_size()
-    if stride < dense or stride % align or t.data_ptr() % 16:
+        return t.data_ptr() or 16, dense
+    strides = t.stride()
+    if (strides[-1] != 1 and width != 1) or (len(shape) == 3 and strides[1] != width and shape[1] != 1):
+        raise ValueError(f"{name}: a token's values have to be dense, the strides are {strides}")
+    stride, at = strides[0] if shape[0] > 1 else dense, t.data_ptr()
+    if stride < dense or stride * t.element_size() % 16 or at % 16:
         raise ValueError(f"{name}: the tokens have to start on 16-byte boundaries and not overlap, the strides are {strides}")
-    return t.data_ptr(), stride
+    return at, stride
 
 
-def _product(width) -> int:
-    n = 1
-    for w in width:
-        n *= w
-    return n
+def _rows(name: str, t) -> int:
+    if not isinstance(t, torch.Tensor) or t.dim() == 0:
+        raise ValueError(f"{name}: a tensor of tokens is needed")
+    return t.shape[0]
+
+
+class _Here:
+    """A stream handle as a context: nothing to switch."""
+
+    __slots__ = ("handle",)
+
+    def __init__(self, handle):
+        self.handle = handle
+
+    def __enter__(self):
+        return self.handle
+
+    def __exit__(self, *exc):
+        pass
+
+
+def _stream_of(device, stream):
+    """The context of a call: the current stream as it is, if the device is current and no other stream is asked for; ``_on``
+    otherwise."""
+    if device.type != "cuda":
+        _gpu(device)
+    if stream is None and torch._C._cuda_getDevice() == device.index:
+        return _Here(torch._C._cuda_getCurrentRawStream(device.index))
+    return _on(device, stream)
 
 
 def _param(name: str, t, shape, device) -> Optional[int]:
@@ -195,7 +220,7 @@ def _new_out(out, rows: int, shape, dtype, device, plan: Plan) -> Tuple[torch.Te
 
 
 def _plan_rows(name: str, t, plan: Plan) -> int:
-    rows = t.shape[0] if isinstance(t, torch.Tensor) and t.dim() > 0 else 0
+    rows = _rows(name, t)
     if rows < plan.max_tokens:
         raise ValueError(f"{name}: the plan reaches over {plan.max_tokens} tokens, the tensor has {rows}")
     return rows
@@ -246,15 +271,14 @@ def conv_step(desc: ConvDesc, state: ConvState, x, weight, bias=None, slot_idx=N
     Padding rows (negative slots) and rows outside the pool stay as they were in the caller's ``out`` and are not defined in a
     tensor that the call makes."""
     dev, io, C = state.window.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
-    B = x.shape[0] if isinstance(x, torch.Tensor) else 0
-    p_x, stride = _tokens("x", x, None, (C,), io, dev)
+    B = _rows("x", x)
+    p_x, stride = _tokens("x", x, (B, C), io, dev)
     p_w, p_b = _want("weight", weight, (C, desc.width), torch.float32, dev), _param("bias", bias, (C,), dev)
     p_slots = _slot_list(slot_idx, B, desc.num_slots, dev)
-    p_win, p_status = state._fits(desc, "state", ConvState._want(desc), dev)
+    p_win, p_status = state._fits(desc, dev)
     if out is not None:
         _want("out", out, (B, C), io, dev)
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         if out is None:
             out = torch.empty((B, C), dtype=io, device=dev)
         rc = load_library().deltalog_conv_step(ctypes.byref(desc.c_struct()), p_win, p_x, stride, p_w, p_b, p_slots, B, out.data_ptr() or 16, p_status, handle)
@@ -268,12 +292,11 @@ def conv_prefill(desc: ConvDesc, state: ConvState, plan: Plan, x, weight, bias=N
     the call does not write: as in ``prefill``."""
     dev, io, C = plan.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
     rows = _plan_rows("x", x, plan)
-    p_x, stride = _tokens("x", x, None, (C,), io, dev)
+    p_x, stride = _tokens("x", x, (rows, C), io, dev)
     p_w, p_b = _want("weight", weight, (C, desc.width), torch.float32, dev), _param("bias", bias, (C,), dev)
     p_fresh = None if fresh is None else _want("fresh", fresh, (plan.n,), torch.int32, dev)
-    p_win, p_status = state._fits(desc, "state", ConvState._want(desc), dev)
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    p_win, p_status = state._fits(desc, dev)
+    with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, C), io, dev, plan)
         rc = load_library().deltalog_conv_prefill(ctypes.byref(desc.c_struct(zero)), p_win, ctypes.byref(plan.c_struct()), p_x, stride, p_w, p_b, p_fresh,
                                                   out.data_ptr() or 16, p_status, handle)
@@ -286,11 +309,10 @@ def conv_forward(desc: ConvDesc, plan: Plan, x, weight, bias=None, init=None, ou
     ``final [n, width - 1, channels]``, the rows' last inputs."""
     dev, io, C = plan.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
     rows, window = _plan_rows("x", x, plan), (plan.n, desc.width - 1, C)
-    p_x, stride = _tokens("x", x, None, (C,), io, dev)
+    p_x, stride = _tokens("x", x, (rows, C), io, dev)
     p_w, p_b = _want("weight", weight, (C, desc.width), torch.float32, dev), _param("bias", bias, (C,), dev)
     p_init = None if init is None else _want("init", init, window, io, dev)
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, C), io, dev, plan)
         final = torch.empty(window, dtype=io, device=dev)
         rc = load_library().deltalog_conv_forward(ctypes.byref(desc.c_struct(zero)), ctypes.byref(plan.c_struct()), p_init, p_x, stride, p_w, p_b,
@@ -321,13 +343,12 @@ def conv_backward(desc: ConvDesc, plan: Plan, x, weight, bias, dout, init=None, 
     """``deltalog_conv_backward``: gradients of ``conv_forward`` for ``dout`` and ``dfinal`` (zeros without it)."""
     dev, io, C = plan.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
     rows, window = _plan_rows("x", x, plan), (plan.n, desc.width - 1, C)
-    p_x, stride = _tokens("x", x, None, (C,), io, dev)
+    p_x, stride = _tokens("x", x, (rows, C), io, dev)
     p_w, p_b = _want("weight", weight, (C, desc.width), torch.float32, dev), _param("bias", bias, (C,), dev)
     p_init = None if init is None else _want("init", init, window, io, dev)
     p_dfinal = None if dfinal is None else _want("dfinal", dfinal, window, io, dev)
     p_dout = _want("dout", dout, (rows, C), io, dev) or 16
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         ws = workspace if workspace is not None else conv_workspace(desc, rows, dev)
         ws = _want_workspace(ws, 0, dev)
         make = torch.zeros if plan.n == 0 else torch.empty  # without rows nothing is launched
@@ -382,30 +403,29 @@ def ssm_workspace(desc: SsmDesc, n: int, max_tokens: int, train: bool = False, d
     return torch.empty(bytes_, dtype=torch.uint8, device=device)
 
 
-def _ssm_inputs(desc: SsmDesc, rows: Optional[int], x, dt, A, B, C, D, z, dt_bias, dev) -> Tuple[_SsmInputs, int]:
+def _ssm_inputs(desc: SsmDesc, rows: int, x, dt, A, B, C, D, z, dt_bias, dev) -> _SsmInputs:
     io, ch = _DT_TO_TORCH[desc.io_dtype], desc.channels
-    p_x, s_x = _tokens("x", x, rows, (ch,), io, dev)
-    rows = x.shape[0]
-    states = (desc.groups, desc.d_state)
-    p_dt, s_dt = _tokens("dt", dt, rows, (ch,), io, dev)
-    p_B, s_B = _tokens("B", B, rows, states, io, dev)
-    p_C, s_C = _tokens("C", C, rows, states, io, dev)
-    p_z, s_z = (None, 0) if z is None else _tokens("z", z, rows, (ch,), io, dev)
+    tokens, states = (rows, ch), (rows, desc.groups, desc.d_state)
+    p_x, s_x = _tokens("x", x, tokens, io, dev)
+    p_dt, s_dt = _tokens("dt", dt, tokens, io, dev)
+    p_B, s_B = _tokens("B", B, states, io, dev)
+    p_C, s_C = _tokens("C", C, states, io, dev)
+    p_z, s_z = (None, 0) if z is None else _tokens("z", z, tokens, io, dev)
     p_A = _want("A", A, (ch, desc.d_state), torch.float32, dev)
-    return _SsmInputs(p_x, p_dt, p_B, p_C, p_z, s_x, s_dt, s_B, s_C, s_z, p_A, _param("D", D, (ch,), dev), _param("dt_bias", dt_bias, (ch,), dev)), rows
+    return _SsmInputs(p_x, p_dt, p_B, p_C, p_z, s_x, s_dt, s_B, s_C, s_z, p_A, _param("D", D, (ch,), dev), _param("dt_bias", dt_bias, (ch,), dev))
 
 
 def ssm_step(desc: SsmDesc, state: SsmState, x, dt, A, B, C, D=None, z=None, dt_bias=None, slot_idx=None, out=None, stream=None) -> torch.Tensor:
     """``deltalog_ssm_step``: one token per row; row b advances state ``slot_idx[b]`` (b without a list).  Rows that the call
     skips: as in ``conv_step``."""
     dev, io = state.S.device, _DT_TO_TORCH[desc.io_dtype]
-    inputs, rows = _ssm_inputs(desc, None, x, dt, A, B, C, D, z, dt_bias, dev)
+    rows = _rows("x", x)
+    inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     p_slots = _slot_list(slot_idx, rows, desc.num_slots, dev)
-    p_S, p_status = state._fits(desc, "state", SsmState._want(desc), dev)
+    p_S, p_status = state._fits(desc, dev)
     if out is not None:
         _want("out", out, (rows, desc.channels), io, dev)
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         if out is None:
             out = torch.empty((rows, desc.channels), dtype=io, device=dev)
         rc = load_library().deltalog_ssm_step(ctypes.byref(desc.c_struct()), p_S, ctypes.byref(inputs), p_slots, rows, out.data_ptr() or 16, p_status, handle)
@@ -418,12 +438,11 @@ def ssm_prefill(desc: SsmDesc, state: SsmState, plan: Plan, x, dt, A, B, C, D=No
     """``deltalog_ssm_prefill``: the rows of ``plan.scan_slots`` run their tokens through their slots' states; returns ``out
     [tokens, channels]``.  ``fresh`` and rows that the call does not write: as in ``prefill``."""
     dev, io = plan.device, _DT_TO_TORCH[desc.io_dtype]
-    _plan_rows("x", x, plan)
-    inputs, rows = _ssm_inputs(desc, None, x, dt, A, B, C, D, z, dt_bias, dev)
+    rows = _plan_rows("x", x, plan)
+    inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     p_fresh = None if fresh is None else _want("fresh", fresh, (plan.n,), torch.int32, dev)
-    p_S, p_status = state._fits(desc, "state", SsmState._want(desc), dev)
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    p_S, p_status = state._fits(desc, dev)
+    with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, desc.channels), io, dev, plan)
         ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
         rc = load_library().deltalog_ssm_prefill(ctypes.byref(desc.c_struct(zero)), p_S, ctypes.byref(plan.c_struct()), ctypes.byref(inputs), p_fresh,
@@ -438,14 +457,13 @@ def ssm_forward(desc: SsmDesc, plan: Plan, x, dt, A, B, C, D=None, z=None, dt_bi
     ``S_final [n, channels, d_state]`` fp32.  ``save``: the workspace (``ssm_workspace(.., train=True)``) keeps what
     ``ssm_backward(.., saved=True)`` reads."""
     dev, io = plan.device, _DT_TO_TORCH[desc.io_dtype]
-    _plan_rows("x", x, plan)
-    inputs, rows = _ssm_inputs(desc, None, x, dt, A, B, C, D, z, dt_bias, dev)
+    rows = _plan_rows("x", x, plan)
+    inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     s_shape = (plan.n, desc.channels, desc.d_state)
     p_init = None if S_init is None else _want("S_init", S_init, s_shape, torch.float32, dev)
     if save and workspace is None:
         raise ValueError("workspace: save=True needs the caller's workspace, which ssm_backward reads")
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, desc.channels), io, dev, plan)
         ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
         S_final = torch.empty(s_shape, dtype=torch.float32, device=dev)
@@ -475,16 +493,15 @@ def ssm_backward(desc: SsmDesc, plan: Plan, x, dt, A, B, C, D, z, dt_bias, dout,
     """``deltalog_ssm_backward``: gradients of ``ssm_forward`` for ``dout`` and ``dS_final`` (zeros without it).  ``saved``: the
     workspace is the one that ``ssm_forward(.., save=True)`` left for these inputs; otherwise its states are computed again."""
     dev, io, ch = plan.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
-    _plan_rows("x", x, plan)
-    inputs, rows = _ssm_inputs(desc, None, x, dt, A, B, C, D, z, dt_bias, dev)
+    rows = _plan_rows("x", x, plan)
+    inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     s_shape = (plan.n, ch, desc.d_state)
     p_init = None if S_init is None else _want("S_init", S_init, s_shape, torch.float32, dev)
     p_dS = None if dS_final is None else _want("dS_final", dS_final, s_shape, torch.float32, dev)
     p_dout = _want("dout", dout, (rows, ch), io, dev) or 16
     if saved and workspace is None:
         raise ValueError("workspace: saved=True needs the workspace of ssm_forward")
-    _gpu(dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, rows, train=True, device=dev)
         make = torch.zeros if plan.n == 0 else torch.empty  # without rows nothing is launched
 
@@ -540,13 +557,11 @@ def ssm(desc: SsmDesc, plan: Plan, x, dt, A, B, C, D=None, z=None, dt_bias=None,
 # ---- norm and rotation of heads -----------------------------------------------------------------------------------------
 def _norm_inputs(desc: NormDesc, q, k, w_q, w_k, cos, sin, positions):
     """The call's descriptor and the pointers of its inputs, checked; and the tokens."""
-    if not isinstance(q, torch.Tensor):
-        raise ValueError("q: a tensor is needed")
+    rows = _rows("q", q)
     dev, io, d = q.device, _DT_TO_TORCH[desc.io_dtype], desc.d
-    p_q, s_q = _tokens("q", q, None, (desc.H_q, d), io, dev)
-    rows = q.shape[0]
+    p_q, s_q = _tokens("q", q, (rows, desc.H_q, d), io, dev)
     if desc.H_k:
-        p_k, s_k = _tokens("k", k, rows, (desc.H_k, d), io, dev)
+        p_k, s_k = _tokens("k", k, (rows, desc.H_k, d), io, dev)
     elif k is not None:
         raise ValueError("k: the descriptor has no key heads")
     else:
@@ -562,10 +577,9 @@ def _norm_inputs(desc: NormDesc, q, k, w_q, w_k, cos, sin, positions):
         p_cos = _want("cos", cos, (None, desc.rot // 2), torch.float32, dev)
         p_sin = _want("sin", sin, tuple(cos.shape), torch.float32, dev)
         p_pos = _want("positions", positions, (rows,), torch.int32, dev) or 16
-        c = desc.with_table(cos.shape[0])
+        c = desc.c_struct(cos.shape[0])
     else:
         c = desc.c_struct()
-    _gpu(dev)
     return c, rows, (p_q, s_q, p_k, s_k, p_wq, p_wk, p_cos, p_sin, p_pos, rows)
 
 
@@ -580,7 +594,7 @@ def head_norm_forward(desc: NormDesc, q, k, w_q=None, w_k=None, cos=None, sin=No
     if out_k is not None:
         _want("out_k", out_k, (rows, desc.H_k, d), io, dev)
     p_status = None if status is None else _want("status", status, (1,), torch.int32, dev)
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         if out_q is None:
             out_q = torch.empty((rows, desc.H_q, d), dtype=io, device=dev)
         if out_k is None and desc.H_k:
@@ -607,7 +621,7 @@ def head_norm_backward(desc: NormDesc, q, k, w_q, w_k, cos, sin, positions, dout
     dev, io, d = q.device, q.dtype, desc.d
     p_dq = _want("dout_q", dout_q, (rows, desc.H_q, d), io, dev) or 16
     p_dk = (_want("dout_k", dout_k, (rows, desc.H_k, d), io, dev) or 16) if desc.H_k else None
-    with _on(dev, stream) as handle:
+    with _stream_of(dev, stream) as handle:
         lib = load_library()
         if workspace is None:
             bytes_ = lib.deltalog_head_norm_workspace_bytes(ctypes.byref(c), rows) if w_q is not None else 0
@@ -653,7 +667,7 @@ def head_norm(desc: NormDesc, q, k, w_q=None, w_k=None, cos=None, sin=None, posi
     _no_tangent("head_norm", tensors + (cos, sin))
     if any(isinstance(t, torch.Tensor) and t.requires_grad for t in (cos, sin)):
         raise ValueError("cos, sin: the rotation's tables have no gradient")
-    _norm_inputs(desc, q, k, w_q, w_k, cos, sin, positions)
     if _differentiable(tensors):
+        _norm_inputs(desc, q, k, w_q, w_k, cos, sin, positions)
         return _HeadNorm.apply(desc, q, k, w_q, w_k, cos, sin, positions)
     return head_norm_forward(desc, q, k, w_q, w_k, cos, sin, positions)
