@@ -40,59 +40,60 @@ __device__ __forceinline__ int conv_slot(const ConvArgs &a, int row, bool tell) 
     return -1;
 }
 
-template <int W, int V>
-__device__ __forceinline__ void conv_weights(const ConvArgs &a, int c, float (&w)[W][V], float (&b)[V]) {
-    // [channels, W]: V * W consecutive floats
-    float flat[W * V];
-#pragma unroll
-    for (int i = 0; i < W * V / 4; ++i) {
-        const float4 f = __ldg(reinterpret_cast<const float4 *>(a.w + (size_t)c * W) + i);
-        flat[4 * i] = f.x, flat[4 * i + 1] = f.y, flat[4 * i + 2] = f.z, flat[4 * i + 3] = f.w;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        b[v] = a.bias ? __ldg(a.bias + c + v) : 0.f;
-#pragma unroll
-        for (int j = 0; j < W; ++j) w[j][v] = flat[v * W + j];
-    }
+// A lane's four channels as two pairs, for the packed arithmetic.
+struct Quad { float2 a, b; };
+__device__ __forceinline__ Quad quad(float4 f) { return {make_float2(f.x, f.y), make_float2(f.z, f.w)}; }
+__device__ __forceinline__ Quad quad_zero() { return {both(0.f), both(0.f)}; }
+template <typename IO>
+__device__ __forceinline__ Quad quad(const Pack<IO, kConvVec> &v) { return {load2(v.e), load2(v.e + 2)}; }
+__device__ __forceinline__ Quad quad_fma(const Quad &x, const Quad &y, const Quad &z) { return {__ffma2_rn(x.a, y.a, z.a), __ffma2_rn(x.b, y.b, z.b)}; }
+template <typename IO>
+__device__ __forceinline__ Pack<IO, kConvVec> quad_round(const Quad &q) {
+    Pack<IO, kConvVec> v;
+    store2(v.e, q.a), store2(v.e + 2, q.b);
+    return v;
 }
 
-// pre-activations from the window `p` (p[0] the oldest input): as it is in memory, or widened
-template <int W, int V>
-__device__ __forceinline__ void conv_pre(const float (&p)[W][V], const float (&w)[W][V], const float (&b)[V], float (&pre)[V]) {
+// Weights [channels, W]: 4 W consecutive floats.
+template <int W>
+__device__ __forceinline__ void conv_weights(const ConvArgs &a, int c, Quad (&w)[W], Quad &b) {
+    float f[W * kConvVec];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        pre[v] = b[v];
-#pragma unroll
-        for (int j = 0; j < W; ++j) pre[v] = fmaf(w[j][v], p[j][v], pre[v]);
+    for (int i = 0; i < W; ++i) {
+        const float4 v = __ldg(reinterpret_cast<const float4 *>(a.w + (size_t)c * W) + i);
+        f[4 * i] = v.x, f[4 * i + 1] = v.y, f[4 * i + 2] = v.z, f[4 * i + 3] = v.w;
     }
+    b = a.bias ? quad(__ldg(reinterpret_cast<const float4 *>(a.bias + c))) : quad_zero();
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j] = {make_float2(f[j], f[W + j]), make_float2(f[2 * W + j], f[3 * W + j])};
 }
-template <typename IO, int V>
-__device__ __forceinline__ void conv_floats(const Pack<IO, V> &v, float (&f)[V]) {
+
+// Pre-activations from the window p (p[0] the oldest input).
+template <int W>
+__device__ __forceinline__ Quad conv_pre(const Quad (&p)[W], const Quad (&w)[W], const Quad &b) {
+    Quad r = b;
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_f32(v.e[i]);
+    for (int j = 0; j < W; ++j) r = quad_fma(w[j], p[j], r);
+    return r;
 }
-template <typename IO, int W, int V>
-__device__ __forceinline__ void conv_pre(const Pack<IO, V> (&p)[W], const float (&w)[W][V], const float (&b)[V], float (&pre)[V]) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        pre[v] = b[v];
-#pragma unroll
-        for (int j = 0; j < W; ++j) pre[v] = fmaf(w[j][v], to_f32(p[j].e[v]), pre[v]);
+template <typename IO>
+__device__ __forceinline__ Pack<IO, kConvVec> conv_act(Quad r, bool silu) {
+    if (silu) {
+        r.a = __fmul2_rn(r.a, make_float2(sigmoid(r.a.x), sigmoid(r.a.y)));
+        r.b = __fmul2_rn(r.b, make_float2(sigmoid(r.b.x), sigmoid(r.b.y)));
     }
+    return quad_round<IO>(r);
 }
-template <typename IO, int V>
-__device__ __forceinline__ Pack<IO, V> conv_act(float (&pre)[V], bool silu) {
+template <int W>
+__device__ __forceinline__ void conv_shift(Quad (&p)[W]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (silu) pre[v] *= sigmoid(pre[v]);
-    return pack_round<IO, V>(pre);
+    for (int j = 0; j < W - 1; ++j) p[j] = p[j + 1];
 }
 
 // ---- forward over packed rows ------------------------------------------------------------------------------------
 // Blocks [0, head_blocks): the rows' first tokens and windows.  The others: runs of tokens.
 template <typename IO, int W>
-__global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
+__global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
     constexpr int V = kConvVec, U = 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
@@ -100,10 +101,9 @@ __global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const Con
     const int cc = live ? c : 0;
     const IO *x = static_cast<const IO *>(a.x) + cc;
     IO *out = static_cast<IO *>(a.out) + cc;
-    float w[W][V], b[V];
-    conv_weights<W, V>(a, cc, w, b);
-    Pack<IO, V> p[W];
+    Quad w[W], b, p[W];
     const long long block = blockIdx.x / col_blocks;
+    auto input = [&](long long t) { return pack_load<IO, V>(x + t * a.x_stride); };
     if (block < head_blocks) {
         const long long row = block * (kConvThreads / 32) + warp;
         if (row >= a.rows.n) return;
@@ -111,36 +111,31 @@ __global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const Con
         if (slot < 0) return;
         const int s = a.rows.starts[row], len = a.rows.starts[row + 1] - s;
         if (len == 0 && (a.slots || !a.final)) return;
+        conv_weights<W>(a, cc, w, b);
         const bool old = a.init && !(a.fresh && a.fresh[row]);
         const size_t at = (size_t)slot * (W - 1) * a.C + cc;
-#pragma unroll
-        for (int j = 0; j < W - 1; ++j) p[j] = old ? pack_load<IO, V>(static_cast<const IO *>(a.init) + at + (size_t)j * a.C) : pack_zero<IO, V>();
-        Pack<IO, V> last[W - 1];  // of the row's tokens, in front of which come the window's
+        Pack<IO, V> keep[W - 1], win[W - 1];
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
-            const int t = len - (W - 1) + j;
-            if (t >= 0) last[j] = pack_load<IO, V>(x + (size_t)(s + t) * a.x_stride);
+            win[j] = old ? pack_load<IO, V>(static_cast<const IO *>(a.init) + at + (size_t)j * a.C) : pack_zero<IO, V>();
+            p[j] = quad(win[j]);
         }
-        Pack<IO, V> keep[W - 1];
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
-            const int t = len - (W - 1) + j;  // t < 0: input W - 1 + t of the window
-            keep[j] = p[j];
-            if (t >= 0) keep[j] = last[j];
+            const int t = len - (W - 1) + j;  // token t of the row; in front of it, input W - 1 + t of the window
+            keep[j] = win[j];
+            if (t >= 0) keep[j] = input(s + t);
 #pragma unroll
             for (int i = 0; i < W - 1; ++i)
-                if (t < 0 && W - 1 + t == i) keep[j] = p[i];
+                if (t < 0 && W - 1 + t == i) keep[j] = win[i];
         }
 #pragma unroll
         for (int t = 0; t < W - 1; ++t) {
             if (t >= len) break;
-            p[W - 1] = pack_load<IO, V>(x + (size_t)(s + t) * a.x_stride);
-            float pre[V];
-            conv_pre<IO, W, V>(p, w, b, pre);
-            const Pack<IO, V> o = conv_act<IO, V>(pre, a.silu);
+            p[W - 1] = quad(input(s + t));
+            const Pack<IO, V> o = conv_act<IO>(conv_pre<W>(p, w, b), a.silu);
             if (live) pack_store(out + (size_t)(s + t) * a.C, o);
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j) p[j] = p[j + 1];
+            conv_shift(p);
         }
         if (live && a.final)
 #pragma unroll
@@ -150,33 +145,26 @@ __global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const Con
     const long long first = ((block - head_blocks) * (kConvThreads / 32) + warp) * a.run;
     if (first >= a.max_tokens) return;
     const int t0 = (int)first, t1 = (int)min((long long)a.max_tokens, first + a.run);
-    int row = a.rows.of(t0), end = a.max_tokens, begin = 0;
+    // every load of the first tokens is on its way before the look-ups of the row, each of which waits for the one before
+    Pack<IO, V> in[U], win[W - 1];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) in[u] = input(min(t + u, t1 - 1));
+    };
+    fetch(t0);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) win[j] = input(max(t0 - (W - 1) + j, 0));  // (of a row in front, perhaps: then it is not used)
+    conv_weights<W>(a, cc, w, b);
+    int end = a.max_tokens, begin = 0;
     bool mine = false;
     auto enter = [&](int r) {  // r < 0: behind the last sequence
-        row = r;
         mine = r >= 0 && conv_slot(a, r, false) >= 0;
         begin = r >= 0 ? a.rows.starts[r] : 0;
         end = r >= 0 ? a.rows.starts[r + 1] : a.max_tokens;
     };
-    enter(row);
-    float f[W][V];
+    enter(a.rows.of(t0));
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-        const int t = t0 - (W - 1) + j;
-        conv_floats(t >= 0 ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : pack_zero<IO, V>(), f[j]);
-    }
-    Pack<IO, V> in[U];
-    auto fetch = [&](int t) {
-        if (t + U <= t1) {
-            const IO *from = x + (size_t)t * a.x_stride;
-#pragma unroll
-            for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(from + u * a.x_stride);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) in[u] = pack_load<IO, V>(x + (size_t)min(t + u, t1 - 1) * a.x_stride);
-        }
-    };
-    fetch(t0);
+    for (int j = 0; j < W - 1; ++j) p[j] = quad(win[j]);
     for (int t = t0; t < t1; t += U) {
         Pack<IO, V> cur[U];
 #pragma unroll
@@ -184,20 +172,16 @@ __global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const Con
         if (t + U < t1) fetch(t + U);
         IO *to = out + (size_t)t * a.C;
         auto token = [&](int u) {
-            conv_floats(cur[u], f[W - 1]);
-            float pre[V];
-            conv_pre<W, V>(f, w, b, pre);
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-                for (int v = 0; v < V; ++v) f[j][v] = f[j + 1][v];
-            return conv_act<IO, V>(pre, a.silu);
+            p[W - 1] = quad(cur[u]);
+            const Pack<IO, V> o = conv_act<IO>(conv_pre<W>(p, w, b), a.silu);
+            conv_shift(p);
+            return o;
         };
         if (mine && t - begin >= W - 1 && t + U <= min(t1, end)) {  // one row, none of its first tokens
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const Pack<IO, V> o = token(u);
-                if (live) pack_store(to + u * a.C, o);
+                if (live) pack_store(to + (size_t)u * a.C, o);
             }
             continue;
         }
@@ -208,9 +192,9 @@ __global__ void __launch_bounds__(kConvThreads, 5) conv_forward_kernel(const Con
             if (at >= end) enter(a.rows.of(at));
             const Pack<IO, V> o = token(u);
             if (mine) {
-                if (live && at - begin >= W - 1) pack_store(to + u * a.C, o);
+                if (live && at - begin >= W - 1) pack_store(to + (size_t)u * a.C, o);
             } else if (a.clear && live) {
-                pack_store(to + u * a.C, pack_zero<IO, V>());
+                pack_store(to + (size_t)u * a.C, pack_zero<IO, V>());
             }
         }
     }
@@ -226,7 +210,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs 
     const long long first = ((long long)(blockIdx.x / col_blocks) * (kConvThreads / 32) + warp) * a.run;
     if (c >= a.C || first >= a.total_rows) return;
     const int end = (int)min((long long)a.total_rows, first + a.run);
-    float w[W][V], b[V];
+    Quad w[W], b;
     for (int row = (int)first; row < end; row += U) {
         int slot[U];
         Pack<IO, V> p[U][W];
@@ -239,14 +223,15 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs 
             for (int j = 0; j < W - 1; ++j) p[u][j] = pack_load<IO, V>(win + (size_t)j * a.C);
             p[u][W - 1] = pack_load<IO, V>(static_cast<const IO *>(a.x) + (size_t)(row + u) * a.x_stride + c);
         }
-        if (row == (int)first) conv_weights<W, V>(a, c, w, b);
+        if (row == (int)first) conv_weights<W>(a, c, w, b);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (slot[u] < 0) continue;
             IO *win = static_cast<IO *>(a.final) + (size_t)slot[u] * (W - 1) * a.C + c;
-            float pre[V];
-            conv_pre<IO, W, V>(p[u], w, b, pre);
-            pack_store(static_cast<IO *>(a.out) + (size_t)(row + u) * a.C + c, conv_act<IO, V>(pre, a.silu));
+            Quad f[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j) f[j] = quad(p[u][j]);
+            pack_store(static_cast<IO *>(a.out) + (size_t)(row + u) * a.C + c, conv_act<IO>(conv_pre<W>(f, w, b), a.silu));
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) pack_store(win + (size_t)j * a.C, p[u][j + 1]);
         }
@@ -259,21 +244,15 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs 
 // The walk goes W - 1 tokens beyond its run, since dx[t] is complete with dpre[t + W - 1]; dx of the last W tokens waits in
 // registers.  dw and dbias: a thread's sums over its run, a block's over its warps, then conv_reduce_kernel over the blocks,
 // each in a fixed order.
-template <int V>
-__device__ __forceinline__ void conv_dpre(float (&pre)[V], const float (&g)[V], bool silu) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        if (silu) {
-            const float s = sigmoid(pre[v]);
-            pre[v] = g[v] * s * (1.f + pre[v] * (1.f - s));
-        } else {
-            pre[v] = g[v];
-        }
-    }
+__device__ __forceinline__ float2 conv_dpre(float2 pre, float2 g) {
+    const float2 s = make_float2(sigmoid(pre.x), sigmoid(pre.y));
+    const float2 slope = __ffma2_rn(pre, __ffma2_rn(s, both(-1.f), both(1.f)), both(1.f));  // silu' = s (1 + pre (1 - s))
+    return __fmul2_rn(__fmul2_rn(g, s), slope);
 }
+__device__ __forceinline__ Quad conv_dpre(const Quad &pre, const Quad &g, bool silu) { return silu ? Quad{conv_dpre(pre.a, g.a), conv_dpre(pre.b, g.b)} : g; }
 
 template <typename IO, int W>
-__global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
+__global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_backward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
     constexpr int V = kConvVec, U = 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
@@ -281,9 +260,7 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const Co
     const int cc = live ? c : 0;
     const IO *x = static_cast<const IO *>(a.x) + cc, *dout = static_cast<const IO *>(a.dout) + cc;
     const IO *init = static_cast<const IO *>(a.init), *dfinal = static_cast<const IO *>(a.dfinal);
-    float w[W][V], b[V];
-    conv_weights<W, V>(a, cc, w, b);
-    Pack<IO, V> p[W];
+    Quad w[W], b, p[W];
     auto window = [&](int row, int j) {  // input j of the row's window
         return init ? pack_load<IO, V>(init + ((size_t)row * (W - 1) + j) * a.C + cc) : pack_zero<IO, V>();
     };
@@ -291,71 +268,60 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const Co
     if (block < head_blocks) {  // gradients of the windows
         const long long row = block * (kConvThreads / 32) + warp;
         if (row >= a.rows.n || !live) return;
+        conv_weights<W>(a, cc, w, b);
         const int s = a.rows.starts[row], len = a.rows.starts[row + 1] - s;
-        float d[W - 1][V];
+        Quad d[W - 1];
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) {
-            p[i] = window((int)row, i);
-#pragma unroll
-            for (int v = 0; v < V; ++v) d[i][v] = 0.f;
-            if (dfinal && i >= len) conv_floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (i - len)) * a.C + cc), d[i]);
+            p[i] = quad(window((int)row, i)), d[i] = quad_zero();
+            if (dfinal && i >= len) d[i] = quad(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (i - len)) * a.C + cc));
         }
 #pragma unroll
         for (int t = 0; t < W - 1; ++t) {
             if (t >= len) break;
-            p[W - 1] = pack_load<IO, V>(x + (size_t)(s + t) * a.x_stride);
-            float pre[V], g[V];
-            conv_pre<IO, W, V>(p, w, b, pre);
-            conv_floats(pack_load<IO, V>(dout + (size_t)(s + t) * a.C), g);
-            conv_dpre<V>(pre, g, a.silu);
+            p[W - 1] = quad(pack_load<IO, V>(x + (size_t)(s + t) * a.x_stride));
+            const Quad g = conv_dpre(conv_pre<W>(p, w, b), quad(pack_load<IO, V>(dout + (size_t)(s + t) * a.C)), a.silu);
 #pragma unroll
-            for (int i = t; i < W - 1; ++i)  // input i of the window is input i - t of this token's
-#pragma unroll
-                for (int v = 0; v < V; ++v) d[i][v] = fmaf(w[i - t][v], pre[v], d[i][v]);
-#pragma unroll
-            for (int j = 0; j < W - 1; ++j) p[j] = p[j + 1];
+            for (int i = t; i < W - 1; ++i) d[i] = quad_fma(w[i - t], g, d[i]);  // input i of the window is input i - t of this token's
+            conv_shift(p);
         }
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) pack_store(static_cast<IO *>(a.dinit) + ((size_t)row * (W - 1) + i) * a.C + cc, pack_round<IO, V>(d[i]));
+        for (int i = 0; i < W - 1; ++i) pack_store(static_cast<IO *>(a.dinit) + ((size_t)row * (W - 1) + i) * a.C + cc, quad_round<IO>(d[i]));
         return;
     }
     const long long group = block - head_blocks;
     const long long first = (group * (kConvThreads / 32) + warp) * a.run;
     const int t0 = (int)min(first, (long long)a.total_rows), t1 = (int)min((long long)a.total_rows, first + a.run);
-    float dw[W + 1][V], pend[W][V];  // pend[k]: dx of token t - k so far
+    Quad dw[W + 1], pend[W];  // pend[k]: dx of token t - k so far
 #pragma unroll
-    for (int j = 0; j <= W; ++j)
+    for (int j = 0; j <= W; ++j) dw[j] = quad_zero();
 #pragma unroll
-        for (int v = 0; v < V; ++v) dw[j][v] = 0.f;
-#pragma unroll
-    for (int k = 0; k < W; ++k)
-#pragma unroll
-        for (int v = 0; v < V; ++v) pend[k][v] = 0.f;
+    for (int k = 0; k < W; ++k) pend[k] = quad_zero();
     if (t0 < t1) {
         const int tokens = a.rows.n ? a.rows.starts[a.rows.n] : 0, te = min(t1 + W - 1, tokens);  // tokens whose dpre counts
+        Pack<IO, V> in[U], dn[U];
+        auto fetch = [&](int t) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long long at = max(0, min(t + u, te - 1));
+                in[u] = pack_load<IO, V>(x + at * a.x_stride), dn[u] = pack_load<IO, V>(dout + at * a.C);
+            }
+        };
+        if (t0 < te) fetch(t0);
+        conv_weights<W>(a, cc, w, b);
         int row = -1, begin = 0, end = 0;
         auto enter = [&](int t) {
             row = a.rows.of(t);
             begin = a.rows.starts[row], end = a.rows.starts[row + 1];
         };
-        float f[W][V];
         if (t0 < tokens) {
             enter(t0);
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {
                 const int t = t0 - (W - 1) + j;  // of the row, or of its window
-                conv_floats(t >= begin ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : window(row, W - 1 + t - begin), f[j]);
+                p[j] = quad(t >= begin ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : window(row, W - 1 + t - begin));
             }
         }
-        Pack<IO, V> in[U], dn[U];
-        auto fetch = [&](int t) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t at = max(0, min(t + u, te - 1));
-                in[u] = pack_load<IO, V>(x + at * a.x_stride), dn[u] = pack_load<IO, V>(dout + at * a.C);
-            }
-        };
-        if (t0 < te) fetch(t0);
         for (int t = t0; t < t1 + W - 1; t += U) {
             Pack<IO, V> cur[U], dcur[U];
 #pragma unroll
@@ -364,41 +330,28 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const Co
             IO *to = static_cast<IO *>(a.dx) + cc + ((long long)t - (W - 1)) * a.C;
             auto shift = [&]() {
 #pragma unroll
-                for (int k = W - 1; k > 0; --k)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) pend[k][v] = pend[k - 1][v];
-#pragma unroll
-                for (int v = 0; v < V; ++v) pend[0][v] = 0.f;
+                for (int k = W - 1; k > 0; --k) pend[k] = pend[k - 1];
+                pend[0] = quad_zero();
             };
             auto token = [&](int u, int reach, bool own) {  // dpre of a token, into its own and the `reach` pending dx in front
-                conv_floats(cur[u], f[W - 1]);
-                float pre[V], g[V];
-                conv_pre<W, V>(f, w, b, pre);
-                conv_floats(dcur[u], g);
-                conv_dpre<V>(pre, g, a.silu);
-                if (own)
+                p[W - 1] = quad(cur[u]);
+                const Quad g = conv_dpre(conv_pre<W>(p, w, b), quad(dcur[u]), a.silu);
+                if (own) {
+                    dw[W].a = __fadd2_rn(dw[W].a, g.a), dw[W].b = __fadd2_rn(dw[W].b, g.b);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        dw[W][v] += pre[v];
-#pragma unroll
-                        for (int j = 0; j < W; ++j) dw[j][v] = fmaf(pre[v], f[j][v], dw[j][v]);
-                    }
+                    for (int j = 0; j < W; ++j) dw[j] = quad_fma(g, p[j], dw[j]);
+                }
 #pragma unroll
                 for (int k = 0; k < W; ++k)
-                    if (k <= reach)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) pend[k][v] = fmaf(w[W - 1 - k][v], pre[v], pend[k][v]);
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) f[j][v] = f[j + 1][v];
+                    if (k <= reach) pend[k] = quad_fma(w[W - 1 - k], g, pend[k]);
+                conv_shift(p);
             };
             if (t - t0 >= W - 1 && t - begin >= W - 1 && t + U <= min(t1, end - (W - 1))) {  // one row, away from both ends
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     shift();
                     token(u, W - 1, true);
-                    if (live) pack_store(to + u * a.C, pack_round<IO, V>(pend[W - 1]));
+                    if (live) pack_store(to + (long long)u * a.C, quad_round<IO>(pend[W - 1]));
                 }
                 continue;
             }
@@ -411,30 +364,30 @@ __global__ void __launch_bounds__(kConvThreads, 3) conv_backward_kernel(const Co
                     if (at >= end) {
                         enter(at);
 #pragma unroll
-                        for (int j = 0; j < W - 1; ++j) conv_floats(window(row, j), f[j]);
+                        for (int j = 0; j < W - 1; ++j) p[j] = quad(window(row, j));
                     }
                     if (at < t1 && dfinal && at >= end - (W - 1))
-                        conv_floats(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (at - end + W - 1)) * a.C + cc), pend[0]);
+                        pend[0] = quad(pack_load<IO, V>(dfinal + ((size_t)row * (W - 1) + (at - end + W - 1)) * a.C + cc));
                     token(u, at - begin, at < t1);
                 }
-                if (at - (W - 1) >= t0 && live) pack_store(to + u * a.C, pack_round<IO, V>(pend[W - 1]));
+                if (at - (W - 1) >= t0 && live) pack_store(to + (long long)u * a.C, quad_round<IO>(pend[W - 1]));
             }
         }
     }
-    __shared__ float sums[kConvThreads / 32][W + 1][32 * V];
+    __shared__ float4 sums[kConvThreads / 32][W + 1][32];
 #pragma unroll
-    for (int j = 0; j <= W; ++j)
-#pragma unroll
-        for (int v = 0; v < V; ++v) sums[warp][j][v * 32 + lane] = dw[j][v];
+    for (int j = 0; j <= W; ++j) sums[warp][j][lane] = make_float4(dw[j].a.x, dw[j].a.y, dw[j].b.x, dw[j].b.y);
     __syncthreads();
-    const int c0 = (int)(blockIdx.x % col_blocks) * 32 * V;
-    for (int i = threadIdx.x; i < (W + 1) * 32 * V; i += kConvThreads) {
-        const int j = i / (32 * V), col = i % (32 * V), at = (col % V) * 32 + col / V;
-        if (c0 + col >= a.C) continue;
-        float s = 0.f;
+    for (int i = threadIdx.x; i < (W + 1) * 32; i += kConvThreads) {
+        const int j = i / 32, col = (int)(blockIdx.x % col_blocks) * 32 * V + i % 32 * V;
+        if (col >= a.C) continue;
+        float4 s = sums[0][j][i % 32];
 #pragma unroll
-        for (int k = 0; k < kConvThreads / 32; ++k) s += sums[k][j][at];
-        a.partial[((size_t)group * (W + 1) + j) * a.C + c0 + col] = s;
+        for (int k = 1; k < kConvThreads / 32; ++k) {
+            const float4 f = sums[k][j][i % 32];
+            s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
+        }
+        *reinterpret_cast<float4 *>(a.partial + ((size_t)group * (W + 1) + j) * a.C + col) = s;
     }
 }
 

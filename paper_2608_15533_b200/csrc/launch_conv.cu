@@ -43,9 +43,10 @@ long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 int conv_packed(const deltalog_conv_desc *d, ConvArgs &a, cudaStream_t s) {
     const int cols = conv_columns(d);
-    // A run of 32 tokens reads 3 more than it owns; where that leaves SMs without warps the runs are shorter.
-    const long long warps = (long long)cols * a.max_tokens;
-    a.run = warps >= 32ll * 16 * device_info().sms ? 32 : 8;
+    // A run of 8 tokens reads 3 more than it owns and looks its row up: the longer the better, as long as every SM has sixty
+    // warps to take (three waves).
+    const long long warps = (long long)cols * a.max_tokens / (60ll * device_info().sms);
+    a.run = warps >= 128 ? 128 : warps >= 64 ? 64 : warps >= 32 ? 32 : 8;
     const long long heads = ceil_div(a.rows.n, kWarpsPerCta), runs = ceil_div(ceil_div(a.max_tokens, a.run), kWarpsPerCta);
     const long long grid = (heads + runs) * cols;
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;

@@ -45,16 +45,18 @@ int norm_lanes(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 template <int HEADS>
 long long norm_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     const int L = norm_lanes(d->d);
-    const long long items = L == 4 ? norm_items<4, HEADS>(tokens, d->H_q, d->H_k) : L == 8 ? norm_items<8, HEADS>(tokens, d->H_q, d->H_k)
-                          : L == 16 ? norm_items<16, HEADS>(tokens, d->H_q, d->H_k) : norm_items<32, HEADS>(tokens, d->H_q, d->H_k);
-    return (items + kNormThreads / 32 - 1) / (kNormThreads / 32);
+    auto items = [&](int heads) {
+        return L == 4 ? norm_items<4, HEADS>(tokens, heads) : L == 8 ? norm_items<8, HEADS>(tokens, heads)
+             : L == 16 ? norm_items<16, HEADS>(tokens, heads) : norm_items<32, HEADS>(tokens, heads);
+    };
+    return (items(d->H_q) + items(d->H_k) + kNormThreads / 32 - 1) / (kNormThreads / 32);
 }
 
-// Blocks of the backward pass with weights, whose sums they keep: eight an SM (of 148, whichever device is current: the
+// Blocks of the backward pass with weights, whose sums they keep: sixteen an SM (of 148, whichever device is current: the
 // workspace's size depends on it).
 long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     const long long b = norm_blocks<kNormHeadsBack>(d, tokens);
-    return b < 148 * 8 ? b : 148 * 8;
+    return b < 148 * 16 ? b : 148 * 16;
 }
 
 #define NORM_DISPATCH(desc_, CALL)                                                                  \

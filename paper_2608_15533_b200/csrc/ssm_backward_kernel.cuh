@@ -28,6 +28,7 @@ template <typename IO, int N> struct SsmBackward {
         float2 step[kTile * kCols];                          // delta, delta x
         float dy[kTile * kCols], slope[kTile * kCols];       // slope: softplus'
         float sums[3][kTile * kPitch];                       // C . h, sum dh B, sum dh a h_(t-1) A (A in powers of two)
+        float B[kTile * N], C[kTile * N];
         float bc[kSsmWarps][kTile][2 * N];
         int state[kTile], row[kTile];
         unsigned begins, ends, there;
@@ -180,6 +181,14 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             }
             for (int i = tid; i < TT * N; i += kSsmThreads)
                 if (!(there >> (i / N) & 1)) r.B[i] = r.C[i] = from_f32<IO>(0.f);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i0 = 0; i0 < TT * N / 2; i0 += kSsmThreads) {
+            const int i = 2 * (i0 + tid);
+            if (TT * N / 2 % kSsmThreads && i >= TT * N) break;
+            if (!LOCAL) store2(s.B + i, load2(r.B + i));
+            store2(s.C + i, load2(r.C + i));
         }
         __syncthreads();
         // four tokens; MARKED: where rows may begin or end
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             for (int i = 3; i >= 0; --i) {
                 if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
                 float2 c[2];
-                ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
+                ssm_pairs(s.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
                     const float d = step[i * CB + q * LC].x, dy = dys[i * CB + q * LC];
@@ -209,7 +218,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             for (int i = 0; i < 4; ++i) {
                 if (MARKED && (begins >> (k0 + i) & 1)) load(a.S_in, s.state[k0 + i], h);
                 float2 b[2];
-                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+                ssm_pairs(s.B + (k0 + i) * N + nl * 4, b);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
                     const float2 d = step[i * CB + q * LC];
@@ -228,7 +237,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             for (int i = 0; i < 4; ++i) {
                 if (MARKED && (begins >> (k0 + i) & 1)) load(a.S_in, s.state[k0 + i], h);
                 float2 b[2];
-                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
+                ssm_pairs(s.B + (k0 + i) * N + nl * 4, b);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
                     const float2 d = step[i * CB + q * LC];
@@ -246,8 +255,8 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             for (int i = 3; i >= 0; --i) {
                 if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
                 float2 b[2], c[2], bc[4];
-                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
-                ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
+                ssm_pairs(s.B + (k0 + i) * N + nl * 4, b);
+                ssm_pairs(s.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
                     const float2 d = step[i * CB + q * LC];

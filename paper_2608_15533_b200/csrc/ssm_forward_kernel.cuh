@@ -14,13 +14,14 @@ template <typename IO, int N> struct SsmForward {
     static constexpr int kPer = N <= 32 ? 2 : 4;                                            // channels per lane
     static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = 32;    // channels of a CTA, tokens of a tile
     static constexpr int kPitch = kCols + 8;  // lanes that answer for neighbouring tokens store to different banks
-    static constexpr int kCtas = N <= 32 ? 5 : 3;                                           // on an SM, by their registers
+    static constexpr int kCtas = N <= 32 ? 4 : 3;                                           // on an SM, by their registers
     struct Raw {
         IO x[kTile * kCols], dt[kTile * kCols], z[kTile * kCols], B[kTile * N], C[kTile * N];
     };
     struct alignas(16) Shared {
         Raw raw[2];
         float2 step[kTile * kPitch];  // delta, delta x; then C . h in the first's place
+        float B[kTile * N], C[kTile * N];
         int state[kTile], row[kTile];
         unsigned begins, ends, there, open;  // one bit per token of the tile; open: its row goes on behind the stretch
     };
@@ -128,9 +129,9 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
         typename F::Raw &r = s.raw[stage];
         if (warp == 0) {
             SsmToken k{-1, -1, 0, 0};
-            if (t + lane < hi) k = ssm_token(a, t + lane, !LOCAL && blockIdx.x == 0);
+            if (lane < TT && t + lane < hi) k = ssm_token(a, t + lane, !LOCAL && blockIdx.x == 0);
             if (LOCAL && k.row != only) k.row = -1;
-            s.state[lane] = k.state, s.row[lane] = k.row;
+            if (lane < TT) s.state[lane] = k.state, s.row[lane] = k.row;
             const unsigned begins = __ballot_sync(0xffffffffu, k.row >= 0 && k.begin == t + lane);
             const unsigned ends = __ballot_sync(0xffffffffu, k.row >= 0 && k.end == t + lane + 1);
             const unsigned there = __ballot_sync(0xffffffffu, k.row >= 0), open = __ballot_sync(0xffffffffu, k.row >= 0 && k.end > hi);
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
             const float2 u = __fmul2_rn(d, load2(r.x + k * CB + col));
             *reinterpret_cast<float4 *>(s.step + k * PB + col) = make_float4(d.x, u.x, d.y, u.y);
         }
-        if (there != 0xffffffffu) {  // a skipped token may hold anything, and changes nothing
+        if (there != (unsigned)((1ull << TT) - 1)) {  // a skipped token may hold anything, and changes nothing
 #pragma unroll
             for (int i = 0; i < TT / kTokenStep; ++i) {
                 const int k = col_token + i * kTokenStep;
@@ -156,6 +157,14 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
             }
             for (int i = tid; i < TT * N; i += kSsmThreads)
                 if (!(there >> (i / N) & 1)) r.B[i] = r.C[i] = from_f32<IO>(0.f);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i0 = 0; i0 < TT * N / 2; i0 += kSsmThreads) {
+            const int i = 2 * (i0 + tid);
+            if (TT * N / 2 % kSsmThreads && i >= TT * N) break;
+            store2(s.B + i, load2(r.B + i));
+            if (!LOCAL) store2(s.C + i, load2(r.C + i));
         }
         __syncthreads();
         // four tokens; MARKED: where rows may begin or end
@@ -174,8 +183,8 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
                     if (LOCAL && a.front) store_state(a.front, span);
                 }
                 float2 b[2], c[2];
-                ssm_pairs(r.B + (k0 + i) * N + nl * 4, b);
-                if (!LOCAL) ssm_pairs(r.C + (k0 + i) * N + nl * 4, c);
+                ssm_pairs(s.B + (k0 + i) * N + nl * 4, b);
+                if (!LOCAL) ssm_pairs(s.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
                     const float2 d = step[i * PB + q * LC];

@@ -20,7 +20,7 @@ inline int ssm_blocks(const deltalog_ssm_desc *d, bool backward) { return (int)s
 // Stretches that the tokens are cut into at most: as many as one wave of CTAs has (a cut makes the row that crosses it run twice
 // behind its last border).  (148 SMs whatever the device: workspaces depend on it.)
 inline int ssm_most_spans(const deltalog_ssm_desc *d, bool backward) {
-    const int blocks = ssm_blocks(d, backward) * d->groups, wave = 148 * (backward || d->d_state == 64 ? 3 : 5);
+    const int blocks = ssm_blocks(d, backward) * d->groups, wave = 148 * (backward || d->d_state == 64 ? 3 : 4);
     return blocks >= wave ? 1 : wave / blocks;
 }
 struct SsmCut { int span, spans; };
