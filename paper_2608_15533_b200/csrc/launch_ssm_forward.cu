@@ -6,17 +6,17 @@ namespace deltalog {
 
 namespace {
 
-template <typename IO, int N>
+template <typename IO, int N, bool WIDE>
 int forward(const SsmArgs &a, cudaStream_t s) {
-    const size_t smem = sizeof(typename SsmForward<IO, N>::Shared);
+    const size_t smem = sizeof(typename SsmForward<IO, N, WIDE>::Shared);
     const unsigned cols = (unsigned)(a.G * a.blocks);
     if (a.spans > 1) {
-        auto local = ssm_forward_kernel<IO, N, true>;
+        auto local = ssm_forward_kernel<IO, N, true, WIDE>;
         if (int rc = ensure_smem(local, smem)) return rc;
         local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
     }
-    auto kernel = ssm_forward_kernel<IO, N, false>;
+    auto kernel = ssm_forward_kernel<IO, N, false, WIDE>;
     if (int rc = ensure_smem(kernel, smem)) return rc;
     // one more row of CTAs for the rows without tokens, whose states a training call hands on
     const unsigned rest = a.S_out && !a.slots ? 1 : 0;
@@ -38,7 +38,7 @@ int step(const SsmArgs &a, cudaStream_t s) {
 }  // namespace
 
 int launch_ssm_forward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s) {
-#define CALL(IO, N) return forward<IO, N>(a, s)
+#define CALL(IO, N) return a.wide ? forward<IO, N, true>(a, s) : forward<IO, N, false>(a, s)
     SSM_DISPATCH(d, CALL);
 #undef CALL
 }

@@ -47,8 +47,9 @@ SsmArgs ssm_args(const deltalog_ssm_desc *d, const deltalog_ssm_inputs *in) {
 void ssm_forward_args(const deltalog_ssm_desc *d, const deltalog_plan *p, int32_t room, bool train, void *workspace, SsmArgs &a) {
     a.rows = Rows{p->starts, p->token_seq, p->n};
     a.max_tokens = p->max_tokens;
-    const SsmCut c = ssm_cut(d, p->max_tokens, false);
-    a.span = c.span, a.spans = c.spans, a.blocks = ssm_blocks(d, false);
+    const SsmForm form = ssm_forward_form(d, p->max_tokens);
+    const SsmCut c = ssm_cut(d, p->max_tokens, form);
+    a.span = c.span, a.spans = c.spans, a.blocks = c.blocks, a.wide = form == kSsmWide;
     const SsmLayout l = ssm_layout(d, room, train);
     char *w = static_cast<char *>(workspace);
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
@@ -128,8 +129,8 @@ int deltalog_ssm_backward(const deltalog_ssm_desc *desc, const deltalog_plan *pl
     const SsmLayout l = ssm_layout(desc, rows, true);
     char *w = static_cast<char *>(workspace);
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
-    const SsmCut c = ssm_cut(desc, rows, true);
-    a.span = c.span, a.spans = c.spans, a.blocks = ssm_blocks(desc, true), a.total_rows = rows;
+    const SsmCut c = ssm_cut(desc, rows, kSsmBack);
+    a.span = c.span, a.spans = c.spans, a.blocks = c.blocks, a.total_rows = rows;
     a.part_bc = floats(l.part_bc), a.part_A = floats(l.part_A), a.part_cols = floats(l.part_cols);
     a.dout = dout, a.dS_final = dS_final;
     a.dx = grads->x, a.ddt = grads->dt, a.dB = grads->B, a.dC = grads->C, a.dz = in->z ? grads->z : nullptr;

@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                     sum[q] += d;
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        carry[q][p] = __fmul2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d))), __ffma2_rn(c[p], both(dy), carry[q][p]));
+                        carry[q][p] = __fmul2_rn(ssm_decay(A2[q][p], d), __ffma2_rn(c[p], both(dy), carry[q][p]));
                 }
             }
         };
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                     const float2 d = step[i * CB + q * LC];
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d.x))), h[q][p], __fmul2_rn(both(d.y), b[p]));
+                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x), h[q][p], __fmul2_rn(both(d.y), b[p]));
                 }
             }
         };
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                     const float2 d = step[i * CB + q * LC];
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        decay[i][q][p] = exp2_fast(__fmul2_rn(A2[q][p], both(d.x)));
+                        decay[i][q][p] = ssm_decay(A2[q][p], d.x);
                         moved[i][q][p] = __fmul2_rn(decay[i][q][p], h[q][p]);
                         if (i < 3) h[q][p] = __ffma2_rn(both(d.y), b[p], moved[i][q][p]);
                     }

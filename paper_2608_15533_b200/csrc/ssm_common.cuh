@@ -30,7 +30,7 @@ struct SsmArgs {
     Rows rows;
     int32_t D_, G, num_slots, softplus, clear;  // D_: channels
     int32_t max_tokens, total_rows;             // tokens that the plan reaches; rows of the token tensors
-    int32_t span, spans, blocks;                // stretches and blocks of channels per group
+    int32_t span, spans, blocks, wide;          // stretches, blocks of channels per group, the forward pass's form
     float *local, *front, *sums;                // [spans, D_, N] state a stretch leaves, its open row's first state; [spans, D_] step sizes
     float *kept;                                // [max_tokens / 8, D_, N], or NULL
     // backward
@@ -47,6 +47,12 @@ template <int N> struct SsmLanes {
 };
 
 __device__ __forceinline__ float2 exp2_fast(float2 x) { return make_float2(exp2_fast(x.x), exp2_fast(x.y)); }
+
+// Decays of a token, 2^(A delta).  Measured against 64 bits, the hardware's 2^x is low by 2e-8 on average for x in [-1, -0.003], by 6e-9
+// nearer to zero: little in one decay, but the same in all of them, so that a state that remembers a hundred tokens and the
+// gradients that go back over them were off by a hundred times as much (dA 2.1e-6 where 1e-6 comes from the roundings).  The product's
+// addend is free: 2.2e-8 in the exponent, 1.5e-8 of the result, between the two.
+__device__ __forceinline__ float2 ssm_decay(float2 A, float delta) { return exp2_fast(__ffma2_rn(A, both(delta), both(2.2e-8f))); }
 
 // softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|) in (0, 1], of two values.  The exponent of two is rounded, by up to |v| / 2^24:
 // what it lost goes into the result by the first-order term.  log(1 + e) = e P(e) with P the polynomial of degree 9 of least relative

@@ -10,8 +10,10 @@
 
 namespace deltalog {
 
-template <typename IO, int N> struct SsmForward {
-    static constexpr int kPer = N <= 32 ? 2 : 4;                                            // channels per lane
+// WIDE: two channels a lane (four where a channel takes sixteen lanes); otherwise half of that, which takes a token's latency down
+// where there are few CTAs.
+template <typename IO, int N, bool WIDE> struct SsmForward {
+    static constexpr int kPer = (N <= 32 ? 2 : 4) / (WIDE ? 1 : 2);                         // channels per lane
     static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = 32;    // channels of a CTA, tokens of a tile
     static constexpr int kPitch = kCols + 8;  // lanes that answer for neighbouring tokens store to different banks
     static constexpr int kCtas = N <= 32 ? 4 : 3;                                           // on an SM, by their registers
@@ -28,9 +30,9 @@ template <typename IO, int N> struct SsmForward {
 };
 
 // LOCAL: the first pass over a stretch whose last row goes on behind it.
-template <typename IO, int N, bool LOCAL>
-__global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_forward_kernel(const SsmArgs a) {
-    using F = SsmForward<IO, N>;
+template <typename IO, int N, bool LOCAL, bool WIDE>
+__global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas)) ssm_forward_kernel(const SsmArgs a) {
+    using F = SsmForward<IO, N, WIDE>;
     constexpr int KC = F::kPer, CB = F::kCols, PB = F::kPitch, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels;
     extern __shared__ __align__(16) char smem[];
     typename F::Shared &s = *reinterpret_cast<typename F::Shared *>(smem);
@@ -64,6 +66,24 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
     }
     const IO *x = static_cast<const IO *>(a.x) + c0, *dt = static_cast<const IO *>(a.dt) + c0, *z = static_cast<const IO *>(a.z) + (a.z ? c0 : 0);
     const IO *Bp = static_cast<const IO *>(a.B) + group * N, *Cp = static_cast<const IO *>(a.C) + group * N;
+
+    auto fetch = [&](int t, int stage) {
+        typename F::Raw &r = s.raw[stage];
+        auto parts = [&](auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            ssm_stage<ALL, TT, CB>(r.x, x, a.x_stride, t, from, hi, cols);
+            ssm_stage<ALL, TT, CB>(r.dt, dt, a.dt_stride, t, from, hi, cols);
+            ssm_stage<ALL, TT, N>(r.B, Bp, a.B_stride, t, from, hi, N);
+            if (!LOCAL) {
+                if (a.z) ssm_stage<ALL, TT, CB>(r.z, z, a.z_stride, t, from, hi, cols);
+                ssm_stage<ALL, TT, N>(r.C, Cp, a.C_stride, t, from, hi, N);
+            }
+        };
+        if (t + TT <= hi && cols == CB) parts(std::true_type{});
+        else parts(std::false_type{});
+        cp_async_commit();
+    };
+    fetch(from, 0);
 
     float2 A2[KC][2], h[KC][2];  // A in powers of two
     float sum[KC];
@@ -107,23 +127,6 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
     const int col = (tid % (CB / 2)) * 2, col_token = tid / (CB / 2);
     constexpr int kTokenStep = kSsmThreads / (CB / 2);
     const float2 bias = a.bias && col < cols ? load2(a.bias + c0 + col) : both(0.f), skip = a.D && col < cols ? load2(a.D + c0 + col) : both(0.f);
-    auto fetch = [&](int t, int stage) {
-        typename F::Raw &r = s.raw[stage];
-        auto parts = [&](auto all) {
-            constexpr bool ALL = decltype(all)::value;
-            ssm_stage<ALL, TT, CB>(r.x, x, a.x_stride, t, from, hi, cols);
-            ssm_stage<ALL, TT, CB>(r.dt, dt, a.dt_stride, t, from, hi, cols);
-            ssm_stage<ALL, TT, N>(r.B, Bp, a.B_stride, t, from, hi, N);
-            if (!LOCAL) {
-                if (a.z) ssm_stage<ALL, TT, CB>(r.z, z, a.z_stride, t, from, hi, cols);
-                ssm_stage<ALL, TT, N>(r.C, Cp, a.C_stride, t, from, hi, N);
-            }
-        };
-        if (t + TT <= hi && cols == CB) parts(std::true_type{});
-        else parts(std::false_type{});
-        cp_async_commit();
-    };
-    fetch(from, 0);
     int stage = 0;
     for (int t = from; t < hi; t += TT, stage ^= 1) {
         typename F::Raw &r = s.raw[stage];
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N>::kCtas)) ssm_f
                     float2 out = both(0.f);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(d.x))), h[q][p], __fmul2_rn(b[p], both(d.y)));
+                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x), h[q][p], __fmul2_rn(b[p], both(d.y)));
                         if (!LOCAL) out = p ? __ffma2_rn(c[p], h[q][p], out) : __fmul2_rn(c[p], h[q][p]);
                     }
                     if (LOCAL) sum[q] += d.x;
@@ -302,7 +305,7 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs a, 
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
                 const float2 bp = load2(b[u].e + 2 * p), cp = load2(cv[u].e + 2 * p);
-                h[u][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[p], both(delta))), h[u][p], __fmul2_rn(bp, both(in)));
+                h[u][p] = __ffma2_rn(ssm_decay(A2[p], delta), h[u][p], __fmul2_rn(bp, both(in)));
                 y = __ffma2_rn(cp, h[u][p], y);
             }
             float o = y.x + y.y;

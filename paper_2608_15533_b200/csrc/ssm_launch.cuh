@@ -9,32 +9,37 @@ namespace deltalog {
 
 inline long long ssm_ceil(long long a, long long b) { return (a + b - 1) / b; }
 
-constexpr int kSsmSpanMin = 256;  // tokens of a stretch at least
+constexpr int kSsmSpanMin = 128;  // tokens of a stretch at least
 
-// Channels of a CTA: forward, backward.
-inline int ssm_cols(const deltalog_ssm_desc *d, bool backward) {
-    return d->d_state == 8 ? 128 : d->d_state == 16 ? 64 : d->d_state == 32 || !backward ? 32 : 16;
+// How the forward pass (`wide` or not) or the backward pass cuts channels into blocks and tokens into stretches.
+enum SsmForm { kSsmWide, kSsmNarrow, kSsmBack };
+inline int ssm_blocks(const deltalog_ssm_desc *d, SsmForm form) {
+    const int n = d->d_state, wide = n == 8 ? 128 : n == 16 ? 64 : 32;  // channels of a CTA
+    return (int)ssm_ceil(d->channels / d->groups, form == kSsmWide || (form == kSsmBack && n != 64) ? wide : wide / 2);
 }
-inline int ssm_blocks(const deltalog_ssm_desc *d, bool backward) { return (int)ssm_ceil(d->channels / d->groups, ssm_cols(d, backward)); }
 
 // Stretches that the tokens are cut into at most: as many as one wave of CTAs has (a cut makes the row that crosses it run twice
 // behind its last border).  (148 SMs whatever the device: workspaces depend on it.)
-inline int ssm_most_spans(const deltalog_ssm_desc *d, bool backward) {
-    const int blocks = ssm_blocks(d, backward) * d->groups, wave = 148 * (backward || d->d_state == 64 ? 3 : 4);
+inline int ssm_most_spans(const deltalog_ssm_desc *d, SsmForm form) {
+    const int blocks = ssm_blocks(d, form) * d->groups, wave = 148 * (form == kSsmBack || d->d_state == 64 ? 3 : 4);
     return blocks >= wave ? 1 : wave / blocks;
 }
-struct SsmCut { int span, spans; };
-inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {
+struct SsmCut { int span, spans, blocks; };
+inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t tokens, SsmForm form) {
+    const long long span = ssm_ceil(ssm_ceil(tokens, ssm_most_spans(d, form)), 32) * 32;
     SsmCut c;
-    const long long most = ssm_most_spans(d, backward);
-    const long long span = ssm_ceil(ssm_ceil(tokens, most), 32) * 32;
     c.span = (int)(span < kSsmSpanMin ? kSsmSpanMin : span);
-    c.spans = (int)ssm_ceil(tokens, c.span);
+    c.spans = (int)ssm_ceil(tokens, c.span), c.blocks = ssm_blocks(d, form);
     return c;
+}
+// Narrow where the wide form would leave SMs without a CTA.
+inline SsmForm ssm_forward_form(const deltalog_ssm_desc *d, int32_t tokens) {
+    const SsmCut c = ssm_cut(d, tokens, kSsmWide);
+    return (long long)c.spans * c.blocks * d->groups < 148 ? kSsmNarrow : kSsmWide;
 }
 // What ssm_cut gives at most for this many tokens or fewer.
 inline int ssm_room(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {
-    const long long most = ssm_most_spans(d, backward), spans = ssm_ceil(tokens, kSsmSpanMin);
+    const long long most = ssm_most_spans(d, backward ? kSsmBack : kSsmWide), spans = ssm_ceil(tokens, kSsmSpanMin);
     return (int)(spans < most ? spans : most);
 }
 
@@ -56,7 +61,7 @@ inline SsmLayout ssm_layout(const deltalog_ssm_desc *d, int32_t tokens, bool tra
     l.local = take(joined > 1, (size_t)joined * D * N * 4);
     l.front = take(f > 1 && !train, (size_t)f * D * N * 4);
     l.sums = take(joined > 1, (size_t)joined * D * 4);
-    l.part_bc = take(train, (size_t)d->groups * ssm_blocks(d, true) * tokens * 2 * N * 4);
+    l.part_bc = take(train, (size_t)d->groups * ssm_blocks(d, kSsmBack) * tokens * 2 * N * 4);
     l.part_A = take(train, (size_t)b * D * N * 4);
     l.part_cols = take(train, (size_t)b * 2 * D * 4);
     l.total = at ? at : 256;
