@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(kConvThreads) conv_step_kernel(const ConvArgs 
     for (int row = (int)first; row < end; row += U) {
         int slot[U];
         Pack<IO, V> p[U][W];
-        step_slots(a.slots, row, end, a.num_slots, a.status, slot);
+        step_slots(a.slots, row, end, slot);
+        step_check(row, end, a.num_slots, a.status, slot);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (slot[u] < 0) continue;

@@ -3,7 +3,7 @@
 //     y = scale (n turned pair by pair)
 // Backward, with g = scale (dy turned back):  dw = sum g x r,  dx = r (g w - c r^2 x sum(g w x)).
 //
-// Bound by HBM: every value is read once and written once.  L lanes hold a head, eight values each: two runs of four that are
+// Bound by HBM: every value is read once and written once.  L lanes hold a head, sixteen values each: two runs of eight that are
 // half a rotation apart (or neighbours, for interleaved pairs and behind the rotated part), so that a lane turns its own values.  A
 // warp takes one token and several of its heads: the token's cosines and sines are loaded once for all of them, and several heads a
 // lane are in flight.  The sums over a head are butterflies over its lanes.
@@ -27,27 +27,53 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 128;
-constexpr int kNormHeads = 4, kNormHeadsBack = 2;  // heads in flight per lane
+constexpr int kNormHeads = 2, kNormHeadsBack = 1;  // heads in flight per lane
 
-// Where a lane's two runs of four values are in a head.
-struct NormAt { int lo, hi; };
+// Where a lane's two runs of eight values are in a head, and whether they are.
+struct NormAt {
+    int lo, hi;
+    bool has_lo, has_hi;
+};
 __device__ __forceinline__ NormAt norm_at(const NormArgs &a, int l) {
-    if (!a.interleaved && l * 8 < a.rot) return {l * 4, a.rot / 2 + l * 4};
-    return {l * 8, l * 8 + 4};
+    NormAt at{l * 16, l * 16 + 8, false, false};
+    if (!a.interleaved && l * 16 < a.rot) at.lo = l * 8, at.hi = a.rot / 2 + l * 8;
+    at.has_lo = l * 16 < a.d, at.has_hi = l * 16 + 8 < a.d;  // (the rotated part is a multiple of sixteen)
+    return at;
 }
 template <typename IO>
-__device__ __forceinline__ void norm_load(const IO *p, NormAt at, float (&x)[8]) {
-    float lo[4], hi[4];
-    load_vec<IO, 4>(p + at.lo, lo);
-    load_vec<IO, 4>(p + at.hi, hi);
+__device__ __forceinline__ void norm_load(const IO *p, const NormAt &at, bool there, Pack<IO, 8> (&x)[2]) {
+    x[0] = x[1] = pack_zero<IO, 8>();
+    constexpr int V = 16 / sizeof(IO);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = lo[e], x[4 + e] = hi[e];
+    for (int e = 0; e < 8; e += V) {
+        if (there && at.has_lo) *reinterpret_cast<uint4 *>(x[0].e + e) = *reinterpret_cast<const uint4 *>(p + at.lo + e);
+        if (there && at.has_hi) *reinterpret_cast<uint4 *>(x[1].e + e) = *reinterpret_cast<const uint4 *>(p + at.hi + e);
+    }
 }
 template <typename IO>
-__device__ __forceinline__ void norm_store(IO *p, NormAt at, const float (&x)[8]) {
-    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
-    pack_store<IO, 4>(p + at.lo, pack_round<IO, 4>(lo));
-    pack_store<IO, 4>(p + at.hi, pack_round<IO, 4>(hi));
+__device__ __forceinline__ void norm_floats(const Pack<IO, 8> (&x)[2], float (&f)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = to_f32(x[e / 8].e[e % 8]);
+}
+template <typename IO>
+__device__ __forceinline__ void norm_store(IO *p, const NormAt &at, const float (&x)[16]) {
+    constexpr int V = 16 / sizeof(IO);
+    Pack<IO, 8> v[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e / 8].e[e % 8] = from_f32<IO>(x[e]);
+#pragma unroll
+    for (int e = 0; e < 8; e += V) {
+        if (at.has_lo) *reinterpret_cast<uint4 *>(p + at.lo + e) = *reinterpret_cast<const uint4 *>(v[0].e + e);
+        if (at.has_hi) *reinterpret_cast<uint4 *>(p + at.hi + e) = *reinterpret_cast<const uint4 *>(v[1].e + e);
+    }
+}
+__device__ __forceinline__ void norm_weights(const float *w, const NormAt &at, float (&f)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = 1.f;
+    if (!w) return;
+    Pack<float, 8> v[2];
+    norm_load(w, at, true, v);
+    norm_floats(v, f);
 }
 
 template <int L>
@@ -57,32 +83,31 @@ __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
-// A token's rotation as a lane of its heads needs it: the angles of its four pairs.
+// A token's rotation as a lane of its heads needs it: the angles of its eight pairs.
 struct Turn {
-    float c[4], s[4];
+    float c[8], s[8];
     bool on;  // this lane's values turn
 };
 
 // false: a token without a valid position.
-__device__ __forceinline__ bool norm_turn(const NormArgs &a, int token, int l, Turn &t) {
+__device__ __forceinline__ bool norm_turn(const NormArgs &a, int p, int l, Turn &t) {
     t.on = false;
     if (a.rot == 0) return true;
-    const int p = a.positions[token];
     if (p < 0 || p >= a.table_rows) {
         if (p >= 0 && l == 0 && a.status) atomicOr(a.status, DELTALOG_STATUS_BAD_POSITION);
         return false;
     }
-    t.on = l * 8 < a.rot;
+    t.on = l * 16 < a.rot;
     if (t.on) {
-        load_vec<float, 4>(a.cos + (size_t)p * (a.rot / 2) + l * 4, t.c);
-        load_vec<float, 4>(a.sin + (size_t)p * (a.rot / 2) + l * 4, t.s);
+        load8(a.cos + (size_t)p * (a.rot / 2) + l * 8, t.c);
+        load8(a.sin + (size_t)p * (a.rot / 2) + l * 8, t.s);
     }
     return true;
 }
 
 // x turned by the token's angles, or back by them.
 template <bool BACK>
-__device__ __forceinline__ void norm_rotate(const NormArgs &a, const Turn &t, float (&x)[8]) {
+__device__ __forceinline__ void norm_rotate(const NormArgs &a, const Turn &t, float (&x)[16]) {
     if (!t.on) return;
     auto turn = [&](float &u, float &v, int e) {
         const float u0 = u, s = BACK ? -t.s[e] : t.s[e];
@@ -90,10 +115,10 @@ __device__ __forceinline__ void norm_rotate(const NormArgs &a, const Turn &t, fl
     };
     if (a.interleaved) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) turn(x[2 * e], x[2 * e + 1], e);
+        for (int e = 0; e < 8; ++e) turn(x[2 * e], x[2 * e + 1], e);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) turn(x[e], x[4 + e], e);
+        for (int e = 0; e < 8; ++e) turn(x[e], x[8 + e], e);
     }
 }
 
@@ -121,110 +146,119 @@ __device__ __forceinline__ NormSide<IO> norm_side(const NormArgs &a, bool is_k) 
 }
 
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads) head_norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, 7) head_norm_forward_kernel(const NormArgs a) {
     constexpr int G = 32 / L, per = kNormHeads * G;
     const int lane = threadIdx.x & 31, l = lane & (L - 1), group = lane / L;
-    const long long item = (long long)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
-    const int cq = (a.H_q + per - 1) / per, chunks = cq + (a.H_k + per - 1) / per;
-    const int token = (int)(item / chunks), chunk = (int)(item - (long long)token * chunks);
+    const unsigned item = blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);  // (fewer than 2^31)
+    const unsigned cq = (a.H_q + per - 1) / per, chunks = cq + (a.H_k + per - 1) / per, chunk = item % chunks;
+    const int token = (int)(item / chunks);
     if (token >= a.tokens) return;
+    const int position = a.rot ? a.positions[token] : 0;  // first: its tables' rows are two trips to memory away
     const NormSide<IO> t = norm_side<IO>(a, chunk >= cq);
-    const int head = (chunk >= cq ? chunk - cq : chunk) * per + group;
-    const bool in = l * 8 < a.d;
+    const int head = (int)(chunk >= cq ? chunk - cq : chunk) * per + group;
     const NormAt at = norm_at(a, l);
     const IO *x = t.x + (size_t)token * t.stride;
     IO *out = t.out + (size_t)token * t.heads * a.d;
-    float v[kNormHeads][8];
+    Pack<IO, 8> raw[kNormHeads][2];
 #pragma unroll
-    for (int i = 0; i < kNormHeads; ++i) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-        if (in && head + i * G < t.heads) norm_load(x + (head + i * G) * a.d, at, v[i]);
-    }
+    for (int i = 0; i < kNormHeads; ++i) norm_load(x + (head + i * G) * a.d, at, head + i * G < t.heads, raw[i]);
+    float weight[16];
+    norm_weights(t.w, at, weight);
     Turn turn;
-    const bool ok = norm_turn(a, token, l, turn);
-    float weight[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) weight[e] = 1.f;
-    if (t.w && in) norm_load(t.w, at, weight);
+    const bool ok = norm_turn(a, position, l, turn);
     const float c = a.norm == DELTALOG_NORM_RMS ? 1.f / (float)a.d : 1.f;
 #pragma unroll
     for (int i = 0; i < kNormHeads; ++i) {
-        float r = t.scale;
+        float v[16], r = t.scale;
+        norm_floats(raw[i], v);
         if (a.norm != DELTALOG_NORM_NONE) {
             float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
+            for (int e = 0; e < 16; ++e) ss = fmaf(v[e], v[e], ss);
             r *= rsqrtf(fmaf(c, lanes_sum<L>(ss), a.eps));
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] *= r * weight[e];
-        norm_rotate<false>(a, turn, v[i]);
-        if (in && head + i * G < t.heads) {
+        for (int e = 0; e < 16; ++e) v[e] *= r * weight[e];
+        norm_rotate<false>(a, turn, v);
+        if (head + i * G < t.heads) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = ok ? v[i][e] : 0.f;
-            norm_store(out + (head + i * G) * a.d, at, v[i]);
+            for (int e = 0; e < 16; ++e) v[e] = ok ? v[e] : 0.f;
+            norm_store(out + (head + i * G) * a.d, at, v);
         }
     }
 }
 
 // With weights the grid is fixed and every warp walks over its items of q, then over those of k, with the weights' gradient in
-// registers; without, every warp has one item.
+// registers and the next item's values on their way; without, every warp has one item.
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads) head_norm_backward_kernel(const NormArgs a) {
-    constexpr int G = 32 / L, per = kNormHeadsBack * G;
+__global__ void __launch_bounds__(kNormThreads, (sizeof(IO) == 4 ? 3 : 4)) head_norm_backward_kernel(const NormArgs a) {
+    constexpr int G = 32 / L, H = kNormHeadsBack, per = H * G;
     __shared__ float sums[kNormThreads / 32][256];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
-    const bool in = l * 8 < a.d, weighted = a.w_q != nullptr;
+    const bool weighted = a.w_q != nullptr, normed = a.norm != DELTALOG_NORM_NONE;
     const NormAt at = norm_at(a, l);
     const float c = a.norm == DELTALOG_NORM_RMS ? 1.f / (float)a.d : 1.f;
     const long long first = (long long)blockIdx.x * (kNormThreads / 32) + warp, step = (long long)gridDim.x * (kNormThreads / 32);
     long long skipped = 0;  // items of the tensor in front
     for (int side = 0; side < 2; ++side) {
         const NormSide<IO> t = norm_side<IO>(a, side == 1);
-        const int chunks = (t.heads + per - 1) / per;
-        const long long items = (long long)a.tokens * chunks;
-        float weight[8], dw[8];
+        const unsigned chunks = (t.heads + per - 1) / per;
+        const long long items = (long long)a.tokens * chunks;  // (fewer than 2^31)
+        float weight[16], dw[16];
+        norm_weights(t.w, at, weight);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) weight[e] = 1.f, dw[e] = 0.f;
-        if (t.w && in) norm_load(t.w, at, weight);
-        for (long long item = first - skipped; item < items; item += step) {
-            if (item < 0) continue;
-            const int token = (int)(item / chunks), head = (int)(item - (long long)token * chunks) * per + group;
-            const IO *x = t.x + (size_t)token * t.stride;
-            const size_t to = (size_t)token * t.heads * a.d;
-            float v[kNormHeadsBack][8], g[kNormHeadsBack][8];
+        for (int e = 0; e < 16; ++e) dw[e] = 0.f;
+        Pack<IO, 8> raw_g[H][2], raw_v[H][2];  // the next item's gradient and value
+        int position = 0;
+        auto fetch = [&](unsigned item) {
+            const unsigned token = item / chunks;
+            const int head = (int)(item % chunks) * per + group;
+            const IO *x = t.x + token * t.stride, *g = t.dout + (size_t)token * t.heads * a.d;
+            position = a.rot ? a.positions[token] : 0;
 #pragma unroll
-            for (int i = 0; i < kNormHeadsBack; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = g[i][e] = 0.f;
-                if (in && head + i * G < t.heads) {
-                    norm_load(t.dout + to + (head + i * G) * a.d, at, g[i]);
-                    if (a.norm != DELTALOG_NORM_NONE) norm_load(x + (head + i * G) * a.d, at, v[i]);
-                }
+            for (int i = 0; i < H; ++i) {
+                const bool there = head + i * G < t.heads;
+                norm_load(g + (head + i * G) * a.d, at, there, raw_g[i]);
+                norm_load(x + (head + i * G) * a.d, at, there && normed, raw_v[i]);
             }
+        };
+        long long item = first - skipped;
+        if (item >= 0 && item < items) fetch((unsigned)item);
+        for (; item >= 0 && item < items; item += step) {
+            const unsigned token = (unsigned)item / chunks;
+            const int head = (int)((unsigned)item % chunks) * per + group;
             Turn turn;
-            const bool ok = norm_turn(a, token, l, turn);
+            const bool ok = norm_turn(a, position, l, turn);
+            float v[H][16], g[H][16];
 #pragma unroll
-            for (int i = 0; i < kNormHeadsBack; ++i) {
+            for (int i = 0; i < H; ++i) norm_floats(raw_g[i], g[i]), norm_floats(raw_v[i], v[i]);
+            if (item + step < items) fetch((unsigned)(item + step));
+            IO *dx = t.out + (size_t)token * t.heads * a.d;
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                float ss = 0.f, gx = 0.f;
+                if (normed) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) ss = fmaf(v[i][e], v[i][e], ss);
+                    ss = lanes_sum<L>(ss);
+                }
                 norm_rotate<true>(a, turn, g[i]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[i][e] *= t.scale;
-                if (a.norm != DELTALOG_NORM_NONE) {
-                    float ss = 0.f, gx = 0.f;
+                for (int e = 0; e < 16; ++e) g[i][e] *= t.scale;
+                if (normed) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss), gx = fmaf(g[i][e] * weight[e], v[i][e], gx);
-                    const float r = rsqrtf(fmaf(c, lanes_sum<L>(ss), a.eps)), k = lanes_sum<L>(gx) * c * r * r * r;
+                    for (int e = 0; e < 16; ++e) gx = fmaf(g[i][e] * weight[e], v[i][e], gx);
+                    const float r = rsqrtf(fmaf(c, ss, a.eps)), k = lanes_sum<L>(gx) * c * r * r * r;
                     if (weighted && ok)  // (a token without a position may hold anything)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dw[e] = fmaf(g[i][e], v[i][e] * r, dw[e]);
+                        for (int e = 0; e < 16; ++e) dw[e] = fmaf(g[i][e], v[i][e] * r, dw[e]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[i][e] = fmaf(r * weight[e], g[i][e], -k * v[i][e]);
+                    for (int e = 0; e < 16; ++e) g[i][e] = fmaf(r * weight[e], g[i][e], -k * v[i][e]);
                 }
-                if (in && head + i * G < t.heads) {
+                if (head + i * G < t.heads) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[i][e] = ok ? g[i][e] : 0.f;
-                    norm_store(static_cast<IO *>(t.out) + to + (head + i * G) * a.d, at, g[i]);
+                    for (int e = 0; e < 16; ++e) g[i][e] = ok ? g[i][e] : 0.f;
+                    norm_store(dx + (head + i * G) * a.d, at, g[i]);
                 }
             }
         }
@@ -235,11 +269,11 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_backward_kernel(const 
         // the block's sums: over the heads side by side in a warp, then over its warps
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
             float s = dw[e];
 #pragma unroll
             for (int o = L; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-            if (group == 0 && in) sums[warp][(e < 4 ? at.lo : at.hi - 4) + e] = s;
+            if (group == 0 && (e < 8 ? at.has_lo : at.has_hi)) sums[warp][(e < 8 ? at.lo : at.hi - 8) + e] = s;
         }
         __syncthreads();
         for (int i = threadIdx.x; i < a.d; i += kNormThreads) {

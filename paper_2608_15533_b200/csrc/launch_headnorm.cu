@@ -40,23 +40,24 @@ NormArgs norm_args(const deltalog_norm_desc *d, const void *q, int64_t q_stride,
     return a;
 }
 
-int norm_lanes(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+int norm_lanes(int d) { return d <= 32 ? 2 : d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
 template <int HEADS>
 long long norm_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     const int L = norm_lanes(d->d);
     auto items = [&](int heads) {
-        return L == 4 ? norm_items<4, HEADS>(tokens, heads) : L == 8 ? norm_items<8, HEADS>(tokens, heads)
-             : L == 16 ? norm_items<16, HEADS>(tokens, heads) : norm_items<32, HEADS>(tokens, heads);
+        return L == 2 ? norm_items<2, HEADS>(tokens, heads) : L == 4 ? norm_items<4, HEADS>(tokens, heads)
+             : L == 8 ? norm_items<8, HEADS>(tokens, heads) : norm_items<16, HEADS>(tokens, heads);
     };
     return (items(d->H_q) + items(d->H_k) + kNormThreads / 32 - 1) / (kNormThreads / 32);
 }
 
-// Blocks of the backward pass with weights, whose sums they keep: sixteen an SM (of 148, whichever device is current: the
+// Blocks of the backward pass with weights, whose sums they keep: one wave (of 148, whichever device is current: the
 // workspace's size depends on it).
 long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     const long long b = norm_blocks<kNormHeadsBack>(d, tokens);
-    return b < 148 * 16 ? b : 148 * 16;
+    const int most = 148 * (d->io_dtype == DELTALOG_F32 ? 3 : 4);
+    return b < most ? b : most;
 }
 
 #define NORM_DISPATCH(desc_, CALL)                                                                  \
@@ -66,7 +67,7 @@ long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
         else { NORM_LANES(__nv_bfloat16, l_, CALL); }                                               \
     } while (0)
 #define NORM_LANES(IO, l_, CALL) \
-    if (l_ == 4) { CALL(IO, 4); } else if (l_ == 8) { CALL(IO, 8); } else if (l_ == 16) { CALL(IO, 16); } else { CALL(IO, 32); }
+    if (l_ == 2) { CALL(IO, 2); } else if (l_ == 4) { CALL(IO, 4); } else if (l_ == 8) { CALL(IO, 8); } else { CALL(IO, 16); }
 
 }  // namespace
 
@@ -81,7 +82,7 @@ int deltalog_head_norm_forward(const deltalog_norm_desc *desc, const void *q, in
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = out_q, a.out_k = out_k, a.status = status;
     const long long grid = norm_blocks<kNormHeads>(desc, tokens);
-    if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
+    if (grid > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
     cudaStream_t s = static_cast<cudaStream_t>(stream);
 #define CALL(IO, L) head_norm_forward_kernel<IO, L><<<(unsigned)grid, kNormThreads, 0, s>>>(a)
     NORM_DISPATCH(desc, CALL);
@@ -108,7 +109,7 @@ int deltalog_head_norm_backward(const deltalog_norm_desc *desc, const void *q, i
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = dq, a.out_k = dk, a.dout_q = dout_q, a.dout_k = dout_k, a.partial = static_cast<float *>(workspace);
     const long long grid = weighted ? norm_kept_blocks(desc, tokens) : norm_blocks<kNormHeadsBack>(desc, tokens);
-    if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
+    if (norm_blocks<kNormHeadsBack>(desc, tokens) > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (grid > 0) {
 #define CALL(IO, L) head_norm_backward_kernel<IO, L><<<(unsigned)grid, kNormThreads, 0, s>>>(a)

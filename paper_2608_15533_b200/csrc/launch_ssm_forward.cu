@@ -28,7 +28,7 @@ int forward(const SsmArgs &a, cudaStream_t s) {
 template <typename IO, int N>
 int step(const SsmArgs &a, cudaStream_t s) {
     const int cols = (int)ssm_ceil(a.D_, kSsmWarps * 32 / (N / 8));
-    constexpr int run = 4;  // 125 rows of 4096 channels with 2, 4, 6, 8, 16 rows a CTA: 20.5, 20.7, 20.5, 22.9, 23.3 us
+    constexpr int run = 4;  // 125 rows of 4096 channels with 2, 4, 8, 16 rows a CTA: 17.1, 16.3, 15.8, 20.6 us
     const long long grid = ssm_ceil(a.total_rows, run) * cols;
     if (grid > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     ssm_step_kernel<IO, N><<<(unsigned)grid, kSsmThreads, 0, s>>>(a, cols, run);

@@ -70,12 +70,15 @@ struct Rows {
     }
 };
 
-// Slots of U rows of a single-token call, -1 for rows that it skips.  The list's entries are loaded together: one after the
-// other, each behind the test of the one before, they would cost a trip to memory each.
+// Slots of U rows of a single-token call as the list has them, and -1 for rows that the call skips.  The list's entries are
+// loaded together: one after the other, each behind the test of the one before, they would cost a trip to memory each.
 template <int U>
-__device__ __forceinline__ void step_slots(const int32_t *slots, int row, int end, int num_slots, int32_t *status, int (&slot)[U]) {
+__device__ __forceinline__ void step_slots(const int32_t *slots, int row, int end, int (&slot)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) slot[u] = slots ? slots[min(row + u, end - 1)] : row + u;
+}
+template <int U>
+__device__ __forceinline__ void step_check(int row, int end, int num_slots, int32_t *status, int (&slot)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (row + u >= end) slot[u] = -1;

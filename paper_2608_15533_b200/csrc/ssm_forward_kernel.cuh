@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
 
 // One token per row.  Bound by HBM, the states' read and write.  A lane holds eight states of a channel (32 bytes, one access),
 // so that step size and gate are worked out by d_state / 8 lanes, and keeps its channel's A for all of its rows, two of which are in
-// flight.
+// flight (four, with fewer CTAs on an SM: 21 us where two take 16).
 __device__ __forceinline__ void ssm_load8(const float *p, float2 (&v)[4]) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y), "=f"(v[2].x), "=f"(v[2].y), "=f"(v[3].x), "=f"(v[3].y) : "l"(p) : "memory");
@@ -269,58 +269,67 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs a, 
     const IO *x = static_cast<const IO *>(a.x) + cc, *dt = static_cast<const IO *>(a.dt) + cc, *z = static_cast<const IO *>(a.z) + (a.z ? cc : 0);
     const IO *B = static_cast<const IO *>(a.B) + group * N + nl * 8, *C = static_cast<const IO *>(a.C) + group * N + nl * 8;
     const size_t at = (size_t)cc * N + nl * 8, pitch = (size_t)a.D_ * N;
+    struct Row {
+        float2 h[4];
+        Pack<IO, 8> b, c;
+        IO x, d, z;
+        int slot;
+    };
+    Row rows[U];
+    if (first >= end) return;
     float2 A2[4];
     float bias = 0.f, skip = 0.f;
     for (int row = (int)first; row < end; row += U) {
-        float2 h[U][4];
-        Pack<IO, 8> b[U], cv[U];
-        IO xv[U], d[U], zv[U];
         int slot[U];
-        step_slots(a.slots, row, end, a.num_slots, a.status, slot);
+        step_slots(a.slots, row, end, slot);
+        step_check(row, end, a.num_slots, a.status, slot);
+        // every row is loaded, a skipped one from wherever is allowed, so that no branch keeps one load behind another
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (slot[u] < 0) continue;
-            const long long t = row + u;
-            ssm_load8(a.S_in + slot[u] * pitch + at, h[u]);
-            xv[u] = x[t * a.x_stride], d[u] = dt[t * a.dt_stride], zv[u] = a.z ? z[t * a.z_stride] : xv[u];
+            Row &r = rows[u];
+            r.slot = slot[u];
+            const long long t = min(row + u, end - 1);
+            ssm_load8(a.S_in + max(r.slot, 0) * pitch + at, r.h);
+            r.x = x[t * a.x_stride], r.d = dt[t * a.dt_stride], r.z = a.z ? z[t * a.z_stride] : r.x;
 #pragma unroll
             for (int e = 0; e < 8; e += 16 / sizeof(IO)) {
-                *reinterpret_cast<uint4 *>(b[u].e + e) = *reinterpret_cast<const uint4 *>(B + t * a.B_stride + e);
-                *reinterpret_cast<uint4 *>(cv[u].e + e) = *reinterpret_cast<const uint4 *>(C + t * a.C_stride + e);
+                *reinterpret_cast<uint4 *>(r.b.e + e) = *reinterpret_cast<const uint4 *>(B + t * a.B_stride + e);
+                *reinterpret_cast<uint4 *>(r.c.e + e) = *reinterpret_cast<const uint4 *>(C + t * a.C_stride + e);
             }
         }
         if (row == (int)first) {
             ssm_load8(a.A + at, A2);
-#pragma unroll
-            for (int p = 0; p < 4; ++p) A2[p] = __fmul2_rn(A2[p], both(1.4426950408889634f));
             if (a.bias) bias = a.bias[cc];
             if (a.D) skip = a.D[cc];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) A2[p] = __fmul2_rn(A2[p], both(1.4426950408889634f));
         }
+        float out[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (slot[u] < 0) continue;
-            const float v = to_f32(d[u]) + bias, xf = to_f32(xv[u]);
+            Row &r = rows[u];
+            const float v = to_f32(r.d) + bias, xf = to_f32(r.x);
             float2 unused, y = both(0.f);
             const float delta = a.softplus ? ssm_softplus(both(v), unused).x : v, in = delta * xf;
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                const float2 bp = load2(b[u].e + 2 * p), cp = load2(cv[u].e + 2 * p);
-                h[u][p] = __ffma2_rn(ssm_decay(A2[p], delta), h[u][p], __fmul2_rn(bp, both(in)));
-                y = __ffma2_rn(cp, h[u][p], y);
+                r.h[p] = __ffma2_rn(ssm_decay(A2[p], delta), r.h[p], __fmul2_rn(load2(r.b.e + 2 * p), both(in)));
+                y = __ffma2_rn(load2(r.c.e + 2 * p), r.h[p], y);
             }
-            float o = y.x + y.y;
+            out[u] = y.x + y.y;
 #pragma unroll
-            for (int k = LN / 2; k > 0; k >>= 1) o += __shfl_xor_sync(0xffffffffu, o, k);
-            if (!live) continue;
-            ssm_store8(a.S_out + slot[u] * pitch + at, h[u]);
-            if (nl == 0) {
-                o = fmaf(skip, xf, o);
-                if (a.z) {
-                    const float g = to_f32(zv[u]);
-                    o *= g * sigmoid(g);
-                }
-                static_cast<IO *>(a.out)[(size_t)(row + u) * a.D_ + cc] = from_f32<IO>(o);
+            for (int k = LN / 2; k > 0; k >>= 1) out[u] += __shfl_xor_sync(0xffffffffu, out[u], k);
+            out[u] = fmaf(skip, xf, out[u]);
+            if (a.z) {
+                const float g = to_f32(r.z);
+                out[u] *= g * sigmoid(g);
             }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (rows[u].slot < 0 || !live) continue;
+            ssm_store8(a.S_out + rows[u].slot * pitch + at, rows[u].h);
+            if (nl == 0) static_cast<IO *>(a.out)[(size_t)(row + u) * a.D_ + cc] = from_f32<IO>(out[u]);
         }
     }
 }
