@@ -405,8 +405,9 @@ int deltalog_scan_backward(const deltalog_desc *desc, const deltalog_plan *plan,
  * place in other layers.  Packed sequences come with a plan (the calls read starts, token_seq and, for prefill, scan_slots),
  * single tokens with a slot list, as above.  `x_stride` and its like are elements from one token to the next: a token's own
  * values are dense, the tokens may be columns of a wider tensor.  Addresses and strides are multiples of 16 bytes where
- * nothing else is said.  Sums, statistics and states are fp32; 16-bit outputs and gradients are rounded once.  Every call
- * gives the same bits for the same arguments.
+ * nothing else is said.  Outputs do not overlap inputs where nothing else is said (the convolution's calls over a plan refuse it).
+ * Sums, statistics and states are fp32; 16-bit outputs and gradients are rounded once.  Every call gives the same bits for the
+ * same arguments.
  */
 
 /*

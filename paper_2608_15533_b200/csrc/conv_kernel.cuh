@@ -162,7 +162,13 @@ __global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvAr
         begin = r >= 0 ? a.rows.starts[r] : 0;
         end = r >= 0 ? a.rows.starts[r + 1] : a.max_tokens;
     };
-    enter(a.rows.of(t0));
+    const int row0 = a.rows.of(t0);
+    if (row0 < 0) {  // all of the run is behind the last sequence
+        if (a.clear && live)
+            for (int t = t0; t < t1; ++t) pack_store(out + (size_t)t * a.C, pack_zero<IO, V>());
+        return;
+    }
+    enter(row0);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) p[j] = quad(win[j]);
     for (int t = t0; t < t1; t += U) {

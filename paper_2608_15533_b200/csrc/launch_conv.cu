@@ -29,6 +29,13 @@ void conv_plan(ConvArgs &a, const deltalog_plan *p) {
     a.max_tokens = p->max_tokens;
 }
 
+// A run reads inputs that another run owns: the output must not lie over them.
+bool conv_overlaps(const deltalog_conv_desc *d, const void *x, int64_t x_stride, const void *out, int32_t tokens) {
+    const uint64_t size = d->io_dtype == DELTALOG_F32 ? 4 : 2, t = tokens;
+    const uint64_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(out);
+    return t > 0 && a < b + t * d->channels * size && b < a + ((t - 1) * x_stride + d->channels) * size;
+}
+
 constexpr int kWarpsPerCta = kConvThreads / 32;
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
@@ -97,6 +104,7 @@ int deltalog_conv_prefill(const deltalog_conv_desc *desc, void *window, const de
     if (int rc = validate_conv(desc, x, x_stride, weight, bias)) return rc;
     if (int rc = validate_plan(plan)) return rc;
     if (desc->num_slots <= 0 || !window || !out || !aligned16(window) || !aligned16(out)) return DELTALOG_ERR_INVALID_ARG;
+    if (conv_overlaps(desc, x, x_stride, out, plan->max_tokens)) return DELTALOG_ERR_INVALID_ARG;
     if (plan->n == 0) return DELTALOG_OK;
     ConvArgs a = conv_args(desc, x, x_stride, weight, bias);
     conv_plan(a, plan);
@@ -110,6 +118,7 @@ int deltalog_conv_forward(const deltalog_conv_desc *desc, const deltalog_plan *p
     if (int rc = validate_conv(desc, x, x_stride, weight, bias)) return rc;
     if (int rc = validate_plan(plan)) return rc;
     if (!out || !aligned16(out) || !aligned16(init) || !aligned16(final)) return DELTALOG_ERR_INVALID_ARG;
+    if (conv_overlaps(desc, x, x_stride, out, plan->max_tokens)) return DELTALOG_ERR_INVALID_ARG;
     if (plan->n == 0) return DELTALOG_OK;
     ConvArgs a = conv_args(desc, x, x_stride, weight, bias);
     conv_plan(a, plan);
@@ -134,6 +143,7 @@ int deltalog_conv_backward(const deltalog_conv_desc *desc, const deltalog_plan *
     if (!dout || !grads || !grads->x || !grads->weight || rows < plan->max_tokens) return DELTALOG_ERR_INVALID_ARG;
     if (!aligned16(init) || !aligned16(dout) || !aligned16(dfinal) || !aligned16(grads->x) || !aligned16(grads->init)) return DELTALOG_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace) || workspace_bytes < deltalog_conv_workspace_bytes(desc, rows)) return DELTALOG_ERR_INVALID_ARG;
+    if (conv_overlaps(desc, x, x_stride, grads->x, rows) || conv_overlaps(desc, dout, desc->channels, grads->x, rows)) return DELTALOG_ERR_INVALID_ARG;
     if (plan->n == 0) return DELTALOG_OK;
     ConvArgs a = conv_args(desc, x, x_stride, weight, bias);
     conv_plan(a, plan);

@@ -16,7 +16,7 @@ int backward(const SsmArgs &a, cudaStream_t s) {
         local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
     }
-    const unsigned rest = a.dS_init ? 1 : 0;
+    const unsigned rest = a.dS_init ? ssm_empty_ctas(a.rows.n) : 0;
     if (a.spans + rest > 0) {
         auto kernel = ssm_backward_kernel<IO, N, false>;
         if (int rc = ensure_smem(kernel, smem)) return rc;

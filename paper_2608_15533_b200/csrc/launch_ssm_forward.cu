@@ -18,8 +18,8 @@ int forward(const SsmArgs &a, cudaStream_t s) {
     }
     auto kernel = ssm_forward_kernel<IO, N, false, WIDE>;
     if (int rc = ensure_smem(kernel, smem)) return rc;
-    // one more row of CTAs for the rows without tokens, whose states a training call hands on
-    const unsigned rest = a.S_out && !a.slots ? 1 : 0;
+    // more CTAs behind them for the rows without tokens, whose states a training call hands on
+    const unsigned rest = a.S_out && !a.slots ? ssm_empty_ctas(a.rows.n) : 0;
     if (a.spans + rest == 0) return DELTALOG_OK;
     kernel<<<dim3(cols, (unsigned)a.spans + rest), kSsmThreads, smem, s>>>(a);
     return finish_launch();

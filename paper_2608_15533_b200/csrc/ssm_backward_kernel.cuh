@@ -63,19 +63,18 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
             if (mine(q)) ssm_store(p + at(state, q), v[q]);
     };
     if (!LOCAL && span >= a.spans) {  // rows without tokens hand on what they get
-        for (int row = 0; row < a.rows.n; ++row) {
-            if (a.rows.starts[row] != a.rows.starts[row + 1]) continue;
+        ssm_empty_rows(a, span - a.spans, [&](int row) {
             float2 v[KC][2];
             load(a.dS_final, row, v);
             store(a.dS_init, row, v);
-        }
+        });
         return;
     }
-    const int lo = span * a.span;
-    int hi = (int)min((long long)a.total_rows, (long long)lo + a.span), only = -1;
+    const int lo = span * a.span, bound = (int)min((long long)a.total_rows, (long long)lo + a.span);
+    int hi = max(lo, min(bound, a.rows.starts[a.rows.n])), only = -1;  // the tokens that there are
     if (LOCAL) {
         const SsmToken head = ssm_token(a, lo, false);
-        if (head.row < 0 || head.begin >= lo) return;
+        if (hi == lo || head.row < 0 || head.begin >= lo) return;
         only = head.row;
         hi = min(hi, head.end);
     }
@@ -92,7 +91,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
 #pragma unroll
         for (int p = 0; p < 2; ++p) A2[q][p] = __fmul2_rn(A2[q][p], both(1.4426950408889634f)), carry[q][p] = dA[q][p] = both(0.f);
     }
-    if (!LOCAL && span + 1 < a.spans) {
+    if (!LOCAL && hi > lo) {
         const SsmToken last = ssm_token(a, hi - 1, false);
         if (last.row >= 0 && last.end > hi) {  // a row that goes on: what the later stretches hand back, joined
             int j = (last.end - 1) / a.span;
@@ -132,11 +131,12 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
         else parts(std::false_type{});
         cp_async_commit();
     };
-    const int top = (hi - 1) & ~(TT - 1);  // lo is a multiple of the tile
-    fetch(top, 0);
-    // (tokens behind the plan's have no kept state)
-    auto fetch_kept = [&](int t) { load(t < a.max_tokens ? a.kept : nullptr, (size_t)t / U, kept); };
-    if (!LOCAL) fetch_kept((hi - 1) & ~(U - 1));
+    const int top = hi > lo ? (hi - 1) & ~(TT - 1) : lo - TT;  // lo is a multiple of the tile
+    auto fetch_kept = [&](int t) { load(a.kept, (size_t)t / U, kept); };
+    if (hi > lo) {
+        fetch(top, 0);
+        if (!LOCAL) fetch_kept((hi - 1) & ~(U - 1));
+    }
     int stage = 0;
     for (int t = top; t >= lo; t -= TT, stage ^= 1) {
         typename F::Raw &r = s.raw[stage];
@@ -337,11 +337,6 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                     if (k >= here) break;
                     const size_t to = (size_t)(t + k) * a.D_ + c0 + col;
                     IO *dx = static_cast<IO *>(a.dx) + to, *ddt = static_cast<IO *>(a.ddt) + to, *dz = static_cast<IO *>(a.dz) + (a.dz ? to : 0);
-                    if (!(there >> k & 1)) {
-                        store2(dx, both(0.f)), store2(ddt, both(0.f));
-                        if (a.dz) store2(dz, both(0.f));
-                        continue;
-                    }
                     const float4 st = *reinterpret_cast<const float4 *>(s.step + n);
                     const float2 xf = load2(r.x + n), dy = load2(s.dy + n), sB = load2(s.sums[1] + sn), sA = load2(s.sums[2] + sn);
                     float2 g = __ffma2_rn(xf, sB, __fmul2_rn(sA, both(0.6931471805599453f)));
@@ -366,6 +361,12 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                 if (mine(q)) a.sums[(size_t)span * a.D_ + c0 + first + q * LC] = sum[q];
     } else {
         store(a.part_A, span, dA);
+        if (col < cols)  // behind the last sequence
+            for (int t = hi + col_token; t < bound; t += kTokenStep) {
+                const size_t to = (size_t)t * a.D_ + c0 + col;
+                store2(static_cast<IO *>(a.dx) + to, both(0.f)), store2(static_cast<IO *>(a.ddt) + to, both(0.f));
+                if (a.dz) store2(static_cast<IO *>(a.dz) + to, both(0.f));
+            }
         // dD and dbias: over the threads that share a pair of channels
         __syncthreads();
         float *over = &s.sums[0][0];  // [2][kTokenStep][CB]

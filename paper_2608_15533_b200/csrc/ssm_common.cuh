@@ -165,4 +165,23 @@ __device__ __forceinline__ SsmToken ssm_token(const SsmArgs &a, int t, bool tell
     return k;
 }
 
+// f(row) for the rows without tokens among the share of one CTA of a grid's last rows, by every thread.
+constexpr int kSsmEmptyRows = 1024;
+inline unsigned ssm_empty_ctas(int n) {
+    const long long ctas = ((long long)n + kSsmEmptyRows - 1) / kSsmEmptyRows;
+    return (unsigned)(ctas < 32768 ? ctas : 32768);
+}
+template <typename F>
+__device__ __forceinline__ void ssm_empty_rows(const SsmArgs &a, int share, F f) {
+    const int lane = threadIdx.x & 31, shares = gridDim.y - a.spans;
+    const int each = ((a.rows.n + shares - 1) / shares + 31) & ~31;
+    const long long first = (long long)share * each;
+    const int end = (int)min((long long)a.rows.n, first + each);
+    for (int row = (int)min(first, (long long)end); row < end; row += 32) {
+        const int mine = min(row + lane, end - 1);
+        unsigned empty = __ballot_sync(0xffffffffu, row + lane < end && a.rows.starts[mine] == a.rows.starts[mine + 1]);
+        for (; empty; empty &= empty - 1) f(row + __ffs(empty) - 1);
+    }
+}
+
 }  // namespace deltalog

@@ -46,19 +46,20 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
     auto mine = [&](int q) { return first + q * LC < cols; };
 
     if (!LOCAL && span >= a.spans) {  // rows without tokens: their state is the one they came with
-        for (int row = 0; row < a.rows.n; ++row) {
-            if (a.rows.starts[row] != a.rows.starts[row + 1]) continue;
+        ssm_empty_rows(a, span - a.spans, [&](int row) {
 #pragma unroll
             for (int q = 0; q < KC; ++q)
                 if (mine(q))
                     *reinterpret_cast<float4 *>(a.S_out + at(row, q)) =
                         a.S_in ? *reinterpret_cast<const float4 *>(a.S_in + at(row, q)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+        });
         return;
     }
-    const int lo = span * a.span, hi = (int)min((long long)a.max_tokens, (long long)lo + a.span);
+    const int lo = span * a.span, bound = (int)min((long long)a.max_tokens, (long long)lo + a.span);
+    const int hi = max(lo, min(bound, a.rows.starts[a.rows.n]));  // the tokens that there are
     int from = lo, only = -1;  // LOCAL: the open row alone
     if (LOCAL) {
+        if (hi == lo) return;
         const SsmToken last = ssm_token(a, hi - 1, false);
         if (last.row < 0 || last.end <= hi) return;
         only = last.row;
@@ -208,10 +209,16 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
                 for (int j = 0; j < (4 * KC > LN ? 4 * KC / LN : 1); ++j) s.step[(k0 + (v0 + j) / KC) * PB + first + (v0 + j) % KC * LC].x = y[j];
             }
         };
-        for (int k0 = 0; k0 < min(TT, hi - t); k0 += 4) {
-            if (!LOCAL && a.kept && k0 % kSsmBlock == 0) store_state(a.kept, (size_t)(t + k0) / kSsmBlock);
-            if ((begins | ends) >> k0 & 15) four(k0, std::true_type{});
-            else four(k0, std::false_type{});
+        const int here = min(TT, hi - t);
+        for (int k0 = 0; k0 < here; k0 += 8) {
+            if (!LOCAL && a.kept) store_state(a.kept, (size_t)(t + k0) / kSsmBlock);
+            if ((begins | ends) >> k0 & 255) {
+                four(k0, std::true_type{});
+                four(k0 + 4, std::true_type{});
+            } else {  // (eight tokens without a branch: one group's sums run beside the next one's decays)
+                four(k0, std::false_type{});
+                four(k0 + 4, std::false_type{});
+            }
         }
         __syncthreads();
         if (LOCAL) continue;
@@ -236,6 +243,8 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
             }
         }
     }
+    if (!LOCAL && a.out && a.clear && col < cols)  // behind the last sequence
+        for (int t = hi + col_token; t < bound; t += kTokenStep) store2(static_cast<IO *>(a.out) + (size_t)t * a.D_ + c0 + col, both(0.f));
     if (LOCAL) {
         store_state(a.local, span);
         if (nl == 0)

@@ -205,6 +205,22 @@ def test_offsets_beyond_32_bits():
     torch.cuda.empty_cache()
 
 
+def test_a_plan_for_many_more_tokens():
+    rows, C, bound = 500, 64, 3000
+    lens = [0] * rows
+    lens[7], lens[499] = 2, 90
+    x, w, b = _inputs((bound + 5,), C, 4, torch.float32)
+    x[92:] = float("nan")
+    plan = dl.Plan(rows, bound, device=DEV)
+    dl.build_plan(torch.tensor(lens, dtype=torch.int32, device=DEV), plan)
+    desc = dl.ConvDesc(C, 4, dl.F32)
+    out, final = dl.conv_forward(desc, plan, x, w, b)
+    _check_forward(out[:92], final[[7, 499]], x[:92], w, b, torch.zeros(2, 3, C, dtype=ref.F64), (2, 90), True)
+    d = dl.conv_backward(desc, plan, x, w, b, torch.where(torch.isnan(x), x, torch.ones_like(x)))
+    assert not out[92:].any() and not d.x[92:].any() and torch.isfinite(d.weight).all() and torch.isfinite(d.x).all()
+    assert not final[[0, 250, 498]].any() and not d.init[[0, 250, 498]].any()
+
+
 def test_streams_and_replays():
     lens, C = (20, 7), 256
     x, w, b = _inputs(lens, C, 4, torch.bfloat16)

@@ -213,6 +213,43 @@ def test_a_prompt_in_parts_and_token_by_token_is_the_prompt():
     ref.close(part.S, ref.f64(whole.S), mag[1], rel, "S")
 
 
+def test_a_plan_for_many_more_tokens_and_rows_without_any():
+    # a captured step's plan: its bounds are fixed, this step brings few tokens; what lies behind them may be anything
+    rows, D, N, bound = 3000, 40, 16, 4000
+    lens = [0] * rows
+    for i, n in ((5, 3), (700, 150), (2999, 20)):
+        lens[i] = n
+    T = sum(lens)
+    c = _case(bound + 9, D, N, 1, torch.float32)
+    for k in ("x", "dt", "B", "C", "z"):
+        c[k][T:] = float("nan")
+    desc, plan = dl.SsmDesc(D, N, 1, dl.F32), dl.Plan(rows, bound, device=DEV)
+    dl.build_plan(torch.tensor(lens, dtype=torch.int32, device=DEV), plan)
+    S0, dS = torch.randn(rows, D, N, device=DEV), torch.randn(rows, D, N, device=DEV)
+    work = dl.ssm_workspace(desc, rows, bound + 9, train=True, device=DEV)
+    work.fill_(0xff)
+    out, S = dl.ssm_forward(desc, plan, *_args(c), S_init=S0, workspace=work, save=True)
+    dout = torch.randn(bound + 9, D, device=DEV)
+    dout[T:] = float("nan")
+    d = dl.ssm_backward(desc, plan, *_args(c), dout, S_init=S0, dS_final=dS, workspace=work, saved=True)
+    cut = {k: v[:T] if k in ("x", "dt", "B", "C", "z") else v for k, v in c.items()}
+    live = [5, 700, 2999]
+    want, mag = (ref.ssm(cut, [3, 150, 20], S0[live], dout[:T], dS[live], mag=m) for m in (False, True))
+    rel = _rel(cut, [150])
+    ref.close(out[:T], want[0], mag[0], rel, "out")
+    ref.close(S[live], want[1], mag[1], rel, "S")
+    dead = torch.ones(rows, dtype=torch.bool, device=DEV)
+    dead[live] = False
+    assert not out[T:].any() and torch.equal(S[dead], S0[dead]) and torch.equal(d.S_init[dead], dS[dead])
+    for k in ("x", "dt", "B", "C", "z"):
+        got = getattr(d, k)
+        assert not got[T:].any()
+        ref.close(got[:T], want[2][k], mag[2][k] + want[2][k].abs(), 2 * rel, "d" + k)
+    for k in ("A", "D", "dt_bias"):
+        ref.close(getattr(d, k), want[2][k], mag[2][k], 2 * rel + T * 2.0 ** -24, "d" + k)
+    ref.close(d.S_init[live], want[2]["S_init"], mag[2]["S_init"], 2 * rel, "dS_init")
+
+
 def test_step_sizes_at_their_ends():
     # delta = 0 leaves the state as it is, a large one replaces it; both without NaN
     D, N = 16, 16

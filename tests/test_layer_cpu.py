@@ -61,6 +61,11 @@ def test_conv_refusals(lib):
     for kw in (dict(dout=None), dict(rows=99), dict(ws=None), dict(ws=0xa00008), dict(size=0), dict(dfinal=0x900002), dict(grads=dict(x=None)), dict(grads=dict(weight=None)),
                dict(grads=dict(x=0xb00004))):
         assert _conv("backward", lib, **kw) == INV, kw
+    for call in ("prefill", "forward"):   # a run reads what its neighbour owns: never in place
+        for out in (0x200000, 0x200010, 0x200000 - 99 * 128):
+            assert _conv(call, lib, out=out) == INV
+        assert _conv(call, lib, out=0x200000 - 100 * 128, plan=_plan(n=0)) == OK
+    assert _conv("backward", lib, grads=dict(x=0x200000)) == INV and _conv("backward", lib, grads=dict(x=0x800000)) == INV
     need = lib.deltalog_conv_workspace_bytes(ctypes.byref(binding._ConvDesc(64, 4, dl.BF16, 1, 4, 0)), 100)
     assert need > 0 and _conv("backward", lib, size=need - 1) == INV
     assert dl.launch_count() == before
