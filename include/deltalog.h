@@ -527,7 +527,7 @@ typedef struct {
 int deltalog_ssm_step(const deltalog_ssm_desc *desc, float *S, const deltalog_ssm_inputs *in, const int32_t *slot_idx, int32_t B, void *out,
                       int32_t *status, void *stream);
 
-/* Bytes of workspace for max_tokens tokens or fewer: train == 0 for prefill and forward without save, train != 0 for save and
+/* Bytes of workspace for max_tokens tokens (2^30 at most) or fewer: train == 0 for prefill and forward without save, train != 0 for save and
  * the backward pass, where max_tokens is the rows of the token tensors.  0: invalid. */
 size_t deltalog_ssm_workspace_bytes(const deltalog_ssm_desc *desc, int32_t n, int32_t max_tokens, int32_t train);
 

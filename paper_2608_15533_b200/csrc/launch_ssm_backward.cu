@@ -13,8 +13,9 @@ int backward(const SsmArgs &a, cudaStream_t s) {
     if (a.spans > 1) {
         auto local = ssm_backward_kernel<IO, N, true>;
         if (int rc = ensure_smem(local, smem)) return rc;
-        local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
+        local<<<dim3(cols, (unsigned)a.parts), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
+        if (int rc = launch_ssm_join<true>(a, N, s)) return rc;
     }
     const unsigned rest = a.dS_init ? ssm_empty_ctas(a.rows.n) : 0;
     if (a.spans + rest > 0) {

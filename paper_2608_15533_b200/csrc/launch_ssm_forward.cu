@@ -13,8 +13,9 @@ int forward(const SsmArgs &a, cudaStream_t s) {
     if (a.spans > 1) {
         auto local = ssm_forward_kernel<IO, N, true, WIDE>;
         if (int rc = ensure_smem(local, smem)) return rc;
-        local<<<dim3(cols, (unsigned)(a.spans - 1)), kSsmThreads, smem, s>>>(a);
+        local<<<dim3(cols, (unsigned)((a.spans - 1) * (a.span / a.part))), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
+        if (int rc = launch_ssm_join<false>(a, N, s)) return rc;
     }
     auto kernel = ssm_forward_kernel<IO, N, false, WIDE>;
     if (int rc = ensure_smem(kernel, smem)) return rc;

@@ -29,7 +29,10 @@ int validate_ssm(const deltalog_ssm_desc *d, const deltalog_ssm_inputs *in) {
     return DELTALOG_OK;
 }
 
+constexpr int32_t kMostTokens = 1 << 30;  // (a stretch is rounded up, and its end has to fit an int)
+
 int validate_room(const deltalog_ssm_desc *d, int32_t tokens, bool train, const void *workspace, size_t bytes) {
+    if (tokens > kMostTokens) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     if (!workspace || !aligned16(workspace) || bytes < ssm_layout(d, tokens, train).total) return DELTALOG_ERR_INVALID_ARG;
     return DELTALOG_OK;
 }
@@ -47,9 +50,9 @@ SsmArgs ssm_args(const deltalog_ssm_desc *d, const deltalog_ssm_inputs *in) {
 void ssm_forward_args(const deltalog_ssm_desc *d, const deltalog_plan *p, int32_t room, bool train, void *workspace, SsmArgs &a) {
     a.rows = Rows{p->starts, p->token_seq, p->n};
     a.max_tokens = p->max_tokens;
-    const SsmForm form = ssm_forward_form(d, p->max_tokens);
-    const SsmCut c = ssm_cut(d, p->max_tokens, form);
-    a.span = c.span, a.spans = c.spans, a.blocks = c.blocks, a.wide = form == kSsmWide;
+    const SsmForm form = ssm_forward_form(d, p->n, p->max_tokens);
+    const SsmCut c = ssm_cut(d, p->n, p->max_tokens, form);
+    a.span = c.span, a.spans = c.spans, a.part = c.part, a.parts = c.parts, a.blocks = c.blocks, a.wide = form == kSsmWide;
     const SsmLayout l = ssm_layout(d, room, train);
     char *w = static_cast<char *>(workspace);
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
@@ -73,7 +76,7 @@ int deltalog_ssm_step(const deltalog_ssm_desc *desc, float *S, const deltalog_ss
 }
 
 size_t deltalog_ssm_workspace_bytes(const deltalog_ssm_desc *desc, int32_t n, int32_t max_tokens, int32_t train) {
-    if (validate_ssm_desc(desc) || n < 0 || max_tokens < 0) return 0;
+    if (validate_ssm_desc(desc) || n < 0 || max_tokens < 0 || max_tokens > kMostTokens) return 0;
     return ssm_layout(desc, max_tokens, train != 0).total;
 }
 
@@ -129,8 +132,8 @@ int deltalog_ssm_backward(const deltalog_ssm_desc *desc, const deltalog_plan *pl
     const SsmLayout l = ssm_layout(desc, rows, true);
     char *w = static_cast<char *>(workspace);
     auto floats = [&](size_t off) { return reinterpret_cast<float *>(w + off); };
-    const SsmCut c = ssm_cut(desc, rows, kSsmBack);
-    a.span = c.span, a.spans = c.spans, a.blocks = c.blocks, a.total_rows = rows;
+    const SsmCut c = ssm_cut(desc, plan->n, rows, kSsmBack);
+    a.span = c.span, a.spans = c.spans, a.part = c.part, a.parts = c.parts, a.blocks = c.blocks, a.total_rows = rows;
     a.part_bc = floats(l.part_bc), a.part_A = floats(l.part_A), a.part_cols = floats(l.part_cols);
     a.dout = dout, a.dS_final = dS_final;
     a.dx = grads->x, a.ddt = grads->dt, a.dB = grads->B, a.dC = grads->C, a.dz = in->z ? grads->z : nullptr;

@@ -35,7 +35,8 @@ template <typename IO, int N> struct SsmBackward {
     };
 };
 
-// LOCAL: the first pass over a stretch whose first row began in front of it: the adjoint that the stretch alone hands back.
+// LOCAL: the first pass over a part of a stretch (`span` is the part), where its first row began in front of the stretch: the adjoint
+// that the part alone hands back.
 template <typename IO, int N, bool LOCAL>
 __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmArgs a) {
     using F = SsmBackward<IO, N>;
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per_group = a.D_ / a.G, group = blockIdx.x / a.blocks, in_group = (blockIdx.x % a.blocks) * CB;
     const int c0 = group * per_group + in_group, cols = min(CB, per_group - in_group);
-    const int span = LOCAL ? blockIdx.y + 1 : blockIdx.y;
+    const int span = blockIdx.y;
     const int nl = lane & (LN - 1), cl = lane / LN;
     const int first = warp * KC * LC + cl;  // this lane's channels of the block: first, first + LC
     auto at = [&](size_t state, int q) { return (state * a.D_ + c0 + first + q * LC) * N + nl * 4; };
@@ -70,11 +71,11 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
         });
         return;
     }
-    const int lo = span * a.span, bound = (int)min((long long)a.total_rows, (long long)lo + a.span);
+    const int length = LOCAL ? a.part : a.span, lo = span * length, bound = (int)min((long long)a.total_rows, (long long)lo + length);
     int hi = max(lo, min(bound, a.rows.starts[a.rows.n])), only = -1;  // the tokens that there are
     if (LOCAL) {
         const SsmToken head = ssm_token(a, lo, false);
-        if (hi == lo || head.row < 0 || head.begin >= lo) return;
+        if (hi == lo || head.row < 0 || head.begin >= lo / a.span * a.span) return;
         only = head.row;
         hi = min(hi, head.end);
     }
@@ -93,20 +94,7 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
     }
     if (!LOCAL && hi > lo) {
         const SsmToken last = ssm_token(a, hi - 1, false);
-        if (last.row >= 0 && last.end > hi) {  // a row that goes on: what the later stretches hand back, joined
-            int j = (last.end - 1) / a.span;
-            load(a.local, j, carry);
-            for (--j; j > span; --j) {
-                float2 own[KC][2];
-                load(a.local, j, own);
-#pragma unroll
-                for (int q = 0; q < KC; ++q) {
-                    const float total = mine(q) ? a.sums[(size_t)j * a.D_ + c0 + first + q * LC] : 0.f;
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) carry[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(total))), carry[q][p], own[q][p]);
-                }
-            }
-        }
+        if (last.row >= 0 && last.end > hi) load(a.local, hi / a.part, carry);  // what the later stretches hand back to a row that goes on
     }
     // the two channels that this thread brings in and out, and its first token of a tile
     const int col = (tid % (CB / 2)) * 2, col_token = tid / (CB / 2);

@@ -4,9 +4,8 @@
 // A lane holds four neighbouring states of a channel (of two or four channels where the state is wide), d_state / 4 lanes a channel, and
 // walks down the tokens.  The packed tokens are cut into flat stretches of `span` tokens, whatever rows they belong to, one
 // CTA per stretch and block of channels, so that ragged rows load the SMs evenly.  A row that goes on behind the end of a
-// stretch is joined by a first pass over the stretch (ssm_local_kernel): the state that the stretch alone leaves, and the sum
-// of its step sizes, whose exponential with A is the decay across it.  The second pass starts from
-//     h = exp(A sum_j) (.. exp(A sum_i) h_i + h_(i+1) ..) + h_j.
+// stretch is joined by a first pass over parts of the stretch, so that it has more CTAs than the second: the state that a part alone
+// leaves, and the sum of its step sizes, whose exponential with A is the decay across it.  ssm_join_kernel puts them together.
 #pragma once
 
 #include <type_traits>
@@ -31,7 +30,8 @@ struct SsmArgs {
     int32_t D_, G, num_slots, softplus, clear;  // D_: channels
     int32_t max_tokens, total_rows;             // tokens that the plan reaches; rows of the token tensors
     int32_t span, spans, blocks, wide;          // stretches, blocks of channels per group, the forward pass's form
-    float *local, *front, *sums;                // [spans, D_, N] state a stretch leaves, its open row's first state; [spans, D_] step sizes
+    int32_t part, parts;                        // parts of stretches, in tokens and in all
+    float *local, *front, *sums;                // [parts, D_, N] state a part leaves, its open row's first state; [parts, D_] step sizes
     float *kept;                                // [max_tokens / 8, D_, N], or NULL
     // backward
     const void *dout;

@@ -29,7 +29,7 @@ template <typename IO, int N, bool WIDE> struct SsmForward {
     };
 };
 
-// LOCAL: the first pass over a stretch whose last row goes on behind it.
+// LOCAL: the first pass over a part of a stretch (`span` is the part), where its last row goes on behind the stretch.
 template <typename IO, int N, bool LOCAL, bool WIDE>
 __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas)) ssm_forward_kernel(const SsmArgs a) {
     using F = SsmForward<IO, N, WIDE>;
@@ -55,13 +55,13 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
         });
         return;
     }
-    const int lo = span * a.span, bound = (int)min((long long)a.max_tokens, (long long)lo + a.span);
+    const int length = LOCAL ? a.part : a.span, lo = span * length, bound = (int)min((long long)a.max_tokens, (long long)lo + length);
     const int hi = max(lo, min(bound, a.rows.starts[a.rows.n]));  // the tokens that there are
     int from = lo, only = -1;  // LOCAL: the open row alone
     if (LOCAL) {
         if (hi == lo) return;
         const SsmToken last = ssm_token(a, hi - 1, false);
-        if (last.row < 0 || last.end <= hi) return;
+        if (last.row < 0 || last.end <= (lo / a.span + 1ll) * a.span) return;
         only = last.row;
         from = max(lo, last.begin) & ~(TT - 1);
     }
@@ -109,20 +109,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
     }
     if (!LOCAL && span > 0) {
         const SsmToken head = ssm_token(a, lo, false);
-        if (head.row >= 0 && head.begin < lo) {  // a row from an earlier stretch: its states joined
-            int j = head.begin / a.span;
-            load_state(a.local, j, h);
-            for (++j; j < span; ++j) {
-                float2 own[KC][2];
-                load_state(a.local, j, own);
-#pragma unroll
-                for (int q = 0; q < KC; ++q) {
-                    const float total = mine(q) ? a.sums[(size_t)j * a.D_ + c0 + first + q * LC] : 0.f;
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) h[q][p] = __ffma2_rn(exp2_fast(__fmul2_rn(A2[q][p], both(total))), h[q][p], own[q][p]);
-                }
-            }
-        }
+        if (head.row >= 0 && head.begin < lo) load_state(a.local, lo / a.part - 1, h);  // a row from an earlier stretch
     }
     // the two channels that this thread brings in and out, and its first token of a tile
     const int col = (tid % (CB / 2)) * 2, col_token = tid / (CB / 2);
@@ -182,7 +169,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
                     const int k = k0 + i;
                     const bool old = a.S_in && !(a.fresh && a.fresh[s.row[k]]);
                     // another CTA may have written the pool's state of an open row already: the first pass kept it
-                    if (!LOCAL && a.front && (s.open >> k & 1)) load_state(a.front, span, h);
+                    if (!LOCAL && a.front && (s.open >> k & 1)) load_state(a.front, (t + k) / a.part, h);
                     else load_state(old ? a.S_in : nullptr, s.state[k], h);
                     if (LOCAL && a.front) store_state(a.front, span);
                 }

@@ -3,13 +3,14 @@
 #pragma once
 
 #include "launch_common.cuh"
-#include "ssm_common.cuh"
+#include "ssm_join_kernel.cuh"
 
 namespace deltalog {
 
 inline long long ssm_ceil(long long a, long long b) { return (a + b - 1) / b; }
 
 constexpr int kSsmSpanMin = 128;  // tokens of a stretch at least
+constexpr int kSsmParts = 2;          // parts of a stretch in the first pass: the stretches alone would leave it a wave with gaps
 
 // How the forward pass (`wide` or not) or the backward pass cuts channels into blocks and tokens into stretches.
 enum SsmForm { kSsmWide, kSsmNarrow, kSsmBack };
@@ -24,17 +25,21 @@ inline int ssm_most_spans(const deltalog_ssm_desc *d, SsmForm form) {
     const int blocks = ssm_blocks(d, form) * d->groups, wave = 148 * (form == kSsmBack || d->d_state == 64 ? 3 : 4);
     return blocks >= wave ? 1 : wave / blocks;
 }
-struct SsmCut { int span, spans, blocks; };
-inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t tokens, SsmForm form) {
-    const long long span = ssm_ceil(ssm_ceil(tokens, ssm_most_spans(d, form)), 32) * 32;
+struct SsmCut { int span, spans, part, parts, blocks; };
+inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t rows, int32_t tokens, SsmForm form) {
+    long long span = ssm_ceil(tokens, ssm_most_spans(d, form)), round = kSsmSpanMin;
+    // (documents of round lengths end where stretches of round lengths do, which then need no first pass: up to an eighth more)
+    while (round < span) round *= 2;
+    if (span < kSsmSpanMin || (rows > 1 && round - span <= span / 8)) span = round;
+    const long long part = ssm_ceil(span, 32 * kSsmParts) * 32;
     SsmCut c;
-    c.span = (int)(span < kSsmSpanMin ? kSsmSpanMin : span);
-    c.spans = (int)ssm_ceil(tokens, c.span), c.blocks = ssm_blocks(d, form);
+    c.part = (int)part, c.span = (int)(part * kSsmParts);
+    c.spans = (int)ssm_ceil(tokens, c.span), c.parts = (int)ssm_ceil(tokens, c.part), c.blocks = ssm_blocks(d, form);
     return c;
 }
 // Narrow where the wide form would leave SMs without a CTA.
-inline SsmForm ssm_forward_form(const deltalog_ssm_desc *d, int32_t tokens) {
-    const SsmCut c = ssm_cut(d, tokens, kSsmWide);
+inline SsmForm ssm_forward_form(const deltalog_ssm_desc *d, int32_t rows, int32_t tokens) {
+    const SsmCut c = ssm_cut(d, rows, tokens, kSsmWide);
     return (long long)c.spans * c.blocks * d->groups < 148 ? kSsmNarrow : kSsmWide;
 }
 // What ssm_cut gives at most for this many tokens or fewer.
@@ -56,11 +61,11 @@ inline SsmLayout ssm_layout(const deltalog_ssm_desc *d, int32_t tokens, bool tra
         return off;
     };
     SsmLayout l;
-    const int f = ssm_room(d, tokens, false), b = train ? ssm_room(d, tokens, true) : 0, joined = f > b ? f : b;
+    const int f = ssm_room(d, tokens, false), b = train ? ssm_room(d, tokens, true) : 0, joined = kSsmParts * (f > b ? f : b);
     l.kept = take(train, (size_t)ssm_ceil(tokens, kSsmBlock) * D * N * 4);
-    l.local = take(joined > 1, (size_t)joined * D * N * 4);
-    l.front = take(f > 1 && !train, (size_t)f * D * N * 4);
-    l.sums = take(joined > 1, (size_t)joined * D * 4);
+    l.local = take(f > 1 || b > 1, (size_t)joined * D * N * 4);
+    l.front = take(f > 1 && !train, (size_t)kSsmParts * f * D * N * 4);
+    l.sums = take(f > 1 || b > 1, (size_t)joined * D * 4);
     l.part_bc = take(train, (size_t)d->groups * ssm_blocks(d, kSsmBack) * tokens * 2 * N * 4);
     l.part_A = take(train, (size_t)b * D * N * 4);
     l.part_cols = take(train, (size_t)b * 2 * D * 4);
@@ -76,6 +81,14 @@ inline SsmLayout ssm_layout(const deltalog_ssm_desc *d, int32_t tokens, bool tra
     } while (0)
 #define SSM_STATES(IO, n_, CALL)                                                                         \
     if ((n_) == 8) { CALL(IO, 8); } else if ((n_) == 16) { CALL(IO, 16); } else if ((n_) == 32) { CALL(IO, 32); } else { CALL(IO, 64); }
+
+template <bool BACK>
+int launch_ssm_join(const SsmArgs &a, int states, cudaStream_t s) {
+    const size_t smem = (size_t)a.parts;
+    if (int rc = ensure_smem(ssm_join_kernel<BACK>, smem)) return rc;
+    ssm_join_kernel<BACK><<<(unsigned)ssm_ceil((long long)a.D_ * states / 4, 128), 128, smem, s>>>(a, states);
+    return finish_launch();
+}
 
 int launch_ssm_forward(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s);   // both passes
 int launch_ssm_step(const deltalog_ssm_desc *d, const SsmArgs &a, cudaStream_t s);
