@@ -19,11 +19,19 @@ inline int ssm_blocks(const deltalog_ssm_desc *d, SsmForm form) {
     return (int)ssm_ceil(d->channels / d->groups, form == kSsmWide || (form == kSsmBack && n != 64) ? wide : wide / 2);
 }
 
-// Stretches that the tokens are cut into at most: as many as one wave of CTAs has (a cut makes the row that crosses it run twice
-// behind its last border).  (148 SMs whatever the device: workspaces depend on it.)
+// Stretches that the tokens are cut into at most: as many as one wave of CTAs has, or two or three waves where those are filled
+// better by more than a twentieth (a cut makes the row that crosses it run twice behind its last border; of few blocks of
+// channels one wave may leave an SM in seven idle).  (148 SMs whatever the device: workspaces depend on it.)
 inline int ssm_most_spans(const deltalog_ssm_desc *d, SsmForm form) {
     const int blocks = ssm_blocks(d, form) * d->groups, wave = 148 * (form == kSsmBack || d->d_state == 64 ? 3 : 4);
-    return blocks >= wave ? 1 : wave / blocks;
+    if (blocks >= wave) return 1;
+    int best = wave / blocks;
+    double full = (double)best * blocks / wave;
+    for (int waves = 2; waves <= 3; ++waves) {
+        const int spans = waves * wave / blocks;
+        if ((double)spans * blocks / (waves * wave) > 1.05 * full) best = spans, full = (double)spans * blocks / (waves * wave);
+    }
+    return best;
 }
 struct SsmCut { int span, spans, part, parts, blocks; };
 inline SsmCut ssm_cut(const deltalog_ssm_desc *d, int32_t rows, int32_t tokens, SsmForm form) {
