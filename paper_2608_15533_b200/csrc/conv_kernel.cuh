@@ -31,6 +31,18 @@ struct ConvArgs {
 
 constexpr int kConvThreads = 128, kConvVec = 4;  // channels per lane: eight would need up to 200 registers
 
+// Inputs on their way: a lane copies its own channels of U tokens a stage into shared memory and reads nothing but its own, so that a
+// wait for its own copies is all it needs.  (Registers would have to hold them otherwise: half of a lane's, or half of the bytes in flight.)
+template <typename IO>
+__device__ __forceinline__ void conv_copy(Pack<IO, kConvVec> *dst, const IO *src) {
+    if constexpr (sizeof(IO) * kConvVec == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void conv_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+
 // Window of a row: slot or row, -1 for a row that the call skips.
 __device__ __forceinline__ int conv_slot(const ConvArgs &a, int row, bool tell) {
     if (!a.slots) return row;
@@ -146,12 +158,17 @@ __global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvAr
     if (first >= a.max_tokens) return;
     const int t0 = (int)first, t1 = (int)min((long long)a.max_tokens, first + a.run);
     // every load of the first tokens is on its way before the look-ups of the row, each of which waits for the one before
-    Pack<IO, V> in[U], win[W - 1];
-    auto fetch = [&](int t) {
+    constexpr int S = sizeof(IO) == 4 ? 2 : 3;
+    __shared__ Pack<IO, V> ring[kConvThreads / 32][S][U][32];
+    Pack<IO, V> win[W - 1];
+    auto fetch = [&](int t, int stage) {
+        if (t < t1)
 #pragma unroll
-        for (int u = 0; u < U; ++u) in[u] = input(min(t + u, t1 - 1));
+            for (int u = 0; u < U; ++u) conv_copy(&ring[warp][stage][u][lane], x + min(t + u, t1 - 1) * a.x_stride);
+        cp_async_commit();
     };
-    fetch(t0);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) fetch(t0 + s * U, s);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) win[j] = input(max(t0 - (W - 1) + j, 0));  // (of a row in front, perhaps: then it is not used)
     conv_weights<W>(a, cc, w, b);
@@ -166,19 +183,19 @@ __global__ void __launch_bounds__(kConvThreads) conv_forward_kernel(const ConvAr
     if (row0 < 0) {  // all of the run is behind the last sequence
         if (a.clear && live)
             for (int t = t0; t < t1; ++t) pack_store(out + (size_t)t * a.C, pack_zero<IO, V>());
+        conv_wait<0>();
         return;
     }
     enter(row0);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) p[j] = quad(win[j]);
-    for (int t = t0; t < t1; t += U) {
-        Pack<IO, V> cur[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) cur[u] = in[u];
-        if (t + U < t1) fetch(t + U);
+    for (int t = t0, stage = 0; t < t1; t += U, stage = stage == S - 1 ? 0 : stage + 1) {
+        fetch(t + (S - 1) * U, stage == 0 ? S - 1 : stage - 1);
+        conv_wait<S - 1>();
+        const Pack<IO, V> (*cur)[32] = ring[warp][stage];
         IO *to = out + (size_t)t * a.C;
         auto token = [&](int u) {
-            p[W - 1] = quad(cur[u]);
+            p[W - 1] = quad(cur[u][lane]);
             const Pack<IO, V> o = conv_act<IO>(conv_pre<W>(p, w, b), a.silu);
             conv_shift(p);
             return o;
@@ -260,7 +277,8 @@ __device__ __forceinline__ Quad conv_dpre(const Quad &pre, const Quad &g, bool s
 
 template <typename IO, int W>
 __global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_backward_kernel(const ConvArgs a, int col_blocks, long long head_blocks) {
-    constexpr int V = kConvVec, U = 4;
+    constexpr int V = kConvVec, U = 4, S = sizeof(IO) == 4 ? 2 : 4;
+    __shared__ Pack<IO, V> ring[kConvThreads / 32][S][2][U][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = ((int)(blockIdx.x % col_blocks) * 32 + lane) * V;
     const bool live = c < a.C;
@@ -306,15 +324,18 @@ __global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_
     for (int k = 0; k < W; ++k) pend[k] = quad_zero();
     if (t0 < t1) {
         const int tokens = a.rows.n ? a.rows.starts[a.rows.n] : 0, te = min(t1 + W - 1, tokens);  // tokens whose dpre counts
-        Pack<IO, V> in[U], dn[U];
-        auto fetch = [&](int t) {
+        auto fetch = [&](int t, int stage) {
+            if (t < te)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const long long at = max(0, min(t + u, te - 1));
-                in[u] = pack_load<IO, V>(x + at * a.x_stride), dn[u] = pack_load<IO, V>(dout + at * a.C);
-            }
+                for (int u = 0; u < U; ++u) {
+                    const long long at = min(t + u, te - 1);
+                    conv_copy(&ring[warp][stage][0][u][lane], x + at * a.x_stride);
+                    conv_copy(&ring[warp][stage][1][u][lane], dout + at * a.C);
+                }
+            cp_async_commit();
         };
-        if (t0 < te) fetch(t0);
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) fetch(t0 + s * U, s);
         conv_weights<W>(a, cc, w, b);
         int row = -1, begin = 0, end = 0;
         auto enter = [&](int t) {
@@ -329,11 +350,10 @@ __global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_
                 p[j] = quad(t >= begin ? pack_load<IO, V>(x + (size_t)t * a.x_stride) : window(row, W - 1 + t - begin));
             }
         }
-        for (int t = t0; t < t1 + W - 1; t += U) {
-            Pack<IO, V> cur[U], dcur[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) cur[u] = in[u], dcur[u] = dn[u];
-            if (t + U < te) fetch(t + U);
+        for (int t = t0, stage = 0; t < t1 + W - 1; t += U, stage = stage == S - 1 ? 0 : stage + 1) {
+            fetch(t + (S - 1) * U, stage == 0 ? S - 1 : stage - 1);
+            conv_wait<S - 1>();
+            const Pack<IO, V> (*cur)[U][32] = ring[warp][stage];
             IO *to = static_cast<IO *>(a.dx) + cc + ((long long)t - (W - 1)) * a.C;
             auto shift = [&]() {
 #pragma unroll
@@ -341,8 +361,8 @@ __global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_
                 pend[0] = quad_zero();
             };
             auto token = [&](int u, int reach, bool own) {  // dpre of a token, into its own and the `reach` pending dx in front
-                p[W - 1] = quad(cur[u]);
-                const Quad g = conv_dpre(conv_pre<W>(p, w, b), quad(dcur[u]), a.silu);
+                p[W - 1] = quad(cur[0][u][lane]);
+                const Quad g = conv_dpre(conv_pre<W>(p, w, b), quad(cur[1][u][lane]), a.silu);
                 if (own) {
                     dw[W].a = __fadd2_rn(dw[W].a, g.a), dw[W].b = __fadd2_rn(dw[W].b, g.b);
 #pragma unroll
@@ -381,7 +401,11 @@ __global__ void __launch_bounds__(kConvThreads, (sizeof(IO) == 4 ? 3 : 4)) conv_
             }
         }
     }
-    __shared__ float4 sums[kConvThreads / 32][W + 1][32];
+    // (the ring has room for the sums: every copy has arrived)
+    conv_wait<0>();
+    __syncthreads();
+    static_assert(sizeof(ring) >= sizeof(float4) * kConvThreads * (W + 1), "the sums fit");
+    auto sums = reinterpret_cast<float4 (*)[W + 1][32]>(&ring);
 #pragma unroll
     for (int j = 0; j <= W; ++j) sums[warp][j][lane] = make_float4(dw[j].a.x, dw[j].a.y, dw[j].b.x, dw[j].b.y);
     __syncthreads();

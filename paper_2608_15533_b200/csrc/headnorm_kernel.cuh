@@ -27,7 +27,7 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 128;
-constexpr int kNormHeads = 2, kNormHeadsBack = 1;  // heads in flight per lane
+constexpr int kNormHeads = 2, kNormHeadsBack = 1;  // heads of a lane's item
 
 // Where a lane's two runs of eight values are in a head, and whether they are.
 struct NormAt {
@@ -50,6 +50,33 @@ __device__ __forceinline__ void norm_load(const IO *p, const NormAt &at, bool th
         if (there && at.has_hi) *reinterpret_cast<uint4 *>(x[1].e + e) = *reinterpret_cast<const uint4 *>(p + at.hi + e);
     }
 }
+// Values on their way: a lane copies its own sixteen into shared memory and reads nothing but its own, so that a wait for its own copies
+// is all it needs.  Runs that a lane does not have are cleared once, before the first copy.
+constexpr int kNormStages = 3;
+template <typename IO> using NormSlot = Pack<IO, 8>[2][32];  // a head of a warp: two runs a lane
+template <typename IO>
+__device__ __forceinline__ void norm_copy(NormSlot<IO> &to, const IO *p, const NormAt &at, bool there, int lane) {
+    constexpr int V = 16 / sizeof(IO);
+#pragma unroll
+    for (int e = 0; e < 8; e += V) {
+        if (there && at.has_lo) cp_async16(to[0][lane].e + e, p + at.lo + e);
+        if (there && at.has_hi) cp_async16(to[1][lane].e + e, p + at.hi + e);
+    }
+}
+template <typename IO>
+__device__ __forceinline__ void norm_clear(NormSlot<IO> &to, const NormAt &at, int lane) {
+    if (!at.has_lo) to[0][lane] = pack_zero<IO, 8>();
+    if (!at.has_hi) to[1][lane] = pack_zero<IO, 8>();
+}
+template <typename IO>
+__device__ __forceinline__ void norm_read(const NormSlot<IO> &from, int lane, float (&f)[16]) {
+    const Pack<IO, 8> v[2] = {from[0][lane], from[1][lane]};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = to_f32(v[e / 8].e[e % 8]);
+}
+template <int N>
+__device__ __forceinline__ void norm_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+
 template <typename IO>
 __device__ __forceinline__ void norm_floats(const Pack<IO, 8> (&x)[2], float (&f)[16]) {
 #pragma unroll
@@ -145,61 +172,82 @@ __device__ __forceinline__ NormSide<IO> norm_side(const NormArgs &a, bool is_k) 
     return {static_cast<const IO *>(a.q), static_cast<const IO *>(a.dout_q), static_cast<IO *>(a.out_q), a.q_stride, a.w_q, a.q_scale, a.H_q};
 }
 
+// A warp walks over its items, two of which are on their way while one is computed.
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads, 7) head_norm_forward_kernel(const NormArgs a) {
-    constexpr int G = 32 / L, per = kNormHeads * G;
-    const int lane = threadIdx.x & 31, l = lane & (L - 1), group = lane / L;
-    const unsigned item = blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);  // (fewer than 2^31)
-    const unsigned cq = (a.H_q + per - 1) / per, chunks = cq + (a.H_k + per - 1) / per, chunk = item % chunks;
-    const int token = (int)(item / chunks);
-    if (token >= a.tokens) return;
-    const int position = a.rot ? a.positions[token] : 0;  // first: its tables' rows are two trips to memory away
-    const NormSide<IO> t = norm_side<IO>(a, chunk >= cq);
-    const int head = (int)(chunk >= cq ? chunk - cq : chunk) * per + group;
+__global__ void __launch_bounds__(kNormThreads, 5) head_norm_forward_kernel(const NormArgs a) {
+    constexpr int G = 32 / L, per = kNormHeads * G, S = kNormStages;
+    __shared__ NormSlot<IO> ring[kNormThreads / 32][S][kNormHeads];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
     const NormAt at = norm_at(a, l);
-    const IO *x = t.x + (size_t)token * t.stride;
-    IO *out = t.out + (size_t)token * t.heads * a.d;
-    Pack<IO, 8> raw[kNormHeads][2];
-#pragma unroll
-    for (int i = 0; i < kNormHeads; ++i) norm_load(x + (head + i * G) * a.d, at, head + i * G < t.heads, raw[i]);
-    float weight[16];
-    norm_weights(t.w, at, weight);
-    Turn turn;
-    const bool ok = norm_turn(a, position, l, turn);
+    const unsigned cq = (a.H_q + per - 1) / per, chunks = cq + (a.H_k + per - 1) / per;
+    const long long items = (long long)a.tokens * chunks, step = (long long)gridDim.x * (kNormThreads / 32);  // (fewer than 2^31)
     const float c = a.norm == DELTALOG_NORM_RMS ? 1.f / (float)a.d : 1.f;
+    long long item = (long long)blockIdx.x * (kNormThreads / 32) + warp;
+    if (item >= items) return;
 #pragma unroll
-    for (int i = 0; i < kNormHeads; ++i) {
-        float v[16], r = t.scale;
-        norm_floats(raw[i], v);
-        if (a.norm != DELTALOG_NORM_NONE) {
-            float ss = 0.f;
+    for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ss = fmaf(v[e], v[e], ss);
-            r *= rsqrtf(fmaf(c, lanes_sum<L>(ss), a.eps));
+        for (int i = 0; i < kNormHeads; ++i) norm_clear<IO>(ring[warp][s][i], at, lane);
+    int position[S];  // of the items on their way, the next first
+    auto fetch = [&](long long item, int stage, int &position) {
+        if (item < items) {
+            const unsigned token = (unsigned)item / chunks, chunk = (unsigned)item % chunks;
+            const NormSide<IO> t = norm_side<IO>(a, chunk >= cq);
+            const int head = (int)(chunk >= cq ? chunk - cq : chunk) * per + group;
+            const IO *x = t.x + token * t.stride;
+            position = a.rot ? a.positions[token] : 0;
+#pragma unroll
+            for (int i = 0; i < kNormHeads; ++i) norm_copy(ring[warp][stage][i], x + (head + i * G) * a.d, at, head + i * G < t.heads, lane);
         }
+        cp_async_commit();
+    };
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] *= r * weight[e];
-        norm_rotate<false>(a, turn, v);
-        if (head + i * G < t.heads) {
+    for (int s = 0; s < S - 1; ++s) fetch(item + s * step, s, position[s]);
+    for (int stage = 0; item < items; item += step, stage = stage == S - 1 ? 0 : stage + 1) {
+        Turn turn;
+        const bool ok = norm_turn(a, position[0], l, turn);
+        fetch(item + (S - 1) * step, stage == 0 ? S - 1 : stage - 1, position[S - 1]);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = ok ? v[e] : 0.f;
-            norm_store(out + (head + i * G) * a.d, at, v);
+        for (int s = 0; s < S - 1; ++s) position[s] = position[s + 1];
+        const unsigned token = (unsigned)item / chunks, chunk = (unsigned)item % chunks;
+        const NormSide<IO> t = norm_side<IO>(a, chunk >= cq);
+        const int head = (int)(chunk >= cq ? chunk - cq : chunk) * per + group;
+        float weight[16];
+        norm_weights(t.w, at, weight);
+        norm_wait<S - 1>();
+        IO *out = t.out + (size_t)token * t.heads * a.d;
+#pragma unroll
+        for (int i = 0; i < kNormHeads; ++i) {
+            float v[16], r = t.scale;
+            norm_read<IO>(ring[warp][stage][i], lane, v);
+            if (a.norm != DELTALOG_NORM_NONE) {
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ss = fmaf(v[e], v[e], ss);
+                r *= rsqrtf(fmaf(c, lanes_sum<L>(ss), a.eps));
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] *= r * weight[e];
+            norm_rotate<false>(a, turn, v);
+            if (head + i * G < t.heads) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = ok ? v[e] : 0.f;
+                norm_store(out + (head + i * G) * a.d, at, v);
+            }
         }
     }
 }
 
-// With weights the grid is fixed and every warp walks over its items of q, then over those of k, with the weights' gradient in
-// registers and the next item's values on their way; without, every warp has one item.
+// A warp walks over its items of q, then over those of k, with the weights' gradient in registers and two items on their way.
 template <typename IO, int L>
 __global__ void __launch_bounds__(kNormThreads, (sizeof(IO) == 4 ? 3 : 4)) head_norm_backward_kernel(const NormArgs a) {
-    constexpr int G = 32 / L, H = kNormHeadsBack, per = H * G;
-    __shared__ float sums[kNormThreads / 32][256];
+    constexpr int G = 32 / L, per = G, S = kNormStages;  // one head a lane
+    __shared__ NormSlot<IO> ring[kNormThreads / 32][S][2];  // gradient, value
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
     const bool weighted = a.w_q != nullptr, normed = a.norm != DELTALOG_NORM_NONE;
     const NormAt at = norm_at(a, l);
     const float c = a.norm == DELTALOG_NORM_RMS ? 1.f / (float)a.d : 1.f;
     const long long first = (long long)blockIdx.x * (kNormThreads / 32) + warp, step = (long long)gridDim.x * (kNormThreads / 32);
-    long long skipped = 0;  // items of the tensor in front
     for (int side = 0; side < 2; ++side) {
         const NormSide<IO> t = norm_side<IO>(a, side == 1);
         const unsigned chunks = (t.heads + per - 1) / per;
@@ -208,66 +256,73 @@ __global__ void __launch_bounds__(kNormThreads, (sizeof(IO) == 4 ? 3 : 4)) head_
         norm_weights(t.w, at, weight);
 #pragma unroll
         for (int e = 0; e < 16; ++e) dw[e] = 0.f;
-        Pack<IO, 8> raw_g[H][2], raw_v[H][2];  // the next item's gradient and value
-        int position = 0;
-        auto fetch = [&](unsigned item) {
-            const unsigned token = item / chunks;
-            const int head = (int)(item % chunks) * per + group;
-            const IO *x = t.x + token * t.stride, *g = t.dout + (size_t)token * t.heads * a.d;
-            position = a.rot ? a.positions[token] : 0;
+        norm_wait<0>();
+        __syncthreads();  // (the ring held the other side's sums)
 #pragma unroll
-            for (int i = 0; i < H; ++i) {
-                const bool there = head + i * G < t.heads;
-                norm_load(g + (head + i * G) * a.d, at, there, raw_g[i]);
-                norm_load(x + (head + i * G) * a.d, at, there && normed, raw_v[i]);
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                norm_clear<IO>(ring[warp][s][i], at, lane);
+                if (i && !normed) ring[warp][s][i][0][lane] = ring[warp][s][i][1][lane] = pack_zero<IO, 8>();
             }
+        int position[S];  // of the items on their way, the next first
+        auto fetch = [&](long long item, int stage, int &position) {
+            if (item < items) {
+                const unsigned token = (unsigned)item / chunks;
+                const int head = (int)((unsigned)item % chunks) * per + group;
+                const bool there = head < t.heads;
+                position = a.rot ? a.positions[token] : 0;
+                norm_copy(ring[warp][stage][0], t.dout + (size_t)token * t.heads * a.d + head * a.d, at, there, lane);
+                norm_copy(ring[warp][stage][1], t.x + token * t.stride + head * a.d, at, there && normed, lane);
+            }
+            cp_async_commit();
         };
-        long long item = first - skipped;
-        if (item >= 0 && item < items) fetch((unsigned)item);
-        for (; item >= 0 && item < items; item += step) {
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) fetch(first + s * step, s, position[s]);
+        int stage = 0;
+        for (long long item = first; item < items; item += step, stage = stage == S - 1 ? 0 : stage + 1) {
+            Turn turn;
+            const bool ok = norm_turn(a, position[0], l, turn);
+            fetch(item + (S - 1) * step, stage == 0 ? S - 1 : stage - 1, position[S - 1]);
+#pragma unroll
+            for (int s = 0; s < S - 1; ++s) position[s] = position[s + 1];
             const unsigned token = (unsigned)item / chunks;
             const int head = (int)((unsigned)item % chunks) * per + group;
-            Turn turn;
-            const bool ok = norm_turn(a, position, l, turn);
-            float v[H][16], g[H][16];
+            norm_wait<S - 1>();
+            float v[16], g[16];
+            norm_read<IO>(ring[warp][stage][0], lane, g);
+            norm_read<IO>(ring[warp][stage][1], lane, v);
+            float ss = 0.f, gx = 0.f;
+            if (normed) {
 #pragma unroll
-            for (int i = 0; i < H; ++i) norm_floats(raw_g[i], g[i]), norm_floats(raw_v[i], v[i]);
-            if (item + step < items) fetch((unsigned)(item + step));
-            IO *dx = t.out + (size_t)token * t.heads * a.d;
+                for (int e = 0; e < 16; ++e) ss = fmaf(v[e], v[e], ss);
+                ss = lanes_sum<L>(ss);
+            }
+            norm_rotate<true>(a, turn, g);
 #pragma unroll
-            for (int i = 0; i < H; ++i) {
-                float ss = 0.f, gx = 0.f;
-                if (normed) {
+            for (int e = 0; e < 16; ++e) g[e] *= t.scale;
+            if (normed) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-                    ss = lanes_sum<L>(ss);
-                }
-                norm_rotate<true>(a, turn, g[i]);
+                for (int e = 0; e < 16; ++e) gx = fmaf(g[e] * weight[e], v[e], gx);
+                const float r = rsqrtf(fmaf(c, ss, a.eps)), k = lanes_sum<L>(gx) * c * r * r * r;
+                if (weighted && ok && head < t.heads)  // (a token without a position may hold anything, and so may a stage without a head)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) g[i][e] *= t.scale;
-                if (normed) {
+                    for (int e = 0; e < 16; ++e) dw[e] = fmaf(g[e], v[e] * r, dw[e]);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) gx = fmaf(g[i][e] * weight[e], v[i][e], gx);
-                    const float r = rsqrtf(fmaf(c, ss, a.eps)), k = lanes_sum<L>(gx) * c * r * r * r;
-                    if (weighted && ok)  // (a token without a position may hold anything)
+                for (int e = 0; e < 16; ++e) g[e] = fmaf(r * weight[e], g[e], -k * v[e]);
+            }
+            if (head < t.heads) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) dw[e] = fmaf(g[i][e], v[i][e] * r, dw[e]);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) g[i][e] = fmaf(r * weight[e], g[i][e], -k * v[i][e]);
-                }
-                if (head + i * G < t.heads) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) g[i][e] = ok ? g[i][e] : 0.f;
-                    norm_store(dx + (head + i * G) * a.d, at, g[i]);
-                }
+                for (int e = 0; e < 16; ++e) g[e] = ok ? g[e] : 0.f;
+                norm_store(t.out + ((size_t)token * t.heads + head) * a.d, at, g);
             }
         }
-        if (!weighted) {
-            skipped += items;  // the items of both tensors in one row
-            continue;
-        }
+        if (!weighted) continue;
         // the block's sums: over the heads side by side in a warp, then over its warps
+        norm_wait<0>();
         __syncthreads();
+        auto sums = reinterpret_cast<float (*)[256]>(&ring);
+        static_assert(sizeof(ring) >= sizeof(float) * 256 * (kNormThreads / 32), "the sums fit");
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             float s = dw[e];

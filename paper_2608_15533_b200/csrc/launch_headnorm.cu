@@ -52,12 +52,11 @@ long long norm_blocks(const deltalog_norm_desc *d, int32_t tokens) {
     return (items(d->H_q) + items(d->H_k) + kNormThreads / 32 - 1) / (kNormThreads / 32);
 }
 
-// Blocks of the backward pass with weights, whose sums they keep: one wave (of 148, whichever device is current: the
-// workspace's size depends on it).
+// One wave of blocks, which walk over the items (of 148 SMs, whichever device is current: with weights the backward pass keeps a
+// block's sums, and the workspace's size depends on it).
+long long norm_wave(long long blocks, int per_sm) { return blocks < 148 * per_sm ? blocks : 148 * per_sm; }
 long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
-    const long long b = norm_blocks<kNormHeadsBack>(d, tokens);
-    const int most = 148 * (d->io_dtype == DELTALOG_F32 ? 3 : 4);
-    return b < most ? b : most;
+    return norm_wave(norm_blocks<kNormHeadsBack>(d, tokens), d->io_dtype == DELTALOG_F32 ? 3 : 4);
 }
 
 #define NORM_DISPATCH(desc_, CALL)                                                                  \
@@ -81,8 +80,8 @@ int deltalog_head_norm_forward(const deltalog_norm_desc *desc, const void *q, in
     if (tokens == 0) return DELTALOG_OK;
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = out_q, a.out_k = out_k, a.status = status;
-    const long long grid = norm_blocks<kNormHeads>(desc, tokens);
-    if (grid > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
+    const long long blocks = norm_blocks<kNormHeads>(desc, tokens), grid = norm_wave(blocks, 5);
+    if (blocks > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
     cudaStream_t s = static_cast<cudaStream_t>(stream);
 #define CALL(IO, L) head_norm_forward_kernel<IO, L><<<(unsigned)grid, kNormThreads, 0, s>>>(a)
     NORM_DISPATCH(desc, CALL);
@@ -108,7 +107,7 @@ int deltalog_head_norm_backward(const deltalog_norm_desc *desc, const void *q, i
         return DELTALOG_ERR_INVALID_ARG;
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = dq, a.out_k = dk, a.dout_q = dout_q, a.dout_k = dout_k, a.partial = static_cast<float *>(workspace);
-    const long long grid = weighted ? norm_kept_blocks(desc, tokens) : norm_blocks<kNormHeadsBack>(desc, tokens);
+    const long long grid = norm_kept_blocks(desc, tokens);
     if (norm_blocks<kNormHeadsBack>(desc, tokens) > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (grid > 0) {

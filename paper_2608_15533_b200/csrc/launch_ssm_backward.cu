@@ -24,7 +24,7 @@ int backward(const SsmArgs &a, cudaStream_t s) {
         kernel<<<dim3(cols, (unsigned)a.spans + rest), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
     }
-    const long long token_blocks = ssm_ceil((long long)a.total_rows * a.G * (2 * N / 4), 256), param_blocks = ssm_ceil((long long)a.D_ * (N + 2), 256);
+    const long long token_blocks = ssm_ceil((long long)a.total_rows * a.G * (2 * N / 4), 64), param_blocks = ssm_ceil((long long)a.D_ * (N + 2), 256);
     if (token_blocks + param_blocks > 0x7fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;
     ssm_sums_kernel<IO, N><<<(unsigned)(token_blocks + param_blocks), 256, 0, s>>>(a, token_blocks);
     return finish_launch();

@@ -375,21 +375,25 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
 // dB and dC over the blocks of channels of a group (blocks [0, token_blocks)), dA, dD and dbias over the stretches (the rest).
 template <typename IO, int N>
 __global__ void __launch_bounds__(256) ssm_sums_kernel(const SsmArgs a, long long token_blocks) {
-    if (blockIdx.x < token_blocks) {  // four values of a token and group
+    if (blockIdx.x < token_blocks) {  // 64 vectors of four values, four threads each: a quarter of the blocks of channels
         constexpr int V = 2 * N / 4;
-        const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+        __shared__ float4 quarter[4][64];
+        const int part = threadIdx.x / 64, item = threadIdx.x % 64;
+        const long long i = (long long)blockIdx.x * 64 + item;
         const int v = (int)(i % V) * 4, g = (int)(i / V % a.G);
         const long long t = i / V / a.G;
-        if (t >= a.total_rows) return;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](const float4 &f) { s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w; };
         if (t < a.rows.starts[a.rows.n]) {
             const float *p = a.part_bc + ((size_t)g * a.blocks * a.total_rows + t) * 2 * N + v;
 #pragma unroll 8
-            for (int b = 0; b < a.blocks; ++b) {
-                const float4 f = *reinterpret_cast<const float4 *>(p + (size_t)b * a.total_rows * 2 * N);
-                s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
-            }
+            for (int b = part; b < a.blocks; b += 4) add(*reinterpret_cast<const float4 *>(p + (size_t)b * a.total_rows * 2 * N));
         }
+        quarter[part][item] = s;
+        __syncthreads();
+        if (part || t >= a.total_rows) return;
+#pragma unroll
+        for (int k = 1; k < 4; ++k) add(quarter[k][item]);
         const float f[4] = {s.x, s.y, s.z, s.w};
         pack_store(static_cast<IO *>(v < N ? a.dB : a.dC) + ((size_t)t * a.G + g) * N + v % N, pack_round<IO, 4>(f));
         return;
