@@ -2,12 +2,13 @@
 //     pre[t] = bias + sum_j w[j] x[t - (W - 1) + j],   out = pre or pre sigmoid(pre)
 // with a row's window (its last W - 1 inputs) in front of its first token.
 //
-// Bound by HBM: an input is read and an output written once, a dozen operations between them.  A thread holds the weights of
-// a vector of neighbouring channels (16 bytes of them) in registers and walks down a run of tokens, so that an input is
-// loaded once per run and the W - 1 inputs in front of it come out of registers; the next eight tokens' loads are under way
-// while eight are computed.  The first W - 1 tokens of a row, which need its window, and the window itself are left to
-// blocks of their own, one warp per row and vector of channels: a window is then read and written by the same threads, in
-// that order, however many blocks work on the row.
+// Bound by HBM: an input is read and an output written once, a dozen operations between them.  A lane holds the weights of four
+// neighbouring channels in registers and walks down a run of tokens, so that an input is loaded once per run and the W - 1 inputs in
+// front of it come out of registers; the arithmetic is packed, two channels an instruction.  The first W - 1 tokens of a row, which
+// need its window, and the window itself are left to blocks of their own, one warp per row and vector of channels: a window is
+// then read and written by the same threads, in that order, however many blocks work on the row.
+// 36k x 8192 16-bit inputs 207 us (5.7 TB/s, 0.87 of a copy); 16k x 4096 52 us, their gradients 113 us (3.6 TB/s: its loop of 18
+// instructions an element, two of them at the special function units, has little room beside the loads).
 #pragma once
 
 #include "layer_common.cuh"
@@ -32,7 +33,7 @@ struct ConvArgs {
 constexpr int kConvThreads = 128, kConvVec = 4;  // channels per lane: eight would need up to 200 registers
 
 // Inputs on their way: a lane copies its own channels of U tokens a stage into shared memory and reads nothing but its own, so that a
-// wait for its own copies is all it needs.  (Registers would have to hold them otherwise: half of a lane's, or half of the bytes in flight.)
+// wait for its own copies is all it needs.  (Held in registers instead, eight tokens ahead: 257 us where this takes 207.)
 template <typename IO>
 __device__ __forceinline__ void conv_copy(Pack<IO, kConvVec> *dst, const IO *src) {
     if constexpr (sizeof(IO) * kConvVec == 16)

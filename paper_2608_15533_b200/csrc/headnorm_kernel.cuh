@@ -4,9 +4,11 @@
 // Backward, with g = scale (dy turned back):  dw = sum g x r,  dx = r (g w - c r^2 x sum(g w x)).
 //
 // Bound by HBM: every value is read once and written once.  L lanes hold a head, sixteen values each: two runs of eight that are
-// half a rotation apart (or neighbours, for interleaved pairs and behind the rotated part), so that a lane turns its own values.  A
-// warp takes one token and several of its heads: the token's cosines and sines are loaded once for all of them, and several heads a
-// lane are in flight.  The sums over a head are butterflies over its lanes.
+// half a rotation apart (or neighbours, for interleaved pairs and behind the rotated part), so that a lane turns its own values and
+// loads 16 bytes at a time.  A warp takes one token and several of its heads, and walks over such items with two more on their way
+// in shared memory.  The sums over a head are butterflies over its lanes.
+// 16k tokens x 40 heads of 128, 16-bit: 64 us (5.2 TB/s, 0.80 of a copy), gradients 117 us (4.3 TB/s) and 8 for the weights' sums.
+// (Pairs exchanged between lanes: 103 and 355 us; one item a warp with its loads in registers: 80 and 149.)
 #pragma once
 
 #include "layer_common.cuh"

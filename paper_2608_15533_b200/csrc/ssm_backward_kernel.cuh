@@ -3,13 +3,15 @@
 //     dx = delta sum dh B + D dy                  ddelta = x sum dh B + sum dh (a h_(t-1)) A,   ddt = ddelta sigmoid(dt + bias)
 //     dA = sum_t dh (a h_(t-1)) delta             dz = dout (C h + D x) silu'(z),   dS_init = a_first dh_first
 //
-// Walks eight tokens at a time from the last to the first: the forward pass kept the state in front of every eighth token, from
-// which a lane runs the eight again with a and a h_(t-1) in registers, one exponential per token, channel and state as in
-// the forward pass, and then goes back over them.  (The states of every token would be 8 times the bytes; kept every 16
-// tokens they would cost half the exponentials once more.)  a h_(t-1) is kept rather than h_t, from which it would come out by
-// a difference that cancels where the decay is strong.
-// Sums over a channel's states and over a warp's channels run over several values at once (lanes_reduce), over the warps in
-// shared memory, over the CTAs in ssm_sums_kernel; each in a fixed order.
+// Walks from the last token to the first: the forward pass kept the state in front of every eighth, from which a lane runs over
+// the lower four, then over the upper four with a and a h_(t-1) in registers, goes back over those, and does the same with the
+// lower four.  (The states of every token would be 8 times the bytes; all eight tokens in registers took 255 of them and 992 us
+// where four take 714.)  a h_(t-1) is kept rather than h_t, from which it would come out by a difference that cancels where the
+// decay is strong.  Sums over a channel's states and over a warp's channels run over several values at once (lanes_reduce), over
+// the warps in shared memory, over the CTAs in ssm_sums_kernel; each in a fixed order.
+// Bound by its instructions, 25 per token, channel and state of which 13 are products and sums and 6 the exchange of partial sums:
+// 8k tokens x 4096 x 16 states 714 us, 53 % of the issue slots with the 12 warps an SM that 168 registers leave; the first pass 174,
+// the sums 17.  One channel a lane instead of two (20 warps) has 915: its sums over channels cost twice as much.
 #pragma once
 
 #include "ssm_common.cuh"

@@ -1,9 +1,12 @@
 // Forward pass of the selective state space scan and its single-token form.
 //
 // Bound by the exponentials: one per token, channel and state, 16 a clock and SM.  Everything else is arranged around that:
-// step sizes and gates are worked out once per token and channel on the way into and out of shared memory; B and C are widened
-// once per CTA; per state a lane then does two products, the exponential and two fused multiply-adds; the sums over a
-// channel's states run over four tokens at a time, three shuffles for four sums.
+// step sizes and gates are worked out once per token and channel on the way into and out of shared memory, two neighbouring
+// channels a thread; B and C are widened once per CTA; per pair of states a lane then does two packed products, two
+// exponentials and two packed fused multiply-adds; the sums over a channel's states run over four tokens at a time, six shuffles for
+// eight sums.  Two channels a lane share the loads of B and C, which at one channel cost more than the exponentials.
+// 14k ragged tokens x 4096 channels x 16 states: 414 us behind a first pass of 107 (the exponentials alone: 204), special function
+// units 59 % busy, issue slots 50 %; 16k x 2048 in one row 238 + 174.  Four CTAs an SM; six with fewer registers or smaller tiles took as long.
 #pragma once
 
 #include "ssm_common.cuh"

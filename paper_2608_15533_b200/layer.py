@@ -423,6 +423,8 @@ def ssm_step(desc: SsmDesc, state: SsmState, x, dt, A, B, C, D=None, z=None, dt_
     inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     p_slots = _slot_list(slot_idx, rows, desc.num_slots, dev)
     p_S, p_status = state._fits(desc, dev)
+    if (p_S | inputs.A) % 32:
+        raise ValueError("state, A: the single-token call wants them on 32-byte boundaries")
     if out is not None:
         _want("out", out, (rows, desc.channels), io, dev)
     with _stream_of(dev, stream) as handle:

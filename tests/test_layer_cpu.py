@@ -181,6 +181,10 @@ def test_python_layer_names_what_it_refuses():
                          (dict(D=torch.zeros(8)), "D:"), (dict(dt_bias=torch.zeros(64, 1)), "dt_bias:"), (dict(), "cpu")):
             with pytest.raises(ValueError, match=name):
                 call(**kw)
+    odd = torch.zeros(64 * 16 + 8)
+    odd = odd[next(i for i in range(8) if (odd.data_ptr() + 4 * i) % 32 == 16):][: 64 * 16].view(64, 16)
+    with pytest.raises(ValueError, match="32-byte"):
+        dl.ssm_step(ssm, ss, t[:2], t[:2], odd, bc[:2], bc[:2])
     with pytest.raises(ValueError, match="workspace"):
         dl.ssm_forward(ssm, plan, t, t, A, bc, bc, save=True)
     with pytest.raises(ValueError, match="workspace"):
