@@ -106,16 +106,23 @@ class _Pool:
             tensor = torch.zeros(shape, dtype=dtype, device=device)
         else:
             _want(name, tensor, shape, dtype, tensor.device)
-        self.status = torch.zeros(1, dtype=torch.int32, device=tensor.device)
-        self._tensor, self._shape = tensor, shape
+        self._status = torch.zeros(1, dtype=torch.int32, device=tensor.device)
+        self._tensor, self._shape, self._seen = tensor, shape, None
+
+    @property
+    def status(self) -> torch.Tensor:
+        return self._status
 
     def _fits(self, desc, device):
         """Addresses of the pool and of the status word for a call with this descriptor."""
-        if desc is not self.desc and (self._shape != self._want(desc) or self._tensor.dtype is not self._dtype(desc)):
-            raise ValueError("state: its tensor was laid out for another descriptor")
+        forms = desc._forms()
+        if forms is not self._seen:  # (a descriptor whose values change makes new ones)
+            if self._shape != self._want(desc) or self._tensor.dtype is not self._dtype(desc):
+                raise ValueError("state: its tensor was laid out for another descriptor")
+            self._seen = forms
         if self._tensor.device != device:
             raise ValueError(f"state: expected a tensor on {device}, got one on {self._tensor.device}")
-        return self._tensor.data_ptr(), self.status.data_ptr()
+        return self._tensor.data_ptr(), self._status.data_ptr()
 
 
 class ConvState(_Pool):
@@ -124,7 +131,10 @@ class ConvState(_Pool):
 
     def __init__(self, desc: ConvDesc, window: Optional[torch.Tensor] = None, device="cuda"):
         super().__init__(desc, window, self._want(desc), self._dtype(desc), device, "window")
-        self.window = self._tensor
+
+    @property
+    def window(self) -> torch.Tensor:
+        return self._tensor
 
     @staticmethod
     def _want(desc):
@@ -141,7 +151,10 @@ class SsmState(_Pool):
 
     def __init__(self, desc: SsmDesc, S: Optional[torch.Tensor] = None, device="cuda"):
         super().__init__(desc, S, self._want(desc), torch.float32, device, "S")
-        self.S = self._tensor
+
+    @property
+    def S(self) -> torch.Tensor:
+        return self._tensor
 
     @staticmethod
     def _want(desc):
@@ -283,7 +296,7 @@ def conv_step(desc: ConvDesc, state: ConvState, x, weight, bias=None, slot_idx=N
     """``deltalog_conv_step``: one token ``x [B, channels]`` per row; row b advances window ``slot_idx[b]`` (b without a list).
     Padding rows (negative slots) and rows outside the pool stay as they were in the caller's ``out`` and are not defined in a
     tensor that the call makes."""
-    dev, io, C = state.window.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
+    dev, io, C = state._tensor.device, _DT_TO_TORCH[desc.io_dtype], desc.channels
     B = _rows("x", x)
     p_x, stride = _tokens("x", x, (B, C), io, dev)
     p_w, p_b = _want("weight", weight, (C, desc.width), torch.float32, dev), _param("bias", bias, (C,), dev)
@@ -431,7 +444,7 @@ def _ssm_inputs(desc: SsmDesc, rows: int, x, dt, A, B, C, D, z, dt_bias, dev) ->
 def ssm_step(desc: SsmDesc, state: SsmState, x, dt, A, B, C, D=None, z=None, dt_bias=None, slot_idx=None, out=None, stream=None) -> torch.Tensor:
     """``deltalog_ssm_step``: one token per row; row b advances state ``slot_idx[b]`` (b without a list).  Rows that the call
     skips: as in ``conv_step``."""
-    dev, io = state.S.device, _DT_TO_TORCH[desc.io_dtype]
+    dev, io = state._tensor.device, _DT_TO_TORCH[desc.io_dtype]
     rows = _rows("x", x)
     inputs = _ssm_inputs(desc, rows, x, dt, A, B, C, D, z, dt_bias, dev)
     p_slots = _slot_list(slot_idx, rows, desc.num_slots, dev)

@@ -264,3 +264,31 @@ def test_reference_gradients_against_differences():
                     return (out * do).sum() + (final * df).sum()
 
                 assert abs(float((g * v).sum()) - _difference(value, args[i], v)) < 1e-7
+
+
+def test_pools_of_a_changed_descriptor_are_refused():
+    """A descriptor that grows behind its pool's back would send slots past the pool's end."""
+    def conv(desc, state):
+        x = torch.zeros(1, 64, dtype=torch.bfloat16)
+        return dl.conv_step(desc, state, x, torch.zeros(64, 4))
+
+    def ssm(desc, state):
+        x, bc = torch.zeros(1, 64, dtype=torch.bfloat16), torch.zeros(1, 1, 16, dtype=torch.bfloat16)
+        return dl.ssm_step(desc, state, x, x, torch.zeros(64, 16), bc, bc)
+
+    for desc, pool, call in ((dl.ConvDesc(64, num_slots=4), dl.ConvState, conv), (dl.SsmDesc(64, num_slots=4), dl.SsmState, ssm)):
+        state = pool(desc, device="cpu")
+        desc.num_slots = 5
+        with pytest.raises(ValueError, match="another descriptor"):
+            call(desc, state)
+        desc.num_slots = 4
+        with pytest.raises(ValueError, match="GPU"):  # it fits again: the device is what is wrong now
+            call(desc, state)
+
+
+@pytest.mark.parametrize("pool,desc,name", [(dl.ConvState, dl.ConvDesc(64), "window"), (dl.SsmState, dl.SsmDesc(64), "S")])
+def test_pool_tensors_are_not_replaced(pool, desc, name):
+    state = pool(desc, device="cpu")
+    for field in (name, "status"):  # the calls would go on with the old one
+        with pytest.raises(AttributeError):
+            setattr(state, field, getattr(state, field).clone())
