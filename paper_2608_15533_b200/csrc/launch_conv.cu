@@ -141,6 +141,7 @@ int deltalog_conv_backward(const deltalog_conv_desc *desc, const deltalog_plan *
     if (int rc = validate_conv(desc, x, x_stride, weight, bias)) return rc;
     if (int rc = validate_plan(plan)) return rc;
     if (!dout || !grads || !grads->x || !grads->weight || rows < plan->max_tokens) return DELTALOG_ERR_INVALID_ARG;
+    if (rows > 0x7fffffff - 64) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // a run walks W - 1 tokens beyond its last one, in 32 bits
     if (!aligned16(init) || !aligned16(dout) || !aligned16(dfinal) || !aligned16(grads->x) || !aligned16(grads->init)) return DELTALOG_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace) || workspace_bytes < deltalog_conv_workspace_bytes(desc, rows)) return DELTALOG_ERR_INVALID_ARG;
     if (conv_overlaps(desc, x, x_stride, grads->x, rows) || conv_overlaps(desc, dout, desc->channels, grads->x, rows)) return DELTALOG_ERR_INVALID_ARG;

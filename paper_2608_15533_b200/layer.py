@@ -184,10 +184,16 @@ def _tokens(name: str, t, shape: Tuple[int, ...], dtype, device) -> Tuple[int, i
     return at, stride
 
 
+_MOST_ROWS = 0x7fffffff - 64  # the C ABI counts rows in 31 bits
+
+
 def _rows(name: str, t) -> int:
     if not isinstance(t, torch.Tensor) or t.dim() == 0:
         raise ValueError(f"{name}: a tensor of tokens is needed")
-    return t.shape[0]
+    rows = t.shape[0]
+    if rows > _MOST_ROWS:
+        raise ValueError(f"{name}: at most {_MOST_ROWS} rows, got {rows}")
+    return rows
 
 
 class _Here:

@@ -292,3 +292,12 @@ def test_pool_tensors_are_not_replaced(pool, desc, name):
     for field in (name, "status"):  # the calls would go on with the old one
         with pytest.raises(AttributeError):
             setattr(state, field, getattr(state, field).clone())
+
+
+def test_more_rows_than_31_bits_are_refused(lib):
+    most = 2 ** 31 - 64
+    assert _conv("backward", lib, x=1 << 44, grads=dict(x=1 << 50), dout=1 << 47, rows=most) == SHAPE
+    desc, weight = dl.ConvDesc(8), torch.zeros(8, 4)
+    x = torch.empty(1, 8, dtype=torch.bfloat16).expand(most, 8)  # (no such memory is needed to be asked)
+    with pytest.raises(ValueError, match="x: .* rows"):
+        dl.conv_step(desc, dl.ConvState(desc, device="cpu"), x, weight)
