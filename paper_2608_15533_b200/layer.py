@@ -703,5 +703,6 @@ def head_norm(desc: NormDesc, q, k, w_q=None, w_k=None, cos=None, sin=None, posi
         raise ValueError("cos, sin: the rotation's tables have no gradient")
     if _differentiable(tensors):
         _norm_inputs(desc, q, k, w_q, w_k, cos, sin, positions)
+        _gpu(q.device)
         return _HeadNorm.apply(desc, q, k, w_q, w_k, cos, sin, positions)
     return head_norm_forward(desc, q, k, w_q, w_k, cos, sin, positions)

@@ -301,3 +301,9 @@ def test_more_rows_than_31_bits_are_refused(lib):
     x = torch.empty(1, 8, dtype=torch.bfloat16).expand(most, 8)  # (no such memory is needed to be asked)
     with pytest.raises(ValueError, match="x: .* rows"):
         dl.conv_step(desc, dl.ConvState(desc, device="cpu"), x, weight)
+
+
+def test_head_norm_of_host_tensors_is_refused():
+    q = torch.zeros(3, 1, 16, requires_grad=True)
+    with pytest.raises(ValueError, match="GPU"):
+        dl.head_norm(dl.NormDesc(1, 0, 16, io_dtype=dl.F32), q, None)
