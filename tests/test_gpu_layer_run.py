@@ -144,3 +144,75 @@ def test_state_space_layer_prompt_then_tokens_is_the_longer_prompt():
         at, first = at + n + more, first + n
     assert (served.state.S - whole.state.S).abs().max() / whole.state.S.abs().max() < 1e-4 and torch.equal(served.window.window, whole.window.window)
     assert int(served.window.status) == 0 and int(served.state.status) == 0
+
+
+def _small(which):
+    """A differentiable call and its leaves, on the device."""
+    g = torch.Generator().manual_seed(5)
+    lens = (40, 3)
+    T, plan = sum(lens), _plan(lens, [0, 1])
+
+    def new(*shape):
+        return torch.randn(*shape, generator=g).to(DEV)
+
+    if which == "conv":
+        desc = dl.ConvDesc(64, 4, dl.F32)
+        return [new(T, 64), new(64, 4), new(64)], lambda x, w, b: dl.conv(desc, plan, x, w, b)
+    if which == "norm":
+        desc = dl.NormDesc(2, 1, 64, dl.F32, dl.NORM_RMS)
+        return [new(T, 2, 64), new(T, 1, 64), new(64), new(64)], lambda q, k, wq, wk: dl.head_norm(desc, q, k, wq, wk)
+    desc = dl.SsmDesc(64, 16, 1, dl.F32)
+    return [new(T, 64), new(T, 64), -new(64, 16).exp(), new(T, 1, 16), new(T, 1, 16)], lambda *a: dl.ssm(desc, plan, *a)
+
+
+def _gradients(call, leaves):
+    a, b = call(*leaves)
+    return torch.autograd.grad(a.square().sum() + b.sum(), leaves)
+
+
+@pytest.mark.parametrize("which", ["conv", "norm"])
+def test_gradients_in_a_graph(which):
+    values, call = _small(which)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        leaves = [v.clone().requires_grad_() for v in values]
+        _gradients(call, leaves)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grads = _gradients(call, leaves)
+    with torch.no_grad():
+        leaves[0].mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, want in zip(grads, _gradients(call, [v.detach().clone().requires_grad_() for v in leaves])):
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("which", ["conv", "norm"])
+def test_capture_beside_an_eager_graph_is_refused(which):
+    values, call = _small(which)
+    values[0].requires_grad_()
+    out, _ = call(*values)
+    with pytest.raises(RuntimeError, match="eager|default stream"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            call(*values)
+    out.sum().backward()
+    assert torch.isfinite(values[0].grad).all()
+
+
+@pytest.mark.parametrize("which", ["conv", "norm", "ssm"])
+def test_gradients_on_two_streams_at_once(which):
+    values, call = _small(which)
+    want = _gradients(call, [v.clone().requires_grad_() for v in values])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(3):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(_gradients(call, [v.clone().requires_grad_() for v in values]))
+    torch.cuda.synchronize()
+    for grads in got:
+        for g, w in zip(grads, want):
+            assert torch.equal(g, w)
