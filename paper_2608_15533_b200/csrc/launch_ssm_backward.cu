@@ -8,10 +8,10 @@ namespace {
 
 template <typename IO, int N>
 int backward(const SsmArgs &a, cudaStream_t s) {
-    const size_t smem = sizeof(typename SsmBackward<IO, N>::Shared);
     const unsigned cols = (unsigned)(a.G * a.blocks);
     if (a.spans > 1) {
         auto local = ssm_backward_kernel<IO, N, true>;
+        const size_t smem = sizeof(typename SsmBackward<IO, N, true>::Shared);
         if (int rc = ensure_smem(local, smem)) return rc;
         local<<<dim3(cols, (unsigned)a.parts), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;
@@ -20,6 +20,7 @@ int backward(const SsmArgs &a, cudaStream_t s) {
     const unsigned rest = a.dS_init ? ssm_empty_ctas(a.rows.n) : 0;
     if (a.spans + rest > 0) {
         auto kernel = ssm_backward_kernel<IO, N, false>;
+        const size_t smem = sizeof(typename SsmBackward<IO, N, false>::Shared);
         if (int rc = ensure_smem(kernel, smem)) return rc;
         kernel<<<dim3(cols, (unsigned)a.spans + rest), kSsmThreads, smem, s>>>(a);
         if (int rc = finish_launch()) return rc;

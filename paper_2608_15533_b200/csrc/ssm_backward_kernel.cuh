@@ -6,32 +6,40 @@
 // Walks from the last token to the first: the forward pass kept the state in front of every eighth, from which a lane runs over
 // the lower four, then over the upper four with a and a h_(t-1) in registers, goes back over those, and does the same with the
 // lower four.  (The states of every token would be 8 times the bytes; all eight tokens in registers took 255 of them and 992 us
-// where four take 714.)  a h_(t-1) is kept rather than h_t, from which it would come out by a difference that cancels where the
-// decay is strong.  Sums over a channel's states and over a warp's channels run over several values at once (lanes_reduce), over
-// the warps in shared memory, over the CTAs in ssm_sums_kernel; each in a fixed order.
-// Bound by its instructions, 25 per token, channel and state of which 13 are products and sums and 6 the exchange of partial sums:
-// 8k tokens x 4096 x 16 states 714 us, 53 % of the issue slots with the 12 warps an SM that 168 registers leave; the first pass 174,
-// the sums 17.  One channel a lane instead of two (20 warps) has 915: its sums over channels cost twice as much.
+// where four took 714.)  a h_(t-1) is kept rather than h_t, from which it would come out by a difference that cancels where the
+// decay is strong.  Sums over a channel's states run over several values at once (lanes_reduce), over a warp's channels in the same way
+// or in shared memory, over the warps in shared memory, over the CTAs in ssm_sums_kernel; each in a fixed order.
+// Bound by its instructions, 22 per token, channel and state of which 13 are products and sums and 4 the exchange of partial sums:
+// 8k tokens x 4096 x 16 states 681 us with the 12 warps an SM that 168 registers leave; the first pass 153 (175 in the second pass's
+// layout), the sums 17.  One channel a lane instead of two (20 warps) had 915 where two had 714: its sums over channels cost twice as much.
 #pragma once
 
 #include "ssm_common.cuh"
 
 namespace deltalog {
 
-template <typename IO, int N> struct SsmBackward {
+// The first pass brings in no x and no B, and needs none of the sums: it has room for tiles twice as long and a fourth CTA.
+template <typename IO, int N, bool LOCAL> struct SsmBackward {
     static constexpr int kPer = 2;
-    static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = 16;
+    static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = LOCAL ? 32 : 16;
+    static constexpr int kCtas = LOCAL && N <= 32 ? 4 : 3;  // on an SM, by their registers
+    // dB and dC over a warp's channels: eight or more of them in shared memory, two tokens at a time (each token by exchanges between
+    // the lanes: 714 us where 681 are taken); of four or two the exchanges are short (32 states: 400 us, in shared memory 405).
+    static constexpr bool kInMemory = !LOCAL && SsmLanes<N>::kChannels >= 8;
+    static constexpr int full(int n) { return LOCAL ? 8 : n; }  // elements of what the first pass does without (multiples of 16 bytes)
     struct Raw {
-        IO x[kTile * kCols], dt[kTile * kCols], z[kTile * kCols], dout[kTile * kCols], B[kTile * N], C[kTile * N];
+        IO dt[kTile * kCols], z[kTile * kCols], dout[kTile * kCols], C[kTile * N], x[full(kTile * kCols)], B[full(kTile * N)];
     };
     static constexpr int kPitch = kCols + 16;  // lanes that answer for neighbouring tokens store to different banks
     struct alignas(16) Shared {
         Raw raw[2];
-        float2 step[kTile * kCols];                          // delta, delta x
-        float dy[kTile * kCols], slope[kTile * kCols];       // slope: softplus'
-        float sums[3][kTile * kPitch];                       // C . h, sum dh B, sum dh a h_(t-1) A (A in powers of two)
-        float B[kTile * N], C[kTile * N];
-        float bc[kSsmWarps][kTile][2 * N];
+        float2 step[kTile * kCols];                          // delta, delta x; in the first pass delta, dy
+        float C[kTile * N];
+        float dy[full(kTile * kCols)], slope[full(kTile * kCols)];  // slope: softplus'
+        float sums[3][full(kTile * kPitch)];                 // C . h, sum dh B, sum dh a h_(t-1) A (A in powers of two)
+        float B[full(kTile * N)];
+        float bc[kSsmWarps][full(kTile)][2 * N];
+        float4 product[kInMemory ? kSsmWarps : 1][2][2][32]; // of two tokens: a lane's four states of dB and of dC
         int state[kTile], row[kTile];
         unsigned begins, ends, there;
     };
@@ -40,8 +48,8 @@ template <typename IO, int N> struct SsmBackward {
 // LOCAL: the first pass over a part of a stretch (`span` is the part), where its first row began in front of the stretch: the adjoint
 // that the part alone hands back.
 template <typename IO, int N, bool LOCAL>
-__global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmArgs a) {
-    using F = SsmBackward<IO, N>;
+__global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas)) ssm_backward_kernel(const SsmArgs a) {
+    using F = SsmBackward<IO, N, LOCAL>;
     constexpr int KC = F::kPer, CB = F::kCols, PB = F::kPitch, TT = F::kTile, LN = SsmLanes<N>::kStates, LC = SsmLanes<N>::kChannels, U = kSsmBlock;
     extern __shared__ __align__(16) char smem[];
     typename F::Shared &s = *reinterpret_cast<typename F::Shared *>(smem);
@@ -157,20 +165,23 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                 const float2 zf = load2(r.z + to);
                 g = __fmul2_rn(g, make_float2(zf.x * sigmoid(zf.x), zf.y * sigmoid(zf.y)));
             }
-            if (!LOCAL) u = __fmul2_rn(d, load2(r.x + to));
+            if (LOCAL) u = g;
+            else u = __fmul2_rn(d, load2(r.x + to)), store2(s.dy + to, g);
             *reinterpret_cast<float4 *>(s.step + to) = make_float4(d.x, u.x, d.y, u.y);
-            store2(s.dy + to, g);
         }
-        if (there != (1u << TT) - 1) {  // a skipped token may hold anything, and changes nothing
+        if (there != (unsigned)((1ull << TT) - 1)) {  // a skipped token may hold anything, and changes nothing
 #pragma unroll
             for (int i = 0; i < TT / kTokenStep; ++i) {
                 const int k = col_token + i * kTokenStep, to = k * CB + col;
                 if (there >> k & 1) continue;
                 *reinterpret_cast<float4 *>(s.step + to) = make_float4(0.f, 0.f, 0.f, 0.f);
-                store2(s.dy + to, both(0.f));
+                if (!LOCAL) store2(s.dy + to, both(0.f));
             }
             for (int i = tid; i < TT * N; i += kSsmThreads)
-                if (!(there >> (i / N) & 1)) r.B[i] = r.C[i] = from_f32<IO>(0.f);
+                if (!(there >> (i / N) & 1)) {
+                    r.C[i] = from_f32<IO>(0.f);
+                    if (!LOCAL) r.B[i] = from_f32<IO>(0.f);
+                }
             __syncthreads();
         }
 #pragma unroll
@@ -185,7 +196,6 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
         auto back = [&](int k0, auto marked) {
             constexpr bool MARKED = decltype(marked)::value;
             const float2 *step = s.step + k0 * CB + first;
-            const float *dys = s.dy + k0 * CB + first;
 #pragma unroll
             for (int i = 3; i >= 0; --i) {
                 if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
@@ -193,11 +203,11 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                 ssm_pairs(s.C + (k0 + i) * N + nl * 4, c);
 #pragma unroll
                 for (int q = 0; q < KC; ++q) {
-                    const float d = step[i * CB + q * LC].x, dy = dys[i * CB + q * LC];
-                    sum[q] += d;
+                    const float2 d = step[i * CB + q * LC];
+                    sum[q] += d.x;
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        carry[q][p] = __fmul2_rn(ssm_decay(A2[q][p], d), __ffma2_rn(c[p], both(dy), carry[q][p]));
+                        carry[q][p] = __fmul2_rn(ssm_decay(A2[q][p], d.x), __ffma2_rn(c[p], both(d.y), carry[q][p]));
                 }
             }
         };
@@ -217,6 +227,21 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
                         h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x), h[q][p], __fmul2_rn(both(d.y), b[p]));
                 }
             }
+        };
+        // dB and dC of two tokens over the warp's channels: a lane sums N / 8 neighbouring values over the channels' LC rows.  (The rows
+        // are walked from another one in each quarter of the values, so that lanes side by side read different banks.)
+        auto sum_products = [&](int k0) {
+            constexpr int V = N / 8;
+            const int part = lane / 8, v = lane % 8 * V;  // part: token, dB or dC
+            const float *p = reinterpret_cast<const float *>(s.product[warp][part / 2][part % 2]) + v;
+            Pack<float, V> sum = pack_load<float, V>(p + (part & (LC - 1)) * N);
+#pragma unroll
+            for (int r = 1; r < LC; ++r) {
+                const Pack<float, V> f = pack_load<float, V>(p + ((r + part) & (LC - 1)) * N);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum.e[e] += f.e[e];
+            }
+            pack_store(&s.bc[warp][k0 + part / 2][part % 2 * N + v], sum);
         };
         auto both_ways = [&](int k0, auto &h, auto marked) {
             constexpr bool MARKED = decltype(marked)::value;
@@ -271,10 +296,20 @@ __global__ void __launch_bounds__(kSsmThreads, 3) ssm_backward_kernel(const SsmA
 #pragma unroll
                     for (int q = 0; q < KC; ++q) carry[q][0] = carry[q][1] = both(0.f);
                 }
-                float v[8] = {bc[0].x, bc[0].y, bc[1].x, bc[1].y, bc[2].x, bc[2].y, bc[3].x, bc[3].y};
-                const int v0 = lanes_reduce<8, LC, LN>(v, lane);
+                if constexpr (F::kInMemory) {
+                    s.product[warp][i % 2][0][lane] = make_float4(bc[0].x, bc[0].y, bc[1].x, bc[1].y);
+                    s.product[warp][i % 2][1][lane] = make_float4(bc[2].x, bc[2].y, bc[3].x, bc[3].y);
+                    if (i % 2 == 0) {
+                        __syncwarp();
+                        sum_products(k0 + i);
+                        __syncwarp();
+                    }
+                } else {
+                    float v[8] = {bc[0].x, bc[0].y, bc[1].x, bc[1].y, bc[2].x, bc[2].y, bc[3].x, bc[3].y};
+                    const int v0 = lanes_reduce<8, LC, LN>(v, lane);
 #pragma unroll
-                for (int j = 0; j < (LC >= 8 ? 1 : 8 / LC); ++j) s.bc[warp][k0 + i][((v0 + j) / 4) * N + nl * 4 + (v0 + j) % 4] = v[j];
+                    for (int j = 0; j < 8 / LC; ++j) s.bc[warp][k0 + i][((v0 + j) / 4) * N + nl * 4 + (v0 + j) % 4] = v[j];
+                }
                 if (i % kTogether == 0) {
                     const int o0 = lanes_reduce<3 * KC * kTogether, LN>(out, lane) / 3;
                     const int to = (k0 + i + o0 / KC) * PB + first + o0 % KC * LC;
