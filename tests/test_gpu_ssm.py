@@ -398,3 +398,69 @@ def test_no_rows_and_a_rebuilt_plan():
     dl.build_plan(torch.tensor([3], dtype=torch.int32, device=DEV), plan)
     with pytest.raises(RuntimeError, match="rebuilt"):
         out.float().sum().backward()
+
+
+def _lowest(io):
+    return torch.finfo(io).min
+
+
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("value", ["-inf", "lowest", "-2.4e38"])
+@pytest.mark.parametrize("N,lens", [(16, (9, 40)), (8, (300,)), (64, (33, 140))])
+def test_tokens_masked_by_their_step_size(io, value, N, lens):
+    # softplus is 0 there: the token leaves the state as it is, and no gradient passes through its step size
+    D, T = 72, sum(lens)
+    c = _case(T, D, N, 1, io, wide=True)
+    masked = torch.zeros(T, dtype=torch.bool, device=DEV)
+    masked[::3], masked[-1], masked[140:142] = True, True, True
+    whole = c["dt"].clone()
+    c["dt"][masked] = _lowest(io) if value == "lowest" else float(value)
+    live = {**c, "dt": torch.where(masked[:, None], torch.full_like(whole, -1e30), whole)}   # a softplus of 0 for the 64-bit form
+    desc, plan = dl.SsmDesc(D, N, 1, DT[io], num_slots=len(lens)), _plan(lens)
+    g = torch.Generator().manual_seed(7)
+    S0, dS = (torch.randn(len(lens), D, N, generator=g).to(DEV) for _ in range(2))
+    dout = torch.randn(T, D, generator=g).to(io).to(DEV)
+    out, S = dl.ssm_forward(desc, plan, *_args(c), S_init=S0)
+    d = dl.ssm_backward(desc, plan, *_args(c), dout, S_init=S0, dS_final=dS)
+    want, mag = (ref.ssm(live, lens, S0, dout, dS, mag=m) for m in (False, True))
+    rel = _rel(live, lens)
+    ref.close(out, want[0], mag[0], rel, "out")
+    ref.close(S, want[1], mag[1], rel, "S")
+    many = rel + T * 2.0 ** -24
+    for k, e in (("x", rel), ("dt", rel), ("A", many), ("B", rel), ("C", rel), ("D", many), ("z", rel), ("dt_bias", many), ("S_init", rel)):
+        ref.close(getattr(d, k), want[2][k], mag[2][k] + want[2][k].abs(), 2 * e, "d" + k)
+    assert not d.dt[masked].any()
+    state = dl.SsmState(desc, S0.clone())
+    assert torch.equal(dl.ssm_prefill(desc, state, plan, *_args(c)), out) and torch.equal(state.S, S)
+    # nothing but masked tokens, of a prompt and one by one: the bits of the state stay
+    c["dt"][:] = c["dt"][0].clone()
+    state = dl.SsmState(desc, S0.clone())
+    dl.ssm_prefill(desc, state, plan, *_args(c))
+    assert torch.equal(state.S, S0)
+    token = {k: v[: len(lens)] if k in ("x", "dt", "B", "C", "z") else v for k, v in c.items()}
+    out = dl.ssm_step(desc, state, *_args(token))
+    assert torch.equal(state.S, S0) and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("io", [torch.float32, torch.bfloat16])
+def test_step_sizes_as_large_as_they_get(io):
+    # softplus is its argument there: the old state is gone, the new one delta x B; infinite where delta is
+    D, N = 16, 16
+    c = _case(3, D, N, 1, io, bias=False, gate=False)
+    c["A"] = torch.full((D, N), -1.0, device=DEV)
+    c["x"], c["B"] = torch.full_like(c["x"], 0.5), torch.full_like(c["B"], 0.25)
+    c["dt"][2] = float("nan")
+    for value in (2.4e38, 3e38, float("inf")):
+        c["dt"][:2] = value
+        delta = float(c["dt"][0, 0])
+        one = {k: v[:2] if k in ("x", "dt", "B", "C") else v for k, v in c.items()}
+        S0 = torch.randn(1, D, N, device=DEV)
+        S = dl.ssm_forward(dl.SsmDesc(D, N, 1, DT[io]), _plan((2,)), *_args(one), S_init=S0)[1]
+        if value < float("inf"):
+            assert torch.equal(S, torch.full_like(S, delta * 0.125))
+            state = dl.SsmState(dl.SsmDesc(D, N, 1, DT[io], num_slots=2), S0.repeat(2, 1, 1))
+            dl.ssm_step(state.desc, state, *_args(one))
+            assert torch.equal(state.S, torch.full_like(state.S, delta * 0.125))
+        state = dl.SsmState(dl.SsmDesc(D, N, 1, DT[io], num_slots=3), S0.repeat(3, 1, 1))
+        dl.ssm_step(state.desc, state, *_args(c))
+        assert bool((state.S[:2] == delta * 0.125).all()) and torch.isnan(state.S[2]).all()   # (a step size that is no number stays none)
