@@ -464,3 +464,27 @@ def test_step_sizes_as_large_as_they_get(io):
         state = dl.SsmState(dl.SsmDesc(D, N, 1, DT[io], num_slots=3), S0.repeat(3, 1, 1))
         dl.ssm_step(state.desc, state, *_args(c))
         assert bool((state.S[:2] == delta * 0.125).all()) and torch.isnan(state.S[2]).all()   # (a step size that is no number stays none)
+
+
+def test_step_sizes_keep_their_relative_accuracy():
+    # The step size alone as a state, its derivative alone as a gradient, over all that is no denormal number.  A power of two is 2^-22 off,
+    # its correction's sum rounds once (2^-24), the polynomial's last sums and the product with e three times more, and its own error is 2^-27:
+    # 2^-21 together.  The derivative: the same e, 1 + e, a reciprocal of 2^-23 and a product.
+    B, D, N = 2048, 256, 8
+    v = torch.linspace(-85, 80, B * D, dtype=torch.float64).to(torch.float32).view(B, D).to(DEV)
+    one = torch.zeros(B, 1, N, device=DEV)
+    one[..., 0] = 1
+    A = torch.full((D, N), -1.0, device=DEV)
+    desc = dl.SsmDesc(D, N, 1, dl.F32, num_slots=B)
+    args = (torch.ones(B, D, device=DEV), v, A, one, torch.zeros_like(one))
+    state, V = dl.SsmState(desc, device=DEV), v.double()
+    dl.ssm_step(desc, state, *args)
+    want = V.clamp(min=0) + torch.log1p(torch.exp(-V.abs()))
+    assert float((state.S[..., 0].double() / want - 1).abs().max()) < 2.0 ** -21
+    plan = _plan((1,) * B)
+    dS = torch.zeros(B, D, N, device=DEV)
+    dS[..., 0] = 1
+    S = dl.ssm_forward(desc, plan, *args)[1]
+    assert torch.equal(S, state.S)
+    d = dl.ssm_backward(desc, plan, *args, None, None, None, torch.zeros(B, D, device=DEV), dS_final=dS)
+    assert float((d.dt.double() * (1 + torch.exp(-V)) - 1).abs().max()) < 2.0 ** -21
