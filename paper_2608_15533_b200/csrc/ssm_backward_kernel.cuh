@@ -40,6 +40,7 @@ template <typename IO, int N, bool LOCAL> struct SsmBackward {
         float B[full(kTile * N)];
         float bc[kSsmWarps][full(kTile)][2 * N];
         float4 product[kInMemory ? kSsmWarps : 1][2][2][32]; // of two tokens: a lane's four states of dB and of dC
+        float lift[LOCAL ? 1 : kPer][kSsmThreads];           // a thread's own (in registers they made the sums spill: 730 us where 683 are taken)
         int state[kTile], row[kTile];
         unsigned begins, ends, there;
     };
@@ -95,12 +96,21 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
 
     float2 A2[KC][2], carry[KC][2], dA[KC][2], kept[KC][2];
     float sum[KC];
+    struct Lift { float of[KC]; };
+    Lift lift;  // of the decays; at first the bias that it goes by
+#pragma unroll
+    for (int q = 0; q < KC; ++q) lift.of[q] = a.bias && mine(q) ? a.bias[c0 + first + q * LC] : 0.f;
     load(a.A, 0, A2);
 #pragma unroll
     for (int q = 0; q < KC; ++q) {
         sum[q] = 0.f;
 #pragma unroll
         for (int p = 0; p < 2; ++p) A2[q][p] = __fmul2_rn(A2[q][p], both(1.4426950408889634f)), carry[q][p] = dA[q][p] = both(0.f);
+    }
+#pragma unroll
+    for (int q = 0; q < KC; ++q) {
+        lift.of[q] = ssm_lift(a, A2[q], lift.of[q]);
+        if (!LOCAL) s.lift[q][tid] = lift.of[q];
     }
     if (!LOCAL && hi > lo) {
         const SsmToken last = ssm_token(a, hi - 1, false);
@@ -192,10 +202,18 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
             store2(s.C + i, load2(r.C + i));
         }
         __syncthreads();
+        auto lifts = [&]() {
+            Lift v = lift;
+            if constexpr (!LOCAL)
+#pragma unroll
+                for (int q = 0; q < KC; ++q) v.of[q] = s.lift[q][tid];
+            return v;
+        };
         // four tokens; MARKED: where rows may begin or end
         auto back = [&](int k0, auto marked) {
             constexpr bool MARKED = decltype(marked)::value;
             const float2 *step = s.step + k0 * CB + first;
+            const Lift up = lifts();
 #pragma unroll
             for (int i = 3; i >= 0; --i) {
                 if (MARKED && (ends >> (k0 + i) & 1)) load(a.dS_final, s.state[k0 + i], carry);
@@ -207,13 +225,14 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
                     sum[q] += d.x;
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        carry[q][p] = __fmul2_rn(ssm_decay(A2[q][p], d.x), __ffma2_rn(c[p], both(d.y), carry[q][p]));
+                        carry[q][p] = __fmul2_rn(ssm_decay(A2[q][p], d.x, up.of[q]), __ffma2_rn(c[p], both(d.y), carry[q][p]));
                 }
             }
         };
         auto ahead = [&](int k0, auto &h, auto marked) {
             constexpr bool MARKED = decltype(marked)::value;
             const float2 *step = s.step + k0 * CB + first;
+            const Lift up = lifts();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (MARKED && (begins >> (k0 + i) & 1)) load(a.S_in, s.state[k0 + i], h);
@@ -224,7 +243,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
                     const float2 d = step[i * CB + q * LC];
 #pragma unroll
                     for (int p = 0; p < 2; ++p)
-                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x), h[q][p], __fmul2_rn(both(d.y), b[p]));
+                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x, up.of[q]), h[q][p], __fmul2_rn(both(d.y), b[p]));
                 }
             }
         };
@@ -247,6 +266,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
             constexpr bool MARKED = decltype(marked)::value;
             const float2 *step = s.step + k0 * CB + first;
             const float *dys = s.dy + k0 * CB + first;
+            const Lift up = lifts();
             float2 decay[4][KC][2], moved[4][KC][2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -258,7 +278,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmBackward<IO, N, LOCAL>::kCtas
                     const float2 d = step[i * CB + q * LC];
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        decay[i][q][p] = ssm_decay(A2[q][p], d.x);
+                        decay[i][q][p] = ssm_decay(A2[q][p], d.x, up.of[q]);
                         moved[i][q][p] = __fmul2_rn(decay[i][q][p], h[q][p]);
                         if (i < 3) h[q][p] = __ffma2_rn(both(d.y), b[p], moved[i][q][p]);
                     }

@@ -48,11 +48,8 @@ template <int N> struct SsmLanes {
 
 __device__ __forceinline__ float2 exp2_fast(float2 x) { return make_float2(exp2_fast(x.x), exp2_fast(x.y)); }
 
-// Decays of a token, 2^(A delta).  Measured against 64 bits, the hardware's 2^x is low by 2e-8 on average for x in [-1, -0.003], by 6e-9
-// nearer to zero: little in one decay, but the same in all of them, so that a state that remembers a hundred tokens and the
-// gradients that go back over them were off by a hundred times as much (dA 2.1e-6 where 1e-6 comes from the roundings).  The product's
-// addend is free: 2.2e-8 in the exponent, 1.5e-8 of the result, between the two.
-__device__ __forceinline__ float2 ssm_decay(float2 A, float delta) { return exp2_fast(__ffma2_rn(A, both(delta), both(2.2e-8f))); }
+// Decays of a token, 2^(A delta), lifted by what the hardware's 2^x is low on average (ssm_lift).
+__device__ __forceinline__ float2 ssm_decay(float2 A, float delta, float lift) { return exp2_fast(__ffma2_rn(A, both(delta), both(lift))); }
 
 // softplus(v) = max(v, 0) + log(1 + e), e = exp(-|v|) in [0, 1], of two values.  The exponent of two is rounded, by up to |v| / 2^24,
 // and so is its constant: what both lost, m - x log 2 (Cody and Waite's reduction), goes into the result by the first-order term
@@ -82,6 +79,21 @@ __device__ __forceinline__ float2 ssm_softplus(float2 v, float2 &e) {
 __device__ __forceinline__ float ssm_sigmoid(float v, float e) {
     const float r = rcp_fast(1.f + e);
     return v >= 0.f ? r : e * r;
+}
+
+// What lifts the decays' exponents x = A delta (in powers of two).  Measured against 64 bits, the hardware's 2^x is low on average, by
+// 5e-9 to 7e-9 for x in [-3e-3, -1e-4], by 2.4e-8 from -2^-8 to -1 and by 5e-8 below.  That is little in one decay, but the same in all of
+// them: a state that remembers 1.4 / |x| tokens, and the gradients that go back over them, are off by as many times as much.  An addend
+// of the product, which is free, takes it out, of one size on either side of -2^-8.  A lane's four states of a channel share one, by the
+// slowest of them, in which it counts most: in the scans by the step size that the channel's bias stands for, one choice for all
+// tokens, so that a row's bits do not depend on its neighbours; without a bias or a softplus by a value in between.
+// (dA, dbias, dS_init of 4 x 2048 tokens x 4096 channels, distance from 64 bits: 8.8e-7, 5.8e-7, 9.4e-7; with 2.2e-8 for all 1.6e-6, 7.1e-7,
+// 1.4e-6, and slow channels (|x| of 1e-3) 1.4e-5 off where they now are 2e-6; with 0.9e-8 for all 1.6e-6, 7.8e-7, 1.2e-6.)
+__device__ __forceinline__ float ssm_lift(float x) { return x > -0.00390625f ? 0.9e-8f : 2.9e-8f; }
+__device__ __forceinline__ float ssm_lift(const SsmArgs &a, const float2 (&A2)[2], float bias) {
+    float2 unused;
+    const float x = fmaxf(fmaxf(A2[0].x, A2[0].y), fmaxf(A2[1].x, A2[1].y)) * ssm_softplus(both(bias), unused).x;
+    return a.softplus && a.bias ? ssm_lift(x) : 1.4e-8f;
 }
 
 // Sums over the LN lanes of a group (STRIDE apart) of V values at once: every step halves the values that a lane answers for, as

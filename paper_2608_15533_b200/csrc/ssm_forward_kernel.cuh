@@ -104,6 +104,9 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
         for (int q = 0; q < KC; ++q)
             if (mine(q)) ssm_store(p + at(state, q), h[q]);
     };
+    float lift[KC];  // of the decays; at first the bias that it goes by
+#pragma unroll
+    for (int q = 0; q < KC; ++q) lift[q] = a.bias && mine(q) ? a.bias[c0 + first + q * LC] : 0.f;
     load_state(a.A, 0, A2);
 #pragma unroll
     for (int q = 0; q < KC; ++q) {
@@ -111,6 +114,8 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
 #pragma unroll
         for (int p = 0; p < 2; ++p) A2[q][p] = __fmul2_rn(A2[q][p], both(1.4426950408889634f)), h[q][p] = both(0.f);
     }
+#pragma unroll
+    for (int q = 0; q < KC; ++q) lift[q] = ssm_lift(a, A2[q], lift[q]);
     if (!LOCAL && span > 0) {
         const SsmToken head = ssm_token(a, lo, false);
         if (head.row >= 0 && head.begin < lo) load_state(a.local, lo / a.part - 1, h);  // a row from an earlier stretch
@@ -186,7 +191,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
                     float2 out = both(0.f);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x), h[q][p], __fmul2_rn(b[p], both(d.y)));
+                        h[q][p] = __ffma2_rn(ssm_decay(A2[q][p], d.x, lift[q]), h[q][p], __fmul2_rn(b[p], both(d.y)));
                         if (!LOCAL) out = p ? __ffma2_rn(c[p], h[q][p], out) : __fmul2_rn(c[p], h[q][p]);
                     }
                     if (LOCAL) sum[q] += d.x;
@@ -247,7 +252,7 @@ __global__ void __launch_bounds__(kSsmThreads, (SsmForward<IO, N, WIDE>::kCtas))
 
 // One token per row.  Bound by HBM, the states' read and write.  A lane holds eight states of a channel (32 bytes, one access),
 // so that step size and gate are worked out by d_state / 8 lanes, and keeps its channel's A for all of its rows, two of which are in
-// flight (four, with fewer CTAs on an SM: 21 us where two take 16).
+// flight (four, with fewer CTAs on an SM: 21 us where two take 16; with the 92 registers that a free choice takes, 20).
 __device__ __forceinline__ void ssm_load8(const float *p, float2 (&v)[4]) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y), "=f"(v[2].x), "=f"(v[2].y), "=f"(v[3].x), "=f"(v[3].y) : "l"(p) : "memory");
@@ -257,8 +262,15 @@ __device__ __forceinline__ void ssm_store8(float *p, const float2 (&v)[4]) {
                  ::"l"(p), "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y) : "memory");
 }
 
+__device__ __forceinline__ float ssm_slowest(const float2 (&A2)[4]) {
+    float m = fmaxf(A2[0].x, A2[0].y);
+#pragma unroll
+    for (int p = 1; p < 4; ++p) m = fmaxf(m, fmaxf(A2[p].x, A2[p].y));
+    return m;
+}
+
 template <typename IO, int N>
-__global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs a, int col_blocks, int run) {
+__global__ void __launch_bounds__(kSsmThreads, (sizeof(IO) == 4 ? 5 : 7)) ssm_step_kernel(const SsmArgs a, int col_blocks, int run) {
     constexpr int LN = N / 8, LC = 32 / LN, U = 2;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nl = lane & (LN - 1), cl = lane / LN;
     const int c = ((int)(blockIdx.x % col_blocks) * kSsmWarps + warp) * LC + cl;
@@ -311,9 +323,10 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs a, 
             const float v = to_f32(r.d) + bias, xf = to_f32(r.x);
             float2 unused, y = both(0.f);
             const float delta = a.softplus ? ssm_softplus(both(v), unused).x : v, in = delta * xf;
+            const float lift = ssm_lift(ssm_slowest(A2) * delta);
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                r.h[p] = __ffma2_rn(ssm_decay(A2[p], delta), r.h[p], __fmul2_rn(load2(r.b.e + 2 * p), both(in)));
+                r.h[p] = __ffma2_rn(ssm_decay(A2[p], delta, lift), r.h[p], __fmul2_rn(load2(r.b.e + 2 * p), both(in)));
                 y = __ffma2_rn(load2(r.c.e + 2 * p), r.h[p], y);
             }
             out[u] = y.x + y.y;

@@ -2,6 +2,7 @@
 // everything in front of it, part by part,
 //     h_p <- h_p + exp(A sum_p) h_(p-1)      where the row that is open at the end of part p began in front of the part,
 // and from the last part to the first for the adjoints, where the row that part p begins in goes on behind it.
+// (One decay a part: what the hardware's 2^x is low on average, ssm_lift, does not add up here.)
 // A lane holds four states of a channel and runs over the parts, sixteen of whose values are loaded at a time: the steps between
 // depend on one another, the loads do not (one at a time, in the second pass, they took 0.5 us a part).
 #pragma once

@@ -488,3 +488,33 @@ def test_step_sizes_keep_their_relative_accuracy():
     assert torch.equal(S, state.S)
     d = dl.ssm_backward(desc, plan, *args, None, None, None, torch.zeros(B, D, device=DEV), dS_final=dS)
     assert float((d.dt.double() * (1 + torch.exp(-V)) - 1).abs().max()) < 2.0 ** -21
+
+
+@pytest.mark.parametrize("known", [True, False])
+def test_slow_channels_forget_at_their_rate(known):
+    # A state without input is the product of its decays.  Their roundings to fp32 cancel over thousands of channels; what does not is a
+    # mean error, which a state that remembers 1000 tokens holds 1000 times.  Under a sixteenth of half a step of fp32 a token (2^-28)
+    # is asked for, where the bias says what the step sizes are like or every token is looked at, and under an eighth otherwise: the
+    # channels' mean is itself known to 2e-10 (1e-7 a token of a channel, 128 tokens, 4096 channels and states).
+    D, N, T = 256, 16, 128
+    g = torch.Generator().manual_seed(11)
+    A = -(0.5 + 0.5 * torch.rand(D, N, generator=g)).to(DEV)
+    bias = torch.log(torch.expm1(0.0005 + 0.0015 * torch.rand(D, generator=g))).to(DEV) if known else None
+    dt = (0.5 * torch.randn(T, D, generator=g) if known else 0.0005 + 0.0015 * torch.rand(T, D, generator=g)).to(DEV)
+    delta = torch.log1p(torch.exp(dt.double() + bias.double())) if known else dt.double()
+    zero, bc = torch.zeros(T, D, device=DEV), torch.zeros(T, 1, N, device=DEV)
+    desc, plan = dl.SsmDesc(D, N, 1, dl.F32, softplus=known, num_slots=1), _plan((T,))
+    ones = torch.ones(1, D, N, device=DEV)
+    want = torch.exp(delta.sum(0)[:, None] * A.double())
+
+    def mean_error(S):
+        return abs(float((S[0].double() / want - 1).mean())) / T
+
+    S = dl.ssm_forward(desc, plan, zero, dt, A, bc, bc, dt_bias=bias, S_init=ones)[1]
+    assert mean_error(S) < (2.0 ** -28 if known else 2.0 ** -27)
+    d = dl.ssm_backward(desc, plan, zero, dt, A, bc, bc, None, None, bias, zero, S_init=ones, dS_final=ones)
+    assert mean_error(d.S_init) < (2.0 ** -28 if known else 2.0 ** -27)
+    state = dl.SsmState(desc, ones.clone())
+    for t in range(T):
+        dl.ssm_step(desc, state, zero[t : t + 1], dt[t : t + 1], A, bc[t : t + 1], bc[t : t + 1], dt_bias=bias)
+    assert mean_error(state.S) < 2.0 ** -28
