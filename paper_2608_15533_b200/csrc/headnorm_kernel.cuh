@@ -30,6 +30,11 @@ struct NormArgs {
 
 constexpr int kNormThreads = 128;
 constexpr int kNormHeads = 2, kNormHeadsBack = 1;  // heads of a lane's item
+// CTAs of a wave on an SM, forward and of the gradients, by their registers, or with fp32 by the forward pass's ring (a grid for five, of
+// which four fit, left a fifth for a second wave: 16k x 40 heads of 128 186 us where 168 are taken).
+template <typename IO> constexpr int kNormCtas = sizeof(IO) == 4 ? 4 : 5;
+template <typename IO> constexpr int kNormBackCtas = sizeof(IO) == 4 ? 3 : 4;
+constexpr size_t kNormShared = 228 * 1024, kNormReserved = 1024;  // bytes of an SM, and of every CTA for the system
 
 // Where a lane's two runs of eight values are in a head, and whether they are.
 struct NormAt {
@@ -176,9 +181,10 @@ __device__ __forceinline__ NormSide<IO> norm_side(const NormArgs &a, bool is_k) 
 
 // A warp walks over its items, two of which are on their way while one is computed.
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads, 5) head_norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, kNormCtas<IO>) head_norm_forward_kernel(const NormArgs a) {
     constexpr int G = 32 / L, per = kNormHeads * G, S = kNormStages;
     __shared__ NormSlot<IO> ring[kNormThreads / 32][S][kNormHeads];
+    static_assert(kNormCtas<IO> * (sizeof(ring) + kNormReserved) <= kNormShared, "a wave of CTAs fits");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
     const NormAt at = norm_at(a, l);
     const unsigned cq = (a.H_q + per - 1) / per, chunks = cq + (a.H_k + per - 1) / per;
@@ -242,9 +248,10 @@ __global__ void __launch_bounds__(kNormThreads, 5) head_norm_forward_kernel(cons
 
 // A warp walks over its items of q, then over those of k, with the weights' gradient in registers and two items on their way.
 template <typename IO, int L>
-__global__ void __launch_bounds__(kNormThreads, (sizeof(IO) == 4 ? 3 : 4)) head_norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, kNormBackCtas<IO>) head_norm_backward_kernel(const NormArgs a) {
     constexpr int G = 32 / L, per = G, S = kNormStages;  // one head a lane
     __shared__ NormSlot<IO> ring[kNormThreads / 32][S][2];  // gradient, value
+    static_assert(kNormBackCtas<IO> * (sizeof(ring) + kNormReserved) <= kNormShared, "a wave of CTAs fits");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane & (L - 1), group = lane / L;
     const bool weighted = a.w_q != nullptr, normed = a.norm != DELTALOG_NORM_NONE;
     const NormAt at = norm_at(a, l);

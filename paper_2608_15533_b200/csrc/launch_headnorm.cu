@@ -56,7 +56,7 @@ long long norm_blocks(const deltalog_norm_desc *d, int32_t tokens) {
 // block's sums, and the workspace's size depends on it).
 long long norm_wave(long long blocks, int per_sm) { return blocks < 148 * per_sm ? blocks : 148 * per_sm; }
 long long norm_kept_blocks(const deltalog_norm_desc *d, int32_t tokens) {
-    return norm_wave(norm_blocks<kNormHeadsBack>(d, tokens), d->io_dtype == DELTALOG_F32 ? 3 : 4);
+    return norm_wave(norm_blocks<kNormHeadsBack>(d, tokens), d->io_dtype == DELTALOG_F32 ? kNormBackCtas<float> : kNormBackCtas<__nv_bfloat16>);
 }
 
 #define NORM_DISPATCH(desc_, CALL)                                                                  \
@@ -80,7 +80,8 @@ int deltalog_head_norm_forward(const deltalog_norm_desc *desc, const void *q, in
     if (tokens == 0) return DELTALOG_OK;
     NormArgs a = norm_args(desc, q, q_stride, k, k_stride, w_q, w_k, cos, sin, positions, tokens);
     a.out_q = out_q, a.out_k = out_k, a.status = status;
-    const long long blocks = norm_blocks<kNormHeads>(desc, tokens), grid = norm_wave(blocks, 5);
+    const long long blocks = norm_blocks<kNormHeads>(desc, tokens);
+    const long long grid = norm_wave(blocks, desc->io_dtype == DELTALOG_F32 ? kNormCtas<float> : kNormCtas<__nv_bfloat16>);
     if (blocks > 0x1fffffffll) return DELTALOG_ERR_UNSUPPORTED_SHAPE;  // items are counted in 31 bits
     cudaStream_t s = static_cast<cudaStream_t>(stream);
 #define CALL(IO, L) head_norm_forward_kernel<IO, L><<<(unsigned)grid, kNormThreads, 0, s>>>(a)
