@@ -289,9 +289,7 @@ def _differentiable(tensors) -> bool:
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
-def _want_workspace(workspace, bytes_: int, device) -> torch.Tensor:
-    if workspace is None:
-        return torch.empty(bytes_, dtype=torch.uint8, device=device)
+def _want_workspace(workspace, device) -> torch.Tensor:
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor on {device}")
     return workspace
@@ -381,8 +379,7 @@ def conv_backward(desc: ConvDesc, plan: Plan, x, weight, bias, dout, init=None, 
     p_dfinal = None if dfinal is None else _want("dfinal", dfinal, window, io, dev)
     p_dout = _want("dout", dout, (rows, C), io, dev) or 16
     with _stream_of(dev, stream) as handle:
-        ws = workspace if workspace is not None else conv_workspace(desc, rows, dev)
-        ws = _want_workspace(ws, 0, dev)
+        ws = _want_workspace(workspace, dev) if workspace is not None else conv_workspace(desc, rows, dev)
         make = _zeros if plan.n == 0 else _empty  # without rows nothing is launched
         new = ConvGrads(make((rows, C), io, dev), make((C, desc.width), torch.float32, dev), None if bias is None else make((C,), torch.float32, dev),
                         _empty(window, io, dev))
@@ -478,7 +475,7 @@ def ssm_prefill(desc: SsmDesc, state: SsmState, plan: Plan, x, dt, A, B, C, D=No
     p_S, p_status = state._fits(desc, dev)
     with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, desc.channels), io, dev, plan)
-        ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
+        ws = _want_workspace(workspace, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
         rc = load_library().deltalog_ssm_prefill(ctypes.byref(desc.c_struct(zero)), p_S, ctypes.byref(plan.c_struct()), ctypes.byref(inputs), p_fresh,
                                                  out.data_ptr() or 16, p_status, ws.data_ptr(), _bytes(ws), handle)
     _check(rc, "deltalog_ssm_prefill")
@@ -499,7 +496,7 @@ def ssm_forward(desc: SsmDesc, plan: Plan, x, dt, A, B, C, D=None, z=None, dt_bi
         raise ValueError("workspace: save=True needs the caller's workspace, which ssm_backward reads")
     with _stream_of(dev, stream) as handle:
         out, zero = _new_out(out, rows, (rows, desc.channels), io, dev, plan)
-        ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
+        ws = _want_workspace(workspace, dev) if workspace is not None else ssm_workspace(desc, plan.n, plan.max_tokens, device=dev)
         S_final = _empty(s_shape, torch.float32, dev)
         rc = load_library().deltalog_ssm_forward(ctypes.byref(desc.c_struct(zero)), ctypes.byref(plan.c_struct()), p_init, ctypes.byref(inputs),
                                                  out.data_ptr() or 16, S_final.data_ptr(), int(bool(save)), ws.data_ptr(), _bytes(ws), handle)
@@ -536,7 +533,7 @@ def ssm_backward(desc: SsmDesc, plan: Plan, x, dt, A, B, C, D, z, dt_bias, dout,
     if saved and workspace is None:
         raise ValueError("workspace: saved=True needs the workspace of ssm_forward")
     with _stream_of(dev, stream) as handle:
-        ws = _want_workspace(workspace, 0, dev) if workspace is not None else ssm_workspace(desc, plan.n, rows, train=True, device=dev)
+        ws = _want_workspace(workspace, dev) if workspace is not None else ssm_workspace(desc, plan.n, rows, train=True, device=dev)
         make = _zeros if plan.n == 0 else _empty  # without rows nothing is launched
 
         def grad(t, dtype):
@@ -660,7 +657,7 @@ def head_norm_backward(desc: NormDesc, q, k, w_q, w_k, cos, sin, positions, dout
         if workspace is None:
             bytes_ = lib.deltalog_head_norm_workspace_bytes(ctypes.byref(c), rows) if w_q is not None else 0
             workspace = torch.empty(max(bytes_, 16), dtype=torch.uint8, device=dev)
-        ws = _want_workspace(workspace, 0, dev)
+        ws = _want_workspace(workspace, dev)
         new = HeadNormGrads(_empty((rows, desc.H_q, d), io, dev), _empty((rows, desc.H_k, d), io, dev) if desc.H_k else None,
                             None if w_q is None else torch.empty_like(w_q), None if w_k is None else torch.empty_like(w_k))
         rc = lib.deltalog_head_norm_backward(ctypes.byref(c), *ptr, p_dq, p_dk, new.q.data_ptr() or 16, None if new.k is None else new.k.data_ptr() or 16,
