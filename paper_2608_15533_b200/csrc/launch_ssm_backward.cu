@@ -8,6 +8,7 @@ namespace {
 
 template <typename IO, int N>
 int backward(const SsmArgs &a, cudaStream_t s) {
+    static_assert(SsmBackward<IO, N, false>::kCtas == ssm_on_sm(sizeof(IO) == 4, N, kSsmBack), "a wave is what the cuts take it for");
     const unsigned cols = (unsigned)(a.G * a.blocks);
     if (a.spans > 1) {
         auto local = ssm_backward_kernel<IO, N, true>;

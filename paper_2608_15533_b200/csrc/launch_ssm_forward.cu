@@ -8,6 +8,7 @@ namespace {
 
 template <typename IO, int N, bool WIDE>
 int forward(const SsmArgs &a, cudaStream_t s) {
+    static_assert(SsmForward<IO, N, WIDE>::kCtas == ssm_on_sm(sizeof(IO) == 4, N, WIDE ? kSsmWide : kSsmNarrow), "a wave is what the cuts take it for");
     const size_t smem = sizeof(typename SsmForward<IO, N, WIDE>::Shared);
     const unsigned cols = (unsigned)(a.G * a.blocks);
     if (a.spans > 1) {

@@ -22,7 +22,6 @@ namespace deltalog {
 template <typename IO, int N, bool LOCAL> struct SsmBackward {
     static constexpr int kPer = 2;
     static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = LOCAL ? 32 : 16;
-    static constexpr int kCtas = LOCAL && N <= 32 ? 4 : 3;  // on an SM, by their registers
     // dB and dC over a warp's channels: eight or more of them in shared memory, two tokens at a time (each token by exchanges between
     // the lanes: 714 us where 681 are taken); of four or two the exchanges are short (32 states: 400 us, in shared memory 405).
     static constexpr bool kInMemory = !LOCAL && SsmLanes<N>::kChannels >= 8;
@@ -44,6 +43,7 @@ template <typename IO, int N, bool LOCAL> struct SsmBackward {
         int state[kTile], row[kTile];
         unsigned begins, ends, there;
     };
+    static constexpr int kCtas = ssm_ctas(LOCAL && N <= 32 ? 4 : 3, sizeof(Shared));  // on an SM
 };
 
 // LOCAL: the first pass over a part of a stretch (`span` is the part), where its first row began in front of the stretch: the adjoint

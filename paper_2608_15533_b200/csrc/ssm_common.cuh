@@ -41,6 +41,11 @@ struct SsmArgs {
     float *part_bc, *part_A, *part_cols;        // [G * blocks, rows, 2 N], [spans, D_, N], [spans, 2, D_]
 };
 
+// CTAs of a kernel that an SM holds, by its registers and its shared memory: 228 KB, of which the system takes one for every CTA.
+constexpr int ssm_ctas(int by_registers, size_t shared) {
+    return by_registers < (int)(228 * 1024 / (shared + 1024)) ? by_registers : (int)(228 * 1024 / (shared + 1024));
+}
+
 // Lanes of a channel, channels side by side in a warp.
 template <int N> struct SsmLanes {
     static constexpr int kStates = N / 4, kChannels = 32 / kStates;

@@ -20,7 +20,6 @@ template <typename IO, int N, bool WIDE> struct SsmForward {
     static constexpr int kPer = (N <= 32 ? 2 : 4) / (WIDE ? 1 : 2);                         // channels per lane
     static constexpr int kCols = kSsmWarps * SsmLanes<N>::kChannels * kPer, kTile = 32;    // channels of a CTA, tokens of a tile
     static constexpr int kPitch = kCols + 8;  // lanes that answer for neighbouring tokens store to different banks
-    static constexpr int kCtas = N <= 32 ? 4 : 3;                                           // on an SM, by their registers
     struct Raw {
         IO x[kTile * kCols], dt[kTile * kCols], z[kTile * kCols], B[kTile * N], C[kTile * N];
     };
@@ -31,6 +30,7 @@ template <typename IO, int N, bool WIDE> struct SsmForward {
         int state[kTile], row[kTile];
         unsigned begins, ends, there, open;  // one bit per token of the tile; open: its row goes on behind the stretch
     };
+    static constexpr int kCtas = ssm_ctas(N <= 32 ? 4 : 3, sizeof(Shared));  // on an SM
 };
 
 // LOCAL: the first pass over a part of a stretch (`span` is the part), where its last row goes on behind the stretch.

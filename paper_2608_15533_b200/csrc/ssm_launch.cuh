@@ -19,11 +19,24 @@ inline int ssm_blocks(const deltalog_ssm_desc *d, SsmForm form) {
     return (int)ssm_ceil(d->channels / d->groups, form == kSsmWide || (form == kSsmBack && n != 64) ? wide : wide / 2);
 }
 
+// CTAs of a form that an SM holds (the launches assert that it is what the kernels' shared memory and registers leave).  With four, and
+// three backward, for all, a wave was one and a half of what fits with fp32 or 8 states.  fp32, 8k tokens in 4 rows x 4096 channels,
+// then 4k in 9 rows x 2560, four for all / as here, us: 8 states 595 / 548, 202 / 118; 16 476 / 478, 185 / 198; 32 636 / 679, 288 / 236;
+// 64 1326 / 927, 437 / 472; gradients 1019 / 986, 347 / 327; 1033 / 1071, 380 / 344; 1609 / 1609, 540 / 570; 3721 / 3333, 1222 / 1121.
+constexpr int ssm_on_sm(bool fp32, int states, SsmForm form) {
+    switch (states) {
+    case 8: return form == kSsmNarrow ? (fp32 ? 3 : 4) : fp32 ? 1 : 2;
+    case 16: return form == kSsmNarrow ? 4 : form == kSsmBack ? (fp32 ? 2 : 3) : fp32 ? 2 : 4;
+    case 32: return form == kSsmNarrow ? 4 : form == kSsmBack ? 3 : fp32 ? 3 : 4;
+    default: return form != kSsmNarrow && fp32 ? 2 : 3;
+    }
+}
+
 // Stretches that the tokens are cut into at most: as many as one wave of CTAs has, or two or three waves where those are filled
 // better by more than a twentieth (a cut makes the row that crosses it run twice behind its last border; of few blocks of
 // channels one wave may leave an SM in seven idle).  (148 SMs whatever the device: workspaces depend on it.)
 inline int ssm_most_spans(const deltalog_ssm_desc *d, SsmForm form) {
-    const int blocks = ssm_blocks(d, form) * d->groups, wave = 148 * (form == kSsmBack || d->d_state == 64 ? 3 : 4);
+    const int blocks = ssm_blocks(d, form) * d->groups, wave = 148 * ssm_on_sm(d->io_dtype == DELTALOG_F32, d->d_state, form);
     if (blocks >= wave) return 1;
     int best = wave / blocks;
     double full = (double)best * blocks / wave;
@@ -50,9 +63,10 @@ inline SsmForm ssm_forward_form(const deltalog_ssm_desc *d, int32_t rows, int32_
     const SsmCut c = ssm_cut(d, rows, tokens, kSsmWide);
     return (long long)c.spans * c.blocks * d->groups < 148 ? kSsmNarrow : kSsmWide;
 }
-// What ssm_cut gives at most for this many tokens or fewer.
+// What ssm_cut gives at most for this many tokens or fewer, in whichever form.
 inline int ssm_room(const deltalog_ssm_desc *d, int32_t tokens, bool backward) {
-    const long long most = ssm_most_spans(d, backward ? kSsmBack : kSsmWide), spans = ssm_ceil(tokens, kSsmSpanMin);
+    const long long wide = ssm_most_spans(d, backward ? kSsmBack : kSsmWide), narrow = backward ? 1 : ssm_most_spans(d, kSsmNarrow);
+    const long long most = wide > narrow ? wide : narrow, spans = ssm_ceil(tokens, kSsmSpanMin);
     return (int)(spans < most ? spans : most);
 }
 
