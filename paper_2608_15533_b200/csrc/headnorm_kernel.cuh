@@ -7,7 +7,8 @@
 // half a rotation apart (or neighbours, for interleaved pairs and behind the rotated part), so that a lane turns its own values and
 // loads 16 bytes at a time.  A warp takes one token and several of its heads, and walks over such items with two more on their way
 // in shared memory.  The sums over a head are butterflies over its lanes.
-// 16k tokens x 40 heads of 128, 16-bit: 64 us (5.2 TB/s, 0.80 of a copy), gradients 117 us (4.3 TB/s) and 8 for the weights' sums.
+// 16k tokens x 40 heads of 128, 16-bit: 64 us (5.2 TB/s, 0.80 of a copy), gradients 117 us (4.3 TB/s; 65 % of the issue slots, 32
+// instructions a value, forward 19) and 8 for the weights' sums, whose eight blocks are bound by latency.
 // (Pairs exchanged between lanes: 103 and 355 us; one item a warp with its loads in registers: 80 and 149.)
 #pragma once
 

@@ -9,9 +9,11 @@
 // where four took 714.)  a h_(t-1) is kept rather than h_t, from which it would come out by a difference that cancels where the
 // decay is strong.  Sums over a channel's states run over several values at once (lanes_reduce), over a warp's channels in the same way
 // or in shared memory, over the warps in shared memory, over the CTAs in ssm_sums_kernel; each in a fixed order.
-// Bound by its instructions, 22 per token, channel and state of which 13 are products and sums and 4 the exchange of partial sums:
-// 8k tokens x 4096 x 16 states 681 us with the 12 warps an SM that 168 registers leave; the first pass 153 (175 in the second pass's
-// layout), the sums 17.  One channel a lane instead of two (20 warps) had 915 where two had 714: its sums over channels cost twice as much.
+// Bound by latency between its instructions: 56 % of the issue slots and 35 % of the special function units are busy.  24 instructions per
+// token, channel and state by the counters (13 of them products and sums, 4 the exchange of partial sums), three barriers a tile between
+// phases of different kinds, and the 12 warps an SM that 168 registers leave.  8k tokens x 4096 x 16 states 684 us; the first pass 153 (175
+// in the second pass's layout), the sums 17.  One channel a lane instead of two (20 warps) had 915 where two had 714: its sums over channels
+// cost twice as much.
 #pragma once
 
 #include "ssm_common.cuh"

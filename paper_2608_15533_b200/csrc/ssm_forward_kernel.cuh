@@ -5,9 +5,10 @@
 // channels a thread; B and C are widened once per CTA; per pair of states a lane then does two packed products, two
 // exponentials and two packed fused multiply-adds; the sums over a channel's states run over four tokens at a time, six shuffles for
 // eight sums.  Two channels a lane share the loads of B and C, which at one channel cost more than the exponentials.
-// 14k ragged tokens x 4096 channels x 16 states: 416 us behind a first pass of 107 (the exponentials alone: 204), special function
-// units 64 % busy, issue slots 53 %; 16k x 2048 in one row 239 + 174.  Four CTAs an SM; six with fewer registers or smaller tiles took as
-// long; four channels a lane in tiles of 16 tokens, three CTAs, have 420 behind 233.
+// 14k ragged tokens x 4096 channels x 16 states: 414 us behind a first pass of 107 (the exponentials alone: 204), special function
+// units 64 % busy, issue slots 53 %: the rest is latency between the phases of a tile, three barriers apart; 16k x 2048 in one row 238 +
+// 175.  Four CTAs an SM; six with fewer registers or smaller tiles took as long; four channels a lane in tiles of 16 tokens, three CTAs,
+// have 420 behind 233.
 #pragma once
 
 #include "ssm_common.cuh"
