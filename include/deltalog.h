@@ -504,7 +504,7 @@ int deltalog_head_norm_backward(const deltalog_norm_desc *desc, const void *q, i
  *     S <- exp(delta A) S + delta x B                         (S, A [channels, d_state]; B, C [tokens, groups, d_state])
  *     y = S C + D x,   out = y, or y z sigmoid(z)
  * Channel c belongs to group c / (channels / groups).
- * With softplus, a dt of -infinity or of its type's lowest value has delta = 0: the token leaves the state as it is, bit for bit.
+ * With softplus, a dt of -infinity or of its type's lowest value has delta = 0: the token, of finite x and B, leaves the state as it is, bit for bit.
  *   x, dt, z, out [tokens, channels] io_dtype; B, C [tokens, groups, d_state] io_dtype, the groups of a token dense; A fp32 (negative in
  *   use: a decay); D, dt_bias [channels] fp32 or NULL; z may be NULL; states fp32 [num_slots or n, channels, d_state].
  */

@@ -46,7 +46,8 @@ def _lens(total, seed, longest=300):
 
 # Channels, groups, tokens; channels of a CTA in the wide form, tokens of a stretch: 148 CTAs and more, so that the wide form is taken.
 WIDE = [(8, 1304, 1, 2050, 128, 128, dict()), (16, 776, 1, 1950, 64, 128, dict(wide=True)), (32, 336, 2, 1950, 32, 128, dict(gate=False)),
-        (64, 304, 1, 1950, 32, 128, dict(skip=False)), (16, 4488, 1, 2000, 64, 256, dict(wide=True)), (8, 2640, 2, 1300, 128, 128, dict(softplus=False, bias=False))]
+        (64, 304, 1, 1950, 32, 128, dict(skip=False)), (16, 4488, 1, 2000, 64, 256, dict(wide=True)), (8, 2640, 2, 1300, 128, 128, dict(softplus=False, bias=False)),
+        (8, 16384, 1, 900, 64, 128, dict(gate=False))]  # with fp32 the narrow form in several stretches: the wide one has 128 CTAs
 
 
 @pytest.mark.gpu
